@@ -315,6 +315,92 @@ pw_status pw_moe_forward(pw_ctx* ctx, int layer, const void* hidden_fp16, const 
 pw_status pw_moe_forward_host(pw_ctx* ctx, int layer, const void* hidden_host, const float* logits_host, int T,
                               int top_k, float* out_host, pw_mode mode, pw_stream stream);
 
+/* ---- around the layer ----------------------------------------------------------------- */
+
+/* What a program computes between two layer calls: the residual's addition and the norm in front of the layer, the
+ * router's choice where it is another rule than pw_moe_forward's, and dense products (the router's logits, the
+ * projections around the layer) on 8-bit operands.  (The paper starts at the router's logits; these calls have no
+ * counterpart in it.)  They need a context of the current device, but neither pages nor the page table; nothing is
+ * kept between calls and no workspace is used, so calls on different streams may run at the same time.
+ * Row strides count elements; rows may be further apart than they are long, and what lies between and behind them is
+ * left as it was.  A call for zero rows is valid and enqueues nothing. */
+
+typedef enum { PW_F32 = 0, PW_F16 = 1, PW_BF16 = 2 } pw_type;
+
+/* Scaled 8-bit format: codes in e4m3 (largest value 448), row-major, rows a multiple of 16 bytes apart, and an fp32
+ * scale per block of 128 columns and block_rows rows (1: activations, 128: weights), stored
+ * [ceil(rows / block_rows)][ceil(cols / 128)]; the last block of either direction may be short.  A block's scale is its
+ * largest magnitude / 448 (1 for a block of zeros, at least 2^-126), its codes are e4m3(value * (1 / scale)), rounded
+ * to nearest even and limited to 448: value = code * scale.
+ *
+ * pw_quantize_scaled: x device [rows, cols] of x_type.  The codes' bytes past `cols` in a row are not written.
+ * Errors: INVALID_ARG (a null pointer, block_rows neither 1 nor 128, cols < 1), SHAPE (stride below cols; cols over
+ * 2^30), ALIGN (a pointer, or q_stride, not a multiple of 16), CUDA. */
+pw_status pw_quantize_scaled(pw_ctx* ctx, const void* x, int x_type, int rows, int cols, int64_t x_stride,
+                             int block_rows, void* q, int64_t q_stride, float* scales, pw_stream stream);
+
+/* Residual addition and root-mean-square norm of T rows of H columns, in fp32:
+ *   s = x + residual,  residual_out = s,  y = s * weight / sqrt(mean(s^2) + eps)
+ * each output rounded once from fp32 (the norm works on the unrounded s), and the scaled 8-bit copy (block_rows 1) of
+ * the unrounded y in q / q_scales, as pw_quantize_scaled would make it.
+ * residual may be NULL (s = x); residual_out (type of residual), y and the pair q, q_scales may each be NULL, but one
+ * of y and q is needed.  residual_out may be residual, or x where type and stride are the same; y may be any of the
+ * three where type and stride are the same; other overlaps are not allowed.  H: 1 .. 32768.
+ * For the layer: x = the fp32 output of pw_moe_forward, y = the fp16 hidden states of the next call.
+ * Errors: INVALID_ARG, SHAPE (H over 32768; a stride below H), ALIGN (a pointer, or q_stride, not a multiple of 16),
+ * CUDA. */
+pw_status pw_add_rmsnorm(pw_ctx* ctx, int T, int H, const void* x, int x_type, int64_t x_stride, const void* residual,
+                         int residual_type, int64_t residual_stride, const void* weight, int weight_type, float eps,
+                         void* residual_out, int64_t residual_out_stride, void* y, int y_type, int64_t y_stride, void* q,
+                         int64_t q_stride, float* q_scales, pw_stream stream);
+
+/* Product of two scaled 8-bit matrices: out[t, n] = sum_k a[t, k] * w[n, k], a [T, K] with block_rows 1, w [N, K] with
+ * block_rows 128 (the layout of a linear-block: output features x input features).  Sums in fp32 in a fixed order,
+ * rounded once to out_type.  Any T, N, K from 1 on.  A device-side wait that runs out is reported by
+ * pw_last_device_status.
+ * Errors: INVALID_ARG, SHAPE (a stride below the row's length; N or K over 2^30), ALIGN (a pointer, or a code stride,
+ * not a multiple of 16), CUDA. */
+pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const void* a_codes, int64_t a_stride,
+                           const float* a_scales, const void* w_codes, int64_t w_stride, const float* w_scales,
+                           void* out, int out_type, int64_t out_stride, pw_stream stream);
+
+/* Router: which top_k of n_experts a token takes, and with which gates.
+ *   score    p = softmax of the row, or 1 / (1 + exp(-logit))
+ *   key      p + bias (bias: device [n_experts] fp32 or NULL; it balances the choice and does not enter the gates)
+ *   groups   n_groups equal ranges of experts; only experts of the top_groups best groups can be chosen.  A group's
+ *            score is its best key (group_best 1) or the sum of its best two (group_best 2)
+ *   choice   the top_k largest keys, largest first; equal keys (and groups): lower index first.  Keys are compared in
+ *            64 bits; without a bias and without sums of two their order is that of the logits.
+ *   gate     p, divided by the sum of the chosen p with renormalize (0 where that sum is 0), times scale
+ * A logit of -infinity or NaN masks its expert: it is never chosen, has no part in the softmax or in its group's score
+ * (a group without any other expert comes last).  +infinity counts as the largest finite number.  A row with fewer
+ * than top_k experts to choose from (a row of padding has none) gets id -1 and gate 0 in its last slots.
+ * softmax, no bias, one group, renormalize, scale 1 is the rule of pw_moe_forward.
+ * router_logits: device [T, n_experts] of logits_type; topk_ids int32 [T, top_k], gates fp32 [T, top_k].
+ * Errors: INVALID_ARG (n_experts outside 1 .. 256; top_k outside 1 .. 32 or more than the experts of top_groups groups;
+ * n_groups does not divide n_experts; scale not finite), SHAPE (stride below n_experts), ALIGN, CUDA. */
+typedef enum { PW_SCORE_SOFTMAX = 0, PW_SCORE_SIGMOID = 1 } pw_score;
+typedef struct {
+  int32_t n_experts, top_k;
+  int32_t score;       /* pw_score */
+  int32_t n_groups, top_groups, group_best;
+  int32_t renormalize; /* 0 or 1   */
+  float scale;
+} pw_routing;
+pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* router_logits, int logits_type,
+                          int64_t logits_stride, const float* bias, int T, int32_t* topk_ids, float* gates,
+                          pw_stream stream);
+
+/* pw_moe_forward for a routing that the caller has: topk_ids int32 [T, top_k] and gates fp32 [T, top_k], both device,
+ * e.g. from pw_route_tokens.  A pair with id -1 takes no expert and adds nothing (shared experts still see the token).
+ * An id outside -1 .. n_experts - 1 is treated like -1 and reported by pw_last_device_status as INVALID_ARG.
+ * pw_get_routing then returns the pairs as they were used: perm ends with -1 for every pair without an expert, and
+ * counts, offsets leave them out.  With the ids and gates of pw_moe_forward's own rule the output is the same, bit for
+ * bit.  Errors: as pw_moe_forward. */
+pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16, const int32_t* topk_ids,
+                                const float* gates, int T, int top_k, const pw_page_table* table, float* out, pw_mode mode,
+                                pw_stream stream);
+
 /* The routing decision of the last forward call (Sec. 2.1: top-k experts per token and their gates; Sec. 3.3:
  * the grouping of the routed pairs by expert), copied out of the workspace (device pointers, any may
  * be NULL): topk_ids int32 [T, k], gates fp32 [T, k], counts int32 [E], offsets int32 [E+1],

@@ -139,6 +139,8 @@ extern "C" pw_status pw_create(pw_ctx** out, const pw_config* cfg) {
   bool ok = ctx->host_rows && ctx->host_valid && ctx->records;
   int dev = 0;
   ok = ok && cudaGetDevice(&dev) == cudaSuccess;
+  ctx->device = dev;
+  ctx->encode_tiled = nullptr;
   ok = ok && cudaDeviceGetAttribute(&ctx->num_sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
   // the table (valid = 0), status word, counters and operand padding start out as zeros
   ok = ok && cudaMemset(ctx->base, 0, m.total) == cudaSuccess;
@@ -248,16 +250,18 @@ extern "C" pw_status pw_query_row(pw_ctx* ctx, int layer, int expert, int kind, 
 }
 
 // Argument checks of a forward call: everything that can be refused is refused here, before anything is enqueued.
-static pw_status check_forward_args(pw_ctx* ctx, int layer, const void* hidden, const float* logits, int T, int top_k,
+static pw_status check_forward_args(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k,
                                     const pw_page_table* table, const float* out, pw_mode mode) {
-  if (!ctx || !hidden || !logits || !out) return PW_ERR_INVALID_ARG;
+  if (!ctx || !hidden || !out) return PW_ERR_INVALID_ARG;
+  if (!routing.logits && (!routing.ids || !routing.gates)) return PW_ERR_INVALID_ARG;
   const pw_config& c = ctx->cfg;
   if (table && table->owner != ctx) return PW_ERR_INVALID_ARG;
   if (layer < 0 || layer >= c.n_layers || T < 1 || T > c.max_tokens || top_k < 1 || top_k > c.max_top_k ||
       top_k > c.n_experts)
     return PW_ERR_INVALID_ARG;
   if (mode != PW_MODE_AUTO && mode != PW_MODE_SIMT && mode != PW_MODE_TENSOR) return PW_ERR_INVALID_ARG;
-  if (!aligned16(hidden) || !aligned16(logits) || !aligned16(out)) return PW_ERR_ALIGN;
+  if (!aligned16(hidden) || !aligned16(routing.logits) || !aligned16(routing.ids) || !aligned16(routing.gates) || !aligned16(out))
+    return PW_ERR_ALIGN;
   for (int e = 0; e < ctx->ws.S; ++e)
     for (int u = 0; u < 3; ++u)
       if (!ctx->host_valid[row_index(ctx, layer, e, u)]) return PW_ERR_STATE;
@@ -268,9 +272,9 @@ static pw_status check_forward_args(pw_ctx* ctx, int layer, const void* hidden, 
   return PW_OK;
 }
 
-extern "C" pw_status pw_moe_forward(pw_ctx* ctx, int layer, const void* hidden, const float* logits, int T, int top_k,
-                                    const pw_page_table* table, float* out, pw_mode mode, pw_stream stream) {
-  const pw_status as = check_forward_args(ctx, layer, hidden, logits, T, top_k, table, out, mode);
+static pw_status moe_forward(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k,
+                             const pw_page_table* table, float* out, pw_mode mode, pw_stream stream) {
+  const pw_status as = check_forward_args(ctx, layer, hidden, routing, T, top_k, table, out, mode);
   if (as != PW_OK) return as;
   const pw_config& c = ctx->cfg;
 
@@ -310,7 +314,7 @@ extern "C" pw_status pw_moe_forward(pw_ctx* ctx, int layer, const void* hidden, 
     timing_drain_slot(ctx, ctx->timing_cur);   // waits only when the ring has wrapped onto unfinished work
     ctx->timing_busy[ctx->timing_cur] = true;
   }
-  pw_status st = launch_route(ctx, layer, hidden, logits, T, top_k, nt_tile, ksplit, stream);
+  pw_status st = launch_route(ctx, layer, hidden, routing, T, top_k, nt_tile, ksplit, stream);
   if (st != PW_OK) return st;
   st = mode == PW_MODE_SIMT ? launch_ffn_simt(ctx, layer, T, top_k, stream)
                             : launch_ffn_tensor(ctx, layer, T, top_k, nt_tile, ksplit, stream);
@@ -323,6 +327,16 @@ extern "C" pw_status pw_moe_forward(pw_ctx* ctx, int layer, const void* hidden, 
   return st;
 }
 
+extern "C" pw_status pw_moe_forward(pw_ctx* ctx, int layer, const void* hidden, const float* logits, int T, int top_k,
+                                    const pw_page_table* table, float* out, pw_mode mode, pw_stream stream) {
+  return moe_forward(ctx, layer, hidden, Routing{logits, nullptr, nullptr}, T, top_k, table, out, mode, stream);
+}
+
+extern "C" pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden, const int32_t* topk_ids, const float* gates,
+                                           int T, int top_k, const pw_page_table* table, float* out, pw_mode mode, pw_stream stream) {
+  return moe_forward(ctx, layer, hidden, Routing{nullptr, topk_ids, gates}, T, top_k, table, out, mode, stream);
+}
+
 extern "C" pw_status pw_moe_forward_host(pw_ctx* ctx, int layer, const void* hidden_host, const float* logits_host, int T,
                                          int top_k, float* out_host, pw_mode mode, pw_stream stream) {
   if (!ctx || !hidden_host || !logits_host || !out_host) return PW_ERR_INVALID_ARG;
@@ -331,7 +345,7 @@ extern "C" pw_status pw_moe_forward_host(pw_ctx* ctx, int layer, const void* hid
   char* b = ctx->base;
   const WsMap& w = ctx->ws;
   // refuse what the forward call would refuse before the first copy is enqueued (the staging buffers stay untouched)
-  const pw_status as = check_forward_args(ctx, layer, b + w.io_hidden, reinterpret_cast<const float*>(b + w.io_logits), T,
+  const pw_status as = check_forward_args(ctx, layer, b + w.io_hidden, Routing{reinterpret_cast<const float*>(b + w.io_logits), nullptr, nullptr}, T,
                                           top_k, nullptr, reinterpret_cast<const float*>(b + w.io_out), mode);
   if (as != PW_OK) return as;
   PW_CUDA_OK(cudaMemcpyAsync(b + w.io_hidden, hidden_host, (size_t)T * c.hidden * 2, cudaMemcpyHostToDevice, stream));

@@ -112,6 +112,8 @@ struct pw_ctx {
   uint64_t launches;
   int last_T, last_k;
   int num_sms;
+  int device;                     // the device the context was created on
+  void* encode_tiled;             // driver entry point for tensor maps (looked up by the first scaled product)
   void* tc_state;                 // tensor-core path state (set up lazily)
   uint32_t wait_polls;            // limit of the device-side waits in polls of 20 us (0 = the default, 2 s)
   uint32_t test_hook;             // device-side test hooks (pw_debug_set_wait)
@@ -142,7 +144,13 @@ inline size_t row_index(const pw_ctx* ctx, int layer, int expert, int kind) {
 namespace pw {
 
 // entry points of the other translation units
-pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const float* logits, int T, int k, int nt_tile,
+// the routing a forward call starts from: logits to be routed by the library's rule, or the caller's ids and gates
+struct Routing {
+  const float* logits;
+  const int32_t* ids;
+  const float* gates;
+};
+pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int k, int nt_tile,
                        int ksplit, cudaStream_t s);
 pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cudaStream_t s);
 pw_status launch_observe(pw_ctx* ctx, int layer, int T, int k, cudaStream_t s);

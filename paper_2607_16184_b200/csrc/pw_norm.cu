@@ -1,0 +1,478 @@
+// Residual addition + root-mean-square norm (with the scaled 8-bit copy of its result), and the quantizer of the
+// scaled 8-bit format.
+//
+//   s = x + r        r' = round(s)        y = s * w / sqrt(mean(s^2) + eps)
+//   per block: top = max |y|, scale = top / 448, code = e4m3(y * (1 / scale))
+//
+// Both read every input element once and write every output element once; nothing else leaves the registers, so
+// HBM bounds them at large sizes and the launch and one round trip to memory at small ones.
+#include "pw_scaled.cuh"
+
+namespace pw {
+
+struct NormArgs {
+  const void* x;
+  const void* r;
+  const void* w;
+  void* r_out;
+  void* y;
+  uint8_t* q;
+  float* q_scales;
+  int64_t x_stride, r_stride, r_out_stride, y_stride, q_stride;
+  int H, w_type, y_type;
+  float eps;
+};
+
+__device__ __forceinline__ float warp_add(float v) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+
+// One CTA per row; the row stays in registers between the sum and the output.  Elements a thread holds:
+//   VEC   eight consecutive ones (16- and 32-byte accesses), half a warp = one group of 128;
+//   else  every 32nd of 256 consecutive ones of its warp, so that single-element accesses are contiguous over the
+//         lanes whatever the row's alignment is; entries 0..3 and 4..7 of a thread belong to one group each.
+// The loads of x, r and (for short rows) w are all issued before the first use; a thread of a long row has no registers
+// to keep w in across the sum and reads it afterwards.  TR = void: no residual.
+template <class TX, class TR, bool VEC, int VPT>
+__global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
+  grid_dep_sync();      // the row may come from the kernel directly ahead
+  grid_dep_trigger();
+  constexpr bool kRes = !std::is_void<TR>::value;
+  using R = typename std::conditional<kRes, TR, float>::type;
+  __shared__ float part[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
+  const int64_t row = blockIdx.x;
+  const TX* x = static_cast<const TX*>(a.x) + row * a.x_stride;
+  const R* r = static_cast<const R*>(a.r) + (kRes ? row * a.r_stride : 0);
+  const int H = a.H;
+  float z[VPT][8];
+  auto at = [&](int v, int j) { return VEC ? (v * (int)blockDim.x + tid) * 8 + j : ((v * n_warps + warp) * 8 + j) * 32 + lane; };
+  // the weights (the same row for every CTA: an L2 hit)
+  constexpr bool kEarly = VPT <= 2;
+  auto weights = [&](int v, float* w) {
+    if constexpr (VEC) {
+      if (at(v, 0) >= H) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = 0.f;
+      } else if (a.w_type == PW_F32) {
+        Raw8<float> t;
+        t.load(static_cast<const float*>(a.w) + at(v, 0));
+        t.get(w);
+      } else if (a.w_type == PW_F16) {
+        Raw8<__half> t;
+        t.load(static_cast<const __half*>(a.w) + at(v, 0));
+        t.get(w);
+      } else {
+        Raw8<__nv_bfloat16> t;
+        t.load(static_cast<const __nv_bfloat16*>(a.w) + at(v, 0));
+        t.get(w);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = at(v, j) < H ? load1(a.w, at(v, j), a.w_type) : 0.f;
+    }
+  };
+  float early[kEarly ? VPT : 1][8];
+  if constexpr (VEC) {
+    Raw8<TX> rx[VPT];
+    Raw8<R> rr[VPT];
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      rx[v].zero();
+      if (at(v, 0) < H) rx[v].load(x + at(v, 0));
+    }
+    if constexpr (kRes) {
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) {
+        rr[v].zero();
+        if (at(v, 0) < H) rr[v].load(r + at(v, 0));
+      }
+    }
+    if constexpr (kEarly) {
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) weights(v, early[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      rx[v].get(z[v]);
+      if constexpr (kRes) {
+        float b[8];
+        rr[v].get(b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[v][j] = __fadd_rn(z[v][j], b[j]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < VPT; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[v][j] = at(v, j) < H ? to_f32(x[at(v, j)]) : 0.f;
+    if constexpr (kRes) {
+      float b[VPT][8];
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[v][j] = at(v, j) < H ? to_f32(r[at(v, j)]) : 0.f;
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[v][j] = __fadd_rn(z[v][j], b[v][j]);
+    }
+  }
+  // sum of squares in 32 bits, in a fixed order: thread, warp, warps
+  float ss = 0.f;
+#pragma unroll
+  for (int v = 0; v < VPT; ++v)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(z[v][j], z[v][j], ss);
+  ss = warp_add(ss);
+  if (lane == 0) part[warp] = ss;
+  if (a.r_out) {
+    const int type = std::is_same<R, float>::value ? PW_F32 : std::is_same<R, __half>::value ? PW_F16 : PW_BF16;
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      if constexpr (VEC) {
+        if (at(v, 0) < H) store8(a.r_out, row * a.r_out_stride + at(v, 0), type, z[v]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (at(v, j) < H) store1(a.r_out, row * a.r_out_stride + at(v, j), type, z[v][j]);
+      }
+    }
+  }
+  __syncthreads();
+  ss = warp_add(lane < n_warps ? part[lane] : 0.f);
+  const float inv = __frcp_rn(__fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)H), a.eps)));
+#pragma unroll
+  for (int v = 0; v < VPT; ++v) {
+    float w[8];
+    if constexpr (VEC && kEarly) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = early[v][j];
+    } else {
+      weights(v, w);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[v][j] = __fmul_rn(__fmul_rn(z[v][j], inv), w[j]);
+  }
+  if (a.y) {
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      if constexpr (VEC) {
+        if (at(v, 0) < H) store8(a.y, row * a.y_stride + at(v, 0), a.y_type, z[v]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (at(v, j) < H) store1(a.y, row * a.y_stride + at(v, j), a.y_type, z[v][j]);
+      }
+    }
+  }
+  if (!a.q) return;
+  // codes of the unrounded values
+  const int G = (H + kGroup - 1) / kGroup;
+  uint8_t* q = a.q + row * a.q_stride;
+  float* qs = a.q_scales + row * G;
+#pragma unroll
+  for (int v = 0; v < VPT; ++v) {
+    if constexpr (VEC) {
+      float top = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = abs_max(top, z[v][j]);
+#pragma unroll
+      for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float scale = block_scale(top), rinv = __frcp_rn(scale);
+      const int c = at(v, 0);
+      if (c >= H) continue;
+      if ((lane & 15) == 0) qs[c / kGroup] = scale;
+      uint2 o;
+      o.x = pack_e4m3(z[v][0] * rinv, z[v][1] * rinv) | (pack_e4m3(z[v][2] * rinv, z[v][3] * rinv) << 16);
+      o.y = pack_e4m3(z[v][4] * rinv, z[v][5] * rinv) | (pack_e4m3(z[v][6] * rinv, z[v][7] * rinv) << 16);
+      *reinterpret_cast<uint2*>(q + c) = o;
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = abs_max(top, z[v][4 * h + j]);
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float scale = block_scale(top), rinv = __frcp_rn(scale);
+        const int c = at(v, 4 * h);
+        if (lane == 0 && c < H) qs[c / kGroup] = scale;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (at(v, 4 * h + j) < H) q[at(v, 4 * h + j)] = (uint8_t)pack_e4m3(z[v][4 * h + j] * rinv, 0.f);
+      }
+    }
+  }
+}
+
+template <class TX, class TR>
+static pw_status launch_norm(const NormArgs& a, bool vec, int T, cudaStream_t s) {
+  // Elements per thread: one vector up to 4096 columns (more threads hide the latency of a short row better than
+  // longer threads do), then as few as 512 threads allow.
+  const int n8 = (a.H + 7) / 8;
+  const int vpt = n8 <= 512 ? 1 : n8 <= 1024 ? 2 : n8 <= 2048 ? 4 : 8;
+  const int threads = ((n8 + vpt - 1) / vpt + 31) / 32 * 32;
+  void (*k)(NormArgs);
+  if (vec) k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, true, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, true, 2> : vpt == 4 ? add_rmsnorm_kernel<TX, TR, true, 4> : add_rmsnorm_kernel<TX, TR, true, 8>;
+  else k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, false, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, false, 2> : vpt == 4 ? add_rmsnorm_kernel<TX, TR, false, 4> : add_rmsnorm_kernel<TX, TR, false, 8>;
+  PW_CUDA_OK(launch_dependent(k, dim3(T), dim3(threads), 0, s, a));
+  return PW_OK;
+}
+template <class TX>
+static pw_status launch_norm_r(const NormArgs& a, int r_type, bool vec, int T, cudaStream_t s) {
+  if (!a.r) return launch_norm<TX, void>(a, vec, T, s);
+  if (r_type == PW_F32) return launch_norm<TX, float>(a, vec, T, s);
+  if (r_type == PW_F16) return launch_norm<TX, __half>(a, vec, T, s);
+  return launch_norm<TX, __nv_bfloat16>(a, vec, T, s);
+}
+
+// ---- quantizer ---------------------------------------------------------------------------------
+
+struct QuantArgs {
+  const void* x;
+  uint8_t* q;
+  float* scales;
+  int64_t x_stride, q_stride;
+  int rows, cols;
+};
+
+// Blocks of one row: a warp takes 256 columns of a row at a time (two groups), U such pieces in flight.
+template <class TX, bool VEC>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a) {
+  grid_dep_sync();
+  grid_dep_trigger();
+  constexpr int U = 4;
+  const int lane = threadIdx.x & 31;
+  const int G = (a.cols + kGroup - 1) / kGroup, P = (G + 1) / 2;
+  const int64_t total = (int64_t)a.rows * P;
+  const int64_t step = (int64_t)gridDim.x * 8 * U;
+  for (int64_t u0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * U; u0 < total; u0 += step) {
+    float z[U][8];
+    Raw8<TX> raw[U];
+    int64_t row[U];
+    int c0[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t un = u0 + u;
+      row[u] = un / P;
+      c0[u] = un < total ? (int)(un - row[u] * P) * 256 : a.cols;      // past the end: every column is out of range
+      const TX* x = static_cast<const TX*>(a.x) + row[u] * a.x_stride;
+      if constexpr (VEC) {
+        raw[u].zero();
+        if (c0[u] + lane * 8 < a.cols) raw[u].load(x + c0[u] + lane * 8);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = c0[u] + j * 32 + lane;
+          z[u][j] = c < a.cols ? to_f32(x[c]) : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint8_t* q = a.q + row[u] * a.q_stride;
+      float* qs = a.scales + row[u] * G;
+      if constexpr (VEC) {
+        raw[u].get(z[u]);
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = abs_max(top, z[u][j]);
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float scale = block_scale(top), rinv = __frcp_rn(scale);
+        const int c = c0[u] + lane * 8;
+        if (c >= a.cols) continue;
+        if ((lane & 15) == 0) qs[c / kGroup] = scale;
+        uint2 o;
+        o.x = pack_e4m3(z[u][0] * rinv, z[u][1] * rinv) | (pack_e4m3(z[u][2] * rinv, z[u][3] * rinv) << 16);
+        o.y = pack_e4m3(z[u][4] * rinv, z[u][5] * rinv) | (pack_e4m3(z[u][6] * rinv, z[u][7] * rinv) << 16);
+        *reinterpret_cast<uint2*>(q + c) = o;
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float top = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = abs_max(top, z[u][4 * h + j]);
+#pragma unroll
+          for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const float scale = block_scale(top), rinv = __frcp_rn(scale);
+          const int c = c0[u] + h * kGroup;
+          if (lane == 0 && c < a.cols) qs[c / kGroup] = scale;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int cj = c + j * 32 + lane;
+            if (cj < a.cols) q[cj] = (uint8_t)pack_e4m3(z[u][4 * h + j] * rinv, 0.f);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Blocks of 128 x 128: a CTA per block, 64 elements of it per thread, all loaded before the maximum is taken.
+//   VEC   half a warp per row, eight columns per lane, eight passes of 16 rows;
+//   else  a warp per row, every 32nd column per lane, 16 passes of 8 rows.
+template <class TX, bool VEC>
+__global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantArgs a) {
+  grid_dep_sync();
+  grid_dep_trigger();
+  __shared__ float part[8];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int G = (a.cols + kGroup - 1) / kGroup;
+  const int64_t rb = blockIdx.x / G;
+  const int g = (int)(blockIdx.x - rb * G);
+  const int64_t r0 = rb * kTileRows;
+  const int c0 = g * kGroup;
+  const TX* x = static_cast<const TX*>(a.x);
+  float z[8][8];
+  if constexpr (VEC) {
+    Raw8<TX> raw[8];
+    const int c = c0 + (lane & 15) * 8;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const int64_t r = r0 + p * 16 + (tid >> 4);
+      raw[p].zero();
+      if (r < a.rows && c < a.cols) raw[p].load(x + r * a.x_stride + c);
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) raw[p].get(z[p]);
+  } else {
+#pragma unroll
+    for (int p = 0; p < 16; ++p)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t r = r0 + p * 8 + warp;
+        const int c = c0 + j * 32 + lane;
+        z[p >> 1][(p & 1) * 4 + j] = r < a.rows && c < a.cols ? to_f32(x[r * a.x_stride + c]) : 0.f;
+      }
+  }
+  float top = 0.f;
+#pragma unroll
+  for (int p = 0; p < 8; ++p)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = abs_max(top, z[p][j]);
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if (lane == 0) part[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, part[i]);
+  const float scale = block_scale(top), rinv = __frcp_rn(scale);
+  if (tid == 0) a.scales[rb * G + g] = scale;
+  if constexpr (VEC) {
+    const int c = c0 + (lane & 15) * 8;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const int64_t r = r0 + p * 16 + (tid >> 4);
+      if (r >= a.rows || c >= a.cols) continue;
+      uint2 o;
+      o.x = pack_e4m3(z[p][0] * rinv, z[p][1] * rinv) | (pack_e4m3(z[p][2] * rinv, z[p][3] * rinv) << 16);
+      o.y = pack_e4m3(z[p][4] * rinv, z[p][5] * rinv) | (pack_e4m3(z[p][6] * rinv, z[p][7] * rinv) << 16);
+      *reinterpret_cast<uint2*>(a.q + r * a.q_stride + c) = o;
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < 16; ++p)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t r = r0 + p * 8 + warp;
+        const int c = c0 + j * 32 + lane;
+        if (r < a.rows && c < a.cols) a.q[r * a.q_stride + c] = (uint8_t)pack_e4m3(z[p >> 1][(p & 1) * 4 + j] * rinv, 0.f);
+      }
+  }
+}
+
+template <class TX>
+static pw_status launch_quant(const QuantArgs& a, int block_rows, bool vec, int num_sms, cudaStream_t s) {
+  const int64_t G = (a.cols + kGroup - 1) / kGroup;
+  if (block_rows == 1) {
+    const int64_t pieces = (int64_t)a.rows * ((G + 1) / 2), ctas = (pieces + 31) / 32;
+    const int64_t cap = (int64_t)num_sms * 64;
+    PW_CUDA_OK(launch_dependent(vec ? quantize_rows_kernel<TX, true> : quantize_rows_kernel<TX, false>,
+                                dim3((unsigned)(ctas < cap ? ctas : cap)), dim3(256), 0, s, a));
+  } else {
+    const int64_t ctas = ((int64_t)a.rows + kTileRows - 1) / kTileRows * G;
+    if (ctas > 0x7fffffff) return PW_ERR_SHAPE;
+    PW_CUDA_OK(launch_dependent(vec ? quantize_blocks_kernel<TX, true> : quantize_blocks_kernel<TX, false>,
+                                dim3((unsigned)ctas), dim3(256), 0, s, a));
+  }
+  return PW_OK;
+}
+
+constexpr int kMaxNormWidth = 32768;            // 512 threads x eight vectors of eight
+
+}  // namespace pw
+
+using namespace pw;
+
+extern "C" pw_status pw_add_rmsnorm(pw_ctx* ctx, int T, int H, const void* x, int x_type, int64_t x_stride,
+                                    const void* residual, int residual_type, int64_t residual_stride, const void* weight,
+                                    int weight_type, float eps, void* residual_out, int64_t residual_out_stride, void* y,
+                                    int y_type, int64_t y_stride, void* q, int64_t q_stride, float* q_scales,
+                                    pw_stream stream) {
+  if (!ctx || T < 0 || H < 1 || !(eps >= 0.f)) return PW_ERR_INVALID_ARG;
+  if (H > kMaxNormWidth) return PW_ERR_SHAPE;
+  if (!type_ok(x_type) || !type_ok(weight_type) || (residual && !type_ok(residual_type)) || (y && !type_ok(y_type)))
+    return PW_ERR_INVALID_ARG;
+  if (T == 0) return PW_OK;
+  if (!x || !weight || (residual_out && !residual) || (!y && !q) || (!q != !q_scales)) return PW_ERR_INVALID_ARG;
+  if (T > 1 && ((x_stride < H) || (residual && residual_stride < H) || (residual_out && residual_out_stride < H) ||
+                (y && y_stride < H) || (q && q_stride < H)))
+    return PW_ERR_SHAPE;
+  const void* ptrs[7] = {x, residual, weight, residual_out, y, q, q_scales};
+  for (const void* p : ptrs)
+    if (!is_aligned(p, 16)) return PW_ERR_ALIGN;
+  if (q && q_stride % 16) return PW_ERR_ALIGN;
+  const pw_status ds = check_device(ctx);
+  if (ds != PW_OK) return ds;
+  NormArgs a{};
+  a.x = x;
+  a.r = residual;
+  a.w = weight;
+  a.r_out = residual_out;
+  a.y = y;
+  a.q = static_cast<uint8_t*>(q);
+  a.q_scales = q_scales;
+  a.x_stride = x_stride;
+  a.r_stride = residual_stride;
+  a.r_out_stride = residual_out_stride;
+  a.y_stride = y_stride;
+  a.q_stride = q_stride;
+  a.H = H;
+  a.w_type = weight_type;
+  a.y_type = y_type;
+  a.eps = eps;
+  // 16-byte accesses where every row of every tensor starts on a 16-byte boundary and holds whole vectors
+  auto rows16 = [&](const void* p, int type, int64_t stride) { return !p || (stride * type_size(type)) % 16 == 0; };
+  const bool vec = H % 8 == 0 && rows16(x, x_type, x_stride) && rows16(residual, residual_type, residual_stride) &&
+                   rows16(residual_out, residual_type, residual_out_stride) && rows16(y, y_type, y_stride);
+  const pw_status st = x_type == PW_F32   ? launch_norm_r<float>(a, residual_type, vec, T, stream)
+                       : x_type == PW_F16 ? launch_norm_r<__half>(a, residual_type, vec, T, stream)
+                                          : launch_norm_r<__nv_bfloat16>(a, residual_type, vec, T, stream);
+  if (st == PW_OK) ctx->launches++;
+  return st;
+}
+
+extern "C" pw_status pw_quantize_scaled(pw_ctx* ctx, const void* x, int x_type, int rows, int cols, int64_t x_stride,
+                                        int block_rows, void* q, int64_t q_stride, float* scales, pw_stream stream) {
+  if (!ctx || rows < 0 || cols < 1 || !type_ok(x_type) || (block_rows != 1 && block_rows != kTileRows))
+    return PW_ERR_INVALID_ARG;
+  if (cols > 1 << 30) return PW_ERR_SHAPE;
+  if (rows == 0) return PW_OK;
+  if (!x || !q || !scales) return PW_ERR_INVALID_ARG;
+  if (rows > 1 && (x_stride < cols || q_stride < cols)) return PW_ERR_SHAPE;
+  if (!is_aligned(x, 16) || !is_aligned(q, 16) || !is_aligned(scales, 16) || q_stride % 16) return PW_ERR_ALIGN;
+  const pw_status ds = check_device(ctx);
+  if (ds != PW_OK) return ds;
+  QuantArgs a{x, static_cast<uint8_t*>(q), scales, x_stride, q_stride, rows, cols};
+  const bool vec = cols % 8 == 0 && (x_stride * type_size(x_type)) % 16 == 0;
+  const pw_status st = x_type == PW_F32   ? launch_quant<float>(a, block_rows, vec, ctx->num_sms, stream)
+                       : x_type == PW_F16 ? launch_quant<__half>(a, block_rows, vec, ctx->num_sms, stream)
+                                          : launch_quant<__nv_bfloat16>(a, block_rows, vec, ctx->num_sms, stream);
+  if (st == PW_OK) ctx->launches++;
+  return st;
+}

@@ -98,8 +98,11 @@ __device__ __forceinline__ void warp_exclusive_scan(const int32_t* in, int32_t* 
 // Single CTA.  Stable counting sort of the P = T*k pairs by expert (positions come from ordered
 // prefix counts, never from atomics), segment table including the shared experts, operand-row ->
 // token map, and the unit lists of the tensor-core kernels.  With `logits` given the CTA routes the tokens
-// itself first (a warp per token, 32 at a time): for a decode batch that is cheaper than a launch of its own.
-__global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__ logits, float* __restrict__ gates,
+// itself first (a warp per token, 32 at a time): for a decode batch that is cheaper than a launch of its own.  With
+// `ids_in` given the caller has routed: its ids and gates are copied in, an id that is no expert becomes -1.  Such a
+// pair gets no operand row (inv_perm -1); the shared experts' rows follow the rows that there are.
+__global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__ logits, const int32_t* ids_in,
+                                                       const float* gates_in, float* __restrict__ gates,
                                                        int32_t* topk_ids, int T, int k, int E,
                                                        int n_shared, int32_t* __restrict__ counts,
                                                        int32_t* __restrict__ offsets, int32_t* __restrict__ perm,
@@ -126,11 +129,26 @@ __global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__
     for (int t = warp; t < T; t += (int)(blockDim.x >> 5)) route_token(logits, t, E, k, topk_ids, gates, lane);
     __syncthreads();                                 // the pairs below are read back from global memory
   }
+  if (ids_in) {
+    for (int p = tid; p < P; p += blockDim.x) {
+      int id = ids_in[p];
+      if (id < -1 || id >= E) {
+        atomicMax(status, (int)PW_ERR_INVALID_ARG);
+        id = -1;
+      }
+      topk_ids[p] = id;
+      gates[p] = gates_in[p];
+    }
+    __syncthreads();
+  }
   for (int e = tid; e < S; e += blockDim.x) cnt[e] = e < E ? 0 : T;
   for (int e = tid; e < E; e += blockDim.x) run[e] = 0;
   if (tid < 64) counter[tid] = 0;
   __syncthreads();
-  for (int p = tid; p < P; p += blockDim.x) atomicAdd(&cnt[topk_ids[p]], 1);
+  for (int p = tid; p < P; p += blockDim.x) {
+    const int e = topk_ids[p];
+    if (e >= 0) atomicAdd(&cnt[e], 1);
+  }
   __syncthreads();
   if (warp == 0) warp_exclusive_scan(cnt, off, S, lane);
   __syncthreads();
@@ -161,11 +179,14 @@ __global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__
       perm[pos] = p;
       inv_perm[p] = pos;
       row_token[pos] = p / k;
+    } else if (p < P) {
+      inv_perm[p] = -1;
     }
     __syncthreads();
   }
-  const int R = off[S];
-  for (int i = tid; i < n_shared * T; i += blockDim.x) row_token[P + i] = i % T;
+  const int R = off[S], routed = off[E];             // routed: the pairs that have an expert
+  for (int p = routed + tid; p < P; p += blockDim.x) perm[p] = -1;
+  for (int i = tid; i < n_shared * T; i += blockDim.x) row_token[routed + i] = i % T;
   for (int i = tid; i < kPadRows; i += blockDim.x) row_token[R + i] = -1;
 
   if (nt_tile <= 0) return;  // SIMT path: no unit lists
@@ -310,7 +331,7 @@ constexpr int kCombineCols = 64, kCombineRows = 4, kMaxSplit = 8;
 template <int kCombineChunks>
 __global__ void __launch_bounds__(kCombineCols * kCombineRows)
     combine_kernel(const float4* y /* written by the kernel directly ahead */, const float* __restrict__ gates, const int32_t* __restrict__ inv_perm,
-                   int T, int k, int n_shared, int H4, int ksplit, size_t split_stride4, float4* __restrict__ out) {
+                   const int32_t* __restrict__ routed_rows, int T, int k, int n_shared, int H4, int ksplit, size_t split_stride4, float4* __restrict__ out) {
   grid_dep_sync();
   grid_dep_trigger();
   __shared__ float4 term[kCombineRows][kCombineChunks][kCombineCols];
@@ -330,7 +351,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
         row = inv_perm[(size_t)t * k + j];
         g = gates[(size_t)t * k + j];
       } else {
-        row = T * k + (j - k) * T + t;
+        row = *routed_rows + (j - k) * T + t;
         g = 1.0f;
       }
 #pragma unroll
@@ -340,7 +361,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
         float4 v[kMaxSplit];
 #pragma unroll
         for (int s = 0; s < kMaxSplit; ++s)
-          if (s < ksplit) v[s] = y[s * split_stride4 + (size_t)row * H4 + c];
+          if (s < ksplit) v[s] = row >= 0 ? y[s * split_stride4 + (size_t)row * H4 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
         float4 a = v[0];
 #pragma unroll
         for (int s = 1; s < kMaxSplit; ++s)
@@ -350,6 +371,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
             a.z = __fadd_rn(a.z, v[s].z);
             a.w = __fadd_rn(a.w, v[s].w);
           }
+        if (row < 0) g = 0.f;                        // a pair without an expert adds nothing, whatever its gate says
         term[ty][cc][tx] = make_float4(__fmul_rn(g, a.x), __fmul_rn(g, a.y), __fmul_rn(g, a.z), __fmul_rn(g, a.w));
       }
     }
@@ -382,7 +404,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
 template <int U>
 __global__ void __launch_bounds__(128)
     combine_stream_kernel(const float4* y /* written by the kernel directly ahead */, const float* __restrict__ gates, const int32_t* __restrict__ inv_perm,
-                          int T, int k, int n_shared, int H4, int ksplit, size_t split_stride4, float4* __restrict__ out) {
+                          const int32_t* __restrict__ routed_rows, int T, int k, int n_shared, int H4, int ksplit, size_t split_stride4, float4* __restrict__ out) {
   grid_dep_sync();
   grid_dep_trigger();
   const int c = blockIdx.x * blockDim.x + threadIdx.x;
@@ -391,31 +413,30 @@ __global__ void __launch_bounds__(128)
   const int J = k + n_shared;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int j0 = 0; j0 < J; j0 += U) {
-    size_t row[U];
+    int row[U];                                      // -1: a pair without an expert, adds nothing
     float g[U];
     float4 a[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int j = j0 + i;
       if (j < k) {
-        row[i] = (size_t)inv_perm[(size_t)t * k + j];
-        g[i] = gates[(size_t)t * k + j];
+        row[i] = inv_perm[(size_t)t * k + j];
+        g[i] = row[i] >= 0 ? gates[(size_t)t * k + j] : 0.f;
       } else {
-        row[i] = (size_t)T * k + (size_t)(j - k) * T + t;
+        row[i] = j < J ? *routed_rows + (j - k) * T + t : -1;
         g[i] = 1.0f;
       }
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (j0 + i < J) a[i] = y[row[i] * H4 + c];
+    for (int i = 0; i < U; ++i) a[i] = row[i] >= 0 ? y[(size_t)row[i] * H4 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
     for (int sp = 1; sp < ksplit; ++sp) {
       float4 v[U];
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (j0 + i < J) v[i] = y[sp * split_stride4 + row[i] * H4 + c];
+        if (row[i] >= 0) v[i] = y[sp * split_stride4 + (size_t)row[i] * H4 + c];
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (j0 + i < J) {
+        if (row[i] >= 0) {
           a[i].x = __fadd_rn(a[i].x, v[i].x);
           a[i].y = __fadd_rn(a[i].y, v[i].y);
           a[i].z = __fadd_rn(a[i].z, v[i].z);
@@ -434,17 +455,18 @@ __global__ void __launch_bounds__(128)
   out[(size_t)t * H4 + c] = acc;
 }
 
-pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const float* logits, int T, int k, int nt_tile,
+pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int k, int nt_tile,
                        int ksplit, cudaStream_t s) {
+  const float* logits = routing.logits;
   const pw_config& c = ctx->cfg;
   const WsMap& w = ctx->ws;
   char* b = ctx->base;
   const int E = c.n_experts, S = w.S;
   int32_t* ids = reinterpret_cast<int32_t*>(b + w.topk_ids);
   // a decode batch is routed by the grouping kernel's own CTA; a long prompt gets a grid of its own
-  const bool fused = (long long)T * k * ((E + 31) / 32) <= kFusedRouteWork;
+  const bool fused = logits && (long long)T * k * ((E + 31) / 32) <= kFusedRouteWork;
   timing_mark(ctx, PW_K_ROUTER, s);
-  if (!fused) {
+  if (logits && !fused) {
     PW_CUDA_OK(launch_dependent(router_kernel, dim3((T * 32 + 255) / 256), dim3(256), 0, s, logits, T, E, k, ids,
                                 reinterpret_cast<float*>(b + w.gates)));
     ctx->launches += 1;
@@ -454,6 +476,7 @@ pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const float* 
   const DevRow* rows = reinterpret_cast<const DevRow*>(b + w.table) + (size_t)layer * S * 3;
   PW_CUDA_OK(launch_dependent(
       permute_kernel, dim3(1), dim3(1024), smem, s, fused ? logits : static_cast<const float*>(nullptr),
+      logits ? static_cast<const int32_t*>(nullptr) : routing.ids, logits ? static_cast<const float*>(nullptr) : routing.gates,
       reinterpret_cast<float*>(b + w.gates), ids, T, k, E, c.n_shared, reinterpret_cast<int32_t*>(b + w.counts),
       reinterpret_cast<int32_t*>(b + w.offsets), reinterpret_cast<int32_t*>(b + w.perm),
       reinterpret_cast<int32_t*>(b + w.inv_perm), reinterpret_cast<int32_t*>(b + w.row_token),
@@ -489,7 +512,8 @@ pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cuda
   if ((long long)T * ((H4 + 127) / 128) >= 2 * ctx->num_sms) {   // enough (token, column) CTAs to fill the machine
     PW_CUDA_OK(launch_dependent(combine_stream_kernel<4>, dim3((H4 + 127) / 128, T), dim3(128), 0, s,
                                 reinterpret_cast<const float4*>(b + w.y), reinterpret_cast<const float*>(b + w.gates),
-                                reinterpret_cast<const int32_t*>(b + w.inv_perm), T, k, c.n_shared, H4, ksplit,
+                                reinterpret_cast<const int32_t*>(b + w.inv_perm),
+                                reinterpret_cast<const int32_t*>(b + w.offsets) + c.n_experts, T, k, c.n_shared, H4, ksplit,
                                 (size_t)R * H4, reinterpret_cast<float4*>(out)));
     ctx->launches += 1;
     PW_CUDA_OK(cudaGetLastError());
@@ -497,7 +521,8 @@ pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cuda
   }
   PW_CUDA_OK(launch_dependent(chunks == 4 ? combine_kernel<4> : combine_kernel<1>, grid, dim3(kCombineCols, kCombineRows), 0, s, reinterpret_cast<const float4*>(b + w.y),
                               reinterpret_cast<const float*>(b + w.gates),
-                              reinterpret_cast<const int32_t*>(b + w.inv_perm), T, k, c.n_shared, H4, ksplit,
+                              reinterpret_cast<const int32_t*>(b + w.inv_perm),
+                                reinterpret_cast<const int32_t*>(b + w.offsets) + c.n_experts, T, k, c.n_shared, H4, ksplit,
                               (size_t)R * H4, reinterpret_cast<float4*>(out)));
   ctx->launches += 1;
   PW_CUDA_OK(cudaGetLastError());
@@ -548,7 +573,7 @@ extern "C" pw_status pw_route_tokens_static(const float* router_logits, int T, i
   const int S = n_experts;
   const size_t smem = sizeof(int32_t) * ((size_t)S + (S + 1) + n_experts + 32 * (size_t)n_experts + (S + 1) + S);
   // the grouping kernel clears the counters it uses; everything else in the scratch is overwritten before it is read
-  permute_kernel<<<1, 1024, smem, stream>>>(nullptr, nullptr, topk_ids, T, top_k, n_experts, 0, counts, offsets, perm,
+  permute_kernel<<<1, 1024, smem, stream>>>(nullptr, nullptr, nullptr, nullptr, topk_ids, T, top_k, n_experts, 0, counts, offsets, perm,
                                             reinterpret_cast<int32_t*>(sc + kStaticInvPerm),
                                             reinterpret_cast<int32_t*>(sc + kStaticRowToken),
                                             reinterpret_cast<int32_t*>(sc + kStaticCounter), nullptr, 0, 0, 0, 1, nullptr,
