@@ -13,17 +13,20 @@
 namespace pw {
 
 constexpr int kBlockK = 128;                    // columns of a scale block = bytes of an operand row in a stage
+constexpr int kScaleRun = 8;                    // scales of a row travel eight blocks (a 32-byte sector) at a time
 constexpr int kWaitPolls = 100000;              // x 20 us suspend time = 2 s
 constexpr int kWaitPollsTest = 200;             // 4 ms (pw_debug_set_wait)
 
 struct LinearArgs {
   CUtensorMap ma, mw;                           // codes of a [T, K] and of w [N, K]
+  CUtensorMap mo;                               // the output, in boxes of 32 rows x 128 bytes (with tma_out)
   const float* sa;
   const float* sw;
   void* out;
   int32_t* status;
   int64_t ld_out;
   int T, N, G, out_type;
+  int tma_out;
   int polls;
   uint32_t hook;
 };
@@ -40,12 +43,15 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar_s, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// Called by a whole warp, with the same answer for all lanes: the lanes of one poll may see the phase flip at different
+// moments, and what follows a wait (tensor-memory loads, cluster barriers) must not be run by a part of the warp.
 // False when the limit ran out or another role of the CTA has given up.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar_s, uint32_t parity, volatile int* gave_up, int polls, int32_t* status) {
-  if (mbar_try(bar_s, parity)) return true;
+  if (__any_sync(0xffffffffu, mbar_try(bar_s, parity))) return true;
+#pragma unroll 1
   for (int n = 0; n < polls; ++n) {
-    if (mbar_try(bar_s, parity)) return true;
-    if (*gave_up) return false;
+    if (__any_sync(0xffffffffu, mbar_try(bar_s, parity))) return true;
+    if (__any_sync(0xffffffffu, *gave_up != 0)) return false;
   }
   *gave_up = 1;
   atomicMax(status, (int)PW_ERR_TIMEOUT);
@@ -59,15 +65,43 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst_s, const CUtensorMap* m
                "l"(map), "r"(x), "r"(y), "r"(bar_s)
                : "memory");
 }
-__device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void mma_commit(uint32_t bar_s) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar_s) : "memory");
+// The MMAs of one stage (four steps of 32 columns) and the commit behind them, on the stage's `done` barrier: the stage
+// is free again and its accumulator complete.  The whole warp runs this on the same values and the lane with on != 0
+// issues: the operands can then live in uniform registers, which a single lane inside a branch would have to fill for
+// every instruction.  PAIR: the forms of a CTA pair, whose commit arrives on the barrier at this offset in both CTAs.
+template <bool PAIR>
+__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t done, uint32_t on) {
+  if constexpr (PAIR) {
+    asm volatile(
+        "{\n\t.reg .pred q, f, t;\n\t.reg .b32 x, y;\n\t.reg .b64 ad, bd;\n\t.reg .b16 both;\n\tmov.b16 both, 3;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\tsetp.ne.b32 f, 0, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "mov.b64 ad, {%1, %3};\n\tmov.b64 bd, {%2, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], ad, bd, %4, f;\n\t"
+        "add.u32 x, %1, 2;\n\tadd.u32 y, %2, 2;\n\tmov.b64 ad, {x, %3};\n\tmov.b64 bd, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], ad, bd, %4, t;\n\t"
+        "add.u32 x, %1, 4;\n\tadd.u32 y, %2, 4;\n\tmov.b64 ad, {x, %3};\n\tmov.b64 bd, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], ad, bd, %4, t;\n\t"
+        "add.u32 x, %1, 6;\n\tadd.u32 y, %2, 6;\n\tmov.b64 ad, {x, %3};\n\tmov.b64 bd, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], ad, bd, %4, t;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], both;\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(done), "r"(on)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred q, f, t;\n\t.reg .b32 x, y;\n\t.reg .b64 ad, bd;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\tsetp.ne.b32 f, 0, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "mov.b64 ad, {%1, %3};\n\tmov.b64 bd, {%2, %3};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, f;\n\t"
+        "add.u32 x, %1, 2;\n\tadd.u32 y, %2, 2;\n\tmov.b64 ad, {x, %3};\n\tmov.b64 bd, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, t;\n\t"
+        "add.u32 x, %1, 4;\n\tadd.u32 y, %2, 4;\n\tmov.b64 ad, {x, %3};\n\tmov.b64 bd, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, t;\n\t"
+        "add.u32 x, %1, 6;\n\tadd.u32 y, %2, 6;\n\tmov.b64 ad, {x, %3};\n\tmov.b64 bd, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, t;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(done), "r"(on)
+        : "memory");
+  }
 }
 // Waits for the tensor-memory loads into v[0 .. 15]; the registers pass through, so that no use moves ahead of it.
 __device__ __forceinline__ void tmem_wait16(float* v) {
@@ -78,70 +112,115 @@ __device__ __forceinline__ void tmem_wait16(float* v) {
                : "memory");
 }
 // Operand tile in shared memory: rows of 128 bytes along K, 128-byte swizzle, groups of eight rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t swizzled_desc(uint32_t saddr) {
-  return (uint64_t)((saddr >> 4) & 0x3fffu) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// The descriptor's low word is the address (and a leading offset that this layout ignores), 32 columns = 2 further on;
+// the high word: offset between the groups, version of sm_100, swizzle mode.
+__device__ __forceinline__ uint32_t swizzled_lo(uint32_t saddr) { return ((saddr >> 4) & 0x3fffu) | 1u << 16; }
+constexpr uint32_t kSwizzledHi = (1024u >> 4) | 1u << 14 | 2u << 29;
 __host__ __device__ constexpr uint32_t e4m3_idesc(int m, int n) {
   return 1u << 4 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;   // fp32 sums, both operands e4m3 and K-major
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+// (all lanes of a warp together)
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float load_cluster(uint32_t addr_s, uint32_t rank) {
-  float v;
-  asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
-               : "=f"(v)
-               : "r"(addr_s), "r"(rank)
-               : "memory");
-  return v;
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr_s, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr_s), "r"(rank));
+  return r;
+}
+// Scales of ROWS rows and the blocks g .. g + 7, one warp: a sector of 32 bytes per row, all loads in flight together,
+// written as [block][row], times a factor (rows padded by four, which keeps both sides free of bank conflicts).  Rows
+// and blocks past the end get 0.
+template <int ROWS>
+__device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T, int G, int g, int g_end, float times, float* dst, int lane) {
+  constexpr int kLoads = ROWS / 4 < 16 ? ROWS / 4 : 16;      // in flight at a time
+  const int j = lane & 7, r0 = lane >> 3;
+  const bool in = g + j < g_end;
+#pragma unroll 1
+  for (int base = 0; base < ROWS; base += kLoads * 4) {
+    float v[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int64_t r = row0 + base + i * 4 + r0;
+      v[i] = in && r < T ? sa[r * G + g + j] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) dst[j * (ROWS + 4) + base + i * 4 + r0] = v[i] * times;
+  }
 }
 
 // ---- few rows: the weights on the M side ---------------------------------------------------------
 // D[128 weight rows, NT tokens].  A CTA takes one 128-row tile of w, up to NT tokens and a range of the blocks; the
-// CTAs of a cluster share the tile and the tokens, each with a range of its own, and add their sums through distributed
-// shared memory in rank order (no workspace, the same bits on every run).
-//   warps 0-3  tensor memory -> registers, scales, output; thread = weight row
-//   warp 4     copies (one stage = a 128 x 128 tile of w and the same columns of NT tokens)
-//   warp 5     MMAs; owns tensor memory (two accumulators of NT columns in turn)
-constexpr int kFewThreads = 192;
+// CTAs of a cluster share the tile and the tokens, each with a range of its own.  Each then owns a share of the tokens:
+// the others copy their sums for those into its shared memory, counted on a barrier there, and it adds them in rank order
+// (no workspace, the same bits on every run).  (Fetched or sent word by word the sums took longer than the product: 10 of
+// 24 us at 64 tokens.)
+//   warps 0 .. kSum - 1  tensor memory -> registers, scales, output; thread = weight row; with 64 tokens on, warps 0-3
+//              take the first half of the columns and 4-7 the second
+//   then one   copies (one stage = a 128 x 128 tile of w and the same columns of NT tokens)
+//   then two   MMAs, even and odd blocks (issuing a stage and its wait cost a warp 500 cycles whatever their size); the
+//              first owns tensor memory: an accumulator of NT columns per stage, so a stage that has been filled again
+//              says that its accumulator has been read, and the MMA warps have one barrier to wait for.  The number of
+//              stages is even: a stage then always belongs to the same MMA warp, which sees every phase of its barrier
+//              (a warp that saw every other one could take an old phase for the one it waits for)
+//   then one   scales, eight blocks at a time, multiplied, into shared memory: loaded by the warps that use them they
+//              were 16 times as many requests as they are sectors, and the bound of the kernel
+// One CTA per SM, its ring as deep as shared memory: the weights come from HBM.  Persistent where there are more tiles
+// than SMs (the CTAs of a cluster then take one unit only, see the launch).
 template <int NT>
 struct FewCfg {
+  static constexpr int kSum = NT >= 64 ? 8 : 4;
+  static constexpr int kThreads = (kSum + 4) * 32;
   static constexpr int kStage = 16384 + NT * 128;
-  static constexpr int kStages = NT <= 16 ? 5 : NT <= 32 ? 5 : NT <= 64 ? 4 : 3;   // two CTAs fit on an SM
+  static constexpr int kStages = NT <= 32 ? 10 : 8;
   static constexpr int kSmem = kStages * kStage + 1024;
-  static constexpr int kCols = 2 * NT;
+  static constexpr int kCols = NT <= 16 ? 256 : 512;   // kStages * NT, a power of two
+  static constexpr int kSums = NT * 512;          // a CTA's sums, and what it receives from a cluster of any size
+  static_assert(kStages % 2 == 0, "a stage belongs to one MMA warp");
+  static_assert(2 * kSums <= kStages * kStage, "both take the ring's place");
+  static_assert(kStages * NT <= kCols, "an accumulator per stage");
 };
+__device__ __forceinline__ void bulk_to_rank(uint32_t dst, uint32_t src_s, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "r"(src_s), "r"(bytes), "r"(bar) : "memory");
+}
 
 template <int NT>
-__global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_constant__ LinearArgs a, int split, int token_tiles) {
+__global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
+    linear_few_kernel(const __grid_constant__ LinearArgs a, int token_tiles, int n_units, int split) {
   using C = FewCfg<NT>;
-  constexpr int S = C::kStages;
+  constexpr int S = C::kStages, NW = C::kSum, QC = NT * 4 / NW;   // columns of a summing warp
   extern __shared__ char smem_raw[];
-  __shared__ unsigned long long full[S], empty[S], acc_full[2], acc_empty[2];
+  __shared__ unsigned long long full[S], done[S], freed[S], sc_full[2], sc_empty[2], sums_in;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int gave_up;
-  __shared__ alignas(16) float col_scale[4][2][NT];      // read four at a time
+  __shared__ alignas(16) float scales[2][kScaleRun][NT + 4];     // read four at a time
   const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x % split);
-  const int unit = (int)(blockIdx.x / split);
-  const int row_tile = unit / token_tiles, tok0 = (unit % token_tiles) * NT;
+  const int unit0 = (int)(blockIdx.x / split), stride = (int)(gridDim.x / split);   // unit: (row tile, token tile), token tiles fastest
   const int g0 = (int)((int64_t)a.G * rank / split), g1 = (int)((int64_t)a.G * (rank + 1) / split);
   const int n_blocks = g1 - g0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+      mbar_init(&done[i], 1);
+      mbar_init(&freed[i], NW);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 4);
+      mbar_init(&sc_full[i], 1);
+      mbar_init(&sc_empty[i], NW);
     }
+    mbar_init(&sums_in, 1);
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 5) {
+  if (warp == NW + 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(C::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -152,130 +231,452 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
   grid_dep_sync();          // codes and scales may come from the kernel directly ahead
   grid_dep_trigger();
 
-  float acc[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) acc[j] = 0.f;
+  float acc[QC];
+  const int col = (warp >> 2) * QC, row = (warp & 3) * 32 + lane;   // of a summing warp
 
-  if (warp == 4) {
+  if (warp == NW) {
     bool ok = true;
-    int i = 0;
-    for (; ok && i < n_blocks; ++i) {
-      if ((a.hook & 2u) && i == 1) break;          // test hook: the waits on the second stage run out
-      const int s = i % S;
-      if (i >= S) ok = mbar_wait(smem_u32(&empty[s]), (i / S - 1) & 1, &gave_up, a.polls, a.status);
-      if (!ok) break;
-      if (lane == 0) {
-        const uint32_t bar = smem_u32(&full[s]), dst = ring_s + s * C::kStage;
-        mbar_expect_tx(bar, C::kStage);
-        tma_load_2d(dst, &a.mw, (g0 + i) * kBlockK, row_tile * 128, bar);
-        tma_load_2d(dst + 16384, &a.ma, (g0 + i) * kBlockK, tok0, bar);
+    int i = 0, s = 0;
+    uint32_t par = 1;                              // of the stage's next `freed` phase (the first pass waits for none)
+    for (int u = unit0; ok && u < n_units; u += stride) {
+      const int row0 = u / token_tiles * 128, tok0 = u % token_tiles * NT;
+      for (int g = g0; g < g1; ++g, ++i) {
+        if ((a.hook & 2u) && i == 1) ok = false;   // test hook: the waits on the second stage run out
+        if (ok && i >= S) ok = mbar_wait(smem_u32(&freed[s]), par, &gave_up, a.polls, a.status);
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&full[s]), dst = ring_s + s * C::kStage;
+          mbar_expect_tx(bar, C::kStage);
+          tma_load_2d(dst, &a.mw, g * kBlockK, row0, bar);
+          tma_load_2d(dst + 16384, &a.ma, g * kBlockK, tok0, bar);
+        }
+        __syncwarp();
+        if (++s == S) {
+          s = 0;
+          par ^= 1u;
+        }
       }
-      __syncwarp();
     }
     if (!ok)                                       // leave nothing in flight
       for (int j = i < S ? 0 : i - S; j < i; ++j)
         for (int n = 0; n < 200 && !mbar_try(smem_u32(&full[j % S]), (j / S) & 1); ++n) {
         }
-  } else if (warp == 5) {
+  } else if (warp == NW + 1 || warp == NW + 2) {
     bool ok = true;
-    for (int i = 0; ok && i < n_blocks; ++i) {
-      const int s = i % S, b = i & 1;
-      if (i >= 2) ok = mbar_wait(smem_u32(&acc_empty[b]), ((i >> 1) - 1) & 1, &gave_up, a.polls, a.status);
-      if (ok) ok = mbar_wait(smem_u32(&full[s]), (i / S) & 1, &gave_up, a.polls, a.status);
+    const uint32_t on = lane == 0 ? 1u : 0u;
+    const int units = unit0 < n_units ? (n_units - 1 - unit0) / stride + 1 : 0, items = units * n_blocks;
+    for (int i = warp - NW - 1; ok && i < items; i += 2) {
+      const int s = i % S;
+      ok = mbar_wait(smem_u32(&full[s]), (i / S) & 1, &gave_up, a.polls, a.status);
       if (!ok) break;
       tc_fence_after();
-      if (lane == 0) {
-        const uint32_t w_s = ring_s + s * C::kStage;
-        const uint64_t wd = swizzled_desc(w_s), xd = swizzled_desc(w_s + 16384);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)                // 32 columns (bytes) per instruction
-          mma_e4m3(tmem + b * NT, wd + 2 * k, xd + 2 * k, e4m3_idesc(128, NT), k > 0);
-        mma_commit(smem_u32(&empty[s]));
-        mma_commit(smem_u32(&acc_full[b]));
+      const uint32_t w_s = ring_s + s * C::kStage;
+      mma_stage<false>(tmem + s * NT, swizzled_lo(w_s), swizzled_lo(w_s + 16384), kSwizzledHi, e4m3_idesc(128, NT), smem_u32(&done[s]), on);
+    }
+  } else if (warp == NW + 3) {
+    bool ok = true;
+    int run = 0;
+    for (int u = unit0; ok && u < n_units; u += stride) {
+      const float* sw = a.sw + (int64_t)(u / token_tiles) * a.G;
+      for (int g = g0; g < g1; g += kScaleRun, ++run) {
+        const float w = g + (lane & 7) < g1 ? sw[g + (lane & 7)] : 0.f;
+        if (run >= 2) ok = mbar_wait(smem_u32(&sc_empty[run & 1]), ((run >> 1) - 1) & 1, &gave_up, a.polls, a.status);
+        if (!ok) break;
+        load_scales<NT>(a.sa, (int64_t)(u % token_tiles) * NT, a.T, a.G, g, g1, w, &scales[run & 1][0][0], lane);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sc_full[run & 1]);
       }
-      __syncwarp();
     }
   } else {
-    const float* sw = a.sw + (int64_t)row_tile * a.G + g0;
-    constexpr int M = (NT + 31) / 32;
-    float next[M];
-    auto fetch = [&](int i) {                      // scales of block i for the columns lane, lane + 32, ..
-      const float w = sw[i];
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const int j = lane + 32 * m;
-        next[m] = j < NT && tok0 + j < a.T ? a.sa[(int64_t)(tok0 + j) * a.G + g0 + i] * w : 0.f;
-      }
-    };
-    if (n_blocks > 0) fetch(0);
     bool ok = true;
-    for (int i = 0; ok && i < n_blocks; ++i) {
-      const int b = i & 1;
-      float* cs = col_scale[warp][b];
-      __syncwarp();
+    int s = 0, run = 0;
+    uint32_t par = 0;                              // of the stage's next `done` phase
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
+    for (int u = unit0; ok && u < n_units; u += stride) {
 #pragma unroll
-      for (int m = 0; m < M; ++m)
-        if (lane + 32 * m < NT) cs[lane + 32 * m] = next[m];
-      __syncwarp();
-      if (i + 1 < n_blocks) fetch(i + 1);
-      ok = mbar_wait(smem_u32(&acc_full[b]), (i >> 1) & 1, &gave_up, a.polls, a.status);
-      if (!ok) break;
-      tc_fence_after();
-      constexpr int W = NT < 64 ? NT : 64;
+      for (int j = 0; j < QC; ++j) acc[j] = 0.f;
+      int in_run = 0;
+#pragma unroll 1
+      for (int g = g0; g < g1; ++g) {
+        if (in_run == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+        if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        const float* cs = scales[run & 1][in_run] + col;
+        constexpr int W = QC < 32 ? QC : 32;       // columns loaded at once
 #pragma unroll
-      for (int h = 0; h < NT; h += W) {
-        float v[W];
+        for (int h = 0; h < QC; h += W) {
+          float v[W];
 #pragma unroll
-        for (int c = 0; c < W; c += 16) tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + b * NT + h + c, v + c);
+          for (int c = 0; c < W; c += 16) tmem_ld16(lane_base + s * NT + h + c, v + c);
 #pragma unroll
-        for (int c = 0; c < W; c += 16) tmem_wait16(v + c);
-        if (h + W == NT) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&acc_empty[b]);
+          for (int c = 0; c < W; c += 16) tmem_wait16(v + c);
+          if (h + W == QC) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&freed[s]);
+          }
+#pragma unroll
+          for (int j = 0; j < W; j += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(cs + h + j);
+            acc[h + j] = fmaf(v[j], f.x, acc[h + j]);
+            acc[h + j + 1] = fmaf(v[j + 1], f.y, acc[h + j + 1]);
+            acc[h + j + 2] = fmaf(v[j + 2], f.z, acc[h + j + 2]);
+            acc[h + j + 3] = fmaf(v[j + 3], f.w, acc[h + j + 3]);
+          }
         }
-#pragma unroll
-        for (int j = 0; j < W; j += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(cs + h + j);
-          acc[h + j] = fmaf(v[j], f.x, acc[h + j]);
-          acc[h + j + 1] = fmaf(v[j + 1], f.y, acc[h + j + 1]);
-          acc[h + j + 2] = fmaf(v[j + 2], f.z, acc[h + j + 2]);
-          acc[h + j + 3] = fmaf(v[j + 3], f.w, acc[h + j + 3]);
+        if (++in_run == kScaleRun || g + 1 == g1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_empty[run & 1]);
+          in_run = 0;
+          ++run;
+        }
+        if (++s == S) {
+          s = 0;
+          par ^= 1u;
         }
       }
+      const int64_t n = (int64_t)(u / token_tiles) * 128 + row;
+      const int t0 = u % token_tiles * NT + col;
+      if (split == 1 && ok && n < a.N) {
+#pragma unroll
+        for (int j = 0; j < QC; ++j)
+          if (t0 + j < a.T) store1(a.out, (int64_t)(t0 + j) * a.ld_out + n, a.out_type, acc[j]);
+      }
+      __syncwarp();
     }
   }
 
-  const int n = row_tile * 128 + (int)threadIdx.x;       // threads 0 .. 127: my weight row
-  if (split == 1) {
-    if (warp < 4 && n < a.N) {
+  if (split > 1) {
+    // The sums as [token][row] in the ring, which is free (every copy has landed and every MMA has read its operands:
+    // the last accumulator was complete), then the part of each owner with one bulk copy into its [rank][token][row]
+    // behind, once its ring is free too.  Whoever gave up on a wait sends all the same, so the wait for the others' sums
+    // outlasts any of theirs.
+    const int64_t n = (int64_t)(unit0 / token_tiles) * 128 + row;
+    const int tok0 = unit0 % token_tiles * NT;
+    const int own = NT / split;                    // tokens of the tile that a CTA of the cluster adds up
+    const int mine = min(max(a.T - tok0 - rank * own, 0), own);
+    const uint32_t sums_s = ring_s + C::kSums;
+    if (warp < NW) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        if (tok0 + j < a.T) store1(a.out, (int64_t)(tok0 + j) * a.ld_out + n, a.out_type, acc[j]);
+      for (int j = 0; j < QC; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring_s + (col + j) * 512 + row * 4), "f"(acc[j]) : "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    } else if (warp == NW && lane == 0) {
+      mbar_expect_tx(smem_u32(&sums_in), (uint32_t)(split * mine) * 512);
     }
-  } else {
-    // every copy has landed and every MMA has read its operands (the last accumulator was complete): the ring is free
-    const uint32_t mine_s = ring_s + threadIdx.x * 4;
-    if (warp < 4) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine_s + j * 512), "f"(acc[j]) : "memory");
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    if (warp == NW && lane < split) {
+      const int theirs = min(max(a.T - tok0 - lane * own, 0), own);
+      if (theirs > 0)
+        bulk_to_rank(map_rank(sums_s + rank * own * 512, lane), ring_s + lane * own * 512, theirs * 512, map_rank(smem_u32(&sums_in), lane));
     }
     __syncwarp();
-    cluster_sync();
-    if (warp < 4 && n < a.N) {
-      for (int j = NT * rank / split; j < NT * (rank + 1) / split && tok0 + j < a.T; ++j) {
-        float v = 0.f;
-        for (int r = 0; r < split; ++r) v += load_cluster(mine_s + j * 512, r);
-        store1(a.out, (int64_t)(tok0 + j) * a.ld_out + n, a.out_type, v);
+    if (warp < NW && mine > 0) {
+      volatile int no_matter = 0;
+      if (mbar_wait(smem_u32(&sums_in), 0, &no_matter, 8 * a.polls, a.status) && n < a.N) {
+        const float* sums = reinterpret_cast<const float*>(smem_raw + (sums_s - smem_u32(smem_raw))) + row;
+        // tokens four at a time, in turn between the halves of the warps
+        for (int j0 = (warp >> 2) * 4; j0 < mine; j0 += NW) {
+          float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+          for (int r = 0; r < split; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (j0 + j < mine) v[j] += sums[(r * own + j0 + j) * 128];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (j0 + j < mine) store1(a.out, (int64_t)(tok0 + rank * own + j0 + j) * a.ld_out + n, a.out_type, v[j]);
+        }
       }
     }
-    __syncwarp();
-    cluster_sync();                                      // nobody leaves while its sums are being read
+    cluster_arrive();                              // the copies read this CTA's ring until the owners have their sums
+    cluster_wait();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::kCols));
+  __syncwarp();
+  if (warp == NW + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::kCols));
+}
+
+// ---- many rows: pairs of CTAs --------------------------------------------------------------------
+// D[256 tokens, BN weight rows] by two CTAs of a cluster on one tile (cta_group::2): each holds 128 of the token rows and
+// half of the weight rows in its shared memory, and the accumulators of its own 128 tokens.  A block of 128 columns gets
+// a fresh accumulator (512 / BN of them in turn); its sums leave tensor memory in one pass, are scaled and stay in
+// registers until the tile is complete, so the epilogue warps work all the time, next to the MMAs.
+//   warps 0-7   tensor memory -> registers, scales, output: warps 0-3 the first half of the columns, 4-7 the second;
+//               thread = token row
+//   warp 8      copies (both CTAs; a stage = 128 token rows and BN / 2 weight rows of one block, all counted on the
+//               first CTA's barrier)
+//   warps 9,10  MMAs (first CTA only), even and odd blocks; warp 9 owns tensor memory
+//   warp 11     scales, eight blocks at a time, into shared memory
+// The last four warps hand most of their registers to the first eight, whose sums fill 128 each.
+// Persistent: a pair takes every n_pairs-th tile, token tiles fastest, so that the pairs at work share weight rows in L2.
+constexpr int kPairThreads = 384;
+template <int BN>
+struct PairCfg {
+  static constexpr int kStage = 16384 + BN / 2 * 128;
+  static constexpr int kStages = BN == 256 ? 4 : 6;   // 128 KB in flight: what the latency of L2 times its rate asks for
+  static_assert(kStages % 2 == 0, "a stage belongs to one MMA warp, see linear_few_kernel");
+  static constexpr int kSmem = kStages * kStage + 65536 + 1024;   // and two boxes of output for each of eight warps
+  static constexpr int kAcc = 512 / BN;           // accumulators in tensor memory (an even number, for the same reason)
+};
+// copy into this CTA's shared memory, counted on a barrier of the pair (shared::cluster address)
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_s, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst_s),
+               "l"(map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+// (nothing in memory is handed over with it, only tensor memory, which the tcgen05 fences order: a release at cluster
+// scope would make the warp wait for its outstanding loads and stores first)
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(float* v) {
+  tmem_wait16(v);
+  tmem_wait16(v + 16);
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src_s) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src_s) : "memory");
+}
+
+// A warp's 32 rows x COLS outputs, thread = row, by way of boxes of 32 rows x 128 bytes in shared memory (128-byte
+// swizzle: 16-byte piece c of row r lies at c ^ (r mod 8)).  With a tensor map of the output the boxes leave by
+// asynchronous copies, while the next tile is being summed; a box is written again once its copy has read it.  Without
+// one (rows that are no multiple of 16 bytes long and apart) the lanes store element by element, contiguous along a row.
+// (Stored straight from registers, 32 rows apart in every instruction, a tile's output took 10000 cycles.)
+// One box: `words` are the row's 128 bytes.
+__device__ __forceinline__ void store_box(uint32_t box_s, const char* box, const uint32_t* words, const LinearArgs& a, int64_t m0, int n, int size, int lane) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box_s + lane * 128 + ((c ^ (lane & 7)) << 4)), "r"(words[c * 4]),
+                 "r"(words[c * 4 + 1]), "r"(words[c * 4 + 2]), "r"(words[c * 4 + 3])
+                 : "memory");
+  if (a.tma_out) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      if (m0 < a.T && n < a.N) tma_store_2d(&a.mo, n, (int)m0, box_s);   // rows and columns past the end are left out
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  } else {
+    __syncwarp();
+    for (int r = 0; r < 32 && m0 + r < a.T; ++r)
+      for (int e = lane; e * size < 128 && n + e < a.N; e += 32) {
+        const int byte = e * size;
+        const char* from = box + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15);
+        const int64_t at = (m0 + r) * a.ld_out + n + e;
+        if (size == 4) static_cast<uint32_t*>(a.out)[at] = *reinterpret_cast<const uint32_t*>(from);
+        else static_cast<uint16_t*>(a.out)[at] = *reinterpret_cast<const uint16_t*>(from);
+      }
+    __syncwarp();
+  }
+}
+template <int COLS>
+__device__ __forceinline__ void store_tile(uint32_t box_s, const char* box, const float* acc, const LinearArgs& a, int64_t m0, int n0, int lane) {
+  uint32_t words[32];
+  auto boxes_read = [&] {                                     // by the copies so far
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+  };
+  boxes_read();
+  if (a.out_type == PW_F32) {
+#pragma unroll
+    for (int p = 0; p < COLS / 32; ++p) {
+      if (p == 2) boxes_read();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) words[j] = __float_as_uint(acc[p * 32 + j]);
+      store_box(box_s + (p & 1) * 4096, box + (p & 1) * 4096, words, a, m0, n0 + p * 32, 4, lane);
+    }
+  } else {
+    const bool half = a.out_type == PW_F16;
+#pragma unroll
+    for (int p = 0; p < COLS / 64; ++p) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        words[j] = half ? pack_half(acc[p * 64 + 2 * j], acc[p * 64 + 2 * j + 1]) : pack_bf(acc[p * 64 + 2 * j], acc[p * 64 + 2 * j + 1]);
+      store_box(box_s + p * 4096, box + p * 4096, words, a, m0, n0 + p * 64, 2, lane);
+    }
+  }
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __grid_constant__ LinearArgs a, int token_tiles, int n_tiles) {
+  using C = PairCfg<BN>;
+  constexpr int S = C::kStages, A = C::kAcc, HC = BN / 2;
+  static_assert(A <= S, "a stage's barrier stands for its accumulator too");
+  extern __shared__ char smem_raw[];
+  __shared__ unsigned long long full[S], done[S], acc_empty[A], sc_full[2], sc_empty[2];
+  __shared__ uint32_t tmem_base;
+  __shared__ volatile int gave_up;
+  __shared__ float scales[2][kScaleRun][128 + 4], w_scales[2][2][kScaleRun];
+  const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const uint32_t rank = blockIdx.x & 1;           // cluster of two along x
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&done[i], 1);
+    }
+    for (int i = 0; i < A; ++i) mbar_init(&acc_empty[i], 16);   // the epilogue warps of both CTAs
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sc_full[i], 1);
+      mbar_init(&sc_empty[i], 8);
+    }
+    gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                                 // the other CTA's barriers and tensor memory are ready too
+  tc_fence_after();
+  const uint32_t tmem = tmem_base;
+  grid_dep_sync();          // codes and scales may come from the kernel directly ahead
+  grid_dep_trigger();
+
+  // 384 threads of 168 registers: four warps at 40 leave eight 232 each
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 8) {
+      bool ok = true;
+      int item = 0;
+      for (int t = pair; ok && t < n_tiles; t += n_pairs) {
+        const int m0 = (t % token_tiles) * 256 + (int)rank * 128, n0 = (t / token_tiles) * BN + (int)rank * HC;
+        for (int g = 0; g < a.G; ++g, ++item) {
+          const int s = item % S;
+          if ((a.hook & 2u) && item == 1) ok = false;   // test hook: the waits on the second stage run out
+          if (ok && item >= S) ok = mbar_wait(smem_u32(&done[s]), (item / S - 1) & 1, &gave_up, a.polls, a.status);
+          if (!ok) break;
+          if (lane == 0) {
+            const uint32_t bar_s = smem_u32(&full[s]), dst = ring_s + s * C::kStage;
+            if (rank == 0) mbar_expect_tx(bar_s, 2 * C::kStage);
+            const uint32_t bar = map_rank(bar_s, 0);
+            tma_load_2d_pair(dst, &a.ma, g * kBlockK, m0, bar);
+            tma_load_2d_pair(dst + 16384, &a.mw, g * kBlockK, n0, bar);
+          }
+          __syncwarp();
+        }
+      }
+      // leave nothing behind: every stage handed back (its arrival crosses to the other CTA), or at least every copy landed
+      for (int j = item < S ? 0 : item - S; ok && j < item; ++j)
+        ok = mbar_wait(smem_u32(&done[j % S]), (j / S) & 1, &gave_up, a.polls, a.status);
+      if (!ok && rank == 0)
+        for (int j = item < S ? 0 : item - S; j < item; ++j)
+          for (int n = 0; n < 200 && !mbar_try(smem_u32(&full[j % S]), (j / S) & 1); ++n) {
+          }
+    } else if (warp == 9 || warp == 10) {
+      // two warps issue, blocks in turn: every block has an accumulator of its own, so their order does not matter
+      bool ok = rank == 0;
+      const uint32_t on = lane == 0 ? 1u : 0u;
+      const int my_tiles = pair < n_tiles ? (n_tiles - 1 - pair) / n_pairs + 1 : 0;
+      const int64_t items = (int64_t)my_tiles * a.G;
+      for (int64_t it = warp - 9; ok && it < items; it += 2) {
+        const int item = (int)it, s = item % S, b = item % A;
+        if (item >= A) ok = mbar_wait(smem_u32(&acc_empty[b]), (item / A - 1) & 1, &gave_up, a.polls, a.status);
+        if (ok) ok = mbar_wait(smem_u32(&full[s]), (item / S) & 1, &gave_up, a.polls, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t x_s = ring_s + s * C::kStage;
+        mma_stage<true>(tmem + b * BN, swizzled_lo(x_s), swizzled_lo(x_s + 16384), kSwizzledHi, e4m3_idesc(256, BN), smem_u32(&done[s]), on);
+      }
+    } else if (warp == 11) {
+      bool ok = true;
+      int run = 0;
+      for (int t = pair; ok && t < n_tiles; t += n_pairs) {
+        const int64_t m0 = (int64_t)(t % token_tiles) * 256 + rank * 128;
+        const int wb = (t / token_tiles) * BN / 128 + (lane >> 3);       // lanes 0-7, 8-15: the tile's weight blocks
+        for (int g = 0; g < a.G; g += kScaleRun, ++run) {
+          const float w = lane < 16 && (int64_t)wb * 128 < a.N && g + (lane & 7) < a.G ? a.sw[(int64_t)wb * a.G + g + (lane & 7)] : 0.f;
+          if (run >= 2) ok = mbar_wait(smem_u32(&sc_empty[run & 1]), ((run >> 1) - 1) & 1, &gave_up, a.polls, a.status);
+          if (!ok) break;
+          if (lane < 16) w_scales[run & 1][lane >> 3][lane & 7] = w;
+          load_scales<128>(a.sa, m0, a.T, a.G, g, a.G, 1.f, &scales[run & 1][0][0], lane);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_full[run & 1]);
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    const int row = (warp & 3) * 32 + lane, col = (warp >> 2) * HC;
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
+    const uint32_t box_s = ring_s + S * C::kStage + warp * 8192;
+    const char* box = smem_raw + (box_s - smem_u32(smem_raw));
+    bool ok = true;
+    int s = 0, b = 0, run = 0;
+    uint32_t par = 0;                               // of the stage's next `done` phase
+    for (int t = pair; ok && t < n_tiles; t += n_pairs) {
+      float acc[HC];
+#pragma unroll
+      for (int j = 0; j < HC; ++j) acc[j] = 0.f;
+#pragma unroll 1
+      for (int g = 0; g < a.G; ++g) {
+        if (g % kScaleRun == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+        const float f = scales[run & 1][g % kScaleRun][row] * w_scales[run & 1][col / 128][g % kScaleRun];
+        if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        float v[2][32];
+        tmem_ld32(lane_base + b * BN, v[0]);
+#pragma unroll
+        for (int c = 0; c < HC / 32; ++c) {
+          tmem_wait32(v[c & 1]);
+          if (c + 1 < HC / 32) {
+            tmem_ld32(lane_base + b * BN + (c + 1) * 32, v[(c + 1) & 1]);
+          } else {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_cluster(map_rank(smem_u32(&acc_empty[b]), 0));
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[c * 32 + j] = fmaf(v[c & 1][j], f, acc[c * 32 + j]);
+        }
+        if (g % kScaleRun == kScaleRun - 1 || g == a.G - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_empty[run & 1]);
+          ++run;
+        }
+        b = b + 1 == A ? 0 : b + 1;
+        if (++s == S) {
+          s = 0;
+          par ^= 1u;
+        }
+      }
+      if (ok) store_tile<HC>(box_s, box, acc, a, (int64_t)(t % token_tiles) * 256 + rank * 128 + (warp & 3) * 32, (t / token_tiles) * BN + col, lane);
+      __syncwarp();
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // the output is written, the boxes are read
+    __syncwarp();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                                 // nobody leaves while the other CTA may still arrive on its barriers
+  tc_fence_after();
+  __syncwarp();
+  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512));
 }
 
 // ---- host side -----------------------------------------------------------------------------------
@@ -293,6 +694,17 @@ static bool codes_map(void* encode, const void* base, int rows, int cols, int64_
                                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Map of the output: boxes of 32 rows x 128 bytes, swizzled.
+static bool out_map(void* encode, void* base, int rows, int cols, int64_t stride, int type, CUtensorMap* m) {
+  const int size = type_size(type);
+  const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t pitch[1] = {(cuuint64_t)stride * size};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / size), 32}, step[2] = {1, 1};
+  return reinterpret_cast<EncodeTiledFn>(encode)(m, size == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, dim, pitch,
+                                                 box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                 CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static pw_status linear_setup(pw_ctx* ctx) {
   if (ctx->encode_tiled) return PW_OK;
   void* fn = nullptr;
@@ -302,13 +714,15 @@ static pw_status linear_setup(pw_ctx* ctx) {
   PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<16>::kSmem));
   PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<32>::kSmem));
   PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<64>::kSmem));
-  PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<128>::kSmem));
+  PW_CUDA_OK(cudaFuncSetAttribute(linear_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<128>::kSmem));
+  PW_CUDA_OK(cudaFuncSetAttribute(linear_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<256>::kSmem));
   ctx->encode_tiled = fn;
   return PW_OK;
 }
 
-static cudaError_t launch_cluster(void (*kernel)(LinearArgs, int, int), unsigned ctas, unsigned cluster, int threads, size_t smem,
-                                  cudaStream_t s, const LinearArgs& a, int p0, int p1) {
+template <class... Args>
+static cudaError_t launch_cluster(void (*kernel)(LinearArgs, Args...), unsigned ctas, unsigned cluster, int threads, size_t smem, cudaStream_t s,
+                                  const LinearArgs& a, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(threads);
@@ -321,19 +735,57 @@ static cudaError_t launch_cluster(void (*kernel)(LinearArgs, int, int), unsigned
   attr[1].val.clusterDim.x = cluster;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, a, p0, p1);
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, args...);
+}
+
+// How a product is cut: the kernel (few: nt tokens per tile, or pair: bn weight rows per tile), the units of work and,
+// for the few kernel, over how many CTAs of a cluster the blocks of a unit are split.
+struct LinearPlan {
+  int nt, bn, split;
+  int64_t token_tiles, units;
+  double us;                                       // estimate
+};
+static int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
+
+static LinearPlan plan_few(int T, int N, int G, int nt, int sms) {
+  LinearPlan p{nt, 0, 1, tiles_of(T, nt), 0, 0.};
+  p.units = p.token_tiles * tiles_of(N, 128);
+  // few units: their blocks are split over a cluster, while there is an SM for every CTA and two blocks for each
+  while (p.split < 8 && p.units * p.split * 2 <= sms && G >= p.split * 4) p.split *= 2;
+  const int64_t blocks = p.split > 1 ? tiles_of(G, p.split) : tiles_of(p.units, sms) * G;
+  p.us = 5.0 + (p.split > 1 ? 1.3 : 0.) + (nt == 16 ? 0.24 : nt == 32 ? 0.32 : 0.375) * blocks;
+  return p;
+}
+static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
+  LinearPlan p{0, bn, 1, tiles_of(T, 256), 0, 0.};
+  p.units = p.token_tiles * tiles_of(N, bn);
+  p.us = 4.6 + (bn == 128 ? 0.32 : 0.5) * tiles_of(p.units, sms / 2) * G;
+  return p;
+}
+// The plan that finishes soonest by a model that is linear in the blocks of 128 columns a CTA (pair) goes through one
+// after the other; the times per block are measured (us, contraction 4096: tokens x weight rows, few 64 / pair 128 /
+// pair 256):  64 x 4096  9.4 / 14.1 / 18.5,  128 x 4096  11.7 / 14.4 / 19.3,  128 x 14336  27.3 / 27.6 / 22.7,
+// 256 x 4096  14.9 / 14.5 / 19.3,  512 x 4096  26.2 / 15.6 / 20.0,  512 x 14336  80 / 48 / 38.
+static LinearPlan plan_linear(int T, int N, int G, int sms) {
+  LinearPlan best = plan_few(T, N, G, T <= 16 ? 16 : T <= 32 ? 32 : 64, sms);
+  for (int bn = 128; bn <= 256; bn *= 2) {
+    const LinearPlan p = plan_pair(T, N, G, bn, sms);
+    if (p.us < best.us) best = p;
+  }
+  return best;
 }
 
 template <int NT>
-static pw_status launch_few(pw_ctx* ctx, LinearArgs& a, int64_t row_tiles, int64_t token_tiles, cudaStream_t s) {
-  // Split the blocks over a cluster until there are two CTAs per SM, and at least two blocks per CTA.
-  int split = 1;
-  while (split < 8 && row_tiles * token_tiles * split * 2 <= 2 * ctx->num_sms && a.G >= split * 4) split *= 2;
-  const int64_t ctas = row_tiles * token_tiles * split;
-  if (ctas > 0x7fffffff) return PW_ERR_SHAPE;
-  PW_CUDA_OK(launch_cluster(linear_few_kernel<NT>, (unsigned)ctas, split, kFewThreads, FewCfg<NT>::kSmem, s, a, split, (int)token_tiles));
-  return PW_OK;
+static cudaError_t launch_few(const LinearPlan& p, const LinearArgs& a, int sms, cudaStream_t s) {
+  const int64_t ctas = p.split > 1 || p.units < sms ? p.units * p.split : sms;
+  return launch_cluster(linear_few_kernel<NT>, (unsigned)ctas, p.split, FewCfg<NT>::kThreads, FewCfg<NT>::kSmem, s, a, (int)p.token_tiles,
+                        (int)p.units, p.split);
+}
+template <int BN>
+static cudaError_t launch_pair(const LinearPlan& p, const LinearArgs& a, int sms, cudaStream_t s) {
+  const int64_t pairs = p.units < sms / 2 ? p.units : sms / 2;
+  return launch_cluster(linear_pair_kernel<BN>, (unsigned)pairs * 2, 2, kPairThreads, PairCfg<BN>::kSmem, s, a, (int)p.token_tiles, (int)p.units);
 }
 
 }  // namespace pw
@@ -354,9 +806,9 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
   if (a_stride % 16 || w_stride % 16) return PW_ERR_ALIGN;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
-  pw_status st = linear_setup(ctx);
+  const pw_status st = linear_setup(ctx);
   if (st != PW_OK) return st;
-  LinearArgs a;
+  LinearArgs a{};
   a.sa = a_scales;
   a.sw = w_scales;
   a.out = out;
@@ -368,18 +820,21 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
   a.out_type = out_type;
   a.polls = ctx->wait_polls ? kWaitPollsTest : kWaitPolls;
   a.hook = ctx->test_hook;
-  const int64_t row_tiles = ((int64_t)N + 127) / 128;
-  const int nt = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
-  const int64_t token_tiles = ((int64_t)T + nt - 1) / nt;
+  const LinearPlan p = plan_linear(T, N, a.G, ctx->num_sms);
+  if (p.units > 0x7fffffff) return PW_ERR_SHAPE;
   // a single row's stride is never used: give the map one that it accepts
-  const int64_t min_pitch = ((int64_t)K + 15) / 16 * 16;
-  const int64_t pa = a_stride < min_pitch ? min_pitch : a_stride, pwgt = w_stride < min_pitch ? min_pitch : w_stride;
-  if (!codes_map(ctx->encode_tiled, a_codes, T, K, pa, nt, &a.ma) || !codes_map(ctx->encode_tiled, w_codes, N, K, pwgt, 128, &a.mw))
+  const int64_t pitch = ((int64_t)K + 15) / 16 * 16, out_pitch = T > 1 ? out_stride : N;
+  if (!codes_map(ctx->encode_tiled, a_codes, T, K, a_stride < pitch ? pitch : a_stride, p.bn ? 128 : p.nt, &a.ma) ||
+      !codes_map(ctx->encode_tiled, w_codes, N, K, w_stride < pitch ? pitch : w_stride, p.bn ? p.bn / 2 : 128, &a.mw))
     return PW_ERR_CUDA;
-  st = nt == 16   ? launch_few<16>(ctx, a, row_tiles, token_tiles, stream)
-       : nt == 32 ? launch_few<32>(ctx, a, row_tiles, token_tiles, stream)
-       : nt == 64 ? launch_few<64>(ctx, a, row_tiles, token_tiles, stream)
-                  : launch_few<128>(ctx, a, row_tiles, token_tiles, stream);
-  if (st == PW_OK) ctx->launches++;
-  return st;
+  // the copies of output boxes are cut at a row's end in units of 16 bytes only
+  const int size = type_size(out_type);
+  if (p.bn) a.tma_out = out_pitch * size % 16 == 0 && (int64_t)N * size % 16 == 0 && out_map(ctx->encode_tiled, out, T, N, out_pitch, out_type, &a.mo);
+  PW_CUDA_OK(p.bn == 256   ? launch_pair<256>(p, a, ctx->num_sms, stream)
+             : p.bn == 128 ? launch_pair<128>(p, a, ctx->num_sms, stream)
+             : p.nt == 16  ? launch_few<16>(p, a, ctx->num_sms, stream)
+             : p.nt == 32  ? launch_few<32>(p, a, ctx->num_sms, stream)
+                           : launch_few<64>(p, a, ctx->num_sms, stream));
+  ctx->launches++;
+  return PW_OK;
 }

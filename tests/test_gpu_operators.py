@@ -202,10 +202,22 @@ def operands(ctx, T, N, K, seed=0, pad=0):
 
 @pytest.mark.parametrize("out_type", [F32, F16, BF16])
 @pytest.mark.parametrize("T,N,K", [(1, 1, 1), (1, 8, 16), (1, 128, 128), (2, 129, 127), (7, 64, 2056), (16, 130, 384), (17, 256, 1000), (33, 200, 2048),
-                                   (64, 384, 640), (65, 127, 500), (128, 128, 4096), (129, 257, 300), (301, 64, 2056), (300, 1000, 1408)])
+                                   (64, 384, 640), (65, 127, 500), (128, 128, 4096), (129, 257, 300), (301, 64, 2056), (300, 1000, 1408),
+                                   (1030, 520, 700), (2048, 4100, 512), (1500, 4099, 300)])
 def test_product_sizes_and_types(ctx, T, N, K, out_type):
     a, sa, w, sw = operands(ctx, T, N, K, seed=T + N + K)
     out, whole = strided(T, N, 5, out_type, 7.0)
+    check_linear(ctx, a, sa, w, sw, out)
+    assert guards_left(whole, out, 7.0)
+
+
+@pytest.mark.parametrize("out_type", [F32, F16, BF16])
+@pytest.mark.parametrize("T,N,K,pad", [(70, 127, 500, 1), (200, 130, 129, 6), (200, 132, 300, 4), (300, 264, 700, 8), (300, 520, 256, 24), (129, 1032, 256, 16),
+                                       (2000, 4104, 256, 8), (2000, 4108, 256, 4), (1999, 4097, 256, 7)])
+def test_product_leaves_what_lies_between_rows(ctx, T, N, K, pad, out_type):
+    """Rows a multiple of 16 bytes apart, whose length may or may not be one."""
+    a, sa, w, sw = operands(ctx, T, N, K, seed=T + N + K)
+    out, whole = strided(T, N, pad, out_type, 7.0)
     check_linear(ctx, a, sa, w, sw, out)
     assert guards_left(whole, out, 7.0)
 
@@ -233,6 +245,22 @@ def test_product_gives_the_same_bits_again(ctx):
         first = ctx.pw_scaled_linear(a, sa, w, sw, out_dtype=F32)
         for _ in range(5):
             assert torch.equal(first, ctx.pw_scaled_linear(a, sa, w, sw, out_dtype=F32))
+
+
+@pytest.mark.parametrize("T", [1, 20, 40, 64, 300])
+def test_product_back_to_back(ctx, T):
+    """Long contractions from HBM, launch after launch: copies land out of order, stages and barriers are used many times."""
+    N, K = 4096, 14336
+    sets = [operands(ctx, T, N, K, seed=100 * i) for i in range(3)]
+    want = [ctx.pw_scaled_linear(*s, out_dtype=F32) for s in sets]
+    torch.cuda.synchronize()
+    outs = [[torch.empty_like(want[0]) for _ in range(3)] for _ in range(2)]
+    for i in range(60):
+        ctx.pw_scaled_linear(*sets[i % 3], out=outs[i % 2][i % 3])
+    torch.cuda.synchronize()
+    assert ctx.pw_last_device_status() == 0
+    for group in outs:
+        assert all(torch.equal(o, w) for o, w in zip(group, want))
 
 
 def test_product_wait_that_runs_out_is_reported():
