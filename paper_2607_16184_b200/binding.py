@@ -15,7 +15,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpw.so")
 
-PW_OK, PW_ERR_INVALID_ARG, PW_ERR_SHAPE = 0, 1, 2
+PW_OK = 0
 STATUS_NAMES = {0: "PW_OK", 1: "PW_ERR_INVALID_ARG", 2: "PW_ERR_SHAPE", 3: "PW_ERR_BITS", 4: "PW_ERR_ALIGN",
                 5: "PW_ERR_STATE", 6: "PW_ERR_NOMEM", 7: "PW_ERR_CUDA", 8: "PW_ERR_TIMEOUT"}
 PW_GATE, PW_UP, PW_DOWN = 0, 1, 2
@@ -35,10 +35,8 @@ EXPORTS = ("pw_workspace_bytes", "pw_create", "pw_destroy", "pw_page_bytes", "pw
            "pw_kernel_timing", "pw_get_kernel_times", "pw_launch_count", "pw_debug_set_wait", "pw_status_str")
 PW_F32, PW_F16, PW_BF16 = 0, 1, 2
 PW_SCORE_SOFTMAX, PW_SCORE_SIGMOID = 0, 1
-_TYPES = {torch.float32: PW_F32, torch.float16: PW_F16, torch.bfloat16: PW_BF16}
 _SCORES = {"softmax": PW_SCORE_SOFTMAX, "sigmoid": PW_SCORE_SIGMOID, PW_SCORE_SOFTMAX: PW_SCORE_SOFTMAX,
            PW_SCORE_SIGMOID: PW_SCORE_SIGMOID}
-_CODE_TYPES = (torch.float8_e4m3fn, torch.uint8)
 KERNEL_NAMES = ("router", "permute", "gather", "ffn_gate_up", "ffn_down", "combine", "observe")
 PW_OBS_FIELDS = 8
 OBS_FIELD_NAMES = ("sum_r", "pairs", "sum_r_nx", "sum_r_nx2", "max_nx", "sum_r_nh", "sum_r_nh2", "max_nh")
@@ -86,16 +84,18 @@ class pw_plan_item(C.Structure):
 
 
 _lib = None
+_pwtorch = None
 
 
 def load():
     """Loads libpw.so (built by ``paper_2607_16184_b200.build``).  Raises if it is missing."""
-    global _lib
+    global _lib, _pwtorch
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libpw.so is missing: run `python -m paper_2607_16184_b200.build` (there is no fallback path)")
     L = C.CDLL(LIB_PATH)
+    from . import _pwtorch                          # loads libpw.so next to it
     vp, i32, u32, sz = C.c_void_p, C.c_int, C.c_uint32, C.c_size_t
     L.pw_workspace_bytes.restype = sz
     L.pw_workspace_bytes.argtypes = [C.POINTER(pw_config)]
@@ -421,6 +421,7 @@ class Context:
         self.handle = C.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.L.pw_create(C.byref(self.handle), C.byref(cfg)), "pw_create")
+        self._ptr = self.handle.value                 # 0 once closed: the calls that take it then refuse
         self.n_segments = n_experts + n_shared
         self._committed = {}          # (layer, expert, kind) -> the page the row points to
         self.obs = None               # accumulators of the observation taps while they are on
@@ -435,7 +436,7 @@ class Context:
     def close(self):
         if self.handle:
             self.L.pw_destroy(self.handle)      # waits for the device: nothing reads the pages any more
-            self.handle = C.c_void_p()
+            self.handle, self._ptr = C.c_void_p(), 0
             self._committed = {}
             self.obs = None
 
@@ -581,29 +582,19 @@ class Context:
                               out: Optional[torch.Tensor] = None, mode: int = PW_MODE_AUTO,
                               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The layer call for a routing the caller has (ids [T, k], -1 = no expert; gates [T, k])."""
-        T, H = self._matrix(hidden, (torch.float16,), "hidden")
-        k = self._matrix(topk_ids, (torch.int32,), "topk_ids", T)[1]
-        self._matrix(gates, (torch.float32,), "gates", T, k)
-        if H != self.cfg.hidden or not (hidden.is_contiguous() and topk_ids.is_contiguous() and gates.is_contiguous()):
-            raise PwError(PW_ERR_SHAPE, "pw_moe_forward_routed: hidden [T, H], ids and gates [T, k], contiguous")
         if out is None:
-            out = self._new(stream, lambda: torch.empty(T, H, dtype=torch.float32, device=self.device))
-        if self._matrix(out, (torch.float32,), "out", T, H) and not out.is_contiguous():
-            raise PwError(PW_ERR_SHAPE, "pw_moe_forward_routed: out [T, H] contiguous")
-        self._call(self.L.pw_moe_forward_routed, "pw_moe_forward_routed", stream, layer, hidden.data_ptr(), topk_ids.data_ptr(),
-                   gates.data_ptr(), T, k, None, out.data_ptr(), mode)
+            out = self._new(stream, lambda: torch.empty(hidden.shape, dtype=torch.float32, device=self.device))
+        st = _pwtorch.moe_forward_routed(self._ptr, self._index, None if stream is None else stream.cuda_stream, layer, hidden, topk_ids,
+                                         gates, out, mode, self.cfg.hidden)
+        if st:
+            self._refused(st, "pw_moe_forward_routed", ("layer", "hidden", "topk_ids", "gates", "out"))
         return out
 
     # ---- around the layer ----
-    def _call(self, fn, where: str, stream: Optional[torch.cuda.Stream], *args):
-        """One C call with this context's device current, on ``stream`` (default: the device's current stream)."""
-        if torch.cuda.current_device() != self._index:
-            with torch.cuda.device(self._index):
-                return self._call(fn, where, stream, *args)
-        s = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
-        st = fn(self.handle, *args, s)
-        if st != PW_OK:
-            raise PwError(st, where)
+    # Tensors are checked and handed on by _pwtorch (csrc/pw_torch.cpp), with this context's device current and on
+    # ``stream`` (default: the device's current stream).  Row strides are free, columns must be contiguous.
+    def _refused(self, status: int, where: str, names: Sequence[str]):
+        raise PwError(status & 255, "%s (%s)" % (where, names[(status >> 8) - 1]) if status >> 8 else where)
 
     def _new(self, stream: Optional[torch.cuda.Stream], make):
         """An output tensor from the pool of the stream the kernel will run on."""
@@ -612,33 +603,15 @@ class Context:
         with torch.cuda.stream(stream):
             return make()
 
-    def _matrix(self, t: torch.Tensor, types, name: str, rows: int = -1, cols: int = -1) -> Tuple[int, int]:
-        """Shape of a 2-D tensor on this context's device whose rows are contiguous; raises otherwise."""
-        if t.dtype not in types or t.get_device() != self._index:
-            raise PwError(PW_ERR_INVALID_ARG, "%s (%s on %s)" % (name, t.dtype, t.device))
-        if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (rows >= 0 and t.shape[0] != rows) or (cols >= 0 and t.shape[1] != cols):
-            raise PwError(PW_ERR_SHAPE, "%s %s with strides %s" % (name, tuple(t.shape), t.stride()))
-        return t.shape[0], t.shape[1]
-
-    def _scales(self, t: torch.Tensor, rows: int, cols: int, block_rows: int, name: str):
-        if t.dtype != torch.float32 or t.get_device() != self._index:
-            raise PwError(PW_ERR_INVALID_ARG, "%s (%s on %s)" % (name, t.dtype, t.device))
-        if tuple(t.shape) != ((rows + block_rows - 1) // block_rows, (cols + GROUP - 1) // GROUP) or not t.is_contiguous():
-            raise PwError(PW_ERR_SHAPE, "%s %s" % (name, tuple(t.shape)))
-
     def pw_quantize_scaled(self, x: torch.Tensor, block_rows: int, q: Optional[torch.Tensor] = None,
                            scales: Optional[torch.Tensor] = None,
                            stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(codes, scales) of a matrix in the scaled 8-bit format; block_rows 1 (activations) or 128 (weights)."""
-        rows, cols = self._matrix(x, _TYPES, "x")
-        if block_rows not in (1, GROUP) or (q is None) != (scales is None):
-            raise PwError(PW_ERR_INVALID_ARG, "pw_quantize_scaled")
-        if q is None:
-            q, scales = self._new(stream, lambda: scaled_empty(rows, cols, block_rows, self.device))
-        self._matrix(q, _CODE_TYPES, "q", rows, cols)
-        self._scales(scales, rows, cols, block_rows, "scales")
-        self._call(self.L.pw_quantize_scaled, "pw_quantize_scaled", stream, x.data_ptr(), _TYPES[x.dtype], rows, cols, x.stride(0),
-                   block_rows, q.data_ptr(), q.stride(0), scales.data_ptr())
+        if q is None and scales is None and x.dim() == 2 and block_rows > 0:
+            q, scales = self._new(stream, lambda: scaled_empty(x.shape[0], x.shape[1], block_rows, self.device))
+        st = _pwtorch.quantize_scaled(self._ptr, self._index, None if stream is None else stream.cuda_stream, x, block_rows, q, scales)
+        if st:
+            self._refused(st, "pw_quantize_scaled", ("x", "block_rows", "q", "scales"))
         return q, scales
 
     def pw_add_rmsnorm(self, x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
@@ -648,81 +621,40 @@ class Context:
         """s = x + residual; y = s * weight / sqrt(mean(s^2) + eps).  Writes the outputs it is given (residual_out: s,
         y, and the scaled 8-bit copy of y in q, q_scales) and returns (residual_out, y, q, q_scales); without y and q
         it makes an fp16 y."""
-        T, H = self._matrix(x, _TYPES, "x")
-        if weight.dtype not in _TYPES or weight.get_device() != self._index:
-            raise PwError(PW_ERR_INVALID_ARG, "weight (%s on %s)" % (weight.dtype, weight.device))
-        if weight.dim() != 1 or weight.shape[0] != H or not weight.is_contiguous():
-            raise PwError(PW_ERR_SHAPE, "weight %s" % (tuple(weight.shape),))
         if y is None and q is None:
-            y = self._new(stream, lambda: torch.empty(T, H, dtype=torch.float16, device=self.device))
-        if (q is None) != (q_scales is None) or (residual is None and residual_out is not None):
-            raise PwError(PW_ERR_INVALID_ARG, "pw_add_rmsnorm: q with q_scales, residual_out with residual")
-        args = [T, H, x.data_ptr(), _TYPES[x.dtype], x.stride(0)]
-        if residual is None:
-            args += (None, 0, 0)
-        else:
-            self._matrix(residual, _TYPES, "residual", T, H)
-            args += (residual.data_ptr(), _TYPES[residual.dtype], residual.stride(0))
-        args += (weight.data_ptr(), _TYPES[weight.dtype], eps)
-        if residual_out is None:
-            args += (None, 0)
-        else:
-            self._matrix(residual_out, (residual.dtype,), "residual_out", T, H)
-            args += (residual_out.data_ptr(), residual_out.stride(0))
-        if y is None:
-            args += (None, 0, 0)
-        else:
-            self._matrix(y, _TYPES, "y", T, H)
-            args += (y.data_ptr(), _TYPES[y.dtype], y.stride(0))
-        if q is None:
-            args += (None, 0, None)
-        else:
-            self._matrix(q, _CODE_TYPES, "q", T, H)
-            self._scales(q_scales, T, H, 1, "q_scales")
-            args += (q.data_ptr(), q.stride(0), q_scales.data_ptr())
-        self._call(self.L.pw_add_rmsnorm, "pw_add_rmsnorm", stream, *args)
+            y = self._new(stream, lambda: torch.empty(x.shape, dtype=torch.float16, device=self.device))
+        st = _pwtorch.add_rmsnorm(self._ptr, self._index, None if stream is None else stream.cuda_stream, x, weight, eps, residual,
+                                  residual_out, y, q, q_scales)
+        if st:
+            self._refused(st, "pw_add_rmsnorm", ("x", "weight", "eps", "residual", "residual_out", "y", "q", "q_scales"))
         return residual_out, y, q, q_scales
 
     def pw_scaled_linear(self, a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor,
                          out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float16,
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """out [T, N] = a [T, K] . w [N, K]^T, both in the scaled 8-bit format (a: block_rows 1, w: block_rows 128)."""
-        T, K = self._matrix(a, _CODE_TYPES, "a")
-        N, _ = self._matrix(w, _CODE_TYPES, "w", -1, K)
-        self._scales(a_scales, T, K, 1, "a_scales")
-        self._scales(w_scales, N, K, GROUP, "w_scales")
         if out is None:
-            if out_dtype not in _TYPES:
-                raise PwError(PW_ERR_INVALID_ARG, "out_dtype %s" % (out_dtype,))
-            out = self._new(stream, lambda: torch.empty(T, N, dtype=out_dtype, device=self.device))
-        self._matrix(out, _TYPES, "out", T, N)
-        self._call(self.L.pw_scaled_linear, "pw_scaled_linear", stream, T, N, K, a.data_ptr(), a.stride(0), a_scales.data_ptr(),
-                   w.data_ptr(), w.stride(0), w_scales.data_ptr(), out.data_ptr(), _TYPES[out.dtype], out.stride(0))
+            out = self._new(stream, lambda: torch.empty(a.shape[0], w.shape[0], dtype=out_dtype, device=self.device))
+        st = _pwtorch.scaled_linear(self._ptr, self._index, None if stream is None else stream.cuda_stream, a, a_scales, w, w_scales, out)
+        if st:
+            self._refused(st, "pw_scaled_linear", ("a", "a_scales", "w", "w_scales", "out"))
         return out
 
     def pw_route_tokens(self, router_logits: torch.Tensor, top_k: int, score="softmax", bias: Optional[torch.Tensor] = None,
                         n_groups: int = 1, top_groups: int = 1, group_best: int = 1, renormalize: bool = True,
                         scale: float = 1.0, ids: Optional[torch.Tensor] = None, gates: Optional[torch.Tensor] = None,
                         stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-        """(ids int32 [T, k], gates fp32 [T, k]) by the rule described at pw_route_tokens in include/pw.h."""
-        T, E = self._matrix(router_logits, _TYPES, "router_logits")
-        if score not in _SCORES or (ids is None) != (gates is None) or not 1 <= top_k <= 32:
-            raise PwError(PW_ERR_INVALID_ARG, "pw_route_tokens")
-        if bias is not None:
-            if bias.dtype != torch.float32 or bias.get_device() != self._index:
-                raise PwError(PW_ERR_INVALID_ARG, "bias (%s on %s)" % (bias.dtype, bias.device))
-            if tuple(bias.shape) != (E,) or not bias.is_contiguous():
-                raise PwError(PW_ERR_SHAPE, "bias %s" % (tuple(bias.shape),))
-        if ids is None:
-            ids, gates = self._new(stream, lambda: (torch.empty(T, top_k, dtype=torch.int32, device=self.device),
-                                                    torch.empty(T, top_k, dtype=torch.float32, device=self.device)))
-        self._matrix(ids, (torch.int32,), "ids", T, top_k)
-        self._matrix(gates, (torch.float32,), "gates", T, top_k)
-        if not (ids.is_contiguous() and gates.is_contiguous()):
-            raise PwError(PW_ERR_SHAPE, "pw_route_tokens: ids and gates contiguous")
-        rule = pw_routing(E, top_k, _SCORES[score], n_groups, top_groups, group_best, 1 if renormalize else 0, scale)
-        self._call(self.L.pw_route_tokens, "pw_route_tokens", stream, C.byref(rule), router_logits.data_ptr(), _TYPES[router_logits.dtype],
-                   router_logits.stride(0), None if bias is None else bias.data_ptr(), T, ids.data_ptr(), gates.data_ptr())
+        """(ids int32 [T, k], gates fp32 [T, k]) by the rule described at pw_route_tokens in include/pw.h; score is
+        "softmax", "sigmoid" or a PW_SCORE_* value."""
+        if ids is None and gates is None and top_k > 0:
+            shape = (router_logits.shape[0], top_k)
+            ids, gates = self._new(stream, lambda: (torch.empty(shape, dtype=torch.int32, device=self.device),
+                                                    torch.empty(shape, dtype=torch.float32, device=self.device)))
+        st = _pwtorch.route_tokens(self._ptr, self._index, None if stream is None else stream.cuda_stream, router_logits, top_k,
+                                   _SCORES.get(score, -1), bias, n_groups, top_groups, group_best, renormalize, scale, ids, gates)
+        if st:
+            self._refused(st, "pw_route_tokens", ("router_logits", "top_k", "score", "bias", "n_groups", "top_groups", "group_best",
+                                                  "renormalize", "scale", "ids", "gates"))
         return ids, gates
 
     def pw_moe_forward_host(self, layer: int, hidden_host: torch.Tensor, logits_host: torch.Tensor, top_k: int,

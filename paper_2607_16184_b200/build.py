@@ -5,10 +5,13 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpw.so")
+MODULE = os.path.join(HERE, "_pwtorch.so")         # argument marshalling for torch tensors
+MODULE_SOURCE = os.path.join(CSRC, "pw_torch.cpp")
 
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a", "-Xcompiler", "-fPIC",
               "-shared", "-cudart", "static"]
@@ -26,8 +29,24 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_module(force: bool = False) -> str:
+    """The CPython module that marshals torch tensors for the calls of libpw.so."""
+    deps = (MODULE_SOURCE, os.path.join(HERE, "..", "include", "pw.h"))
+    if not force and os.path.exists(MODULE) and all(os.path.getmtime(d) <= os.path.getmtime(MODULE) for d in deps):
+        return MODULE
+    import torch
+    from torch.utils import cpp_extension
+    dirs = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch.compiled_with_cxx11_abi())] +
+                          ["-I" + d for d in dirs] + [MODULE_SOURCE, "-o", MODULE, "-L" + libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L" + HERE, "-l:libpw.so",
+                                                      "-Wl,-rpath,$ORIGIN"])
+    return MODULE
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
+        build_module()
         return LIB
     objs = []
     procs = []
@@ -47,6 +66,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         raise RuntimeError("nvcc failed")
     subprocess.check_call(["nvcc", "-shared", "-cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a",
                            "-o", LIB] + objs)
+    build_module(force)
     return LIB
 
 
