@@ -369,8 +369,8 @@ pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const void* a_codes
  *   key      p + bias (bias: device [n_experts] fp32 or NULL; it balances the choice and does not enter the gates)
  *   groups   n_groups equal ranges of experts; only experts of the top_groups best groups can be chosen.  A group's
  *            score is its best key (group_best 1) or the sum of its best two (group_best 2)
- *   choice   the top_k largest keys, largest first; equal keys (and groups): lower index first.  Keys are compared in
- *            64 bits; without a bias and without sums of two their order is that of the logits.
+ *   choice   the top_k largest keys, largest first; equal keys (and groups): lower index first.  Decided as in 64 bits;
+ *            without a bias the order of the experts is that of the logits.
  *   gate     p, divided by the sum of the chosen p with renormalize (0 where that sum is 0), times scale
  * A logit of -infinity or NaN masks its expert: it is never chosen, has no part in the softmax or in its group's score
  * (a group without any other expert comes last).  +infinity counts as the largest finite number.  A row with fewer

@@ -240,73 +240,70 @@ struct QuantArgs {
   int rows, cols;
 };
 
-// Blocks of one row: a warp takes 256 columns of a row at a time (two groups), U such pieces in flight.
+// Blocks of one row: a warp takes 1024 columns of a row (U pieces of two groups), all loaded before the first is used.
 template <class TX, bool VEC>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a) {
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a, uint32_t units, uint32_t per_row) {
   grid_dep_sync();
   grid_dep_trigger();
   constexpr int U = 4;
   const int lane = threadIdx.x & 31;
-  const int G = (a.cols + kGroup - 1) / kGroup, P = (G + 1) / 2;
-  const int64_t total = (int64_t)a.rows * P;
-  const int64_t step = (int64_t)gridDim.x * 8 * U;
-  for (int64_t u0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * U; u0 < total; u0 += step) {
-    float z[U][8];
-    Raw8<TX> raw[U];
-    int64_t row[U];
-    int c0[U];
+  const int G = (a.cols + kGroup - 1) / kGroup;
+  for (uint32_t unit = blockIdx.x * 8 + (threadIdx.x >> 5); unit < units; unit += gridDim.x * 8) {
+    const uint32_t row = unit / per_row;
+    const int c0 = (int)(unit - row * per_row) * 256 * U;
+    const TX* x = static_cast<const TX*>(a.x) + row * a.x_stride;
+    uint8_t* q = a.q + row * a.q_stride;
+    float* qs = a.scales + (int64_t)row * G;
+    if constexpr (VEC) {
+      Raw8<TX> raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t un = u0 + u;
-      row[u] = un / P;
-      c0[u] = un < total ? (int)(un - row[u] * P) * 256 : a.cols;      // past the end: every column is out of range
-      const TX* x = static_cast<const TX*>(a.x) + row[u] * a.x_stride;
-      if constexpr (VEC) {
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * 256 + lane * 8;
         raw[u].zero();
-        if (c0[u] + lane * 8 < a.cols) raw[u].load(x + c0[u] + lane * 8);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int c = c0[u] + j * 32 + lane;
-          z[u][j] = c < a.cols ? to_f32(x[c]) : 0.f;
-        }
+        if (c < a.cols) raw[u].load(x + c);
       }
-    }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      uint8_t* q = a.q + row[u] * a.q_stride;
-      float* qs = a.scales + row[u] * G;
-      if constexpr (VEC) {
-        raw[u].get(z[u]);
+      for (int u = 0; u < U; ++u) {
+        float z[8];
+        raw[u].get(z);
         float top = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = abs_max(top, z[u][j]);
+        for (int j = 0; j < 8; ++j) top = abs_max(top, z[j]);
 #pragma unroll
         for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         const float scale = block_scale(top), rinv = __frcp_rn(scale);
-        const int c = c0[u] + lane * 8;
+        const int c = c0 + u * 256 + lane * 8;
         if (c >= a.cols) continue;
         if ((lane & 15) == 0) qs[c / kGroup] = scale;
         uint2 o;
-        o.x = pack_e4m3(z[u][0] * rinv, z[u][1] * rinv) | (pack_e4m3(z[u][2] * rinv, z[u][3] * rinv) << 16);
-        o.y = pack_e4m3(z[u][4] * rinv, z[u][5] * rinv) | (pack_e4m3(z[u][6] * rinv, z[u][7] * rinv) << 16);
+        o.x = pack_e4m3(z[0] * rinv, z[1] * rinv) | (pack_e4m3(z[2] * rinv, z[3] * rinv) << 16);
+        o.y = pack_e4m3(z[4] * rinv, z[5] * rinv) | (pack_e4m3(z[6] * rinv, z[7] * rinv) << 16);
         *reinterpret_cast<uint2*>(q + c) = o;
-      } else {
+      }
+    } else {
+      TX raw[U * 8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float top = 0.f;
+      for (int i = 0; i < U * 8; ++i) {
+        const int c = c0 + i * 32 + lane;
+        raw[i] = c < a.cols ? x[c] : (TX)0.f;
+      }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) top = abs_max(top, z[u][4 * h + j]);
+      for (int h = 0; h < U * 2; ++h) {            // groups
+        float z[4], top = 0.f;
 #pragma unroll
-          for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-          const float scale = block_scale(top), rinv = __frcp_rn(scale);
-          const int c = c0[u] + h * kGroup;
-          if (lane == 0 && c < a.cols) qs[c / kGroup] = scale;
+        for (int j = 0; j < 4; ++j) {
+          z[j] = to_f32(raw[h * 4 + j]);
+          top = abs_max(top, z[j]);
+        }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int cj = c + j * 32 + lane;
-            if (cj < a.cols) q[cj] = (uint8_t)pack_e4m3(z[u][4 * h + j] * rinv, 0.f);
-          }
+        for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float scale = block_scale(top), rinv = __frcp_rn(scale);
+        const int c = c0 + h * kGroup;
+        if (lane == 0 && c < a.cols) qs[c / kGroup] = scale;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int cj = c + j * 32 + lane;
+          if (cj < a.cols) q[cj] = (uint8_t)pack_e4m3(z[j] * rinv, 0.f);
         }
       }
     }
@@ -328,7 +325,19 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantArgs a)
   const int64_t r0 = rb * kTileRows;
   const int c0 = g * kGroup;
   const TX* x = static_cast<const TX*>(a.x);
-  float z[8][8];
+  // (the elements are kept as they were loaded and converted twice: fewer registers, twice as many CTAs on an SM)
+  float top = 0.f;
+  auto scale_of_block = [&](float m) {
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    if (lane == 0) part[warp] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, part[i]);
+    const float scale = block_scale(m);
+    if (tid == 0) a.scales[rb * G + g] = scale;
+    return __frcp_rn(scale);
+  };
   if constexpr (VEC) {
     Raw8<TX> raw[8];
     const int c = c0 + (lane & 15) * 8;
@@ -339,50 +348,43 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantArgs a)
       if (r < a.rows && c < a.cols) raw[p].load(x + r * a.x_stride + c);
     }
 #pragma unroll
-    for (int p = 0; p < 8; ++p) raw[p].get(z[p]);
-  } else {
+    for (int p = 0; p < 8; ++p) {
+      float z[8];
+      raw[p].get(z);
 #pragma unroll
-    for (int p = 0; p < 16; ++p)
+      for (int j = 0; j < 8; ++j) top = abs_max(top, z[j]);
+    }
+    const float rinv = scale_of_block(top);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t r = r0 + p * 8 + warp;
-        const int c = c0 + j * 32 + lane;
-        z[p >> 1][(p & 1) * 4 + j] = r < a.rows && c < a.cols ? to_f32(x[r * a.x_stride + c]) : 0.f;
-      }
-  }
-  float top = 0.f;
-#pragma unroll
-  for (int p = 0; p < 8; ++p)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = abs_max(top, z[p][j]);
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  if (lane == 0) part[warp] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, part[i]);
-  const float scale = block_scale(top), rinv = __frcp_rn(scale);
-  if (tid == 0) a.scales[rb * G + g] = scale;
-  if constexpr (VEC) {
-    const int c = c0 + (lane & 15) * 8;
+    for (int p = 0; p < 8; ++p) raw[p].forget();
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
       const int64_t r = r0 + p * 16 + (tid >> 4);
       if (r >= a.rows || c >= a.cols) continue;
+      float z[8];
+      raw[p].get(z);
       uint2 o;
-      o.x = pack_e4m3(z[p][0] * rinv, z[p][1] * rinv) | (pack_e4m3(z[p][2] * rinv, z[p][3] * rinv) << 16);
-      o.y = pack_e4m3(z[p][4] * rinv, z[p][5] * rinv) | (pack_e4m3(z[p][6] * rinv, z[p][7] * rinv) << 16);
+      o.x = pack_e4m3(z[0] * rinv, z[1] * rinv) | (pack_e4m3(z[2] * rinv, z[3] * rinv) << 16);
+      o.y = pack_e4m3(z[4] * rinv, z[5] * rinv) | (pack_e4m3(z[6] * rinv, z[7] * rinv) << 16);
       *reinterpret_cast<uint2*>(a.q + r * a.q_stride + c) = o;
     }
   } else {
+    TX raw[64];
 #pragma unroll
-    for (int p = 0; p < 16; ++p)
+    for (int i = 0; i < 64; ++i) {
+      const int64_t r = r0 + (i >> 2) * 8 + warp;
+      const int c = c0 + (i & 3) * 32 + lane;
+      raw[i] = r < a.rows && c < a.cols ? x[r * a.x_stride + c] : (TX)0.f;
+    }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t r = r0 + p * 8 + warp;
-        const int c = c0 + j * 32 + lane;
-        if (r < a.rows && c < a.cols) a.q[r * a.q_stride + c] = (uint8_t)pack_e4m3(z[p >> 1][(p & 1) * 4 + j] * rinv, 0.f);
-      }
+    for (int i = 0; i < 64; ++i) top = abs_max(top, to_f32(raw[i]));
+    const float rinv = scale_of_block(top);
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+      const int64_t r = r0 + (i >> 2) * 8 + warp;
+      const int c = c0 + (i & 3) * 32 + lane;
+      if (r < a.rows && c < a.cols) a.q[r * a.q_stride + c] = (uint8_t)pack_e4m3(to_f32(raw[i]) * rinv, 0.f);
+    }
   }
 }
 
@@ -390,10 +392,11 @@ template <class TX>
 static pw_status launch_quant(const QuantArgs& a, int block_rows, bool vec, int num_sms, cudaStream_t s) {
   const int64_t G = (a.cols + kGroup - 1) / kGroup;
   if (block_rows == 1) {
-    const int64_t pieces = (int64_t)a.rows * ((G + 1) / 2), ctas = (pieces + 31) / 32;
-    const int64_t cap = (int64_t)num_sms * 64;
+    const uint32_t per_row = (uint32_t)((G + 7) / 8);
+    const int64_t units = (int64_t)a.rows * per_row, ctas = (units + 7) / 8, cap = (int64_t)num_sms * 64;
+    if (units > 0x7fffffff) return PW_ERR_SHAPE;
     PW_CUDA_OK(launch_dependent(vec ? quantize_rows_kernel<TX, true> : quantize_rows_kernel<TX, false>,
-                                dim3((unsigned)(ctas < cap ? ctas : cap)), dim3(256), 0, s, a));
+                                dim3((unsigned)(ctas < cap ? ctas : cap)), dim3(256), 0, s, a, (uint32_t)units, per_row));
   } else {
     const int64_t ctas = ((int64_t)a.rows + kTileRows - 1) / kTileRows * G;
     if (ctas > 0x7fffffff) return PW_ERR_SHAPE;

@@ -49,6 +49,8 @@ struct Raw8 {
   uint4 a;
   __device__ __forceinline__ void load(const T* p) { a = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+  // keeps the compiler from holding on to values it has converted before
+  __device__ __forceinline__ void forget() { asm volatile("" : "+r"(a.x), "+r"(a.y), "+r"(a.z), "+r"(a.w)); }
   __device__ __forceinline__ void get(float* v) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -72,6 +74,7 @@ struct Raw8<float> {
     b = reinterpret_cast<const float4*>(p)[1];
   }
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void forget() {}
   __device__ __forceinline__ void get(float* v) const {
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
     v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;

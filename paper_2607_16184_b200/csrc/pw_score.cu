@@ -2,10 +2,12 @@
 //
 //   p = softmax(l) or 1 / (1 + exp(-l))      key = p + bias      gate = p [/ sum of the chosen p] * scale
 //
-// One warp per token, expert e in lane e mod 32.  A row of logits is read once and 8 k bytes are written per token:
-// launch, one round trip to memory and the chain of k selections bound it.  Which of two near scores is larger decides
-// whole numbers, so the order is exact where it can be: without a bias and without sums of scores the keys are the
-// logits themselves (both scores grow with the logit); otherwise p and the key are computed in 64 bits.
+// One warp per token, expert e in lane e mod 32.  A row of logits is read once and 8 k bytes are written per token: a
+// batch of a few hundred tokens costs a launch and one round trip to memory, a long prompt the instructions of the
+// selections.  Which of two near scores is larger decides whole numbers, so the choice has to be that of exact keys:
+// without a bias the keys are the logits themselves (both scores grow with the logit); otherwise they are computed in
+// 32 bits together with a bound of their error, and a token for which two keys that decide anything are closer than that
+// is done again in 64 bits (4096 tokens x 256 experts in 8 groups, everything in 64 bits: 28.4 us).
 #include "pw_scaled.cuh"
 
 namespace pw {
@@ -20,6 +22,8 @@ struct RouteArgs {
   float* gates;
   int64_t stride;
   int T, E, k, type, sigmoid, groups, top_groups, group_best, renorm;
+  int group_strides;
+  uint32_t per_inverse;
   float scale;
 };
 
@@ -35,6 +39,7 @@ __device__ __forceinline__ uint64_t ordered(double v) {
 __device__ __forceinline__ double from_ordered(uint64_t u) {
   return __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u));
 }
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 __device__ __forceinline__ uint32_t warp_max_key(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
 __device__ __forceinline__ uint64_t warp_max_key(uint64_t v) {
   const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32));
@@ -54,156 +59,289 @@ __device__ __forceinline__ K warp_best(const K* key, int lane, int* expert) {
       at = lane + 32 * i;
     }
   const K top = warp_max_key(best);
-  *expert = (int)__reduce_min_sync(0xffffffffu, best == top ? (uint32_t)at : 0xffffffffu);
+  const uint32_t holders = __ballot_sync(0xffffffffu, best == top);
+  if ((holders & (holders - 1)) == 0) *expert = __shfl_sync(0xffffffffu, at, __ffs((int)holders) - 1);
+  else *expert = (int)__reduce_min_sync(0xffffffffu, best == top ? (uint32_t)at : 0xffffffffu);
   return top;
 }
+// What the choice of one token needs beyond its keys.
+struct Chooser {
+  int groups, top_groups, group_best, k, lane;
+  int strides;                    // 32-expert strides of a group, 0 where groups do not consist of whole ones
+  uint32_t per_inverse;           // e / (experts of a group) = e * per_inverse >> 32 for every e < 256; 0: groups of one
+  __device__ __forceinline__ int group_of(int e) const { return per_inverse ? (int)__umulhi((uint32_t)e, per_inverse) : e; }
+};
 
-// NS = 32-expert strides a lane holds; WIDE: keys in 64 bits.
-template <int NS, bool WIDE>
-__global__ void __launch_bounds__(256) score_kernel(const RouteArgs a) {
-  using K = typename std::conditional<WIDE, uint64_t, uint32_t>::type;
+// The experts of slots 0 .. k - 1 and their keys (slot j in lane j; -1: none left).  `score(first, second)`: a group's score, as a key,
+// of its two best keys.  `far(a, b)`: whether a is larger than the next key b beyond doubt; the function returns false
+// when a decision was not.  `far_groups` the same for scores of groups.
+template <int NS, bool GROUPS, class K, class Score, class Far, class FarGroups>
+__device__ __forceinline__ bool choose(const Chooser& c, K* key, Score score, Far far, FarGroups far_groups, int* slot, K* slot_key) {
+  bool sure = true;
+  if (GROUPS && c.groups > 1) {
+    K mine[NS];                                   // scores of the groups lane, lane + 32, ..
+    int group[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) group[i] = c.group_of(c.lane + 32 * i);
+    if (c.strides) {
+      // groups of whole strides: a lane's keys of a group are known without looking
+      K b1 = 0, b2 = 0;
+      int g = 0, left = c.strides;
+      mine[0] = 0;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const K k = key[i];
+        b2 = k > b1 ? b1 : k > b2 ? k : b2;
+        b1 = k > b1 ? k : b1;
+        if (--left == 0) {
+          const K first = warp_max_key(b1);
+          const uint32_t holders = __ballot_sync(0xffffffffu, b1 == first);
+          const K second = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
+          if (c.lane == g && first) mine[0] = score(first, second);
+          ++g;
+          left = c.strides;
+          b1 = b2 = 0;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) mine[i] = 0;
+      for (int g = 0; g < c.groups; ++g) {
+        K b1 = 0, b2 = 0;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const K k = group[i] == g ? key[i] : (K)0;
+          b2 = k > b1 ? b1 : k > b2 ? k : b2;
+          b1 = k > b1 ? k : b1;
+        }
+        const K first = warp_max_key(b1);
+        const uint32_t holders = __ballot_sync(0xffffffffu, b1 == first);
+        const K second = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
+        if (c.lane == (g & 31) && first) {
+          const K s = score(first, second);
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+            if ((g >> 5) == i) mine[i] = s;
+        }
+      }
+    }
+    K last = 0, next = 0;
+    uint32_t keep = 0;                            // bit i: the group of my expert i stays
+    for (int j = 0; j <= c.top_groups; ++j) {     // one more than is kept: the best that is not
+      int g;
+      next = c.groups <= 32 ? warp_best<1>(mine, c.lane, &g) : warp_best<NS>(mine, c.lane, &g);
+      if (!next || j == c.top_groups) break;      // only groups without an expert are left, or enough
+      last = next;
+      if (c.groups <= 32) {
+        if (c.lane == g) mine[0] = 0;
+      } else {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+          if (c.lane + 32 * i == g) mine[i] = 0;
+      }
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+        if (group[i] == g) keep |= 1u << i;
+    }
+    if (next && !far_groups(last, next)) sure = false;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (!((keep >> i) & 1u)) key[i] = 0;
+  }
+  *slot = -1;
+  K last = 0;
+  for (int j = 0; j <= c.k; ++j) {                // one more than is taken: the first that is not
+    int e;
+    const K best = warp_best<NS>(key, c.lane, &e);
+    if (!best) break;
+    if (j > 0 && !far(last, best)) sure = false;
+    if (j == c.k) break;
+    last = best;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (c.lane + 32 * i == e) key[i] = 0;
+    if (c.lane == j) {
+      *slot = e;
+      *slot_key = best;
+    }
+  }
+  return sure;
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+  return v;
+}
+template <class F>
+__device__ __forceinline__ F warp_sum(F v) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+
+// A token's logits: masked ones (NaN too) -infinity, +infinity as the largest number, -0 as +0.
+__device__ __forceinline__ float tidy(float v) { return v > -INFINITY ? fminf(v, 3.402823466e38f) + 0.f : -INFINITY; }
+template <int NS>
+__device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int lane, float* l) {
+  auto row = [&](auto* p) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int e = lane + 32 * i;
+      l[i] = e < a.E ? to_f32(p[e]) : -INFINITY;
+    }
+  };
+  if (a.type == PW_F32) row(static_cast<const float*>(a.logits) + t * a.stride);
+  else if (a.type == PW_F16) row(static_cast<const __half*>(a.logits) + t * a.stride);
+  else row(static_cast<const __nv_bfloat16*>(a.logits) + t * a.stride);
+#pragma unroll
+  for (int i = 0; i < NS; ++i) l[i] = tidy(l[i]);
+}
+
+// The choice with everything in 64 bits.
+template <int NS>
+__device__ __noinline__ int choose_exactly(const RouteArgs& a, int64_t t, const Chooser& c, float top) {
+  float l[NS];
+  load_logits<NS>(a, t, c.lane, l);
+  double total = 0.0;
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (l[i] > -INFINITY && !a.sigmoid) total += exp((double)l[i] - (double)top);
+  total = warp_sum(total);
+  auto p_of = [&](double v) { return a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - (double)top) / total; };
+  uint64_t key[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const int e = c.lane + 32 * i;
+    double v = l[i];
+    if (a.bias && l[i] > -INFINITY && e < a.E) v = p_of(v) + (double)a.bias[e];
+    key[i] = l[i] > -INFINITY && v > -INFINITY ? ordered(v + 0.0) : 0ull;
+  }
+  int slot;
+  uint64_t slot_key;
+  auto always = [](uint64_t, uint64_t) { return true; };
+  choose<NS, true>(c, key, [&](uint64_t first, uint64_t second) {
+    if (c.group_best == 1 || (!second && a.bias)) return first;
+    const double u = from_ordered(first), v = from_ordered(second);
+    return ordered((a.bias ? u + v : second ? p_of(u) + p_of(v) : p_of(u)) + 0.0);
+  }, always, always, &slot, &slot_key);
+  return slot;
+}
+
+// NS = 32-expert strides a lane holds.  PLAIN: no bias and no groups, nothing but the logits decides (a program a third
+// as long: one token 1.9 us instead of 2.4, most of it instructions on their way to the SM).
+template <int NS, bool PLAIN>
+__global__ void __launch_bounds__(128) score_kernel(const __grid_constant__ RouteArgs a) {
   grid_dep_sync();
   grid_dep_trigger();
   const int64_t t = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (t >= a.T) return;
   float l[NS];
-  K key[NS];
-#pragma unroll
-  for (int i = 0; i < NS; ++i) {
-    const int e = lane + 32 * i;
-    float v = e < a.E ? load1(a.logits, t * a.stride + e, a.type) : -INFINITY;
-    if (!(v > -INFINITY)) v = -INFINITY;          // NaN counts as masked
-    l[i] = fminf(v, 3.402823466e38f) + 0.f;       // +infinity as the largest number; -0 as +0
-  }
-  float top = -INFINITY;
-  double total = 1.0;                             // softmax: sum of exp(l - top) over the experts that are not masked
+  load_logits<NS>(a, t, lane, l);
+  const Chooser c{a.groups, a.top_groups, a.group_best, a.k, lane, a.group_strides, a.per_inverse};
+  // softmax: the largest logit, and the sum of exp(l - top) where something needs it
+  float top = -INFINITY, total = 1.f;
   if (!a.sigmoid) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) top = fmaxf(top, l[i]);
+    top = warp_max(top);
+    if (!a.renorm || (!PLAIN && (a.bias || a.groups > 1))) {
+      total = 0.f;
 #pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      for (int i = 0; i < NS; ++i) total += l[i] > -INFINITY ? expf(l[i] - top) : 0.f;
+      total = warp_sum(total);
+    }
   }
-  if (WIDE) {
-    double p[NS];
-    double sum = 0.0;
+  int my_id;
+  uint32_t my_key = 0;
+  if constexpr (PLAIN) {
+    uint32_t key[NS];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      p[i] = l[i] > -INFINITY ? (a.sigmoid ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - (double)top)) : 0.0;
-      sum += p[i];
-    }
-    if (!a.sigmoid) {
-#pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      total = sum;
-    }
+    for (int i = 0; i < NS; ++i) key[i] = l[i] > -INFINITY ? ordered(l[i]) : 0u;
+    auto always = [](uint32_t, uint32_t) { return true; };
+    choose<NS, false>(c, key, [](uint32_t first, uint32_t) { return first; }, always, always, &my_id, &my_key);
+  } else {
+    auto p_of = [&](float v) { return a.sigmoid ? __fdividef(1.f, 1.f + __expf(-v)) : __fdividef(__expf(v - top), total); };
+    // Error of p in 32 bits, in half steps of 1: the fast exponential 4 and its argument's two roundings 0.37 * 2 (their
+    // effect on d e^-d), the same and the 13 additions of the denominator, the fast division 4: below 32.  With the bias's
+    // addition a key is off by less than (32 + |key|) half steps; two keys decide when they are further apart than both
+    // errors together.
+    constexpr float kHalfStep = 5.9604645e-8f;
+    uint32_t key[NS];
+    float size = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       const int e = lane + 32 * i;
-      const double b = a.bias && e < a.E ? (double)a.bias[e] : 0.0;
-      const double v = p[i] / total + b;
-      key[i] = l[i] > -INFINITY && v > -INFINITY ? (K)ordered(v + 0.0) : (K)0;
+      float v = l[i];
+      if (a.bias && v > -INFINITY && e < a.E) {
+        v = p_of(v) + a.bias[e];
+        if (!(v > -INFINITY)) v = -INFINITY;        // a bias that is no number: never chosen
+        else size = fmaxf(size, fabsf(v));
+      }
+      key[i] = v > -INFINITY ? ordered(v + 0.f) : 0u;
     }
+    if (a.bias) size = warp_max(size);
+    const float apart = 2.f * (32.f + size) * kHalfStep;
+    // without a bias the keys are exact, and so is a group's best; a sum of two scores never is
+    auto far = [&](uint32_t x, uint32_t y) { return !a.bias || from_ordered(x) - from_ordered(y) > apart; };
+    auto far_groups = [&](uint32_t x, uint32_t y) {
+      if (!a.bias && a.group_best == 1) return true;
+      const float u = from_ordered(x), v = from_ordered(y);
+      return u - v > 2.f * apart + (fabsf(u) + fabsf(v)) * kHalfStep;
+    };
+    const bool sure = choose<NS, true>(c, key, [&](uint32_t first, uint32_t second) -> uint32_t {
+      if (a.group_best == 1) return first;
+      const float u = from_ordered(first), v = second ? from_ordered(second) : 0.f;
+      const float s = a.bias ? (second ? u + v : u) : (second ? p_of(u) + p_of(v) : p_of(u));
+      return ordered(s + 0.f);
+    }, far, far_groups, &my_id, &my_key);
+    if (!sure) my_id = choose_exactly<NS>(a, t, c, top);
+  }
+  // the logit of the chosen, slot j in lane j: the key itself where no bias is in it
+  float my_l = -INFINITY;
+  if (my_id >= 0) my_l = PLAIN ? from_ordered(my_key) : tidy(load1(a.logits, t * a.stride + my_id, a.type));
+  // Gates.  Renormalised softmax gates need no denominator over the row: exp(l - largest chosen l) over their sum.  In 32
+  // bits while the exponents are small; else in 64, where neither the rounding of a large exponent nor an underflowing
+  // score of a sum of underflowing scores is lost.
+  const bool chosen = my_id >= 0;
+  const float base = a.sigmoid ? 0.f : a.renorm ? warp_max(my_l) : top;
+  const float d = chosen ? my_l - base : 0.f;
+  float gate;
+  if (__any_sync(0xffffffffu, fabsf(d) > 16.f)) {
+    double p = 0.0;
+    if (chosen) {
+      if (a.sigmoid) p = 1.0 / (1.0 + exp(-(double)my_l));
+      else p = exp((double)my_l - (double)base) / (a.renorm ? 1.0 : (double)total);
+    }
+    if (a.renorm) {
+      const double sum = warp_sum(p);
+      p = sum > 0.0 ? p / sum : 0.0;
+    }
+    gate = (float)(p * (double)a.scale);
   } else {
-    if (!a.sigmoid && !a.renorm) {
-      // the denominator only scales the gates: 32 bits are enough for it
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < NS; ++i) sum += l[i] > -INFINITY ? expf(l[i] - top) : 0.f;
-#pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      total = sum;
+    float p = 0.f;
+    if (chosen) {
+      const float e = expf(a.sigmoid ? -d : d);
+      p = a.sigmoid ? __fdiv_rn(1.f, 1.f + e) : a.renorm ? e : __fdiv_rn(e, total);
     }
-#pragma unroll
-    for (int i = 0; i < NS; ++i) key[i] = l[i] > -INFINITY ? (K)ordered(l[i]) : (K)0;
-  }
-  if (a.groups > 1) {
-    // Score of a group: its best key, or the sum of its best two (of the one that is not masked).  Lane g keeps
-    // group g's; then the top_groups best groups are taken and the keys of the others cleared.
-    const int per = a.E / a.groups;
-    int group[NS];
-#pragma unroll
-    for (int i = 0; i < NS; ++i) group[i] = (lane + 32 * i) / per;
-    K mine[NS];                                   // scores of the groups lane, lane + 32, ..
-#pragma unroll
-    for (int i = 0; i < NS; ++i) mine[i] = 0;
-    for (int g = 0; g < a.groups; ++g) {
-      K sub[NS];
-#pragma unroll
-      for (int i = 0; i < NS; ++i) sub[i] = group[i] == g ? key[i] : (K)0;
-      int e;
-      K score = warp_best<NS>(sub, lane, &e);
-      if (WIDE && a.group_best == 2 && score) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-          if (lane + 32 * i == e) sub[i] = 0;
-        int e2;
-        const K second = warp_best<NS>(sub, lane, &e2);
-        if (second) score = (K)ordered(from_ordered((uint64_t)score) + from_ordered((uint64_t)second) + 0.0);
-      }
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-        if (lane + 32 * i == g) mine[i] = score;
+    if (a.renorm) {
+      const float sum = warp_sum(p);
+      p = sum > 0.f ? __fdiv_rn(p, sum) : 0.f;
     }
-    uint32_t keep = 0;                            // bit i: the group of my expert i stays
-    for (int j = 0; j < a.top_groups; ++j) {
-      int g;
-      if (!warp_best<NS>(mine, lane, &g)) break;  // only groups without an expert are left
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        if (lane + 32 * i == g) mine[i] = 0;
-        if (group[i] == g) keep |= 1u << i;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-      if (!((keep >> i) & 1u)) key[i] = 0;
-  }
-  // slot j in lane j: the j-th best expert and its logit
-  int my_id = -1;
-  float my_l = -INFINITY, first = -INFINITY;
-  for (int j = 0; j < a.k; ++j) {
-    int e;
-    const bool any = warp_best<NS>(key, lane, &e) != 0;
-    if (!any) break;
-    float v = 0.f;
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-      if (lane + 32 * i == e) {
-        key[i] = 0;
-        v = l[i];
-      }
-    v = __shfl_sync(0xffffffffu, v, e & 31);
-    if (j == 0) first = v;
-    first = fmaxf(first, v);
-    if (lane == j) {
-      my_id = e;
-      my_l = v;
-    }
-  }
-  // Gates in 64 bits (one exponential per lane), rounded once.  Renormalised softmax gates need no denominator over
-  // the row: exp(l - largest chosen l) over their sum.
-  double p = 0.0;
-  if (my_id >= 0) {
-    if (a.sigmoid) p = 1.0 / (1.0 + exp(-(double)my_l));
-    else p = exp((double)my_l - (double)(a.renorm ? first : top)) / (a.renorm ? 1.0 : total);
-  }
-  if (a.renorm) {
-    double sum = p;
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    p = sum > 0.0 ? p / sum : 0.0;
+    gate = p * a.scale;
   }
   if (lane < a.k) {
     a.ids[t * a.k + lane] = my_id;
-    a.gates[t * a.k + lane] = (float)(p * (double)a.scale);
+    a.gates[t * a.k + lane] = gate;
   }
 }
 
-template <bool WIDE>
 static cudaError_t launch_score(const RouteArgs& a, cudaStream_t s) {
-  const int ns = (a.E + 31) / 32;
-  void (*k)(RouteArgs) = ns <= 1 ? score_kernel<1, WIDE> : ns <= 2 ? score_kernel<2, WIDE> : ns <= 4 ? score_kernel<4, WIDE> : score_kernel<8, WIDE>;
+  const int ns = (a.E + 31) / 32, n = ns <= 1 ? 0 : ns <= 2 ? 1 : ns <= 4 ? 2 : 3;
+  static void (*const table[2][4])(RouteArgs) = {{score_kernel<1, false>, score_kernel<2, false>, score_kernel<4, false>, score_kernel<8, false>},
+                                                 {score_kernel<1, true>, score_kernel<2, true>, score_kernel<4, true>, score_kernel<8, true>}};
+  void (*k)(RouteArgs) = table[!a.bias && a.groups == 1][n];
   // four tokens per CTA: a batch of a few hundred tokens still reaches every SM
   return launch_dependent(k, dim3((unsigned)(((int64_t)a.T + 3) / 4)), dim3(128), 0, s, a);
 }
@@ -244,11 +382,13 @@ extern "C" pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const 
   a.sigmoid = r.score == PW_SCORE_SIGMOID;
   a.groups = r.top_groups == r.n_groups ? 1 : r.n_groups;   // every group stays: nothing to choose
   a.top_groups = r.top_groups;
+  const int per = r.n_experts / a.groups;
+  a.group_strides = per % 32 == 0 ? per / 32 : 0;
+  a.per_inverse = per > 1 ? (uint32_t)((0x100000000ull + per - 1) / per) : 0u;   // exact for numerators below 256
   a.group_best = r.group_best;
   a.renorm = r.renormalize != 0;
   a.scale = r.scale;
-  const bool wide = bias || (a.groups > 1 && r.group_best == 2);
-  PW_CUDA_OK(wide ? launch_score<true>(a, stream) : launch_score<false>(a, stream));
+  PW_CUDA_OK(launch_score(a, stream));
   ctx->launches++;
   return PW_OK;
 }

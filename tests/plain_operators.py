@@ -74,13 +74,12 @@ def route(logits, top_k, score, bias, n_groups, top_groups, group_best, renormal
             p = {e: v / total for e, v in p.items()}
         else:
             p = {e: 1.0 / (1.0 + math.exp(-x[t, e])) if x[t, e] > -700 else 0.0 for e in open_}
-        key = {e: p[e] + (0.0 if bias is None else float(bias[e])) for e in open_}
-        if bias is None and (group_best == 1 or n_groups == 1 or n_groups == top_groups):
-            key = {e: x[t, e] for e in open_}               # the order of the logits
+        sums = {e: p[e] + (0.0 if bias is None else float(bias[e])) for e in open_}
+        key = {e: x[t, e] for e in open_} if bias is None else sums     # without a bias: the order of the logits
         if n_groups > 1:
             best = {}
             for e in open_:
-                best.setdefault(e // per, []).append(key[e])
+                best.setdefault(e // per, []).append(key[e] if group_best == 1 else sums[e])
             rank = sorted(best, key=lambda g: (-sum(sorted(best[g], reverse=True)[:group_best]), g))[:top_groups]
             open_ = [e for e in open_ if e // per in rank]
         chosen = sorted(open_, key=lambda e: (-key[e], e))[:top_k]

@@ -331,6 +331,29 @@ def test_router_masks(ctx, rule):
     check_route(ctx, x, rule)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_best", [1, 2])
+def test_router_near_ties(ctx, score, group_best):
+    """Keys that 32 bits cannot tell apart: logits one step apart, biases that nearly cancel differences of scores, and
+    pairs of experts that are equal in everything."""
+    E, T = 64, 200
+    x = randn(1, T, E, scale=0.5)
+    x[:, 1::2] = torch.nextafter(x[:, ::2], torch.full_like(x[:, ::2], math.inf))
+    x[::3, 1::2] = x[::3, ::2]
+    bias = randn(2, E, scale=0.05)
+    bias[1::2] = bias[::2]
+    # rows whose scores differ between two experts by what the bias gives back, up to a part in 2^24 and more
+    far = plain.f64(x)
+    p = 1 / (1 + np.exp(-far[7])) if score == "sigmoid" else np.exp(far[7] - far[7].max()) / np.exp(far[7] - far[7].max()).sum()
+    bias[5], bias[9] = float(0.3 - p[5]), float(0.3 - p[9])
+    for b in (None, bias):
+        args = dict(score=score, n_groups=8, top_groups=3, group_best=group_best, renormalize=True, scale=1.0)
+        ids, gates = ctx.pw_route_tokens(x, 6, bias=b, **args)
+        ref_ids, ref_gates = plain.route(x, 6, bias=None if b is None else plain.f64(b), **args)
+        assert np.array_equal(ids.cpu().numpy(), ref_ids)
+        np.testing.assert_allclose(gates.cpu().numpy(), ref_gates, rtol=52 * U)
+
+
 def test_router_agrees_with_the_layers_own_rule(ctx):
     cfg = synth.CONFIGS["finegrained_decode"]
     logits = synth.router_logits(cfg, device="cuda")
