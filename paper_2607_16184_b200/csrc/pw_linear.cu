@@ -45,9 +45,18 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar_s, uint32_t parity) {
 }
 // Called by a whole warp, with the same answer for all lanes: the lanes of one poll may see the phase flip at different
 // moments, and what follows a wait (tensor-memory loads, cluster barriers) must not be run by a part of the warp.
-// False when the limit ran out or another role of the CTA has given up.
+// False when the limit ran out or another role of the CTA has given up.  (The first look goes without a suspend time: a
+// phase that is complete costs 79 cycles, with one 105.)
 __device__ __forceinline__ bool mbar_wait(uint32_t bar_s, uint32_t parity, volatile int* gave_up, int polls, int32_t* status) {
-  if (__any_sync(0xffffffffu, mbar_try(bar_s, parity))) return true;
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar_s), "r"(parity)
+      : "memory");
+  if (__any_sync(0xffffffffu, ok != 0)) return true;
 #pragma unroll 1
   for (int n = 0; n < polls; ++n) {
     if (__any_sync(0xffffffffu, mbar_try(bar_s, parity))) return true;
@@ -57,20 +66,27 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar_s, uint32_t parity, volat
   atomicMax(status, (int)PW_ERR_TIMEOUT);
   return false;
 }
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar_s, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_s), "r"(bytes) : "memory");
+// The forms of a copy warp: the whole warp runs its loop on the same values and the lane with on != 0 acts, so that the
+// operands stay in uniform registers, where these instructions take them from.  (From one lane inside a branch an
+// expected count and a copy took 300 cycles, and one warp could not ask for more than 71 GB/s.)
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar_s, uint32_t bytes, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar_s), "r"(bytes), "r"(on)
+      : "memory");
 }
-__device__ __forceinline__ void tma_load_2d(uint32_t dst_s, const CUtensorMap* map, int x, int y, uint32_t bar_s) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst_s),
-               "l"(map), "r"(x), "r"(y), "r"(bar_s)
-               : "memory");
+__device__ __forceinline__ void tma_load_2d(uint32_t dst_s, const CUtensorMap* map, int x, int y, uint32_t bar_s, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}" ::"r"(dst_s),
+      "l"(map), "r"(x), "r"(y), "r"(bar_s), "r"(on)
+      : "memory");
 }
-// The MMAs of one stage (four steps of 32 columns) and the commit behind them, on the stage's `done` barrier: the stage
-// is free again and its accumulator complete.  The whole warp runs this on the same values and the lane with on != 0
+// The MMAs of one block (four steps of 32 columns) and the commit behind them, on the stage's `done` barrier: the stage
+// is free again and its accumulators complete.  The whole warp runs this on the same values and the lane with on != 0
 // issues: the operands can then live in uniform registers, which a single lane inside a branch would have to fill for
 // every instruction.  PAIR: the forms of a CTA pair, whose commit arrives on the barrier at this offset in both CTAs.
 template <bool PAIR>
-__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t done, uint32_t on) {
+__device__ __forceinline__ void mma_block(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t done, uint32_t on) {
   if constexpr (PAIR) {
     asm volatile(
         "{\n\t.reg .pred q, f, t;\n\t.reg .b32 x, y;\n\t.reg .b64 ad, bd;\n\t.reg .b16 both;\n\tmov.b16 both, 3;\n\t"
@@ -103,6 +119,14 @@ __device__ __forceinline__ void mma_stage(uint32_t d, uint32_t a_lo, uint32_t b_
         : "memory");
   }
 }
+// Arrives on `done` once the MMAs that this thread has issued so far are complete.
+__device__ __forceinline__ void mma_commit(uint32_t done, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(done),
+      "r"(on)
+      : "memory");
+}
 // Waits for the tensor-memory loads into v[0 .. 15]; the registers pass through, so that no use moves ahead of it.
 __device__ __forceinline__ void tmem_wait16(float* v) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -110,6 +134,17 @@ __device__ __forceinline__ void tmem_wait16(float* v) {
                  "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
                :
                : "memory");
+}
+// Two fp32 multiply-adds in one instruction, each rounded once.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  return r;
 }
 // Operand tile in shared memory: rows of 128 bytes along K, 128-byte swizzle, groups of eight rows 1024 bytes apart.
 // The descriptor's low word is the address (and a leading offset that this layout ignores), 32 columns = 2 further on;
@@ -156,38 +191,41 @@ __device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T
 
 // ---- few rows: the weights on the M side ---------------------------------------------------------
 // D[128 weight rows, NT tokens].  A CTA takes one 128-row tile of w, up to NT tokens and a range of the blocks; the
-// CTAs of a cluster share the tile and the tokens, each with a range of its own.  Each then owns a share of the tokens:
-// the others copy their sums for those into its shared memory, counted on a barrier there, and it adds them in rank order
-// (no workspace, the same bits on every run).  (Fetched or sent word by word the sums took longer than the product: 10 of
-// 24 us at 64 tokens.)
-//   warps 0 .. kSum - 1  tensor memory -> registers, scales, output; thread = weight row; with 64 tokens on, warps 0-3
-//              take the first half of the columns and 4-7 the second
-//   then one   copies (one stage = a 128 x 128 tile of w and the same columns of NT tokens)
-//   then two   MMAs, even and odd blocks (issuing a stage and its wait cost a warp 500 cycles whatever their size); the
-//              first owns tensor memory: an accumulator of NT columns per stage, so a stage that has been filled again
-//              says that its accumulator has been read, and the MMA warps have one barrier to wait for.  The number of
-//              stages is even: a stage then always belongs to the same MMA warp, which sees every phase of its barrier
-//              (a warp that saw every other one could take an old phase for the one it waits for)
+// CTAs of a cluster share the tile and the tokens, each with a range of its own.  Every four tokens have an owner among
+// them: the others store their sums for those into its shared memory (counted on a barrier there), and it adds them in
+// rank order: no workspace, the same bits on every run.  One CTA per SM, its ring as deep as shared memory, for the weights
+// come from HBM; persistent where there are more tiles than SMs (a cluster takes one unit only).
+// A stage holds two blocks: what every role spends per barrier phase (a look 80 cycles, a copy or an MMA 70 to 90) is
+// what bounds it where the weights are in L2.
+//   warps 0 .. kSum - 1  tensor memory -> registers, scales, output; thread = weight row; with 64 tokens, warps 0-3 take
+//              the first half of the columns and 4-7 the second
+//   then one   copies (128 x 128 tiles of w and the same columns of NT tokens)
+//   then two   MMAs, the first and the second block of every stage; the first owns tensor memory: an accumulator of NT
+//              columns per block of the ring, so a stage that has been filled again says that its accumulators have been
+//              read.  (Stages in turn between the two would need an even number of them: a warp that sees every other phase
+//              of a barrier can take an old one for the one it waits for.)
 //   then one   scales, eight blocks at a time, multiplied, into shared memory: loaded by the warps that use them they
 //              were 16 times as many requests as they are sectors, and the bound of the kernel
-// One CTA per SM, its ring as deep as shared memory: the weights come from HBM.  Persistent where there are more tiles
-// than SMs (the CTAs of a cluster then take one unit only, see the launch).
 template <int NT>
 struct FewCfg {
   static constexpr int kSum = NT >= 64 ? 8 : 4;
   static constexpr int kThreads = (kSum + 4) * 32;
-  static constexpr int kStage = 16384 + NT * 128;
-  static constexpr int kStages = NT <= 32 ? 10 : 8;
-  static constexpr int kSmem = kStages * kStage + 1024;
-  static constexpr int kCols = NT <= 16 ? 256 : 512;   // kStages * NT, a power of two
-  static constexpr int kSums = NT * 512;          // a CTA's sums, and what it receives from a cluster of any size
-  static_assert(kStages % 2 == 0, "a stage belongs to one MMA warp");
-  static_assert(2 * kSums <= kStages * kStage, "both take the ring's place");
-  static_assert(kStages * NT <= kCols, "an accumulator per stage");
+  static constexpr int kBlock = 16384 + NT * 128;  // bytes of a block in the ring
+  static constexpr int kStages = NT <= 32 ? 5 : 3;
+  static constexpr int kChunks = NT / 4;           // of four tokens
+  static constexpr int kSums = (kChunks < 8 ? 8 : kChunks) * 2048;   // what a CTA receives from a cluster of up to eight
+  static constexpr int kSmem = kStages * 2 * kBlock + kSums + 1024;
+  static constexpr int kCols = NT <= 16 ? 256 : 512;
+  static_assert(kStages * 2 * NT <= kCols, "an accumulator per block of the ring");
 };
-__device__ __forceinline__ void bulk_to_rank(uint32_t dst, uint32_t src_s, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "r"(src_s), "r"(bytes), "r"(bar) : "memory");
+// 16 bytes into the shared memory of a CTA of the cluster, counted on a barrier there.
+__device__ __forceinline__ void send4(uint32_t dst, float x, float y, float z, float w, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst), "f"(x), "f"(y), "f"(z),
+               "f"(w), "r"(bar)
+               : "memory");
 }
+__device__ __forceinline__ float lo_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 
 template <int NT>
 __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
@@ -199,16 +237,18 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
   __shared__ uint32_t tmem_base;
   __shared__ volatile int gave_up;
   __shared__ alignas(16) float scales[2][kScaleRun][NT + 4];     // read four at a time
-  const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u, sums_s = ring_s + S * 2 * C::kBlock;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x % split);
   const int unit0 = (int)(blockIdx.x / split), stride = (int)(gridDim.x / split);   // unit: (row tile, token tile), token tiles fastest
   const int g0 = (int)((int64_t)a.G * rank / split), g1 = (int)((int64_t)a.G * (rank + 1) / split);
-  const int n_blocks = g1 - g0;
+  // chunks of four tokens that this CTA adds up: rank, rank + split, ..
+  const int chunks = split > 1 ? (min(a.T - unit0 % token_tiles * NT, NT) + 3) / 4 : 0;
+  const int mine = rank < chunks ? (chunks - 1 - rank) / split + 1 : 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&done[i], 1);
+      mbar_init(&done[i], 2);                      // both MMA warps
       mbar_init(&freed[i], NW);
     }
     for (int i = 0; i < 2; ++i) {
@@ -219,7 +259,9 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (mine > 0) mbar_expect_tx(smem_u32(&sums_in), (uint32_t)(mine * split) * 2048u, 1u);
   }
+  if (split > 1) cluster_arrive();
   if (warp == NW + 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(C::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -228,29 +270,27 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base;
+  if (split > 1) cluster_wait();                   // the others' barriers are ready
   grid_dep_sync();          // codes and scales may come from the kernel directly ahead
   grid_dep_trigger();
-
-  float acc[QC];
-  const int col = (warp >> 2) * QC, row = (warp & 3) * 32 + lane;   // of a summing warp
 
   if (warp == NW) {
     bool ok = true;
     int i = 0, s = 0;
     uint32_t par = 1;                              // of the stage's next `freed` phase (the first pass waits for none)
+    const uint32_t on = lane == 0 ? 1u : 0u, full_s = smem_u32(&full[0]);
     for (int u = unit0; ok && u < n_units; u += stride) {
       const int row0 = u / token_tiles * 128, tok0 = u % token_tiles * NT;
-      for (int g = g0; g < g1; ++g, ++i) {
+      for (int g = g0; g < g1; g += 2, ++i) {
         if ((a.hook & 2u) && i == 1) ok = false;   // test hook: the waits on the second stage run out
         if (ok && i >= S) ok = mbar_wait(smem_u32(&freed[s]), par, &gave_up, a.polls, a.status);
         if (!ok) break;
-        if (lane == 0) {
-          const uint32_t bar = smem_u32(&full[s]), dst = ring_s + s * C::kStage;
-          mbar_expect_tx(bar, C::kStage);
-          tma_load_2d(dst, &a.mw, g * kBlockK, row0, bar);
-          tma_load_2d(dst + 16384, &a.ma, g * kBlockK, tok0, bar);
-        }
-        __syncwarp();
+        const uint32_t bar = full_s + 8 * s, dst = ring_s + s * 2 * C::kBlock, second = g + 1 < g1 ? on : 0u;
+        mbar_expect_tx(bar, g + 1 < g1 ? 2 * C::kBlock : C::kBlock, on);
+        tma_load_2d(dst, &a.mw, g * kBlockK, row0, bar, on);
+        tma_load_2d(dst + 16384, &a.ma, g * kBlockK, tok0, bar, on);
+        tma_load_2d(dst + C::kBlock, &a.mw, (g + 1) * kBlockK, row0, bar, second);
+        tma_load_2d(dst + C::kBlock + 16384, &a.ma, (g + 1) * kBlockK, tok0, bar, second);
         if (++s == S) {
           s = 0;
           par ^= 1u;
@@ -263,16 +303,25 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
         }
   } else if (warp == NW + 1 || warp == NW + 2) {
     bool ok = true;
-    const uint32_t on = lane == 0 ? 1u : 0u;
-    const int units = unit0 < n_units ? (n_units - 1 - unit0) / stride + 1 : 0, items = units * n_blocks;
-    for (int i = warp - NW - 1; ok && i < items; i += 2) {
-      const int s = i % S;
-      ok = mbar_wait(smem_u32(&full[s]), (i / S) & 1, &gave_up, a.polls, a.status);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t w_s = ring_s + s * C::kStage;
-      mma_stage<false>(tmem + s * NT, swizzled_lo(w_s), swizzled_lo(w_s + 16384), kSwizzledHi, e4m3_idesc(128, NT), smem_u32(&done[s]), on);
-    }
+    int s = 0;
+    uint32_t par = 0;                              // of the stage's next `full` phase
+    const int k = warp - NW - 1;                   // which of the two blocks
+    const uint32_t on = lane == 0 ? 1u : 0u, full_s = smem_u32(&full[0]), done_s = smem_u32(&done[0]);
+    for (int u = unit0; ok && u < n_units; u += stride)
+      for (int g = g0; g < g1; g += 2) {
+        ok = mbar_wait(full_s + 8 * s, par, &gave_up, a.polls, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t w_s = ring_s + (s * 2 + k) * C::kBlock;
+        if (g + k < g1)
+          mma_block<false>(tmem + (s * 2 + k) * NT, swizzled_lo(w_s), swizzled_lo(w_s + 16384), kSwizzledHi, e4m3_idesc(128, NT), done_s + 8 * s, on);
+        else
+          mma_commit(done_s + 8 * s, on);
+        if (++s == S) {
+          s = 0;
+          par ^= 1u;
+        }
+      }
   } else if (warp == NW + 3) {
     bool ok = true;
     int run = 0;
@@ -288,44 +337,49 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
       }
     }
   } else {
+    const int col = (warp >> 2) * QC, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
     bool ok = true;
     int s = 0, run = 0;
     uint32_t par = 0;                              // of the stage's next `done` phase
-    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
-    for (int u = unit0; ok && u < n_units; u += stride) {
+    uint64_t acc[QC / 2];                          // pairs of tokens: a packed multiply-add does two
+    for (int u = unit0; u < n_units; u += stride) {
 #pragma unroll
-      for (int j = 0; j < QC; ++j) acc[j] = 0.f;
+      for (int j = 0; j < QC / 2; ++j) acc[j] = 0;
       int in_run = 0;
 #pragma unroll 1
-      for (int g = g0; g < g1; ++g) {
+      for (int g = g0; ok && g < g1; g += 2) {
         if (in_run == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
         if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
         if (!ok) break;
         tc_fence_after();
-        const float* cs = scales[run & 1][in_run] + col;
-        constexpr int W = QC < 32 ? QC : 32;       // columns loaded at once
+        const bool two = g + 1 < g1;
+        float v[2][QC];
 #pragma unroll
-        for (int h = 0; h < QC; h += W) {
-          float v[W];
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int c = 0; c < W; c += 16) tmem_ld16(lane_base + s * NT + h + c, v + c);
+          for (int c = 0; c < QC; c += 16)
+            if (k == 0 || two) tmem_ld16(lane_base + (s * 2 + k) * NT + c, v[k] + c);
 #pragma unroll
-          for (int c = 0; c < W; c += 16) tmem_wait16(v + c);
-          if (h + W == QC) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&freed[s]);
-          }
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int j = 0; j < W; j += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(cs + h + j);
-            acc[h + j] = fmaf(v[j], f.x, acc[h + j]);
-            acc[h + j + 1] = fmaf(v[j + 1], f.y, acc[h + j + 1]);
-            acc[h + j + 2] = fmaf(v[j + 2], f.z, acc[h + j + 2]);
-            acc[h + j + 3] = fmaf(v[j + 3], f.w, acc[h + j + 3]);
+          for (int c = 0; c < QC; c += 16) tmem_wait16(v[k] + c);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&freed[s]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (k == 1 && !two) break;
+          const ulonglong2* cs = reinterpret_cast<const ulonglong2*>(scales[run & 1][in_run + k] + col);
+#pragma unroll
+          for (int j = 0; j < QC / 4; ++j) {
+            const ulonglong2 f = cs[j];
+            acc[2 * j] = fma2(pack2(v[k][4 * j], v[k][4 * j + 1]), f.x, acc[2 * j]);
+            acc[2 * j + 1] = fma2(pack2(v[k][4 * j + 2], v[k][4 * j + 3]), f.y, acc[2 * j + 1]);
           }
         }
-        if (++in_run == kScaleRun || g + 1 == g1) {
+        in_run += 2;
+        if (in_run == kScaleRun || g + 2 >= g1) {
           __syncwarp();
           if (lane == 0) mbar_arrive(&sc_empty[run & 1]);
           in_run = 0;
@@ -337,62 +391,51 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
         }
       }
       const int64_t n = (int64_t)(u / token_tiles) * 128 + row;
-      const int t0 = u % token_tiles * NT + col;
-      if (split == 1 && ok && n < a.N) {
+      const int t0 = u % token_tiles * NT;
+      if (split == 1) {
+        if (ok && n < a.N) {
 #pragma unroll
-        for (int j = 0; j < QC; ++j)
-          if (t0 + j < a.T) store1(a.out, (int64_t)(t0 + j) * a.ld_out + n, a.out_type, acc[j]);
+          for (int j = 0; j < QC; ++j)
+            if (t0 + col + j < a.T)
+              store1(a.out, (int64_t)(t0 + col + j) * a.ld_out + n, a.out_type, j & 1 ? hi_of(acc[j / 2]) : lo_of(acc[j / 2]));
+        }
+        __syncwarp();
+        if (!ok) break;
+        continue;
+      }
+      // [owner's chunk][rank][row] of four tokens.  Whoever gave up on a wait sends all the same, so the wait for the
+      // others' sums outlasts any of theirs; a CTA that has received what is its own is sent nothing more and may leave.
+#pragma unroll
+      for (int k = 0; k < QC / 4; ++k) {
+        const int c = col / 4 + k;
+        if (c < chunks) {
+          const int lc = c / split, owner = c - lc * split;
+          send4(map_rank(sums_s + ((lc * split + rank) * 128 + row) * 16, owner), lo_of(acc[2 * k]), hi_of(acc[2 * k]), lo_of(acc[2 * k + 1]),
+                hi_of(acc[2 * k + 1]), map_rank(smem_u32(&sums_in), owner));
+        }
+      }
+      __syncwarp();
+      volatile int no_matter = 0;
+      if (mine > 0 && mbar_wait(smem_u32(&sums_in), 0, &no_matter, 8 * a.polls, a.status) && n < a.N) {
+        const float4* sums = reinterpret_cast<const float4*>(smem_raw + (sums_s - smem_u32(smem_raw))) + row;
+        for (int lc = warp >> 2; lc < mine; lc += NW / 4) {
+          float4 x = sums[lc * split * 128];
+          for (int r = 1; r < split; ++r) {
+            const float4 y = sums[(lc * split + r) * 128];
+            x.x += y.x;
+            x.y += y.y;
+            x.z += y.z;
+            x.w += y.w;
+          }
+          const int t = t0 + (lc * split + rank) * 4;
+          const float o[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (t + j < a.T) store1(a.out, (int64_t)(t + j) * a.ld_out + n, a.out_type, o[j]);
+        }
       }
       __syncwarp();
     }
-  }
-
-  if (split > 1) {
-    // The sums as [token][row] in the ring, which is free (every copy has landed and every MMA has read its operands:
-    // the last accumulator was complete), then the part of each owner with one bulk copy into its [rank][token][row]
-    // behind, once its ring is free too.  Whoever gave up on a wait sends all the same, so the wait for the others' sums
-    // outlasts any of theirs.
-    const int64_t n = (int64_t)(unit0 / token_tiles) * 128 + row;
-    const int tok0 = unit0 % token_tiles * NT;
-    const int own = NT / split;                    // tokens of the tile that a CTA of the cluster adds up
-    const int mine = min(max(a.T - tok0 - rank * own, 0), own);
-    const uint32_t sums_s = ring_s + C::kSums;
-    if (warp < NW) {
-#pragma unroll
-      for (int j = 0; j < QC; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring_s + (col + j) * 512 + row * 4), "f"(acc[j]) : "memory");
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    } else if (warp == NW && lane == 0) {
-      mbar_expect_tx(smem_u32(&sums_in), (uint32_t)(split * mine) * 512);
-    }
-    __syncthreads();
-    cluster_arrive();
-    cluster_wait();
-    if (warp == NW && lane < split) {
-      const int theirs = min(max(a.T - tok0 - lane * own, 0), own);
-      if (theirs > 0)
-        bulk_to_rank(map_rank(sums_s + rank * own * 512, lane), ring_s + lane * own * 512, theirs * 512, map_rank(smem_u32(&sums_in), lane));
-    }
-    __syncwarp();
-    if (warp < NW && mine > 0) {
-      volatile int no_matter = 0;
-      if (mbar_wait(smem_u32(&sums_in), 0, &no_matter, 8 * a.polls, a.status) && n < a.N) {
-        const float* sums = reinterpret_cast<const float*>(smem_raw + (sums_s - smem_u32(smem_raw))) + row;
-        // tokens four at a time, in turn between the halves of the warps
-        for (int j0 = (warp >> 2) * 4; j0 < mine; j0 += NW) {
-          float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-          for (int r = 0; r < split; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (j0 + j < mine) v[j] += sums[(r * own + j0 + j) * 128];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (j0 + j < mine) store1(a.out, (int64_t)(tok0 + rank * own + j0 + j) * a.ld_out + n, a.out_type, v[j]);
-        }
-      }
-    }
-    cluster_arrive();                              // the copies read this CTA's ring until the owners have their sums
-    cluster_wait();
   }
   tc_fence_before();
   __syncthreads();
@@ -424,10 +467,12 @@ struct PairCfg {
   static constexpr int kAcc = 512 / BN;           // accumulators in tensor memory (an even number, for the same reason)
 };
 // copy into this CTA's shared memory, counted on a barrier of the pair (shared::cluster address)
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_s, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst_s),
-               "l"(map), "r"(x), "r"(y), "r"(bar)
-               : "memory");
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_s, const CUtensorMap* map, int x, int y, uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}" ::"r"(dst_s),
+      "l"(map), "r"(x), "r"(y), "r"(bar), "r"(on)
+      : "memory");
 }
 // (nothing in memory is handed over with it, only tensor memory, which the tcgen05 fences order: a release at cluster
 // scope would make the warp wait for its outstanding loads and stores first)
@@ -488,7 +533,7 @@ __device__ __forceinline__ void store_box(uint32_t box_s, const char* box, const
   }
 }
 template <int COLS>
-__device__ __forceinline__ void store_tile(uint32_t box_s, const char* box, const float* acc, const LinearArgs& a, int64_t m0, int n0, int lane) {
+__device__ __forceinline__ void store_tile(uint32_t box_s, const char* box, const uint64_t* acc, const LinearArgs& a, int64_t m0, int n0, int lane) {
   uint32_t words[32];
   auto boxes_read = [&] {                                     // by the copies so far
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -500,7 +545,10 @@ __device__ __forceinline__ void store_tile(uint32_t box_s, const char* box, cons
     for (int p = 0; p < COLS / 32; ++p) {
       if (p == 2) boxes_read();
 #pragma unroll
-      for (int j = 0; j < 32; ++j) words[j] = __float_as_uint(acc[p * 32 + j]);
+      for (int j = 0; j < 16; ++j) {
+        words[2 * j] = (uint32_t)acc[p * 16 + j];
+        words[2 * j + 1] = (uint32_t)(acc[p * 16 + j] >> 32);
+      }
       store_box(box_s + (p & 1) * 4096, box + (p & 1) * 4096, words, a, m0, n0 + p * 32, 4, lane);
     }
   } else {
@@ -508,8 +556,10 @@ __device__ __forceinline__ void store_tile(uint32_t box_s, const char* box, cons
 #pragma unroll
     for (int p = 0; p < COLS / 64; ++p) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
-        words[j] = half ? pack_half(acc[p * 64 + 2 * j], acc[p * 64 + 2 * j + 1]) : pack_bf(acc[p * 64 + 2 * j], acc[p * 64 + 2 * j + 1]);
+      for (int j = 0; j < 32; ++j) {
+        const float lo = __uint_as_float((uint32_t)acc[p * 32 + j]), hi = __uint_as_float((uint32_t)(acc[p * 32 + j] >> 32));
+        words[j] = half ? pack_half(lo, hi) : pack_bf(lo, hi);
+      }
       store_box(box_s + p * 4096, box + p * 4096, words, a, m0, n0 + p * 64, 2, lane);
     }
   }
@@ -561,22 +611,24 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 8) {
       bool ok = true;
-      int item = 0;
+      int item = 0, s = 0;
+      uint32_t par = 1;                             // of the stage's next `done` phase (the first pass waits for none)
+      const uint32_t on = lane == 0 ? 1u : 0u, lead_on = rank == 0 ? on : 0u;
+      const uint32_t full_s = smem_u32(&full[0]), lead_s = map_rank(full_s, 0);
       for (int t = pair; ok && t < n_tiles; t += n_pairs) {
         const int m0 = (t % token_tiles) * 256 + (int)rank * 128, n0 = (t / token_tiles) * BN + (int)rank * HC;
         for (int g = 0; g < a.G; ++g, ++item) {
-          const int s = item % S;
           if ((a.hook & 2u) && item == 1) ok = false;   // test hook: the waits on the second stage run out
-          if (ok && item >= S) ok = mbar_wait(smem_u32(&done[s]), (item / S - 1) & 1, &gave_up, a.polls, a.status);
+          if (ok && item >= S) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
           if (!ok) break;
-          if (lane == 0) {
-            const uint32_t bar_s = smem_u32(&full[s]), dst = ring_s + s * C::kStage;
-            if (rank == 0) mbar_expect_tx(bar_s, 2 * C::kStage);
-            const uint32_t bar = map_rank(bar_s, 0);
-            tma_load_2d_pair(dst, &a.ma, g * kBlockK, m0, bar);
-            tma_load_2d_pair(dst + 16384, &a.mw, g * kBlockK, n0, bar);
+          const uint32_t dst = ring_s + s * C::kStage;
+          mbar_expect_tx(full_s + 8 * s, 2 * C::kStage, lead_on);
+          tma_load_2d_pair(dst, &a.ma, g * kBlockK, m0, lead_s + 8 * s, on);
+          tma_load_2d_pair(dst + 16384, &a.mw, g * kBlockK, n0, lead_s + 8 * s, on);
+          if (++s == S) {
+            s = 0;
+            par ^= 1u;
           }
-          __syncwarp();
         }
       }
       // leave nothing behind: every stage handed back (its arrival crosses to the other CTA), or at least every copy landed
@@ -594,12 +646,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
       const int64_t items = (int64_t)my_tiles * a.G;
       for (int64_t it = warp - 9; ok && it < items; it += 2) {
         const int item = (int)it, s = item % S, b = item % A;
-        if (item >= A) ok = mbar_wait(smem_u32(&acc_empty[b]), (item / A - 1) & 1, &gave_up, a.polls, a.status);
-        if (ok) ok = mbar_wait(smem_u32(&full[s]), (item / S) & 1, &gave_up, a.polls, a.status);
+        ok = mbar_wait(smem_u32(&full[s]), (item / S) & 1, &gave_up, a.polls, a.status);   // the accumulator comes last
+        if (ok && item >= A) ok = mbar_wait(smem_u32(&acc_empty[b]), (item / A - 1) & 1, &gave_up, a.polls, a.status);
         if (!ok) break;
         tc_fence_after();
         const uint32_t x_s = ring_s + s * C::kStage;
-        mma_stage<true>(tmem + b * BN, swizzled_lo(x_s), swizzled_lo(x_s + 16384), kSwizzledHi, e4m3_idesc(256, BN), smem_u32(&done[s]), on);
+        mma_block<true>(tmem + b * BN, swizzled_lo(x_s), swizzled_lo(x_s + 16384), kSwizzledHi, e4m3_idesc(256, BN), smem_u32(&done[s]), on);
       }
     } else if (warp == 11) {
       bool ok = true;
@@ -624,47 +676,60 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
     const uint32_t box_s = ring_s + S * C::kStage + warp * 8192;
     const char* box = smem_raw + (box_s - smem_u32(smem_raw));
+    // The loads run one step of 32 columns ahead of the multiply-adds, over the blocks' ends too: the last step of a
+    // block is multiplied while the first of the next one is on its way.
+    constexpr int Q = HC / 32;
+    static_assert(Q % 2 == 0, "a block begins in the first buffer");
     bool ok = true;
-    int s = 0, b = 0, run = 0;
+    int s = 0, b = 0, run = 0, in_run = 0;
     uint32_t par = 0;                               // of the stage's next `done` phase
+    float v[2][32], f = 0.f;
+    // waits for the next block's accumulator (b, s), takes its scale, starts its first load
+    auto begin = [&] {
+      if (in_run == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+      if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
+      if (!ok) return;
+      tc_fence_after();
+      tmem_ld32(lane_base + b * BN, v[0]);
+    };
+    if (pair < n_tiles) begin();
     for (int t = pair; ok && t < n_tiles; t += n_pairs) {
-      float acc[HC];
+      uint64_t acc[HC / 2];                         // pairs of columns: a packed multiply-add does two
 #pragma unroll
-      for (int j = 0; j < HC; ++j) acc[j] = 0.f;
+      for (int j = 0; j < HC / 2; ++j) acc[j] = 0;
 #pragma unroll 1
-      for (int g = 0; g < a.G; ++g) {
-        if (g % kScaleRun == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
-        const float f = scales[run & 1][g % kScaleRun][row] * w_scales[run & 1][col / 128][g % kScaleRun];
-        if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
-        if (!ok) break;
-        tc_fence_after();
-        float v[2][32];
-        tmem_ld32(lane_base + b * BN, v[0]);
+      for (int g = 0; ok && g < a.G; ++g) {
+        f = scales[run & 1][in_run][row] * w_scales[run & 1][col / 128][in_run];
+        const uint64_t ff = pack2(f, f);
 #pragma unroll
-        for (int c = 0; c < HC / 32; ++c) {
+        for (int c = 0; c < Q; ++c) {
           tmem_wait32(v[c & 1]);
-          if (c + 1 < HC / 32) {
+          if (c + 1 < Q) {
             tmem_ld32(lane_base + b * BN + (c + 1) * 32, v[(c + 1) & 1]);
           } else {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_cluster(map_rank(smem_u32(&acc_empty[b]), 0));
+            if (lane == 0) {
+              arrive_cluster(map_rank(smem_u32(&acc_empty[b]), 0));
+              if (in_run == kScaleRun - 1 || g == a.G - 1) mbar_arrive(&sc_empty[run & 1]);
+            }
+            if (++in_run == kScaleRun || g == a.G - 1) {
+              in_run = 0;
+              ++run;
+            }
+            b = b + 1 == A ? 0 : b + 1;
+            if (++s == S) {
+              s = 0;
+              par ^= 1u;
+            }
+            if (g + 1 < a.G || t + n_pairs < n_tiles) begin();
           }
 #pragma unroll
-          for (int j = 0; j < 32; ++j) acc[c * 32 + j] = fmaf(v[c & 1][j], f, acc[c * 32 + j]);
-        }
-        if (g % kScaleRun == kScaleRun - 1 || g == a.G - 1) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sc_empty[run & 1]);
-          ++run;
-        }
-        b = b + 1 == A ? 0 : b + 1;
-        if (++s == S) {
-          s = 0;
-          par ^= 1u;
+          for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fma2(pack2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), ff, acc[c * 16 + j]);
         }
       }
-      if (ok) store_tile<HC>(box_s, box, acc, a, (int64_t)(t % token_tiles) * 256 + rank * 128 + (warp & 3) * 32, (t / token_tiles) * BN + col, lane);
+      // (after a wait that gave up the sums are not complete; what is stored is undefined then)
+      store_tile<HC>(box_s, box, acc, a, (int64_t)(t % token_tiles) * 256 + rank * 128 + (warp & 3) * 32, (t / token_tiles) * BN + col, lane);
       __syncwarp();
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // the output is written, the boxes are read
@@ -754,19 +819,19 @@ static LinearPlan plan_few(int T, int N, int G, int nt, int sms) {
   // few units: their blocks are split over a cluster, while there is an SM for every CTA and two blocks for each
   while (p.split < 8 && p.units * p.split * 2 <= sms && G >= p.split * 4) p.split *= 2;
   const int64_t blocks = p.split > 1 ? tiles_of(G, p.split) : tiles_of(p.units, sms) * G;
-  p.us = 5.0 + (p.split > 1 ? 1.3 : 0.) + (nt == 16 ? 0.24 : nt == 32 ? 0.32 : 0.375) * blocks;
+  p.us = nt == 16 ? 3.3 + 0.26 * blocks : nt == 32 ? 3.8 + 0.33 * blocks : 4.6 + 0.35 * blocks;
   return p;
 }
 static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
   LinearPlan p{0, bn, 1, tiles_of(T, 256), 0, 0.};
   p.units = p.token_tiles * tiles_of(N, bn);
-  p.us = 4.6 + (bn == 128 ? 0.32 : 0.5) * tiles_of(p.units, sms / 2) * G;
+  p.us = 4.6 + (bn == 128 ? 0.32 : 0.52) * tiles_of(p.units, sms / 2) * G;
   return p;
 }
 // The plan that finishes soonest by a model that is linear in the blocks of 128 columns a CTA (pair) goes through one
 // after the other; the times per block are measured (us, contraction 4096: tokens x weight rows, few 64 / pair 128 /
-// pair 256):  64 x 4096  9.4 / 14.1 / 18.5,  128 x 4096  11.7 / 14.4 / 19.3,  128 x 14336  27.3 / 27.6 / 22.7,
-// 256 x 4096  14.9 / 14.5 / 19.3,  512 x 4096  26.2 / 15.6 / 20.0,  512 x 14336  80 / 48 / 38.
+// pair 256):  64 x 4096  7.6 / 14.1 / 18.3,  128 x 4096  9.9 / 14.4 / 18.9,  64 x 14336  16.0 / 26.2 / 20.9,
+// 128 x 14336  27 / 27.6 / 22.7,  256 x 4096  14.9 / 14.7 / 19.1,  512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
 static LinearPlan plan_linear(int T, int N, int G, int sms) {
   LinearPlan best = plan_few(T, N, G, T <= 16 ? 16 : T <= 32 ? 32 : 64, sms);
   for (int bn = 128; bn <= 256; bn *= 2) {

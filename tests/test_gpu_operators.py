@@ -266,7 +266,7 @@ def test_product_back_to_back(ctx, T):
 def test_product_wait_that_runs_out_is_reported():
     c = B.Context(1, 8, 0, 256, 512, 16, 2)
     try:
-        for T, N, K in ((5, 300, 1024), (1000, 512, 1024)):
+        for T, N, K in ((5, 300, 14336), (40, 300, 4096), (1000, 512, 1024)):
             a, sa, w, sw = operands(c, T, N, K)
             c.pw_debug_set_wait(1, 2)
             c.pw_scaled_linear(a, sa, w, sw)
