@@ -72,91 +72,90 @@ struct Chooser {
   __device__ __forceinline__ int group_of(int e) const { return per_inverse ? (int)__umulhi((uint32_t)e, per_inverse) : e; }
 };
 
-// The experts of slots 0 .. k - 1 and their keys (slot j in lane j; -1: none left).  `score(first, second)`: a group's score, as a key,
-// of its two best keys.  `far(a, b)`: whether a is larger than the next key b beyond doubt; the function returns false
-// when a decision was not.  `far_groups` the same for scores of groups.
-template <int NS, bool GROUPS, class K, class Score, class Far, class FarGroups>
-__device__ __forceinline__ bool choose(const Chooser& c, K* key, Score score, Far far, FarGroups far_groups, int* slot, K* slot_key) {
-  bool sure = true;
-  if (GROUPS && c.groups > 1) {
-    K mine[NS];                                   // scores of the groups lane, lane + 32, ..
-    int group[NS];
+// Clears the keys of all but the best top_groups groups.  `score(first, second)`: a group's score, as a key, of its two
+// best keys.  `far(a, b)`: whether the score a is larger than the next one, b, beyond doubt; false when the decision was
+// not.
+template <int NS, class K, class Score, class Far>
+__device__ __forceinline__ bool keep_groups(const Chooser& c, K* key, Score score, Far far) {
+  // the two best keys of the groups lane, lane + 32, .., then their scores, all groups at once
+  K mine[NS], second[NS];
+  int group[NS];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) group[i] = c.group_of(c.lane + 32 * i);
-    if (c.strides) {
-      // groups of whole strides: a lane's keys of a group are known without looking
-      K b1 = 0, b2 = 0;
-      int g = 0, left = c.strides;
-      mine[0] = 0;
+  for (int i = 0; i < NS; ++i) {
+    group[i] = c.group_of(c.lane + 32 * i);
+    mine[i] = second[i] = 0;
+  }
+  auto two_best = [&](K b1, K b2, K* first, K* next) {
+    *first = warp_max_key(b1);
+    const uint32_t holders = __ballot_sync(0xffffffffu, b1 == *first);
+    *next = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
+  };
+  if (c.strides == 1) {
+    // a stride is a group: nothing to look for, and the groups' reductions overlap
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      K first, next;
+      two_best(key[i], (K)0, &first, &next);
+      if (c.lane == i) {
+        mine[0] = first;
+        second[0] = next;
+      }
+    }
+  } else {
+#pragma unroll 1
+    for (int g = 0; g < c.groups; ++g) {
+      K b1 = 0, b2 = 0, first, next;
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const K k = key[i];
+        const K k = group[i] == g ? key[i] : (K)0;
         b2 = k > b1 ? b1 : k > b2 ? k : b2;
         b1 = k > b1 ? k : b1;
-        if (--left == 0) {
-          const K first = warp_max_key(b1);
-          const uint32_t holders = __ballot_sync(0xffffffffu, b1 == first);
-          const K second = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
-          if (c.lane == g && first) mine[0] = score(first, second);
-          ++g;
-          left = c.strides;
-          b1 = b2 = 0;
-        }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NS; ++i) mine[i] = 0;
-      for (int g = 0; g < c.groups; ++g) {
-        K b1 = 0, b2 = 0;
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          const K k = group[i] == g ? key[i] : (K)0;
-          b2 = k > b1 ? b1 : k > b2 ? k : b2;
-          b1 = k > b1 ? k : b1;
-        }
-        const K first = warp_max_key(b1);
-        const uint32_t holders = __ballot_sync(0xffffffffu, b1 == first);
-        const K second = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
-        if (c.lane == (g & 31) && first) {
-          const K s = score(first, second);
-#pragma unroll
-          for (int i = 0; i < NS; ++i)
-            if ((g >> 5) == i) mine[i] = s;
-        }
-      }
-    }
-    K last = 0, next = 0;
-    uint32_t keep = 0;                            // bit i: the group of my expert i stays
-    for (int j = 0; j <= c.top_groups; ++j) {     // one more than is kept: the best that is not
-      int g;
-      next = c.groups <= 32 ? warp_best<1>(mine, c.lane, &g) : warp_best<NS>(mine, c.lane, &g);
-      if (!next || j == c.top_groups) break;      // only groups without an expert are left, or enough
-      last = next;
-      if (c.groups <= 32) {
-        if (c.lane == g) mine[0] = 0;
-      } else {
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-          if (c.lane + 32 * i == g) mine[i] = 0;
-      }
+      two_best(b1, b2, &first, &next);
 #pragma unroll
       for (int i = 0; i < NS; ++i)
-        if (group[i] == g) keep |= 1u << i;
+        if (c.lane + 32 * i == g) {
+          mine[i] = first;
+          second[i] = next;
+        }
     }
-    if (next && !far_groups(last, next)) sure = false;
+  }
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (i == 0 || c.groups > 32) mine[i] = mine[i] ? score(mine[i], second[i]) : (K)0;
+  K last = 0, next = 0;
+  uint32_t keep = 0;                            // bit i: the group of my expert i stays
+  for (int j = 0; j <= c.top_groups; ++j) {     // one more than is kept: the best that is not
+    int g;
+    next = c.groups <= 32 ? warp_best<1>(mine, c.lane, &g) : warp_best<NS>(mine, c.lane, &g);
+    if (!next || j == c.top_groups) break;      // only groups without an expert are left, or enough
+    last = next;
+    if (c.groups <= 32) {
+      if (c.lane == g) mine[0] = 0;
+    } else {
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+        if (c.lane + 32 * i == g) mine[i] = 0;
+    }
 #pragma unroll
     for (int i = 0; i < NS; ++i)
-      if (!((keep >> i) & 1u)) key[i] = 0;
+      if (group[i] == g) keep |= 1u << i;
   }
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (!((keep >> i) & 1u)) key[i] = 0;
+  return !next || far(last, next);
+}
+
+// The experts of slots 0 .. k - 1 and their keys (slot j in lane j; -1: none left), by k searches for the largest key.
+// Consumes the keys.  Equal keys: lower expert first.
+template <int NS, class K>
+__device__ __forceinline__ void take_best(const Chooser& c, K* key, int* slot, K* slot_key) {
   *slot = -1;
-  K last = 0;
-  for (int j = 0; j <= c.k; ++j) {                // one more than is taken: the first that is not
+  for (int j = 0; j < c.k; ++j) {
     int e;
     const K best = warp_best<NS>(key, c.lane, &e);
     if (!best) break;
-    if (j > 0 && !far(last, best)) sure = false;
-    if (j == c.k) break;
-    last = best;
 #pragma unroll
     for (int i = 0; i < NS; ++i)
       if (c.lane + 32 * i == e) key[i] = 0;
@@ -165,7 +164,90 @@ __device__ __forceinline__ bool choose(const Chooser& c, K* key, Score score, Fa
       *slot_key = best;
     }
   }
-  return sure;
+}
+
+// The same from sorted lists: a lane sorts its keys once (NS = 8: 19 comparisons, of which each takes two instructions),
+// after that a step looks at one key per lane instead of NS.  The keys are kept.  Returns
+//   kSure  every key was `far` enough above the next one, the first that is not taken among them
+//   kNear  some were not, but the `count` slots filled (k or more) are far above whatever follows: the choice is among them
+//   kEqual equal keys followed one another (the slots are not valid), or 32 slots did not separate the choice
+enum { kSure, kNear, kEqual };
+template <int NS, class Far>
+__device__ __forceinline__ int take_best_sorted(const Chooser& c, const uint32_t* key, Far far, int* slot, uint32_t* slot_key, int* count) {
+  static_assert(NS == 4 || NS == 8, "sorting networks");
+  uint32_t s[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) s[i] = key[i];
+  auto order = [&](int x, int y) {
+    const uint32_t hi = max(s[x], s[y]);
+    s[y] = min(s[x], s[y]);
+    s[x] = hi;
+  };
+  if constexpr (NS == 8) {
+    order(0, 1), order(2, 3), order(4, 5), order(6, 7);
+    order(0, 2), order(1, 3), order(4, 6), order(5, 7);
+    order(1, 2), order(5, 6), order(0, 4), order(3, 7);
+    order(1, 5), order(2, 6);
+    order(1, 4), order(3, 6);
+    order(2, 4), order(3, 5);
+    order(3, 4);
+  } else {
+    order(0, 1), order(2, 3);
+    order(0, 2), order(1, 3);
+    order(1, 2);
+  }
+  int how = kSure, source = 0, j = 0;             // source: lane that had slot j's key
+  uint32_t mine = 0, last = 0;
+  for (;; ++j) {
+    const uint32_t best = __reduce_max_sync(0xffffffffu, s[0]);
+    if (!best) break;
+    if (j > 0) {
+      const bool apart = far(last, best);
+      if (j >= c.k && apart) break;               // the first that is not taken
+      if (!apart) how = last == best || how == kEqual ? kEqual : kNear;
+      if (how == kEqual) break;
+    }
+    if (j == 32) {
+      how = kEqual;
+      break;
+    }
+    last = best;
+    const int w = __ffs((int)__ballot_sync(0xffffffffu, s[0] == best)) - 1;
+    if (c.lane == w) {
+#pragma unroll
+      for (int i = 0; i + 1 < NS; ++i) s[i] = s[i + 1];
+      s[NS - 1] = 0;
+    }
+    if (c.lane == j) {
+      source = w;
+      mine = best;
+    }
+  }
+  *slot = -1;
+  *slot_key = mine;
+  *count = j;
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const uint32_t v = __shfl_sync(0xffffffffu, key[i], source);
+    if (mine && v == mine) *slot = source + 32 * i;
+  }
+  return how;
+}
+
+// Puts the first `count` slots in the order of exact keys; equal keys: lower expert first.
+__device__ __forceinline__ void order_slots(double key, int count, int lane, int* slot) {
+  int rank = lane < count ? 0 : 32;
+  for (int i = 0; i < count; ++i) {
+    const double k = __shfl_sync(0xffffffffu, key, i);
+    const int e = __shfl_sync(0xffffffffu, *slot, i);
+    if (lane < count && (k > key || (k == key && e < *slot))) ++rank;
+  }
+  const int had = *slot;
+  *slot = -1;
+  for (int i = 0; i < count; ++i) {
+    const int r = __shfl_sync(0xffffffffu, rank, i), e = __shfl_sync(0xffffffffu, had, i);
+    if (r == lane) *slot = e;
+  }
 }
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -217,14 +299,15 @@ __device__ __noinline__ int choose_exactly(const RouteArgs& a, int64_t t, const 
     if (a.bias && l[i] > -INFINITY && e < a.E) v = p_of(v) + (double)a.bias[e];
     key[i] = l[i] > -INFINITY && v > -INFINITY ? ordered(v + 0.0) : 0ull;
   }
+  if (c.groups > 1)
+    keep_groups<NS>(c, key, [&](uint64_t first, uint64_t second) {
+      if (c.group_best == 1 || (!second && a.bias)) return first;
+      const double u = from_ordered(first), v = from_ordered(second);
+      return ordered((a.bias ? u + v : second ? p_of(u) + p_of(v) : p_of(u)) + 0.0);
+    }, [](uint64_t, uint64_t) { return true; });
   int slot;
   uint64_t slot_key;
-  auto always = [](uint64_t, uint64_t) { return true; };
-  choose<NS, true>(c, key, [&](uint64_t first, uint64_t second) {
-    if (c.group_best == 1 || (!second && a.bias)) return first;
-    const double u = from_ordered(first), v = from_ordered(second);
-    return ordered((a.bias ? u + v : second ? p_of(u) + p_of(v) : p_of(u)) + 0.0);
-  }, always, always, &slot, &slot_key);
+  take_best<NS>(c, key, &slot, &slot_key);
   return slot;
 }
 
@@ -259,8 +342,13 @@ __global__ void __launch_bounds__(128) score_kernel(const __grid_constant__ Rout
     uint32_t key[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) key[i] = l[i] > -INFINITY ? ordered(l[i]) : 0u;
-    auto always = [](uint32_t, uint32_t) { return true; };
-    choose<NS, false>(c, key, [](uint32_t first, uint32_t) { return first; }, always, always, &my_id, &my_key);
+    if constexpr (NS >= 4) {
+      int count;
+      if (take_best_sorted<NS>(c, key, [](uint32_t x, uint32_t y) { return x > y; }, &my_id, &my_key, &count) != kSure)
+        take_best<NS>(c, key, &my_id, &my_key);
+    } else {
+      take_best<NS>(c, key, &my_id, &my_key);
+    }
   } else {
     auto p_of = [&](float v) { return a.sigmoid ? __fdividef(1.f, 1.f + __expf(-v)) : __fdividef(__expf(v - top), total); };
     // Error of p in 32 bits, in half steps of 1: the fast exponential 4 and its argument's two roundings 0.37 * 2 (their
@@ -284,18 +372,51 @@ __global__ void __launch_bounds__(128) score_kernel(const __grid_constant__ Rout
     if (a.bias) size = warp_max(size);
     const float apart = 2.f * (32.f + size) * kHalfStep;
     // without a bias the keys are exact, and so is a group's best; a sum of two scores never is
-    auto far = [&](uint32_t x, uint32_t y) { return !a.bias || from_ordered(x) - from_ordered(y) > apart; };
-    auto far_groups = [&](uint32_t x, uint32_t y) {
-      if (!a.bias && a.group_best == 1) return true;
-      const float u = from_ordered(x), v = from_ordered(y);
-      return u - v > 2.f * apart + (fabsf(u) + fabsf(v)) * kHalfStep;
-    };
-    const bool sure = choose<NS, true>(c, key, [&](uint32_t first, uint32_t second) -> uint32_t {
-      if (a.group_best == 1) return first;
-      const float u = from_ordered(first), v = second ? from_ordered(second) : 0.f;
-      const float s = a.bias ? (second ? u + v : u) : (second ? p_of(u) + p_of(v) : p_of(u));
-      return ordered(s + 0.f);
-    }, far, far_groups, &my_id, &my_key);
+    bool sure = true;
+    if (a.groups > 1)
+      sure = keep_groups<NS>(c, key, [&](uint32_t first, uint32_t second) -> uint32_t {
+        if (a.group_best == 1) return first;
+        const float u = from_ordered(first), v = second ? from_ordered(second) : 0.f;
+        const float x = a.bias ? (second ? u + v : u) : (second ? p_of(u) + p_of(v) : p_of(u));
+        return ordered(x + 0.f);
+      }, [&](uint32_t x, uint32_t y) {
+        if (!a.bias && a.group_best == 1) return true;
+        const float u = from_ordered(x), v = from_ordered(y);
+        return u - v > 2.f * apart + (fabsf(u) + fabsf(v)) * kHalfStep;
+      });
+    if (sure) {
+      auto far = [&](uint32_t x, uint32_t y) { return a.bias ? from_ordered(x) - from_ordered(y) > apart : x > y; };
+      if constexpr (NS >= 4) {
+        int count;
+        const int how = take_best_sorted<NS>(c, key, far, &my_id, &my_key, &count);
+        if (how != kSure) {
+          if (!a.bias) {
+            take_best<NS>(c, key, &my_id, &my_key);
+          } else if (how == kNear && a.sigmoid) {
+            // the scores of a few experts, each of its own logit, one per lane
+            double exact = 0.0;
+            if (lane < count) exact = 1.0 / (1.0 + exp(-(double)tidy(load1(a.logits, t * a.stride + my_id, a.type)))) + (double)a.bias[my_id];
+            order_slots(exact, count, lane, &my_id);
+            if (lane >= a.k) my_id = -1;
+          } else {
+            sure = false;
+          }
+        }
+      } else {
+        // (two strides: k searches are as short; one more for the first that is not taken)
+        Chooser more = c;
+        more.k = c.k + 1;
+        uint32_t copy[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) copy[i] = key[i];
+        my_id = -1;
+        take_best<NS>(more, copy, &my_id, &my_key);
+        const uint32_t next = __shfl_down_sync(0xffffffffu, my_id >= 0 ? my_key : 0u, 1);
+        const bool decided = !a.bias || lane >= c.k || my_id < 0 || !next || (lane < 31 && far(my_key, next));   // (no lane has slot 32)
+        sure = __all_sync(0xffffffffu, decided);
+        if (lane >= c.k) my_id = -1;
+      }
+    }
     if (!sure) my_id = choose_exactly<NS>(a, t, c, top);
   }
   // the logit of the chosen, slot j in lane j: the key itself where no bias is in it
