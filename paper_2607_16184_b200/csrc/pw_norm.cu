@@ -35,8 +35,15 @@ __device__ __forceinline__ float warp_add(float v) {
 //         lanes whatever the row's alignment is; entries 0..3 and 4..7 of a thread belong to one group each.
 // The loads of x, r and (for short rows) w are all issued before the first use; a thread of a long row has no registers
 // to keep w in across the sum and reads it afterwards.  TR = void: no residual.
+// Threads.  One vector each up to 4096 columns: more threads hide the latency of a short row better than longer threads
+// do.  Then CTAs of up to 512 threads, several on an SM, before larger ones: rows of 12672 bf16 take 36 us as 416 threads
+// of four vectors and 45 us as 800 of two (2048 rows; HBM 32).  Above 16384 columns only 1024 threads keep a thread's
+// share in its registers (1024 rows x 24576: 40 us, 53 us as 512 threads of up to eight; HBM 31).  Single-element accesses
+// take up to 1024 threads from 8192 columns on (478 rows x 12671, with codes: 23 us, 33 us as 512; 1024 x 24575: 78 us,
+// 291 us): they are bound by their instructions, 64 bytes of a row each.
+constexpr int norm_threads(bool vec, int vpt) { return vpt == 4 || (!vec && vpt == 2) ? 1024 : 512; }
 template <class TX, class TR, bool VEC, int VPT>
-__global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(norm_threads(VEC, VPT)) add_rmsnorm_kernel(const NormArgs a) {
   grid_dep_sync();      // the row may come from the kernel directly ahead
   grid_dep_trigger();
   constexpr bool kRes = !std::is_void<TR>::value;
@@ -49,6 +56,7 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
   const int H = a.H;
   float z[VPT][8];
   auto at = [&](int v, int j) { return VEC ? (v * (int)blockDim.x + tid) * 8 + j : ((v * n_warps + warp) * 8 + j) * 32 + lane; };
+  auto left = [&](int v, int j) { return H - at(v, 0) > j * 32; };   // !VEC: whether the row has entry j
   // the weights (the same row for every CTA: an L2 hit)
   constexpr bool kEarly = VPT <= 2;
   auto weights = [&](int v, float* w) {
@@ -70,8 +78,13 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
         t.get(w);
       }
     } else {
+      auto every = [&](auto* p) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = at(v, j) < H ? load1(a.w, at(v, j), a.w_type) : 0.f;
+        for (int j = 0; j < 8; ++j) w[j] = left(v, j) ? to_f32(p[j * 32]) : 0.f;
+      };
+      if (a.w_type == PW_F32) every(static_cast<const float*>(a.w) + at(v, 0));
+      else if (a.w_type == PW_F16) every(static_cast<const __half*>(a.w) + at(v, 0));
+      else every(static_cast<const __nv_bfloat16*>(a.w) + at(v, 0));
     }
   };
   float early[kEarly ? VPT : 1][8];
@@ -106,19 +119,16 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
     }
   } else {
 #pragma unroll
-    for (int v = 0; v < VPT; ++v)
+    for (int v = 0; v < VPT; ++v) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[v][j] = at(v, j) < H ? to_f32(x[at(v, j)]) : 0.f;
-    if constexpr (kRes) {
-      float b[VPT][8];
+      for (int j = 0; j < 8; ++j) z[v][j] = left(v, j) ? to_f32((x + at(v, 0))[j * 32]) : 0.f;
+      if constexpr (kRes) {
+        float b[8];
 #pragma unroll
-      for (int v = 0; v < VPT; ++v)
+        for (int j = 0; j < 8; ++j) b[j] = left(v, j) ? to_f32((r + at(v, 0))[j * 32]) : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) b[v][j] = at(v, j) < H ? to_f32(r[at(v, j)]) : 0.f;
-#pragma unroll
-      for (int v = 0; v < VPT; ++v)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[v][j] = __fadd_rn(z[v][j], b[v][j]);
+        for (int j = 0; j < 8; ++j) z[v][j] = __fadd_rn(z[v][j], b[j]);
+      }
     }
   }
   // sum of squares in 32 bits, in a fixed order: thread, warp, warps
@@ -136,9 +146,10 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
       if constexpr (VEC) {
         if (at(v, 0) < H) store8(a.r_out, row * a.r_out_stride + at(v, 0), type, z[v]);
       } else {
+        R* out = static_cast<R*>(a.r_out) + row * a.r_out_stride + at(v, 0);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (at(v, j) < H) store1(a.r_out, row * a.r_out_stride + at(v, j), type, z[v][j]);
+          if (left(v, j)) out[j * 32] = from_f32<R>(z[v][j]);
       }
     }
   }
@@ -163,9 +174,15 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
       if constexpr (VEC) {
         if (at(v, 0) < H) store8(a.y, row * a.y_stride + at(v, 0), a.y_type, z[v]);
       } else {
+        auto every = [&](auto* p) {
+          using Y = std::remove_pointer_t<decltype(p)>;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (at(v, j) < H) store1(a.y, row * a.y_stride + at(v, j), a.y_type, z[v][j]);
+          for (int j = 0; j < 8; ++j)
+            if (left(v, j)) p[j * 32] = from_f32<Y>(z[v][j]);
+        };
+        if (a.y_type == PW_F32) every(static_cast<float*>(a.y) + row * a.y_stride + at(v, 0));
+        else if (a.y_type == PW_F16) every(static_cast<__half*>(a.y) + row * a.y_stride + at(v, 0));
+        else every(static_cast<__nv_bfloat16*>(a.y) + row * a.y_stride + at(v, 0));
       }
     }
   }
@@ -203,7 +220,7 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
         if (lane == 0 && c < H) qs[c / kGroup] = scale;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (at(v, 4 * h + j) < H) q[at(v, 4 * h + j)] = (uint8_t)pack_e4m3(z[v][4 * h + j] * rinv, 0.f);
+          if (left(v, 4 * h + j)) (q + at(v, 0))[(4 * h + j) * 32] = (uint8_t)pack_e4m3(z[v][4 * h + j] * rinv, 0.f);
       }
     }
   }
@@ -211,14 +228,12 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(const NormArgs a) {
 
 template <class TX, class TR>
 static pw_status launch_norm(const NormArgs& a, bool vec, int T, cudaStream_t s) {
-  // Elements per thread: one vector up to 4096 columns (more threads hide the latency of a short row better than
-  // longer threads do), then as few as 512 threads allow.
   const int n8 = (a.H + 7) / 8;
-  const int vpt = n8 <= 512 ? 1 : n8 <= 1024 ? 2 : n8 <= 2048 ? 4 : 8;
+  const int vpt = n8 <= 512 ? 1 : n8 <= (vec ? 1024 : 2048) ? 2 : 4;
   const int threads = ((n8 + vpt - 1) / vpt + 31) / 32 * 32;
   void (*k)(NormArgs);
-  if (vec) k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, true, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, true, 2> : vpt == 4 ? add_rmsnorm_kernel<TX, TR, true, 4> : add_rmsnorm_kernel<TX, TR, true, 8>;
-  else k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, false, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, false, 2> : vpt == 4 ? add_rmsnorm_kernel<TX, TR, false, 4> : add_rmsnorm_kernel<TX, TR, false, 8>;
+  if (vec) k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, true, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, true, 2> : add_rmsnorm_kernel<TX, TR, true, 4>;
+  else k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, false, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, false, 2> : add_rmsnorm_kernel<TX, TR, false, 4>;
   PW_CUDA_OK(launch_dependent(k, dim3(T), dim3(threads), 0, s, a));
   return PW_OK;
 }

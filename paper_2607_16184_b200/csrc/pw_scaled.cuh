@@ -41,6 +41,12 @@ __device__ __forceinline__ float abs_max(float m, float v) { return fmaxf(m, fab
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <class T>
+__device__ __forceinline__ T from_f32(float v) {          // to nearest, ties to even
+  if constexpr (std::is_same<T, float>::value) return v;
+  else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(v);
+  else return __float2bfloat16_rn(v);
+}
 
 // Eight consecutive elements as they lie in memory (16 or 32 bytes): loads of several of these stay in flight
 // together, the conversion comes afterwards.
