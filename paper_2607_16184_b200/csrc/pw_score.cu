@@ -3,11 +3,14 @@
 //   p = softmax(l) or 1 / (1 + exp(-l))      key = p + bias      gate = p [/ sum of the chosen p] * scale
 //
 // One warp per token, expert e in lane e mod 32.  A row of logits is read once and 8 k bytes are written per token: a
-// batch of a few hundred tokens costs a launch and one round trip to memory, a long prompt the instructions of the
-// selections.  Which of two near scores is larger decides whole numbers, so the choice has to be that of exact keys:
-// without a bias the keys are the logits themselves (both scores grow with the logit); otherwise they are computed in
-// 32 bits together with a bound of their error, and a token for which two keys that decide anything are closer than that
-// is done again in 64 bits (4096 tokens x 256 experts in 8 groups, everything in 64 bits: 28.4 us).
+// batch of a few hundred tokens costs a launch, one round trip to memory and a chain of warp-wide steps of 30 cycles each,
+// a long prompt the instructions of the selections.  Which of two near scores is larger decides whole numbers, so the
+// choice has to be that of exact keys: without a bias the keys are the logits themselves (both scores grow with the
+// logit); otherwise they are computed in 32 bits together with a bound of their error.  Where two keys or two groups that
+// decide anything are closer than that, the few experts concerned are computed in 64 bits, one per lane, and where that
+// does not settle it either the whole token is.
+// 4096 tokens x 256 experts in 8 groups: 10.1 us (everything in 64 bits 28.4, every unsettled token in 64 bits 13.5), one
+// token 4.8; without groups 9.3, without bias either 6.3; 4.2 MB read at the copy rate: 0.7.
 #include "pw_scaled.cuh"
 
 namespace pw {
@@ -22,7 +25,7 @@ struct RouteArgs {
   float* gates;
   int64_t stride;
   int T, E, k, type, sigmoid, groups, top_groups, group_best, renorm;
-  int group_strides;
+  int group_lanes, group_pitch;    // groups of experts in shared memory: see keep_groups
   uint32_t per_inverse;
   float scale;
 };
@@ -66,85 +69,103 @@ __device__ __forceinline__ K warp_best(const K* key, int lane, int* expert) {
 }
 // What the choice of one token needs beyond its keys.
 struct Chooser {
-  int groups, top_groups, group_best, k, lane;
-  int strides;                    // 32-expert strides of a group, 0 where groups do not consist of whole ones
+  int groups, per, top_groups, group_best, k, lane;
+  int lanes, pitch;               // lanes that look through a group, words from a group's keys to the next one's
   uint32_t per_inverse;           // e / (experts of a group) = e * per_inverse >> 32 for every e < 256; 0: groups of one
   __device__ __forceinline__ int group_of(int e) const { return per_inverse ? (int)__umulhi((uint32_t)e, per_inverse) : e; }
 };
 
-// Clears the keys of all but the best top_groups groups.  `score(first, second)`: a group's score, as a key, of its two
-// best keys.  `far(a, b)`: whether the score a is larger than the next one, b, beyond doubt; false when the decision was
-// not.
-template <int NS, class K, class Score, class Far>
-__device__ __forceinline__ bool keep_groups(const Chooser& c, K* key, Score score, Far far) {
-  // the two best keys of the groups lane, lane + 32, .., then their scores, all groups at once
-  K mine[NS], second[NS];
+// Clears the keys of all but the best top_groups groups; equal scores: lower group first.  `score(first, second)`: a
+// group's score, as a key, of its two best keys (second 0: none, or only the best counts).
+template <int NS, class K, class Score>
+__device__ __forceinline__ void keep_groups_exactly(const Chooser& c, K* key, Score score) {
+  // scores of the groups lane, lane + 32, ..
+  K mine[NS];
   int group[NS];
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     group[i] = c.group_of(c.lane + 32 * i);
-    mine[i] = second[i] = 0;
+    mine[i] = 0;
   }
-  auto two_best = [&](K b1, K b2, K* first, K* next) {
-    *first = warp_max_key(b1);
-    const uint32_t holders = __ballot_sync(0xffffffffu, b1 == *first);
-    *next = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
-  };
-  if (c.strides == 1) {
-    // a stride is a group: nothing to look for, and the groups' reductions overlap
+#pragma unroll 1
+  for (int g = 0; g < c.groups; ++g) {
+    K b1 = 0, b2 = 0;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      K first, next;
-      two_best(key[i], (K)0, &first, &next);
-      if (c.lane == i) {
-        mine[0] = first;
-        second[0] = next;
-      }
+      const K k = group[i] == g ? key[i] : (K)0;
+      b2 = k > b1 ? b1 : k > b2 ? k : b2;
+      b1 = k > b1 ? k : b1;
     }
-  } else {
-#pragma unroll 1
-    for (int g = 0; g < c.groups; ++g) {
-      K b1 = 0, b2 = 0, first, next;
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        const K k = group[i] == g ? key[i] : (K)0;
-        b2 = k > b1 ? b1 : k > b2 ? k : b2;
-        b1 = k > b1 ? k : b1;
-      }
-      two_best(b1, b2, &first, &next);
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-        if (c.lane + 32 * i == g) {
-          mine[i] = first;
-          second[i] = next;
-        }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < NS; ++i)
-    if (i == 0 || c.groups > 32) mine[i] = mine[i] ? score(mine[i], second[i]) : (K)0;
-  K last = 0, next = 0;
-  uint32_t keep = 0;                            // bit i: the group of my expert i stays
-  for (int j = 0; j <= c.top_groups; ++j) {     // one more than is kept: the best that is not
-    int g;
-    next = c.groups <= 32 ? warp_best<1>(mine, c.lane, &g) : warp_best<NS>(mine, c.lane, &g);
-    if (!next || j == c.top_groups) break;      // only groups without an expert are left, or enough
-    last = next;
-    if (c.groups <= 32) {
-      if (c.lane == g) mine[0] = 0;
-    } else {
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-        if (c.lane + 32 * i == g) mine[i] = 0;
-    }
+    const K first = warp_max_key(b1);
+    const uint32_t holders = __ballot_sync(0xffffffffu, b1 == first);
+    const K second = c.group_best == 2 ? warp_max_key(c.lane == __ffs((int)holders) - 1 ? b2 : b1) : (K)0;
+    const K s = first ? score(first, second) : (K)0;
 #pragma unroll
     for (int i = 0; i < NS; ++i)
+      if (c.lane + 32 * i == g) mine[i] = s;
+  }
+  uint32_t keep = 0;                            // bit i: the group of my expert i stays
+  for (int j = 0; j < c.top_groups; ++j) {
+    int g;
+    if (!warp_best<NS>(mine, c.lane, &g)) break;   // only groups without an expert are left
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      if (c.lane + 32 * i == g) mine[i] = 0;
       if (group[i] == g) keep |= 1u << i;
+    }
   }
 #pragma unroll
   for (int i = 0; i < NS; ++i)
     if (!((keep >> i) & 1u)) key[i] = 0;
-  return !next || far(last, next);
+}
+
+// The same for up to 32 groups and keys that may be off.  The keys change places by way of shared memory: `lanes` lanes
+// (32 over the groups' number, rounded up to a power of two) look through a group and join their two best; `pitch` is an
+// odd multiple of `lanes`, so that all of them read different banks.  A group's rank is the number of groups before it.
+// `far(a, b)`: whether the score a is larger than b beyond doubt.  When that does not settle the last group that stays
+// against the first that does not, `settle` decides on those in doubt (score and group of a lane, the two scores at the
+// cut, the groups that stay as bits lanes * group); false: it could not.
+template <int NS, class Score, class Far, class Settle>
+__device__ __forceinline__ bool keep_groups(const Chooser& c, uint32_t* key, uint32_t* mem, Score score, Far far, Settle settle) {
+  int bit[NS];                                  // of my expert's group
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const int e = c.lane + 32 * i, g = c.group_of(e);
+    bit[i] = g < c.groups ? g * c.lanes : 0;
+    if (g < c.groups) mem[g * c.pitch + e - g * c.per] = key[i];
+  }
+  __syncwarp();
+  const int shift = __ffs(c.lanes) - 1, g = c.lane >> shift, part = c.lane & (c.lanes - 1);
+  uint32_t b1 = 0, b2 = 0;
+  if (g < c.groups) {
+#pragma unroll 4
+    for (int o = part; o < c.per; o += c.lanes) {
+      const uint32_t k = mem[g * c.pitch + o];
+      b2 = max(b2, min(b1, k));
+      b1 = max(b1, k);
+    }
+  }
+  for (int d = 1; d < c.lanes; d <<= 1) {
+    const uint32_t o1 = __shfl_xor_sync(0xffffffffu, b1, d), o2 = __shfl_xor_sync(0xffffffffu, b2, d);
+    b2 = max(min(b1, o1), max(b2, o2));
+    b1 = max(b1, o1);
+  }
+  const uint32_t s = b1 ? score(b1, c.group_best == 2 ? b2 : 0u) : 0u;
+  int rank = 0;
+#pragma unroll 4
+  for (int h = 0; h < c.groups; ++h) {
+    const uint32_t o = __shfl_sync(0xffffffffu, s, h << shift);
+    rank += o > s || (o == s && h < g);
+  }
+  const bool stays = s && rank < c.top_groups;
+  uint32_t kept = __ballot_sync(0xffffffffu, stays && part == 0);
+  const uint32_t last = __reduce_min_sync(0xffffffffu, stays ? s : 0xffffffffu), next = __reduce_max_sync(0xffffffffu, stays ? 0u : s);
+  bool sure = !next || far(last, next);         // (a group is left out: then top_groups stay)
+  if (!sure) sure = settle(s, g, part == 0, last, next, &kept);
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (!((kept >> bit[i]) & 1u)) key[i] = 0;
+  return sure;
 }
 
 // The experts of slots 0 .. k - 1 and their keys (slot j in lane j; -1: none left), by k searches for the largest key.
@@ -280,10 +301,18 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int l
   for (int i = 0; i < NS; ++i) l[i] = tidy(l[i]);
 }
 
+// The experts' biases, all loads in flight together.
+template <int NS>
+__device__ __forceinline__ void load_bias(const RouteArgs& a, int lane, float* b) {
+#pragma unroll
+  for (int i = 0; i < NS; ++i) b[i] = a.bias && lane + 32 * i < a.E ? a.bias[lane + 32 * i] : 0.f;
+}
+
 // The choice with everything in 64 bits.
 template <int NS>
 __device__ __noinline__ int choose_exactly(const RouteArgs& a, int64_t t, const Chooser& c, float top) {
-  float l[NS];
+  float l[NS], b[NS];
+  load_bias<NS>(a, c.lane, b);
   load_logits<NS>(a, t, c.lane, l);
   double total = 0.0;
 #pragma unroll
@@ -294,35 +323,60 @@ __device__ __noinline__ int choose_exactly(const RouteArgs& a, int64_t t, const 
   uint64_t key[NS];
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
-    const int e = c.lane + 32 * i;
     double v = l[i];
-    if (a.bias && l[i] > -INFINITY && e < a.E) v = p_of(v) + (double)a.bias[e];
+    if (a.bias && l[i] > -INFINITY) v = p_of(v) + (double)b[i];
     key[i] = l[i] > -INFINITY && v > -INFINITY ? ordered(v + 0.0) : 0ull;
   }
   if (c.groups > 1)
-    keep_groups<NS>(c, key, [&](uint64_t first, uint64_t second) {
+    keep_groups_exactly<NS>(c, key, [&](uint64_t first, uint64_t second) {
       if (c.group_best == 1 || (!second && a.bias)) return first;
       const double u = from_ordered(first), v = from_ordered(second);
       return ordered((a.bias ? u + v : second ? p_of(u) + p_of(v) : p_of(u)) + 0.0);
-    }, [](uint64_t, uint64_t) { return true; });
+    });
   int slot;
   uint64_t slot_key;
   take_best<NS>(c, key, &slot, &slot_key);
   return slot;
 }
 
+// Exact score (and bias) of one expert per lane, e < 0: none (0 then).  Without a bias softmax scores keep their common
+// denominator.
+template <int NS>
+__device__ __noinline__ double exact_key(const RouteArgs& a, int64_t t, int lane, float top, int e) {
+  double total = 1.0;
+  if (!a.sigmoid && a.bias) {
+    float l[NS];
+    load_logits<NS>(a, t, lane, l);
+    total = 0.0;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (l[i] > -INFINITY) total += exp((double)l[i] - (double)top);
+    total = warp_sum(total);
+  }
+  double key = 0.0;
+  if (e >= 0) {
+    const double v = tidy(load1(a.logits, t * a.stride + e, a.type));
+    key = a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - (double)top) / total;
+    if (a.bias) key += (double)a.bias[e];
+  }
+  return key;
+}
+
+// (Seven CTAs on an SM: 4096 tokens are one wave, and only choose_exactly would want more than 72 registers; five CTAs of
+// 96 registers 11.7 us, eight 10.6.)
 // NS = 32-expert strides a lane holds.  PLAIN: no bias and no groups, nothing but the logits decides (a program a third
 // as long: one token 1.9 us instead of 2.4, most of it instructions on their way to the SM).
 template <int NS, bool PLAIN>
-__global__ void __launch_bounds__(128) score_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(128, 7) score_kernel(const __grid_constant__ RouteArgs a) {
   grid_dep_sync();
   grid_dep_trigger();
   const int64_t t = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (t >= a.T) return;
-  float l[NS];
+  float l[NS], b[PLAIN ? 1 : NS];
+  if constexpr (!PLAIN) load_bias<NS>(a, lane, b);
   load_logits<NS>(a, t, lane, l);
-  const Chooser c{a.groups, a.top_groups, a.group_best, a.k, lane, a.group_strides, a.per_inverse};
+  const Chooser c{a.groups, a.E / a.groups, a.top_groups, a.group_best, a.k, lane, a.group_lanes, a.group_pitch, a.per_inverse};
   // softmax: the largest logit, and the sum of exp(l - top) where something needs it
   float top = -INFINITY, total = 1.f;
   if (!a.sigmoid) {
@@ -360,43 +414,83 @@ __global__ void __launch_bounds__(128) score_kernel(const __grid_constant__ Rout
     float size = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      const int e = lane + 32 * i;
       float v = l[i];
-      if (a.bias && v > -INFINITY && e < a.E) {
-        v = p_of(v) + a.bias[e];
-        if (!(v > -INFINITY)) v = -INFINITY;        // a bias that is no number: never chosen
-        else size = fmaxf(size, fabsf(v));
+      if (a.bias) {
+        v = v > -INFINITY ? p_of(v) + b[i] : v;
+        v = v > -INFINITY ? v : -INFINITY;          // a bias that is no number: never chosen
+        size = v > -INFINITY ? fmaxf(size, fabsf(v)) : size;
       }
       key[i] = v > -INFINITY ? ordered(v + 0.f) : 0u;
     }
     if (a.bias) size = warp_max(size);
     const float apart = 2.f * (32.f + size) * kHalfStep;
+    auto far_keys = [&](uint32_t x, uint32_t y) { return a.bias ? from_ordered(x) - from_ordered(y) > apart : x > y; };
     // without a bias the keys are exact, and so is a group's best; a sum of two scores never is
-    bool sure = true;
-    if (a.groups > 1)
-      sure = keep_groups<NS>(c, key, [&](uint32_t first, uint32_t second) -> uint32_t {
+    bool sure = a.groups <= 32;
+    if (sure && a.groups > 1) {
+      __shared__ uint32_t mem[4][kMaxRouteExperts + 64];
+      auto far_scores = [&](uint32_t x, uint32_t y) {
+        if (!a.bias && a.group_best == 1) return true;
+        const float u = from_ordered(x), v = from_ordered(y);
+        return u - v > 2.f * apart + (fabsf(u) + fabsf(v)) * kHalfStep;
+      };
+      sure = keep_groups<NS>(c, key, mem[threadIdx.x >> 5], [&](uint32_t first, uint32_t second) -> uint32_t {
         if (a.group_best == 1) return first;
         const float u = from_ordered(first), v = second ? from_ordered(second) : 0.f;
         const float x = a.bias ? (second ? u + v : u) : (second ? p_of(u) + p_of(v) : p_of(u));
         return ordered(x + 0.f);
-      }, [&](uint32_t x, uint32_t y) {
-        if (!a.bias && a.group_best == 1) return true;
-        const float u = from_ordered(x), v = from_ordered(y);
-        return u - v > 2.f * apart + (fabsf(u) + fabsf(v)) * kHalfStep;
+      }, far_scores, [&](uint32_t s, int g, bool first_lane, uint32_t last, uint32_t next, uint32_t* kept) {
+        // A group beyond doubt above the last that stays is above all that are not larger than it: it stays; one as far
+        // below the first that does not stay goes.  Of the others the exact scores decide, from the exact keys of their
+        // two best, two lanes each, if it is beyond doubt which two those are.
+        const bool in_doubt = s && first_lane && !far_scores(s, last) && !far_scores(next, s);
+        uint32_t left = __ballot_sync(0xffffffffu, in_doubt);
+        const uint32_t above = *kept & ~left;
+        if (__popc(left) > 16) return false;
+        int my_expert = -1, my_bit = 0, n = 0;
+#pragma unroll 1
+        for (; left; left &= left - 1, ++n) {
+          const int bit = __ffs((int)left) - 1, group = __shfl_sync(0xffffffffu, g, bit);
+          uint32_t k[NS], best[3];
+          int e[3];
+#pragma unroll
+          for (int i = 0; i < NS; ++i) k[i] = c.group_of(lane + 32 * i) == group ? key[i] : 0u;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) {
+            best[j] = warp_best<NS>(k, lane, &e[j]);
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+              if (lane + 32 * i == e[j]) k[i] = 0;
+          }
+          const int taken = a.group_best - 1;
+          if (a.bias && best[taken] && best[taken + 1] && !far_keys(best[taken], best[taken + 1])) return false;
+          if ((lane >> 1) == n) {
+            my_bit = bit;
+            my_expert = !(lane & 1) ? e[0] : a.group_best == 2 && best[1] ? e[1] : -1;
+          }
+        }
+        double exact = exact_key<NS>(a, t, lane, top, my_expert);
+        exact += __shfl_xor_sync(0xffffffffu, exact, 1);
+        int before = 0;
+        for (int j = 0; j < n; ++j) {
+          const double o = __shfl_sync(0xffffffffu, exact, 2 * j);
+          before += o > exact || (o == exact && j < (lane >> 1));
+        }
+        const bool goes_in = (lane >> 1) < n && before < a.top_groups - __popc(above);
+        *kept = above | __reduce_or_sync(0xffffffffu, goes_in ? 1u << my_bit : 0u);
+        return true;
       });
+    }
     if (sure) {
-      auto far = [&](uint32_t x, uint32_t y) { return a.bias ? from_ordered(x) - from_ordered(y) > apart : x > y; };
       if constexpr (NS >= 4) {
         int count;
-        const int how = take_best_sorted<NS>(c, key, far, &my_id, &my_key, &count);
+        const int how = take_best_sorted<NS>(c, key, far_keys, &my_id, &my_key, &count);
         if (how != kSure) {
           if (!a.bias) {
             take_best<NS>(c, key, &my_id, &my_key);
-          } else if (how == kNear && a.sigmoid) {
-            // the scores of a few experts, each of its own logit, one per lane
-            double exact = 0.0;
-            if (lane < count) exact = 1.0 / (1.0 + exp(-(double)tidy(load1(a.logits, t * a.stride + my_id, a.type)))) + (double)a.bias[my_id];
-            order_slots(exact, count, lane, &my_id);
+          } else if (how == kNear) {
+            // the scores of a few experts, one per lane
+            order_slots(exact_key<NS>(a, t, lane, top, lane < count ? my_id : -1), count, lane, &my_id);
             if (lane >= a.k) my_id = -1;
           } else {
             sure = false;
@@ -412,7 +506,7 @@ __global__ void __launch_bounds__(128) score_kernel(const __grid_constant__ Rout
         my_id = -1;
         take_best<NS>(more, copy, &my_id, &my_key);
         const uint32_t next = __shfl_down_sync(0xffffffffu, my_id >= 0 ? my_key : 0u, 1);
-        const bool decided = !a.bias || lane >= c.k || my_id < 0 || !next || (lane < 31 && far(my_key, next));   // (no lane has slot 32)
+        const bool decided = !a.bias || lane >= c.k || my_id < 0 || !next || (lane < 31 && far_keys(my_key, next));   // (no lane has slot 32)
         sure = __all_sync(0xffffffffu, decided);
         if (lane >= c.k) my_id = -1;
       }
@@ -504,7 +598,9 @@ extern "C" pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const 
   a.groups = r.top_groups == r.n_groups ? 1 : r.n_groups;   // every group stays: nothing to choose
   a.top_groups = r.top_groups;
   const int per = r.n_experts / a.groups;
-  a.group_strides = per % 32 == 0 ? per / 32 : 0;
+  a.group_lanes = 32;
+  while (a.group_lanes > 1 && a.group_lanes * a.groups > 32) a.group_lanes /= 2;
+  a.group_pitch = ((per + a.group_lanes - 1) / a.group_lanes | 1) * a.group_lanes;   // groups <= 32: below 256 + 64 words in all
   a.per_inverse = per > 1 ? (uint32_t)((0x100000000ull + per - 1) / per) : 0u;   // exact for numerators below 256
   a.group_best = r.group_best;
   a.renorm = r.renormalize != 0;

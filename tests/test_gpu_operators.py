@@ -354,6 +354,32 @@ def test_router_near_ties(ctx, score, group_best):
         np.testing.assert_allclose(gates.cpu().numpy(), ref_gates, rtol=52 * U)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_best", [1, 2])
+@pytest.mark.parametrize("E,n_groups,top_groups", [(256, 8, 4), (160, 8, 3), (96, 3, 2), (64, 32, 7), (256, 16, 15), (250, 2, 1), (128, 64, 5)])
+def test_router_groups_close(ctx, score, group_best, E, n_groups, top_groups):
+    """Groups whose scores differ by a few steps of 32 bits or not at all: the same logits in every group, in another
+    order, some of them moved by up to three steps; in a third of the rows one group is far above, one masked."""
+    T, per = 120, E // n_groups
+    gen = torch.Generator().manual_seed(E + n_groups)
+    base = torch.randn(T, 1, per, generator=gen).expand(T, n_groups, per).clone()
+    for _ in range(3):
+        move = torch.rand(base.shape, generator=gen) < 0.3
+        base = torch.where(move, torch.nextafter(base, torch.full_like(base, math.inf)), base)
+    base[1::3, n_groups // 2] += 0.5
+    base[2::3, n_groups - 1] = -math.inf
+    bias = torch.randn(per, generator=gen) * 0.1               # goes with the logit
+    order = torch.argsort(torch.rand(n_groups, per, generator=gen), dim=1)
+    x = torch.gather(base, 2, order.expand(T, n_groups, per)).reshape(T, E).cuda()
+    for b in (None, bias[order].reshape(E).cuda()):
+        args = dict(score=score, n_groups=n_groups, top_groups=top_groups, group_best=group_best, renormalize=True, scale=1.0)
+        k = min(8, top_groups * per)
+        ids, gates = ctx.pw_route_tokens(x, k, bias=b, **args)
+        ref_ids, ref_gates = plain.route(x, k, bias=None if b is None else plain.f64(b), **args)
+        assert np.array_equal(ids.cpu().numpy(), ref_ids)
+        np.testing.assert_allclose(gates.cpu().numpy(), ref_gates, rtol=52 * U)
+
+
 def test_router_agrees_with_the_layers_own_rule(ctx):
     cfg = synth.CONFIGS["finegrained_decode"]
     logits = synth.router_logits(cfg, device="cuda")
