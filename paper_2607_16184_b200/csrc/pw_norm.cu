@@ -247,6 +247,18 @@ static pw_status launch_norm_r(const NormArgs& a, int r_type, bool vec, int T, c
 
 // ---- quantizer ---------------------------------------------------------------------------------
 
+// Four codes at column c of a row of codes (it starts on a 16-byte boundary; nothing is written behind its end).
+__device__ __forceinline__ void store_four(uint8_t* q, int c, int cols, const float* z, float rinv) {
+  const uint32_t o = pack_e4m3(z[0] * rinv, z[1] * rinv) | (pack_e4m3(z[2] * rinv, z[3] * rinv) << 16);
+  if (c + 4 <= cols) {
+    *reinterpret_cast<uint32_t*>(q + c) = o;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (c + k < cols) q[c + k] = (uint8_t)(o >> (8 * k));
+  }
+}
+
 struct QuantArgs {
   const void* x;
   uint8_t* q;
@@ -296,30 +308,27 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a, u
         *reinterpret_cast<uint2*>(q + c) = o;
       }
     } else {
-      TX raw[U * 8];
+      constexpr int N = U * 2;                     // groups
+      const int left = a.cols - c0;
+      x += c0;
+      TX raw[N][4];
 #pragma unroll
-      for (int i = 0; i < U * 8; ++i) {
-        const int c = c0 + i * 32 + lane;
-        raw[i] = c < a.cols ? x[c] : (TX)0.f;
-      }
+      for (int h = 0; h < N; ++h)
 #pragma unroll
-      for (int h = 0; h < U * 2; ++h) {            // groups
+        for (int j = 0; j < 4; ++j) raw[h][j] = h * kGroup + lane * 4 + j < left ? x[h * kGroup + lane * 4 + j] : (TX)0.f;
+#pragma unroll
+      for (int h = 0; h < N; ++h) {
         float z[4], top = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          z[j] = to_f32(raw[h * 4 + j]);
-          top = abs_max(top, z[j]);
-        }
+        for (int j = 0; j < 4; ++j) z[j] = to_f32(raw[h][j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = abs_max(top, z[j]);
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         const float scale = block_scale(top), rinv = __frcp_rn(scale);
         const int c = c0 + h * kGroup;
         if (lane == 0 && c < a.cols) qs[c / kGroup] = scale;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int cj = c + j * 32 + lane;
-          if (cj < a.cols) q[cj] = (uint8_t)pack_e4m3(z[j] * rinv, 0.f);
-        }
+        store_four(q, c + lane * 4, a.cols, z, rinv);
       }
     }
   }
@@ -327,7 +336,8 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantArgs a, u
 
 // Blocks of 128 x 128: a CTA per block, 64 elements of it per thread, all loaded before the maximum is taken.
 //   VEC   half a warp per row, eight columns per lane, eight passes of 16 rows;
-//   else  a warp per row, every 32nd column per lane, 16 passes of 8 rows.
+//   else  a warp per row, two passes over the rows, the second from L1 or L2 (14336 x 4095 bf16: 61 us; all 64 elements
+//         of a thread kept in registers, two CTAs on an SM, 80 us).
 template <class TX, bool VEC>
 __global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantArgs a) {
   grid_dep_sync();
@@ -384,21 +394,23 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantArgs a)
       *reinterpret_cast<uint2*>(a.q + r * a.q_stride + c) = o;
     }
   } else {
-    TX raw[64];
+    const int n = (int)(a.rows - r0 < kTileRows ? a.rows - r0 : kTileRows);
+    const TX* block = x + r0 * a.x_stride + c0;
+    const int cols = a.cols - c0;
+#pragma unroll 4
+    for (int r = warp; r < n; r += 8) {
+      const TX* row = block + r * a.x_stride;
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-      const int64_t r = r0 + (i >> 2) * 8 + warp;
-      const int c = c0 + (i & 3) * 32 + lane;
-      raw[i] = r < a.rows && c < a.cols ? x[r * a.x_stride + c] : (TX)0.f;
+      for (int j = 0; j < 4; ++j) top = abs_max(top, j * 32 + lane < cols ? to_f32(row[j * 32 + lane]) : 0.f);
     }
-#pragma unroll
-    for (int i = 0; i < 64; ++i) top = abs_max(top, to_f32(raw[i]));
     const float rinv = scale_of_block(top);
+#pragma unroll 4
+    for (int r = warp; r < n; r += 8) {
+      const TX* row = block + r * a.x_stride;
+      float z[4];
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-      const int64_t r = r0 + (i >> 2) * 8 + warp;
-      const int c = c0 + (i & 3) * 32 + lane;
-      if (r < a.rows && c < a.cols) a.q[r * a.q_stride + c] = (uint8_t)pack_e4m3(to_f32(raw[i]) * rinv, 0.f);
+      for (int j = 0; j < 4; ++j) z[j] = lane * 4 + j < cols ? to_f32(row[lane * 4 + j]) : 0.f;
+      store_four(a.q + (r0 + r) * a.q_stride + c0, lane * 4, cols, z, rinv);
     }
   }
 }

@@ -51,7 +51,8 @@ def guards_left(whole, view, fill):
 
 @pytest.mark.parametrize("block_rows", [1, 128])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
-@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 128, 0), (3, 127, 1), (5, 129, 7), (130, 264, 8), (257, 520, 0), (33, 1408, 16), (300, 2055, 3)])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 128, 0), (3, 127, 1), (5, 129, 7), (130, 264, 8), (257, 520, 0), (33, 1408, 16), (300, 2055, 3), (67, 1001, 0),
+                                           (40, 2047, 0), (9, 1025, 2), (200, 3, 0), (150, 1, 0), (131, 5, 1), (140, 1023, 4)])
 def test_quantizer_bit_for_bit(ctx, rows, cols, pad, dtype, block_rows):
     x, _ = strided(rows, cols, pad, dtype)
     x.copy_(randn(rows * cols, rows, cols))
