@@ -319,7 +319,7 @@ static pw_status moe_forward(pw_ctx* ctx, int layer, const void* hidden, const R
   st = mode == PW_MODE_SIMT ? launch_ffn_simt(ctx, layer, T, top_k, stream)
                             : launch_ffn_tensor(ctx, layer, T, top_k, nt_tile, ksplit, stream);
   if (st != PW_OK) return st;
-  st = launch_combine(ctx, T, top_k, ksplit, out, stream);
+  st = launch_combine(ctx, !routing.logits, T, top_k, ksplit, out, stream);
   if (st != PW_OK) return st;
   st = launch_observe(ctx, layer, T, top_k, stream);
   ctx->last_T = T;

@@ -152,7 +152,7 @@ struct Routing {
 };
 pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int k, int nt_tile,
                        int ksplit, cudaStream_t s);
-pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cudaStream_t s);
+pw_status launch_combine(pw_ctx* ctx, bool given, int T, int k, int ksplit, float* out, cudaStream_t s);
 pw_status launch_observe(pw_ctx* ctx, int layer, int T, int k, cudaStream_t s);
 // residency records: the state of (row, bits) after looking at its transfer event; registration of a page
 // that is being committed (PW_ERR_STATE if the record says that page is away or on its way)

@@ -98,9 +98,11 @@ __device__ __forceinline__ void warp_exclusive_scan(const int32_t* in, int32_t* 
 // Single CTA.  Stable counting sort of the P = T*k pairs by expert (positions come from ordered
 // prefix counts, never from atomics), segment table including the shared experts, operand-row ->
 // token map, and the unit lists of the tensor-core kernels.  With `logits` given the CTA routes the tokens
-// itself first (a warp per token, 32 at a time): for a decode batch that is cheaper than a launch of its own.  With
-// `ids_in` given the caller has routed: its ids and gates are copied in, an id that is no expert becomes -1.  Such a
-// pair gets no operand row (inv_perm -1); the shared experts' rows follow the rows that there are.
+// itself first (a warp per token, 32 at a time): for a decode batch that is cheaper than a launch of its own.
+// GIVEN: the caller has routed.  Its ids and gates are copied in, an id that is no expert becomes -1.  Such a pair gets
+// no operand row (inv_perm -1); the shared experts' rows follow the rows that there are.  (A variant of its own: the
+// checks cost a one-token layer 0.7 us of 44.)
+template <bool GIVEN>
 __global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__ logits, const int32_t* ids_in,
                                                        const float* gates_in, float* __restrict__ gates,
                                                        int32_t* topk_ids, int T, int k, int E,
@@ -125,11 +127,11 @@ __global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__
   int32_t* order = ubase + S + 1;    // [S]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int P = T * k;
-  if (logits) {
+  if (!GIVEN && logits) {
     for (int t = warp; t < T; t += (int)(blockDim.x >> 5)) route_token(logits, t, E, k, topk_ids, gates, lane);
     __syncthreads();                                 // the pairs below are read back from global memory
   }
-  if (ids_in) {
+  if constexpr (GIVEN) {
     for (int p = tid; p < P; p += blockDim.x) {
       int id = ids_in[p];
       if (id < -1 || id >= E) {
@@ -147,7 +149,7 @@ __global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__
   __syncthreads();
   for (int p = tid; p < P; p += blockDim.x) {
     const int e = topk_ids[p];
-    if (e >= 0) atomicAdd(&cnt[e], 1);
+    if (!GIVEN || e >= 0) atomicAdd(&cnt[e], 1);
   }
   __syncthreads();
   if (warp == 0) warp_exclusive_scan(cnt, off, S, lane);
@@ -179,13 +181,14 @@ __global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__
       perm[pos] = p;
       inv_perm[p] = pos;
       row_token[pos] = p / k;
-    } else if (p < P) {
+    } else if (GIVEN && p < P) {
       inv_perm[p] = -1;
     }
     __syncthreads();
   }
-  const int R = off[S], routed = off[E];             // routed: the pairs that have an expert
-  for (int p = routed + tid; p < P; p += blockDim.x) perm[p] = -1;
+  const int R = off[S], routed = GIVEN ? off[E] : P;   // routed: the pairs that have an expert
+  if constexpr (GIVEN)
+    for (int p = routed + tid; p < P; p += blockDim.x) perm[p] = -1;
   for (int i = tid; i < n_shared * T; i += blockDim.x) row_token[routed + i] = i % T;
   for (int i = tid; i < kPadRows; i += blockDim.x) row_token[R + i] = -1;
 
@@ -328,7 +331,8 @@ __global__ void __launch_bounds__(256) gather_kernel(const uint4* __restrict__ h
 constexpr int kCombineCols = 64, kCombineRows = 4, kMaxSplit = 8;
 // kCombineChunks columns per thread, 64 apart: that many independent load chains in flight.  Four for a long
 // prompt (thousands of tokens: fewer, fatter CTAs), one for a decode batch (more CTAs for the few tokens).
-template <int kCombineChunks>
+// GIVEN: pairs without an expert (row -1) add nothing, whatever their gates say.
+template <int kCombineChunks, bool GIVEN>
 __global__ void __launch_bounds__(kCombineCols * kCombineRows)
     combine_kernel(const float4* y /* written by the kernel directly ahead */, const float* __restrict__ gates, const int32_t* __restrict__ inv_perm,
                    const int32_t* __restrict__ routed_rows, int T, int k, int n_shared, int H4, int ksplit, size_t split_stride4, float4* __restrict__ out) {
@@ -351,7 +355,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
         row = inv_perm[(size_t)t * k + j];
         g = gates[(size_t)t * k + j];
       } else {
-        row = *routed_rows + (j - k) * T + t;
+        row = (GIVEN ? *routed_rows : T * k) + (j - k) * T + t;
         g = 1.0f;
       }
 #pragma unroll
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
         float4 v[kMaxSplit];
 #pragma unroll
         for (int s = 0; s < kMaxSplit; ++s)
-          if (s < ksplit) v[s] = row >= 0 ? y[s * split_stride4 + (size_t)row * H4 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
+          if (s < ksplit) v[s] = !GIVEN || row >= 0 ? y[s * split_stride4 + (size_t)row * H4 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
         float4 a = v[0];
 #pragma unroll
         for (int s = 1; s < kMaxSplit; ++s)
@@ -371,7 +375,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
             a.z = __fadd_rn(a.z, v[s].z);
             a.w = __fadd_rn(a.w, v[s].w);
           }
-        if (row < 0) g = 0.f;                        // a pair without an expert adds nothing, whatever its gate says
+        if (GIVEN && row < 0) g = 0.f;
         term[ty][cc][tx] = make_float4(__fmul_rn(g, a.x), __fmul_rn(g, a.y), __fmul_rn(g, a.z), __fmul_rn(g, a.w));
       }
     }
@@ -401,7 +405,7 @@ __global__ void __launch_bounds__(kCombineCols * kCombineRows)
 // The same sum for batches with enough tokens to fill the machine by themselves: one thread per (token, float4
 // column), U expert choices in flight at a time, no shared memory and no barrier.  The arithmetic and its order
 // are those of combine_kernel (splits added in split order, times the gate, terms added in choice order).
-template <int U>
+template <int U, bool GIVEN>
 __global__ void __launch_bounds__(128)
     combine_stream_kernel(const float4* y /* written by the kernel directly ahead */, const float* __restrict__ gates, const int32_t* __restrict__ inv_perm,
                           const int32_t* __restrict__ routed_rows, int T, int k, int n_shared, int H4, int ksplit, size_t split_stride4, float4* __restrict__ out) {
@@ -413,30 +417,35 @@ __global__ void __launch_bounds__(128)
   const int J = k + n_shared;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int j0 = 0; j0 < J; j0 += U) {
-    int row[U];                                      // -1: a pair without an expert, adds nothing
+    size_t row[U];
+    bool on[U];
     float g[U];
     float4 a[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int j = j0 + i;
       if (j < k) {
-        row[i] = inv_perm[(size_t)t * k + j];
-        g[i] = row[i] >= 0 ? gates[(size_t)t * k + j] : 0.f;
+        const int r = inv_perm[(size_t)t * k + j];
+        row[i] = (size_t)r;
+        on[i] = !GIVEN || r >= 0;
+        g[i] = gates[(size_t)t * k + j];
       } else {
-        row[i] = j < J ? *routed_rows + (j - k) * T + t : -1;
+        row[i] = (size_t)(GIVEN ? *routed_rows : T * k) + (size_t)(j - k) * T + t;
+        on[i] = j < J;
         g[i] = 1.0f;
       }
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) a[i] = row[i] >= 0 ? y[(size_t)row[i] * H4 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < U; ++i)
+      if (on[i]) a[i] = y[row[i] * H4 + c];
     for (int sp = 1; sp < ksplit; ++sp) {
       float4 v[U];
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (row[i] >= 0) v[i] = y[sp * split_stride4 + (size_t)row[i] * H4 + c];
+        if (on[i]) v[i] = y[sp * split_stride4 + row[i] * H4 + c];
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (row[i] >= 0) {
+        if (on[i]) {
           a[i].x = __fadd_rn(a[i].x, v[i].x);
           a[i].y = __fadd_rn(a[i].y, v[i].y);
           a[i].z = __fadd_rn(a[i].z, v[i].z);
@@ -445,7 +454,7 @@ __global__ void __launch_bounds__(128)
     }
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (j0 + i < J) {
+      if (on[i]) {
         acc.x = __fadd_rn(acc.x, __fmul_rn(g[i], a[i].x));
         acc.y = __fadd_rn(acc.y, __fmul_rn(g[i], a[i].y));
         acc.z = __fadd_rn(acc.z, __fmul_rn(g[i], a[i].z));
@@ -475,7 +484,7 @@ pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const Routing
   const size_t smem = sizeof(int32_t) * ((size_t)S + (S + 1) + E + 32 * (size_t)E + (S + 1) + S);
   const DevRow* rows = reinterpret_cast<const DevRow*>(b + w.table) + (size_t)layer * S * 3;
   PW_CUDA_OK(launch_dependent(
-      permute_kernel, dim3(1), dim3(1024), smem, s, fused ? logits : static_cast<const float*>(nullptr),
+      logits ? permute_kernel<false> : permute_kernel<true>, dim3(1), dim3(1024), smem, s, fused ? logits : static_cast<const float*>(nullptr),
       logits ? static_cast<const int32_t*>(nullptr) : routing.ids, logits ? static_cast<const float*>(nullptr) : routing.gates,
       reinterpret_cast<float*>(b + w.gates), ids, T, k, E, c.n_shared, reinterpret_cast<int32_t*>(b + w.counts),
       reinterpret_cast<int32_t*>(b + w.offsets), reinterpret_cast<int32_t*>(b + w.perm),
@@ -500,7 +509,7 @@ pw_status launch_route(pw_ctx* ctx, int layer, const void* hidden, const Routing
   return PW_OK;
 }
 
-pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cudaStream_t s) {
+pw_status launch_combine(pw_ctx* ctx, bool given, int T, int k, int ksplit, float* out, cudaStream_t s) {
   const pw_config& c = ctx->cfg;
   const WsMap& w = ctx->ws;
   char* b = ctx->base;
@@ -510,7 +519,7 @@ pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cuda
   dim3 grid((H4 + kCombineCols * chunks - 1) / (kCombineCols * chunks), T);
   timing_mark(ctx, PW_K_COMBINE, s);
   if ((long long)T * ((H4 + 127) / 128) >= 2 * ctx->num_sms) {   // enough (token, column) CTAs to fill the machine
-    PW_CUDA_OK(launch_dependent(combine_stream_kernel<4>, dim3((H4 + 127) / 128, T), dim3(128), 0, s,
+    PW_CUDA_OK(launch_dependent(given ? combine_stream_kernel<4, true> : combine_stream_kernel<4, false>, dim3((H4 + 127) / 128, T), dim3(128), 0, s,
                                 reinterpret_cast<const float4*>(b + w.y), reinterpret_cast<const float*>(b + w.gates),
                                 reinterpret_cast<const int32_t*>(b + w.inv_perm),
                                 reinterpret_cast<const int32_t*>(b + w.offsets) + c.n_experts, T, k, c.n_shared, H4, ksplit,
@@ -519,10 +528,11 @@ pw_status launch_combine(pw_ctx* ctx, int T, int k, int ksplit, float* out, cuda
     PW_CUDA_OK(cudaGetLastError());
     return PW_OK;
   }
-  PW_CUDA_OK(launch_dependent(chunks == 4 ? combine_kernel<4> : combine_kernel<1>, grid, dim3(kCombineCols, kCombineRows), 0, s, reinterpret_cast<const float4*>(b + w.y),
+  auto kernel = given ? (chunks == 4 ? combine_kernel<4, true> : combine_kernel<1, true>) : (chunks == 4 ? combine_kernel<4, false> : combine_kernel<1, false>);
+  PW_CUDA_OK(launch_dependent(kernel, grid, dim3(kCombineCols, kCombineRows), 0, s, reinterpret_cast<const float4*>(b + w.y),
                               reinterpret_cast<const float*>(b + w.gates),
                               reinterpret_cast<const int32_t*>(b + w.inv_perm),
-                                reinterpret_cast<const int32_t*>(b + w.offsets) + c.n_experts, T, k, c.n_shared, H4, ksplit,
+                              reinterpret_cast<const int32_t*>(b + w.offsets) + c.n_experts, T, k, c.n_shared, H4, ksplit,
                               (size_t)R * H4, reinterpret_cast<float4*>(out)));
   ctx->launches += 1;
   PW_CUDA_OK(cudaGetLastError());
@@ -573,7 +583,7 @@ extern "C" pw_status pw_route_tokens_static(const float* router_logits, int T, i
   const int S = n_experts;
   const size_t smem = sizeof(int32_t) * ((size_t)S + (S + 1) + n_experts + 32 * (size_t)n_experts + (S + 1) + S);
   // the grouping kernel clears the counters it uses; everything else in the scratch is overwritten before it is read
-  permute_kernel<<<1, 1024, smem, stream>>>(nullptr, nullptr, nullptr, nullptr, topk_ids, T, top_k, n_experts, 0, counts, offsets, perm,
+  permute_kernel<false><<<1, 1024, smem, stream>>>(nullptr, nullptr, nullptr, nullptr, topk_ids, T, top_k, n_experts, 0, counts, offsets, perm,
                                             reinterpret_cast<int32_t*>(sc + kStaticInvPerm),
                                             reinterpret_cast<int32_t*>(sc + kStaticRowToken),
                                             reinterpret_cast<int32_t*>(sc + kStaticCounter), nullptr, 0, 0, 0, 1, nullptr,

@@ -463,6 +463,61 @@ def test_routed_layer_skips_pairs_without_an_expert(mode, T, n_shared):
         c.close()
 
 
+@pytest.mark.parametrize("mode", [B.PW_MODE_SIMT, B.PW_MODE_TENSOR])
+@pytest.mark.parametrize("T", [1, 9, 200])
+def test_routed_layer_with_an_expert_twice(mode, T):
+    """A caller's routing may name an expert twice, and one expert in every pair: its gates add up."""
+    cfg = synth.LayerConfig("ops_twice", 16, 4, 256, 384, T, n_shared=1, bit_rule="int4_10fp16_20int2")
+    c = make_ctx(cfg)
+    try:
+        pages, _ = build_layer(c, cfg)
+        x = synth.activations(cfg, device="cuda")
+        ids, gates = c.pw_route_tokens(synth.router_logits(cfg, device="cuda"), 4)
+        for same in ([0, 0, 2, 3], [0, 0, 0, 0]):
+            twice = ids[:, same] if same[2] else torch.full_like(ids, 11)
+            once, sums = twice.clone(), gates.clone()
+            for j in range(3, 0, -1):
+                dup = twice[:, j] == twice[:, 0]
+                once[dup, j] = -1
+                sums[:, 0] += torch.where(dup, gates[:, j], torch.zeros_like(gates[:, j]))
+            near(c.pw_moe_forward_routed(0, x, twice, gates, mode=mode), c.pw_moe_forward_routed(0, x, once, sums, mode=mode))
+        assert c.pw_last_device_status() == 0
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("mode", [B.PW_MODE_SIMT, B.PW_MODE_TENSOR])
+def test_routed_layer_replayed_with_other_ids(mode):
+    """Router and experts captured together: a replay takes the logits that are there then."""
+    cfg = synth.LayerConfig("ops_graph", 16, 4, 256, 384, 33, n_shared=1, bit_rule="int4_10fp16_20int2")
+    c = make_ctx(cfg)
+    try:
+        pages, _ = build_layer(c, cfg)
+        x, out = synth.activations(cfg, device="cuda"), torch.empty(33, 256, device="cuda")
+        ids, gates = torch.empty(33, 4, dtype=torch.int32, device="cuda"), torch.empty(33, 4, device="cuda")
+        logits = torch.zeros(33, 16, device="cuda")
+        s = torch.cuda.Stream()
+        step = lambda: (c.pw_route_tokens(logits, 4, ids=ids, gates=gates, stream=s), c.pw_moe_forward_routed(0, x, ids, gates, out=out, mode=mode, stream=s))
+        with torch.cuda.stream(s):
+            step()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            step()
+        for seed in (3, 4):
+            logits.copy_(randn(seed, 33, 16))
+            logits[7] = -math.inf                                      # a token without any expert
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            got, i, w = out.clone(), ids.clone(), gates.clone()
+            assert bool((i[7] == -1).all())
+            assert torch.equal(c.pw_moe_forward_routed(0, x, i, w, mode=mode), got)
+        assert c.pw_last_device_status() == 0
+    finally:
+        c.close()
+
+
 def test_routed_layer_refuses(ctx):
     x = torch.zeros(4, 256, dtype=F16, device="cuda")
     ids, gates = torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
