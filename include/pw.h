@@ -358,7 +358,7 @@ pw_status pw_add_rmsnorm(pw_ctx* ctx, int T, int H, const void* x, int x_type, i
  * block_rows 128 (the layout of a linear-block: output features x input features).  Sums in fp32 in a fixed order,
  * rounded once to out_type.  Any T, N, K from 1 on.  A device-side wait that runs out is reported by
  * pw_last_device_status.
- * Errors: INVALID_ARG, SHAPE (a stride below the row's length; N or K over 2^30), ALIGN (a pointer, or a code stride,
+ * Errors: INVALID_ARG, SHAPE (a stride below the row's length; T, N or K over 2^30), ALIGN (a pointer, or a code stride,
  * not a multiple of 16), CUDA. */
 pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const void* a_codes, int64_t a_stride,
                            const float* a_scales, const void* w_codes, int64_t w_stride, const float* w_scales,

@@ -197,8 +197,8 @@ __device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T
 // come from HBM; persistent where there are more tiles than SMs (a cluster takes one unit only).
 // A stage holds two blocks: what every role spends per barrier phase (a look 80 cycles, a copy or an MMA 70 to 90) is
 // what bounds it where the weights are in L2.
-//   warps 0 .. kSum - 1  tensor memory -> registers, scales, output; thread = weight row; with 64 tokens, warps 0-3 take
-//              the first half of the columns and 4-7 the second
+//   warps 0 .. kSum - 1  tensor memory -> registers, scales, output; thread = weight row, four warps for 16 tokens (with
+//              32 tokens to a warp 64 x 14336 x 4096 took 15.8 us instead of 14.6)
 //   then one   copies (128 x 128 tiles of w and the same columns of NT tokens)
 //   then two   MMAs, the first and the second block of every stage; the first owns tensor memory: an accumulator of NT
 //              columns per block of the ring, so a stage that has been filled again says that its accumulators have been
@@ -206,14 +206,14 @@ __device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T
 //              of a barrier can take an old one for the one it waits for.)
 //   then one   scales, eight blocks at a time, multiplied, into shared memory: loaded by the warps that use them they
 //              were 16 times as many requests as they are sectors, and the bound of the kernel
-template <int NT>
+template <int NT, bool SPLIT>
 struct FewCfg {
-  static constexpr int kSum = NT >= 64 ? 8 : 4;
+  static constexpr int kSum = NT / 4;              // four warps for 16 tokens each
   static constexpr int kThreads = (kSum + 4) * 32;
   static constexpr int kBlock = 16384 + NT * 128;  // bytes of a block in the ring
-  static constexpr int kStages = NT <= 32 ? 5 : 3;
+  static constexpr int kStages = NT <= 32 ? 5 : SPLIT ? 3 : 4;
   static constexpr int kChunks = NT / 4;           // of four tokens
-  static constexpr int kSums = (kChunks < 8 ? 8 : kChunks) * 2048;   // what a CTA receives from a cluster of up to eight
+  static constexpr int kSums = SPLIT ? (kChunks < 8 ? 8 : kChunks) * 2048 : 0;   // what a CTA receives from a cluster of up to eight
   static constexpr int kSmem = kStages * 2 * kBlock + kSums + 1024;
   static constexpr int kCols = NT <= 16 ? 256 : 512;
   static_assert(kStages * 2 * NT <= kCols, "an accumulator per block of the ring");
@@ -227,11 +227,11 @@ __device__ __forceinline__ void send4(uint32_t dst, float x, float y, float z, f
 __device__ __forceinline__ float lo_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float hi_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 
-template <int NT>
-__global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
+template <int NT, bool SPLIT>
+__global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
     linear_few_kernel(const __grid_constant__ LinearArgs a, int token_tiles, int n_units, int split) {
-  using C = FewCfg<NT>;
-  constexpr int S = C::kStages, NW = C::kSum, QC = NT * 4 / NW;   // columns of a summing warp
+  using C = FewCfg<NT, SPLIT>;
+  constexpr int S = C::kStages, NW = C::kSum, QC = 16;   // columns of a summing warp
   extern __shared__ char smem_raw[];
   __shared__ unsigned long long full[S], done[S], freed[S], sc_full[2], sc_empty[2], sums_in;
   __shared__ uint32_t tmem_base;
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
   const int unit0 = (int)(blockIdx.x / split), stride = (int)(gridDim.x / split);   // unit: (row tile, token tile), token tiles fastest
   const int g0 = (int)((int64_t)a.G * rank / split), g1 = (int)((int64_t)a.G * (rank + 1) / split);
   // chunks of four tokens that this CTA adds up: rank, rank + split, ..
-  const int chunks = split > 1 ? (min(a.T - unit0 % token_tiles * NT, NT) + 3) / 4 : 0;
+  const int chunks = SPLIT ? (min(a.T - unit0 % token_tiles * NT, NT) + 3) / 4 : 0;
   const int mine = rank < chunks ? (chunks - 1 - rank) / split + 1 : 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     if (mine > 0) mbar_expect_tx(smem_u32(&sums_in), (uint32_t)(mine * split) * 2048u, 1u);
   }
-  if (split > 1) cluster_arrive();
+  if constexpr (SPLIT) cluster_arrive();
   if (warp == NW + 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base)), "n"(C::kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base;
-  if (split > 1) cluster_wait();                   // the others' barriers are ready
+  if constexpr (SPLIT) cluster_wait();                   // the others' barriers are ready
   grid_dep_sync();          // codes and scales may come from the kernel directly ahead
   grid_dep_trigger();
 
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(FewCfg<NT>::kThreads, 1)
       }
       const int64_t n = (int64_t)(u / token_tiles) * 128 + row;
       const int t0 = u % token_tiles * NT;
-      if (split == 1) {
+      if constexpr (!SPLIT) {
         if (ok && n < a.N) {
 #pragma unroll
           for (int j = 0; j < QC; ++j)
@@ -776,11 +776,29 @@ static pw_status linear_setup(pw_ctx* ctx) {
   cudaDriverEntryPointQueryResult found;
   PW_CUDA_OK(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
   if (!fn || found != cudaDriverEntryPointSuccess) return PW_ERR_CUDA;
-  PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<16>::kSmem));
-  PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<32>::kSmem));
-  PW_CUDA_OK(cudaFuncSetAttribute(linear_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<64>::kSmem));
+  PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<16, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<16, false>::kSmem)));
+  PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<16, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<16, true>::kSmem)));
+  PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<32, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<32, false>::kSmem)));
+  PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<32, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<32, true>::kSmem)));
+  PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<64, false>::kSmem)));
+  PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<64, true>::kSmem)));
   PW_CUDA_OK(cudaFuncSetAttribute(linear_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<128>::kSmem));
   PW_CUDA_OK(cudaFuncSetAttribute(linear_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<256>::kSmem));
+  // how many clusters of 2, 4, 8 CTAs of this size, one per SM, run at the same time: an SM left over in its group of SMs
+  // is of no use to a cluster (16 of 8 CTAs did not fit on 148 SMs: 64 x 2048 x 2048 took 10.8 us, two rounds)
+  for (int i = 0; i < 3; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2u << i;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(2u << i);
+    cfg.blockDim = dim3(FewCfg<64, true>::kThreads);
+    cfg.dynamicSmemBytes = FewCfg<64, true>::kSmem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    PW_CUDA_OK((cudaOccupancyMaxActiveClusters(&ctx->max_clusters[i], linear_few_kernel<64, true>, &cfg)));
+  }
   ctx->encode_tiled = fn;
   return PW_OK;
 }
@@ -813,13 +831,14 @@ struct LinearPlan {
 };
 static int64_t tiles_of(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
-static LinearPlan plan_few(int T, int N, int G, int nt, int sms) {
+static LinearPlan plan_few(int T, int N, int G, int nt, int sms, const int* max_clusters) {
   LinearPlan p{nt, 0, 1, tiles_of(T, nt), 0, 0.};
   p.units = p.token_tiles * tiles_of(N, 128);
-  // few units: their blocks are split over a cluster, while there is an SM for every CTA and two blocks for each
-  while (p.split < 8 && p.units * p.split * 2 <= sms && G >= p.split * 4) p.split *= 2;
+  // few units: their blocks are split over a cluster, while all clusters run at the same time and two blocks are left for
+  // every CTA
+  for (int i = 0; i < 3 && p.units <= max_clusters[i] && G >= p.split * 4; ++i) p.split *= 2;
   const int64_t blocks = p.split > 1 ? tiles_of(G, p.split) : tiles_of(p.units, sms) * G;
-  p.us = nt == 16 ? 3.3 + 0.26 * blocks : nt == 32 ? 3.8 + 0.33 * blocks : 4.6 + 0.35 * blocks;
+  p.us = nt == 16 ? 3.3 + 0.26 * blocks : nt == 32 ? 3.8 + 0.30 * blocks : 4.4 + 0.32 * blocks;
   return p;
 }
 static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
@@ -830,10 +849,10 @@ static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
 }
 // The plan that finishes soonest by a model that is linear in the blocks of 128 columns a CTA (pair) goes through one
 // after the other; the times per block are measured (us, contraction 4096: tokens x weight rows, few 64 / pair 128 /
-// pair 256):  64 x 4096  7.6 / 14.1 / 18.3,  128 x 4096  9.9 / 14.4 / 18.9,  64 x 14336  16.0 / 26.2 / 20.9,
-// 128 x 14336  27 / 27.6 / 22.7,  256 x 4096  14.9 / 14.7 / 19.1,  512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
-static LinearPlan plan_linear(int T, int N, int G, int sms) {
-  LinearPlan best = plan_few(T, N, G, T <= 16 ? 16 : T <= 32 ? 32 : 64, sms);
+// pair 256):  64 x 4096  7.6 / 14.1 / 18.3,  128 x 4096  9.6 / 14.4 / 18.9,  64 x 14336  14.6 / 26.2 / 20.9,
+// 128 x 14336  27 / 27.6 / 22.7,  256 x 4096  11.7 / 14.7 / 19.1,  512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
+static LinearPlan plan_linear(int T, int N, int G, int sms, const int* max_clusters) {
+  LinearPlan best = plan_few(T, N, G, T <= 16 ? 16 : T <= 32 ? 32 : 64, sms, max_clusters);
   for (int bn = 128; bn <= 256; bn *= 2) {
     const LinearPlan p = plan_pair(T, N, G, bn, sms);
     if (p.us < best.us) best = p;
@@ -844,8 +863,10 @@ static LinearPlan plan_linear(int T, int N, int G, int sms) {
 template <int NT>
 static cudaError_t launch_few(const LinearPlan& p, const LinearArgs& a, int sms, cudaStream_t s) {
   const int64_t ctas = p.split > 1 || p.units < sms ? p.units * p.split : sms;
-  return launch_cluster(linear_few_kernel<NT>, (unsigned)ctas, p.split, FewCfg<NT>::kThreads, FewCfg<NT>::kSmem, s, a, (int)p.token_tiles,
-                        (int)p.units, p.split);
+  return p.split > 1 ? launch_cluster(linear_few_kernel<NT, true>, (unsigned)ctas, p.split, FewCfg<NT, true>::kThreads, FewCfg<NT, true>::kSmem, s, a,
+                                      (int)p.token_tiles, (int)p.units, p.split)
+                     : launch_cluster(linear_few_kernel<NT, false>, (unsigned)ctas, 1, FewCfg<NT, false>::kThreads, FewCfg<NT, false>::kSmem, s, a,
+                                      (int)p.token_tiles, (int)p.units, 1);
 }
 template <int BN>
 static cudaError_t launch_pair(const LinearPlan& p, const LinearArgs& a, int sms, cudaStream_t s) {
@@ -861,7 +882,7 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
                                       const float* a_scales, const void* w_codes, int64_t w_stride, const float* w_scales,
                                       void* out, int out_type, int64_t out_stride, pw_stream stream) {
   if (!ctx || T < 0 || N < 1 || K < 1 || !type_ok(out_type)) return PW_ERR_INVALID_ARG;
-  if (N > 1 << 30 || K > 1 << 30) return PW_ERR_SHAPE;
+  if (T > 1 << 30 || N > 1 << 30 || K > 1 << 30) return PW_ERR_SHAPE;
   if (T == 0) return PW_OK;
   if (!a_codes || !a_scales || !w_codes || !w_scales || !out) return PW_ERR_INVALID_ARG;
   if ((T > 1 && (a_stride < K || out_stride < N)) || (N > 1 && w_stride < K)) return PW_ERR_SHAPE;
@@ -885,7 +906,7 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
   a.out_type = out_type;
   a.polls = ctx->wait_polls ? kWaitPollsTest : kWaitPolls;
   a.hook = ctx->test_hook;
-  const LinearPlan p = plan_linear(T, N, a.G, ctx->num_sms);
+  const LinearPlan p = plan_linear(T, N, a.G, ctx->num_sms, ctx->max_clusters);
   if (p.units > 0x7fffffff) return PW_ERR_SHAPE;
   // a single row's stride is never used: give the map one that it accepts
   const int64_t pitch = ((int64_t)K + 15) / 16 * 16, out_pitch = T > 1 ? out_stride : N;

@@ -61,7 +61,7 @@ Matrix matrix(Call& c, PyObject* o, int arg, int kind, int64_t rows = -1, int64_
   const at::Tensor& t = THPVariable_Unpack(o);
   m.type = type_of(t);
   const bool kind_ok = kind < 0 ? m.type >= PW_F32 && m.type <= PW_BF16 : m.type == kind;
-  if (!kind_ok || !t.is_cuda() || t.get_device() != c.index) return c.fail(PW_ERR_INVALID_ARG, arg), m;
+  if (!kind_ok || !t.is_cuda() || t.is_neg() || t.get_device() != c.index) return c.fail(PW_ERR_INVALID_ARG, arg), m;
   if (t.dim() != 2) return c.fail(PW_ERR_SHAPE, arg), m;
   m.rows = t.size(0);
   m.cols = t.size(1);
@@ -80,7 +80,7 @@ Matrix vector(Call& c, PyObject* o, int arg, int kind, int64_t n) {
   const at::Tensor& t = THPVariable_Unpack(o);
   m.type = type_of(t);
   const bool kind_ok = kind < 0 ? m.type >= PW_F32 && m.type <= PW_BF16 : m.type == kind;
-  if (!kind_ok || !t.is_cuda() || t.get_device() != c.index) return c.fail(PW_ERR_INVALID_ARG, arg), m;
+  if (!kind_ok || !t.is_cuda() || t.is_neg() || t.get_device() != c.index) return c.fail(PW_ERR_INVALID_ARG, arg), m;
   if (t.dim() != 1 || t.size(0) != n || !t.is_contiguous()) return c.fail(PW_ERR_SHAPE, arg), m;
   m.data = t.data_ptr();
   return m;
