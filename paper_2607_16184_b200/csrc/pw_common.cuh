@@ -114,7 +114,7 @@ struct pw_ctx {
   int num_sms;
   int device;                     // the device the context was created on
   void* encode_tiled;             // driver entry point for tensor maps (looked up by the first scaled product)
-  int max_clusters[3];            // clusters of 2, 4, 8 CTAs of that product that run at the same time (with it)
+  int max_clusters[5];            // clusters of that product's CTAs that run at the same time, by size (looked up with it)
   void* tc_state;                 // tensor-core path state (set up lazily)
   uint32_t wait_polls;            // limit of the device-side waits in polls of 20 us (0 = the default, 2 s)
   uint32_t test_hook;             // device-side test hooks (pw_debug_set_wait)

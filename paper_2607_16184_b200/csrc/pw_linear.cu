@@ -213,7 +213,9 @@ struct FewCfg {
   static constexpr int kBlock = 16384 + NT * 128;  // bytes of a block in the ring
   static constexpr int kStages = NT <= 32 ? 5 : SPLIT ? 3 : 4;
   static constexpr int kChunks = NT / 4;           // of four tokens
-  static constexpr int kSums = SPLIT ? (kChunks < 8 ? 8 : kChunks) * 2048 : 0;   // what a CTA receives from a cluster of up to eight
+  // what a CTA receives at most: its share of the chunks, rounded up, from every CTA of a cluster of 2 to 5, or 8
+  static constexpr int kSums = SPLIT ? (NT <= 16 ? 8 : NT <= 32 ? 10 : 20) * 2048 : 0;
+  static_assert(!SPLIT || ((kChunks + 2) / 3 * 3 * 2048 <= kSums && (kChunks + 4) / 5 * 5 * 2048 <= kSums && (kChunks + 7) / 8 * 8 * 2048 <= kSums), "");
   static constexpr int kSmem = kStages * 2 * kBlock + kSums + 1024;
   static constexpr int kCols = NT <= 16 ? 256 : 512;
   static_assert(kStages * 2 * NT <= kCols, "an accumulator per block of the ring");
@@ -770,6 +772,10 @@ static bool out_map(void* encode, void* base, int rows, int cols, int64_t stride
                                                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Over how many CTAs of a cluster the blocks of a unit may be split.
+constexpr int kSplits = 5;
+constexpr int kSplit[kSplits] = {2, 3, 4, 5, 8};
+
 static pw_status linear_setup(pw_ctx* ctx) {
   if (ctx->encode_tiled) return PW_OK;
   void* fn = nullptr;
@@ -784,15 +790,15 @@ static pw_status linear_setup(pw_ctx* ctx) {
   PW_CUDA_OK((cudaFuncSetAttribute(linear_few_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<64, true>::kSmem)));
   PW_CUDA_OK(cudaFuncSetAttribute(linear_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<128>::kSmem));
   PW_CUDA_OK(cudaFuncSetAttribute(linear_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg<256>::kSmem));
-  // how many clusters of 2, 4, 8 CTAs of this size, one per SM, run at the same time: an SM left over in its group of SMs
-  // is of no use to a cluster (16 of 8 CTAs did not fit on 148 SMs: 64 x 2048 x 2048 took 10.8 us, two rounds)
-  for (int i = 0; i < 3; ++i) {
+  // how many clusters run at the same time, one CTA per SM: an SM left over in its group of SMs is of no use to a cluster
+  // (16 of 8 CTAs did not fit on 148 SMs: 64 x 2048 x 2048 took 10.8 us, two rounds)
+  for (int i = 0; i < kSplits; ++i) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2u << i;
+    attr.val.clusterDim.x = kSplit[i];
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.gridDim = dim3(2u << i);
+    cfg.gridDim = dim3(kSplit[i]);
     cfg.blockDim = dim3(FewCfg<64, true>::kThreads);
     cfg.dynamicSmemBytes = FewCfg<64, true>::kSmem;
     cfg.attrs = &attr;
@@ -836,7 +842,8 @@ static LinearPlan plan_few(int T, int N, int G, int nt, int sms, const int* max_
   p.units = p.token_tiles * tiles_of(N, 128);
   // few units: their blocks are split over a cluster, while all clusters run at the same time and two blocks are left for
   // every CTA
-  for (int i = 0; i < 3 && p.units <= max_clusters[i] && G >= p.split * 4; ++i) p.split *= 2;
+  for (int i = 0; i < kSplits; ++i)
+    if (p.units <= max_clusters[i] && G >= kSplit[i] * 2) p.split = kSplit[i];
   const int64_t blocks = p.split > 1 ? tiles_of(G, p.split) : tiles_of(p.units, sms) * G;
   p.us = nt == 16 ? 3.3 + 0.26 * blocks : nt == 32 ? 3.8 + 0.30 * blocks : 4.4 + 0.32 * blocks;
   return p;

@@ -35,15 +35,8 @@ __device__ __forceinline__ float warp_add(float v) {
 //         lanes whatever the row's alignment is; entries 0..3 and 4..7 of a thread belong to one group each.
 // The loads of x, r and (for short rows) w are all issued before the first use; a thread of a long row has no registers
 // to keep w in across the sum and reads it afterwards.  TR = void: no residual.
-// Threads.  One vector each up to 4096 columns: more threads hide the latency of a short row better than longer threads
-// do.  Then CTAs of up to 512 threads, several on an SM, before larger ones: rows of 12672 bf16 take 36 us as 416 threads
-// of four vectors and 45 us as 800 of two (2048 rows; HBM 32).  Above 16384 columns only 1024 threads keep a thread's
-// share in its registers (1024 rows x 24576: 40 us, 53 us as 512 threads of up to eight; HBM 31).  Single-element accesses
-// take up to 1024 threads from 8192 columns on (478 rows x 12671, with codes: 23 us, 33 us as 512; 1024 x 24575: 78 us,
-// 291 us): they are bound by their instructions, 64 bytes of a row each.
-constexpr int norm_threads(bool vec, int vpt) { return vpt == 4 || (!vec && vpt == 2) ? 1024 : 512; }
 template <class TX, class TR, bool VEC, int VPT>
-__global__ void __launch_bounds__(norm_threads(VEC, VPT)) add_rmsnorm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const NormArgs a) {
   grid_dep_sync();      // the row may come from the kernel directly ahead
   grid_dep_trigger();
   constexpr bool kRes = !std::is_void<TR>::value;
@@ -227,9 +220,15 @@ __global__ void __launch_bounds__(norm_threads(VEC, VPT)) add_rmsnorm_kernel(con
 }
 
 template <class TX, class TR>
-static pw_status launch_norm(const NormArgs& a, bool vec, int T, cudaStream_t s) {
+static pw_status launch_norm(const NormArgs& a, bool vec, int T, int num_sms, cudaStream_t s) {
+  // Threads.  With a row per SM at most, as many as there are vectors: more of them hide more latency (14 rows x 9728 fp32
+  // with codes 5.0 -> 3.7 us).  With more rows one vector each up to 4096 columns, then CTAs of up to 512 threads, several
+  // on an SM, before larger ones: rows of 12672 bf16 take 36 us as 416 threads of four vectors and 45 us as 800 of two
+  // (2048 rows; HBM 32).  Above 16384 columns only 1024 threads keep a thread's share in its registers (1024 rows x 24576:
+  // 40 us, 53 us as 512 threads of up to eight; HBM 31).  Single-element accesses take up to 1024 threads from 8192 columns
+  // on (478 rows x 12671, with codes: 23 us, 33 us as 512): they are bound by their instructions, 64 bytes of a row each.
   const int n8 = (a.H + 7) / 8;
-  const int vpt = n8 <= 512 ? 1 : n8 <= (vec ? 1024 : 2048) ? 2 : 4;
+  const int vpt = n8 <= (T <= num_sms ? 1024 : 512) ? 1 : n8 <= (T > num_sms && vec ? 1024 : 2048) ? 2 : 4;
   const int threads = ((n8 + vpt - 1) / vpt + 31) / 32 * 32;
   void (*k)(NormArgs);
   if (vec) k = vpt == 1 ? add_rmsnorm_kernel<TX, TR, true, 1> : vpt == 2 ? add_rmsnorm_kernel<TX, TR, true, 2> : add_rmsnorm_kernel<TX, TR, true, 4>;
@@ -238,11 +237,11 @@ static pw_status launch_norm(const NormArgs& a, bool vec, int T, cudaStream_t s)
   return PW_OK;
 }
 template <class TX>
-static pw_status launch_norm_r(const NormArgs& a, int r_type, bool vec, int T, cudaStream_t s) {
-  if (!a.r) return launch_norm<TX, void>(a, vec, T, s);
-  if (r_type == PW_F32) return launch_norm<TX, float>(a, vec, T, s);
-  if (r_type == PW_F16) return launch_norm<TX, __half>(a, vec, T, s);
-  return launch_norm<TX, __nv_bfloat16>(a, vec, T, s);
+static pw_status launch_norm_r(const NormArgs& a, int r_type, bool vec, int T, int num_sms, cudaStream_t s) {
+  if (!a.r) return launch_norm<TX, void>(a, vec, T, num_sms, s);
+  if (r_type == PW_F32) return launch_norm<TX, float>(a, vec, T, num_sms, s);
+  if (r_type == PW_F16) return launch_norm<TX, __half>(a, vec, T, num_sms, s);
+  return launch_norm<TX, __nv_bfloat16>(a, vec, T, num_sms, s);
 }
 
 // ---- quantizer ---------------------------------------------------------------------------------
@@ -480,9 +479,9 @@ extern "C" pw_status pw_add_rmsnorm(pw_ctx* ctx, int T, int H, const void* x, in
   auto rows16 = [&](const void* p, int type, int64_t stride) { return !p || (stride * type_size(type)) % 16 == 0; };
   const bool vec = H % 8 == 0 && rows16(x, x_type, x_stride) && rows16(residual, residual_type, residual_stride) &&
                    rows16(residual_out, residual_type, residual_out_stride) && rows16(y, y_type, y_stride);
-  const pw_status st = x_type == PW_F32   ? launch_norm_r<float>(a, residual_type, vec, T, stream)
-                       : x_type == PW_F16 ? launch_norm_r<__half>(a, residual_type, vec, T, stream)
-                                          : launch_norm_r<__nv_bfloat16>(a, residual_type, vec, T, stream);
+  const pw_status st = x_type == PW_F32   ? launch_norm_r<float>(a, residual_type, vec, T, ctx->num_sms, stream)
+                       : x_type == PW_F16 ? launch_norm_r<__half>(a, residual_type, vec, T, ctx->num_sms, stream)
+                                          : launch_norm_r<__nv_bfloat16>(a, residual_type, vec, T, ctx->num_sms, stream);
   if (st == PW_OK) ctx->launches++;
   return st;
 }
