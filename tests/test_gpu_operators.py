@@ -132,6 +132,16 @@ def test_norm_types_and_widths(ctx, T, H, pad, x_type, res_type, w_type, y_type)
         assert guards_left(y_whole, y, 7.0)
 
 
+@pytest.mark.parametrize("T", [100, 300])
+@pytest.mark.parametrize("H", [5120, 8191, 9728, 9729, 16384, 20000])
+def test_norm_of_fewer_and_more_rows_than_sms(ctx, T, H):
+    x, w, r = randn(1, T, H, dtype=BF16), randn(2, H), randn(3, T, H)
+    y, ro = torch.empty(T, H, dtype=BF16, device="cuda"), torch.empty_like(r)
+    q, qs = B.scaled_empty(T, H, 1)
+    ctx.pw_add_rmsnorm(x, w, 1e-5, residual=r, residual_out=ro, y=y, q=q, q_scales=qs)
+    check_norm(x, r, w, 1e-5, ro, y, q, qs)
+
+
 @pytest.mark.parametrize("H", [24573, 32768])
 def test_norm_of_the_widest_rows(ctx, H):
     x, w, r = randn(1, 2, H), randn(2, H), randn(3, 2, H, dtype=F16)
@@ -223,7 +233,8 @@ def test_product_leaves_what_lies_between_rows(ctx, T, N, K, pad, out_type):
     assert guards_left(whole, out, 7.0)
 
 
-@pytest.mark.parametrize("T,N,K", [(1, 4096, 4096), (64, 2048, 14336), (256, 4096, 1408), (512, 1500, 2048), (1000, 2048, 1024), (1030, 770, 391), (2048, 4096, 512)])
+@pytest.mark.parametrize("T,N,K", [(1, 4096, 4096), (64, 2048, 14336), (48, 5244, 2607), (16, 4999, 1300), (3, 3700, 700), (30, 3200, 1290), (64, 3300, 1290),
+                                   (64, 20000, 260), (13, 30000, 130), (256, 4096, 1408), (512, 1500, 2048), (1000, 2048, 1024), (1030, 770, 391), (2048, 4096, 512)])
 def test_product_larger(ctx, T, N, K):
     a, sa, w, sw = operands(ctx, T, N, K, seed=T, pad=32)
     check_linear(ctx, a, sa, w, sw, torch.empty(T, N, dtype=F16, device="cuda"))
@@ -246,6 +257,25 @@ def test_product_gives_the_same_bits_again(ctx):
         first = ctx.pw_scaled_linear(a, sa, w, sw, out_dtype=F32)
         for _ in range(5):
             assert torch.equal(first, ctx.pw_scaled_linear(a, sa, w, sw, out_dtype=F32))
+
+
+def test_products_on_two_streams_at_once(ctx):
+    """No call keeps anything that another one uses."""
+    shapes = [(40, 4096, 1400), (300, 1000, 900), (5, 5000, 700), (64, 2048, 2048), (1000, 600, 512), (20, 20000, 260)]
+    sets = [operands(ctx, *s, seed=i) for i, s in enumerate(shapes)]
+    want = [ctx.pw_scaled_linear(*s, out_dtype=F32) for s in sets]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[torch.empty_like(w) for w in want] for _ in range(2)]
+    for n in range(20):
+        for k, st in enumerate(streams):
+            for i in range(len(sets)):
+                j = (i + 3 * k + n) % len(sets)
+                ctx.pw_scaled_linear(*sets[j], out=got[k][j], stream=st)
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(want, got[k]))
+    assert ctx.pw_last_device_status() == 0
 
 
 @pytest.mark.parametrize("T", [1, 20, 40, 64, 300])
