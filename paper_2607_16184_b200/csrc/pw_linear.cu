@@ -844,8 +844,8 @@ static LinearPlan plan_few(int T, int N, int G, int nt, int sms, const int* max_
   // every CTA
   for (int i = 0; i < kSplits; ++i)
     if (p.units <= max_clusters[i] && G >= kSplit[i] * 2) p.split = kSplit[i];
-  const int64_t blocks = p.split > 1 ? tiles_of(G, p.split) : tiles_of(p.units, sms) * G;
-  p.us = nt == 16 ? 3.3 + 0.26 * blocks : nt == 32 ? 3.8 + 0.30 * blocks : 4.4 + 0.32 * blocks;
+  const int64_t rounds = p.split > 1 ? 1 : tiles_of(p.units, sms), blocks = p.split > 1 ? tiles_of(G, p.split) : rounds * G;
+  p.us = 1.5 * (rounds - 1) + (nt == 16 ? 3.3 + 0.26 * blocks : nt == 32 ? 3.8 + 0.30 * blocks : 4.4 + 0.32 * blocks);
   return p;
 }
 static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
@@ -855,11 +855,17 @@ static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
   return p;
 }
 // The plan that finishes soonest by a model that is linear in the blocks of 128 columns a CTA (pair) goes through one
-// after the other; the times per block are measured (us, contraction 4096: tokens x weight rows, few 64 / pair 128 /
-// pair 256):  64 x 4096  7.6 / 14.1 / 18.3,  128 x 4096  9.6 / 14.4 / 18.9,  64 x 14336  14.6 / 26.2 / 20.9,
-// 128 x 14336  27 / 27.6 / 22.7,  256 x 4096  11.7 / 14.7 / 19.1,  512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
+// after the other and in the units it does (301 x 64 x 2056: 16 tokens to a tile 4.7 us, 64 5.6; 3711 x 187 x 119: 16
+// tokens, four units one after the other, 8.8, 64 tokens 4.9).  The times per block are measured (us, contraction 4096,
+// tokens x weight rows, few 64 / pair 128 / pair 256):  64 x 4096  7.6 / 14.1 / 18.3,  128 x 4096  9.6 / 14.4 / 18.9,
+// 64 x 14336  14.6 / 26.2 / 20.9,  128 x 14336  27 / 27.6 / 22.7,  256 x 4096  11.7 / 14.7 / 19.1,
+// 512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
 static LinearPlan plan_linear(int T, int N, int G, int sms, const int* max_clusters) {
-  LinearPlan best = plan_few(T, N, G, T <= 16 ? 16 : T <= 32 ? 32 : 64, sms, max_clusters);
+  LinearPlan best = plan_few(T, N, G, 16, sms, max_clusters);
+  for (int nt = 32; nt <= 64 && T > nt / 2; nt *= 2) {
+    const LinearPlan p = plan_few(T, N, G, nt, sms, max_clusters);
+    if (p.us < best.us) best = p;
+  }
   for (int bn = 128; bn <= 256; bn *= 2) {
     const LinearPlan p = plan_pair(T, N, G, bn, sms);
     if (p.us < best.us) best = p;
