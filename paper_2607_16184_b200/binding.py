@@ -1,4 +1,5 @@
-"""Thin ctypes binding of the C ABI declared in ``include/pw.h``.
+"""Thin binding of the C ABI declared in ``include/pw.h``: ctypes, and for the calls around the layer a
+compiled module (``csrc/pw_torch.cpp``).
 
 Argument marshalling only: every step of the hot path runs inside ``libpw.so``.
 PyTorch supplies device memory (``tensor.data_ptr()``) and streams.  There is no
