@@ -332,6 +332,8 @@ typedef enum { PW_F32 = 0, PW_F16 = 1, PW_BF16 = 2 } pw_type;
  * [ceil(rows / block_rows)][ceil(cols / 128)]; the last block of either direction may be short.  A block's scale is its
  * largest magnitude / 448 (1 for a block of zeros, at least 2^-126), its codes are e4m3(value * (1 / scale)), rounded
  * to nearest even and limited to 448: value = code * scale.
+ * A NaN becomes a NaN code and has no part in the scale; an infinity makes its block's scale infinite, its own code NaN
+ * and the others 0.
  *
  * pw_quantize_scaled: x device [rows, cols] of x_type.  The codes' bytes past `cols` in a row are not written.
  * Errors: INVALID_ARG (a null pointer, block_rows neither 1 nor 128, cols < 1), SHAPE (stride below cols; cols over

@@ -81,6 +81,28 @@ def test_quantizer_of_extreme_values(ctx):
     assert np.array_equal(plain.code_values(q), plain.code_values(torch.from_numpy(codes)))
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("cols", [256, 131])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantizer_of_infinities_and_nan(ctx, cols, dtype, block_rows):
+    x = randn(cols, 140, cols, dtype=dtype)
+    x[0, 3], x[1, 7], x[130, 130] = math.nan, -math.inf, math.inf
+    x[131] = math.nan
+    x[139, 128:] = math.nan
+    q, s = ctx.pw_quantize_scaled(x, block_rows)
+    # scales of the numbers that are none left out; infinite where an infinity is in the block
+    clean = torch.where(x.isfinite(), x, torch.zeros_like(x))
+    codes, ref = plain.quantize_bits(clean, block_rows)
+    inf = plain.block_tops(x.isinf().double().cpu().numpy(), block_rows) > 0
+    assert inf.sum() == 2
+    ref[inf] = np.inf
+    assert np.array_equal(s.cpu().numpy(), ref)
+    want = plain.code_values(torch.from_numpy(codes))
+    want[plain.spread(inf, block_rows, want.shape)] = 0
+    want[~x.isfinite().cpu().numpy()] = np.nan
+    assert np.array_equal(plain.code_values(q), want, equal_nan=True)
+
+
 # ---- norm ------------------------------------------------------------------------------------------
 
 # Relative error of y before its rounding: one rounding of s; the sum of squares is a chain of at most 64 fused
