@@ -9,8 +9,8 @@
 // logit); otherwise they are computed in 32 bits together with a bound of their error.  Where two keys or two groups that
 // decide anything are closer than that, the few experts concerned are computed in 64 bits, one per lane, and where that
 // does not settle it either the whole token is.
-// 4096 tokens x 256 experts in 8 groups: 10.1 us (everything in 64 bits 28.4, every unsettled token in 64 bits 13.5), one
-// token 4.8; without groups 9.3, without bias either 6.3; 4.2 MB read at the copy rate: 0.7.
+// 4096 tokens x 256 experts in 8 groups: 9.3 us (everything in 64 bits 28.4, every unsettled token in 64 bits 13.5), one
+// token 4.7; without groups 9.2, without bias either 6.3; 4.2 MB read at the copy rate: 0.7.
 #include "pw_scaled.cuh"
 
 namespace pw {
@@ -404,11 +404,18 @@ __global__ void __launch_bounds__(128, 7) score_kernel(const __grid_constant__ R
       take_best<NS>(c, key, &my_id, &my_key);
     }
   } else {
-    auto p_of = [&](float v) { return a.sigmoid ? __fdividef(1.f, 1.f + __expf(-v)) : __fdividef(__expf(v - top), total); };
-    // Error of p in 32 bits, in half steps of 1: the fast exponential 4 and its argument's two roundings 0.37 * 2 (their
-    // effect on d e^-d), the same and the 13 additions of the denominator, the fast division 4: below 32.  With the bias's
-    // addition a key is off by less than (32 + |key|) half steps; two keys decide when they are further apart than both
-    // errors together.
+    // (one exponential and one division for both scores: a branch for each key is twice the code to fetch)
+    const float sign = a.sigmoid ? -1.f : 1.f, shift = a.sigmoid ? 0.f : -top;
+    auto p_of = [&](float v) {
+      const float e = __expf(fmaf(sign, v, shift));
+      return __fdividef(a.sigmoid ? 1.f : e, a.sigmoid ? 1.f + e : total);
+    };
+    // Error of p in 32 bits, in half steps of 1.  The fast exponential of x is (2 + 1.173 |x|) steps off, the fast division 2.
+    //   sigmoid: p (1 - p) (4 + 2.35 |v|) + p + 4 p <= 1 + 0.53 + 1 + 4, below 8
+    //   softmax: 4 + 0.87 of the exponential (d e^-d <= 0.37) and 0.37 of the rounding of its argument, as much and 13
+    //            additions of the denominator, 4 of the division: below 32
+    // With the bias's addition a key is off by less than (8 or 32 + |key|) half steps; two keys decide when they are further
+    // apart than both errors together.
     constexpr float kHalfStep = 5.9604645e-8f;
     uint32_t key[NS];
     float size = 0.f;
@@ -416,14 +423,14 @@ __global__ void __launch_bounds__(128, 7) score_kernel(const __grid_constant__ R
     for (int i = 0; i < NS; ++i) {
       float v = l[i];
       if (a.bias) {
-        v = v > -INFINITY ? p_of(v) + b[i] : v;
-        v = v > -INFINITY ? v : -INFINITY;          // a bias that is no number: never chosen
+        const float k = p_of(v) + b[i];
+        v = v > -INFINITY && k > -INFINITY ? k : -INFINITY;   // a bias that is no number: never chosen
         size = v > -INFINITY ? fmaxf(size, fabsf(v)) : size;
       }
       key[i] = v > -INFINITY ? ordered(v + 0.f) : 0u;
     }
     if (a.bias) size = warp_max(size);
-    const float apart = 2.f * (32.f + size) * kHalfStep;
+    const float apart = 2.f * ((a.sigmoid ? 8.f : 32.f) + size) * kHalfStep;
     auto far_keys = [&](uint32_t x, uint32_t y) { return a.bias ? from_ordered(x) - from_ordered(y) > apart : x > y; };
     // without a bias the keys are exact, and so is a group's best; a sum of two scores never is
     bool sure = a.groups <= 32;
