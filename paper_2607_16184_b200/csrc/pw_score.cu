@@ -413,9 +413,9 @@ __global__ void __launch_bounds__(128, 7) score_kernel(const __grid_constant__ R
     // Error of p in 32 bits, in half steps of 1.  The fast exponential of x is (2 + 1.173 |x|) steps off, the fast division 2.
     //   sigmoid: p (1 - p) (4 + 2.35 |v|) + p + 4 p <= 1 + 0.53 + 1 + 4, below 8
     //   softmax: 4 + 0.87 of the exponential (d e^-d <= 0.37) and 0.37 of the rounding of its argument, as much and 13
-    //            additions of the denominator, 4 of the division: below 32
-    // With the bias's addition a key is off by less than (8 or 32 + |key|) half steps; two keys decide when they are further
-    // apart than both errors together.
+    //            additions of the denominator, 4 of the division: below 32, all of it relative to p, which is 1 / total at most
+    // With the bias's addition a key is off by less than (8 or 32 / total, + |key|) half steps; two keys decide when they are
+    // further apart than both errors together.
     constexpr float kHalfStep = 5.9604645e-8f;
     uint32_t key[NS];
     float size = 0.f;
@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(128, 7) score_kernel(const __grid_constant__ R
       key[i] = v > -INFINITY ? ordered(v + 0.f) : 0u;
     }
     if (a.bias) size = warp_max(size);
-    const float apart = 2.f * ((a.sigmoid ? 8.f : 32.f) + size) * kHalfStep;
+    const float apart = 2.f * ((a.sigmoid ? 8.f : __fdividef(32.f, total)) + size) * kHalfStep;
     auto far_keys = [&](uint32_t x, uint32_t y) { return a.bias ? from_ordered(x) - from_ordered(y) > apart : x > y; };
     // without a bias the keys are exact, and so is a group's best; a sum of two scores never is
     bool sure = a.groups <= 32;
