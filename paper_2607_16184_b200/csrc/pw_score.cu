@@ -10,7 +10,7 @@
 // decide anything are closer than that, the few experts concerned are computed in 64 bits, one per lane, and where that
 // does not settle it either the whole token is.
 // 4096 tokens x 256 experts in 8 groups: 9 to 11 us, by the near ties among them (everything in 64 bits 28.4, every
-// unsettled token in 64 bits 13.5), one token 4.7; without groups 9.2, without bias either 6.3; 4.2 MB read at the copy rate: 0.7.
+// unsettled token in 64 bits 13.5), one token 4.7; without groups 9.2, without bias either 4.9; 4.2 MB read at the copy rate: 0.7.
 #include "pw_scaled.cuh"
 
 namespace pw {
@@ -362,12 +362,14 @@ __device__ __noinline__ double exact_key(const RouteArgs& a, int64_t t, int lane
   return key;
 }
 
-// (Seven CTAs on an SM: 4096 tokens are one wave, and only choose_exactly would want more than 72 registers; five CTAs of
-// 96 registers 11.7 us, eight 10.6.)
+// CTAs on an SM.  Sixteen of the PLAIN kernel: the CTAs of a call come to their SMs while those of the call before are
+// there, if both fit (4096 tokens x 256 experts 6.3 -> 4.9 us; at 12 CTAs an SM everything above 3552 tokens took 1.9 us
+// more).  Seven of the other: 4096 tokens are one wave, and only choose_exactly would want more than 72 registers (five
+// CTAs of 96 registers 11.7 us, eight 10.6, seven 10.1).
 // NS = 32-expert strides a lane holds.  PLAIN: no bias and no groups, nothing but the logits decides (a program a third
 // as long: one token 1.9 us instead of 2.4, most of it instructions on their way to the SM).
 template <int NS, bool PLAIN>
-__global__ void __launch_bounds__(128, 7) score_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(128, PLAIN ? 16 : 7) score_kernel(const __grid_constant__ RouteArgs a) {
   grid_dep_sync();
   grid_dep_trigger();
   const int64_t t = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
