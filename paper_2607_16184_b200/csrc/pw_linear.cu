@@ -32,34 +32,54 @@ struct LinearArgs {
 };
 
 // ---- bounded waits -------------------------------------------------------------------------------
-__device__ __forceinline__ bool mbar_try(uint32_t bar_s, uint32_t parity) {
+// One look at a phase, with the suspend time of a poll or without any.  CLUSTER: what the phase counted was written by
+// other CTAs of the cluster, so its completion is acquired at that scope (the instruction's own is the CTA).
+template <bool SUSPEND, bool CLUSTER = false>
+__device__ __forceinline__ bool mbar_look(uint32_t bar_s, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar_s), "r"(parity), "r"(20000u)
-      : "memory");
+  if constexpr (CLUSTER)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar_s), "r"(parity), "r"(20000u)
+        : "memory");
+  else if constexpr (SUSPEND)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar_s), "r"(parity), "r"(20000u)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar_s), "r"(parity)
+        : "memory");
   return ok != 0;
+}
+// Whether any lane has seen the phase.  A lane that has not goes on all the same, and reads what was written before the
+// phase by order of the one that has: a vote orders no memory, __syncwarp does.
+__device__ __forceinline__ bool warp_saw(bool ok) {
+  const bool any = __any_sync(0xffffffffu, ok);
+  __syncwarp();
+  return any;
 }
 // Called by a whole warp, with the same answer for all lanes: the lanes of one poll may see the phase flip at different
 // moments, and what follows a wait (tensor-memory loads, cluster barriers) must not be run by a part of the warp.
 // False when the limit ran out or another role of the CTA has given up.  (The first look goes without a suspend time: a
 // phase that is complete costs 79 cycles, with one 105.)
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar_s, uint32_t parity, volatile int* gave_up, int polls, int32_t* status) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar_s), "r"(parity)
-      : "memory");
-  if (__any_sync(0xffffffffu, ok != 0)) return true;
+  if (warp_saw(mbar_look<false, CLUSTER>(bar_s, parity))) return true;
 #pragma unroll 1
   for (int n = 0; n < polls; ++n) {
-    if (__any_sync(0xffffffffu, mbar_try(bar_s, parity))) return true;
+    if (warp_saw(mbar_look<true, CLUSTER>(bar_s, parity))) return true;
     if (__any_sync(0xffffffffu, *gave_up != 0)) return false;
   }
   *gave_up = 1;
@@ -303,7 +323,7 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
     }
     if (!ok)                                       // leave nothing in flight
       for (int j = i < S ? 0 : i - S; j < i; ++j)
-        for (int n = 0; n < 200 && !mbar_try(smem_u32(&full[j % S]), (j / S) & 1); ++n) {
+        for (int n = 0; n < 200 && !mbar_look<true>(smem_u32(&full[j % S]), (j / S) & 1); ++n) {
         }
   } else if (warp == NW + 1 || warp == NW + 2) {
     bool ok = true;
@@ -420,7 +440,7 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
       }
       __syncwarp();
       volatile int no_matter = 0;
-      if (mine > 0 && mbar_wait(smem_u32(&sums_in), 0, &no_matter, 8 * a.polls, a.status) && n < a.N) {
+      if (mine > 0 && mbar_wait<true>(smem_u32(&sums_in), 0, &no_matter, 8 * a.polls, a.status) && n < a.N) {
         const float4* sums = reinterpret_cast<const float4*>(smem_raw + (sums_s - smem_u32(smem_raw))) + row;
         for (int lc = warp >> 2; lc < mine; lc += NW / 4) {
           float4 x = sums[lc * split * 128];
@@ -644,7 +664,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
         ok = mbar_wait(smem_u32(&done[j % S]), (j / S) & 1, &gave_up, a.polls, a.status);
       if (!ok && rank == 0)
         for (int j = item < S ? 0 : item - S; j < item; ++j)
-          for (int n = 0; n < 200 && !mbar_try(smem_u32(&full[j % S]), (j / S) & 1); ++n) {
+          for (int n = 0; n < 200 && !mbar_look<true>(smem_u32(&full[j % S]), (j / S) & 1); ++n) {
           }
     } else if (warp == 9 || warp == 10) {
       // two warps issue, blocks in turn: every block has an accumulator of its own, so their order does not matter

@@ -1,0 +1,38 @@
+"""Rules of the kernels' sources that no run shows reliably: how memory is handed over (CPU only)."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_16184_b200", "csrc")
+
+
+def source(name):
+    text = open(os.path.join(CSRC, name)).read()
+    return re.sub(r"//[^\n]*", "", text)
+
+
+def body(text, start):
+    """From `start` to the end of the braces that follow it."""
+    at = text.index(start)
+    i = text.index("{", at)
+    depth, j = 1, i + 1
+    while depth:
+        depth += {"{": 1, "}": -1}.get(text[j], 0)
+        j += 1
+    return text[at:j]
+
+
+def test_a_wait_that_a_vote_decides_orders_memory():
+    """A lane whose own look at a barrier failed acquires nothing by a vote; __syncwarp hands it what the others saw."""
+    text = source("pw_linear.cu")
+    vote = body(text, "bool warp_saw(")
+    assert vote.index("__any_sync") < vote.index("__syncwarp")
+    wait = body(text, "bool mbar_wait(")
+    returns = re.findall(r"if \(([^;]*)\) return true;", wait)
+    assert len(returns) == 2 and all(r.startswith("warp_saw(") for r in returns)
+
+
+def test_sums_of_other_blocks_are_acquired_at_cluster_scope():
+    text = source("pw_linear.cu")
+    waits = re.findall(r"mbar_wait(<\w+>)?\(smem_u32\(&sums_in\)", text)
+    assert waits == ["<true>"]
+    assert "try_wait.parity.acquire.cluster" in body(text, "bool mbar_look(")
