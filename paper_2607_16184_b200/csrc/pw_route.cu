@@ -8,8 +8,9 @@ constexpr int kMaxExpertsPerLane = 8;  // E <= 256
 constexpr int kFusedRouteWork = 256;   // (token, choice) pairs x 32-expert strides up to which the grouping kernel routes itself
 
 // Routing of one token by one warp.  Slot j holds the j-th largest logit; equal logits: lower expert index first.
+// (The logits may be written by the kernel directly ahead, pw_scaled_linear's: plain pointers all the way.)
 template <int NS>   // NS = 32-expert strides a lane holds (1, 2, 4 or 8): the loops below cost in proportion
-__device__ __forceinline__ void route_token_n(const float* __restrict__ logits, int token, int E, int k,
+__device__ __forceinline__ void route_token_n(const float* logits, int token, int E, int k,
                                               int32_t* __restrict__ topk_ids, float* __restrict__ gates, int lane) {
   const float* l = logits + (size_t)token * E;
   float v[NS];
@@ -58,7 +59,7 @@ __device__ __forceinline__ void route_token_n(const float* __restrict__ logits, 
   }
 }
 
-__device__ __forceinline__ void route_token(const float* __restrict__ logits, int token, int E, int k,
+__device__ __forceinline__ void route_token(const float* logits, int token, int E, int k,
                                             int32_t* __restrict__ topk_ids, float* __restrict__ gates, int lane) {
   if (E <= 32) route_token_n<1>(logits, token, E, k, topk_ids, gates, lane);
   else if (E <= 64) route_token_n<2>(logits, token, E, k, topk_ids, gates, lane);
@@ -67,7 +68,7 @@ __device__ __forceinline__ void route_token(const float* __restrict__ logits, in
 }
 
 // One warp per token.
-__global__ void __launch_bounds__(256) router_kernel(const float* __restrict__ logits, int T, int E, int k,
+__global__ void __launch_bounds__(256) router_kernel(const float* logits, int T, int E, int k,
                                                      int32_t* __restrict__ topk_ids, float* __restrict__ gates) {
   grid_dep_sync();   // the gates of the call before this one may still be read by its combine kernel
   grid_dep_trigger();
@@ -103,7 +104,7 @@ __device__ __forceinline__ void warp_exclusive_scan(const int32_t* in, int32_t* 
 // no operand row (inv_perm -1); the shared experts' rows follow the rows that there are.  (A variant of its own: the
 // checks cost a one-token layer 0.7 us of 44.)
 template <bool GIVEN>
-__global__ void __launch_bounds__(1024) permute_kernel(const float* __restrict__ logits, const int32_t* ids_in,
+__global__ void __launch_bounds__(1024) permute_kernel(const float* logits, const int32_t* ids_in,
                                                        const float* gates_in, float* __restrict__ gates,
                                                        int32_t* topk_ids, int T, int k, int E,
                                                        int n_shared, int32_t* __restrict__ counts,

@@ -36,3 +36,12 @@ def test_sums_of_other_blocks_are_acquired_at_cluster_scope():
     waits = re.findall(r"mbar_wait(<\w+>)?\(smem_u32\(&sums_in\)", text)
     assert waits == ["<true>"]
     assert "try_wait.parity.acquire.cluster" in body(text, "bool mbar_look(")
+
+
+def test_first_kernels_of_the_layer_read_the_callers_buffers_through_plain_pointers():
+    """Logits, ids and gates may come from the kernel directly ahead, which may still run when a dependent one is placed:
+    `const __restrict__` would let the compiler read them through the non-coherent path."""
+    text = source("pw_route.cu")
+    for name in ("logits", "ids_in", "gates_in"):
+        declared = re.findall(r"const (?:float|int32_t)\*\s*(__restrict__)?\s*%s\b" % name, text)
+        assert declared and not any(declared), name
