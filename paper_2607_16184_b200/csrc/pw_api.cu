@@ -418,7 +418,7 @@ extern "C" pw_status pw_debug_set_wait(pw_ctx* ctx, uint32_t polls, uint32_t hoo
   return PW_OK;
 }
 
-extern "C" uint64_t pw_launch_count(pw_ctx* ctx) { return ctx ? ctx->launches : 0; }
+extern "C" uint64_t pw_launch_count(pw_ctx* ctx) { return ctx ? ctx->launches.load() : 0; }
 
 extern "C" const char* pw_status_str(pw_status s) {
   switch (s) {

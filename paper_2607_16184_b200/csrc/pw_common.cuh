@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/pw.h"
 
 namespace pw {
@@ -109,12 +111,14 @@ struct pw_ctx {
   uint8_t* host_valid;
   uint64_t epoch;
   size_t n_rows;                  // rows of the table = n_layers * (n_experts + n_shared) * 3
-  uint64_t launches;
+  std::atomic<uint64_t> launches; // counted by calls on any thread
   int last_T, last_k;
   int num_sms;
   int device;                     // the device the context was created on
-  void* encode_tiled;             // driver entry point for tensor maps (looked up by the first scaled product)
-  int max_clusters[5];            // clusters of that product's CTAs that run at the same time, by size (looked up with it)
+  // looked up by the first scaled product, on whichever threads make it (all of them find the same, and the entry point
+  // is set last)
+  std::atomic<void*> encode_tiled;    // driver entry point for tensor maps
+  std::atomic<int> max_clusters[5];   // clusters of that product's CTAs that run at the same time, by size
   void* tc_state;                 // tensor-core path state (set up lazily)
   uint32_t wait_polls;            // limit of the device-side waits in polls of 20 us (0 = the default, 2 s)
   uint32_t test_hook;             // device-side test hooks (pw_debug_set_wait)

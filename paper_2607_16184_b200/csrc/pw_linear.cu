@@ -803,7 +803,7 @@ constexpr int kSplits = 5;
 constexpr int kSplit[kSplits] = {2, 3, 4, 5, 8};
 
 static pw_status linear_setup(pw_ctx* ctx) {
-  if (ctx->encode_tiled) return PW_OK;
+  if (ctx->encode_tiled.load(std::memory_order_acquire)) return PW_OK;
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult found;
   PW_CUDA_OK(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
@@ -829,9 +829,11 @@ static pw_status linear_setup(pw_ctx* ctx) {
     cfg.dynamicSmemBytes = FewCfg<64, true>::kSmem;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    PW_CUDA_OK((cudaOccupancyMaxActiveClusters(&ctx->max_clusters[i], linear_few_kernel<64, true>, &cfg)));
+    int clusters = 0;
+    PW_CUDA_OK((cudaOccupancyMaxActiveClusters(&clusters, linear_few_kernel<64, true>, &cfg)));
+    ctx->max_clusters[i].store(clusters, std::memory_order_relaxed);
   }
-  ctx->encode_tiled = fn;
+  ctx->encode_tiled.store(fn, std::memory_order_release);
   return PW_OK;
 }
 
@@ -945,16 +947,19 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
   a.out_type = out_type;
   a.polls = ctx->wait_polls ? kWaitPollsTest : kWaitPolls;
   a.hook = ctx->test_hook;
-  const LinearPlan p = plan_linear(T, N, a.G, ctx->num_sms, ctx->max_clusters);
+  void* const encode = ctx->encode_tiled.load(std::memory_order_acquire);
+  int max_clusters[kSplits];
+  for (int i = 0; i < kSplits; ++i) max_clusters[i] = ctx->max_clusters[i].load(std::memory_order_relaxed);
+  const LinearPlan p = plan_linear(T, N, a.G, ctx->num_sms, max_clusters);
   if (p.units > 0x7fffffff) return PW_ERR_SHAPE;
   // a single row's stride is never used: give the map one that it accepts
   const int64_t pitch = ((int64_t)K + 15) / 16 * 16, out_pitch = T > 1 ? out_stride : N;
-  if (!codes_map(ctx->encode_tiled, a_codes, T, K, a_stride < pitch ? pitch : a_stride, p.bn ? 128 : p.nt, &a.ma) ||
-      !codes_map(ctx->encode_tiled, w_codes, N, K, w_stride < pitch ? pitch : w_stride, p.bn ? p.bn / 2 : 128, &a.mw))
+  if (!codes_map(encode, a_codes, T, K, a_stride < pitch ? pitch : a_stride, p.bn ? 128 : p.nt, &a.ma) ||
+      !codes_map(encode, w_codes, N, K, w_stride < pitch ? pitch : w_stride, p.bn ? p.bn / 2 : 128, &a.mw))
     return PW_ERR_CUDA;
   // the copies of output boxes are cut at a row's end in units of 16 bytes only
   const int size = type_size(out_type);
-  if (p.bn) a.tma_out = out_pitch * size % 16 == 0 && (int64_t)N * size % 16 == 0 && out_map(ctx->encode_tiled, out, T, N, out_pitch, out_type, &a.mo);
+  if (p.bn) a.tma_out = out_pitch * size % 16 == 0 && (int64_t)N * size % 16 == 0 && out_map(encode, out, T, N, out_pitch, out_type, &a.mo);
   PW_CUDA_OK(p.bn == 256   ? launch_pair<256>(p, a, ctx->num_sms, stream)
              : p.bn == 128 ? launch_pair<128>(p, a, ctx->num_sms, stream)
              : p.nt == 16  ? launch_few<16>(p, a, ctx->num_sms, stream)

@@ -90,6 +90,19 @@ Matrix scales(Call& c, PyObject* o, int arg, int64_t rows, int64_t cols, int64_t
   return matrix(c, o, arg, PW_F32, (rows + block_rows - 1) / block_rows, (cols + kGroup - 1) / kGroup, true);
 }
 
+// Around a call of the library, once all arguments are read: the call's device current and the interpreter released.  A
+// launch waits when the stream's queue is full, and for a host function in it that wants the interpreter it would wait for
+// good.  (The caller's frame holds the tensors.)
+struct Released {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Released() { PyEval_RestoreThread(state); }
+};
+struct Outside {
+  Released released;
+  c10::cuda::CUDAGuard device;
+  explicit Outside(const Call& c) : device((c10::DeviceIndex)c.index) {}
+};
+
 // Runs the marshalling of one call; a C++ exception of torch's (a tensor without storage, say) is an invalid argument.
 template <class F>
 PyObject* guarded(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F f) {
@@ -118,7 +131,7 @@ PyObject* quantize_scaled(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (c.bad) return c.bad;
     const Matrix q = matrix(c, a[2], 3, kCodes, x.rows, x.cols), s = scales(c, a[3], 4, x.rows, x.cols, block);
     if (c.bad) return c.bad;
-    c10::cuda::CUDAGuard device((c10::DeviceIndex)c.index);
+    Outside outside(c);
     return pw_quantize_scaled(c.ctx, x.data, x.type, (int)x.rows, (int)x.cols, x.stride, block, q.data, q.stride,
                               static_cast<float*>(s.data), c.stream);
   });
@@ -143,7 +156,7 @@ PyObject* add_rmsnorm(PyObject*, PyObject* const* args, Py_ssize_t n) {
       s = scales(c, a[7], 8, x.rows, x.cols, 1);
     }
     if (c.bad) return c.bad;
-    c10::cuda::CUDAGuard device((c10::DeviceIndex)c.index);
+    Outside outside(c);
     return pw_add_rmsnorm(c.ctx, (int)x.rows, (int)x.cols, x.data, x.type, x.stride, r.data, r.type, r.stride, w.data, w.type, eps, ro.data, ro.stride,
                           y.data, y.type, y.stride, q.data, q.stride, static_cast<float*>(s.data), c.stream);
   });
@@ -157,7 +170,7 @@ PyObject* scaled_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Matrix sx = scales(c, a[1], 2, x.rows, x.cols, 1), sw = scales(c, a[3], 4, w.rows, x.cols, kGroup);
     const Matrix out = matrix(c, a[4], 5, -1, x.rows, w.rows);
     if (c.bad) return c.bad;
-    c10::cuda::CUDAGuard device((c10::DeviceIndex)c.index);
+    Outside outside(c);
     return pw_scaled_linear(c.ctx, (int)x.rows, (int)w.rows, (int)x.cols, x.data, x.stride, static_cast<float*>(sx.data), w.data, w.stride,
                             static_cast<float*>(sw.data), out.data, out.type, out.stride, c.stream);
   });
@@ -180,7 +193,7 @@ PyObject* route_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a[3] != Py_None) b = vector(c, a[3], 4, PW_F32, l.cols);
     const Matrix ids = matrix(c, a[9], 10, kWords, l.rows, r.top_k, true), gates = matrix(c, a[10], 11, PW_F32, l.rows, r.top_k, true);
     if (c.bad) return c.bad;
-    c10::cuda::CUDAGuard device((c10::DeviceIndex)c.index);
+    Outside outside(c);
     return pw_route_tokens(c.ctx, &r, l.data, l.type, l.stride, static_cast<float*>(b.data), (int)l.rows, static_cast<int32_t*>(ids.data),
                            static_cast<float*>(gates.data), c.stream);
   });
@@ -193,10 +206,11 @@ PyObject* moe_forward_routed(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Matrix h = matrix(c, a[1], 2, PW_F16, -1, PyLong_AsLongLong(a[6]), true);
     const Matrix ids = matrix(c, a[2], 3, kWords, h.rows, -1, true), gates = matrix(c, a[3], 4, PW_F32, h.rows, ids.cols, true);
     const Matrix out = matrix(c, a[4], 5, PW_F32, h.rows, h.cols, true);
+    const pw_mode mode = (pw_mode)PyLong_AsLong(a[5]);
     if (c.bad) return c.bad;
-    c10::cuda::CUDAGuard device((c10::DeviceIndex)c.index);
+    Outside outside(c);
     return pw_moe_forward_routed(c.ctx, layer, h.data, static_cast<int32_t*>(ids.data), static_cast<float*>(gates.data), (int)h.rows, (int)ids.cols, nullptr,
-                                 static_cast<float*>(out.data), (pw_mode)PyLong_AsLong(a[5]), c.stream);
+                                 static_cast<float*>(out.data), mode, c.stream);
   });
 }
 

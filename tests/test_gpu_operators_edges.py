@@ -78,3 +78,68 @@ def test_logits_of_a_product_directly_ahead_of_the_layer(T, n_experts, mode):
         assert not torch.equal(steps[0][2], steps[1][2]) and c.pw_last_device_status() == 0
     finally:
         c.close()
+
+
+def test_other_threads_run_while_a_call_waits_for_the_queue(ctx):
+    """A stream whose queue is full holds the call that launches, not the interpreter."""
+    x, w = randn(1, 1, 256), randn(2, 256)
+    y, s = torch.empty(1, 256, dtype=F16, device="cuda"), torch.cuda.Stream()
+    ctx.pw_add_rmsnorm(x, w, y=y, stream=s)
+    torch.cuda.synchronize()
+    gap, stop = [0.0], threading.Event()
+
+    def watch():
+        last = time.perf_counter()
+        while not stop.is_set():
+            time.sleep(0.001)
+            now = time.perf_counter()
+            gap[0], last = max(gap[0], now - last), now
+
+    other = threading.Thread(target=watch)
+    other.start()
+    try:
+        start = time.perf_counter()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(2_000_000_000)                 # about a second
+        for _ in range(4000):
+            ctx.pw_add_rmsnorm(x, w, y=y, stream=s)
+        waited = time.perf_counter() - start
+    finally:
+        stop.set()
+        other.join()
+        torch.cuda.synchronize()
+    assert gap[0] < 0.25, (gap[0], waited)
+
+
+def test_first_products_on_several_threads():
+    """The first product of a context looks things up; four threads make it at the same time, and all launches count."""
+    c = B.Context(1, 8, 0, 256, 512, 16, 2)
+    try:
+        sets = [operands(c, T, N, K, seed=T) for T, N, K in ((3, 2000, 1100), (40, 1000, 2100), (300, 500, 700), (1000, 520, 260))]
+        before, outs, errors = c.pw_launch_count(), [[] for _ in sets], []
+        torch.cuda.synchronize()
+        ready = threading.Barrier(4)
+
+        def work(i):
+            try:
+                s = torch.cuda.Stream()
+                ready.wait()
+                for _ in range(500):
+                    outs[i] = outs[i][-3:] + [c.pw_scaled_linear(*sets[i], out_dtype=F32, stream=s)]
+                s.synchronize()
+            except Exception as e:                           # noqa: BLE001 - reported by the test
+                errors.append(e)
+
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not errors and c.pw_launch_count() - before == 2000
+        for i, (T, N) in enumerate(((3, 2000), (40, 1000), (300, 500), (1000, 520))):
+            out = torch.empty(T, N, device="cuda")
+            check_linear(c, *sets[i], out)
+            assert all(torch.equal(o, out) for o in outs[i])
+        assert c.pw_last_device_status() == 0
+    finally:
+        c.close()
