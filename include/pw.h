@@ -358,8 +358,9 @@ pw_status pw_add_rmsnorm(pw_ctx* ctx, int T, int H, const void* x, int x_type, i
 
 /* Product of two scaled 8-bit matrices: out[t, n] = sum_k a[t, k] * w[n, k], a [T, K] with block_rows 1, w [N, K] with
  * block_rows 128 (the layout of a linear-block: output features x input features).  Sums in fp32 in a fixed order,
- * rounded once to out_type.  Any T, N, K from 1 on.  A device-side wait that runs out is reported by
- * pw_last_device_status.
+ * rounded once to out_type.  The product of two scales may lie outside fp32's range on either side: it loses no bits and
+ * does not overflow by itself, only the sums do (one that has become infinite stays so).  Any T, N, K from 1 on.
+ * A device-side wait that runs out is reported by pw_last_device_status.
  * Errors: INVALID_ARG, SHAPE (a stride below the row's length; T, N or K over 2^30), ALIGN (a pointer, or a code stride,
  * not a multiple of 16), CUDA. */
 pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const void* a_codes, int64_t a_stride,

@@ -4,7 +4,8 @@
 //
 // The inner sums run on the tensor cores (tcgen05.mma, kind::f8f6f4: products of e4m3 codes, fp32 sums in tensor
 // memory), one fresh accumulator per block of 128 columns; the scales are applied in fp32 on its way from tensor memory
-// to registers, where the sums over the blocks stay.
+// to registers, where the sums over the blocks stay.  Their product is rounded once; where it leaves fp32's range, or has
+// fewer than 24 bits there, a power of two goes onto the block's sum instead (split_factor).
 #include <cuda.h>
 
 #include "pw_ptx.cuh"
@@ -188,14 +189,36 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t addr_s, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr_s), "r"(rank));
   return r;
 }
+// What a block's sum is multiplied with: the product of two scales, as f * m with m a power of two.  Scales are 2^-126 or
+// more and sums 2^-18 to 2^24.7 (or 0), so that the product of two scales can leave fp32's range on either side where the
+// result does not.  m goes onto the sum first, exactly, and f keeps its 24 bits: below the range down to 2^-174, where even
+// the largest sum underflows, above it up to 2^176, where the smallest one overflows.
+struct Factor {
+  float f, m;
+};
+__device__ __forceinline__ Factor split_factor(float x, float y) {
+  Factor r{x * y, 1.f};
+  if (x == 0.f || y == 0.f || !(fabsf(x) <= 3.402823466e38f && fabsf(y) <= 3.402823466e38f)) return r;
+  if (fabsf(r.f) < 1.17549435e-38f) {
+    r.f = (x * 16777216.f) * (y * 16777216.f);                  // 2^24 each
+    r.m = 3.5527137e-15f;                                       // 2^-48
+  } else if (fabsf(r.f) > 3.402823466e38f) {
+    r.f = fminf(fmaxf((x * 5.9604645e-8f) * (y * 5.9604645e-8f), -3.402823466e38f), 3.402823466e38f);
+    r.m = 2.8147498e14f;
+  }
+  return r;
+}
 // Scales of ROWS rows and the blocks g .. g + 7, one warp: a sector of 32 bytes per row, all loads in flight together,
 // written as [block][row], times a factor (rows padded by four, which keeps both sides free of bank conflicts).  Rows
-// and blocks past the end get 0.
+// and blocks past the end get 0.  Returns whether split_factor has anything to do for one of these scales and w0 or w1,
+// a lane's scales of the weights for block g + lane % 8: a lane's smallest and largest scale tell.
 template <int ROWS>
-__device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T, int G, int g, int g_end, float times, float* dst, int lane) {
+__device__ __forceinline__ bool load_scales(const float* sa, int64_t row0, int T, int G, int g, int g_end, float times, float w0, float w1, float* dst,
+                                            int lane) {
   constexpr int kLoads = ROWS / 4 < 16 ? ROWS / 4 : 16;      // in flight at a time
   const int j = lane & 7, r0 = lane >> 3;
   const bool in = g + j < g_end;
+  float low = INFINITY, high = 0.f;
 #pragma unroll 1
   for (int base = 0; base < ROWS; base += kLoads * 4) {
     float v[kLoads];
@@ -205,8 +228,14 @@ __device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T
       v[i] = in && r < T ? sa[r * G + g + j] : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) dst[j * (ROWS + 4) + base + i * 4 + r0] = v[i] * times;
+    for (int i = 0; i < kLoads; ++i) {
+      low = fminf(low, v[i] == 0.f ? INFINITY : fabsf(v[i]));
+      high = fmaxf(high, fabsf(v[i]));
+      dst[j * (ROWS + 4) + base + i * 4 + r0] = v[i] * times;
+    }
   }
+  auto leaves = [&](float w) { return w != 0.f && high > 0.f && (low * fabsf(w) < 1.17549435e-38f || high * fabsf(w) > 3.402823466e38f); };
+  return __any_sync(0xffffffffu, leaves(w0) || leaves(w1));
 }
 
 // ---- few rows: the weights on the M side ---------------------------------------------------------
@@ -261,6 +290,7 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
   __shared__ uint32_t tmem_base;
   __shared__ volatile int gave_up;
   __shared__ alignas(16) float scales[2][kScaleRun][NT + 4];     // read four at a time
+  __shared__ int extreme_run[2];                                   // whether split_factor has anything to do for them
   const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u, sums_s = ring_s + S * 2 * C::kBlock;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x % split);
@@ -355,7 +385,8 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
         const float w = g + (lane & 7) < g1 ? sw[g + (lane & 7)] : 0.f;
         if (run >= 2) ok = mbar_wait(smem_u32(&sc_empty[run & 1]), ((run >> 1) - 1) & 1, &gave_up, a.polls, a.status);
         if (!ok) break;
-        load_scales<NT>(a.sa, (int64_t)(u % token_tiles) * NT, a.T, a.G, g, g1, w, &scales[run & 1][0][0], lane);
+        const bool any = load_scales<NT>(a.sa, (int64_t)(u % token_tiles) * NT, a.T, a.G, g, g1, w, w, w, &scales[run & 1][0][0], lane);
+        if (lane == 0) extreme_run[run & 1] = any;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sc_full[run & 1]);
       }
@@ -363,7 +394,7 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
   } else {
     const int col = (warp >> 2) * QC, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
-    bool ok = true;
+    bool ok = true, extreme = false;
     int s = 0, run = 0;
     uint32_t par = 0;                              // of the stage's next `done` phase
     uint64_t acc[QC / 2];                          // pairs of tokens: a packed multiply-add does two
@@ -373,7 +404,10 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
       int in_run = 0;
 #pragma unroll 1
       for (int g = g0; ok && g < g1; g += 2) {
-        if (in_run == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+        if (in_run == 0) {
+          ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+          extreme = extreme_run[run & 1] != 0;
+        }
         if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
         if (!ok) break;
         tc_fence_after();
@@ -391,15 +425,31 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&freed[s]);
+        if (extreme) {                               // rare: from the two scales themselves
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (k == 1 && !two) break;
-          const ulonglong2* cs = reinterpret_cast<const ulonglong2*>(scales[run & 1][in_run + k] + col);
+          for (int k = 0; k < 2; ++k) {
+            if (k == 1 && !two) break;
+            const float* sa = a.sa + g + k;
+            const float sw = a.sw[(int64_t)(u / token_tiles) * a.G + g + k];
+            const int t = u % token_tiles * NT + col;
 #pragma unroll
-          for (int j = 0; j < QC / 4; ++j) {
-            const ulonglong2 f = cs[j];
-            acc[2 * j] = fma2(pack2(v[k][4 * j], v[k][4 * j + 1]), f.x, acc[2 * j]);
-            acc[2 * j + 1] = fma2(pack2(v[k][4 * j + 2], v[k][4 * j + 3]), f.y, acc[2 * j + 1]);
+            for (int j = 0; j < QC; j += 2) {
+              const Factor x = split_factor(t + j < a.T ? sa[(int64_t)(t + j) * a.G] : 0.f, sw);
+              const Factor y = split_factor(t + j + 1 < a.T ? sa[(int64_t)(t + j + 1) * a.G] : 0.f, sw);
+              acc[j / 2] = fma2(pack2(v[k][j] * x.m, v[k][j + 1] * y.m), pack2(x.f, y.f), acc[j / 2]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if (k == 1 && !two) break;
+            const ulonglong2* cs = reinterpret_cast<const ulonglong2*>(scales[run & 1][in_run + k] + col);
+#pragma unroll
+            for (int j = 0; j < QC / 4; ++j) {
+              const ulonglong2 f = cs[j];
+              acc[2 * j] = fma2(pack2(v[k][4 * j], v[k][4 * j + 1]), f.x, acc[2 * j]);
+              acc[2 * j + 1] = fma2(pack2(v[k][4 * j + 2], v[k][4 * j + 3]), f.y, acc[2 * j + 1]);
+            }
           }
         }
         in_run += 2;
@@ -603,6 +653,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
   __shared__ uint32_t tmem_base;
   __shared__ volatile int gave_up;
   __shared__ float scales[2][kScaleRun][128 + 4], w_scales[2][2][kScaleRun];
+  __shared__ int extreme_run[2];                     // whether split_factor has anything to do for them
   const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const uint32_t rank = blockIdx.x & 1;           // cluster of two along x
@@ -692,7 +743,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
           if (run >= 2) ok = mbar_wait(smem_u32(&sc_empty[run & 1]), ((run >> 1) - 1) & 1, &gave_up, a.polls, a.status);
           if (!ok) break;
           if (lane < 16) w_scales[run & 1][lane >> 3][lane & 7] = w;
-          load_scales<128>(a.sa, m0, a.T, a.G, g, a.G, 1.f, &scales[run & 1][0][0], lane);
+          const float w0 = __shfl_sync(0xffffffffu, w, lane & 7), w1 = __shfl_sync(0xffffffffu, w, 8 + (lane & 7));
+          const bool any = load_scales<128>(a.sa, m0, a.T, a.G, g, a.G, 1.f, w0, w1, &scales[run & 1][0][0], lane);
+          if (lane == 0) extreme_run[run & 1] = any;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sc_full[run & 1]);
         }
@@ -708,53 +761,72 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     // block is multiplied while the first of the next one is on its way.
     constexpr int Q = HC / 32;
     static_assert(Q % 2 == 0, "a block begins in the first buffer");
-    bool ok = true;
+    bool ok = true, extreme = false;
     int s = 0, b = 0, run = 0, in_run = 0;
     uint32_t par = 0;                               // of the stage's next `done` phase
-    float v[2][32], f = 0.f;
-    // waits for the next block's accumulator (b, s), takes its scale, starts its first load
-    auto begin = [&] {
-      if (in_run == 0) ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+    float v[2][32];
+    // waits for the next block's accumulator (b, s) and its scales, starts its first load
+    auto begin = [&](bool new_run) {
+      if (new_run) {
+        ok = mbar_wait(smem_u32(&sc_full[run & 1]), (run >> 1) & 1, &gave_up, a.polls, a.status);
+        extreme = extreme_run[run & 1] != 0;
+      }
       if (ok) ok = mbar_wait(smem_u32(&done[s]), par, &gave_up, a.polls, a.status);
       if (!ok) return;
       tc_fence_after();
       tmem_ld32(lane_base + b * BN, v[0]);
     };
-    if (pair < n_tiles) begin();
+    if (pair < n_tiles) begin(true);
     for (int t = pair; ok && t < n_tiles; t += n_pairs) {
       uint64_t acc[HC / 2];                         // pairs of columns: a packed multiply-add does two
 #pragma unroll
       for (int j = 0; j < HC / 2; ++j) acc[j] = 0;
+      // The blocks of a run of scales: a loop of each kind.  (4096 x 14336 x 4096 in a loop of calls: 260 us without the rare
+      // kind, 268 so, of which 5 are load_scales' look at the scales; with the test inside one loop 285, inside a block 334.)
+      auto blocks = [&](auto kind, int first, int end) {
+        constexpr bool kExtreme = decltype(kind)::value;
 #pragma unroll 1
-      for (int g = 0; ok && g < a.G; ++g) {
-        f = scales[run & 1][in_run][row] * w_scales[run & 1][col / 128][in_run];
-        const uint64_t ff = pack2(f, f);
+        for (int g = first; ok && g < end; ++g) {
+          const float x = scales[run & 1][in_run][row], y = w_scales[run & 1][col / 128][in_run];
+          const Factor fm = kExtreme ? split_factor(x, y) : Factor{x * y, 1.f};
+          const uint64_t ff = pack2(fm.f, fm.f);
 #pragma unroll
-        for (int c = 0; c < Q; ++c) {
-          tmem_wait32(v[c & 1]);
-          if (c + 1 < Q) {
-            tmem_ld32(lane_base + b * BN + (c + 1) * 32, v[(c + 1) & 1]);
-          } else {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-              arrive_cluster(map_rank(smem_u32(&acc_empty[b]), 0));
-              if (in_run == kScaleRun - 1 || g == a.G - 1) mbar_arrive(&sc_empty[run & 1]);
+          for (int c = 0; c < Q; ++c) {
+            tmem_wait32(v[c & 1]);
+            if constexpr (kExtreme) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[c & 1][j] *= fm.m;
             }
-            if (++in_run == kScaleRun || g == a.G - 1) {
-              in_run = 0;
-              ++run;
+            if (c + 1 < Q) {
+              tmem_ld32(lane_base + b * BN + (c + 1) * 32, v[(c + 1) & 1]);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) {
+                arrive_cluster(map_rank(smem_u32(&acc_empty[b]), 0));
+                if (in_run == kScaleRun - 1 || g == a.G - 1) mbar_arrive(&sc_empty[run & 1]);
+              }
+              if (++in_run == kScaleRun || g == a.G - 1) {
+                in_run = 0;
+                ++run;
+              }
+              b = b + 1 == A ? 0 : b + 1;
+              if (++s == S) {
+                s = 0;
+                par ^= 1u;
+              }
+              if (g + 1 < a.G || t + n_pairs < n_tiles) begin(in_run == 0);
             }
-            b = b + 1 == A ? 0 : b + 1;
-            if (++s == S) {
-              s = 0;
-              par ^= 1u;
-            }
-            if (g + 1 < a.G || t + n_pairs < n_tiles) begin();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fma2(pack2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), ff, acc[c * 16 + j]);
           }
-#pragma unroll
-          for (int j = 0; j < 16; ++j) acc[c * 16 + j] = fma2(pack2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), ff, acc[c * 16 + j]);
         }
+      };
+#pragma unroll 1
+      for (int g = 0; ok && g < a.G; g += kScaleRun) {
+        const int end = min(g + kScaleRun, a.G);
+        if (extreme) blocks(std::true_type{}, g, end);
+        else blocks(std::false_type{}, g, end);
       }
       // (after a wait that gave up the sums are not complete; what is stored is undefined then)
       store_tile<HC>(box_s, box, acc, a, (int64_t)(t % token_tiles) * 256 + rank * 128 + (warp & 3) * 32, (t / token_tiles) * BN + col, lane);

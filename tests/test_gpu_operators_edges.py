@@ -143,3 +143,76 @@ def test_first_products_on_several_threads():
         assert c.pw_last_device_status() == 0
     finally:
         c.close()
+
+
+SCALE_SHAPES = [(5, 300, 1400), (40, 390, 1300), (20, 20000, 390), (64, 19000, 260), (300, 500, 700), (1000, 512, 700), (2048, 4096, 390)]
+
+
+def check_scales(ctx, a, sa, w, sw, out):
+    """As check_linear, with the roundings of sums that are subnormal: one per block, half of 2^-149 each, and one when
+    they are stored, which plain.rounding counts."""
+    ctx.pw_scaled_linear(a, sa, w, sw, out=out)
+    ref, mags = plain.linear(a, sa, w, sw)
+    G = sa.shape[1]
+    bound = mags * (4 * 2.0 ** -22 + (2 + G + 7) * U) + plain.rounding(ref, out.dtype) + (G + 7) * 2.0 ** -150
+    got = plain.f64(out)
+    assert np.isfinite(ref).all() and np.abs(ref).max() < 2.0 ** 127
+    assert np.isfinite(got).all()
+    assert np.all(np.abs(got - ref) <= bound * (1 + 4 * U)), float((np.abs(got - ref) / np.maximum(bound, 1e-300)).max())
+    return ref
+
+
+@pytest.mark.parametrize("out_type", [F32, BF16])
+@pytest.mark.parametrize("T,N,K", SCALE_SHAPES)
+def test_product_of_scales_below_the_range(ctx, T, N, K, out_type):
+    """Products of two scales that are subnormal or 0 in fp32, next to ordinary ones, while their sums are numbers."""
+    a, sa, w, sw = operands(ctx, T, N, K, seed=T)
+    rows = torch.tensor([0, -60, -80, -100, -118], device="cuda")[torch.arange(T, device="cuda") % 5]
+    cols = torch.tensor([0, -20, -30, 10], device="cuda")[torch.arange(sw.shape[1], device="cuda") % 4]
+    sa, sw = torch.ldexp(sa, rows[:, None]), torch.ldexp(sw, cols[None, :])
+    f = plain.f64(sa)[:, :1] * plain.f64(sw)[:1, :]
+    assert (f < 2.0 ** -126).any() and (f < 2.0 ** -149).any() and (f > 2.0 ** -100).any()
+    ref = check_scales(ctx, a, sa, w, sw, torch.empty(T, N, dtype=out_type, device="cuda"))
+    assert np.abs(ref).max() > 2.0 ** -20
+
+
+def test_product_of_scales_the_quantizer_makes(ctx):
+    """Activations near the smallest number that has a scale of its own, weights of ordinary size."""
+    for T in (3, 1000):
+        a, sa = ctx.pw_quantize_scaled(randn(1, T, 700, scale=2.0 ** -119), 1)
+        w, sw = ctx.pw_quantize_scaled(randn(2, 600, 700, scale=0.01), 128)
+        check_scales(ctx, a, sa, w, sw, torch.empty(T, 600, device="cuda"))
+
+
+@pytest.mark.parametrize("out_type", [F32, BF16])
+@pytest.mark.parametrize("T,N,K", SCALE_SHAPES)
+def test_product_of_scales_above_the_range(ctx, T, N, K, out_type):
+    """Products of two scales over the largest number: sums of the smallest codes are numbers, and sums of 0 are 0."""
+    def small(rows, seed):
+        q, s = B.scaled_empty(rows, K, 1)
+        q.view(torch.uint8).copy_(torch.randint(0, 3, (rows, K), generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda",
+                                                dtype=torch.uint8))                 # 0, 2^-9, 2^-8
+        q.view(torch.uint8)[::2] |= 0x80
+        return q
+    a, w = small(T, 1), small(N, 2)
+    G = (K + 127) // 128
+    sa = torch.ldexp(torch.ones(T, G, device="cuda"), torch.tensor([0, 60, 62, 100], device="cuda")[torch.arange(T, device="cuda") % 4][:, None])
+    sw = torch.ldexp(torch.ones((N + 127) // 128, G, device="cuda"), torch.tensor([70, 10, 68], device="cuda")[torch.arange(G, device="cuda") % 3][None, :])
+    a.view(torch.uint8)[3::4] = 0                                  # 2^100 * 2^70 times nothing
+    check_scales(ctx, a, sa, w, sw, torch.empty(T, N, dtype=out_type, device="cuda"))
+
+
+def test_product_of_scales_out_of_every_range(ctx):
+    """What overflows is infinite, with the sign of the first block's sum (an fp32 sum that is infinite stays so, whatever
+    finite product is added); what underflows is 0; a scale that is no number stays visible."""
+    for T in (3, 1000):
+        a, sa, w, sw = operands(ctx, T, 500, 200, seed=3)
+        ref = plain.linear(a[:, :128], sa[:, :1], w[:, :128], sw[:, :1])[0]
+        big = ctx.pw_scaled_linear(a, sa * 2.0 ** 110, w, sw * 2.0 ** 110, out_dtype=F32).cpu().numpy()
+        assert np.array_equal(big, np.where(ref > 0, np.inf, -np.inf))
+        none = ctx.pw_scaled_linear(a, torch.ldexp(sa, torch.tensor(-110, device="cuda")), w, torch.ldexp(sw, torch.tensor(-110, device="cuda")), out_dtype=F32)
+        assert bool((none == 0).all())
+        bad = sa.clone()
+        bad[1], bad[2, 1] = math.inf, math.nan
+        out = ctx.pw_scaled_linear(a, bad, w, sw, out_dtype=F32).cpu().numpy()
+        assert not np.isfinite(out[1:3]).any() and np.isnan(out[2]).all() and np.isfinite(out[0]).all()
