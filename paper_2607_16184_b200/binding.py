@@ -88,15 +88,31 @@ _lib = None
 _pwtorch = None
 
 
+def _load_pwtorch():
+    """The compiled marshalling, on the first call that goes through it.  Raises if it is missing or was built for another
+    torch or Python; libpw.so and the calls through ctypes do without it."""
+    global _pwtorch
+    from .build import module_stamp
+    load()
+    try:
+        from . import _pwtorch as module               # loads libpw.so next to it
+    except ImportError as e:
+        raise RuntimeError("_pwtorch.so is missing or does not load (%s): run `python -m paper_2607_16184_b200.build`" % e) from e
+    if getattr(module, "built_for", None) != module_stamp():
+        raise RuntimeError("_pwtorch.so was built for %s, this is %s: run `python -m paper_2607_16184_b200.build`" %
+                           (getattr(module, "built_for", "something else"), module_stamp()))
+    _pwtorch = module
+    return module
+
+
 def load():
     """Loads libpw.so (built by ``paper_2607_16184_b200.build``).  Raises if it is missing."""
-    global _lib, _pwtorch
+    global _lib
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libpw.so is missing: run `python -m paper_2607_16184_b200.build` (there is no fallback path)")
     L = C.CDLL(LIB_PATH)
-    from . import _pwtorch                          # loads libpw.so next to it
     vp, i32, u32, sz = C.c_void_p, C.c_int, C.c_uint32, C.c_size_t
     L.pw_workspace_bytes.restype = sz
     L.pw_workspace_bytes.argtypes = [C.POINTER(pw_config)]
@@ -585,7 +601,7 @@ class Context:
         """The layer call for a routing the caller has (ids [T, k], -1 = no expert; gates [T, k])."""
         if out is None:
             out = self._new(stream, lambda: torch.empty(hidden.shape, dtype=torch.float32, device=self.device))
-        st = _pwtorch.moe_forward_routed(self._ptr, self._index, None if stream is None else stream.cuda_stream, layer, hidden, topk_ids,
+        st = (_pwtorch or _load_pwtorch()).moe_forward_routed(self._ptr, self._index, None if stream is None else stream.cuda_stream, layer, hidden, topk_ids,
                                          gates, out, mode, self.cfg.hidden)
         if st:
             self._refused(st, "pw_moe_forward_routed", ("layer", "hidden", "topk_ids", "gates", "out"))
@@ -610,7 +626,7 @@ class Context:
         """(codes, scales) of a matrix in the scaled 8-bit format; block_rows 1 (activations) or 128 (weights)."""
         if q is None and scales is None and x.dim() == 2 and block_rows > 0:
             q, scales = self._new(stream, lambda: scaled_empty(x.shape[0], x.shape[1], block_rows, self.device))
-        st = _pwtorch.quantize_scaled(self._ptr, self._index, None if stream is None else stream.cuda_stream, x, block_rows, q, scales)
+        st = (_pwtorch or _load_pwtorch()).quantize_scaled(self._ptr, self._index, None if stream is None else stream.cuda_stream, x, block_rows, q, scales)
         if st:
             self._refused(st, "pw_quantize_scaled", ("x", "block_rows", "q", "scales"))
         return q, scales
@@ -624,7 +640,7 @@ class Context:
         it makes an fp16 y."""
         if y is None and q is None:
             y = self._new(stream, lambda: torch.empty(x.shape, dtype=torch.float16, device=self.device))
-        st = _pwtorch.add_rmsnorm(self._ptr, self._index, None if stream is None else stream.cuda_stream, x, weight, eps, residual,
+        st = (_pwtorch or _load_pwtorch()).add_rmsnorm(self._ptr, self._index, None if stream is None else stream.cuda_stream, x, weight, eps, residual,
                                   residual_out, y, q, q_scales)
         if st:
             self._refused(st, "pw_add_rmsnorm", ("x", "weight", "eps", "residual", "residual_out", "y", "q", "q_scales"))
@@ -636,7 +652,7 @@ class Context:
         """out [T, N] = a [T, K] . w [N, K]^T, both in the scaled 8-bit format (a: block_rows 1, w: block_rows 128)."""
         if out is None:
             out = self._new(stream, lambda: torch.empty(a.shape[0], w.shape[0], dtype=out_dtype, device=self.device))
-        st = _pwtorch.scaled_linear(self._ptr, self._index, None if stream is None else stream.cuda_stream, a, a_scales, w, w_scales, out)
+        st = (_pwtorch or _load_pwtorch()).scaled_linear(self._ptr, self._index, None if stream is None else stream.cuda_stream, a, a_scales, w, w_scales, out)
         if st:
             self._refused(st, "pw_scaled_linear", ("a", "a_scales", "w", "w_scales", "out"))
         return out
@@ -651,7 +667,7 @@ class Context:
             shape = (router_logits.shape[0], top_k)
             ids, gates = self._new(stream, lambda: (torch.empty(shape, dtype=torch.int32, device=self.device),
                                                     torch.empty(shape, dtype=torch.float32, device=self.device)))
-        st = _pwtorch.route_tokens(self._ptr, self._index, None if stream is None else stream.cuda_stream, router_logits, top_k,
+        st = (_pwtorch or _load_pwtorch()).route_tokens(self._ptr, self._index, None if stream is None else stream.cuda_stream, router_logits, top_k,
                                    _SCORES.get(score, -1), bias, n_groups, top_groups, group_best, renormalize, scale, ids, gates)
         if st:
             self._refused(st, "pw_route_tokens", ("router_logits", "top_k", "score", "bias", "n_groups", "top_groups", "group_best",

@@ -29,18 +29,32 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def module_stamp() -> str:
+    """What the module has to be built for to load: it uses torch's C++ interface and this Python's."""
+    import torch
+    return "torch %s, python %d.%d" % ((torch.__version__,) + sys.version_info[:2])
+
+
+def module_is_current() -> bool:
+    deps = (MODULE_SOURCE, os.path.join(HERE, "..", "include", "pw.h"))
+    if not os.path.exists(MODULE) or any(os.path.getmtime(d) > os.path.getmtime(MODULE) for d in deps):
+        return False
+    with open(MODULE, "rb") as f:
+        return (module_stamp() + "\0").encode() in f.read()
+
+
 def build_module(force: bool = False) -> str:
     """The CPython module that marshals torch tensors for the calls of libpw.so."""
-    deps = (MODULE_SOURCE, os.path.join(HERE, "..", "include", "pw.h"))
-    if not force and os.path.exists(MODULE) and all(os.path.getmtime(d) <= os.path.getmtime(MODULE) for d in deps):
+    if not force and module_is_current():
         return MODULE
     import torch
     from torch.utils import cpp_extension
     dirs = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
-    subprocess.check_call(["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch.compiled_with_cxx11_abi())] +
-                          ["-I" + d for d in dirs] + [MODULE_SOURCE, "-o", MODULE, "-L" + libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L" + HERE, "-l:libpw.so",
-                                                      "-Wl,-rpath,$ORIGIN"])
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch.compiled_with_cxx11_abi()),
+                           '-DPW_BUILT_FOR="%s"' % module_stamp()] + [a for d in dirs for a in ("-isystem", d)] +
+                          [MODULE_SOURCE, "-o", MODULE, "-L" + libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L" + HERE, "-l:libpw.so",
+                           "-Wl,-rpath,$ORIGIN"])
     return MODULE
 
 

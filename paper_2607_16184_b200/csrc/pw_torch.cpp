@@ -221,4 +221,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pwtorch", "Argument marshalling f
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__pwtorch(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__pwtorch(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", PW_BUILT_FOR) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
