@@ -22,7 +22,8 @@
  *     on the device (a bounded wait that ran out, a failed self check) are written
  *     to a status word that pw_last_device_status reads back.
  *   - Every device pointer must be 16-byte aligned.  rows and cols of a block
- *     must be multiples of 128.  Inputs must be finite.
+ *     must be multiples of 128.  Inputs must be finite, except where a call says
+ *     what becomes of other numbers.
  */
 #ifndef PW_H_
 #define PW_H_
@@ -301,12 +302,24 @@ pw_status pw_plane_state(pw_ctx* ctx, int layer, int expert, int kind, int plane
  * hidden_fp16: device [T, H] fp16.  router_logits: device [T, E] fp32.  out: device [T, H] fp32.
  * table: pw_get_page_table(ctx) or NULL (same thing).  All rows of `layer` must have been
  * published.  Operands of the contractions are fp16, accumulation is fp32.
+ * The call works in the context's workspace: the forward calls of a context follow one another, on one stream or ordered
+ * by the caller; two at a time need two contexts.
  * Errors: INVALID_ARG (T < 1, T > max_tokens, top_k < 1, top_k > min(E, max_top_k), bad layer),
  * ALIGN, STATE (a row of the layer is unpublished). */
 pw_status pw_moe_forward(pw_ctx* ctx, int layer, const void* hidden_fp16, const float* router_logits, int T,
                          int top_k, const pw_page_table* table, float* out, pw_mode mode, pw_stream stream);
 
-/* The same layer call for callers whose activations live in host memory: copies hidden_host
+/* The layer call for a routing that the caller has: topk_ids int32 [T, top_k] and gates fp32 [T, top_k], both device,
+ * e.g. from pw_route_tokens.  A pair with id -1 takes no expert and adds nothing (shared experts still see the token).
+ * An id outside -1 .. n_experts - 1 is treated like -1 and reported by pw_last_device_status as INVALID_ARG.
+ * pw_get_routing then returns the pairs as they were used: perm ends with -1 for every pair without an expert, and
+ * counts, offsets leave them out.  With the ids and gates of pw_moe_forward's own rule the output is the same, bit for
+ * bit.  Pages, page table, workspace and errors: as pw_moe_forward. */
+pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16, const int32_t* topk_ids,
+                                const float* gates, int T, int top_k, const pw_page_table* table, float* out, pw_mode mode,
+                                pw_stream stream);
+
+/* pw_moe_forward for callers whose activations live in host memory: copies hidden_host
  * ([T, H] fp16) and logits_host ([T, E] fp32) to staging buffers in the workspace, runs
  * pw_moe_forward on them and copies the fp32 result to out_host ([T, H]), all ordered on `stream`.
  * The three host buffers should be pinned for the copies to be asynchronous, and must stay valid
@@ -318,9 +331,9 @@ pw_status pw_moe_forward_host(pw_ctx* ctx, int layer, const void* hidden_host, c
 /* ---- around the layer ----------------------------------------------------------------- */
 
 /* What a program computes between two layer calls: the residual's addition and the norm in front of the layer, the
- * router's choice where it is another rule than pw_moe_forward's, and dense products (the router's logits, the
- * projections around the layer) on 8-bit operands.  (The paper starts at the router's logits; these calls have no
- * counterpart in it.)  They need a context of the current device, but neither pages nor the page table; nothing is
+ * router's choice where it is another rule than pw_moe_forward's (pw_moe_forward_routed, above, takes it), and dense
+ * products (the router's logits, the projections around the layer) on 8-bit operands.  (The paper starts at the router's
+ * logits; these calls have no counterpart in it.)  They need a context of the current device, but neither pages nor the page table; nothing is
  * kept between calls and no workspace is used, so calls on different streams may run at the same time.
  * Row strides count elements; rows may be further apart than they are long, and what lies between and behind them is
  * left as it was.  A call for zero rows is valid and enqueues nothing. */
@@ -394,15 +407,7 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
                           int64_t logits_stride, const float* bias, int T, int32_t* topk_ids, float* gates,
                           pw_stream stream);
 
-/* pw_moe_forward for a routing that the caller has: topk_ids int32 [T, top_k] and gates fp32 [T, top_k], both device,
- * e.g. from pw_route_tokens.  A pair with id -1 takes no expert and adds nothing (shared experts still see the token).
- * An id outside -1 .. n_experts - 1 is treated like -1 and reported by pw_last_device_status as INVALID_ARG.
- * pw_get_routing then returns the pairs as they were used: perm ends with -1 for every pair without an expert, and
- * counts, offsets leave them out.  With the ids and gates of pw_moe_forward's own rule the output is the same, bit for
- * bit.  Errors: as pw_moe_forward. */
-pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16, const int32_t* topk_ids,
-                                const float* gates, int T, int top_k, const pw_page_table* table, float* out, pw_mode mode,
-                                pw_stream stream);
+/* ---- routing of a call ----------------------------------------------------------------- */
 
 /* The routing decision of the last forward call (Sec. 2.1: top-k experts per token and their gates; Sec. 3.3:
  * the grouping of the routed pairs by expert), copied out of the workspace (device pointers, any may

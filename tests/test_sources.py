@@ -45,3 +45,15 @@ def test_first_kernels_of_the_layer_read_the_callers_buffers_through_plain_point
     for name in ("logits", "ids_in", "gates_in"):
         declared = re.findall(r"const (?:float|int32_t)\*\s*(__restrict__)?\s*%s\b" % name, text)
         assert declared and not any(declared), name
+
+
+def test_header_says_which_calls_use_the_workspace():
+    """Calls of the section around the layer may run at the same time; those that work in the context's workspace stand
+    with pw_moe_forward, which says that they may not."""
+    header = open(os.path.join(CSRC, "..", "..", "include", "pw.h")).read()
+    sections = re.split(r"/\* -{3,} ([^-]+?) -{3,} \*/", header)
+    where = {name: text for name, text in zip(sections[1::2], sections[2::2])}
+    calls = {name: set(re.findall(r"^pw_status (pw_[a-z_]+)\(", text, re.M)) for name, text in where.items()}
+    assert calls["around the layer"] == {"pw_quantize_scaled", "pw_add_rmsnorm", "pw_scaled_linear", "pw_route_tokens"}
+    assert {"pw_moe_forward", "pw_moe_forward_routed", "pw_moe_forward_host"} <= calls["forward"]
+    assert "two at a time need two contexts" in where["forward"]
