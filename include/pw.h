@@ -350,7 +350,8 @@ typedef enum { PW_F32 = 0, PW_F16 = 1, PW_BF16 = 2 } pw_type;
  *
  * pw_quantize_scaled: x device [rows, cols] of x_type.  The codes' bytes past `cols` in a row are not written.
  * Errors: INVALID_ARG (a null pointer, block_rows neither 1 nor 128, cols < 1), SHAPE (stride below cols; cols over
- * 2^30), ALIGN (a pointer, or q_stride, not a multiple of 16), CUDA. */
+ * 2^30), ALIGN (a pointer, or q_stride, not a multiple of 16), CUDA.  Strides of a matrix of one row are not looked at,
+ * here and below. */
 pw_status pw_quantize_scaled(pw_ctx* ctx, const void* x, int x_type, int rows, int cols, int64_t x_stride,
                              int block_rows, void* q, int64_t q_stride, float* scales, pw_stream stream);
 

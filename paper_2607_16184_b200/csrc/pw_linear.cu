@@ -1002,7 +1002,7 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
   const void* ptrs[5] = {a_codes, a_scales, w_codes, w_scales, out};
   for (const void* p : ptrs)
     if (!is_aligned(p, 16)) return PW_ERR_ALIGN;
-  if (a_stride % 16 || w_stride % 16) return PW_ERR_ALIGN;
+  if ((T > 1 && a_stride % 16) || (N > 1 && w_stride % 16)) return PW_ERR_ALIGN;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
   const pw_status st = linear_setup(ctx);
@@ -1026,8 +1026,8 @@ extern "C" pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const vo
   if (p.units > 0x7fffffff) return PW_ERR_SHAPE;
   // a single row's stride is never used: give the map one that it accepts
   const int64_t pitch = ((int64_t)K + 15) / 16 * 16, out_pitch = T > 1 ? out_stride : N;
-  if (!codes_map(encode, a_codes, T, K, a_stride < pitch ? pitch : a_stride, p.bn ? 128 : p.nt, &a.ma) ||
-      !codes_map(encode, w_codes, N, K, w_stride < pitch ? pitch : w_stride, p.bn ? p.bn / 2 : 128, &a.mw))
+  if (!codes_map(encode, a_codes, T, K, T > 1 ? a_stride : pitch, p.bn ? 128 : p.nt, &a.ma) ||
+      !codes_map(encode, w_codes, N, K, N > 1 ? w_stride : pitch, p.bn ? p.bn / 2 : 128, &a.mw))
     return PW_ERR_CUDA;
   // the copies of output boxes are cut at a row's end in units of 16 bytes only
   const int size = type_size(out_type);

@@ -457,7 +457,7 @@ extern "C" pw_status pw_add_rmsnorm(pw_ctx* ctx, int T, int H, const void* x, in
   const void* ptrs[7] = {x, residual, weight, residual_out, y, q, q_scales};
   for (const void* p : ptrs)
     if (!is_aligned(p, 16)) return PW_ERR_ALIGN;
-  if (q && q_stride % 16) return PW_ERR_ALIGN;
+  if (q && T > 1 && q_stride % 16) return PW_ERR_ALIGN;       // (a single row's stride is never used)
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
   NormArgs a{};
@@ -496,7 +496,7 @@ extern "C" pw_status pw_quantize_scaled(pw_ctx* ctx, const void* x, int x_type, 
   if (rows == 0) return PW_OK;
   if (!x || !q || !scales) return PW_ERR_INVALID_ARG;
   if (rows > 1 && (x_stride < cols || q_stride < cols)) return PW_ERR_SHAPE;
-  if (!is_aligned(x, 16) || !is_aligned(q, 16) || !is_aligned(scales, 16) || q_stride % 16) return PW_ERR_ALIGN;
+  if (!is_aligned(x, 16) || !is_aligned(q, 16) || !is_aligned(scales, 16) || (rows > 1 && q_stride % 16)) return PW_ERR_ALIGN;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
   QuantArgs a{x, static_cast<uint8_t*>(q), scales, x_stride, q_stride, rows, cols};

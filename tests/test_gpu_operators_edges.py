@@ -216,3 +216,25 @@ def test_product_of_scales_out_of_every_range(ctx):
         bad[1], bad[2, 1] = math.inf, math.nan
         out = ctx.pw_scaled_linear(a, bad, w, sw, out_dtype=F32).cpu().numpy()
         assert not np.isfinite(out[1:3]).any() and np.isnan(out[2]).all() and np.isfinite(out[0]).all()
+
+
+@pytest.mark.parametrize("cols", [1, 300, 264])
+def test_single_rows_of_codes_as_they_lie(ctx, cols):
+    """One row needs no stride: contiguous codes of a width that is no multiple of 16, and a stride that is one of nothing."""
+    x, w, r = randn(1, 1, cols), randn(2, cols), randn(3, 1, cols)
+    for q in (torch.empty(1, cols, dtype=torch.uint8, device="cuda"), torch.empty(5000, dtype=torch.uint8, device="cuda").as_strided((1, cols), (1237, 1))):
+        want, scales = ctx.pw_quantize_scaled(x, 1)
+        _, s = ctx.pw_quantize_scaled(x, 1, q=q, scales=torch.empty_like(scales))
+        assert torch.equal(q, want.view(torch.uint8)) and torch.equal(s, scales)
+        want, scales = B.scaled_empty(1, cols, 1)
+        ctx.pw_add_rmsnorm(x, w, residual=r, q=want, q_scales=scales)
+        _, _, _, s = ctx.pw_add_rmsnorm(x, w, residual=r, q=q, q_scales=torch.empty_like(scales))
+        assert torch.equal(q, want.view(torch.uint8)) and torch.equal(s, scales)
+        many, ms = ctx.pw_quantize_scaled(randn(4, 200, cols), 128)
+        out = torch.empty(1, 200, device="cuda")
+        check_linear(ctx, q.view(torch.float8_e4m3fn), s, many, ms, out)
+        assert torch.equal(out, ctx.pw_scaled_linear(want, scales, many, ms, out_dtype=F32))
+        one, os = ctx.pw_quantize_scaled(x, 128, q=q, scales=torch.empty_like(scales))
+        for T in (1, 70, 1000):
+            a, sa = ctx.pw_quantize_scaled(randn(5, T, cols), 1)
+            check_linear(ctx, a, sa, one.view(torch.float8_e4m3fn), os, torch.empty(T, 1, device="cuda"))
