@@ -604,7 +604,7 @@ class Context:
         st = (_pwtorch or _load_pwtorch()).moe_forward_routed(self._ptr, self._index, None if stream is None else stream.cuda_stream, layer, hidden, topk_ids,
                                          gates, out, mode, self.cfg.hidden)
         if st:
-            self._refused(st, "pw_moe_forward_routed", ("layer", "hidden", "topk_ids", "gates", "out"))
+            self._refused(st, "pw_moe_forward_routed", ("layer", "hidden", "topk_ids", "gates", "out", "mode"))
         return out
 
     # ---- around the layer ----

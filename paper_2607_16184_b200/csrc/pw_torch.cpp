@@ -33,6 +33,24 @@ struct Call {
   void fail(int status, int arg) {
     if (!bad) bad = status | arg << 8;
   }
+  // Arguments that are no tensors.  What is not of the kind leaves Python's error set and the call not made; what does
+  // not fit the C type is an invalid argument, never another one.
+  int integer(PyObject* o, int arg) {
+    int overflow = 0;
+    const long v = PyLong_AsLongAndOverflow(o, &overflow);
+    if (overflow || v < INT32_MIN || v > INT32_MAX || (v == -1 && PyErr_Occurred())) return fail(PW_ERR_INVALID_ARG, arg), -1;
+    return (int)v;
+  }
+  float number(PyObject* o, int arg) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) fail(PW_ERR_INVALID_ARG, arg);
+    return (float)v;
+  }
+  int truth(PyObject* o, int arg) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) fail(PW_ERR_INVALID_ARG, arg);
+    return v;
+  }
 };
 
 struct Matrix {
@@ -126,7 +144,7 @@ PyObject* guarded(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F f) {
 PyObject* quantize_scaled(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded(args, n, 7, [](Call& c, PyObject* const* a) -> int {
     const Matrix x = matrix(c, a[0], 1, -1);
-    const int block = (int)PyLong_AsLong(a[1]);
+    const int block = c.integer(a[1], 2);
     if (block != 1 && block != kGroup) c.fail(PW_ERR_INVALID_ARG, 2);
     if (c.bad) return c.bad;
     const Matrix q = matrix(c, a[2], 3, kCodes, x.rows, x.cols), s = scales(c, a[3], 4, x.rows, x.cols, block);
@@ -142,7 +160,7 @@ PyObject* add_rmsnorm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded(args, n, 11, [](Call& c, PyObject* const* a) -> int {
     const Matrix x = matrix(c, a[0], 1, -1);
     const Matrix w = vector(c, a[1], 2, -1, x.cols);
-    const float eps = (float)PyFloat_AsDouble(a[2]);
+    const float eps = c.number(a[2], 3);
     Matrix r, ro, y, q, s;
     if (a[3] != Py_None) r = matrix(c, a[3], 4, -1, x.rows, x.cols);
     if (a[4] != Py_None) {
@@ -182,13 +200,13 @@ PyObject* route_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Matrix l = matrix(c, a[0], 1, -1);
     pw_routing r;
     r.n_experts = (int32_t)l.cols;
-    r.top_k = (int32_t)PyLong_AsLong(a[1]);
-    r.score = (int32_t)PyLong_AsLong(a[2]);
-    r.n_groups = (int32_t)PyLong_AsLong(a[4]);
-    r.top_groups = (int32_t)PyLong_AsLong(a[5]);
-    r.group_best = (int32_t)PyLong_AsLong(a[6]);
-    r.renormalize = PyObject_IsTrue(a[7]);
-    r.scale = (float)PyFloat_AsDouble(a[8]);
+    r.top_k = c.integer(a[1], 2);
+    r.score = c.integer(a[2], 3);
+    r.n_groups = c.integer(a[4], 5);
+    r.top_groups = c.integer(a[5], 6);
+    r.group_best = c.integer(a[6], 7);
+    r.renormalize = c.truth(a[7], 8);
+    r.scale = c.number(a[8], 9);
     Matrix b;
     if (a[3] != Py_None) b = vector(c, a[3], 4, PW_F32, l.cols);
     const Matrix ids = matrix(c, a[9], 10, kWords, l.rows, r.top_k, true), gates = matrix(c, a[10], 11, PW_F32, l.rows, r.top_k, true);
@@ -202,11 +220,11 @@ PyObject* route_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // layer, hidden, topk_ids, gates, out, mode, H
 PyObject* moe_forward_routed(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded(args, n, 10, [](Call& c, PyObject* const* a) -> int {
-    const int layer = (int)PyLong_AsLong(a[0]);
+    const int layer = c.integer(a[0], 1);
     const Matrix h = matrix(c, a[1], 2, PW_F16, -1, PyLong_AsLongLong(a[6]), true);
     const Matrix ids = matrix(c, a[2], 3, kWords, h.rows, -1, true), gates = matrix(c, a[3], 4, PW_F32, h.rows, ids.cols, true);
     const Matrix out = matrix(c, a[4], 5, PW_F32, h.rows, h.cols, true);
-    const pw_mode mode = (pw_mode)PyLong_AsLong(a[5]);
+    const pw_mode mode = (pw_mode)c.integer(a[5], 6);
     if (c.bad) return c.bad;
     Outside outside(c);
     return pw_moe_forward_routed(c.ctx, layer, h.data, static_cast<int32_t*>(ids.data), static_cast<float*>(gates.data), (int)h.rows, (int)ids.cols, nullptr,

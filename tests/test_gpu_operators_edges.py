@@ -238,3 +238,28 @@ def test_single_rows_of_codes_as_they_lie(ctx, cols):
         for T in (1, 70, 1000):
             a, sa = ctx.pw_quantize_scaled(randn(5, T, cols), 1)
             check_linear(ctx, a, sa, one.view(torch.float8_e4m3fn), os, torch.empty(T, 1, device="cuda"))
+
+
+def test_arguments_that_do_not_fit_are_refused_and_nothing_runs(ctx):
+    """Integers beyond 32 bits are not cut to others; what is no number at all raises before anything is launched."""
+    x, big = randn(1, 1, 256), 1 << 32
+    q, s = B.scaled_empty(1, 256, 1)
+    ids, gates = torch.full((1, 2), 7, dtype=torch.int32, device="cuda"), torch.full((1, 2), 7.0, device="cuda")
+    hidden = torch.zeros(1, 256, dtype=F16, device="cuda")
+    torch.cuda.synchronize()
+    before = ctx.pw_launch_count()
+    route = lambda **kw: ctx.pw_route_tokens(x, **{**dict(top_k=2, ids=ids, gates=gates), **kw})
+    for call in (lambda: ctx.pw_quantize_scaled(x, big + 1, q=q, scales=s), lambda: route(top_k=big + 2), lambda: route(top_k=-big + 2),
+                 lambda: route(n_groups=big + 1), lambda: route(top_groups=big + 1), lambda: route(group_best=(1 << 70) + 1), lambda: route(scale=1e300),
+                 lambda: ctx.pw_moe_forward_routed(big, hidden, ids, gates), lambda: ctx.pw_moe_forward_routed(0, hidden, ids, gates, mode=big)):
+        with pytest.raises(B.PwError) as e:
+            call()
+        assert e.value.status == 1, str(e.value)
+    for call in (lambda: ctx.pw_quantize_scaled(x, 1.0, q=q, scales=s), lambda: route(scale=None), lambda: route(scale="1"), lambda: route(n_groups=1.0),
+                 lambda: ctx.pw_add_rmsnorm(x, x[0], eps=None, y=torch.empty_like(x)), lambda: ctx.pw_moe_forward_routed("0", hidden, ids, gates)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(RuntimeError):
+        route(renormalize=torch.zeros(2))
+    torch.cuda.synchronize()
+    assert ctx.pw_launch_count() == before and bool((ids == 7).all()) and bool((gates == 7).all())
