@@ -423,7 +423,9 @@ class Context:
         (``workspace_guards_intact`` looks at them): a check that no kernel writes outside it."""
         self.L = load()
         self.device = torch.device(device)
-        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        if self.device.index is None:               # "cuda": the device that is current now, whichever is at a later call
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        self._index = self.device.index
         cfg = pw_config(n_layers, n_experts, n_shared, hidden, ffn, GROUP, max_tokens, max_top_k, None, 0)
         nbytes = self.L.pw_workspace_bytes(C.byref(cfg))
         if nbytes == 0:

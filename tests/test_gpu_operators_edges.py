@@ -263,3 +263,9 @@ def test_arguments_that_do_not_fit_are_refused_and_nothing_runs(ctx):
         route(renormalize=torch.zeros(2))
     torch.cuda.synchronize()
     assert ctx.pw_launch_count() == before and bool((ids == 7).all()) and bool((gates == 7).all())
+
+
+def test_context_keeps_the_device_it_was_made_on(ctx):
+    """A context of "cuda" belongs to one device, on which its outputs are made whatever device is current later."""
+    assert ctx.device == torch.device("cuda", torch.cuda.current_device())
+    assert ctx.pw_quantize_scaled(randn(1, 2, 128), 1)[0].device == ctx.device == ctx.workspace.device
