@@ -302,6 +302,8 @@ pw_status pw_plane_state(pw_ctx* ctx, int layer, int expert, int kind, int plane
  * hidden_fp16: device [T, H] fp16.  router_logits: device [T, E] fp32.  out: device [T, H] fp32.
  * table: pw_get_page_table(ctx) or NULL (same thing).  All rows of `layer` must have been
  * published.  Operands of the contractions are fp16, accumulation is fp32.
+ * A logit that is NaN counts as -infinity: its expert is taken when fewer than top_k others are left, with gate 0 (a row
+ * without any number has NaN gates, and its output is NaN).
  * The call works in the context's workspace: the forward calls of a context follow one another, on one stream or ordered
  * by the caller; two at a time need two contexts.
  * Errors: INVALID_ARG (T < 1, T > max_tokens, top_k < 1, top_k > min(E, max_top_k), bad layer),

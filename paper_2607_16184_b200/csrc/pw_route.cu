@@ -17,7 +17,7 @@ __device__ __forceinline__ void route_token_n(const float* logits, int token, in
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     const int e = lane + 32 * i;
-    v[i] = e < E ? l[e] : -INFINITY;
+    v[i] = e < E ? fmaxf(l[e], -INFINITY) : -INFINITY;   // a NaN loses every comparison: without k others no expert would be found
   }
   uint32_t taken = 0;
   float l0 = 0.f, S = 0.f, myp = 0.f;

@@ -269,3 +269,37 @@ def test_context_keeps_the_device_it_was_made_on(ctx):
     """A context of "cuda" belongs to one device, on which its outputs are made whatever device is current later."""
     assert ctx.device == torch.device("cuda", torch.cuda.current_device())
     assert ctx.pw_quantize_scaled(randn(1, 2, 128), 1)[0].device == ctx.device == ctx.workspace.device
+
+
+@pytest.mark.parametrize("T,n_experts", [(4, 16), (4, 64), (4, 200), (300, 16)])
+def test_layer_of_logits_that_are_no_numbers(T, n_experts):
+    """Rows with fewer numbers than choices: distinct experts, gate 0 for those without a number, other rows as they were."""
+    cfg = synth.LayerConfig("ops_nan", n_experts, 4, 256, 384, T, n_shared=1, bit_rule="int4_10fp16_20int2")
+    c = make_ctx(cfg)
+    try:
+        pages, _ = build_layer(c, cfg)
+        x = synth.activations(cfg, device="cuda")
+        logits = randn(1, T, n_experts)
+        want = c.pw_moe_forward(0, x, logits, 4).clone()
+        bad = logits.clone()
+        bad[0] = math.nan
+        bad[1] = math.nan
+        bad[1, 5], bad[1, 11] = 0.5, -0.5
+        bad[2, ::2] = math.nan
+        got = c.pw_moe_forward(0, x, bad, 4)
+        r = {n: v.cpu().numpy() for n, v in c.pw_get_routing(T, 4).items()}
+        ids, gates = r["topk_ids"], r["gates"]
+        assert ids.min() >= 0 and ids.max() < n_experts and all(len(set(row)) == 4 for row in ids)
+        assert np.array_equal(np.sort(r["perm"]), np.arange(T * 4)) and r["counts"].sum() == T * 4
+        assert list(ids[0]) == [0, 1, 2, 3] and np.isnan(gates[0]).all()
+        assert list(ids[1]) == [5, 11, 0, 1] and np.allclose(gates[1], [1 / (1 + math.exp(-1)), 1 - 1 / (1 + math.exp(-1)), 0, 0])
+        assert (ids[2] % 2 == 1).all()
+        got, want = got.cpu().numpy(), want.cpu().numpy()
+        assert np.isnan(got[0]).all() and np.isfinite(got[1:]).all()
+        near = np.abs(got[3:] - want[3:])
+        assert near.max() <= 2e-2                              # other neighbours in their tiles, so other orders of sums
+        static = B.pw_route_tokens_static(bad, 4)
+        assert np.array_equal(static["topk_ids"].cpu().numpy(), ids)
+        assert c.pw_last_device_status() == 0
+    finally:
+        c.close()
