@@ -303,3 +303,61 @@ def test_layer_of_logits_that_are_no_numbers(T, n_experts):
         assert c.pw_last_device_status() == 0
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k", [(72, 6), (128, 8), (160, 6), (256, 8), (256, 31), (250, 1), (100, 32)])
+def test_router_near_ties_with_a_bias_and_no_groups(ctx, score, E, k):
+    """Keys that 32 bits cannot tell apart among more than 64 experts: logits one step apart under the same bias, runs of
+    such logits at the cut, equal ones, and biases that give back what the scores differ by."""
+    T = 160
+    g = torch.Generator().manual_seed(E + k)
+    x = torch.randn(T, E, generator=g) * 0.5
+    bias = torch.randn(E, generator=g) * 0.05
+    bias[1::2] = bias[: E // 2 * 2: 2]
+    x[:, 1::2] = torch.nextafter(x[:, : E // 2 * 2: 2], torch.full((T, E // 2), math.inf))
+    x[::3, 1::2] = x[::3, : E // 2 * 2: 2]                        # equal in everything
+    # runs of 3, 12 and 40 experts on one logit and one bias, moved by up to two steps, from the best on
+    for row, n in ((1, 3), (4, 12), (7, 40), (10, 3), (13, 12), (16, 40)):
+        x[row, : n] = 2.0
+        for _ in range(2):
+            move = torch.rand(n, generator=g) < 0.5
+            x[row, :n] = torch.where(move, torch.nextafter(x[row, :n], torch.full((n,), math.inf)), x[row, :n])
+    bias[: 40] = bias[0]
+    # a row whose keys are all alike up to the rounding of the bias
+    far = plain.f64(x[20])
+    p = 1 / (1 + np.exp(-far)) if score == "sigmoid" else np.exp(far - far.max()) / np.exp(far - far.max()).sum()
+    flat = torch.from_numpy((0.5 - p).astype(np.float32))
+    for b in (bias, flat):
+        logits = x.cuda()
+        ids, gates = ctx.pw_route_tokens(logits, k, score=score, bias=b.cuda())
+        ref_ids, ref_gates = plain.route(logits, k, score, plain.f64(b), 1, 1, 1, True, 1.0)
+        assert np.array_equal(ids.cpu().numpy(), ref_ids)
+        np.testing.assert_allclose(gates.cpu().numpy(), ref_gates, rtol=52 * U)
+
+
+def test_first_product_of_a_context_inside_a_capture():
+    """What the first product looks up is no work on the stream: it may happen while one is captured."""
+    c = B.Context(1, 8, 0, 256, 512, 16, 2)
+    try:
+        shapes = [(3, 700, 1100), (40, 1000, 2100), (300, 500, 700), (1000, 2048, 512)]
+        sets = [operands(c, T, N, K, seed=T) for T, N, K in shapes]
+        outs = [torch.full((T, N), 5.0, device="cuda") for T, N, _ in shapes]
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            for ops, out in zip(sets, outs):
+                c.pw_scaled_linear(*ops, out=out, stream=s)
+        torch.cuda.synchronize()
+        assert all(bool((o == 5).all()) for o in outs)                 # captured, not run
+        g.replay()
+        torch.cuda.synchronize()
+        for ops, out in zip(sets, outs):
+            want = torch.empty_like(out)
+            check_linear(c, *ops, want)
+            assert torch.equal(out, want)
+        assert c.pw_last_device_status() == 0
+        del g
+    finally:
+        c.close()
