@@ -346,7 +346,8 @@ typedef enum { PW_F32 = 0, PW_F16 = 1, PW_BF16 = 2 } pw_type;
  * scale per block of 128 columns and block_rows rows (1: activations, 128: weights), stored
  * [ceil(rows / block_rows)][ceil(cols / 128)]; the last block of either direction may be short.  A block's scale is its
  * largest magnitude / 448 (1 for a block of zeros, at least 2^-126), its codes are e4m3(value * (1 / scale)), rounded
- * to nearest even and limited to 448: value = code * scale.
+ * to nearest even and limited to 448: value = code * scale.  (Reciprocal and product round once each in fp32, so a value
+ * that lies between two codes within two such roundings of their middle may get either.)
  * A NaN becomes a NaN code and has no part in the scale; an infinity makes its block's scale infinite, its own code NaN
  * and the others 0.
  *
@@ -360,7 +361,9 @@ pw_status pw_quantize_scaled(pw_ctx* ctx, const void* x, int x_type, int rows, i
 /* Residual addition and root-mean-square norm of T rows of H columns, in fp32:
  *   s = x + residual,  residual_out = s,  y = s * weight / sqrt(mean(s^2) + eps)
  * each output rounded once from fp32 (the norm works on the unrounded s), and the scaled 8-bit copy (block_rows 1) of
- * the unrounded y in q / q_scales, as pw_quantize_scaled would make it.
+ * the unrounded y in q / q_scales, as pw_quantize_scaled would make it.  s^2 and its sum have fp32's range: a row whose
+ * sum of squares is over it (elements from 2^63 on) gives 0, and with eps 0 a row whose squares are all below it (elements
+ * under 2^-75) no number.
  * residual may be NULL (s = x); residual_out (type of residual), y and the pair q, q_scales may each be NULL, but one
  * of y and q is needed.  residual_out may be residual, or x where type and stride are the same; y may be any of the
  * three where type and stride are the same; other overlaps are not allowed.  H: 1 .. 32768.
@@ -385,7 +388,8 @@ pw_status pw_scaled_linear(pw_ctx* ctx, int T, int N, int K, const void* a_codes
 
 /* Router: which top_k of n_experts a token takes, and with which gates.
  *   score    p = softmax of the row, or 1 / (1 + exp(-logit))
- *   key      p + bias (bias: device [n_experts] fp32 or NULL; it balances the choice and does not enter the gates)
+ *   key      p + bias (bias: device [n_experts] fp32 or NULL; it balances the choice and does not enter the gates; an
+ *            expert whose bias is NaN or -infinity is never chosen)
  *   groups   n_groups equal ranges of experts; only experts of the top_groups best groups can be chosen.  A group's
  *            score is its best key (group_best 1) or the sum of its best two (group_best 2)
  *   choice   the top_k largest keys, largest first; equal keys (and groups): lower index first.  Decided as in 64 bits;

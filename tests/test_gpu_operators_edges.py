@@ -361,3 +361,49 @@ def test_first_product_of_a_context_inside_a_capture():
         del g
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_codes_are_those_of_the_quotient_but_next_to_a_middle(ctx, block_rows):
+    """A code is within half a step of value / scale, and of two fp32 roundings (reciprocal, product) of the quotient."""
+    x = randn(block_rows, 300, 1000) * torch.exp(randn(2, 300, 1) * 3)
+    q, s = ctx.pw_quantize_scaled(x, block_rows)
+    v = plain.f64(x) / plain.spread(plain.f64(s), block_rows, x.shape)
+    step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(v), 2.0 ** -30))), -6) - 3)
+    assert np.all(np.abs(plain.code_values(q) - v) <= step / 2 + np.abs(v) * 2 * U * (1 + U))
+
+
+@pytest.mark.parametrize("n_groups", [1, 4])
+@pytest.mark.parametrize("E", [16, 64, 128])
+def test_router_biases_that_are_no_numbers(ctx, E, n_groups):
+    """NaN and -infinity close an expert, +infinity takes it first; the gates are those of the scores alone."""
+    T, k = 40, 6
+    x = randn(E, T, E)
+    bias = randn(E + 1, E, scale=0.1)
+    bias[E // 2] = math.inf
+    bias[:3], bias[3] = math.nan, -math.inf
+    few = torch.full_like(bias, -math.inf)
+    few[5], few[E - 1] = 0.0, 1.0
+    for b, open_ in ((bias, None), (few, {5, E - 1})):
+        ids, gates = ctx.pw_route_tokens(x, k, score="sigmoid", bias=b, n_groups=n_groups, top_groups=2 if n_groups > 1 else 1, renormalize=False)
+        i, g = ids.cpu().numpy(), plain.f64(gates)
+        if open_ is None:
+            assert i.min() >= 4 and (i[:, 0] == E // 2).all() and all(len(set(r)) == k for r in i)
+        else:
+            assert all(set(r) == open_ | {-1} and list(r[2:]) == [-1] * 4 and r[0] == E - 1 for r in i)
+        p = 1 / (1 + np.exp(-plain.f64(x)))
+        want = np.where(i >= 0, np.take_along_axis(p, np.maximum(i, 0), 1), 0.0)
+        assert np.all(np.abs(g - want) <= want * 52 * U)
+
+
+def test_norm_at_the_ends_of_the_range(ctx):
+    """Squares over fp32's range give 0, squares under it count as 0; the row of the residual is what it is."""
+    x = torch.zeros(4, 256, device="cuda")
+    x[0], x[1], x[2, 0] = 2.0 ** 64, 2.0 ** -76, 2.0 ** 62
+    w, r = torch.ones(256, device="cuda"), torch.zeros(4, 256, device="cuda")
+    ro, y = torch.empty_like(x), torch.empty_like(x)
+    ctx.pw_add_rmsnorm(x, w, 1e-6, residual=r, residual_out=ro, y=y)
+    assert torch.equal(ro, x) and bool((y[0] == 0).all()) and bool((y[3] == 0).all())
+    assert abs(float(y[2, 0]) - 16.0) <= 16 * 43 * U and abs(float(y[1, 0]) * 2.0 ** 76 / 1e3 - 1) <= 43 * U + 1e-6
+    ctx.pw_add_rmsnorm(x, w, 0.0, y=y)
+    assert bool(torch.isnan(y[3]).all()) and not bool(torch.isfinite(y[1]).any())
