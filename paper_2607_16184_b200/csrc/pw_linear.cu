@@ -209,33 +209,61 @@ __device__ __forceinline__ Factor split_factor(float x, float y) {
   return r;
 }
 // Scales of ROWS rows and the blocks g .. g + 7, one warp: a sector of 32 bytes per row, all loads in flight together,
-// written as [block][row], times a factor (rows padded by four, which keeps both sides free of bank conflicts).  Rows
-// and blocks past the end get 0.  Returns whether split_factor has anything to do for one of these scales and w0 or w1,
-// a lane's scales of the weights for block g + lane % 8: a lane's smallest and largest scale tell.
-template <int ROWS>
-__device__ __forceinline__ bool load_scales(const float* sa, int64_t row0, int T, int G, int g, int g_end, float times, float w0, float w1, float* dst,
-                                            int lane) {
+// stored as [block][row] (rows padded by four, which keeps both sides free of bank conflicts).  Rows and blocks past the
+// end, whose codes read as 0, get `past`.
+template <int ROWS, class Store>
+__device__ __forceinline__ void load_scales(const float* sa, int64_t row0, int T, int G, int g, int g_end, float past, int lane, Store store) {
   constexpr int kLoads = ROWS / 4 < 16 ? ROWS / 4 : 16;      // in flight at a time
   const int j = lane & 7, r0 = lane >> 3;
   const bool in = g + j < g_end;
-  float low = INFINITY, high = 0.f;
 #pragma unroll 1
   for (int base = 0; base < ROWS; base += kLoads * 4) {
     float v[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int64_t r = row0 + base + i * 4 + r0;
-      v[i] = in && r < T ? sa[r * G + g + j] : 0.f;
+      v[i] = in && r < T ? sa[r * G + g + j] : past;
     }
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      low = fminf(low, v[i] == 0.f ? INFINITY : fabsf(v[i]));
-      high = fmaxf(high, fabsf(v[i]));
-      dst[j * (ROWS + 4) + base + i * 4 + r0] = v[i] * times;
-    }
+    for (int i = 0; i < kLoads; ++i) store(j * (ROWS + 4) + base + i * 4 + r0, v[i]);
   }
-  auto leaves = [&](float w) { return w != 0.f && high > 0.f && (low * fabsf(w) < 1.17549435e-38f || high * fabsf(w) > 3.402823466e38f); };
-  return __any_sync(0xffffffffu, leaves(w0) || leaves(w1));
+}
+// The same times w, a lane's scale of the weights for block g + lane % 8 (1 past the end).  Returns whether one of the
+// products is 0, subnormal or no number; then they are split_factor's, with the powers of two beside them.
+template <int ROWS>
+__device__ __forceinline__ bool load_products(const float* sa, int64_t row0, int T, int G, int g, int g_end, float w, float* dst, float* powers,
+                                              int lane) {
+  uint32_t worst = 0;                              // an exponent of 0 wraps round to the top
+  load_scales<ROWS>(sa, row0, T, G, g, g_end, 1.f, lane, [&](int at, float v) {
+    const float f = v * w;
+    worst = max(worst, 2 * __float_as_uint(f) - 0x01000000u);
+    dst[at] = f;
+  });
+  const bool any = __any_sync(0xffffffffu, worst >= 0xfe000000u);
+  if (any)
+    load_scales<ROWS>(sa, row0, T, G, g, g_end, 1.f, lane, [&](int at, float v) {
+      const Factor x = split_factor(v, w);
+      dst[at] = x.f;
+      powers[at] = x.m;
+    });
+  return any;
+}
+// Whether a product of one of ROWS x 8 scales in shared memory and a scale between two others can leave the range.
+template <int ROWS>
+__device__ __forceinline__ bool products_leave(const float* scales, float w_low, float w_high, int lane) {
+  static_assert(ROWS == 128, "four rows a lane");
+  uint32_t least = 0xffffffffu;                    // twice the smallest magnitude's bits, less one: 0 is the largest
+  float high = 0.f;
+#pragma unroll
+  for (int j = 0; j < kScaleRun; ++j) {
+    const float4 q = *reinterpret_cast<const float4*>(scales + j * (ROWS + 4) + lane * 4);
+    least = min(min(least, 2 * __float_as_uint(q.x) - 1), 2 * __float_as_uint(q.y) - 1);
+    least = min(min(least, 2 * __float_as_uint(q.z) - 1), 2 * __float_as_uint(q.w) - 1);
+    high = fmaxf(fmaxf(high, fabsf(q.x)), fabsf(q.y));
+    high = fmaxf(fmaxf(high, fabsf(q.z)), fabsf(q.w));
+  }
+  const float low = __uint_as_float((least >> 1) + 1);
+  return __any_sync(0xffffffffu, high > 0.f && (low * w_low < 1.17549435e-38f || high * w_high > 3.402823466e38f));
 }
 
 // ---- few rows: the weights on the M side ---------------------------------------------------------
@@ -289,8 +317,8 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
   __shared__ unsigned long long full[S], done[S], freed[S], sc_full[2], sc_empty[2], sums_in;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int gave_up;
-  __shared__ alignas(16) float scales[2][kScaleRun][NT + 4];     // read four at a time
-  __shared__ int extreme_run[2];                                   // whether split_factor has anything to do for them
+  __shared__ alignas(16) float scales[2][kScaleRun][NT + 4], powers[2][kScaleRun][NT + 4];   // read four at a time
+  __shared__ int extreme_run[2];                                 // whether there are powers
   const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u, sums_s = ring_s + S * 2 * C::kBlock;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x % split);
@@ -382,10 +410,10 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
     for (int u = unit0; ok && u < n_units; u += stride) {
       const float* sw = a.sw + (int64_t)(u / token_tiles) * a.G;
       for (int g = g0; g < g1; g += kScaleRun, ++run) {
-        const float w = g + (lane & 7) < g1 ? sw[g + (lane & 7)] : 0.f;
+        const float w = g + (lane & 7) < g1 ? sw[g + (lane & 7)] : 1.f;
         if (run >= 2) ok = mbar_wait(smem_u32(&sc_empty[run & 1]), ((run >> 1) - 1) & 1, &gave_up, a.polls, a.status);
         if (!ok) break;
-        const bool any = load_scales<NT>(a.sa, (int64_t)(u % token_tiles) * NT, a.T, a.G, g, g1, w, w, w, &scales[run & 1][0][0], lane);
+        const bool any = load_products<NT>(a.sa, (int64_t)(u % token_tiles) * NT, a.T, a.G, g, g1, w, scales[run & 1][0], powers[run & 1][0], lane);
         if (lane == 0) extreme_run[run & 1] = any;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sc_full[run & 1]);
@@ -425,31 +453,27 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&freed[s]);
-        if (extreme) {                               // rare: from the two scales themselves
+        if (extreme) {                               // rare; kept this small: with the scales loaded and split here 4 % on 256 x 4096 x 4096
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (k == 1 && !two) break;
-            const float* sa = a.sa + g + k;
-            const float sw = a.sw[(int64_t)(u / token_tiles) * a.G + g + k];
-            const int t = u % token_tiles * NT + col;
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int j = 0; j < QC; j += 2) {
-              const Factor x = split_factor(t + j < a.T ? sa[(int64_t)(t + j) * a.G] : 0.f, sw);
-              const Factor y = split_factor(t + j + 1 < a.T ? sa[(int64_t)(t + j + 1) * a.G] : 0.f, sw);
-              acc[j / 2] = fma2(pack2(v[k][j] * x.m, v[k][j + 1] * y.m), pack2(x.f, y.f), acc[j / 2]);
+            for (int j = 0; j < QC; j += 4) {
+              const float4 m = *reinterpret_cast<const float4*>(&powers[run & 1][in_run + k][col + j]);
+              v[k][j] *= m.x;
+              v[k][j + 1] *= m.y;
+              v[k][j + 2] *= m.z;
+              v[k][j + 3] *= m.w;
             }
-          }
-        } else {
+        }
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (k == 1 && !two) break;
-            const ulonglong2* cs = reinterpret_cast<const ulonglong2*>(scales[run & 1][in_run + k] + col);
+        for (int k = 0; k < 2; ++k) {
+          if (k == 1 && !two) break;
+          const ulonglong2* cs = reinterpret_cast<const ulonglong2*>(scales[run & 1][in_run + k] + col);
 #pragma unroll
-            for (int j = 0; j < QC / 4; ++j) {
-              const ulonglong2 f = cs[j];
-              acc[2 * j] = fma2(pack2(v[k][4 * j], v[k][4 * j + 1]), f.x, acc[2 * j]);
-              acc[2 * j + 1] = fma2(pack2(v[k][4 * j + 2], v[k][4 * j + 3]), f.y, acc[2 * j + 1]);
-            }
+          for (int j = 0; j < QC / 4; ++j) {
+            const ulonglong2 f = cs[j];
+            acc[2 * j] = fma2(pack2(v[k][4 * j], v[k][4 * j + 1]), f.x, acc[2 * j]);
+            acc[2 * j + 1] = fma2(pack2(v[k][4 * j + 2], v[k][4 * j + 3]), f.y, acc[2 * j + 1]);
           }
         }
         in_run += 2;
@@ -652,8 +676,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
   __shared__ unsigned long long full[S], done[S], acc_empty[A], sc_full[2], sc_empty[2];
   __shared__ uint32_t tmem_base;
   __shared__ volatile int gave_up;
-  __shared__ float scales[2][kScaleRun][128 + 4], w_scales[2][2][kScaleRun];
-  __shared__ int extreme_run[2];                     // whether split_factor has anything to do for them
+  __shared__ alignas(16) float scales[2][kScaleRun][128 + 4];    // read four at a time
+  __shared__ float w_scales[2][2][kScaleRun];
+  __shared__ int extreme_run[2];                                 // whether split_factor may have anything to do for them
   const uint32_t ring_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const uint32_t rank = blockIdx.x & 1;           // cluster of two along x
@@ -743,8 +768,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
           if (run >= 2) ok = mbar_wait(smem_u32(&sc_empty[run & 1]), ((run >> 1) - 1) & 1, &gave_up, a.polls, a.status);
           if (!ok) break;
           if (lane < 16) w_scales[run & 1][lane >> 3][lane & 7] = w;
-          const float w0 = __shfl_sync(0xffffffffu, w, lane & 7), w1 = __shfl_sync(0xffffffffu, w, 8 + (lane & 7));
-          const bool any = load_scales<128>(a.sa, m0, a.T, a.G, g, a.G, 1.f, w0, w1, &scales[run & 1][0][0], lane);
+          const uint32_t w_least = __reduce_min_sync(0xffffffffu, 2 * __float_as_uint(w) - 1), w_most = __reduce_max_sync(0xffffffffu, 2 * __float_as_uint(w));
+          float* dst = scales[run & 1][0];
+          load_scales<128>(a.sa, m0, a.T, a.G, g, a.G, 0.f, lane, [&](int at, float v) { dst[at] = v; });
+          __syncwarp();
+          const bool any = w_most && products_leave<128>(dst, __uint_as_float((w_least >> 1) + 1), __uint_as_float(w_most >> 1), lane);
           if (lane == 0) extreme_run[run & 1] = any;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sc_full[run & 1]);
@@ -781,8 +809,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
       uint64_t acc[HC / 2];                         // pairs of columns: a packed multiply-add does two
 #pragma unroll
       for (int j = 0; j < HC / 2; ++j) acc[j] = 0;
-      // The blocks of a run of scales: a loop of each kind.  (4096 x 14336 x 4096 in a loop of calls: 260 us without the rare
-      // kind, 268 so, of which 5 are load_scales' look at the scales; with the test inside one loop 285, inside a block 334.)
+      // The blocks of a run of scales: a loop of each kind.  (4096 x 14336 x 4096: 226 us without the rare kind, 231 so; with
+      // the test for every block a tenth more, inside a block a third.)
       auto blocks = [&](auto kind, int first, int end) {
         constexpr bool kExtreme = decltype(kind)::value;
 #pragma unroll 1
