@@ -407,3 +407,26 @@ def test_norm_at_the_ends_of_the_range(ctx):
     assert abs(float(y[2, 0]) - 16.0) <= 16 * 43 * U and abs(float(y[1, 0]) * 2.0 ** 76 / 1e3 - 1) <= 43 * U + 1e-6
     ctx.pw_add_rmsnorm(x, w, 0.0, y=y)
     assert bool(torch.isnan(y[3]).all()) and not bool(torch.isfinite(y[1]).any())
+
+
+@pytest.mark.parametrize("T,H,pad", [(3, 520, 0), (3, 521, 2), (200, 4096, 0), (2, 20001, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_outputs_over_its_inputs(ctx, T, H, pad, dtype):
+    """Every overlap that the header allows gives what separate buffers give."""
+    def buffer(seed):
+        whole = torch.zeros(T, H + pad, dtype=dtype, device="cuda")
+        whole[:, :H] = randn(seed, T, H)
+        return whole[:, :H]
+
+    w = randn(3, H)
+    x, r, ro, y = buffer(1), buffer(2), torch.zeros(T, H + pad, dtype=dtype, device="cuda")[:, :H], torch.zeros(T, H + pad, dtype=dtype, device="cuda")[:, :H]
+    q, qs = B.scaled_empty(T, H, 1)
+    ctx.pw_add_rmsnorm(x, w, residual=r, residual_out=ro, y=y, q=q, q_scales=qs)
+    for where_ro, where_y in (("x", None), ("r", None), ("r", "x"), ("x", "r"), (None, "x"), (None, "r"), ("x", "x"), ("r", "r"), ("new", "new")):
+        b = {"x": buffer(1), "r": buffer(2), "new": torch.zeros(T, H + pad, dtype=dtype, device="cuda")[:, :H]}
+        out = torch.zeros(T, H + pad, dtype=dtype, device="cuda")[:, :H] if where_y is None else b[where_y]
+        q2, qs2 = B.scaled_empty(T, H, 1)
+        ctx.pw_add_rmsnorm(b["x"], w, residual=b["r"], residual_out=None if where_ro is None else b[where_ro], y=out, q=q2, q_scales=qs2)
+        assert torch.equal(out, y) and torch.equal(qs2, qs) and torch.equal(q2.view(torch.uint8), q.view(torch.uint8))
+        if where_ro is not None and where_ro != where_y:
+            assert torch.equal(b[where_ro], ro)
