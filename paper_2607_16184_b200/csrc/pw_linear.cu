@@ -283,7 +283,7 @@ __device__ __forceinline__ bool products_leave(const float* scales, float w_low,
 //              of a barrier can take an old one for the one it waits for.)
 //   then one   scales, eight blocks at a time, multiplied, into shared memory: loaded by the warps that use them they
 //              were 16 times as many requests as they are sectors, and the bound of the kernel
-// 64 x 14336 x 4096: 14.5 us (weights once from HBM: 8.9; the rest is the launch, filling and draining), one token 12.1;
+// 64 x 14336 x 4096: 14.4 us (weights once from HBM: 8.9; the rest is the launch, filling and draining), one token 12.1;
 // one token x 4096 x 4096: 5.1.
 template <int NT, bool SPLIT>
 struct FewCfg {
@@ -555,10 +555,10 @@ __global__ void __launch_bounds__(FewCfg<NT, SPLIT>::kThreads, 1)
 //   warp 11     scales, eight blocks at a time, into shared memory
 // The last four warps hand most of their registers to the first eight, whose sums fill 128 each.
 // Persistent: a pair takes every n_pairs-th tile, token tiles fastest, so that the pairs at work share weight rows in L2.
-// 4096 x 14336 x 4096: 220 us = 2.18 PFLOP/s (power capped in a loop: 250).  The MMAs alone take 153, the epilogue alone
-// 182: a block's 64 packed multiply-adds per warp (320 cycles of the FMA pipe) come behind the wait for its accumulator, of
-// which two fill tensor memory.  Sixteen epilogue warps (240) and accumulators handed over in halves (222 to 249) are no
-// faster.
+// 4096 x 14336 x 4096: 222 to 231 us from GPU to GPU = 2.1 to 2.2 PFLOP/s (power capped in a loop: 265).  When it took 220,
+// the MMAs alone were 153 of them and the epilogue alone 182: a block's 64 packed multiply-adds per warp (320 cycles of the
+// FMA pipe) come behind the wait for its accumulator, of which two fill tensor memory.  Sixteen epilogue warps (240) and
+// accumulators handed over in halves (222 to 249) were no faster.
 constexpr int kPairThreads = 384;
 template <int BN>
 struct PairCfg {
@@ -985,9 +985,9 @@ static LinearPlan plan_pair(int T, int N, int G, int bn, int sms) {
 // The plan that finishes soonest by a model that is linear in the blocks of 128 columns a CTA (pair) goes through one
 // after the other and in the units it does (301 x 64 x 2056: 16 tokens to a tile 4.7 us, 64 5.6; 3711 x 187 x 119: 16
 // tokens, four units one after the other, 8.8, 64 tokens 4.9).  The times per block are measured (us, contraction 4096,
-// tokens x weight rows, few 64 / pair 128 / pair 256):  64 x 4096  7.6 / 14.1 / 18.3,  128 x 4096  9.6 / 14.4 / 18.9,
-// 64 x 14336  14.6 / 26.2 / 20.9,  128 x 14336  27 / 27.6 / 22.7,  256 x 4096  11.7 / 14.7 / 19.1,
-// 512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
+// tokens x weight rows, few 64 / pair 128 / pair 256; the pair kernel takes 2 to 5 % more since):  64 x 4096  7.6 / 14.1 /
+// 18.3,  128 x 4096  9.6 / 14.4 / 18.9,  64 x 14336  14.6 / 26.2 / 20.9,  128 x 14336  27 / 27.6 / 22.7,
+// 256 x 4096  11.7 / 14.7 / 19.1,  512 x 4096  26 / 16.4 / 20.0,  512 x 14336  80 / 48 / 38.
 static LinearPlan plan_linear(int T, int N, int G, int sms, const int* max_clusters) {
   LinearPlan best = plan_few(T, N, G, 16, sms, max_clusters);
   for (int nt = 32; nt <= 64 && T > nt / 2; nt *= 2) {

@@ -5,9 +5,13 @@
 //   per block: top = max |y|, scale = top / 448, code = e4m3(y * (1 / scale))
 //
 // Both read every input element once and write every output element once; nothing else leaves the registers, so
-// HBM bounds them at large sizes and the launch and one round trip to memory at small ones.  Measured: norm of 4096 x 4096
-// fp32 with residual, fp16 output and codes 29.2 us, quantizer of 14336 x 4096 fp16 27.7 us (both 97 % of the copy
-// bandwidth); one row of 4096 2.0 us, where the emptiest launch takes 1.9.
+// HBM bounds them at large sizes and the launch and one round trip to memory at small ones.  Measured in a graph of calls
+// one behind the other: norm of 4096 x 4096 fp32 with residual, fp16 output and codes 29.2 us, quantizer of 14336 x 4096
+// fp16 27.7 us (both 97 % of the copy bandwidth; launched call by call 31.0 and 29.6, 91 %); one row of 4096 2.0 us, where
+// the emptiest launch takes 1.9.
+//
+// A code is rounded from y times the reciprocal of its scale, two fp32 roundings instead of one division's: 1.7 us less
+// for the quantizer's case above.  A value that lies within them of the middle between two codes may get the other one.
 #include "pw_scaled.cuh"
 
 namespace pw {
@@ -229,6 +233,8 @@ static pw_status launch_norm(const NormArgs& a, bool vec, int T, int num_sms, cu
   // (2048 rows; HBM 32).  Above 16384 columns only 1024 threads keep a thread's share in its registers (1024 rows x 24576:
   // 40 us, 53 us as 512 threads of up to eight; HBM 31).  Single-element accesses take up to 1024 threads from 8192 columns
   // on (478 rows x 12671, with codes: 23 us, 33 us as 512): they are bound by their instructions, 64 bytes of a row each.
+  // Above 16384 columns those threads hold four vectors in the 64 registers that 1024 of them leave, and spill 228 to 244
+  // bytes each: part of the 71 us of 1024 rows x 24575 (24576, in vectors: 40).
   const int n8 = (a.H + 7) / 8;
   const int vpt = n8 <= (T <= num_sms ? 1024 : 512) ? 1 : n8 <= (T > num_sms && vec ? 1024 : 2048) ? 2 : 4;
   const int threads = ((n8 + vpt - 1) / vpt + 31) / 32 * 32;
@@ -434,7 +440,7 @@ static pw_status launch_quant(const QuantArgs& a, int block_rows, bool vec, int 
   return PW_OK;
 }
 
-constexpr int kMaxNormWidth = 32768;            // 512 threads x eight vectors of eight
+constexpr int kMaxNormWidth = 32768;            // 1024 threads x four vectors of eight
 
 }  // namespace pw
 

@@ -414,8 +414,10 @@ __global__ void __launch_bounds__(128, PLAIN ? 16 : 7) score_kernel(const __grid
     };
     // Error of p in 32 bits, in half steps of 1.  The fast exponential of x is (2 + 1.173 |x|) steps off, the fast division 2.
     //   sigmoid: p (1 - p) (4 + 2.35 |v|) + p + 4 p <= 1 + 0.53 + 1 + 4, below 8
-    //   softmax: 4 + 0.87 of the exponential (d e^-d <= 0.37) and 0.37 of the rounding of its argument, as much and 13
-    //            additions of the denominator, 4 of the division: below 32, all of it relative to p, which is 1 / total at most
+    //   softmax: with d = how far a logit is below the largest, a term e^-d is off by 4 + 2.35 d + d of it (exponential and
+    //            rounding of its argument), at most 5.3 in all for d e^-d <= 0.37.  The denominator's terms are off by 2 + d
+    //            each (expf), 2 + 3.4 of the sum (the mean of d over the terms is largest for 255 of them at 4.2), and 13
+    //            additions; the division 4: below 28, taken as 32, all of it relative to p, which is 1 / total at most
     // With the bias's addition a key is off by less than (8 or 32 / total, + |key|) half steps; two keys decide when they are
     // further apart than both errors together.
     constexpr float kHalfStep = 5.9604645e-8f;
@@ -526,8 +528,10 @@ __global__ void __launch_bounds__(128, PLAIN ? 16 : 7) score_kernel(const __grid
   float my_l = -INFINITY;
   if (my_id >= 0) my_l = PLAIN ? from_ordered(my_key) : tidy(load1(a.logits, t * a.stride + my_id, a.type));
   // Gates.  Renormalised softmax gates need no denominator over the row: exp(l - largest chosen l) over their sum.  In 32
-  // bits while the exponents are small; else in 64, where neither the rounding of a large exponent nor an underflowing
-  // score of a sum of underflowing scores is lost.
+  // bits while the exponents are small: a gate is a weight of the experts' outputs, whose operands have 11 bits (off by
+  // 5.7e-8 of the gates' norm for 256 tokens x 64 experts, 2.4e-8 if everything is in 64 bits).  Else in 64 bits, where
+  // neither the rounding of a large exponent nor an underflowing score of a sum of underflowing scores is lost; the
+  // softmax's denominator over the row stays the sum in 32 bits, of positive terms, off by 13 roundings and their own.
   const bool chosen = my_id >= 0;
   const float base = a.sigmoid ? 0.f : a.renorm ? warp_max(my_l) : top;
   const float d = chosen ? my_l - base : 0.f;

@@ -1,6 +1,7 @@
 // Argument marshalling of the calls around the layer: torch tensors in, one C call of include/pw.h out.  These calls take
 // a few microseconds on the GPU, and marshalled in Python (ctypes, five or six tensors to look at) they took 8 to 14
-// microseconds of the host's time; here it is 3 to 5, the launch included.
+// microseconds of the host's time.  Here the marshalling is 0.3 to 0.5 of them, and a call from Python with its launch 2.4
+// (three tensors) to 4.3 (five).
 //
 // Every function gets the context, its device index, a stream (None: the device's current one) and the arguments of the
 // Python method, and returns 0 or  status | (number of the argument that is wrong) << 8.
