@@ -430,3 +430,42 @@ def test_norm_outputs_over_its_inputs(ctx, T, H, pad, dtype):
         assert torch.equal(out, y) and torch.equal(qs2, qs) and torch.equal(q2.view(torch.uint8), q.view(torch.uint8))
         if where_ro is not None and where_ro != where_y:
             assert torch.equal(b[where_ro], ro)
+
+
+def test_layer_and_operators_on_two_streams_at_once(ctx):
+    """A layer on one stream, the operators around another one on a second: neither changes what the other computes."""
+    cfg = synth.LayerConfig("ops_beside", 16, 4, 512, 1024, 64, n_shared=1, bit_rule="int4_10fp16_20int2")
+    c = make_ctx(cfg)
+    try:
+        pages, _ = build_layer(c, cfg)
+        x, logits = synth.activations(cfg, device="cuda"), synth.router_logits(cfg, device="cuda")
+        sets = [operands(ctx, T, N, K, seed=T) for T, N, K in ((5, 4096, 2048), (64, 3000, 2048), (300, 1000, 1024), (1500, 2048, 1024))]
+        rows, w = randn(1, 700, 2056), randn(2, 2056)
+        wide = randn(3, 900, 256)
+
+        def around(s=None):
+            return [ctx.pw_scaled_linear(*ops, out_dtype=F32, stream=s) for ops in sets] + [ctx.pw_add_rmsnorm(rows, w, stream=s)[1]] + \
+                list(ctx.pw_route_tokens(wide, 8, score="sigmoid", bias=wide[0], n_groups=8, top_groups=4, group_best=2, stream=s)) + \
+                list(ctx.pw_quantize_scaled(rows, 128, stream=s))
+
+        def layer(s=None):
+            ids, gates = c.pw_route_tokens(logits, 4, stream=s)
+            return [c.pw_moe_forward(0, x, logits, 4, stream=s), c.pw_moe_forward_routed(0, x, ids, gates, stream=s)]
+
+        want_a, want_l = around(), layer()
+        torch.cuda.synchronize()
+        a, b = torch.cuda.Stream(), torch.cuda.Stream()
+        got_a, got_l = [], []
+        for _ in range(15):
+            with torch.cuda.stream(b):
+                got_l.append(layer(b))
+            with torch.cuda.stream(a):
+                got_a.append(around(a))
+        torch.cuda.synchronize()
+        bits = lambda t: t.contiguous().view(torch.uint8)
+        for want, runs in ((want_a, got_a), (want_l, got_l)):
+            for got in runs:
+                assert all(torch.equal(bits(g), bits(v)) for g, v in zip(got, want))
+        assert c.pw_last_device_status() == 0 and ctx.pw_last_device_status() == 0
+    finally:
+        c.close()
