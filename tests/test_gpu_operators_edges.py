@@ -108,7 +108,7 @@ def test_other_threads_run_while_a_call_waits_for_the_queue(ctx):
         stop.set()
         other.join()
         torch.cuda.synchronize()
-    assert gap[0] < 0.25, (gap[0], waited)
+    assert gap[0] < max(0.25, 0.6 * waited), (gap[0], waited)    # it was all of the wait when the call kept the interpreter
 
 
 def test_first_products_on_several_threads():
