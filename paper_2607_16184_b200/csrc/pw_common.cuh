@@ -119,6 +119,7 @@ struct pw_ctx {
   // is set last)
   std::atomic<void*> encode_tiled;    // driver entry point for tensor maps
   std::atomic<int> max_clusters[5];   // clusters of that product's CTAs that run at the same time, by size
+  std::atomic<int> few_ready;     // the kernels for few tokens have their attributes
   void* tc_state;                 // tensor-core path state (set up lazily)
   uint32_t wait_polls;            // limit of the device-side waits in polls of 20 us (0 = the default, 2 s)
   uint32_t test_hook;             // device-side test hooks (pw_debug_set_wait)

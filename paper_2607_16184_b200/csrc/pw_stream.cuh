@@ -1,0 +1,491 @@
+// Rows of weight pages against the operand rows of up to eight tokens: the inner loop of the calls for few tokens.
+//
+// A unit of work is 32 rows of a block.  Every warp streams a part of the block's columns ("steps") through a ring of its
+// own in shared memory with 16-byte asynchronous copies and multiplies it on the spot; nothing is shared between warps
+// before their sums meet at the end of a unit.  With so few tokens a weight is used at most eight times, so what counts is
+// that the copies never pause: a warp waits for the step it asked for STAGES steps ago, multiplies it, asks for the next and
+// goes on, without a barrier.
+//
+// The product runs on mma.sync m16n8k16 (two of them, 16 weight rows x 8 tokens each), not on tcgen05: a decoded weight goes
+// from a register straight into the instruction, where the larger one wants 128 rows and its operand written to tensor
+// memory first (the layer's kernels for batches, which do that, read a 4-bit page at 53 % of the copy bandwidth).
+//
+// A group of 128 columns of a row contributes
+//     sum x * (code * scale + zero) = scale * sum x * code + zero * sum x
+// and the codes themselves are the operands: a field of a code word is cut out with one logic instruction and is, in
+// place, an fp16 number -- a subnormal, field << p reads field * 2^(p - 24) for every p with the field below bit 10.
+// (The tensor core multiplies subnormals exactly.)  Fields at different p have accumulators of their own, joined with
+// powers of two when scale and zero-point are applied, once per group, in fp32.  So a pair of weights costs one
+// instruction, where turning it into fp16(code * scale + zero) costs three; weights are not rounded to fp16 on this path.
+//
+// Steps: 32 columns of a 16-bit block, 64 of an 8-bit one, a group of 128 otherwise, so that a step is 1 to 2 KB of
+// codes.  Lane (g, t) = (lane / 4, lane % 4) multiplies part t of the step's columns, rows 4g .. 4g + 3 (as rows g and
+// g + 8 of the two products), so that the scales of its rows are one 8-byte load.  The copies are cut the other way, a
+// row's 16 bytes per lane: an instruction then takes 512 bytes in one piece, where one that follows the lanes of the
+// product takes four pieces 2 KB apart (streaming alone, 71 MB out of the L2 cache: 7.6 us against 18.9).  Rows are
+// exchanged inside a unit so that the loads of the product meet 32 banks (code_at).
+//
+// Operand rows are kept in pieces of 16 bytes.  A group's 128 columns are eight stretches of 16, as pairs W0 .. W7; piece
+// 2s + h of stretch s holds W(2h), W(2h + 4), W(2h + 1), W(2h + 5): pairs next to one another are the two halves of an
+// MMA's operand for every format (a field and the one at the same place eight columns on), so they lie in neighbouring
+// registers.  Piece e of row c is the (e ^ (e >> 2) ^ 4 (c mod 2))-th of its 256 bytes: the four lanes of a row take
+// pieces 4t + i, 2t + i or t (4-bit, 8-bit, 16-bit steps), two rows at a time, and meet 32 banks in all three.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "pw_layout.cuh"
+#include "pw_ptx.cuh"
+
+namespace pw {
+
+enum : int { kFmt16 = 0, kFmt8, kFmt4, kFmt3, kFmt2, kFmtP4, kFmtP3, kFmtP2 };
+// -1: not a format
+__host__ __device__ inline int stream_format(int bits, bool planes) {
+  if (planes) return bits == 4 ? kFmtP4 : bits == 3 ? kFmtP3 : bits == 2 ? kFmtP2 : -1;
+  return bits == 16 ? kFmt16 : bits == 8 ? kFmt8 : bits == 4 ? kFmt4 : bits == 3 ? kFmt3 : bits == 2 ? kFmt2 : -1;
+}
+// log2 of the steps of a group
+__host__ __device__ constexpr int step_shift(int fmt) { return fmt == kFmt16 ? 2 : fmt == kFmt8 ? 1 : 0; }
+// bytes from one tile (of the TOP buffer, for planes) to the next, and of the scales inside it
+__host__ __device__ constexpr uint32_t stream_tile_bytes(int fmt) {
+  return fmt >= kFmtP4 ? (uint32_t)kPlaneTopTile : fmt == kFmt16 ? 32768u : fmt == kFmt8 ? 16896u : fmt == kFmt4 ? 8704u : fmt == kFmt3 ? 6656u : 4608u;
+}
+__host__ __device__ constexpr uint32_t stream_scale_offset(int fmt) {
+  return fmt >= kFmtP4 ? (uint32_t)kPlaneTopCodes + 512u * (uint32_t)(kFmtP2 - fmt) : stream_tile_bytes(fmt) - 512u;
+}
+
+constexpr int kStreamWarps = 16;
+constexpr int kStreamThreads = kStreamWarps * 32;
+constexpr int kUnitRows = 32;
+constexpr int kUnitCols = 8;                      // tokens of a unit
+constexpr int kStepCodes = 2048;                  // bytes of a slot: codes, scales and zero-points, streamed operand rows
+constexpr int kStepMeta = 128;
+template <int XC>                                 // XC: operand rows that are streamed with the codes; 0: they are staged
+constexpr int kSlotOf = kStepCodes + kStepMeta + 256 * XC;
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Where the 16 bytes of unit u of row `row` lie in a slot, and with 16-byte (u < 4), 8-byte (u < 2) or 4-byte loads of the
+// product's lanes: the loads take rows 4g + j, j fixed, and what makes them meet different banks goes into bits 0, 1 of the
+// row.
+template <int F>
+__host__ __device__ constexpr uint32_t code_at(uint32_t u, uint32_t row) {
+  return 512 * u + 16 * (row ^ (F <= kFmt4 ? u : u < 2 ? ((row >> 3) & 1) ^ (2 * u) : (row >> 3) & 3));
+}
+__host__ __device__ constexpr uint32_t piece_at(uint32_t e, uint32_t row) { return e ^ (e >> 2) ^ ((row & 1) << 2); }
+
+// What a warp has still to ask for of one block.  The pointers are the lane's own, of the next step.
+struct Feed {
+  const char* codes;
+  const char* bit1;                               // planes
+  const char* bit0;
+  const char* meta;                               // lanes 0 .. 7: 16 bytes of the scales, of the zero-points
+  const char* x;                                  // streamed operand: the lane's bytes of its first row
+  uint32_t x_step;                                // bytes between the rows that a lane copies
+  int fmt, left, sub;                             // sub: step inside the group
+  int copies;                                     // operand rows that this lane copies from
+};
+
+// Sets `f` up for the codes of steps lo .. hi of rows 32 * slice .. of a block of `groups` groups.
+__device__ __forceinline__ void feed_codes(Feed& f, int lane, const char* codes, const char* bit1, const char* bit0, int fmt, int groups, int slice,
+                                           int lo, int hi) {
+  const int ls = step_shift(fmt), sl = slice & 3;
+  const size_t tile = (size_t)(slice >> 2) * groups + (lo >> ls);
+  f.fmt = fmt;
+  f.left = hi - lo;
+  f.sub = lo & ((1 << ls) - 1);
+  const char* at = codes + tile * stream_tile_bytes(fmt);
+  f.meta = at + stream_scale_offset(fmt) + 64 * sl + (lane >> 2) * 256 + (lane & 3) * 16;
+  const uint32_t row = (uint32_t)(32 * sl + lane) * 16;
+  f.codes = at + f.sub * 8192 + row;
+  f.bit1 = bit1 + tile * kPlaneBitTile + row;
+  f.bit0 = bit0 + tile * kPlaneBitTile + row;
+}
+// ... and for operand rows that are streamed with them: `cols` rows of pieces, `pitch` bytes apart, row c in the order of
+// row c.  A lane copies bytes of row lane >> (4 - ls), and of the rows 2 << ls further on.
+__device__ __forceinline__ void feed_operand(Feed& f, int lane, const char* x, uint32_t pitch, int cols, int lo) {
+  const int ls = step_shift(f.fmt);
+  const int c = lane >> (4 - ls);
+  f.copies = (cols - c + (2 << ls) - 1) >> (ls + 1);
+  f.x = x + (size_t)c * pitch + (size_t)(lo >> ls) * 256 + (lane & ((16 >> ls) - 1)) * 16;
+  f.x_step = pitch << (ls + 1);
+}
+
+// Asks for a step in format F (its codes, its streamed operand, or both) and moves on; `left` is the caller's.
+template <int F, int XC, bool CODES, bool OPERAND>
+__device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
+  constexpr int ls = step_shift(F);
+  if constexpr (OPERAND && XC > 0) {
+    // the step's part of a group's pieces: all, the half `sub`, or the quarter `sub` (quarters of odd rows are exchanged)
+    const char* src = f.x;
+    if constexpr (ls == 1) src += f.sub * 128;
+    if constexpr (ls == 2) src += (f.sub ^ ((lane >> 2) & 1)) * 64;
+    const uint32_t dst = slot + kStepCodes + kStepMeta + lane * 16;
+#pragma unroll
+    for (int j = 0; j < (XC >> (ls + 1) > 0 ? XC >> (ls + 1) : 1); ++j)
+      if (j < f.copies) cp16(dst + j * 512, src + j * f.x_step);
+    f.x += ls == 0 || f.sub == (1 << ls) - 1 ? 256 : 0;
+  }
+  if constexpr (CODES) {
+    constexpr uint32_t tile = stream_tile_bytes(F);
+    constexpr int units = F <= kFmt4 ? 4 : F == kFmt3 ? 3 : 2;
+#pragma unroll
+    for (int u = 0; u < units; ++u) cp16(slot + code_at<F>(u, lane), f.codes + u * 2048);
+    if (F != kFmt16 && lane < 8) cp16(slot + kStepCodes + lane * 16, f.meta);
+    if constexpr (F == kFmtP4 || F == kFmtP3) {
+      cp16(slot + code_at<F>(2, lane), f.bit1);
+      f.bit1 += kPlaneBitTile;
+    }
+    if constexpr (F == kFmtP4) {
+      cp16(slot + code_at<F>(3, lane), f.bit0);
+      f.bit0 += kPlaneBitTile;
+    }
+    if constexpr (F == kFmt16) {
+      f.codes += 8192;                            // (a tile of 16 bits has nothing behind its codes)
+    } else if constexpr (F == kFmt8) {
+      f.codes += f.sub ? tile - 8192u : 8192u;
+      f.meta += f.sub ? tile : 0u;
+    } else {
+      f.codes += tile;
+      f.meta += tile;
+    }
+  }
+  if constexpr (ls > 0) f.sub = (f.sub + 1) & ((1 << ls) - 1);
+}
+template <int XC, bool CODES, bool OPERAND>
+__device__ __forceinline__ void ask_any(Feed& f, uint32_t slot, int lane) {
+  f.left--;
+  switch (f.fmt) {
+    case kFmt16: ask<kFmt16, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmt8: ask<kFmt8, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmt4: ask<kFmt4, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmt3: ask<kFmt3, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmt2: ask<kFmt2, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmtP4: ask<kFmtP4, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmtP3: ask<kFmtP3, XC, CODES, OPERAND>(f, slot, lane); break;
+    default: ask<kFmtP2, XC, CODES, OPERAND>(f, slot, lane); break;
+  }
+}
+
+// ---- staged operand ------------------------------------------------------------------------------
+// Two neighbouring pieces (a stretch of 16 columns) of columns as they lie in memory.
+__device__ __forceinline__ void make_pieces(const uint4& lo, const uint4& hi, uint4 (&piece)[2]) {
+  piece[0] = make_uint4(lo.x, hi.x, lo.y, hi.y);
+  piece[1] = make_uint4(lo.z, hi.z, lo.w, hi.w);
+}
+__device__ __forceinline__ float sum_halves(const uint4& v) {
+  const float2 a = __half22float2(u32_as_h2(v.x)), b = __half22float2(u32_as_h2(v.y)), c = __half22float2(u32_as_h2(v.z)), d = __half22float2(u32_as_h2(v.w));
+  return ((a.x + a.y) + (b.x + b.y)) + ((c.x + c.y) + (d.x + d.y));
+}
+// Groups g0 .. g0 + groups of `rows` operand rows (fp16, `pitch` bytes apart, k_bytes of a row count, zeros behind them) ->
+// pieces [group][row][256 bytes] and the sums of the halves of every group, [group][2][row].  By the whole CTA.
+__device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int rows, int g0, int groups, int k_bytes, char* pieces, float* sums) {
+  const int tid = threadIdx.x;
+  const int n = rows * groups * 8;
+  for (int base = tid & ~31; base < n; base += kStreamThreads) {
+    const int i = base + (tid & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
+    uint4 v[2] = {};
+    if (i < n) {
+      const int k = (g0 + g) * 256 + s * 32;
+      const char* src = x + (size_t)c * pitch + k;
+      if (k + 32 <= k_bytes) {
+        v[0] = reinterpret_cast<const uint4*>(src)[0];
+        v[1] = reinterpret_cast<const uint4*>(src)[1];
+      } else {
+        uint16_t h[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) h[j] = k + 2 * j < k_bytes ? reinterpret_cast<const uint16_t*>(src)[j] : (uint16_t)0;
+        v[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        v[1] = make_uint4(h[8] | h[9] << 16, h[10] | h[11] << 16, h[12] | h[13] << 16, h[14] | h[15] << 16);
+      }
+      uint4 piece[2];
+      make_pieces(v[0], v[1], piece);
+      char* row = pieces + (size_t)rg * 256;
+      *reinterpret_cast<uint4*>(row + piece_at(2 * s, c) * 16) = piece[0];
+      *reinterpret_cast<uint4*>(row + piece_at(2 * s + 1, c) * 16) = piece[1];
+    }
+    float a = sum_halves(v[0]) + sum_halves(v[1]);
+    a += __shfl_xor_sync(0xffffffffu, a, 1);
+    a += __shfl_xor_sync(0xffffffffu, a, 2);
+    if (i < n && (s & 3) == 0) sums[(g * 2 + (s >> 2)) * rows + c] = a;
+  }
+}
+
+// The operand of a block's steps, as a lane reads it.
+struct Operand {
+  const char* x;                                  // staged: group 0, this lane's row; streamed: this lane's row in slot 0
+  const float* sum;                               // staged: sums of group 0, of the token 2t
+  int sum_next;                                   // from there to the token 2t + 1
+  int rows;                                       // staged rows
+  uint32_t flip;                                  // 4 for an odd row (see piece_at)
+  int step;                                       // next step of the block
+};
+
+// ---- the product of a step -----------------------------------------------------------------------
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+template <bool FIRST>
+__device__ __forceinline__ void mma16_if(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (FIRST) mma16_first(d, a0, a1, a2, a3, b0, b1);
+  else mma16(d, a0, a1, a2, a3, b0, b1);
+}
+constexpr uint32_t kOnes = 0x3c003c00u;           // two fp16 ones
+
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t moved_by(uint32_t x, int s) { return s >= 0 ? x >> s : x << -s; }
+
+// tot[h]: rows 4g + 2h (0, 1) and 4g + 2h + 1 (2, 3), tokens 2t (0, 2) and 2t + 1 (1, 3).
+struct Scales {
+  float s[4], z[4];
+};
+__device__ __forceinline__ void load_scales(const char* slot, int g, Scales& m) {
+  const uint2 s = *reinterpret_cast<const uint2*>(slot + kStepCodes + 8 * g), z = *reinterpret_cast<const uint2*>(slot + kStepCodes + 64 + 8 * g);
+  const float2 s0 = __half22float2(u32_as_h2(s.x)), s1 = __half22float2(u32_as_h2(s.y));
+  const float2 z0 = __half22float2(u32_as_h2(z.x)), z1 = __half22float2(u32_as_h2(z.y));
+  m.s[0] = s0.x * 16777216.0f, m.s[1] = s0.y * 16777216.0f, m.s[2] = s1.x * 16777216.0f, m.s[3] = s1.y * 16777216.0f;
+  m.z[0] = z0.x, m.z[1] = z0.y, m.z[2] = z1.x, m.z[3] = z1.y;
+}
+// acc: the products of the codes, times 2^-24
+__device__ __forceinline__ void apply_scales(const Scales& m, int h, const float (&acc)[4], float sum0, float sum1, float (&tot)[4]) {
+  tot[0] = fmaf(m.s[2 * h], acc[0], fmaf(m.z[2 * h], sum0, tot[0]));
+  tot[1] = fmaf(m.s[2 * h], acc[1], fmaf(m.z[2 * h], sum1, tot[1]));
+  tot[2] = fmaf(m.s[2 * h + 1], acc[2], fmaf(m.z[2 * h + 1], sum0, tot[2]));
+  tot[3] = fmaf(m.s[2 * h + 1], acc[3], fmaf(m.z[2 * h + 1], sum1, tot[3]));
+}
+
+// One step in format F out of a slot.  xrow: this lane's operand row, with the step's pieces at (at0 ^ i) * 16 bytes;
+// STAGED: the operands' sums are at sum[0] and sum[sum_next] (8-bit steps: of half a group), else they are made here.
+template <int F, bool STAGED>
+__device__ __forceinline__ void multiply_step(const char* slot, int lane, const char* xrow, uint32_t at0, const float* sum, int sum_next, int rows,
+                                              float (&tot)[2][4]) {
+  constexpr int ls = step_shift(F);
+  const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3;
+  uint4 x[4 >> ls];
+#pragma unroll
+  for (int i = 0; i < (4 >> ls); ++i) x[i] = *reinterpret_cast<const uint4*>(xrow + ((at0 ^ i) << 4));
+  float sum0 = 0.f, sum1 = 0.f;
+  if constexpr (F != kFmt16) {
+    if constexpr (STAGED) {
+      sum0 = sum[0];
+      sum1 = sum[sum_next];
+      if constexpr (ls == 0) {
+        sum0 += sum[rows];
+        sum1 += sum[rows + sum_next];
+      }
+    } else {
+      float ones[4];
+#pragma unroll
+      for (int i = 0; i < (4 >> ls); ++i) {
+        if (i == 0) mma16_first(ones, kOnes, kOnes, kOnes, kOnes, x[i].x, x[i].y);
+        else mma16(ones, kOnes, kOnes, kOnes, kOnes, x[i].x, x[i].y);
+        mma16(ones, kOnes, kOnes, kOnes, kOnes, x[i].z, x[i].w);
+      }
+      sum0 = ones[0];
+      sum1 = ones[1];
+    }
+  }
+  Scales m;
+  if constexpr (F != kFmt16) load_scales(slot, (int)g, m);
+  if constexpr (F == kFmt16) {
+    // columns of the lane: pairs 2b, 2b + 1 (b = t mod 2) of both halves of stretch t / 2
+    const char* half = slot + 1024 * (t >> 1) + 8 * (t & 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t r = 4 * g + 2 * h, u = 2 * (t >> 1);
+      const uint2 a0 = *reinterpret_cast<const uint2*>(half + 16 * (r ^ u)), b0 = *reinterpret_cast<const uint2*>(half + 16 * ((r + 1) ^ u));
+      const uint2 a1 = *reinterpret_cast<const uint2*>(half + 512 + 16 * (r ^ (u + 1))), b1 = *reinterpret_cast<const uint2*>(half + 512 + 16 * ((r + 1) ^ (u + 1)));
+      mma16(tot[h], a0.x, b0.x, a1.x, b1.x, x[0].x, x[0].y);
+      mma16(tot[h], a0.y, b0.y, a1.y, b1.y, x[0].z, x[0].w);
+    }
+  } else if constexpr (F == kFmt8 || F == kFmt4) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4 a = *reinterpret_cast<const uint4*>(slot + 512 * t + 16 * ((4 * g + 2 * h) ^ t));
+      const uint4 b = *reinterpret_cast<const uint4*>(slot + 512 * t + 16 * ((4 * g + 2 * h + 1) ^ t));
+      if constexpr (F == kFmt8) {                  // a stretch: words 0, 1 its first eight columns, 2, 3 the others
+        float acc[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t a0 = word_of(a, i), a1 = word_of(a, i + 2), b0 = word_of(b, i), b1 = word_of(b, i + 2);
+          if (i == 0)
+            mma16_first(acc, __byte_perm(a0, 0, 0x4140), __byte_perm(b0, 0, 0x4140), __byte_perm(a1, 0, 0x4140), __byte_perm(b1, 0, 0x4140), x[i].x, x[i].y);
+          else mma16(acc, __byte_perm(a0, 0, 0x4140), __byte_perm(b0, 0, 0x4140), __byte_perm(a1, 0, 0x4140), __byte_perm(b1, 0, 0x4140), x[i].x, x[i].y);
+          mma16(acc, __byte_perm(a0, 0, 0x4342), __byte_perm(b0, 0, 0x4342), __byte_perm(a1, 0, 0x4342), __byte_perm(b1, 0, 0x4342), x[i].z, x[i].w);
+        }
+        apply_scales(m, h, acc, sum0, sum1, tot[h]);
+      } else {                                     // two stretches: words 2s and 2s + 1, a word eight columns
+        float acc[2][4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint32_t a0 = word_of(a, 2 * s), a1 = word_of(a, 2 * s + 1), b0 = word_of(b, 2 * s), b1 = word_of(b, 2 * s + 1);
+          const uint32_t c0 = a0 >> 8, c1 = a1 >> 8, d0 = b0 >> 8, d1 = b1 >> 8;
+          constexpr uint32_t lo = 0x000f000fu, hi = 0x00f000f0u;
+          if (s == 0) {
+            mma16_first(acc[0], a0 & lo, b0 & lo, a1 & lo, b1 & lo, x[0].x, x[0].y);
+            mma16_first(acc[1], a0 & hi, b0 & hi, a1 & hi, b1 & hi, x[0].z, x[0].w);
+          } else {
+            mma16(acc[0], a0 & lo, b0 & lo, a1 & lo, b1 & lo, x[2].x, x[2].y);
+            mma16(acc[1], a0 & hi, b0 & hi, a1 & hi, b1 & hi, x[2].z, x[2].w);
+          }
+          mma16(acc[0], c0 & lo, d0 & lo, c1 & lo, d1 & lo, x[2 * s + 1].x, x[2 * s + 1].y);
+          mma16(acc[1], c0 & hi, d0 & hi, c1 & hi, d1 & hi, x[2 * s + 1].z, x[2 * s + 1].w);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[0][j] = fmaf(acc[1][j], 0.0625f, acc[0][j]);
+        apply_scales(m, h, acc[0], sum0, sum1, tot[h]);
+      }
+    }
+  } else {
+    // Two leading bits in the 2-bit arrangement, further bits in words of their own.  `up`: how many bits stand below
+    // the leading two; the code of pair j of a word is put together with its last bit at 2 (j mod 4).
+    constexpr int up = F == kFmtP4 ? 2 : F == kFmtP3 ? 1 : 0;
+    constexpr bool third = F == kFmt3;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t lead[2][2], h1[2] = {0, 0}, h0[2] = {0, 0};       // [row][stretch], [row]
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t row = 4 * g + 2 * h + r;
+        const uint2 w = *reinterpret_cast<const uint2*>(slot + code_at<F>(t >> 1, row) + 8 * (t & 1));
+        lead[r][0] = w.x;
+        lead[r][1] = w.y;
+        if constexpr (third || up) h1[r] = *reinterpret_cast<const uint32_t*>(slot + code_at<F>(2, row) + 4 * t);
+        if constexpr (up == 2) h0[r] = *reinterpret_cast<const uint32_t*>(slot + code_at<F>(3, row) + 4 * t);
+      }
+      float acc[4][4];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {                // stretch s: a word of sixteen codes
+        uint32_t top[2][2], low[2][2];             // [row][pairs 0 .. 3 / 4 .. 7]
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          top[r][0] = lead[r][s] << up;
+          top[r][1] = lead[r][s] >> (8 - up);
+          if constexpr (third) {                   // the third bit stands above the two: at 2 (j mod 4) + 2
+            low[r][0] = moved_by(h1[r], 8 * s - 2);
+            low[r][1] = moved_by(h1[r], 8 * s - 1);
+          } else if constexpr (up == 1) {
+            low[r][0] = moved_by(h1[r], 8 * s);
+            low[r][1] = moved_by(h1[r], 8 * s + 1);
+          } else if constexpr (up == 2) {
+            low[r][0] = and_or(moved_by(h1[r], 8 * s - 1), 0x00aa00aau, (h0[r] >> (8 * s)) & 0x00550055u);
+            low[r][1] = and_or(moved_by(h1[r], 8 * s), 0x00aa00aau, (h0[r] >> (8 * s + 1)) & 0x00550055u);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t v[2][2];
+          const uint32_t top_mask = (3u << (2 * j + up)) * 0x00010001u;
+          const uint32_t low_mask = (third ? 4u << (2 * j) : up == 2 ? 3u << (2 * j) : 1u << (2 * j)) * 0x00010001u;
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              v[r][p] = top[r][p] & top_mask;
+              if constexpr (third || up) v[r][p] = and_or(low[r][p], low_mask, v[r][p]);
+            }
+          const uint4& xs = x[2 * s + (j >> 1)];
+          const uint32_t b0 = j & 1 ? xs.z : xs.x, b1 = j & 1 ? xs.w : xs.y;
+          if (s == 0) mma16_first(acc[j], v[0][0], v[1][0], v[0][1], v[1][1], b0, b1);
+          else mma16(acc[j], v[0][0], v[1][0], v[0][1], v[1][1], b0, b1);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[0][j] = fmaf(acc[1][j], 0.25f, acc[0][j]);
+        acc[2][j] = fmaf(acc[3][j], 0.25f, acc[2][j]);
+        acc[0][j] = fmaf(acc[2][j], 0.0625f, acc[0][j]);
+      }
+      apply_scales(m, h, acc[0], sum0, sum1, tot[h]);
+    }
+  }
+}
+
+// ---- a warp's walk over its steps ----------------------------------------------------------------
+struct Ring {
+  const char* base;
+  uint32_t base_s, slot;                          // slot: offset of the next step's
+  int lane;
+};
+template <int XC, int STAGES>
+__device__ __forceinline__ void ring_on(Ring& r) {
+  cp_commit();
+  r.slot = r.slot == (STAGES - 1) * kSlotOf<XC> ? 0 : r.slot + kSlotOf<XC>;
+}
+// Multiplies steps of a block in format F, at most n, and asks for the next step of the feed after each while that is in
+// the same format.  Returns with n = 0, or having multiplied a step without having asked (true).
+template <int F, int XC, int STAGES>
+__device__ __forceinline__ bool walk_format(int& n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4]) {
+  constexpr int ls = step_shift(F);
+  const uint32_t t = (uint32_t)r.lane & 3;
+  // The lane's pieces of a step: e = 4t + i, 8q + 2t + i or 4q + t, q the step inside its group, in the order of piece_at:
+  // at0 ^ (what q adds) ^ i.  A streamed row is the part of its step.
+  const uint32_t at0 = ls == 0 ? (5 * t) ^ o.flip : ls == 1 ? (2 * t) ^ (t >> 1) ^ o.flip : XC ? t : t ^ o.flip;
+#pragma unroll 1
+  do {
+    cp_wait<STAGES - 1>();
+    __syncwarp();                                 // what the other lanes have copied
+    const uint32_t q = (uint32_t)o.step & ((1 << ls) - 1);
+    const int grp = o.step >> ls;
+    if constexpr (XC == 0)
+      multiply_step<F, true>(r.base + r.slot, r.lane, o.x + (size_t)grp * o.rows * 256, at0 ^ (ls == 1 ? 10 * q : ls == 2 ? 5 * q : 0),
+                             o.sum + (grp * 2 + (ls == 1 ? q : 0)) * o.rows, o.sum_next, o.rows, tot);
+    else multiply_step<F, false>(r.base + r.slot, r.lane, o.x + r.slot, at0 ^ (ls == 1 ? 2 * q : ls == 2 ? q : 0), nullptr, 0, 0, tot);
+    o.step++;
+    __syncwarp();                                 // every lane has read the slot
+    --n;
+    if (f.fmt != F || f.left == 0) return true;
+    f.left--;
+    ask<F, XC, true, true>(f, r.base_s + r.slot, r.lane);
+    ring_on<XC, STAGES>(r);
+  } while (n);
+  return false;
+}
+// The next n steps, all of one block in format `fmt`.  more(): sets the feed up for the next block; false: there is none.
+template <int XC, int STAGES, class More>
+__device__ __forceinline__ void walk(int fmt, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], More more) {
+  while (n) {
+    bool due;
+    switch (fmt) {
+      case kFmt16: due = walk_format<kFmt16, XC, STAGES>(n, f, r, o, tot); break;
+      case kFmt8: due = walk_format<kFmt8, XC, STAGES>(n, f, r, o, tot); break;
+      case kFmt4: due = walk_format<kFmt4, XC, STAGES>(n, f, r, o, tot); break;
+      case kFmt3: due = walk_format<kFmt3, XC, STAGES>(n, f, r, o, tot); break;
+      case kFmtP4: due = walk_format<kFmtP4, XC, STAGES>(n, f, r, o, tot); break;
+      case kFmtP3: due = walk_format<kFmtP3, XC, STAGES>(n, f, r, o, tot); break;
+      case kFmt2: due = walk_format<kFmt2, XC, STAGES>(n, f, r, o, tot); break;
+      default: due = walk_format<kFmtP2, XC, STAGES>(n, f, r, o, tot); break;
+    }
+    if (due) {
+      if (f.left || more()) ask_any<XC, true, true>(f, r.base_s + r.slot, r.lane);
+      ring_on<XC, STAGES>(r);
+    }
+  }
+}
+
+// ---- sums of the warps ---------------------------------------------------------------------------
+// A warp's 32 x 8 sums in shared memory: [token][kSumPitch], so that neither the stores of a fragment nor the loads of
+// 32 rows meet in a bank.
+constexpr int kSumPitch = 36;
+constexpr int kSumFloats = kUnitCols * kSumPitch;
+__device__ __forceinline__ void put_sums(float* mine, int lane, const float (&tot)[2][4]) {
+  const int g = lane >> 2, t = lane & 3;
+  *reinterpret_cast<float4*>(mine + 2 * t * kSumPitch + 4 * g) = make_float4(tot[0][0], tot[0][2], tot[1][0], tot[1][2]);
+  *reinterpret_cast<float4*>(mine + (2 * t + 1) * kSumPitch + 4 * g) = make_float4(tot[0][1], tot[0][3], tot[1][1], tot[1][3]);
+}
+
+}  // namespace pw

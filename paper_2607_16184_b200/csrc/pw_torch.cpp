@@ -10,6 +10,7 @@
 
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <string.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/pw.h"
@@ -233,9 +234,70 @@ PyObject* moe_forward_routed(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// A Python reference that is given back.
+struct Ref {
+  PyObject* o;
+  explicit Ref(PyObject* p) : o(p) {}
+  ~Ref() { Py_XDECREF(o); }
+  Ref(const Ref&) = delete;
+};
+
+// The header of a Page or PlanePage (its ctypes structure) whose buffer is on the call's device.
+bool page_header(Call& c, PyObject* o, int arg, pw_page* out) {
+  Ref head(PyObject_GetAttrString(o, "c")), codes(head.o ? PyObject_GetAttrString(o, "codes") : nullptr);
+  if (!codes.o) return false;                      // Python's error is set
+  Py_buffer b;
+  if (PyObject_GetBuffer(head.o, &b, PyBUF_SIMPLE) < 0) return false;
+  const bool whole = b.len == (Py_ssize_t)sizeof(pw_page);
+  if (whole) memcpy(out, b.buf, sizeof(pw_page));
+  PyBuffer_Release(&b);
+  if (!whole) return c.fail(PW_ERR_INVALID_ARG, arg), false;
+  if (codes.o == Py_None) return true;             // a page without a buffer: the library says what is wrong with it
+  if (!THPVariable_Check(codes.o) || !THPVariable_Unpack(codes.o).is_cuda() || THPVariable_Unpack(codes.o).get_device() != c.index)
+    return c.fail(PW_ERR_INVALID_ARG, arg), false;
+  return true;
+}
+
+// x, pages, out_features, bias, out
+PyObject* page_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 8, [](Call& c, PyObject* const* a) -> int {
+    const Matrix x = matrix(c, a[0], 1, PW_F16);
+    pw_page page[PW_LINEAR_PAGES];
+    int32_t features[PW_LINEAR_PAGES];
+    Ref pages(PySequence_Fast(a[1], "pages: a sequence of pages"));
+    if (!pages.o) return 0;
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(pages.o);
+    if (count < 1 || count > PW_LINEAR_PAGES) c.fail(PW_ERR_INVALID_ARG, 2);
+    if (c.bad) return c.bad;
+    int64_t total = 0;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      if (!page_header(c, PySequence_Fast_GET_ITEM(pages.o, i), 2, &page[i])) return c.bad;
+      features[i] = (int32_t)page[i].rows;
+      if (page[i].rows > INT32_MAX) return c.fail(PW_ERR_SHAPE, 2), c.bad;
+    }
+    if (a[2] != Py_None) {
+      Ref f(PySequence_Fast(a[2], "out_features: a sequence of numbers"));
+      if (!f.o) return 0;
+      if (PySequence_Fast_GET_SIZE(f.o) != count) c.fail(PW_ERR_SHAPE, 3);
+      for (Py_ssize_t i = 0; i < count && !c.bad; ++i) {
+        features[i] = c.integer(PySequence_Fast_GET_ITEM(f.o, i), 3);
+        if (features[i] < 1) c.fail(PW_ERR_INVALID_ARG, 3);
+      }
+    }
+    for (Py_ssize_t i = 0; i < count; ++i) total += features[i];
+    Matrix bias;
+    if (a[3] != Py_None) bias = vector(c, a[3], 4, -1, total);
+    const Matrix out = matrix(c, a[4], 5, -1, x.rows, total);
+    if (c.bad) return c.bad;
+    Outside outside(c);
+    return pw_page_linear(c.ctx, (int)x.rows, (int)x.cols, x.data, x.stride, page, features, (int)count, bias.data, bias.type, out.data, out.type, out.stride,
+                          c.stream);
+  });
+}
+
 #define PW_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PW_METHOD(quantize_scaled), PW_METHOD(add_rmsnorm), PW_METHOD(scaled_linear), PW_METHOD(route_tokens),
-                         PW_METHOD(moe_forward_routed), {nullptr, nullptr, 0, nullptr}};
+                         PW_METHOD(moe_forward_routed), PW_METHOD(page_linear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pwtorch", "Argument marshalling for torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
