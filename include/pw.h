@@ -321,6 +321,24 @@ pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16,
                                 const float* gates, int T, int top_k, const pw_page_table* table, float* out, pw_mode mode,
                                 pw_stream stream);
 
+/* The two layer calls for a handful of tokens, T <= PW_FEW_TOKENS, in one kernel: the latency of a decode step.  Same pages
+ * (TILED and PLANES), page table, routing rule, routed ids and gates, observation taps; out: device [T, H] of out_type
+ * (pw_type).  They differ from pw_moe_forward in the weights, which are code * scale + zero-point without the rounding to
+ * fp16, and in that a token that names an expert twice is multiplied once, with the sum of the gates.
+ * The activations of the call are kept in an SM's shared memory: T * hidden up to 65536, in a layer of very many
+ * experts somewhat less (SHAPE beyond; T = 1 always has room up to hidden = 32768).
+ * All CTAs of the kernel run at the same time (a cooperative launch): on a device that other kernels keep busy it starts
+ * when they leave room for one CTA per SM.  Works in the context's workspace, like pw_moe_forward, and is ordered with
+ * its calls; pw_get_routing and pw_kernel_timing do not see this call.
+ * A device-side wait that runs out is reported by pw_last_device_status.
+ * Errors: as pw_moe_forward, and INVALID_ARG (T > PW_FEW_TOKENS, out_type), SHAPE (no room). */
+#define PW_FEW_TOKENS 16
+pw_status pw_moe_forward_few(pw_ctx* ctx, int layer, const void* hidden_fp16, const float* router_logits, int T, int top_k,
+                             const pw_page_table* table, void* out, int out_type, pw_stream stream);
+pw_status pw_moe_forward_few_routed(pw_ctx* ctx, int layer, const void* hidden_fp16, const int32_t* topk_ids,
+                                    const float* gates, int T, int top_k, const pw_page_table* table, void* out,
+                                    int out_type, pw_stream stream);
+
 /* pw_moe_forward for callers whose activations live in host memory: copies hidden_host
  * ([T, H] fp16) and logits_host ([T, E] fp32) to staging buffers in the workspace, runs
  * pw_moe_forward on them and copies the fp32 result to out_host ([T, H]), all ordered on `stream`.

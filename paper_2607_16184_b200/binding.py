@@ -31,11 +31,12 @@ EXPORTS = ("pw_workspace_bytes", "pw_create", "pw_destroy", "pw_page_bytes", "pw
            "pw_offload_page", "pw_reload_page", "pw_page_state", "pw_drop_page",
            "pw_offload_plane", "pw_reload_plane", "pw_plane_state",
            "pw_moe_forward", "pw_moe_forward_routed", "pw_moe_forward_host", "pw_quantize_scaled", "pw_add_rmsnorm", "pw_scaled_linear", "pw_route_tokens",
-           "pw_page_linear",
+           "pw_page_linear", "pw_moe_forward_few", "pw_moe_forward_few_routed",
            "pw_get_routing", "pw_route_tokens_static", "pw_observe", "pw_observation_summary", "pw_plan_step", "pw_plan_queue_create", "pw_plan_queue_destroy", "pw_plan_queue_step", "pw_plan_queue_peek", "pw_kv_pressure_bytes",
            "pw_last_device_status",
            "pw_kernel_timing", "pw_get_kernel_times", "pw_launch_count", "pw_debug_set_wait", "pw_status_str")
 PW_F32, PW_F16, PW_BF16 = 0, 1, 2
+PW_FEW_TOKENS, PW_LINEAR_PAGES = 16, 8
 PW_SCORE_SOFTMAX, PW_SCORE_SIGMOID = 0, 1
 _SCORES = {"softmax": PW_SCORE_SOFTMAX, "sigmoid": PW_SCORE_SIGMOID, PW_SCORE_SOFTMAX: PW_SCORE_SOFTMAX,
            PW_SCORE_SIGMOID: PW_SCORE_SIGMOID}
@@ -164,6 +165,10 @@ def load():
     L.pw_scaled_linear.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, i64, vp, vp, i32, i64, vp]
     L.pw_route_tokens.restype = i32
     L.pw_route_tokens.argtypes = [vp, C.POINTER(pw_routing), vp, i32, i64, vp, i32, vp, vp, vp]
+    L.pw_moe_forward_few.restype = i32
+    L.pw_moe_forward_few.argtypes = [vp, i32, vp, vp, i32, i32, vp, vp, i32, vp]
+    L.pw_moe_forward_few_routed.restype = i32
+    L.pw_moe_forward_few_routed.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, vp, i32, vp]
     L.pw_page_linear.restype = i32
     L.pw_page_linear.argtypes = [vp, i32, i32, vp, i64, C.POINTER(pw_page), C.POINTER(C.c_int32), i32, vp, i32, vp, i32, i64, vp]
     L.pw_moe_forward_host.restype = i32
@@ -691,7 +696,31 @@ class Context:
         st = (_pwtorch or _load_pwtorch()).page_linear(self._ptr, self._index, None if stream is None else stream.cuda_stream, x,
                                                        pages, out_features, bias, out)
         if st:
-            self._refused(st, "pw_page_linear", ("x", "pages", "out_features", "bias", "out"))
+            self._refused(st, "pw_page_linear", "pw_moe_forward_few", "pw_moe_forward_few_routed", ("x", "pages", "out_features", "bias", "out"))
+        return out
+
+    def pw_moe_forward_few(self, layer: int, hidden: torch.Tensor, router_logits: torch.Tensor, top_k: int,
+                           out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The layer call for up to PW_FEW_TOKENS tokens in one kernel; out [T, H] in fp32, fp16 or bf16."""
+        if out is None:
+            out = self._new(stream, lambda: torch.empty(hidden.shape, dtype=out_dtype, device=self.device))
+        st = (_pwtorch or _load_pwtorch()).moe_forward_few(self._ptr, self._index, None if stream is None else stream.cuda_stream, layer, hidden,
+                                                           router_logits, top_k, out, self.cfg.hidden, self.cfg.n_experts)
+        if st:
+            self._refused(st, "pw_moe_forward_few", ("layer", "hidden", "router_logits", "top_k", "out"))
+        return out
+
+    def pw_moe_forward_few_routed(self, layer: int, hidden: torch.Tensor, topk_ids: torch.Tensor, gates: torch.Tensor,
+                                  out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The same for a routing the caller has (ids [T, k], -1 = no expert; gates [T, k])."""
+        if out is None:
+            out = self._new(stream, lambda: torch.empty(hidden.shape, dtype=out_dtype, device=self.device))
+        st = (_pwtorch or _load_pwtorch()).moe_forward_few_routed(self._ptr, self._index, None if stream is None else stream.cuda_stream, layer,
+                                                                  hidden, topk_ids, gates, out, self.cfg.hidden)
+        if st:
+            self._refused(st, "pw_moe_forward_few_routed", ("layer", "hidden", "topk_ids", "gates", "out"))
         return out
 
     def pw_moe_forward_host(self, layer: int, hidden_host: torch.Tensor, logits_host: torch.Tensor, top_k: int,

@@ -58,6 +58,10 @@ WsMap make_wsmap(const pw_config& c) {
   m.io_logits = take((size_t)c.max_tokens * c.n_experts * 4);
   m.io_out = take((size_t)c.max_tokens * c.hidden * 4);
   m.obs_part = take(4 * (size_t)kNormSplit * 2 * m.Rpad);
+  const size_t few = c.max_tokens < PW_FEW_TOKENS ? c.max_tokens : PW_FEW_TOKENS, few_pairs = few * (c.max_top_k + c.n_shared);
+  m.few_sync = take(4 * (64 + (size_t)c.hidden / 32));
+  m.few_seen = take(4 * (4 + 2 * (size_t)m.S + 2 * few_pairs));
+  m.few_h = take(few_pairs * c.ffn * 2);
   m.total = o;
   return m;
 }
@@ -121,6 +125,7 @@ extern "C" pw_status pw_create(pw_ctx** out, const pw_config* cfg) {
   ctx->launches = 0;
   ctx->last_T = ctx->last_k = 0;
   ctx->few_ready = 0;
+  ctx->few_layer_ready = false;
   ctx->tc_state = nullptr;
   ctx->wait_polls = 0;
   ctx->test_hook = 0;
@@ -251,8 +256,8 @@ extern "C" pw_status pw_query_row(pw_ctx* ctx, int layer, int expert, int kind, 
 }
 
 // Argument checks of a forward call: everything that can be refused is refused here, before anything is enqueued.
-static pw_status check_forward_args(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k,
-                                    const pw_page_table* table, const float* out, pw_mode mode) {
+pw_status pw::check_forward(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k,
+                            const pw_page_table* table, const void* out, pw_mode mode) {
   if (!ctx || !hidden || !out) return PW_ERR_INVALID_ARG;
   if (!routing.logits && (!routing.ids || !routing.gates)) return PW_ERR_INVALID_ARG;
   const pw_config& c = ctx->cfg;
@@ -275,7 +280,7 @@ static pw_status check_forward_args(pw_ctx* ctx, int layer, const void* hidden, 
 
 static pw_status moe_forward(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k,
                              const pw_page_table* table, float* out, pw_mode mode, pw_stream stream) {
-  const pw_status as = check_forward_args(ctx, layer, hidden, routing, T, top_k, table, out, mode);
+  const pw_status as = check_forward(ctx, layer, hidden, routing, T, top_k, table, out, mode);
   if (as != PW_OK) return as;
   const pw_config& c = ctx->cfg;
 
@@ -346,7 +351,7 @@ extern "C" pw_status pw_moe_forward_host(pw_ctx* ctx, int layer, const void* hid
   char* b = ctx->base;
   const WsMap& w = ctx->ws;
   // refuse what the forward call would refuse before the first copy is enqueued (the staging buffers stay untouched)
-  const pw_status as = check_forward_args(ctx, layer, b + w.io_hidden, Routing{reinterpret_cast<const float*>(b + w.io_logits), nullptr, nullptr}, T,
+  const pw_status as = check_forward(ctx, layer, b + w.io_hidden, Routing{reinterpret_cast<const float*>(b + w.io_logits), nullptr, nullptr}, T,
                                           top_k, nullptr, reinterpret_cast<const float*>(b + w.io_out), mode);
   if (as != PW_OK) return as;
   PW_CUDA_OK(cudaMemcpyAsync(b + w.io_hidden, hidden_host, (size_t)T * c.hidden * 2, cudaMemcpyHostToDevice, stream));
@@ -381,6 +386,7 @@ extern "C" pw_status pw_last_device_status(pw_ctx* ctx) {
   PW_CUDA_OK(cudaMemcpy(&v, ctx->base + ctx->ws.status, 4, cudaMemcpyDeviceToHost));
   if (v != 0) {
     PW_CUDA_OK(cudaMemset(ctx->base + ctx->ws.status, 0, 4));
+    if (v == PW_ERR_TIMEOUT) PW_CUDA_OK(cudaMemset(ctx->base + ctx->ws.few_sync, 0, ctx->ws.few_seen - ctx->ws.few_sync));
   }
   return (pw_status)v;
 }

@@ -65,6 +65,9 @@ struct WsMap {
   size_t io_logits;   // float [Tmax][E]
   size_t io_out;      // float [Tmax][H]
   size_t obs_part;    // float [kNormSplit][2][Rpad]  partial squared norms of the operand rows (observation taps)
+  size_t few_sync;    // int32[64 + hidden / 32]  layer for few tokens: meeting of its CTAs, finished parts of the output (zeros between calls)
+  size_t few_seen;    // int32[]       its active experts and pairs, for the observation taps
+  size_t few_h;       // fp16 [pairs of PW_FEW_TOKENS tokens][F]  its SwiGLU output, in pieces
   size_t total;
   // derived sizes
   int S;              // segments = E + n_shared
@@ -119,7 +122,9 @@ struct pw_ctx {
   // is set last)
   std::atomic<void*> encode_tiled;    // driver entry point for tensor maps
   std::atomic<int> max_clusters[5];   // clusters of that product's CTAs that run at the same time, by size
-  std::atomic<int> few_ready;     // the kernels for few tokens have their attributes
+  std::atomic<int> few_clusters[3];   // the same for the kernels for few tokens: clusters of 2, 4, 8 of their CTAs
+  std::atomic<int> few_ready;     // those are looked up
+  bool few_layer_ready;           // the few-token layer's kernels have their attributes
   void* tc_state;                 // tensor-core path state (set up lazily)
   uint32_t wait_polls;            // limit of the device-side waits in polls of 20 us (0 = the default, 2 s)
   uint32_t test_hook;             // device-side test hooks (pw_debug_set_wait)
@@ -169,6 +174,8 @@ void residency_teardown(pw_ctx* ctx);
 // the same for a row that is committed to a block of bit-planes read at page.bits: the planes 3 .. bits
 pw_status residency_check_commit_planes(pw_ctx* ctx, size_t row, const pw_page& page);
 void residency_note_commit_planes(pw_ctx* ctx, size_t row, const pw_page& page);
+pw_status check_forward(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k,
+                        const pw_page_table* table, const void* out, pw_mode mode);
 pw_status launch_ffn_simt(pw_ctx* ctx, int layer, int T, int k, cudaStream_t s);
 pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, int ksplit, cudaStream_t s);
 int tensor_token_tile(const pw_ctx* ctx, int T, int k);

@@ -1,13 +1,11 @@
-// The calls for few tokens: dense products on weight pages (pw_page_linear) and the whole layer in one kernel
-// (pw_moe_forward_few).  The inner loop is in pw_stream.cuh.
+// Dense products on weight pages for few tokens (pw_page_linear).  The inner loop is in pw_stream.cuh.
 #include "pw_scaled.cuh"
 #include "pw_stream.cuh"
 
 namespace pw {
 
-constexpr int kSmemLimit = 232448;                // 227 KB
 constexpr int kSumsBytes = kStreamWarps * kSumFloats * 4;
-constexpr int kUnitOut = kUnitRows * kUnitCols;
+constexpr int kPartsBytes = 16384;                // sums of a batch of units from the CTAs of a cluster
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -34,140 +32,170 @@ struct LinearPage {
   int col0;                                       // its first column of the output
 };
 struct PageLinearArgs {
-  LinearPage page[PW_LINEAR_PAGES];
+  int T, groups, x_bytes;
+  int width, passes, slices;                      // tokens of a pass
+  int team_shift, split;                          // log2 of the warps that share a unit; CTAs of a cluster, which share the columns
+  int room, split_groups;                         // tokens and groups that there is room for in a CTA
+  int batch;                                      // units of a team between two exchanges of a cluster
+  int pages, out_type, bias_type;
   const char* x;
   size_t x_pitch;                                 // bytes
   void* out;
   const void* bias;
   int64_t ld_out;
-  int T, groups, x_bytes;
-  int width, passes, slices;                      // tokens of a pass (8, fewer for very long rows)
-  int team_shift, split;                          // log2 of the warps that share a unit; CTAs of a cluster, which share the columns
-  int rows, split_groups;                         // most tokens of a pass, most groups of a CTA: what is staged
-  int out_type, bias_type;
+  LinearPage page[PW_LINEAR_PAGES];
 };
 struct LinearUnit {
   int page, slice;
 };
 __device__ __forceinline__ LinearUnit linear_unit(const PageLinearArgs& a, int u) {
   LinearUnit un{0, u};
-  while (u >= a.page[un.page].end) ++un.page;
-  if (un.page) un.slice -= a.page[un.page - 1].end;
+  if (a.pages > 1) {
+    while (u >= a.page[un.page].end) ++un.page;
+    if (un.page) un.slice -= a.page[un.page - 1].end;
+  }
   return un;
+}
+
+__device__ __forceinline__ void put_linear(const PageLinearArgs& a, const LinearUnit& un, int token, int row, float v) {
+  const int m = un.slice * kUnitRows + row;
+  if (m >= a.page[un.page].rows) return;
+  const int at_col = a.page[un.page].col0 + m;
+  if (a.bias) v = __fadd_rn(v, load1(a.bias, at_col, a.bias_type));
+  store1(a.out, (int64_t)token * a.ld_out + at_col, a.out_type, v);
 }
 
 // A cluster takes a pass of up to eight tokens, stages their columns (each CTA its part) and goes through slices of 32
 // rows.  Teams of 4, 8 or 16 warps take a slice each; the warps of a team share the CTA's columns and add their sums in
-// warp order, the CTAs of a cluster (whose team is the whole CTA) theirs in rank order.
-template <int STAGES>
+// warp order, the CTAs of a cluster theirs in rank order, a batch of slices at a time.
+// F: the format of all pages, or kAnyFormat; a kernel for one format is a quarter of the code, and a call for one token
+// spends a large part of its time on fetching code.
+template <int F, int STAGES>
 __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __grid_constant__ PageLinearArgs a) {
   constexpr int kRing = STAGES * kSlotOf<0>;
   extern __shared__ __align__(128) char smem[];
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int ts = a.team_shift, team = warp >> ts, member = warp & ((1 << ts) - 1);
   float* const sums = reinterpret_cast<float*>(smem + kStreamWarps * kRing) + (team << ts) * kSumFloats;
-  float* const parts = reinterpret_cast<float*>(smem + kStreamWarps * kRing + kSumsBytes);   // [2][split][kUnitOut] of rank 0
-  float* const xsum = parts + (a.split > 1 ? 2 * a.split * kUnitOut : 0);
-  char* const pieces = reinterpret_cast<char*>(xsum) + ((a.split_groups * 2 * a.rows * 4 + 127) & ~127);
+  float* const parts = reinterpret_cast<float*>(smem + kStreamWarps * kRing + kSumsBytes);   // [rank][slot / split][token][32 rows], slots: [team][batch]
+  float* const xsum = parts + (a.split > 1 ? kPartsBytes / 4 : 0);
+  char* const pieces = reinterpret_cast<char*>(xsum) + ((a.split_groups * 3 * a.room * 4 + 127) & ~127);
 
   const int rank = a.split > 1 ? (int)cluster_rank() : 0;
   const int cluster = a.split > 1 ? (int)blockIdx.x / a.split : (int)blockIdx.x, clusters = a.split > 1 ? (int)gridDim.x / a.split : (int)gridDim.x;
   const int g0 = a.groups * rank / a.split, my_groups = a.groups * (rank + 1) / a.split - g0;
   // clusters deal out the passes among them; those with the same pass share its slices
   const int sharing = a.passes < clusters ? (clusters - cluster % a.passes + a.passes - 1) / a.passes : 1;
-  const int first = (a.passes < clusters ? cluster / a.passes : 0) + sharing * team, stride = sharing << (4 - ts);
+  const int first = a.passes < clusters ? cluster / a.passes : 0, stride = sharing << (4 - ts);   // of team 0; the others' lie `sharing` apart
 
-  Ring r{smem + warp * kRing, 0, 0, lane};
-  r.base_s = smem_u32(r.base);
+  const Fixed fixed;
+  const uint32_t ring = smem_u32(smem) + warp * kRing;
+  Ring r{ring, ring, lane};
   Feed f;
   f.left = 0;
-  int next = first;                               // slice the feed takes next
+  int next = 0;                                   // slice the feed takes next
   auto more = [&]() -> bool {
     while (next < a.slices) {
       const LinearUnit un = linear_unit(a, next);
       const LinearPage& p = a.page[un.page];
-      const int steps = my_groups << step_shift(p.fmt), from = g0 << step_shift(p.fmt);
-      feed_codes(f, lane, p.codes, p.bit1, p.bit0, p.fmt, a.groups, un.slice, from + ((steps * member) >> ts), from + ((steps * (member + 1)) >> ts));
+      const int fmt = F == kAnyFormat ? p.fmt : F;
+      const int steps = my_groups << step_shift(fmt), from = g0 << step_shift(fmt);
+      feed_codes(f, lane, p.codes, p.bit1, p.bit0, fmt, a.groups, un.slice, from + ((steps * member) >> ts), from + ((steps * (member + 1)) >> ts));
       next += stride;
       if (f.left) return true;
     }
     return false;
   };
 
-  int buf = 0;
-  bool waited = false;
+  bool waited = false, exchanged = false;
 #pragma unroll 1
   for (int pass = cluster % a.passes; pass < a.passes; pass += clusters) {
     // pages are final when this kernel is placed, the operand may be written by the kernel ahead: codes first
-    next = first;
+    next = first + sharing * team;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
-      if (f.left || more()) ask_any<0, true, false>(f, r.base_s + i * kSlotOf<0>, lane);
+      if (f.left || more()) ask_for<F, 0, true, false>(f, r.base + i * kSlotOf<0>, lane);
       cp_commit();
     }
-    r.slot = 0;
+    r.slot = r.base;
     if (!waited) {
       grid_dep_sync();
       grid_dep_trigger();
       waited = true;
     }
-    const int cols = min(a.width, a.T - pass * a.width);
+    const int token0 = pass * a.width, cols = min(a.width, a.T - token0);
     __syncthreads();                              // the pass before has read its operand
-    stage_operand(a.x + (size_t)pass * a.width * a.x_pitch, a.x_pitch, cols, g0, my_groups, a.x_bytes, pieces, xsum);
+    stage_operand(a.x + (size_t)token0 * a.x_pitch, a.x_pitch, cols, a.room, g0, my_groups, a.x_bytes, pieces, xsum, threadIdx.x,
+                  kStreamThreads);
     __syncthreads();
+    // (tokens that there are not: any row and sum, their products are not used)
     const int xc = min(lane >> 2, cols - 1), c0 = min(2 * (lane & 3), cols - 1), c1 = min(2 * (lane & 3) + 1, cols - 1);
+    const uint32_t x_lane = smem_u32(pieces) + xc * 256, sum0 = smem_u32(xsum + c0), sum1 = smem_u32(xsum + c1);
+    const int batch = a.split > 1 ? a.batch : 1, slots = batch << (4 - ts);
 #pragma unroll 1
-    for (int u = first; u < a.slices; u += stride, buf ^= 1) {
-      const LinearUnit un = linear_unit(a, u);
-      const int fmt = a.page[un.page].fmt;
-      const int steps = my_groups << step_shift(fmt), lo = (steps * member) >> ts;
-      float tot[2][4] = {};
-      Operand o{pieces + xc * 256, xsum + c0, c1 - c0, cols, (uint32_t)(xc & 1) << 2, lo};
-      walk<0, STAGES>(fmt, ((steps * (member + 1)) >> ts) - lo, f, r, o, tot, more);
-      put_sums(sums + member * kSumFloats, lane, tot);
-      team_sync(team, ts);
-      for (int i = member * 32 + lane; i < kUnitRows * cols; i += 32 << ts) {
-        const int row = i & (kUnitRows - 1), col = i >> 5;
-        float v = 0.f;
+    for (int u0 = first; u0 < a.slices; u0 += stride * batch) {
+      if (a.split > 1 && exchanged) cluster_sync();   // the parts of the batch before have been read
+      for (int j = 0; j < batch; ++j) {
+        const int u = u0 + sharing * team + stride * j;
+        if (u >= a.slices) break;
+        const LinearUnit un = linear_unit(a, u);
+        const int fmt = F == kAnyFormat ? a.page[un.page].fmt : F;
+        const int steps = my_groups << step_shift(fmt), lo = (steps * member) >> ts;
+        float tot[2][4] = {};
+        Operand o{x_lane, sum0, sum1, a.room, (uint32_t)(xc & 1) << 2, lo};
+        walk<F, 0, STAGES>(fixed, fmt, ((steps * (member + 1)) >> ts) - lo, f, r, o, tot, more);
+        put_sums(sums + member * kSumFloats, lane, tot);
+        team_sync(team, ts);
+        for (int i = member * 32 + lane; i < kUnitRows * cols; i += 32 << ts) {
+          const int row = i & (kUnitRows - 1), col = i >> 5;
+          float v = 0.f;
 #pragma unroll 4
-        for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, sums[w * kSumFloats + col * kSumPitch + row]);
-        if (a.split > 1) {
-          store_to_rank(smem_u32(parts + (buf * a.split + rank) * kUnitOut + i), 0, v);
-        } else {
-          const int m = un.slice * kUnitRows + row;
-          if (m < a.page[un.page].rows) {
-            const int at_col = a.page[un.page].col0 + m;
-            if (a.bias) v = __fadd_rn(v, load1(a.bias, at_col, a.bias_type));
-            store1(a.out, (int64_t)(pass * a.width + col) * a.ld_out + at_col, a.out_type, v);
-          }
+          for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, sums[w * kSumFloats + col * kSumPitch + row]);
+          const int slot = team * batch + j;      // slot s is added up by rank s mod split
+          if (a.split > 1) store_to_rank(smem_u32(parts + ((rank * slots + slot) / a.split * kUnitCols) * kUnitRows + i), slot % a.split, v);
+          else put_linear(a, un, token0 + col, row, v);
         }
+        team_sync(team, ts);                      // the sums are written again
       }
       if (a.split > 1) {
-        cluster_sync();                           // (the other buffer is written next: whoever writes this one again has seen rank 0 past it)
-        if (rank == 0)
+        cluster_sync();
+        exchanged = true;
+        for (int s = rank; s < slots; s += a.split) {
+          const int u = u0 + sharing * (s / batch) + stride * (s % batch);
+          if (u >= a.slices) continue;
+          const LinearUnit un = linear_unit(a, u);
           for (int i = threadIdx.x; i < kUnitRows * cols; i += kStreamThreads) {
-            const int row = i & (kUnitRows - 1), col = i >> 5, m = un.slice * kUnitRows + row;
             float v = 0.f;
-            for (int k = 0; k < a.split; ++k) v = __fadd_rn(v, parts[(buf * a.split + k) * kUnitOut + i]);
-            if (m < a.page[un.page].rows) {
-              const int at_col = a.page[un.page].col0 + m;
-              if (a.bias) v = __fadd_rn(v, load1(a.bias, at_col, a.bias_type));
-              store1(a.out, (int64_t)(pass * a.width + col) * a.ld_out + at_col, a.out_type, v);
-            }
+            for (int k = 0; k < a.split; ++k) v = __fadd_rn(v, parts[((k * slots + s) / a.split * kUnitCols) * kUnitRows + i]);
+            put_linear(a, un, token0 + (i >> 5), i & (kUnitRows - 1), v);
           }
-      } else {
-        team_sync(team, ts);                      // the sums are written again by the next unit
+        }
       }
     }
   }
 }
 
 static size_t page_linear_smem(const PageLinearArgs& a, int stages) {
-  return (size_t)kStreamWarps * stages * kSlotOf<0> + kSumsBytes + (a.split > 1 ? 2 * a.split * kUnitOut * 4 : 0) +
-         (((size_t)a.split_groups * 2 * a.rows * 4 + 127) & ~(size_t)127) + (size_t)a.split_groups * a.rows * 256;
+  return (size_t)kStreamWarps * stages * kSlotOf<0> + kSumsBytes + (a.split > 1 ? kPartsBytes : 0) +
+         (((size_t)a.split_groups * 3 * a.room * 4 + 127) & ~(size_t)127) + (size_t)a.split_groups * a.room * 256;
 }
+typedef void (*PageLinearKernel)(PageLinearArgs);
 template <int STAGES>
-static cudaError_t launch_page_linear(const PageLinearArgs& a, int clusters, size_t smem, cudaStream_t s) {
+static PageLinearKernel page_linear_kernel_of(int fmt) {
+  switch (fmt) {
+    case kFmt16: return page_linear_kernel<kFmt16, STAGES>;
+    case kFmt8: return page_linear_kernel<kFmt8, STAGES>;
+    case kFmt4: return page_linear_kernel<kFmt4, STAGES>;
+    case kFmt3: return page_linear_kernel<kFmt3, STAGES>;
+    case kFmt2: return page_linear_kernel<kFmt2, STAGES>;
+    case kFmtP4: return page_linear_kernel<kFmtP4, STAGES>;
+    case kFmtP3: return page_linear_kernel<kFmtP3, STAGES>;
+    case kFmtP2: return page_linear_kernel<kFmtP2, STAGES>;
+    default: return page_linear_kernel<kAnyFormat, STAGES>;
+  }
+}
+static PageLinearKernel page_linear_kernel_of(int fmt, int stages) { return stages == 4 ? page_linear_kernel_of<4>(fmt) : page_linear_kernel_of<2>(fmt); }
+static cudaError_t launch_page_linear(const PageLinearArgs& a, PageLinearKernel kernel, int clusters, size_t smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(clusters * a.split));
   cfg.blockDim = dim3(kStreamThreads);
@@ -181,52 +209,85 @@ static cudaError_t launch_page_linear(const PageLinearArgs& a, int clusters, siz
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, page_linear_kernel<STAGES>, a);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 // Once per context (more than once does no harm): what the launches need of the device.
+constexpr int kSplits = 3;                        // clusters of 2, 4, 8 CTAs
 static pw_status few_setup(pw_ctx* ctx) {
   if (ctx->few_ready.load(std::memory_order_acquire)) return PW_OK;
-  PW_CUDA_OK(cudaFuncSetAttribute(page_linear_kernel<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
-  PW_CUDA_OK(cudaFuncSetAttribute(page_linear_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
+  for (int fmt = kAnyFormat; fmt <= kFmtP2; ++fmt)
+    for (int stages = 2; stages <= 4; stages += 2)
+      PW_CUDA_OK(cudaFuncSetAttribute(page_linear_kernel_of(fmt, stages), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
+  // how many clusters run at the same time, one CTA per SM: an SM left over in its group of SMs is of no use to a cluster
+  for (int i = 0; i < kSplits; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2 << i;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(2 << i);
+    cfg.blockDim = dim3(kStreamThreads);
+    cfg.dynamicSmemBytes = kSmemLimit;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    PW_CUDA_OK(cudaOccupancyMaxActiveClusters(&clusters, page_linear_kernel_of(kAnyFormat, 4), &cfg));
+    ctx->few_clusters[i].store(clusters, std::memory_order_relaxed);
+  }
   ctx->few_ready.store(1, std::memory_order_release);
   return PW_OK;
 }
 
-// How a product is cut: warps to a unit, CTAs to a cluster, stages of the rings, clusters.  `clusters_of`: how many of a
-// size run at the same time.
+// How a product is cut: tokens to a pass, warps to a unit, CTAs to a cluster, stages of the rings.
 struct PageLinearPlan {
   int stages, clusters;
+  double cycles;                                  // estimate
 };
-static PageLinearPlan plan_page_linear(PageLinearArgs& a, int sms) {
-  PageLinearPlan p{0, 0};
-  int steps = 0, pages = 0;
-  for (; pages < PW_LINEAR_PAGES && a.page[pages].codes; ++pages) steps += a.groups << step_shift(a.page[pages].fmt);
-  for (a.width = kUnitCols; a.width && !p.stages; a.width >>= p.stages ? 0 : 1) {
-    a.rows = a.T < a.width ? a.T : a.width;
-    for (a.split = 1; a.split <= 8; a.split *= 2) {
-      a.split_groups = (a.groups + a.split - 1) / a.split;
-      for (int stages = 4; stages >= 3 && !p.stages; --stages)
-        if (page_linear_smem(a, stages) <= kSmemLimit) p.stages = stages;
-      if (p.stages) break;
-    }
-  }
-  if (!p.stages) return p;
-  a.passes = (a.T + a.width - 1) / a.width;
-  const int64_t most = sms / a.split;
-  const int64_t units = (int64_t)a.slices * a.passes;
+// Fills in the fields of `a` that depend on the cut; cycles < 0: it has no room.
+static PageLinearPlan cut_page_linear(PageLinearArgs& a, int width, int split, int ts, int sms, const int* max_clusters) {
+  PageLinearPlan p{0, 0, -1.};
+  a.width = a.room = width;
+  a.split = split;
+  a.split_groups = (a.groups + split - 1) / split;
+  a.team_shift = ts;
+  a.passes = (a.T + width - 1) / width;
+  a.batch = kPartsBytes / (kUnitRows * 4 * kUnitCols) >> (4 - ts);
+  for (int stages = 4; stages >= 2 && !p.stages; stages -= 2)
+    if (page_linear_smem(a, stages) <= kSmemLimit) p.stages = stages;
+  int most = sms;
+  for (int i = 0; i < kSplits; ++i)
+    if (split == 2 << i) most = max_clusters[i];
+  if (!p.stages || most < 1) return p;
+  const int64_t units = (int64_t)a.slices * a.passes, teams = 16 >> ts;
   p.clusters = (int)(units < most ? units : most);
-  a.team_shift = 4;
-  if (a.split > 1) return p;
-  // warps to a unit: what finishes first, where a warp's share of a unit costs its steps plus about three (the hand-over
-  // at its end), and a CTA's teams work at the same time
-  int64_t least = -1;
-  for (int ts = 4; ts >= 2; --ts) {
-    const int64_t teams = (int64_t)sms << (4 - ts);
-    const int64_t cost = (units + teams - 1) / teams * (3 * pages + ((steps + (1 << ts) - 1) >> ts));
-    if (least < 0 || cost < least) least = cost, a.team_shift = ts;
-  }
+  const int64_t sharing = a.passes < p.clusters ? p.clusters / a.passes : 1, passes = (a.passes + p.clusters - 1) / p.clusters;
+  const int64_t rounds = (a.slices + sharing * teams - 1) / (sharing * teams);
+  int64_t steps = 0;                              // of a warp, for a slice of the average page
+  for (int i = 0; i < a.pages; ++i) steps += (int64_t)a.split_groups << step_shift(a.page[i].fmt);
+  steps = (steps + ((int64_t)a.pages << ts) - 1) / ((int64_t)a.pages << ts);
+  // a step of each of the 16 warps takes the SM about 1100 cycles, and one of few warps 400; then the hand-over of a unit,
+  // the exchange of a cluster, and the operands' way into shared memory
+  const double busy = (double)a.slices / (double)(sharing * teams);
+  double c = (double)rounds * ((double)steps * (busy >= 1. ? 1100. : 1100. * busy > 400. ? 1100. * busy : 400.) + 1500.);
+  if (split > 1) c += 4000. + (double)((rounds + a.batch - 1) / a.batch) * 3000.;
+  c += (double)a.split_groups * width * 256 / 30.;
+  p.cycles = c * (double)passes;
   return p;
+}
+// The cut that finishes soonest by that estimate.
+static PageLinearPlan plan_page_linear(PageLinearArgs& a, int sms, const int* max_clusters) {
+  PageLinearPlan best{0, 0, -1.};
+  PageLinearArgs made = a;
+  for (int width = a.T < kUnitCols ? a.T : kUnitCols; width; width /= 2)
+    for (int split = 1; split <= 8; split *= 2)
+      for (int ts = 4; ts >= 2; --ts) {
+        PageLinearArgs b = a;
+        const PageLinearPlan p = cut_page_linear(b, width, split, ts, sms, max_clusters);
+        if (p.cycles >= 0 && (best.cycles < 0 || p.cycles < best.cycles)) best = p, made = b;
+      }
+  a = made;
+  return best;
 }
 
 }  // namespace pw
@@ -289,12 +350,18 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
   a.groups = (int)(pages[0].cols / kGroup);
   a.x_bytes = 2 * K;
   a.slices = (int)slices;
+  a.pages = n_pages;
   a.out_type = out_type;
   a.bias_type = bias_type;
-  const PageLinearPlan p = plan_page_linear(a, ctx->num_sms);
+  int max_clusters[kSplits];
+  for (int i = 0; i < kSplits; ++i) max_clusters[i] = ctx->few_clusters[i].load(std::memory_order_relaxed);
+  const PageLinearPlan p = plan_page_linear(a, ctx->num_sms, max_clusters);
   if (!p.stages) return PW_ERR_SHAPE;
   const size_t smem = page_linear_smem(a, p.stages);
-  PW_CUDA_OK(p.stages == 4 ? launch_page_linear<4>(a, p.clusters, smem, stream) : launch_page_linear<3>(a, p.clusters, smem, stream));
+  int fmt = a.page[0].fmt;
+  for (int i = 1; i < n_pages; ++i)
+    if (a.page[i].fmt != fmt) fmt = kAnyFormat;
+  PW_CUDA_OK(launch_page_linear(a, page_linear_kernel_of(fmt, p.stages), p.clusters, smem, stream));
   ctx->launches++;
   return PW_OK;
 }

@@ -56,6 +56,7 @@ __host__ __device__ constexpr uint32_t stream_scale_offset(int fmt) {
   return fmt >= kFmtP4 ? (uint32_t)kPlaneTopCodes + 512u * (uint32_t)(kFmtP2 - fmt) : stream_tile_bytes(fmt) - 512u;
 }
 
+constexpr int kSmemLimit = 232448;                // 227 KB
 constexpr int kStreamWarps = 16;
 constexpr int kStreamThreads = kStreamWarps * 32;
 constexpr int kUnitRows = 32;
@@ -71,6 +72,22 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds4(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
 
 // Where the 16 bytes of unit u of row `row` lie in a slot, and with 16-byte (u < 4), 8-byte (u < 2) or 4-byte loads of the
 // product's lanes: the loads take rows 4g + j, j fixed, and what makes them meet different banks goes into bits 0, 1 of the
@@ -185,12 +202,13 @@ __device__ __forceinline__ float sum_halves(const uint4& v) {
   return ((a.x + a.y) + (b.x + b.y)) + ((c.x + c.y) + (d.x + d.y));
 }
 // Groups g0 .. g0 + groups of `rows` operand rows (fp16, `pitch` bytes apart, k_bytes of a row count, zeros behind them) ->
-// pieces [group][row][256 bytes] and the sums of the halves of every group, [group][2][row].  By the whole CTA.
-__device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int rows, int g0, int groups, int k_bytes, char* pieces, float* sums) {
-  const int tid = threadIdx.x;
+// pieces [group][room][256 bytes] and the sums of the first half, the second half and the whole of every group,
+// [group][3][room].  By `threads` threads (whole warps).
+__device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int rows, int room, int g0, int groups, int k_bytes, char* pieces, float* sums,
+                                              int thread, int threads) {
   const int n = rows * groups * 8;
-  for (int base = tid & ~31; base < n; base += kStreamThreads) {
-    const int i = base + (tid & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
+  for (int base = thread & ~31; base < n; base += threads) {
+    const int i = base + (thread & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
     uint4 v[2] = {};
     if (i < n) {
       const int k = (g0 + g) * 256 + s * 32;
@@ -207,23 +225,26 @@ __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int r
       }
       uint4 piece[2];
       make_pieces(v[0], v[1], piece);
-      char* row = pieces + (size_t)rg * 256;
+      char* row = pieces + (size_t)(g * room + c) * 256;
       *reinterpret_cast<uint4*>(row + piece_at(2 * s, c) * 16) = piece[0];
       *reinterpret_cast<uint4*>(row + piece_at(2 * s + 1, c) * 16) = piece[1];
     }
     float a = sum_halves(v[0]) + sum_halves(v[1]);
     a += __shfl_xor_sync(0xffffffffu, a, 1);
     a += __shfl_xor_sync(0xffffffffu, a, 2);
-    if (i < n && (s & 3) == 0) sums[(g * 2 + (s >> 2)) * rows + c] = a;
+    const float b = a + __shfl_xor_sync(0xffffffffu, a, 4);
+    if (i < n && (s & 3) == 0) {
+      sums[(g * 3 + (s >> 2)) * room + c] = a;
+      if (s == 0) sums[(g * 3 + 2) * room + c] = b;
+    }
   }
 }
 
 // The operand of a block's steps, as a lane reads it.
 struct Operand {
-  const char* x;                                  // staged: group 0, this lane's row; streamed: this lane's row in slot 0
-  const float* sum;                               // staged: sums of group 0, of the token 2t
-  int sum_next;                                   // from there to the token 2t + 1
-  int rows;                                       // staged rows
+  uint32_t x;                                     // staged: this lane's row of group 0; streamed: the row in slot 0
+  uint32_t sum0, sum1;                            // staged: sums of group 0, tokens 2t and 2t + 1
+  int room;                                       // staged rows there is room for
   uint32_t flip;                                  // 4 for an odd row (see piece_at)
   int step;                                       // next step of the block
 };
@@ -234,15 +255,19 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+// Constant operands in registers that the compiler takes for unknown values: constants it writes anew in front of every
+// instruction, which was a sixth of a 4-bit step's instructions.
+struct Fixed {
+  float zero[4];
+  __device__ __forceinline__ Fixed() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, 0f00000000;" : "=f"(zero[i]));
+  }
+};
+__device__ __forceinline__ void mma16_first(const Fixed& k, float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
-}
-template <bool FIRST>
-__device__ __forceinline__ void mma16_if(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if constexpr (FIRST) mma16_first(d, a0, a1, a2, a3, b0, b1);
-  else mma16(d, a0, a1, a2, a3, b0, b1);
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(k.zero[0]), "f"(k.zero[1]), "f"(k.zero[2]), "f"(k.zero[3]));
 }
 constexpr uint32_t kOnes = 0x3c003c00u;           // two fp16 ones
 
@@ -253,8 +278,8 @@ __device__ __forceinline__ uint32_t moved_by(uint32_t x, int s) { return s >= 0 
 struct Scales {
   float s[4], z[4];
 };
-__device__ __forceinline__ void load_scales(const char* slot, int g, Scales& m) {
-  const uint2 s = *reinterpret_cast<const uint2*>(slot + kStepCodes + 8 * g), z = *reinterpret_cast<const uint2*>(slot + kStepCodes + 64 + 8 * g);
+__device__ __forceinline__ void load_scales(uint32_t slot, uint32_t g, Scales& m) {
+  const uint2 s = lds8(slot + 8 * g + kStepCodes), z = lds8(slot + 8 * g + kStepCodes + 64);
   const float2 s0 = __half22float2(u32_as_h2(s.x)), s1 = __half22float2(u32_as_h2(s.y));
   const float2 z0 = __half22float2(u32_as_h2(z.x)), z1 = __half22float2(u32_as_h2(z.y));
   m.s[0] = s0.x * 16777216.0f, m.s[1] = s0.y * 16777216.0f, m.s[2] = s1.x * 16777216.0f, m.s[3] = s1.y * 16777216.0f;
@@ -268,147 +293,130 @@ __device__ __forceinline__ void apply_scales(const Scales& m, int h, const float
   tot[3] = fmaf(m.s[2 * h + 1], acc[3], fmaf(m.z[2 * h + 1], sum1, tot[3]));
 }
 
-// One step in format F out of a slot.  xrow: this lane's operand row, with the step's pieces at (at0 ^ i) * 16 bytes;
-// STAGED: the operands' sums are at sum[0] and sum[sum_next] (8-bit steps: of half a group), else they are made here.
-template <int F, bool STAGED>
-__device__ __forceinline__ void multiply_step(const char* slot, int lane, const char* xrow, uint32_t at0, const float* sum, int sum_next, int rows,
-                                              float (&tot)[2][4]) {
-  constexpr int ls = step_shift(F);
-  const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3;
-  uint4 x[4 >> ls];
-#pragma unroll
-  for (int i = 0; i < (4 >> ls); ++i) x[i] = *reinterpret_cast<const uint4*>(xrow + ((at0 ^ i) << 4));
-  float sum0 = 0.f, sum1 = 0.f;
-  if constexpr (F != kFmt16) {
-    if constexpr (STAGED) {
-      sum0 = sum[0];
-      sum1 = sum[sum_next];
-      if constexpr (ls == 0) {
-        sum0 += sum[rows];
-        sum1 += sum[rows + sum_next];
-      }
+// The codes of one row's stretch of 16 columns as operands: pair(j, p) = pair j of its first (p = 0) and second eight
+// columns, as integers where they lie: at bit 0 or 4 (4 bits), 2j (two leading bits), 0 (8 bits); set(j): the accumulator
+// for that place.
+template <int F>
+struct Codes {
+  static constexpr int up = F == kFmtP4 ? 2 : F == kFmtP3 ? 1 : 0;   // planes: bits below the leading two
+  static constexpr bool third = F == kFmt3;
+  static constexpr int sets = F == kFmt8 ? 1 : F == kFmt4 ? 2 : 4;
+  static __device__ __forceinline__ constexpr int set(int j) { return sets == 1 ? 0 : sets == 2 ? j & 1 : j; }
+
+  uint32_t w[4];                                  // 8 bits: the words of a stretch; 4 bits: the two; else top codes and low bits
+  // stretch s of the step for this lane (8 bits: the only one)
+  __device__ __forceinline__ void take(const uint4& wide, const uint2& lead, uint32_t h1, uint32_t h0, int s) {
+    if constexpr (F == kFmt8) {
+      w[0] = wide.x, w[1] = wide.y, w[2] = wide.z, w[3] = wide.w;
+    } else if constexpr (F == kFmt4) {
+      w[0] = word_of(wide, 2 * s), w[1] = word_of(wide, 2 * s + 1);
     } else {
-      float ones[4];
-#pragma unroll
-      for (int i = 0; i < (4 >> ls); ++i) {
-        if (i == 0) mma16_first(ones, kOnes, kOnes, kOnes, kOnes, x[i].x, x[i].y);
-        else mma16(ones, kOnes, kOnes, kOnes, kOnes, x[i].x, x[i].y);
-        mma16(ones, kOnes, kOnes, kOnes, kOnes, x[i].z, x[i].w);
+      const uint32_t l = s ? lead.y : lead.x;
+      w[0] = l << up;
+      w[1] = l >> (8 - up);
+      if constexpr (third) {                      // the third bit stands above the two: at 2j + 2
+        w[2] = moved_by(h1, 8 * s - 2);
+        w[3] = moved_by(h1, 8 * s - 1);
+      } else if constexpr (up == 1) {
+        w[2] = moved_by(h1, 8 * s);
+        w[3] = moved_by(h1, 8 * s + 1);
+      } else if constexpr (up == 2) {
+        w[2] = and_or(moved_by(h1, 8 * s - 1), 0x00aa00aau, (h0 >> (8 * s)) & 0x00550055u);
+        w[3] = and_or(moved_by(h1, 8 * s), 0x00aa00aau, (h0 >> (8 * s + 1)) & 0x00550055u);
       }
-      sum0 = ones[0];
-      sum1 = ones[1];
     }
   }
-  Scales m;
-  if constexpr (F != kFmt16) load_scales(slot, (int)g, m);
+  __device__ __forceinline__ uint32_t pair(int j, int p) const {
+    if constexpr (F == kFmt8) {
+      return __byte_perm(w[2 * p + (j >> 1)], 0, j & 1 ? 0x4342 : 0x4140);
+    } else if constexpr (F == kFmt4) {
+      return ((j & 2) ? w[p] >> 8 : w[p]) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
+    } else {
+      constexpr uint32_t one = 0x00010001u;
+      uint32_t v = w[p] & ((3u << (2 * j + up)) * one);
+      if constexpr (third || up) v = and_or(w[2 + p], (third ? 4u << (2 * j) : up == 2 ? 3u << (2 * j) : 1u << (2 * j)) * one, v);
+      return v;
+    }
+  }
+};
+
+// One step in format F out of a slot.  x: this lane's operand row, with the step's pieces at (at0 ^ i) * 16 bytes.  STAGED:
+// the operands' sums are at at_sum0 and at_sum1, else they are made here, by a row of ones on the same fragments.
+template <int F, bool STAGED>
+__device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int lane, uint32_t xrow, uint32_t at0, uint32_t at_sum0, uint32_t at_sum1,
+                                              float (&tot)[2][4]) {
+  const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3;
   if constexpr (F == kFmt16) {
     // columns of the lane: pairs 2b, 2b + 1 (b = t mod 2) of both halves of stretch t / 2
-    const char* half = slot + 1024 * (t >> 1) + 8 * (t & 1);
+    const uint32_t at = slot + 1024 * (t >> 1) + 8 * (t & 1);
+    const uint4 x = lds16(xrow + (at0 << 4));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint32_t r = 4 * g + 2 * h, u = 2 * (t >> 1);
-      const uint2 a0 = *reinterpret_cast<const uint2*>(half + 16 * (r ^ u)), b0 = *reinterpret_cast<const uint2*>(half + 16 * ((r + 1) ^ u));
-      const uint2 a1 = *reinterpret_cast<const uint2*>(half + 512 + 16 * (r ^ (u + 1))), b1 = *reinterpret_cast<const uint2*>(half + 512 + 16 * ((r + 1) ^ (u + 1)));
-      mma16(tot[h], a0.x, b0.x, a1.x, b1.x, x[0].x, x[0].y);
-      mma16(tot[h], a0.y, b0.y, a1.y, b1.y, x[0].z, x[0].w);
-    }
-  } else if constexpr (F == kFmt8 || F == kFmt4) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint4 a = *reinterpret_cast<const uint4*>(slot + 512 * t + 16 * ((4 * g + 2 * h) ^ t));
-      const uint4 b = *reinterpret_cast<const uint4*>(slot + 512 * t + 16 * ((4 * g + 2 * h + 1) ^ t));
-      if constexpr (F == kFmt8) {                  // a stretch: words 0, 1 its first eight columns, 2, 3 the others
-        float acc[4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t a0 = word_of(a, i), a1 = word_of(a, i + 2), b0 = word_of(b, i), b1 = word_of(b, i + 2);
-          if (i == 0)
-            mma16_first(acc, __byte_perm(a0, 0, 0x4140), __byte_perm(b0, 0, 0x4140), __byte_perm(a1, 0, 0x4140), __byte_perm(b1, 0, 0x4140), x[i].x, x[i].y);
-          else mma16(acc, __byte_perm(a0, 0, 0x4140), __byte_perm(b0, 0, 0x4140), __byte_perm(a1, 0, 0x4140), __byte_perm(b1, 0, 0x4140), x[i].x, x[i].y);
-          mma16(acc, __byte_perm(a0, 0, 0x4342), __byte_perm(b0, 0, 0x4342), __byte_perm(a1, 0, 0x4342), __byte_perm(b1, 0, 0x4342), x[i].z, x[i].w);
-        }
-        apply_scales(m, h, acc, sum0, sum1, tot[h]);
-      } else {                                     // two stretches: words 2s and 2s + 1, a word eight columns
-        float acc[2][4];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const uint32_t a0 = word_of(a, 2 * s), a1 = word_of(a, 2 * s + 1), b0 = word_of(b, 2 * s), b1 = word_of(b, 2 * s + 1);
-          const uint32_t c0 = a0 >> 8, c1 = a1 >> 8, d0 = b0 >> 8, d1 = b1 >> 8;
-          constexpr uint32_t lo = 0x000f000fu, hi = 0x00f000f0u;
-          if (s == 0) {
-            mma16_first(acc[0], a0 & lo, b0 & lo, a1 & lo, b1 & lo, x[0].x, x[0].y);
-            mma16_first(acc[1], a0 & hi, b0 & hi, a1 & hi, b1 & hi, x[0].z, x[0].w);
-          } else {
-            mma16(acc[0], a0 & lo, b0 & lo, a1 & lo, b1 & lo, x[2].x, x[2].y);
-            mma16(acc[1], a0 & hi, b0 & hi, a1 & hi, b1 & hi, x[2].z, x[2].w);
-          }
-          mma16(acc[0], c0 & lo, d0 & lo, c1 & lo, d1 & lo, x[2 * s + 1].x, x[2 * s + 1].y);
-          mma16(acc[1], c0 & hi, d0 & hi, c1 & hi, d1 & hi, x[2 * s + 1].z, x[2 * s + 1].w);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[0][j] = fmaf(acc[1][j], 0.0625f, acc[0][j]);
-        apply_scales(m, h, acc[0], sum0, sum1, tot[h]);
-      }
+      const uint2 a0 = lds8(at + 16 * (r ^ u)), b0 = lds8(at + 16 * ((r + 1) ^ u));
+      const uint2 a1 = lds8(at + 16 * (r ^ (u + 1)) + 512), b1 = lds8(at + 16 * ((r + 1) ^ (u + 1)) + 512);
+      mma16(tot[h], a0.x, b0.x, a1.x, b1.x, x.x, x.y);
+      mma16(tot[h], a0.y, b0.y, a1.y, b1.y, x.z, x.w);
     }
   } else {
-    // Two leading bits in the 2-bit arrangement, further bits in words of their own.  `up`: how many bits stand below
-    // the leading two; the code of pair j of a word is put together with its last bit at 2 (j mod 4).
-    constexpr int up = F == kFmtP4 ? 2 : F == kFmtP3 ? 1 : 0;
-    constexpr bool third = F == kFmt3;
+    using C = Codes<F>;
+    constexpr int S = F == kFmt8 ? 1 : 2;         // stretches of a lane
+    uint4 x[2 * S];
+#pragma unroll
+    for (int i = 0; i < 2 * S; ++i) x[i] = lds16(xrow + ((at0 ^ i) << 4));
+    float sum0, sum1;
+    if constexpr (STAGED) {
+      sum0 = __uint_as_float(lds4(at_sum0)), sum1 = __uint_as_float(lds4(at_sum1));
+    } else {
+      float ones[4];
+#pragma unroll
+      for (int i = 0; i < 2 * S; ++i) {
+        if (i == 0) mma16_first(k, ones, kOnes, kOnes, kOnes, kOnes, x[i].x, x[i].y);
+        else mma16(ones, kOnes, kOnes, kOnes, kOnes, x[i].x, x[i].y);
+        mma16(ones, kOnes, kOnes, kOnes, kOnes, x[i].z, x[i].w);
+      }
+      sum0 = ones[0], sum1 = ones[1];
+    }
+    Scales m;
+    load_scales(slot, g, m);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      uint32_t lead[2][2], h1[2] = {0, 0}, h0[2] = {0, 0};       // [row][stretch], [row]
+      uint4 wide[2];
+      uint2 lead[2];
+      uint32_t h1[2], h0[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const uint32_t row = 4 * g + 2 * h + r;
-        const uint2 w = *reinterpret_cast<const uint2*>(slot + code_at<F>(t >> 1, row) + 8 * (t & 1));
-        lead[r][0] = w.x;
-        lead[r][1] = w.y;
-        if constexpr (third || up) h1[r] = *reinterpret_cast<const uint32_t*>(slot + code_at<F>(2, row) + 4 * t);
-        if constexpr (up == 2) h0[r] = *reinterpret_cast<const uint32_t*>(slot + code_at<F>(3, row) + 4 * t);
+        wide[r] = make_uint4(0, 0, 0, 0), lead[r] = make_uint2(0, 0), h1[r] = h0[r] = 0;
+        if constexpr (F <= kFmt4) wide[r] = lds16(slot + code_at<F>(t, row));
+        else lead[r] = lds8(slot + code_at<F>(t >> 1, row) + 8 * (t & 1));
+        if constexpr (C::third || C::up) h1[r] = lds4(slot + code_at<F>(2, row) + 4 * t);
+        if constexpr (C::up == 2) h0[r] = lds4(slot + code_at<F>(3, row) + 4 * t);
       }
-      float acc[4][4];
+      float acc[C::sets][4];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {                // stretch s: a word of sixteen codes
-        uint32_t top[2][2], low[2][2];             // [row][pairs 0 .. 3 / 4 .. 7]
+      for (int s = 0; s < S; ++s) {
+        C c[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          top[r][0] = lead[r][s] << up;
-          top[r][1] = lead[r][s] >> (8 - up);
-          if constexpr (third) {                   // the third bit stands above the two: at 2 (j mod 4) + 2
-            low[r][0] = moved_by(h1[r], 8 * s - 2);
-            low[r][1] = moved_by(h1[r], 8 * s - 1);
-          } else if constexpr (up == 1) {
-            low[r][0] = moved_by(h1[r], 8 * s);
-            low[r][1] = moved_by(h1[r], 8 * s + 1);
-          } else if constexpr (up == 2) {
-            low[r][0] = and_or(moved_by(h1[r], 8 * s - 1), 0x00aa00aau, (h0[r] >> (8 * s)) & 0x00550055u);
-            low[r][1] = and_or(moved_by(h1[r], 8 * s), 0x00aa00aau, (h0[r] >> (8 * s + 1)) & 0x00550055u);
-          }
-        }
+        for (int r = 0; r < 2; ++r) c[r].take(wide[r], lead[r], h1[r], h0[r], s);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          uint32_t v[2][2];
-          const uint32_t top_mask = (3u << (2 * j + up)) * 0x00010001u;
-          const uint32_t low_mask = (third ? 4u << (2 * j) : up == 2 ? 3u << (2 * j) : 1u << (2 * j)) * 0x00010001u;
-#pragma unroll
-          for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-              v[r][p] = top[r][p] & top_mask;
-              if constexpr (third || up) v[r][p] = and_or(low[r][p], low_mask, v[r][p]);
-            }
           const uint4& xs = x[2 * s + (j >> 1)];
           const uint32_t b0 = j & 1 ? xs.z : xs.x, b1 = j & 1 ? xs.w : xs.y;
-          if (s == 0) mma16_first(acc[j], v[0][0], v[1][0], v[0][1], v[1][1], b0, b1);
-          else mma16(acc[j], v[0][0], v[1][0], v[0][1], v[1][1], b0, b1);
+          if (s == 0 && j < C::sets) mma16_first(k, acc[C::set(j)], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
+          else mma16(acc[C::set(j)], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
         }
       }
+      if constexpr (C::sets == 2) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[0][j] = fmaf(acc[1][j], 0.25f, acc[0][j]);
-        acc[2][j] = fmaf(acc[3][j], 0.25f, acc[2][j]);
-        acc[0][j] = fmaf(acc[2][j], 0.0625f, acc[0][j]);
+        for (int i = 0; i < 4; ++i) acc[0][i] = fmaf(acc[1][i], 0.0625f, acc[0][i]);
+      } else if constexpr (C::sets == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[0][i] = fmaf(acc[1][i], 0.25f, acc[0][i]);
+          acc[2][i] = fmaf(acc[3][i], 0.25f, acc[2][i]);
+          acc[0][i] = fmaf(acc[2][i], 0.0625f, acc[0][i]);
+        }
       }
       apply_scales(m, h, acc[0], sum0, sum1, tot[h]);
     }
@@ -417,61 +425,93 @@ __device__ __forceinline__ void multiply_step(const char* slot, int lane, const 
 
 // ---- a warp's walk over its steps ----------------------------------------------------------------
 struct Ring {
-  const char* base;
-  uint32_t base_s, slot;                          // slot: offset of the next step's
+  uint32_t base, slot;                            // shared memory: the warp's slots, the next step's
   int lane;
 };
 template <int XC, int STAGES>
 __device__ __forceinline__ void ring_on(Ring& r) {
   cp_commit();
-  r.slot = r.slot == (STAGES - 1) * kSlotOf<XC> ? 0 : r.slot + kSlotOf<XC>;
+  r.slot = r.slot == r.base + (STAGES - 1) * kSlotOf<XC> ? r.base : r.slot + kSlotOf<XC>;
 }
 // Multiplies steps of a block in format F, at most n, and asks for the next step of the feed after each while that is in
 // the same format.  Returns with n = 0, or having multiplied a step without having asked (true).
 template <int F, int XC, int STAGES>
-__device__ __forceinline__ bool walk_format(int& n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4]) {
+__device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4]) {
   constexpr int ls = step_shift(F);
   const uint32_t t = (uint32_t)r.lane & 3;
   // The lane's pieces of a step: e = 4t + i, 8q + 2t + i or 4q + t, q the step inside its group, in the order of piece_at:
   // at0 ^ (what q adds) ^ i.  A streamed row is the part of its step.
   const uint32_t at0 = ls == 0 ? (5 * t) ^ o.flip : ls == 1 ? (2 * t) ^ (t >> 1) ^ o.flip : XC ? t : t ^ o.flip;
+  const uint32_t x_group = (uint32_t)o.room * 256, sum_part = (uint32_t)o.room * 4, sum_group = 3 * sum_part;
+  uint32_t x = o.x, sum0 = o.sum0, sum1 = o.sum1;
+  if constexpr (XC == 0) {
+    const uint32_t grp = (uint32_t)o.step >> ls;
+    x += grp * x_group;
+    sum0 += grp * sum_group;
+    sum1 += grp * sum_group;
+  }
+  int asks = f.fmt == F ? min(n, f.left) : 0;
+  f.left -= asks;
+  bool due = false;
 #pragma unroll 1
   do {
     cp_wait<STAGES - 1>();
     __syncwarp();                                 // what the other lanes have copied
-    const uint32_t q = (uint32_t)o.step & ((1 << ls) - 1);
-    const int grp = o.step >> ls;
-    if constexpr (XC == 0)
-      multiply_step<F, true>(r.base + r.slot, r.lane, o.x + (size_t)grp * o.rows * 256, at0 ^ (ls == 1 ? 10 * q : ls == 2 ? 5 * q : 0),
-                             o.sum + (grp * 2 + (ls == 1 ? q : 0)) * o.rows, o.sum_next, o.rows, tot);
-    else multiply_step<F, false>(r.base + r.slot, r.lane, o.x + r.slot, at0 ^ (ls == 1 ? 2 * q : ls == 2 ? q : 0), nullptr, 0, 0, tot);
+    const uint32_t q = ls ? (uint32_t)o.step & ((1 << ls) - 1) : 0;
+    if constexpr (XC == 0) {
+      const uint32_t part = ls == 1 ? q * sum_part : 2 * sum_part;
+      multiply_step<F, true>(k, r.slot, r.lane, x, at0 ^ (ls == 1 ? 10 * q : ls == 2 ? 5 * q : 0), sum0 + part, sum1 + part, tot);
+      if (ls == 0 || q == (1 << ls) - 1) {
+        x += x_group;
+        sum0 += sum_group;
+        sum1 += sum_group;
+      }
+    } else {
+      multiply_step<F, false>(k, r.slot, r.lane, x + (r.slot - r.base), at0 ^ (ls == 1 ? 2 * q : ls == 2 ? q : 0), 0, 0, tot);
+    }
     o.step++;
     __syncwarp();                                 // every lane has read the slot
     --n;
-    if (f.fmt != F || f.left == 0) return true;
-    f.left--;
-    ask<F, XC, true, true>(f, r.base_s + r.slot, r.lane);
+    due = asks == 0;
+    if (due) break;
+    --asks;
+    ask<F, XC, true, true>(f, r.slot, r.lane);
     ring_on<XC, STAGES>(r);
   } while (n);
-  return false;
+  return due;
 }
-// The next n steps, all of one block in format `fmt`.  more(): sets the feed up for the next block; false: there is none.
-template <int XC, int STAGES, class More>
-__device__ __forceinline__ void walk(int fmt, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], More more) {
+// The next n steps, all of one block in format `fmt` (F, if that is not kAnyFormat: all blocks are).  more(): sets the feed
+// up for the next block; false: there is none.
+constexpr int kAnyFormat = -1;
+template <int F, int XC, bool CODES, bool OPERAND>
+__device__ __forceinline__ void ask_for(Feed& f, uint32_t slot, int lane) {
+  if constexpr (F == kAnyFormat) {
+    ask_any<XC, CODES, OPERAND>(f, slot, lane);
+  } else {
+    f.left--;
+    ask<F, XC, CODES, OPERAND>(f, slot, lane);
+  }
+}
+template <int F, int XC, int STAGES, class More>
+__device__ __forceinline__ void walk(const Fixed& k, int fmt, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], More more) {
   while (n) {
     bool due;
-    switch (fmt) {
-      case kFmt16: due = walk_format<kFmt16, XC, STAGES>(n, f, r, o, tot); break;
-      case kFmt8: due = walk_format<kFmt8, XC, STAGES>(n, f, r, o, tot); break;
-      case kFmt4: due = walk_format<kFmt4, XC, STAGES>(n, f, r, o, tot); break;
-      case kFmt3: due = walk_format<kFmt3, XC, STAGES>(n, f, r, o, tot); break;
-      case kFmtP4: due = walk_format<kFmtP4, XC, STAGES>(n, f, r, o, tot); break;
-      case kFmtP3: due = walk_format<kFmtP3, XC, STAGES>(n, f, r, o, tot); break;
-      case kFmt2: due = walk_format<kFmt2, XC, STAGES>(n, f, r, o, tot); break;
-      default: due = walk_format<kFmtP2, XC, STAGES>(n, f, r, o, tot); break;
+    if constexpr (F != kAnyFormat) {
+      due = walk_format<F, XC, STAGES>(k, n, f, r, o, tot);
+    } else {
+      switch (fmt) {
+        case kFmt16: due = walk_format<kFmt16, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt8: due = walk_format<kFmt8, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt4: due = walk_format<kFmt4, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt3: due = walk_format<kFmt3, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmtP4: due = walk_format<kFmtP4, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmtP3: due = walk_format<kFmtP3, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt2: due = walk_format<kFmt2, XC, STAGES>(k, n, f, r, o, tot); break;
+        default: due = walk_format<kFmtP2, XC, STAGES>(k, n, f, r, o, tot); break;
+      }
     }
     if (due) {
-      if (f.left || more()) ask_any<XC, true, true>(f, r.base_s + r.slot, r.lane);
+      if (f.left || more()) ask_for<F, XC, true, true>(f, r.slot, r.lane);
       ring_on<XC, STAGES>(r);
     }
   }

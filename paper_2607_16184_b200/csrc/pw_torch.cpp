@@ -234,6 +234,34 @@ PyObject* moe_forward_routed(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// layer, hidden, router_logits, top_k, out, H, E
+PyObject* moe_forward_few(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 10, [](Call& c, PyObject* const* a) -> int {
+    const int layer = c.integer(a[0], 1);
+    const Matrix h = matrix(c, a[1], 2, PW_F16, -1, PyLong_AsLongLong(a[5]), true);
+    const Matrix l = matrix(c, a[2], 3, PW_F32, h.rows, PyLong_AsLongLong(a[6]), true);
+    const int k = c.integer(a[3], 4);
+    const Matrix out = matrix(c, a[4], 5, -1, h.rows, h.cols, true);
+    if (c.bad) return c.bad;
+    Outside outside(c);
+    return pw_moe_forward_few(c.ctx, layer, h.data, static_cast<float*>(l.data), (int)h.rows, k, nullptr, out.data, out.type, c.stream);
+  });
+}
+
+// layer, hidden, topk_ids, gates, out, H
+PyObject* moe_forward_few_routed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 9, [](Call& c, PyObject* const* a) -> int {
+    const int layer = c.integer(a[0], 1);
+    const Matrix h = matrix(c, a[1], 2, PW_F16, -1, PyLong_AsLongLong(a[5]), true);
+    const Matrix ids = matrix(c, a[2], 3, kWords, h.rows, -1, true), gates = matrix(c, a[3], 4, PW_F32, h.rows, ids.cols, true);
+    const Matrix out = matrix(c, a[4], 5, -1, h.rows, h.cols, true);
+    if (c.bad) return c.bad;
+    Outside outside(c);
+    return pw_moe_forward_few_routed(c.ctx, layer, h.data, static_cast<int32_t*>(ids.data), static_cast<float*>(gates.data), (int)h.rows, (int)ids.cols,
+                                     nullptr, out.data, out.type, c.stream);
+  });
+}
+
 // A Python reference that is given back.
 struct Ref {
   PyObject* o;
@@ -297,7 +325,7 @@ PyObject* page_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define PW_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PW_METHOD(quantize_scaled), PW_METHOD(add_rmsnorm), PW_METHOD(scaled_linear), PW_METHOD(route_tokens),
-                         PW_METHOD(moe_forward_routed), PW_METHOD(page_linear), {nullptr, nullptr, 0, nullptr}};
+                         PW_METHOD(moe_forward_routed), PW_METHOD(page_linear), PW_METHOD(moe_forward_few), PW_METHOD(moe_forward_few_routed), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pwtorch", "Argument marshalling for torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
