@@ -51,6 +51,7 @@ struct LinearUnit {
 __device__ __forceinline__ LinearUnit linear_unit(const PageLinearArgs& a, int u) {
   LinearUnit un{0, u};
   if (a.pages > 1) {
+#pragma unroll 1
     while (u >= a.page[un.page].end) ++un.page;
     if (un.page) un.slice -= a.page[un.page - 1].end;
   }
@@ -72,7 +73,7 @@ __device__ __forceinline__ void put_linear(const PageLinearArgs& a, const Linear
 // spends a large part of its time on fetching code.
 template <int F, int STAGES>
 __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __grid_constant__ PageLinearArgs a) {
-  constexpr int kRing = STAGES * kSlotOf<0>;
+  constexpr int kRing = STAGES * slot_bytes(0);
   extern __shared__ __align__(128) char smem[];
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int ts = a.team_shift, team = warp >> ts, member = warp & ((1 << ts) - 1);
@@ -90,11 +91,12 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 
   const Fixed fixed;
   const uint32_t ring = smem_u32(smem) + warp * kRing;
-  Ring r{ring, ring, lane};
+  Ring r{ring, ring, (uint32_t)slot_bytes(0), lane};
   Feed f;
   f.left = 0;
   int next = 0;                                   // slice the feed takes next
   auto more = [&]() -> bool {
+#pragma unroll 1
     while (next < a.slices) {
       const LinearUnit un = linear_unit(a, next);
       const LinearPage& p = a.page[un.page];
@@ -106,18 +108,27 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     }
     return false;
   };
+  auto ask_next = [&](uint32_t slot) {
+    if (f.left == 0 && !more()) return;
+    if constexpr (F == kAnyFormat) {
+      ask_any<false>(f, slot, lane);
+    } else {
+      f.left--;
+      ask<F, false>(f, slot, lane);
+    }
+  };
 
   bool waited = false, exchanged = false;
 #pragma unroll 1
   for (int pass = cluster % a.passes; pass < a.passes; pass += clusters) {
     // pages are final when this kernel is placed, the operand may be written by the kernel ahead: codes first
     next = first + sharing * team;
+    r.slot = r.base;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
-      if (f.left || more()) ask_for<F, 0, true, false>(f, r.base + i * kSlotOf<0>, lane);
-      cp_commit();
+      ask_next(r.slot);
+      ring_on<STAGES>(r);
     }
-    r.slot = r.base;
     if (!waited) {
       grid_dep_sync();
       grid_dep_trigger();
@@ -135,6 +146,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 #pragma unroll 1
     for (int u0 = first; u0 < a.slices; u0 += stride * batch) {
       if (a.split > 1 && exchanged) cluster_sync();   // the parts of the batch before have been read
+#pragma unroll 1
       for (int j = 0; j < batch; ++j) {
         const int u = u0 + sharing * team + stride * j;
         if (u >= a.slices) break;
@@ -143,9 +155,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
         const int steps = my_groups << step_shift(fmt), lo = (steps * member) >> ts;
         float tot[2][4] = {};
         Operand o{x_lane, sum0, sum1, a.room, (uint32_t)(xc & 1) << 2, lo};
-        walk<F, 0, STAGES>(fixed, fmt, ((steps * (member + 1)) >> ts) - lo, f, r, o, tot, more);
+        walk<F, false, STAGES>(fixed, fmt, 0, ((steps * (member + 1)) >> ts) - lo, f, r, o, tot, ask_next);
         put_sums(sums + member * kSumFloats, lane, tot);
         team_sync(team, ts);
+#pragma unroll 1
         for (int i = member * 32 + lane; i < kUnitRows * cols; i += 32 << ts) {
           const int row = i & (kUnitRows - 1), col = i >> 5;
           float v = 0.f;
@@ -160,12 +173,15 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
       if (a.split > 1) {
         cluster_sync();
         exchanged = true;
+#pragma unroll 1
         for (int s = rank; s < slots; s += a.split) {
           const int u = u0 + sharing * (s / batch) + stride * (s % batch);
           if (u >= a.slices) continue;
           const LinearUnit un = linear_unit(a, u);
+#pragma unroll 1
           for (int i = threadIdx.x; i < kUnitRows * cols; i += kStreamThreads) {
             float v = 0.f;
+#pragma unroll 1
             for (int k = 0; k < a.split; ++k) v = __fadd_rn(v, parts[((k * slots + s) / a.split * kUnitCols) * kUnitRows + i]);
             put_linear(a, un, token0 + (i >> 5), i & (kUnitRows - 1), v);
           }
@@ -176,7 +192,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 }
 
 static size_t page_linear_smem(const PageLinearArgs& a, int stages) {
-  return (size_t)kStreamWarps * stages * kSlotOf<0> + kSumsBytes + (a.split > 1 ? kPartsBytes : 0) +
+  return (size_t)kStreamWarps * stages * slot_bytes(0) + kSumsBytes + (a.split > 1 ? kPartsBytes : 0) +
          (((size_t)a.split_groups * 3 * a.room * 4 + 127) & ~(size_t)127) + (size_t)a.split_groups * a.room * 256;
 }
 typedef void (*PageLinearKernel)(PageLinearArgs);

@@ -17,6 +17,9 @@
 namespace pw {
 
 constexpr int kFewParts = 8;                      // most parts of the down blocks' columns
+constexpr int kFewRouters = 4;                    // warps that route
+constexpr size_t kFewAhead = 16 << 20;            // bytes of shared experts that are asked for while the tokens are routed (2.5 us)
+constexpr int kFewAheadSteps = 8;                 // steps of phase 2 that a warp asks the L2 cache for before all CTAs meet
 constexpr uint32_t kFewPolls = 1u << 22;          // about 3 s
 
 struct FewArgs {
@@ -28,12 +31,14 @@ struct FewArgs {
   void* out;
   char* h;                                        // [pair][F] pieces
   float* parts;                                   // [part][T][H]
-  int32_t* sync;                                  // arrivals, generation; from 64 on: finished parts of every 32 output rows
+  int32_t* sync;                                  // arrivals; from 64 on: finished parts of every 32 output rows
   int32_t* status;
   int32_t* seen;                                  // for the observation taps (or null): see few_observe_kernel
   int T, k, E, n_shared, H, F, out_type;
-  int segs, pairs, n_parts;                       // room for active experts and for their (expert, token) pairs
-  int table_bytes, ring_bytes;
+  int segs, pairs;                                // room for active experts and for their (expert, token) pairs
+  int n_parts;                                    // parts of the down blocks' columns
+  uint32_t per_part;                              // 2^32 / n_parts, rounded up
+  int slot2;                                      // bytes of a slot of phase 2
 };
 
 // Tables in shared memory, built once per call.
@@ -42,47 +47,32 @@ struct SegPage {
   const char* bit1;
   const char* bit0;
 };
+// at fixed places, so that a look into one is one instruction.  Two sizes: a few tokens of most layers, and every call.
+template <int SEGS, int PAIRS, int CHOICES>
 struct FewTables {
-  SegPage* page;                                  // [segs][3]
-  float* gate;                                    // [pairs]
-  float* own_gates;                               // [T * k]
-  int32_t* own_ids;                               // [T * k]
-  uint32_t* mask;                                 // [E] tokens of an expert
-  int32_t* unit0;                                 // [segs + 1] first unit of phase 1, by rank
-  int32_t* step0;                                 // [segs + 1] first step of phase 2, of the segment's first pass
-  int32_t* count;                                 // active segments, pairs
-  uint16_t* seg;                                  // [segs] expert, ascending
-  uint16_t* off;                                  // [segs + 1] first pair
-  uint16_t* order;                                // [segs] by weight of a unit of phase 1, heaviest first
-  uint8_t* fmt;                                   // [segs][4]
-  uint8_t* token;                                 // [pairs]
+  static constexpr int kSegs = SEGS, kPairs = PAIRS, kChoices = CHOICES;
+  SegPage page[SEGS * 3];
+  float gate[PAIRS];
+  float own_gates[CHOICES];                       // [T * k]
+  int32_t own_ids[CHOICES];
+  uint32_t mask[256];                             // tokens of an expert
+  int32_t unit0[SEGS + 1];                        // first unit of phase 1, by rank
+  int32_t step0[SEGS + 1];                        // first step of phase 2, of the segment's first pass
+  int32_t weight[SEGS];                           // bytes of a tile of the gate and the up block
+  int32_t count[2];                               // active segments, pairs
+  uint16_t seg[SEGS];                             // expert, ascending
+  uint16_t off[SEGS + 1];                         // first pair
+  uint16_t order[SEGS];                           // shared experts first, then by weight, heaviest first
+  uint8_t fmt[SEGS * 4];
+  uint8_t token[PAIRS];
 };
-__host__ __device__ inline size_t few_tables(FewTables* t, char* base, int segs, int pairs, int Tk, int E) {
-  size_t o = 0;
-  auto take = [&](size_t bytes) {
-    char* at = base + o;
-    o += (bytes + 15) & ~(size_t)15;
-    return at;
-  };
-  FewTables v;
-  v.page = reinterpret_cast<SegPage*>(take(sizeof(SegPage) * 3 * segs));
-  v.gate = reinterpret_cast<float*>(take(4 * (size_t)pairs));
-  v.own_gates = reinterpret_cast<float*>(take(4 * (size_t)Tk));
-  v.own_ids = reinterpret_cast<int32_t*>(take(4 * (size_t)Tk));
-  v.mask = reinterpret_cast<uint32_t*>(take(4 * (size_t)E));
-  v.unit0 = reinterpret_cast<int32_t*>(take(4 * (size_t)(segs + 1)));
-  v.step0 = reinterpret_cast<int32_t*>(take(4 * (size_t)(segs + 1)));
-  v.count = reinterpret_cast<int32_t*>(take(16));
-  v.seg = reinterpret_cast<uint16_t*>(take(2 * (size_t)segs));
-  v.off = reinterpret_cast<uint16_t*>(take(2 * (size_t)(segs + 1)));
-  v.order = reinterpret_cast<uint16_t*>(take(2 * (size_t)segs));
-  v.fmt = reinterpret_cast<uint8_t*>(take(4 * (size_t)segs));
-  v.token = reinterpret_cast<uint8_t*>(take((size_t)pairs));
-  if (t) *t = v;
-  return (o + 127) & ~(size_t)127;
-}
+typedef FewTables<48, 96, 64> FewSmall;
+typedef FewTables<256 + 16, PW_FEW_TOKENS * (32 + 16), PW_FEW_TOKENS * 32> FewAll;
+template <class TAB>
+constexpr int kTableBytes = (int)((sizeof(TAB) + 127) & ~(size_t)127);
 
-__device__ __forceinline__ int passes_of(const FewTables& t, int a) { return (t.off[a + 1] - t.off[a] + kUnitCols - 1) / kUnitCols; }
+template <class TAB>
+__device__ __forceinline__ int passes_of(const TAB& t, int a) { return (t.off[a + 1] - t.off[a] + kUnitCols - 1) / kUnitCols; }
 
 // Teams of a CTA that has m units to do (at most four at a time): log2 of the warps of one.
 __device__ __forceinline__ int few_team_shift(int m) { return m == 1 ? 4 : m == 2 ? 3 : 2; }
@@ -96,23 +86,32 @@ struct GateUp {
   int a, pass, slice, kind, lo, n;                // segment, tokens, rows; the warp's block (PW_GATE, PW_UP) and steps
   int gates;                                      // warps of the team on the gate block
 };
-__device__ __forceinline__ GateUp gate_up_unit(const FewTables& t, int segs, int u, int groups, int ts, int member) {
-  int r = 0;
-  for (int half = 256; half; half >>= 1)
-    if (r + half < segs && t.unit0[r + half] <= u) r += half;
+__constant__ uint32_t kPerShare[17] = {0, 1u << 20, 524289, 349526, 262145, 209716, 174763, 149797, 131073, 116509, 104858, 95326, 87382, 80660, 74899, 69906, 65537};
+// How many of the n ascending numbers are at most v, by a warp.
+__device__ __forceinline__ int count_up_to(const int32_t* number, int n, int v, int lane) {
+  int c = 0;
+#pragma unroll 1
+  for (int base = 0; base < n; base += 32) c += __popc(__ballot_sync(0xffffffffu, base + lane < n && number[base + lane] <= v));
+  return c;
+}
+template <class TAB>
+__device__ __forceinline__ GateUp gate_up_unit(const TAB& t, int segs, int u, int groups, int ts, int member, int lane) {
+  const int r = count_up_to(t.unit0 + 1, segs, u, lane);
   GateUp g;
   g.a = t.order[r];
   const int local = u - t.unit0[r], passes = passes_of(t, g.a);
-  g.slice = passes == 1 ? local : local / passes;
-  g.pass = local - g.slice * passes;
+  g.slice = passes == 1 ? local : local >> 1;     // (at most two passes)
+  g.pass = passes == 1 ? 0 : local & 1;
   const int warps = 1 << ts, sg = step_shift(t.fmt[4 * g.a + PW_GATE]), su = step_shift(t.fmt[4 * g.a + PW_UP]);
   // warps in proportion to the steps of the two blocks, one at least
-  g.gates = max(1, min(warps - 1, (2 * (warps << sg) + (1 << sg) + (1 << su)) / (2 * ((1 << sg) + (1 << su)))));
+  const int both = (1 << sg) + (1 << su);
+  g.gates = max(1, min(warps - 1, (int)((((warps << sg) + (both >> 1)) * kPerShare[both]) >> 20)));
   g.kind = member < g.gates ? PW_GATE : PW_UP;
   const int mine = member < g.gates ? member : member - g.gates, share = member < g.gates ? g.gates : warps - g.gates;
-  const int steps = groups << (member < g.gates ? sg : su);
-  g.lo = steps * mine / share;
-  g.n = steps * (mine + 1) / share - g.lo;
+  const uint32_t steps = (uint32_t)groups << (member < g.gates ? sg : su);
+  // steps * mine / share, rounded down: the product is below 2^20 / share for every block a context may have
+  g.lo = (int)((uint64_t)(steps * mine) * kPerShare[share] >> 20);
+  g.n = (int)((uint64_t)(steps * (mine + 1)) * kPerShare[share] >> 20) - g.lo;
   return g;
 }
 
@@ -126,61 +125,38 @@ __device__ __forceinline__ uint32_t piece_offset(int f, int c) {
 struct DownRun {
   int a, pass, lo, n;
 };
-__device__ __forceinline__ bool down_run(const FewTables& t, int segs, int groups, int& at, int hi, int& hint, DownRun& d) {
+template <class TAB>
+__device__ __forceinline__ bool down_run(const TAB& t, int groups, int& at, int hi, int& hint, DownRun& d) {
   if (at >= hi) return false;
+#pragma unroll 1
   while (t.step0[hint + 1] <= at) ++hint;
   d.a = hint;
   const int per = groups << step_shift(t.fmt[4 * hint + PW_DOWN]), local = at - t.step0[hint];
-  d.pass = local / per;
+  d.pass = local >= per;                          // (at most two passes)
   d.lo = local - d.pass * per;
   d.n = min(per - d.lo, hi - at);
   at += d.n;
   return true;
 }
 
-template <int XC, int STAGES>
-__global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __grid_constant__ FewArgs p) {
-  extern __shared__ __align__(128) char smem[];
-  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  FewTables t;
-  few_tables(&t, smem, p.segs, p.pairs, p.T * p.k, p.E);
-  float* const sums = reinterpret_cast<float*>(smem + p.table_bytes);
-  const int hg = p.H / kGroup, fg = p.F / kGroup;
-
-  // ---- routing ----
-  // phase 1: sums [16 warps], rings, staged operand; phase 2: sums [16 warps][T tokens], rings
-  char* const ring1 = smem + p.table_bytes + kStreamWarps * kSumFloats * 4;
-  float* const xsum = reinterpret_cast<float*>(ring1 + kStreamWarps * STAGES * kSlotOf<0>);
-  char* const pieces = reinterpret_cast<char*>(xsum) + ((hg * 3 * p.T * 4 + 127) & ~127);
-  for (int e = tid; e < p.E; e += kStreamThreads) t.mask[e] = 0;
-  const int P0 = p.T * p.k;
-  if (p.logits) {
-    if (warp < p.T) route_token(p.logits, warp, p.E, p.k, t.own_ids, t.own_gates, lane);
-  } else {
-    for (int i = tid; i < P0; i += kStreamThreads) {
-      int id = p.ids[i];
-      if (id < -1 || id >= p.E) {
-        atomicMax(p.status, (int)PW_ERR_INVALID_ARG);
-        id = -1;
+// The tables of a call from its routing (own_ids, own_gates), by the first kFewRouters warps; t.mask is all zeros.
+__device__ __forceinline__ void routers_sync() { asm volatile("bar.sync 8, %0;" ::"n"(32 * kFewRouters) : "memory"); }
+template <class TAB>
+__device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, int fg, int warp, int lane) {
+  if (warp == 0) {
+#pragma unroll 1
+    for (int tok = 0; tok < p.T; ++tok)
+      if (lane < p.k) {
+        const int e = t.own_ids[tok * p.k + lane];
+        if (e >= 0) atomicOr(&t.mask[e], 1u << tok);
       }
-      t.own_ids[i] = id;
-      t.own_gates[i] = p.gates[i];
-    }
-  }
-  {
-    const int idle = p.logits && p.T <= 8 ? p.T : 0;   // the warps that route leave the staging to the others
-    if (warp >= idle) stage_operand(p.hidden, (size_t)p.H * 2, p.T, p.T, 0, hg, p.H * 2, pieces, xsum, tid - 32 * idle, kStreamThreads - 32 * idle);
-  }
-  __syncthreads();
-  for (int i = tid; i < P0; i += kStreamThreads) {
-    const int e = t.own_ids[i];
-    if (e >= 0) atomicOr(&t.mask[e], 1u << (i / p.k));
-  }
-  __syncthreads();
-  if (warp == 0) {                                // experts with tokens, ascending, then the shared ones
-    int segs = 0, pairs = 0;
+    __syncwarp();
+    int segs = 0, pairs = 0;                      // experts with tokens, ascending, then the shared ones
+#pragma unroll 1
     for (int base = 0; base < p.E; base += 32) {
       const uint32_t m = base + lane < p.E ? t.mask[base + lane] : 0;
+      const uint32_t any = __ballot_sync(0xffffffffu, m != 0);
+      if (!any) continue;
       const int n = __popc(m);
       int incl = n;
 #pragma unroll
@@ -188,7 +164,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         const int y = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += y;
       }
-      const uint32_t any = __ballot_sync(0xffffffffu, n > 0);
       if (n) {
         const int i = segs + __popc(any & ((1u << lane) - 1));
         t.seg[i] = (uint16_t)(base + lane);
@@ -201,71 +176,139 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       t.seg[segs + lane] = (uint16_t)(p.E + lane);
       t.off[segs + lane] = (uint16_t)(pairs + lane * p.T);
     }
+    segs += p.n_shared;
+    pairs += p.n_shared * p.T;
     if (lane == 0) {
-      t.off[segs + p.n_shared] = (uint16_t)(pairs + p.n_shared * p.T);
-      t.count[0] = segs + p.n_shared;
-      t.count[1] = pairs + p.n_shared * p.T;
+      t.off[segs] = (uint16_t)pairs;
+      t.count[0] = segs;
+      t.count[1] = pairs;
     }
+  }
+  routers_sync();
+  const int segs = t.count[0], first = 32 * warp + lane;
+#pragma unroll 1
+  for (int a = first; a < segs; a += 32 * kFewRouters) {
+    const int e = t.seg[a];
+    DevRow row[3];
+#pragma unroll
+    for (int u = 0; u < 3; ++u) row[u] = p.rows[e * 3 + u];
+    // its tokens; an expert that a token names twice takes it once, with both gates
+    int at = t.off[a];
+#pragma unroll 1
+    for (uint32_t m = e < p.E ? t.mask[e] : (1u << p.T) - 1; m; m &= m - 1) {
+      const int tok = __ffs(m) - 1;
+      float g = 1.f;
+      if (e < p.E) {
+        g = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < p.k; ++j)
+          if (t.own_ids[tok * p.k + j] == e) g = __fadd_rn(g, t.own_gates[tok * p.k + j]);
+      }
+      t.token[at] = (uint8_t)tok;
+      t.gate[at++] = g;
+    }
+    int fmt[3];
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      fmt[u] = stream_format((int)row[u].bits, row[u].valid == 2);
+      t.page[3 * a + u] = SegPage{static_cast<const char*>(row[u].codes), static_cast<const char*>(row[u].bit1), static_cast<const char*>(row[u].bit0)};
+      t.fmt[4 * a + u] = (uint8_t)fmt[u];
+    }
+    t.weight[a] = (int)(kTileBytes[fmt[PW_GATE]] + kTileBytes[fmt[PW_UP]]) + (e < p.E ? 0 : 1 << 20);
+  }
+  routers_sync();
+#pragma unroll 1
+  for (int a = first; a < segs; a += 32 * kFewRouters) {
+    const int mine = t.weight[a];
+    int rank = 0;
+#pragma unroll 8
+    for (int o = 0; o < segs; ++o) rank += t.weight[o] > mine || (t.weight[o] == mine && o < a);
+    t.order[rank] = (uint16_t)a;
+  }
+  routers_sync();
+  if (warp > 1) return;
+  // first units of phase 1 by rank; first steps of phase 2
+  int32_t* const to = warp == 0 ? t.unit0 : t.step0;
+  int carry = 0;
+#pragma unroll 1
+  for (int base = 0; base < segs; base += 32) {
+    const int i = base + lane;
+    int n = 0;
+    if (i < segs) n = warp == 0 ? passes_of(t, t.order[i]) * (p.F / kUnitRows) : passes_of(t, i) * (fg << step_shift(t.fmt[4 * i + PW_DOWN]));
+    int incl = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += y;
+    }
+    if (i < segs) to[i] = carry + incl - n;
+    carry += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) to[segs] = carry;
+}
+
+// Both phases go through one loop: its code is by far the largest part of the kernel, and what a phase finds in the
+// instruction cache it does not wait for.
+template <class TAB, int STAGES>
+__global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __grid_constant__ FewArgs p) {
+  extern __shared__ __align__(128) char smem[];
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  TAB& t = *reinterpret_cast<TAB*>(smem);
+  float* const sums = reinterpret_cast<float*>(smem + kTableBytes<TAB>);
+  const int hg = p.H / kGroup, fg = p.F / kGroup;
+
+  // ---- routing ----
+  // phase 1: sums [16 warps], rings, staged operand; phase 2: sums [16 warps][T tokens], rings
+  char* const ring1 = smem + kTableBytes<TAB> + kStreamWarps * kSumFloats * 4;
+  char* const pieces = ring1 + kStreamWarps * STAGES * slot_bytes(0);
+  // a few warps route and make the tables; the others bring the tokens into shared memory and ask the L2 cache for the
+  // shared experts, which are wanted whatever the routing is
+  if (warp < kFewRouters) {
+    if (warp == 0)
+#pragma unroll 1
+      for (int e = lane; e < p.E; e += 32) t.mask[e] = 0;
+    if (p.logits) {
+#pragma unroll 1
+      for (int tok = warp; tok < p.T; tok += kFewRouters) {
+        if (p.E <= 64) route_token_n<2>(p.logits, tok, p.E, p.k, t.own_ids, t.own_gates, lane);
+        else route_token_n<kMaxExpertsPerLane>(p.logits, tok, p.E, p.k, t.own_ids, t.own_gates, lane);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = tid; i < p.T * p.k; i += 32 * kFewRouters) {
+        int id = p.ids[i];
+        if (id < -1 || id >= p.E) {
+          atomicMax(p.status, (int)PW_ERR_INVALID_ARG);
+          id = -1;
+        }
+        t.own_ids[i] = id;
+        t.own_gates[i] = p.gates[i];
+      }
+    }
+    routers_sync();
+    make_tables(p, t, fg, warp, lane);
+  } else {
+    const int thread = tid - 32 * kFewRouters, threads = kStreamThreads - 32 * kFewRouters;
+    const int line = (int)blockIdx.x * threads + thread, lines = (int)gridDim.x * threads;
+    const size_t page_lines = (size_t)p.F * p.H * 2 / 128;
+    int64_t left = kFewAhead / 128;
+#pragma unroll 1
+    for (int i = 0; i < p.n_shared * 2 && left > 0; ++i, left -= page_lines) {
+      const char* page = static_cast<const char*>(p.rows[(p.E + (i >> 1)) * 3 + (i & 1)].codes);
+#pragma unroll 1
+      for (size_t l = line; l < page_lines; l += lines) prefetch_line(page + l * 128);
+    }
+    stage_operand(p.hidden, (size_t)p.H * 2, p.T, p.T, 0, hg, p.H * 2, pieces, nullptr, thread, threads);
   }
   __syncthreads();
   const int segs = t.count[0];
-  for (int i = tid; i < segs * 3; i += kStreamThreads) {
-    const int a = i / 3, u = i - 3 * a;
-    const DevRow row = p.rows[t.seg[a] * 3 + u];
-    t.page[i] = SegPage{static_cast<const char*>(row.codes), static_cast<const char*>(row.bit1), static_cast<const char*>(row.bit0)};
-    t.fmt[4 * a + u] = (uint8_t)stream_format((int)row.bits, row.valid == 2);
-  }
-  for (int i = tid; i < segs * 16; i += kStreamThreads) {
-    const int a = i >> 4, tok = i & 15, e = t.seg[a];
-    if (e >= p.E) {
-      if (tok < p.T) {
-        t.token[t.off[a] + tok] = (uint8_t)tok;
-        t.gate[t.off[a] + tok] = 1.f;
-      }
-    } else if (t.mask[e] >> tok & 1) {            // an expert that a token names twice takes it once, with both gates
-      const int at = t.off[a] + __popc(t.mask[e] & ((1u << tok) - 1));
-      float g = 0.f;
-      for (int j = 0; j < p.k; ++j)
-        if (t.own_ids[tok * p.k + j] == e) g = __fadd_rn(g, t.own_gates[tok * p.k + j]);
-      t.token[at] = (uint8_t)tok;
-      t.gate[at] = g;
-    }
-  }
-  __syncthreads();
-  for (int a = tid; a < segs; a += kStreamThreads) {
-    auto weight = [&](int s) { return (int)stream_tile_bytes(t.fmt[4 * s + PW_GATE]) + (int)stream_tile_bytes(t.fmt[4 * s + PW_UP]); };
-    const int mine = weight(a);
-    int rank = 0;
-    for (int o = 0; o < segs; ++o) {
-      const int w = weight(o);
-      rank += w > mine || (w == mine && o < a);
-    }
-    t.order[rank] = (uint16_t)a;
-  }
-  __syncthreads();
-  if (warp < 2) {                                 // first units of phase 1 by rank; first steps of phase 2
-    int32_t* first = warp == 0 ? t.unit0 : t.step0;
-    int carry = 0;
-    for (int base = 0; base < segs; base += 32) {
-      const int i = base + lane, a = i < segs ? (warp == 0 ? t.order[i] : i) : 0;
-      const int n = i < segs ? passes_of(t, a) * (warp == 0 ? p.F / kUnitRows : fg << step_shift(t.fmt[4 * a + PW_DOWN])) : 0;
-      int incl = n;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += y;
-      }
-      if (i < segs) first[i] = carry + incl - n;
-      carry += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) first[segs] = carry;
-  }
-  __syncthreads();
   if (p.seen && blockIdx.x == 0) {                // what the taps' kernel wants to know
+#pragma unroll 1
     for (int a = tid; a <= segs; a += kStreamThreads) {
       if (a < segs) p.seen[2 + a] = t.seg[a];
       p.seen[2 + p.segs + a] = t.off[a];
     }
+#pragma unroll 1
     for (int i = tid; i < t.count[1]; i += kStreamThreads) {
       p.seen[3 + 2 * p.segs + i] = t.token[i];
       reinterpret_cast<float*>(p.seen)[3 + 2 * p.segs + p.pairs + i] = t.gate[i];
@@ -274,61 +317,200 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   }
 
   const Fixed fixed;
-  Feed f;
-  f.left = 0;
-  Ring r;
-  r.lane = lane;
+  const int G = (int)gridDim.x, b = (int)blockIdx.x;
+  uint32_t before;                                // arrivals, seen before this CTA's: only the top bit matters
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(before) : "l"(p.sync) : "memory");
+  const int steps = t.step0[segs];                // of phase 2, in a slice
+  bool down = false;                              // phase 2
+  // Units of a CTA.  Phase 1: units, heaviest first, are dealt out in turn, the turns in alternating order.  A CTA does four
+  // at a time, each by a team of warps.
+  int mine = t.unit0[segs] / G + ((t.unit0[segs] / G) & 1 ? G - 1 - b < t.unit0[segs] % G : b < t.unit0[segs] % G);
+  auto unit_of = [&](int i) { return i * G + (!down && (i & 1) ? G - 1 - b : b); };
+  auto slice_of = [&](int unit) { return p.n_parts == 1 ? unit : (int)__umulhi((uint32_t)unit, p.per_part); };   // unit / n_parts
+  auto range = [&](int unit, int ts, int member, int& lo, int& hi) {
+    // phase 2: steps * i / (n_parts << ts), rounded down (steps * i is below 2^24)
+    const uint32_t i = ((uint32_t)(unit - slice_of(unit) * p.n_parts) << ts) + member;
+    lo = slice_of((int)(steps * i >> ts));
+    hi = slice_of((int)(steps * (i + 1) >> ts));
+  };
 
-  // ---- phase 1: gate and up ----
-  {
-    const int G = (int)gridDim.x, b = (int)blockIdx.x;
-    const int units = t.unit0[segs];
-    // the units, heaviest first, are dealt out in turn, the turns in alternating order; four at a time, each to a team
-    const int mine = units / G + ((units / G) & 1 ? G - 1 - b < units % G : b < units % G);
-    auto unit_of = [&](int i) { return i * G + (i & 1 ? G - 1 - b : b); };
-    r.base = smem_u32(ring1) + warp * STAGES * kSlotOf<0>;
-    r.slot = r.base;
-    int next = 0;                                 // first of the four units that the feed looks at next
-    auto more = [&]() -> bool {
-      while (next < mine) {
-        const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts;
-        const int i = next + team;
-        next += m;
-        if (team >= m) continue;
-        const GateUp g = gate_up_unit(t, segs, unit_of(i), hg, ts, warp & ((1 << ts) - 1));
+  Ring r{0, 0, (uint32_t)slot_bytes(0), lane};
+  r.base = r.slot = smem_u32(ring1) + warp * STAGES * slot_bytes(0);
+  Feed f;
+  f.left = f.copies = 0;
+  // the feed's next four units; phase 2: its place in the list of steps, and its slice
+  int next = 0, at = 0, end = 0, hint = 0, slice = 0;
+  auto more = [&]() -> bool {
+#pragma unroll 1
+    for (;;) {
+      DownRun d;
+      if (down && down_run(t, fg, at, end, hint, d)) {
+        const SegPage& page = t.page[3 * d.a + PW_DOWN];
+        const int pair0 = t.off[d.a] + d.pass * kUnitCols;
+        feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * d.a + PW_DOWN], fg, slice, d.lo, d.lo + d.n);
+        feed_operand(f, lane, p.h + (size_t)pair0 * p.F * 2, (uint32_t)p.F * 2, min(kUnitCols, t.off[d.a + 1] - pair0), d.lo);
+        return true;
+      }
+      if (next >= mine) return false;
+      const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
+      const int unit = unit_of(next + team);
+      next += m;
+      if (team >= m) continue;
+      if (down) {
+        range(unit, ts, member, at, end);
+        hint = count_up_to(t.step0 + 1, segs, at, lane);
+        slice = slice_of(unit);
+      } else {
+        const GateUp g = gate_up_unit(t, segs, unit, hg, ts, member, lane);
         const SegPage& page = t.page[3 * g.a + g.kind];
         feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * g.a + g.kind], hg, g.slice, g.lo, g.lo + g.n);
         if (f.left) return true;
       }
-      return false;
-    };
-#pragma unroll 1
-    for (int i = 0; i < STAGES; ++i) {
-      if (f.left || more()) ask_any<0, true, false>(f, r.base + i * kSlotOf<0>, lane);
-      cp_commit();
     }
+  };
+  // The first steps of phase 2 are asked for without their operand, which is not there yet.  What a lane will copy of it
+  // waits in the lane's place of the slot.
+  bool without = false;
+  int asked = 0;
+  auto ask_next = [&](uint32_t slot) {
+    if (f.left == 0 && !more()) return;
+    const int copies = f.copies;
+    if (without) {
+      const int ls = step_shift(f.fmt);
+      const char* x = f.x + (ls == 1 ? f.sub * 128 : ls == 2 ? (f.sub ^ ((lane >> 2) & 1)) * 64 : 0);
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(slot + kStepCodes + kStepMeta + lane * 16), "r"((uint32_t)(uintptr_t)x),
+                   "r"((uint32_t)((uintptr_t)x >> 32)), "r"(f.x_step), "r"((uint32_t)copies)
+                   : "memory");
+      ++asked;
+      f.copies = 0;
+    }
+    ask_any<true>(f, slot, lane);
+    f.copies = copies;
+  };
+
+  float* const own = sums + warp * p.T * kSumPitch;
+  int first = 0, prime = STAGES;                  // the first of the four units in work; steps to ask for before any are multiplied
+  bool open = false;                              // phase 2: a unit is in work,
+  int place = 0, stop = 0, where = 0;             // at this place of its steps
 #pragma unroll 1
-    for (int first = 0; first < mine; first += 4) {
-      const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
-      if (team >= m) continue;
-      const GateUp g = gate_up_unit(t, segs, unit_of(first + team), hg, ts, member);
-      const int pair0 = t.off[g.a] + g.pass * kUnitCols, cols = min(kUnitCols, t.off[g.a + 1] - pair0);
-      const int x = t.token[pair0 + min(lane >> 2, cols - 1)];
-      const int t0 = t.token[pair0 + min(2 * (lane & 3), cols - 1)], t1 = t.token[pair0 + min(2 * (lane & 3) + 1, cols - 1)];
-      float tot[2][4] = {};
-      Operand o{smem_u32(pieces) + x * 256, smem_u32(xsum + t0), smem_u32(xsum + t1), p.T, (uint32_t)(x & 1) << 2, g.lo};
-      walk<kAnyFormat, 0, STAGES>(fixed, t.fmt[4 * g.a + g.kind], g.n, f, r, o, tot, more);
+  for (;;) {
+    const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
+    const bool idle = team >= m;
+    const int unit = unit_of(first + team);
+    int fmt = 0, n = 0, pair0 = 0, cols = 1;
+    GateUp g{};
+    Operand o{};
+    if (!prime) {
+      if (first >= mine) {
+        if (down) break;
+        // ---- from phase 1 to phase 2 ----
+        cp_wait<0>();
+        __syncthreads();
+        // The CTAs add up to 2^31 between them: the top bit turns when the last one has come, and again in the next call.
+        // (The values were written before the barrier above: released with this addition.)
+        if (tid == 0)
+          asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(p.sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
+        down = true;
+        const int units = p.H / kUnitRows * p.n_parts;
+        mine = units / G + (b < units % G);
+        r.bytes = p.slot2;
+        r.base = r.slot = smem_u32(smem) + kTableBytes<TAB> + kStreamWarps * p.T * kSumPitch * 4 + warp * STAGES * p.slot2;
+        first = next = 0;
+        f.left = 0;
+        prime = STAGES;
+        without = true;
+        continue;
+      }
+      if (idle) {
+        first += 4;
+        continue;
+      }
+      if (!down) {
+        g = gate_up_unit(t, segs, unit, hg, ts, member, lane);
+        pair0 = t.off[g.a] + g.pass * kUnitCols;
+        cols = min(kUnitCols, t.off[g.a + 1] - pair0);
+        const int x = t.token[pair0 + min(lane >> 2, cols - 1)];
+        fmt = t.fmt[4 * g.a + g.kind];
+        n = g.n;
+        o = Operand{smem_u32(pieces) + x * 256, 0, 0, p.T, (uint32_t)(x & 1) << 2, g.lo};
+      } else {
+        if (!open) {
+          range(unit, ts, member, place, stop);
+          where = count_up_to(t.step0 + 1, segs, place, lane);
+#pragma unroll 1
+          for (int i = lane; i < p.T * kSumPitch; i += 32) own[i] = 0.f;
+          __syncwarp();
+          open = true;
+        }
+        DownRun d;
+        if (down_run(t, fg, place, stop, where, d)) {
+          fmt = t.fmt[4 * d.a + PW_DOWN];
+          const int ls = step_shift(fmt);
+          pair0 = t.off[d.a] + d.pass * kUnitCols;
+          cols = min(kUnitCols, t.off[d.a + 1] - pair0);
+          const int xc = min(lane >> 2, cols - 1);
+          n = d.n;
+          o = Operand{(uint32_t)(kStepCodes + kStepMeta + xc * (256 >> ls)), 0, 0, 0, ls == 2 ? 0 : (uint32_t)(xc & 1) << 2, d.lo};
+        }
+      }
+    }
+    float tot[2][4] = {};
+    walk<kAnyFormat, true, STAGES>(fixed, fmt, prime, n, f, r, o, tot, ask_next);
+    if (prime) {
+      prime = 0;
+      if (!down) continue;
+      // ---- all CTAs have arrived ----
+      // (a CTA that has to wait asks for its next steps' codes first, into the L2 cache: the memory works on meanwhile)
+      without = false;
+      uint32_t arrived;
+      asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(arrived) : "l"(p.sync) : "memory");
+      if (__shfl_sync(0xffffffffu, (arrived ^ before) >> 31, 0) == 0) {
+        const Feed ahead = f;
+        const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
+#pragma unroll 1
+        for (int i = 0; i < kFewAheadSteps && (f.left || more()); ++i) prefetch_step(f, lane);
+        f = ahead;
+        next = a0, at = a1, end = a2, hint = a3, slice = a4;
+      }
+      bool together = true;
+      if (tid == 0) {
+        uint32_t now;
+        together = false;
+#pragma unroll 1
+        for (uint32_t i = 0; i < kFewPolls && !together; ++i) {
+          asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(p.sync) : "memory");
+          together = (now ^ before) >> 31;
+        }
+        if (!together) atomicMax(p.status, (int)PW_ERR_TIMEOUT);
+      }
+      if (!__syncthreads_and(together)) break;
+#pragma unroll 1
+      for (int i = 0; i < STAGES; ++i) {
+        if (i < asked) {
+          const uint32_t to = r.base + i * r.bytes + kStepCodes + kStepMeta + lane * 16;
+          const uint4 w = lds16(to);
+          const char* x = reinterpret_cast<const char*>((uintptr_t)w.x | (uintptr_t)w.y << 32);
+#pragma unroll 1
+          for (int j = 0; j < (int)w.w; ++j) cp16(to + j * 512, x + (size_t)j * w.z);   // (rows behind the first lie behind all lanes' places)
+        }
+        cp_commit();
+      }
+      continue;
+    }
+    if (!down) {
       put_sums(sums + warp * kSumFloats, lane, tot);
       few_team_sync(team, ts);
       const float* set = sums + (team << ts) * kSumFloats;
+#pragma unroll 1
       for (int i = member * 32 + lane; i < kUnitRows * cols; i += 32 << ts) {
         const int row = i & (kUnitRows - 1), col = i >> 5;
-        const float* at = set + col * kSumPitch + row;
+        const float* from = set + col * kSumPitch + row;
         float gate = 0.f, up = 0.f;
+#pragma unroll 4
         for (int w = 0; w < 1 << ts; ++w) {
-          const float v = at[w * kSumFloats];
-          if (w < g.gates) gate = __fadd_rn(gate, v);
-          else up = __fadd_rn(up, v);
+          const float v = from[w * kSumFloats];
+          gate = __fadd_rn(gate, w < g.gates ? v : 0.f);
+          up = __fadd_rn(up, w < g.gates ? 0.f : v);
         }
         // rounded to fp16 as the operand of the down block, like the layer call for batches: the fast exponential and
         // division (relative error ~1e-6) change nothing that survives the rounding
@@ -336,156 +518,63 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         *reinterpret_cast<__half*>(p.h + (size_t)(pair0 + col) * p.F * 2 + piece_offset(g.slice * kUnitRows + row, col)) = __float2half_rn(h);
       }
       few_team_sync(team, ts);                    // the sums are written again
+      first += 4;
+      continue;
     }
-  }
-  cp_wait<0>();
-  __syncthreads();
-
-  // ---- phase 2: down ----
-  constexpr int kSlot2 = kSlotOf<XC>;
-  char* const ring2 = smem + p.table_bytes + kStreamWarps * p.T * kSumPitch * 4;
-  r.base = smem_u32(ring2) + warp * STAGES * kSlot2;
-  r.slot = r.base;
-  {
-    const int G = (int)gridDim.x, b = (int)blockIdx.x;
-    const int units = p.H / kUnitRows * p.n_parts, steps = t.step0[segs];
-    const int mine = units / G + (b < units % G);
-    int next = 0, at = 0, end = 0, hint = 0, slice = 0;
-    f.left = 0;
-    // steps of part `part` for warp `member` of 1 << ts
-    auto range = [&](int unit, int ts, int member, int& lo, int& hi) {
-      const int64_t share = (int64_t)p.n_parts << ts, i = ((int64_t)(unit % p.n_parts) << ts) + member;
-      lo = (int)(steps * i / share);
-      hi = (int)(steps * (i + 1) / share);
-    };
-    auto more = [&]() -> bool {
-      DownRun d;
-      while (!down_run(t, segs, fg, at, end, hint, d)) {
-        if (next >= mine) return false;
-        const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts;
-        const int unit = (next + team) * G + b;
-        next += m;
-        at = end = 0;
-        if (team >= m) continue;
-        range(unit, ts, warp & ((1 << ts) - 1), at, end);
-        hint = 0;
-        slice = unit / p.n_parts;
-      }
-      const SegPage& page = t.page[3 * d.a + PW_DOWN];
-      const int pair0 = t.off[d.a] + d.pass * kUnitCols;
-      feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * d.a + PW_DOWN], fg, slice, d.lo, d.lo + d.n);
-      feed_operand(f, lane, p.h + (size_t)pair0 * p.F * 2, (uint32_t)p.F * 2, min(kUnitCols, t.off[d.a + 1] - pair0), d.lo);
-      return true;
-    };
-    // codes first, then, when every CTA has written its values, the operands that go with them
-#pragma unroll 1
-    for (int i = 0; i < STAGES && (f.left || more()); ++i) ask_any<XC, true, false>(f, r.base + i * kSlot2, lane);
-    bool together = true;
-    if (tid == 0) {
-      const int32_t generation = *reinterpret_cast<volatile int32_t*>(p.sync + 1);
-      __threadfence();
-      if (atomicAdd(p.sync, 1) == G - 1) {
-        p.sync[0] = 0;
-        __threadfence();
-        atomicAdd(p.sync + 1, 1);
-      } else {
-        together = false;
-        for (uint32_t n = 0; n < kFewPolls && !together; ++n) {
-          int32_t now;
-          asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(now) : "l"(p.sync + 1) : "memory");
-          together = now != generation;
-        }
-        if (!together) atomicMax(p.status, (int)PW_ERR_TIMEOUT);
-      }
-      __threadfence();
-    }
-    if (!__syncthreads_and(together)) {
-      cp_commit();
-      cp_wait<0>();
-      return;
-    }
-    {
-      const Feed ahead = f;
-      const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
-      next = at = end = hint = slice = 0;
-      f.left = 0;
-#pragma unroll 1
-      for (int i = 0; i < STAGES; ++i) {
-        if (f.left || more()) ask_any<XC, false, true>(f, r.base + i * kSlot2, lane);
-        cp_commit();
-      }
-      const char* x = f.x;                        // (codes and operand have come to the same step)
-      f = ahead;
-      f.x = x;
-      next = a0, at = a1, end = a2, hint = a3, slice = a4;
-    }
-    float* const own = sums + warp * p.T * kSumPitch;
-#pragma unroll 1
-    for (int first = 0; first < mine; first += 4) {
-      const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
-      if (team >= m) continue;
-      const int unit = (first + team) * G + b;
-      int lo, hi, where = 0;
-      range(unit, ts, member, lo, hi);
-      for (int i = lane; i < p.T * kSumPitch; i += 32) own[i] = 0.f;
-      __syncwarp();
-      DownRun d;
-      while (down_run(t, segs, fg, lo, hi, where, d)) {
-        const int fmt = t.fmt[4 * d.a + PW_DOWN], ls = step_shift(fmt);
-        const int pair0 = t.off[d.a] + d.pass * kUnitCols, cols = min(kUnitCols, t.off[d.a + 1] - pair0);
-        const int xc = min(lane >> 2, cols - 1);
-        float tot[2][4] = {};
-        Operand o{r.base + kStepCodes + kStepMeta + xc * (256 >> ls), 0, 0, 0, (uint32_t)(xc & 1) << 2, d.lo};
-        walk<kAnyFormat, XC, STAGES>(fixed, fmt, d.n, f, r, o, tot, more);
+    if (n) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {             // the tokens of a run are different ones: no two lanes meet
-          const int col = 2 * (lane & 3) + c;
-          if (col < cols) {
-            const float g = t.gate[pair0 + col];
-            float4* to = reinterpret_cast<float4*>(own + t.token[pair0 + col] * kSumPitch + 4 * (lane >> 2));
-            float4 v = *to;
-            v.x = __fadd_rn(v.x, __fmul_rn(g, tot[0][c]));
-            v.y = __fadd_rn(v.y, __fmul_rn(g, tot[0][c + 2]));
-            v.z = __fadd_rn(v.z, __fmul_rn(g, tot[1][c]));
-            v.w = __fadd_rn(v.w, __fmul_rn(g, tot[1][c + 2]));
-            *to = v;
-          }
-        }
-        __syncwarp();
-      }
-      few_team_sync(team, ts);
-      const float* set = sums + (team << ts) * p.T * kSumPitch;
-      const int row0 = unit / p.n_parts * kUnitRows, part = unit % p.n_parts;
-      for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
-        const int row = i & (kUnitRows - 1), tok = i >> 5;
-        float v = 0.f;
-        for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, set[(w * p.T + tok) * kSumPitch + row]);
-        if (p.n_parts == 1) store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
-        else p.parts[((size_t)part * p.T + tok) * p.H + row0 + row] = v;
-      }
-      if (p.n_parts > 1) {
-        // the last of the parts to finish adds all of them up, in their order
-        __threadfence();
-        few_team_sync(team, ts);
-        int last = 0;
-        if (lane == 0 && member == 0) last = atomicAdd(p.sync + 64 + row0 / kUnitRows, 1) == p.n_parts - 1;
-        if (lane == 0 && member == 0) reinterpret_cast<int32_t*>(sums + (size_t)(team << ts) * p.T * kSumPitch)[0] = last;
-        few_team_sync(team, ts);
-        last = *reinterpret_cast<volatile int32_t*>(sums + (size_t)(team << ts) * p.T * kSumPitch);
-        if (last) {
-          __threadfence();
-          for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
-            const int row = i & (kUnitRows - 1), tok = i >> 5;
-            float v = 0.f;
-            for (int q = 0; q < p.n_parts; ++q) v = __fadd_rn(v, __ldcg(p.parts + ((size_t)q * p.T + tok) * p.H + row0 + row));
-            store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
-          }
-          if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
+      for (int c = 0; c < 2; ++c) {               // the tokens of a run are different ones: no two lanes meet
+        const int col = 2 * (lane & 3) + c;
+        if (col < cols) {
+          const float gate = t.gate[pair0 + col];
+          float4* to = reinterpret_cast<float4*>(own + t.token[pair0 + col] * kSumPitch + 4 * (lane >> 2));
+          float4 v = *to;
+          v.x = __fadd_rn(v.x, __fmul_rn(gate, tot[0][c]));
+          v.y = __fadd_rn(v.y, __fmul_rn(gate, tot[0][c + 2]));
+          v.z = __fadd_rn(v.z, __fmul_rn(gate, tot[1][c]));
+          v.w = __fadd_rn(v.w, __fmul_rn(gate, tot[1][c + 2]));
+          *to = v;
         }
       }
-      few_team_sync(team, ts);                    // the sums are written again
+      __syncwarp();
+      if (place < stop) continue;
     }
+    open = false;
+    first += 4;
+    few_team_sync(team, ts);
+    float* const set = sums + (team << ts) * p.T * kSumPitch;
+    const int row0 = slice_of(unit) * kUnitRows, part = unit - slice_of(unit) * p.n_parts;
+#pragma unroll 1
+    for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
+      const int row = i & (kUnitRows - 1), tok = i >> 5;
+      float v = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, set[(w * p.T + tok) * kSumPitch + row]);
+      if (p.n_parts == 1) store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
+      else p.parts[((size_t)part * p.T + tok) * p.H + row0 + row] = v;
+    }
+    if (p.n_parts > 1) {
+      // the last of the parts to finish adds all of them up, in their order
+      __threadfence();
+      few_team_sync(team, ts);
+      if (lane == 0 && member == 0) *reinterpret_cast<int32_t*>(set) = atomicAdd(p.sync + 64 + row0 / kUnitRows, 1) == p.n_parts - 1;
+      few_team_sync(team, ts);
+      if (*reinterpret_cast<volatile int32_t*>(set)) {
+        __threadfence();
+#pragma unroll 1
+        for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
+          const int row = i & (kUnitRows - 1), tok = i >> 5;
+          float v = 0.f;
+#pragma unroll 1
+          for (int q = 0; q < p.n_parts; ++q) v = __fadd_rn(v, __ldcg(p.parts + ((size_t)q * p.T + tok) * p.H + row0 + row));
+          store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
+        }
+        if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
+      }
+    }
+    few_team_sync(team, ts);                      // the sums are written again
   }
+  cp_commit();
   cp_wait<0>();
 }
 
@@ -495,6 +584,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 // tokens and gates.  Sums in a fixed order.
 __device__ __forceinline__ float square_sum(const uint4* row, int n, int lane) {
   float a = 0.f;
+#pragma unroll 1
   for (int i = lane; i < n; i += 32) {
     const uint4 v = __ldcg(row + i);
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -517,6 +607,7 @@ __global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, i
   const int32_t* tokens = seen + 3 + 2 * room;
   const float* gates = reinterpret_cast<const float*>(seen) + 3 + 2 * room + pairs;
   float sr = 0.f, srx = 0.f, srx2 = 0.f, mx = 0.f, srh = 0.f, srh2 = 0.f, mh = 0.f;
+#pragma unroll 1
   for (int i = p0; i < p1; ++i) {
     const float r = gates[i], x2 = square_sum(hidden + (size_t)tokens[i] * (H / 8), H / 8, lane), h2 = square_sum(h + (size_t)i * (F / 8), F / 8, lane);
     const float nx = sqrtf(x2), nh = sqrtf(h2);
@@ -531,6 +622,7 @@ __global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, i
   int n = p1 - p0;
   if (ids && seg < E) {                           // a pair that is named twice counts twice
     n = 0;
+#pragma unroll 1
     for (int i = lane; i < Tk; i += 32) n += ids[i] == seg;
 #pragma unroll
     for (int d = 16; d; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
@@ -551,17 +643,21 @@ __global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, i
 // ---- host ----------------------------------------------------------------------------------------
 typedef void (*FewKernel)(FewArgs);
 struct FewVariant {
-  int xc, stages;
+  int segs, pairs, choices, table_bytes, stages;
   FewKernel kernel;
 };
-// The most stages that fit are the fastest; the operand rows of a slot go by the tokens.
-static const FewVariant kFewVariants[] = {{2, 4, few_layer_kernel<2, 4>}, {4, 3, few_layer_kernel<4, 3>}, {8, 3, few_layer_kernel<8, 3>}, {8, 2, few_layer_kernel<8, 2>}};
+template <class TAB, int STAGES>
+static constexpr FewVariant few_variant() {
+  return {TAB::kSegs, TAB::kPairs, TAB::kChoices, kTableBytes<TAB>, STAGES, few_layer_kernel<TAB, STAGES>};
+}
+// The first that fits is the fastest.
+static const FewVariant kFewVariants[] = {few_variant<FewSmall, 4>(), few_variant<FewSmall, 3>(), few_variant<FewAll, 3>(), few_variant<FewSmall, 2>(),
+                                          few_variant<FewAll, 2>()};
 
 static size_t few_smem(const FewArgs& a, const FewVariant& v) {
-  const size_t first = (size_t)kStreamWarps * (kSumFloats * 4 + v.stages * kSlotOf<0>) + (((size_t)a.H / kGroup * 3 * a.T * 4 + 127) & ~(size_t)127) +
-                       (size_t)a.T * a.H * 2;
-  const size_t second = (size_t)kStreamWarps * ((size_t)a.T * kSumPitch * 4 + (size_t)v.stages * (kStepCodes + kStepMeta + 256 * v.xc));
-  return a.table_bytes + (first > second ? first : second);
+  const size_t first = (size_t)kStreamWarps * (kSumFloats * 4 + v.stages * slot_bytes(0)) + (size_t)a.T * a.H * 2;
+  const size_t second = (size_t)kStreamWarps * ((size_t)a.T * kSumPitch * 4 + (size_t)v.stages * a.slot2);
+  return v.table_bytes + (first > second ? first : second);
 }
 
 static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k, const pw_page_table* table,
@@ -582,10 +678,10 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.out_type = out_type;
   a.segs = (c.n_experts < T * top_k ? c.n_experts : T * top_k) + c.n_shared;
   a.pairs = T * (top_k + c.n_shared);
-  a.table_bytes = (int)few_tables(nullptr, nullptr, a.segs, a.pairs, T * top_k, c.n_experts);
+  a.slot2 = slot_bytes(T < 2 ? 2 : T < kUnitCols ? T : kUnitCols);   // (room for 512 bytes: see ask_next)
   const FewVariant* v = nullptr;
   for (const FewVariant& one : kFewVariants)
-    if (!v && one.xc >= (T < kUnitCols ? T : kUnitCols) && few_smem(a, one) <= kSmemLimit) v = &one;
+    if (!v && a.segs <= one.segs && a.pairs <= one.pairs && T * top_k <= one.choices && few_smem(a, one) <= kSmemLimit) v = &one;
   if (!v) return PW_ERR_SHAPE;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
@@ -610,9 +706,10 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   double best = -1.;
   for (int parts = 1; parts <= kFewParts; ++parts) {
     const int rounds = (slices * parts + ctx->num_sms - 1) / ctx->num_sms;
-    const double cost = (double)rounds / parts * (1. + 0.02 * parts);
+    const double cost = (double)rounds / parts * (1. + 0.05 * parts) + (parts > 1 ? 0.05 : 0.);
     if (best < 0 || cost < best) best = cost, a.n_parts = parts;
   }
+  a.per_part = a.n_parts > 1 ? (uint32_t)((0xffffffffull + a.n_parts) / a.n_parts) : 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctx->num_sms);
   cfg.blockDim = dim3(kStreamThreads);

@@ -56,6 +56,9 @@ __host__ __device__ constexpr uint32_t stream_scale_offset(int fmt) {
   return fmt >= kFmtP4 ? (uint32_t)kPlaneTopCodes + 512u * (uint32_t)(kFmtP2 - fmt) : stream_tile_bytes(fmt) - 512u;
 }
 
+// the same for a format that is known at run time only: one load instead of a chain of selections
+__constant__ uint32_t kTileBytes[8] = {32768, 16896, 8704, 6656, 4608, 5632, 5632, 5632};
+__constant__ uint32_t kScaleOffset[8] = {32256, 16384, 8192, 6144, 4096, 5120, 4608, 4096};
 constexpr int kSmemLimit = 232448;                // 227 KB
 constexpr int kStreamWarps = 16;
 constexpr int kStreamThreads = kStreamWarps * 32;
@@ -63,8 +66,8 @@ constexpr int kUnitRows = 32;
 constexpr int kUnitCols = 8;                      // tokens of a unit
 constexpr int kStepCodes = 2048;                  // bytes of a slot: codes, scales and zero-points, streamed operand rows
 constexpr int kStepMeta = 128;
-template <int XC>                                 // XC: operand rows that are streamed with the codes; 0: they are staged
-constexpr int kSlotOf = kStepCodes + kStepMeta + 256 * XC;
+// rows: operand rows that are streamed with the codes; 0: they are staged
+__host__ __device__ constexpr int slot_bytes(int rows) { return kStepCodes + kStepMeta + 256 * rows; }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -118,12 +121,14 @@ __device__ __forceinline__ void feed_codes(Feed& f, int lane, const char* codes,
   f.fmt = fmt;
   f.left = hi - lo;
   f.sub = lo & ((1 << ls) - 1);
-  const char* at = codes + tile * stream_tile_bytes(fmt);
-  f.meta = at + stream_scale_offset(fmt) + 64 * sl + (lane >> 2) * 256 + (lane & 3) * 16;
+  const char* at = codes + tile * kTileBytes[fmt];
+  f.meta = at + kScaleOffset[fmt] + 64 * sl + (lane >> 2) * 256 + (lane & 3) * 16;
   const uint32_t row = (uint32_t)(32 * sl + lane) * 16;
   f.codes = at + f.sub * 8192 + row;
-  f.bit1 = bit1 + tile * kPlaneBitTile + row;
-  f.bit0 = bit0 + tile * kPlaneBitTile + row;
+  if (fmt >= kFmtP4) {
+    f.bit1 = bit1 + tile * kPlaneBitTile + row;
+    f.bit0 = bit0 + tile * kPlaneBitTile + row;
+  }
 }
 // ... and for operand rows that are streamed with them: `cols` rows of pieces, `pitch` bytes apart, row c in the order of
 // row c.  A lane copies bytes of row lane >> (4 - ls), and of the rows 2 << ls further on.
@@ -135,60 +140,77 @@ __device__ __forceinline__ void feed_operand(Feed& f, int lane, const char* x, u
   f.x_step = pitch << (ls + 1);
 }
 
-// Asks for a step in format F (its codes, its streamed operand, or both) and moves on; `left` is the caller's.
-template <int F, int XC, bool CODES, bool OPERAND>
+// Asks for a step in format F and moves on; `left` is the caller's.  STREAM: with its streamed operand, if it has one.
+template <int F, bool STREAM>
 __device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
   constexpr int ls = step_shift(F);
-  if constexpr (OPERAND && XC > 0) {
+  if constexpr (STREAM) {
     // the step's part of a group's pieces: all, the half `sub`, or the quarter `sub` (quarters of odd rows are exchanged)
     const char* src = f.x;
     if constexpr (ls == 1) src += f.sub * 128;
     if constexpr (ls == 2) src += (f.sub ^ ((lane >> 2) & 1)) * 64;
     const uint32_t dst = slot + kStepCodes + kStepMeta + lane * 16;
 #pragma unroll
-    for (int j = 0; j < (XC >> (ls + 1) > 0 ? XC >> (ls + 1) : 1); ++j)
+    for (int j = 0; j < kUnitCols >> (ls + 1); ++j)
       if (j < f.copies) cp16(dst + j * 512, src + j * f.x_step);
     f.x += ls == 0 || f.sub == (1 << ls) - 1 ? 256 : 0;
   }
-  if constexpr (CODES) {
-    constexpr uint32_t tile = stream_tile_bytes(F);
-    constexpr int units = F <= kFmt4 ? 4 : F == kFmt3 ? 3 : 2;
+  constexpr uint32_t tile = stream_tile_bytes(F);
+  constexpr int units = F <= kFmt4 ? 4 : F == kFmt3 ? 3 : 2;
 #pragma unroll
-    for (int u = 0; u < units; ++u) cp16(slot + code_at<F>(u, lane), f.codes + u * 2048);
-    if (F != kFmt16 && lane < 8) cp16(slot + kStepCodes + lane * 16, f.meta);
-    if constexpr (F == kFmtP4 || F == kFmtP3) {
-      cp16(slot + code_at<F>(2, lane), f.bit1);
-      f.bit1 += kPlaneBitTile;
-    }
-    if constexpr (F == kFmtP4) {
-      cp16(slot + code_at<F>(3, lane), f.bit0);
-      f.bit0 += kPlaneBitTile;
-    }
-    if constexpr (F == kFmt16) {
-      f.codes += 8192;                            // (a tile of 16 bits has nothing behind its codes)
-    } else if constexpr (F == kFmt8) {
-      f.codes += f.sub ? tile - 8192u : 8192u;
-      f.meta += f.sub ? tile : 0u;
-    } else {
-      f.codes += tile;
-      f.meta += tile;
-    }
+  for (int u = 0; u < units; ++u) cp16(slot + code_at<F>(u, lane), f.codes + u * 2048);
+  if (F != kFmt16 && lane < 8) cp16(slot + kStepCodes + lane * 16, f.meta);
+  if constexpr (F == kFmtP4 || F == kFmtP3) {
+    cp16(slot + code_at<F>(2, lane), f.bit1);
+    f.bit1 += kPlaneBitTile;
+  }
+  if constexpr (F == kFmtP4) {
+    cp16(slot + code_at<F>(3, lane), f.bit0);
+    f.bit0 += kPlaneBitTile;
+  }
+  if constexpr (F == kFmt16) {
+    f.codes += 8192;                            // (a tile of 16 bits has nothing behind its codes)
+  } else if constexpr (F == kFmt8) {
+    f.codes += f.sub ? tile - 8192u : 8192u;
+    f.meta += f.sub ? tile : 0u;
+  } else {
+    f.codes += tile;
+    f.meta += tile;
   }
   if constexpr (ls > 0) f.sub = (f.sub + 1) & ((1 << ls) - 1);
 }
-template <int XC, bool CODES, bool OPERAND>
+template <bool STREAM>
 __device__ __forceinline__ void ask_any(Feed& f, uint32_t slot, int lane) {
   f.left--;
   switch (f.fmt) {
-    case kFmt16: ask<kFmt16, XC, CODES, OPERAND>(f, slot, lane); break;
-    case kFmt8: ask<kFmt8, XC, CODES, OPERAND>(f, slot, lane); break;
-    case kFmt4: ask<kFmt4, XC, CODES, OPERAND>(f, slot, lane); break;
-    case kFmt3: ask<kFmt3, XC, CODES, OPERAND>(f, slot, lane); break;
-    case kFmt2: ask<kFmt2, XC, CODES, OPERAND>(f, slot, lane); break;
-    case kFmtP4: ask<kFmtP4, XC, CODES, OPERAND>(f, slot, lane); break;
-    case kFmtP3: ask<kFmtP3, XC, CODES, OPERAND>(f, slot, lane); break;
-    default: ask<kFmtP2, XC, CODES, OPERAND>(f, slot, lane); break;
+    case kFmt16: ask<kFmt16, STREAM>(f, slot, lane); break;
+    case kFmt8: ask<kFmt8, STREAM>(f, slot, lane); break;
+    case kFmt4: ask<kFmt4, STREAM>(f, slot, lane); break;
+    case kFmt3: ask<kFmt3, STREAM>(f, slot, lane); break;
+    case kFmt2: ask<kFmt2, STREAM>(f, slot, lane); break;
+    case kFmtP4: ask<kFmtP4, STREAM>(f, slot, lane); break;
+    case kFmtP3: ask<kFmtP3, STREAM>(f, slot, lane); break;
+    default: ask<kFmtP2, STREAM>(f, slot, lane); break;
   }
+}
+
+// Asks the L2 cache for the codes of a step, and moves on.
+__device__ __forceinline__ void prefetch_line(const char* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
+__device__ __forceinline__ void prefetch_step(Feed& f, int lane) {
+  const int ls = step_shift(f.fmt), units = f.fmt <= kFmt4 ? 4 : f.fmt == kFmt3 ? 3 : 2;
+  const uint32_t tile = kTileBytes[f.fmt];
+  const int u = lane >> 2, line = (lane & 3) * 128;   // lanes 0 .. 15: the lines of unit u; 16, 17: scales and zero-points
+  if (u < units) prefetch_line(f.codes - lane * 16 + u * 2048 + line);
+  else if (u == 2 && (f.fmt == kFmtP4 || f.fmt == kFmtP3)) prefetch_line(f.bit1 - lane * 16 + line);
+  else if (u == 3 && f.fmt == kFmtP4) prefetch_line(f.bit0 - lane * 16 + line);
+  else if (u == 4 && (lane & 3) < 2 && f.fmt != kFmt16) prefetch_line(f.meta - u * 256 - (lane & 3) * 16 + (lane & 3) * 256);
+  f.left--;
+  const bool last = f.sub == (1 << ls) - 1;
+  f.codes += last ? tile - (((uint32_t)1 << ls) - 1) * 8192u : 8192u;
+  f.meta += last ? tile : 0u;
+  f.bit1 += kPlaneBitTile;
+  f.bit0 += kPlaneBitTile;
+  f.sub = last ? 0 : f.sub + 1;
 }
 
 // ---- staged operand ------------------------------------------------------------------------------
@@ -203,10 +225,11 @@ __device__ __forceinline__ float sum_halves(const uint4& v) {
 }
 // Groups g0 .. g0 + groups of `rows` operand rows (fp16, `pitch` bytes apart, k_bytes of a row count, zeros behind them) ->
 // pieces [group][room][256 bytes] and the sums of the first half, the second half and the whole of every group,
-// [group][3][room].  By `threads` threads (whole warps).
+// [group][3][room] (sums may be null).  By `threads` threads (whole warps).
 __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int rows, int room, int g0, int groups, int k_bytes, char* pieces, float* sums,
                                               int thread, int threads) {
   const int n = rows * groups * 8;
+#pragma unroll 1
   for (int base = thread & ~31; base < n; base += threads) {
     const int i = base + (thread & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
     uint4 v[2] = {};
@@ -217,11 +240,15 @@ __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int r
         v[0] = reinterpret_cast<const uint4*>(src)[0];
         v[1] = reinterpret_cast<const uint4*>(src)[1];
       } else {
-        uint16_t h[16];
+        // (one way only for the last, short stretch: it is met once in a row)
+        uint32_t w[8] = {};
 #pragma unroll
-        for (int j = 0; j < 16; ++j) h[j] = k + 2 * j < k_bytes ? reinterpret_cast<const uint16_t*>(src)[j] : (uint16_t)0;
-        v[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-        v[1] = make_uint4(h[8] | h[9] << 16, h[10] | h[11] << 16, h[12] | h[13] << 16, h[14] | h[15] << 16);
+        for (int j = 0; j < 8; ++j) {
+          if (k + 4 * j < k_bytes) w[j] = reinterpret_cast<const uint16_t*>(src)[2 * j];
+          if (k + 4 * j + 2 < k_bytes) w[j] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[2 * j + 1] << 16;
+        }
+        v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        v[1] = make_uint4(w[4], w[5], w[6], w[7]);
       }
       uint4 piece[2];
       make_pieces(v[0], v[1], piece);
@@ -233,7 +260,7 @@ __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int r
     a += __shfl_xor_sync(0xffffffffu, a, 1);
     a += __shfl_xor_sync(0xffffffffu, a, 2);
     const float b = a + __shfl_xor_sync(0xffffffffu, a, 4);
-    if (i < n && (s & 3) == 0) {
+    if (sums && i < n && (s & 3) == 0) {
       sums[(g * 3 + (s >> 2)) * room + c] = a;
       if (s == 0) sums[(g * 3 + 2) * room + c] = b;
     }
@@ -242,10 +269,10 @@ __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int r
 
 // The operand of a block's steps, as a lane reads it.
 struct Operand {
-  uint32_t x;                                     // staged: this lane's row of group 0; streamed: the row in slot 0
-  uint32_t sum0, sum1;                            // staged: sums of group 0, tokens 2t and 2t + 1
-  int room;                                       // staged rows there is room for
-  uint32_t flip;                                  // 4 for an odd row (see piece_at)
+  uint32_t x;                                     // staged: this lane's row of group 0; streamed: the row's place in a slot
+  uint32_t sum0, sum1;                            // staged, with sums: those of group 0, tokens 2t and 2t + 1
+  int room;                                       // staged: rows there is room for; 0: streamed
+  uint32_t flip;                                  // 4 for an odd row (see piece_at; not in a streamed quarter of a group)
   int step;                                       // next step of the block
 };
 
@@ -340,9 +367,9 @@ struct Codes {
   }
 };
 
-// One step in format F out of a slot.  x: this lane's operand row, with the step's pieces at (at0 ^ i) * 16 bytes.  STAGED:
+// One step in format F out of a slot.  x: this lane's operand row, with the step's pieces at (at0 ^ i) * 16 bytes.  SUMS:
 // the operands' sums are at at_sum0 and at_sum1, else they are made here, by a row of ones on the same fragments.
-template <int F, bool STAGED>
+template <int F, bool SUMS>
 __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int lane, uint32_t xrow, uint32_t at0, uint32_t at_sum0, uint32_t at_sum1,
                                               float (&tot)[2][4]) {
   const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3;
@@ -365,7 +392,7 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
 #pragma unroll
     for (int i = 0; i < 2 * S; ++i) x[i] = lds16(xrow + ((at0 ^ i) << 4));
     float sum0, sum1;
-    if constexpr (STAGED) {
+    if constexpr (SUMS) {
       sum0 = __uint_as_float(lds4(at_sum0)), sum1 = __uint_as_float(lds4(at_sum1));
     } else {
       float ones[4];
@@ -426,30 +453,28 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
 // ---- a warp's walk over its steps ----------------------------------------------------------------
 struct Ring {
   uint32_t base, slot;                            // shared memory: the warp's slots, the next step's
+  uint32_t bytes;                                 // of a slot
   int lane;
 };
-template <int XC, int STAGES>
+template <int STAGES>
 __device__ __forceinline__ void ring_on(Ring& r) {
   cp_commit();
-  r.slot = r.slot == r.base + (STAGES - 1) * kSlotOf<XC> ? r.base : r.slot + kSlotOf<XC>;
+  r.slot = r.slot == r.base + (STAGES - 1) * r.bytes ? r.base : r.slot + r.bytes;
 }
 // Multiplies steps of a block in format F, at most n, and asks for the next step of the feed after each while that is in
-// the same format.  Returns with n = 0, or having multiplied a step without having asked (true).
-template <int F, int XC, int STAGES>
+// the same format.  Returns with n = 0, or having multiplied a step without having asked (true).  STREAM: the operand may
+// be streamed, and has no sums.
+template <int F, bool STREAM, int STAGES>
 __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4]) {
   constexpr int ls = step_shift(F);
   const uint32_t t = (uint32_t)r.lane & 3;
   // The lane's pieces of a step: e = 4t + i, 8q + 2t + i or 4q + t, q the step inside its group, in the order of piece_at:
   // at0 ^ (what q adds) ^ i.  A streamed row is the part of its step.
-  const uint32_t at0 = ls == 0 ? (5 * t) ^ o.flip : ls == 1 ? (2 * t) ^ (t >> 1) ^ o.flip : XC ? t : t ^ o.flip;
-  const uint32_t x_group = (uint32_t)o.room * 256, sum_part = (uint32_t)o.room * 4, sum_group = 3 * sum_part;
-  uint32_t x = o.x, sum0 = o.sum0, sum1 = o.sum1;
-  if constexpr (XC == 0) {
-    const uint32_t grp = (uint32_t)o.step >> ls;
-    x += grp * x_group;
-    sum0 += grp * sum_group;
-    sum1 += grp * sum_group;
-  }
+  const uint32_t at0 = (ls == 0 ? 5 * t : ls == 1 ? (2 * t) ^ (t >> 1) : t) ^ o.flip;
+  const bool streamed = STREAM && o.room == 0;
+  const uint32_t of_q = ls == 1 ? (streamed ? 2 : 10) : streamed ? 1 : 5;
+  const uint32_t x_group = (uint32_t)o.room * 256, sum_part = (uint32_t)o.room * 4, sum_group = 3 * sum_part, grp = (uint32_t)o.step >> ls;
+  uint32_t x = o.x + grp * x_group, sum0 = o.sum0 + grp * sum_group, sum1 = o.sum1 + grp * sum_group;
   int asks = f.fmt == F ? min(n, f.left) : 0;
   f.left -= asks;
   bool due = false;
@@ -458,16 +483,12 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
     cp_wait<STAGES - 1>();
     __syncwarp();                                 // what the other lanes have copied
     const uint32_t q = ls ? (uint32_t)o.step & ((1 << ls) - 1) : 0;
-    if constexpr (XC == 0) {
-      const uint32_t part = ls == 1 ? q * sum_part : 2 * sum_part;
-      multiply_step<F, true>(k, r.slot, r.lane, x, at0 ^ (ls == 1 ? 10 * q : ls == 2 ? 5 * q : 0), sum0 + part, sum1 + part, tot);
-      if (ls == 0 || q == (1 << ls) - 1) {
-        x += x_group;
-        sum0 += sum_group;
-        sum1 += sum_group;
-      }
-    } else {
-      multiply_step<F, false>(k, r.slot, r.lane, x + (r.slot - r.base), at0 ^ (ls == 1 ? 2 * q : ls == 2 ? q : 0), 0, 0, tot);
+    const uint32_t part = ls == 1 ? q * sum_part : 2 * sum_part;
+    multiply_step<F, !STREAM>(k, r.slot, r.lane, streamed ? x + r.slot : x, ls ? at0 ^ (of_q * q) : at0, sum0 + part, sum1 + part, tot);
+    if (ls == 0 || q == (1 << ls) - 1) {
+      x += x_group;
+      sum0 += sum_group;
+      sum1 += sum_group;
     }
     o.step++;
     __syncwarp();                                 // every lane has read the slot
@@ -475,44 +496,38 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
     due = asks == 0;
     if (due) break;
     --asks;
-    ask<F, XC, true, true>(f, r.slot, r.lane);
-    ring_on<XC, STAGES>(r);
+    ask<F, STREAM>(f, r.slot, r.lane);
+    ring_on<STAGES>(r);
   } while (n);
   return due;
 }
-// The next n steps, all of one block in format `fmt` (F, if that is not kAnyFormat: all blocks are).  more(): sets the feed
-// up for the next block; false: there is none.
+// Asks for `prime` steps, then multiplies the next n, all of one block in format `fmt` (F, if that is not kAnyFormat: all
+// blocks are), asking for as many.  ask_next(slot): asks for the feed's next step, of the next block if need be, or for
+// nothing if there is none.
 constexpr int kAnyFormat = -1;
-template <int F, int XC, bool CODES, bool OPERAND>
-__device__ __forceinline__ void ask_for(Feed& f, uint32_t slot, int lane) {
-  if constexpr (F == kAnyFormat) {
-    ask_any<XC, CODES, OPERAND>(f, slot, lane);
-  } else {
-    f.left--;
-    ask<F, XC, CODES, OPERAND>(f, slot, lane);
-  }
-}
-template <int F, int XC, int STAGES, class More>
-__device__ __forceinline__ void walk(const Fixed& k, int fmt, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], More more) {
-  while (n) {
-    bool due;
-    if constexpr (F != kAnyFormat) {
-      due = walk_format<F, XC, STAGES>(k, n, f, r, o, tot);
+template <int F, bool STREAM, int STAGES, class AskNext>
+__device__ __forceinline__ void walk(const Fixed& k, int fmt, int prime, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], AskNext ask_next) {
+  while (prime + n) {
+    bool due = true;
+    if (prime) {
+      --prime;
+    } else if constexpr (F != kAnyFormat) {
+      due = walk_format<F, STREAM, STAGES>(k, n, f, r, o, tot);
     } else {
       switch (fmt) {
-        case kFmt16: due = walk_format<kFmt16, XC, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt8: due = walk_format<kFmt8, XC, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt4: due = walk_format<kFmt4, XC, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt3: due = walk_format<kFmt3, XC, STAGES>(k, n, f, r, o, tot); break;
-        case kFmtP4: due = walk_format<kFmtP4, XC, STAGES>(k, n, f, r, o, tot); break;
-        case kFmtP3: due = walk_format<kFmtP3, XC, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt2: due = walk_format<kFmt2, XC, STAGES>(k, n, f, r, o, tot); break;
-        default: due = walk_format<kFmtP2, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt16: due = walk_format<kFmt16, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt8: due = walk_format<kFmt8, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt4: due = walk_format<kFmt4, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt3: due = walk_format<kFmt3, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmtP4: due = walk_format<kFmtP4, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmtP3: due = walk_format<kFmtP3, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt2: due = walk_format<kFmt2, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        default: due = walk_format<kFmtP2, STREAM, STAGES>(k, n, f, r, o, tot); break;
       }
     }
     if (due) {
-      if (f.left || more()) ask_for<F, XC, true, true>(f, r.slot, r.lane);
-      ring_on<XC, STAGES>(r);
+      ask_next(r.slot);
+      ring_on<STAGES>(r);
     }
   }
 }
