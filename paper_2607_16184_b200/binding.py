@@ -696,7 +696,7 @@ class Context:
         st = (_pwtorch or _load_pwtorch()).page_linear(self._ptr, self._index, None if stream is None else stream.cuda_stream, x,
                                                        pages, out_features, bias, out)
         if st:
-            self._refused(st, "pw_page_linear", "pw_moe_forward_few", "pw_moe_forward_few_routed", ("x", "pages", "out_features", "bias", "out"))
+            self._refused(st, "pw_page_linear", ("x", "pages", "out_features", "bias", "out"))
         return out
 
     def pw_moe_forward_few(self, layer: int, hidden: torch.Tensor, router_logits: torch.Tensor, top_k: int,
