@@ -13,10 +13,13 @@
 // A group of 128 columns of a row contributes
 //     sum x * (code * scale + zero) = scale * sum x * code + zero * sum x
 // and the codes themselves are the operands: a field of a code word is cut out with one logic instruction and is, in
-// place, an fp16 number -- a subnormal, field << p reads field * 2^(p - 24) for every p with the field below bit 10.
-// (The tensor core multiplies subnormals exactly.)  Fields at different p have accumulators of their own, joined with
-// powers of two when scale and zero-point are applied, once per group, in fp32.  So a pair of weights costs one
-// instruction, where turning it into fp16(code * scale + zero) costs three; weights are not rounded to fp16 on this path.
+// place, an fp16 number -- a subnormal, field << p reads field * 2^(p - 24) for every p with the field below bit 10.  The
+// tensor core multiplies subnormals exactly, but lines up what it adds by their nominal exponents: leading zeros of a
+// subnormal are bits that the sum does not have (a field at bits 0 .. 3: results off by 1.5e-6 of their norm, at bits 4 .. 7
+// by 1e-7).  So narrow fields are moved up, by a multiplication, which is not the pipe that the logic instructions keep busy.
+// The power of two goes into the scale, which is applied with the zero-point once per group, in fp32.  A pair of weights
+// costs one or two instructions, where turning it into fp16(code * scale + zero) costs three; weights are not rounded to
+// fp16 on this path.
 //
 // Steps: 32 columns of a 16-bit block, 64 of an 8-bit one, a group of 128 otherwise, so that a step is 1 to 2 KB of
 // codes.  Lane (g, t) = (lane / 4, lane % 4) multiplies part t of the step's columns, rows 4g .. 4g + 3 (as rows g and
@@ -305,14 +308,16 @@ __device__ __forceinline__ uint32_t moved_by(uint32_t x, int s) { return s >= 0 
 struct Scales {
   float s[4], z[4];
 };
+template <int F>
 __device__ __forceinline__ void load_scales(uint32_t slot, uint32_t g, Scales& m) {
+  constexpr float up = F == kFmt8 ? 16777216.0f : F == kFmt4 ? 1048576.0f : 262144.0f;   // 2^24 over the place of a code
   const uint2 s = lds8(slot + 8 * g + kStepCodes), z = lds8(slot + 8 * g + kStepCodes + 64);
   const float2 s0 = __half22float2(u32_as_h2(s.x)), s1 = __half22float2(u32_as_h2(s.y));
   const float2 z0 = __half22float2(u32_as_h2(z.x)), z1 = __half22float2(u32_as_h2(z.y));
-  m.s[0] = s0.x * 16777216.0f, m.s[1] = s0.y * 16777216.0f, m.s[2] = s1.x * 16777216.0f, m.s[3] = s1.y * 16777216.0f;
+  m.s[0] = s0.x * up, m.s[1] = s0.y * up, m.s[2] = s1.x * up, m.s[3] = s1.y * up;
   m.z[0] = z0.x, m.z[1] = z0.y, m.z[2] = z1.x, m.z[3] = z1.y;
 }
-// acc: the products of the codes, times 2^-24
+// acc: the products of the codes, over what load_scales puts on the scales
 __device__ __forceinline__ void apply_scales(const Scales& m, int h, const float (&acc)[4], float sum0, float sum1, float (&tot)[4]) {
   tot[0] = fmaf(m.s[2 * h], acc[0], fmaf(m.z[2 * h], sum0, tot[0]));
   tot[1] = fmaf(m.s[2 * h], acc[1], fmaf(m.z[2 * h], sum1, tot[1]));
@@ -321,14 +326,11 @@ __device__ __forceinline__ void apply_scales(const Scales& m, int h, const float
 }
 
 // The codes of one row's stretch of 16 columns as operands: pair(j, p) = pair j of its first (p = 0) and second eight
-// columns, as integers where they lie: at bit 0 or 4 (4 bits), 2j (two leading bits), 0 (8 bits); set(j): the accumulator
-// for that place.
+// columns, as integers at bit 0 (8 bits), 4 (4 bits) or 6.
 template <int F>
 struct Codes {
   static constexpr int up = F == kFmtP4 ? 2 : F == kFmtP3 ? 1 : 0;   // planes: bits below the leading two
   static constexpr bool third = F == kFmt3;
-  static constexpr int sets = F == kFmt8 ? 1 : F == kFmt4 ? 2 : 4;
-  static __device__ __forceinline__ constexpr int set(int j) { return sets == 1 ? 0 : sets == 2 ? j & 1 : j; }
 
   uint32_t w[4];                                  // 8 bits: the words of a stretch; 4 bits: the two; else top codes and low bits
   // stretch s of the step for this lane (8 bits: the only one)
@@ -357,12 +359,13 @@ struct Codes {
     if constexpr (F == kFmt8) {
       return __byte_perm(w[2 * p + (j >> 1)], 0, j & 1 ? 0x4342 : 0x4140);
     } else if constexpr (F == kFmt4) {
-      return ((j & 2) ? w[p] >> 8 : w[p]) & (j & 1 ? 0x00f000f0u : 0x000f000fu);
+      const uint32_t byte = j & 2 ? w[p] >> 8 : w[p];
+      return (j & 1 ? byte : byte * 16) & 0x00f000f0u;
     } else {
       constexpr uint32_t one = 0x00010001u;
       uint32_t v = w[p] & ((3u << (2 * j + up)) * one);
       if constexpr (third || up) v = and_or(w[2 + p], (third ? 4u << (2 * j) : up == 2 ? 3u << (2 * j) : 1u << (2 * j)) * one, v);
-      return v;
+      return v * (64u >> (2 * j));
     }
   }
 };
@@ -405,7 +408,7 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
       sum0 = ones[0], sum1 = ones[1];
     }
     Scales m;
-    load_scales(slot, g, m);
+    load_scales<F>(slot, g, m);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint4 wide[2];
@@ -420,7 +423,7 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
         if constexpr (C::third || C::up) h1[r] = lds4(slot + code_at<F>(2, row) + 4 * t);
         if constexpr (C::up == 2) h0[r] = lds4(slot + code_at<F>(3, row) + 4 * t);
       }
-      float acc[C::sets][4];
+      float acc[S][4];
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         C c[2];
@@ -430,20 +433,13 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
         for (int j = 0; j < 4; ++j) {
           const uint4& xs = x[2 * s + (j >> 1)];
           const uint32_t b0 = j & 1 ? xs.z : xs.x, b1 = j & 1 ? xs.w : xs.y;
-          if (s == 0 && j < C::sets) mma16_first(k, acc[C::set(j)], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
-          else mma16(acc[C::set(j)], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
+          if (j == 0) mma16_first(k, acc[s], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
+          else mma16(acc[s], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
         }
       }
-      if constexpr (C::sets == 2) {
+      if constexpr (S == 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[0][i] = fmaf(acc[1][i], 0.0625f, acc[0][i]);
-      } else if constexpr (C::sets == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[0][i] = fmaf(acc[1][i], 0.25f, acc[0][i]);
-          acc[2][i] = fmaf(acc[3][i], 0.25f, acc[2][i]);
-          acc[0][i] = fmaf(acc[2][i], 0.0625f, acc[0][i]);
-        }
+        for (int i = 0; i < 4; ++i) acc[0][i] += acc[1][i];
       }
       apply_scales(m, h, acc[0], sum0, sum1, tot[h]);
     }
