@@ -435,7 +435,8 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
 /* ---- few tokens ------------------------------------------------------------------------- */
 
 /* Products that read weight pages for a handful of tokens at a time, as decoding does.  Here the weight of a code is
- * code * scale + zero-point, not rounded to fp16 (scale and zero-point are applied to a group's sums, in fp32). */
+ * code * scale + zero-point, not rounded to fp16 (scale and zero-point are applied to a group's sums, in fp32), except
+ * where a call says otherwise. */
 
 /* out[t, col] = sum_k x[t, k] * w[col, k] (+ bias[col]) for the blocks of up to PW_LINEAR_PAGES pages side by side: the
  * columns of page i follow those of page i - 1.  A dense block of the model (queries, keys and values of one input, an
@@ -446,16 +447,21 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
  * them must be finite and does not count.  bias: device [sum of out_features] of bias_type, or NULL.  out: device
  * [T, sum of out_features] of out_type; sums in fp32 in a fixed order, rounded once.
  * Any T: the weights are read once per eight tokens (from the L2 cache after the first time).  T = 0 enqueues nothing.
- * Needs a context of the current device for its status, but neither page table nor workspace: calls on different
- * streams may run at the same time.
+ * workspace: device, or NULL.  With the bytes that pw_page_linear_workspace reports (0: the call has no use for any), many
+ * tokens with a 16-bit output go through the tensor-core kernel of the layer calls instead, with the weights rounded to
+ * fp16 like theirs; with less, or none, the call does without.  pw_page_linear_workspace is 0 for invalid arguments too.
+ * Needs a context of the current device, but neither its page table nor its workspace: calls on different streams may run
+ * at the same time, each with a workspace of its own.
  * Errors: INVALID_ARG (a null pointer, a type, n_pages, out_features below 1), SHAPE (page shapes, K or out_features
  * outside the page, a stride below the row's length, T over 2^24), BITS, STATE (a CANONICAL page; a plane the bitwidth
- * needs is missing), ALIGN (a pointer not a multiple of 16, or x_stride not a multiple of 8; the strides of a single row
- * are not looked at), CUDA. */
+ * needs is missing), ALIGN (a pointer not a multiple of 16, the workspace's of 256, or x_stride not a multiple of 8; the
+ * strides of a single row are not looked at), CUDA. */
 #define PW_LINEAR_PAGES 8
+size_t pw_page_linear_workspace(pw_ctx* ctx, int T, int K, const pw_page* pages, const int32_t* out_features, int n_pages,
+                                int out_type);
 pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp16, int64_t x_stride, const pw_page* pages,
                          const int32_t* out_features, int n_pages, const void* bias, int bias_type, void* out,
-                         int out_type, int64_t out_stride, pw_stream stream);
+                         int out_type, int64_t out_stride, void* workspace, size_t workspace_bytes, pw_stream stream);
 
 /* ---- routing of a call ----------------------------------------------------------------- */
 

@@ -31,7 +31,7 @@ EXPORTS = ("pw_workspace_bytes", "pw_create", "pw_destroy", "pw_page_bytes", "pw
            "pw_offload_page", "pw_reload_page", "pw_page_state", "pw_drop_page",
            "pw_offload_plane", "pw_reload_plane", "pw_plane_state",
            "pw_moe_forward", "pw_moe_forward_routed", "pw_moe_forward_host", "pw_quantize_scaled", "pw_add_rmsnorm", "pw_scaled_linear", "pw_route_tokens",
-           "pw_page_linear", "pw_moe_forward_few", "pw_moe_forward_few_routed",
+           "pw_page_linear", "pw_page_linear_workspace", "pw_moe_forward_few", "pw_moe_forward_few_routed",
            "pw_get_routing", "pw_route_tokens_static", "pw_observe", "pw_observation_summary", "pw_plan_step", "pw_plan_queue_create", "pw_plan_queue_destroy", "pw_plan_queue_step", "pw_plan_queue_peek", "pw_kv_pressure_bytes",
            "pw_last_device_status",
            "pw_kernel_timing", "pw_get_kernel_times", "pw_launch_count", "pw_debug_set_wait", "pw_status_str")
@@ -170,7 +170,9 @@ def load():
     L.pw_moe_forward_few_routed.restype = i32
     L.pw_moe_forward_few_routed.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, vp, i32, vp]
     L.pw_page_linear.restype = i32
-    L.pw_page_linear.argtypes = [vp, i32, i32, vp, i64, C.POINTER(pw_page), C.POINTER(C.c_int32), i32, vp, i32, vp, i32, i64, vp]
+    L.pw_page_linear.argtypes = [vp, i32, i32, vp, i64, C.POINTER(pw_page), C.POINTER(C.c_int32), i32, vp, i32, vp, i32, i64, vp, sz, vp]
+    L.pw_page_linear_workspace.restype = sz
+    L.pw_page_linear_workspace.argtypes = [vp, i32, i32, C.POINTER(pw_page), C.POINTER(C.c_int32), i32, i32]
     L.pw_moe_forward_host.restype = i32
     L.pw_moe_forward_host.argtypes = [vp, i32, vp, vp, i32, i32, vp, i32, vp]
     L.pw_route_tokens_static.restype = i32
@@ -689,12 +691,14 @@ class Context:
                        bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                        out_dtype: torch.dtype = torch.float16, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """out [T, sum of out_features] = x [T, K] . w^T (+ bias) for the blocks of the pages side by side; out_features:
-        how many rows of each page count (default: all), K may end inside the pages' last group of columns."""
+        how many rows of each page count (default: all), K may end inside the pages' last group of columns.  Many tokens
+        with a 16-bit output go through the tensor-core kernel of the layer calls, in a workspace made here."""
         if out is None:
             n = sum(p.rows for p in pages) if out_features is None else sum(out_features)
             out = self._new(stream, lambda: torch.empty(x.shape[0], n, dtype=out_dtype, device=self.device))
         st = (_pwtorch or _load_pwtorch()).page_linear(self._ptr, self._index, None if stream is None else stream.cuda_stream, x,
-                                                       pages, out_features, bias, out)
+                                                       pages, out_features, bias, out, lambda n: self._new(
+                                                           stream, lambda: torch.empty(n, dtype=torch.uint8, device=self.device)))
         if st:
             self._refused(st, "pw_page_linear", ("x", "pages", "out_features", "bias", "out"))
         return out

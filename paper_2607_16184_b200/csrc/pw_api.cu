@@ -126,6 +126,7 @@ extern "C" pw_status pw_create(pw_ctx** out, const pw_config* cfg) {
   ctx->last_T = ctx->last_k = 0;
   ctx->few_ready = 0;
   ctx->few_layer_ready = false;
+  ctx->dense_encode = nullptr;
   ctx->tc_state = nullptr;
   ctx->wait_polls = 0;
   ctx->test_hook = 0;

@@ -124,6 +124,7 @@ struct pw_ctx {
   std::atomic<int> max_clusters[5];   // clusters of that product's CTAs that run at the same time, by size
   std::atomic<int> few_clusters[3];   // the same for the kernels for few tokens: clusters of 2, 4, 8 of their CTAs
   std::atomic<int> few_ready;     // those are looked up
+  std::atomic<void*> dense_encode;    // driver entry point for tensor maps, once the dense product's kernels have their attributes
   bool few_layer_ready;           // the few-token layer's kernels have their attributes
   void* tc_state;                 // tensor-core path state (set up lazily)
   uint32_t wait_polls;            // limit of the device-side waits in polls of 20 us (0 = the default, 2 s)
@@ -179,6 +180,17 @@ pw_status check_forward(pw_ctx* ctx, int layer, const void* hidden, const Routin
 pw_status launch_ffn_simt(pw_ctx* ctx, int layer, int T, int k, cudaStream_t s);
 pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, int ksplit, cudaStream_t s);
 int tensor_token_tile(const pw_ctx* ctx, int T, int k);
+// A dense product on pages by the tensor-core kernel of the down projection.  The caller gives T, cols, pages and the rows of
+// each that count; dense_plan fills in the rest and returns the bytes of workspace (0: too large).
+struct DenseCall {
+  pw_page page[PW_LINEAR_PAGES];
+  int32_t features[PW_LINEAR_PAGES];
+  int T, cols, n_pages;
+  int nt_tile, token_tiles, splits, units, width, Rpad;
+};
+size_t dense_plan(DenseCall* d, int sms);
+pw_status launch_dense(pw_ctx* ctx, const DenseCall& d, const void* x, size_t x_pitch, int x_bytes, const void* bias, int bias_type, void* out, int out_type,
+                       int64_t ld_out, void* workspace, cudaStream_t s);
 void tc_teardown(pw_ctx* ctx);
 // records timing event `i` of the current forward call (no-op unless timing is enabled)
 void timing_mark(pw_ctx* ctx, int i, cudaStream_t s);

@@ -322,14 +322,30 @@ static pw_status check_page(const pw_page& p) {
   return PW_OK;
 }
 
-extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp16, int64_t x_stride, const pw_page* pages,
-                                    const int32_t* out_features, int n_pages, const void* bias, int bias_type, void* out,
-                                    int out_type, int64_t out_stride, pw_stream stream) {
-  if (!ctx || T < 0 || K < 1 || !pages || n_pages < 1 || n_pages > PW_LINEAR_PAGES || !type_ok(out_type) || (bias && !type_ok(bias_type)))
-    return PW_ERR_INVALID_ARG;
+// Whether a call goes through the tensor-core kernel of the layer calls (three launches, and weights rounded to fp16, which
+// an fp32 output would show), and what of its cut does not depend on the device; the pages have been checked.  By estimates
+// of both times in us, linear in the weights (millions) and the tokens; measured, here / there, at 4 bits: 4096 x 4096
+// 24 tokens 9.2 / 12.8, 64 tokens 17.2 / 15.7; 14336 x 4096 17 tokens 23.7 / 21.0, 64 tokens 48.8 / 26.9, 256 tokens - / 63;
+// 1000 x 1024 64 tokens 3.9 / 11.5.
+static bool many_tokens(DenseCall* d, int T, const pw_page* pages, const int32_t* out_features, int n_pages, int out_type) {
+  if (T <= kUnitCols || out_type == PW_F32) return false;
+  double m = 0;
+  for (int i = 0; i < n_pages; ++i) m += 1e-6 * pages[i].cols * (out_features ? out_features[i] : (int32_t)pages[i].rows);
+  if (2.5 + (T + kUnitCols - 1) / kUnitCols * (0.115 * m + 0.1) <= 10. + m * (0.137 + 0.0032 * T)) return false;
+  *d = DenseCall{};
+  d->T = T;
+  d->cols = (int)pages[0].cols;
+  d->n_pages = n_pages;
+  for (int i = 0; i < n_pages; ++i) {
+    d->page[i] = pages[i];
+    d->features[i] = out_features ? out_features[i] : (int32_t)pages[i].rows;
+  }
+  return true;
+}
+static pw_status check_pages(int T, int K, const pw_page* pages, const int32_t* out_features, int n_pages) {
+  if (T < 0 || K < 1 || !pages || n_pages < 1 || n_pages > PW_LINEAR_PAGES) return PW_ERR_INVALID_ARG;
   if (T > 1 << 24) return PW_ERR_SHAPE;
-  PageLinearArgs a{};
-  int64_t slices = 0, columns = 0;
+  int64_t columns = 0;
   for (int i = 0; i < n_pages; ++i) {
     const pw_page& p = pages[i];
     const pw_status ps = check_page(p);
@@ -337,6 +353,29 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
     const int64_t n = out_features ? out_features[i] : (int64_t)p.rows;
     if (n < 1) return PW_ERR_INVALID_ARG;
     if (n > p.rows || K > (int64_t)p.cols || K <= (int64_t)p.cols - kGroup || p.cols != pages[0].cols) return PW_ERR_SHAPE;
+    columns += n;
+    if (columns > 1 << 30) return PW_ERR_SHAPE;
+  }
+  return PW_OK;
+}
+
+extern "C" size_t pw_page_linear_workspace(pw_ctx* ctx, int T, int K, const pw_page* pages, const int32_t* out_features, int n_pages, int out_type) {
+  DenseCall d;
+  if (!ctx || !type_ok(out_type) || check_pages(T, K, pages, out_features, n_pages) != PW_OK || !many_tokens(&d, T, pages, out_features, n_pages, out_type)) return 0;
+  return dense_plan(&d, ctx->num_sms);
+}
+
+extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp16, int64_t x_stride, const pw_page* pages,
+                                    const int32_t* out_features, int n_pages, const void* bias, int bias_type, void* out,
+                                    int out_type, int64_t out_stride, void* workspace, size_t workspace_bytes, pw_stream stream) {
+  if (!ctx || !type_ok(out_type) || (bias && !type_ok(bias_type))) return PW_ERR_INVALID_ARG;
+  const pw_status cs = check_pages(T, K, pages, out_features, n_pages);
+  if (cs != PW_OK) return cs;
+  PageLinearArgs a{};
+  int64_t slices = 0, columns = 0;
+  for (int i = 0; i < n_pages; ++i) {
+    const pw_page& p = pages[i];
+    const int64_t n = out_features ? out_features[i] : (int64_t)p.rows;
     LinearPage& l = a.page[i];
     l.codes = static_cast<const char*>(p.codes);
     l.bit1 = static_cast<const char*>(p.scales);
@@ -346,15 +385,20 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
     l.col0 = (int)columns;
     slices += (n + kUnitRows - 1) / kUnitRows;
     columns += n;
-    if (columns > 1 << 30) return PW_ERR_SHAPE;
     l.end = (int)slices;
   }
   if (T == 0) return PW_OK;
   if (!x_fp16 || !out) return PW_ERR_INVALID_ARG;
   if (T > 1 && (x_stride < K || out_stride < columns)) return PW_ERR_SHAPE;
-  if (!is_aligned(x_fp16, 16) || !is_aligned(out, 16) || !is_aligned(bias, 16) || (T > 1 && x_stride % 8)) return PW_ERR_ALIGN;
+  if (!is_aligned(x_fp16, 16) || !is_aligned(out, 16) || !is_aligned(bias, 16) || !is_aligned(workspace, 256) || (T > 1 && x_stride % 8)) return PW_ERR_ALIGN;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
+  DenseCall d;
+  if (workspace && many_tokens(&d, T, pages, out_features, n_pages, out_type)) {
+    const size_t need = dense_plan(&d, ctx->num_sms);
+    if (need && need <= workspace_bytes)
+      return launch_dense(ctx, d, x_fp16, (size_t)x_stride * 2, 2 * K, bias, bias_type, out, out_type, out_stride, workspace, stream);
+  }
   const pw_status fs = few_setup(ctx);
   if (fs != PW_OK) return fs;
   a.x = static_cast<const char*>(x_fp16);

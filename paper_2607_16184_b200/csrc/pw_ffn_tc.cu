@@ -62,6 +62,7 @@
 #include "pw_common.cuh"
 #include "pw_layout.cuh"
 #include "pw_ptx.cuh"
+#include "pw_scaled.cuh"
 
 namespace pw {
 
@@ -1315,6 +1316,32 @@ static bool planes_layer(const pw_ctx* ctx, int layer) {     // does the layer h
   return false;
 }
 
+// Shared-memory plan of a kernel.  The issuers of a matrix work on as many token tiles at once as there are
+// partial accumulators per matrix (the kernel's own rule, repeated here); one more slot keeps a tile on its
+// way.  The rest of the 227 KB goes to the weight ring.
+static bool plan_slots(int phase, int nt_tile, int* n_bslots, int* n_slots, int* smem) {
+  const int bslot_bytes = nt_tile * 256;
+  const int nmat = phase == 0 ? 2 : 1;
+  int npart = kIssuers / nmat;
+  while (npart > 1 && nmat * npart * nt_tile + kMaxASlots * 64 > kTmemCols) npart >>= 1;
+  // every issuer of a matrix works on a token tile of its own, one more is on its way -- fewer when the tiles are
+  // so wide that the weight ring would fall below six slots
+  const int ipa = phase == 0 && nt_tile > 64 ? kIssuers / nmat : npart;   // active issuers per matrix (the kernel's rule)
+  int nb = ipa + 1 > kMaxBSlots ? kMaxBSlots : ipa + 1;
+  int ns = 0;
+  for (;; --nb) {
+    ns = (kMaxDynSmem - kCtrlBytes - nb * bslot_bytes) / kSlotBytes;
+    if (ns > kMaxSlots) ns = kMaxSlots;
+    ns &= ~1;                                    // an even number of slots: one set per producer
+    if (ns >= 6 || nb <= npart + 1) break;
+  }
+  if (ns < 6) return false;                      // the dequantizers advance up to six slot items at a time
+  *n_bslots = nb;
+  *n_slots = ns;
+  *smem = kCtrlBytes + ns * kSlotBytes + nb * bslot_bytes;
+  return true;
+}
+
 pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, int ksplit, cudaStream_t s) {
   const pw_config& c = ctx->cfg;
   const WsMap& w = ctx->ws;
@@ -1322,31 +1349,9 @@ pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, i
   pw_status pst = tc_setup(ctx);
   if (pst != PW_OK) return pst;
   const TcState* st = reinterpret_cast<const TcState*>(ctx->tc_state);
-  const int bslot_bytes = nt_tile * 256;
-  // Shared-memory plan per kernel.  The issuers of a matrix work on as many token tiles at once as there are
-  // partial accumulators per matrix (the kernel's own rule, repeated here); one more slot keeps a tile on its
-  // way.  The rest of the 227 KB goes to the weight ring.
   int n_bslots[2], n_slots[2], smem[2];
-  for (int phase = 0; phase < 2; ++phase) {
-    const int nmat = phase == 0 ? 2 : 1;
-    int npart = kIssuers / nmat;
-    while (npart > 1 && nmat * npart * nt_tile + kMaxASlots * 64 > kTmemCols) npart >>= 1;
-    // every issuer of a matrix works on a token tile of its own, one more is on its way -- fewer when the tiles are
-    // so wide that the weight ring would fall below six slots
-    const int ipa = phase == 0 && nt_tile > 64 ? kIssuers / nmat : npart;   // active issuers per matrix (the kernel's rule)
-    int nb = ipa + 1 > kMaxBSlots ? kMaxBSlots : ipa + 1;
-    int ns = 0;
-    for (;; --nb) {
-      ns = (kMaxDynSmem - kCtrlBytes - nb * bslot_bytes) / kSlotBytes;
-      if (ns > kMaxSlots) ns = kMaxSlots;
-      ns &= ~1;                                  // an even number of slots: one set per producer
-      if (ns >= 6 || nb <= npart + 1) break;
-    }
-    n_bslots[phase] = nb;
-    if (ns < 6) return PW_ERR_NOMEM;             // the dequantizers advance up to six slot items at a time
-    n_slots[phase] = ns;
-    smem[phase] = kCtrlBytes + ns * kSlotBytes + n_bslots[phase] * bslot_bytes;
-  }
+  for (int phase = 0; phase < 2; ++phase)
+    if (!plan_slots(phase, nt_tile, &n_bslots[phase], &n_slots[phase], &smem[phase])) return PW_ERR_NOMEM;
   const int R = T * k + c.n_shared * T;
   const DevRow* rows = reinterpret_cast<const DevRow*>(b + w.table) + (size_t)layer * w.S * 3;
   int32_t* status = reinterpret_cast<int32_t*>(b + w.status);
@@ -1373,6 +1378,183 @@ pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, i
                               (size_t)R * c.hidden, work_counter + 1, status, reinterpret_cast<int32_t*>(b + w.done), ksplit, c.ffn / kTileRows, 0u));
   ctx->launches += 2;
   PW_CUDA_OK(cudaGetLastError());
+  return PW_OK;
+}
+
+// ---- dense product for many tokens -----------------------------------------------------------------
+// The down kernel on pages that are no layer's: a "segment" is a page, whose row tiles are numbered on from those of the
+// page before it.  The kernel ahead of it writes what the layer's call has from its routing: the operand in k-chunk-major
+// form, the page rows, the unit list (K range outermost, then row tile, then token tile), and completion counters that no
+// unit has to wait for.
+struct DenseWs {
+  size_t rows, units, done, counters, xt, y, total;
+};
+static DenseWs dense_ws(const DenseCall& d) {
+  DenseWs w{};
+  auto take = [&](size_t bytes) {
+    const size_t at = w.total;
+    w.total = align_up(w.total + bytes, 256);
+    return at;
+  };
+  w.rows = take(sizeof(DevRow) * 3 * d.n_pages);
+  w.units = take(sizeof(Unit) * (size_t)d.units);
+  w.done = take(4 * (size_t)d.T * d.splits);
+  w.counters = take(256);
+  w.xt = take((size_t)d.cols * 2 * d.Rpad);
+  w.y = take(4 * (size_t)d.splits * d.T * d.width);
+  return w;
+}
+// Fills in how a product is cut; the weights' rows in tiles of 128, the tokens as in the layer's call, the contraction into
+// as many parts as finish soonest (the rule of the layer's call).
+size_t dense_plan(DenseCall* d, int sms) {
+  const int ng = d->cols / kGroup;
+  d->nt_tile = (d->T + 15) & ~15;
+  const int cap = d->T > 64 ? 128 : 64;
+  if (d->nt_tile > cap) d->nt_tile = cap;
+  int64_t tiles = 0;
+  for (int i = 0; i < d->n_pages; ++i) tiles += (d->features[i] + kTileRows - 1) / kTileRows;
+  d->width = (int)(tiles * kTileRows);
+  d->token_tiles = (d->T + d->nt_tile - 1) / d->nt_tile;
+  const int64_t units = tiles * d->token_tiles;
+  int64_t best = -1;
+  d->splits = 1;
+  for (int ks = 1; ks <= 8 && ks <= ng; ++ks) {
+    const int64_t rounds = (units * ks + sms - 1) / sms, cost = rounds * (3 + (ng + ks - 1) / ks);
+    if (best < 0 || cost < best) {
+      best = cost;
+      d->splits = ks;
+    }
+  }
+  if (units * d->splits > 0x3fffffff || (int64_t)d->T * d->splits > 0x3fffffff) return 0;
+  d->units = (int)(units * d->splits);
+  d->Rpad = d->token_tiles * d->nt_tile < 128 ? 128 : d->token_tiles * d->nt_tile;   // at least a box of the widest map
+  return dense_ws(*d).total;
+}
+
+__global__ void __launch_bounds__(256) dense_prepare_kernel(const __grid_constant__ DenseCall d, const char* x, size_t x_pitch, int x_bytes, DevRow* __restrict__ rows,
+                                                            Unit* __restrict__ units, int32_t* __restrict__ done, int32_t* __restrict__ counters,
+                                                            uint4* __restrict__ xt) {
+  grid_dep_sync();
+  const int threads = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + threadIdx.x;
+  const int ng = d.cols / kGroup, row_tiles = d.width / kTileRows;
+  if (first < 4) counters[first] = first == 3 ? d.units : 0;   // [0] the work counter, [2 + phase] units
+  if (first < d.n_pages) {
+    int base = 0;                                  // row tiles of the pages before this one
+    for (int i = 0; i < first; ++i) base += (d.features[i] + kTileRows - 1) / kTileRows;
+    const pw_page& p = d.page[first];
+    const bool planes = p.layout == PW_LAYOUT_PLANES;
+    const ptrdiff_t tiles = (ptrdiff_t)base * ng;
+    DevRow r{};
+    r.codes = static_cast<const char*>(p.codes) - tiles * (ptrdiff_t)(planes ? kPlaneTopTile : tile_bytes(p.bits));
+    r.bit1 = planes ? static_cast<const char*>(p.scales) - tiles * kPlaneBitTile : nullptr;
+    r.bit0 = planes ? static_cast<const char*>(p.zps) - tiles * kPlaneBitTile : nullptr;
+    r.rows = p.rows;
+    r.cols = p.cols;
+    r.bits = p.bits;
+    r.valid = planes ? 2 : 1;
+    rows[first * 3 + 2] = r;
+  }
+  for (int u = first; u < d.units; u += threads) {
+    const int j = u % d.token_tiles, rs = u / d.token_tiles, rt = rs % row_tiles, sp = rs / row_tiles;
+    int page = 0, end = (d.features[0] + kTileRows - 1) / kTileRows;
+    while (rt >= end) end += (d.features[++page] + kTileRows - 1) / kTileRows;
+    Unit un{};
+    un.seg = page;
+    un.row_tile = rt;
+    un.tok0 = j * d.nt_tile;
+    un.ntok = min(d.nt_tile, d.T - un.tok0);
+    un.g0 = (int)((int64_t)sp * ng / d.splits);
+    un.g1 = (int)((int64_t)(sp + 1) * ng / d.splits);
+    un.split = sp;
+    units[u] = un;
+  }
+  for (int64_t i = first; i < (int64_t)d.T * d.splits; i += threads) done[i] = 0x3fffffff;
+  // operand rows, 16 bytes a thread; columns past the end are zero
+  const int64_t chunks = (int64_t)(d.cols / 8) * d.Rpad;
+  for (int64_t i = first; i < chunks; i += threads) {
+    const int c = (int)(i / d.Rpad), n = (int)(i - (int64_t)c * d.Rpad);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (n < d.T) {
+      const char* src = x + (size_t)n * x_pitch + (size_t)c * 16;
+      const int left = x_bytes - c * 16;
+      if (left >= 16) {
+        v = *reinterpret_cast<const uint4*>(src);
+      } else if (left > 0) {
+        uint32_t w[4] = {0, 0, 0, 0};
+        for (int k = 0; k < left / 2; ++k) w[k >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[k] << (16 * (k & 1));
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    xt[i] = v;
+  }
+}
+
+// out[t, column] = sum of the parts of the contraction, in their order (+ bias), rounded once.
+__global__ void __launch_bounds__(256) dense_finish_kernel(const __grid_constant__ DenseCall d, const float* y, const void* bias, int bias_type, void* __restrict__ out,
+                                                           int out_type, int64_t ld_out) {
+  grid_dep_sync();
+  grid_dep_trigger();
+  const int t = blockIdx.y;
+  const size_t stride = (size_t)d.T * d.width;
+  for (int c = blockIdx.x * blockDim.x + threadIdx.x; c < d.width; c += gridDim.x * blockDim.x) {
+    int page = 0, col0 = 0, pad0 = 0;              // first column of the page, in the output and in y
+    while (page < d.n_pages) {
+      const int wide = (d.features[page] + kTileRows - 1) / kTileRows * kTileRows;
+      if (c < pad0 + wide) break;
+      pad0 += wide;
+      col0 += d.features[page++];
+    }
+    if (c - pad0 >= d.features[page]) continue;
+    const int to = col0 + c - pad0;
+    const float* from = y + (size_t)t * d.width + c;
+    float v = from[0];
+    for (int s = 1; s < d.splits; ++s) v = __fadd_rn(v, from[s * stride]);
+    if (bias) v = __fadd_rn(v, load1(bias, to, bias_type));
+    store1(out, (int64_t)t * ld_out + to, out_type, v);
+  }
+}
+
+pw_status launch_dense(pw_ctx* ctx, const DenseCall& d, const void* x, size_t x_pitch, int x_bytes, const void* bias, int bias_type, void* out, int out_type,
+                       int64_t ld_out, void* workspace, cudaStream_t s) {
+  void* fn = ctx->dense_encode.load(std::memory_order_acquire);
+  if (!fn) {                                       // (any number of threads may do this: all find the same)
+    cudaDriverEntryPointQueryResult found;
+    PW_CUDA_OK(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
+    if (!fn || found != cudaDriverEntryPointSuccess) return PW_ERR_CUDA;
+    for (int i = 0; i < 4; ++i) {
+      PW_CUDA_OK(cudaFuncSetAttribute(ffn_kernel_of(1, i & 1, i >> 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
+      PW_CUDA_OK(cudaFuncSetAttribute(ffn_kernel_of(1, 0, i >> 1, 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
+    }
+    ctx->dense_encode.store(fn, std::memory_order_release);
+  }
+  const DenseWs w = dense_ws(d);
+  char* b = static_cast<char*>(workspace);
+  TmapSet maps;
+  if (!make_maps(reinterpret_cast<EncodeTiledFn>(fn), b + w.xt, d.cols / 8, d.Rpad, &maps)) return PW_ERR_CUDA;
+  int n_bslots, n_slots, smem, planes = 0;
+  if (!plan_slots(1, d.nt_tile, &n_bslots, &n_slots, &smem)) return PW_ERR_NOMEM;
+  for (int i = 0; i < d.n_pages; ++i) planes |= d.page[i].layout == PW_LAYOUT_PLANES;
+  const bool help = d.nt_tile > 64;
+  const int share = (d.cols / kGroup + d.splits - 1) / d.splits <= kShortUnitTiles;
+  int32_t* counters = reinterpret_cast<int32_t*>(b + w.counters);
+  int32_t* status = reinterpret_cast<int32_t*>(ctx->base + ctx->ws.status);
+  const int64_t chunks = (int64_t)(d.cols / 8) * d.Rpad;
+  const int64_t blocks = (chunks + 255) / 256;
+  const int most = 8 * ctx->num_sms;
+  PW_CUDA_OK(launch_dependent(dense_prepare_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, d, static_cast<const char*>(x), x_pitch,
+                              x_bytes, reinterpret_cast<DevRow*>(b + w.rows), reinterpret_cast<Unit*>(b + w.units), reinterpret_cast<int32_t*>(b + w.done), counters,
+                              reinterpret_cast<uint4*>(b + w.xt)));
+  // (launched without overlap: what the kernel reads of its list and counters before it waits for anything is the work of
+  // the kernel directly ahead)
+  ffn_kernel_of(1, help, planes, share)<<<dim3(ctx->num_sms), dim3(kThreads), (size_t)smem, s>>>(
+      reinterpret_cast<const DevRow*>(b + w.rows), reinterpret_cast<const Unit*>(b + w.units), counters + 2, maps, d.Rpad, d.nt_tile, n_bslots, n_slots,
+      (__half*)nullptr, reinterpret_cast<float*>(b + w.y), d.width, (size_t)d.T * d.width, counters, status, reinterpret_cast<int32_t*>(b + w.done), d.splits,
+      d.cols / kTileRows, 0u);
+  PW_CUDA_OK(cudaGetLastError());
+  const int columns = (d.width + 255) / 256;
+  PW_CUDA_OK(launch_dependent(dense_finish_kernel, dim3(columns < 64 ? columns : 64, d.T), dim3(256), 0, s, d, reinterpret_cast<const float*>(b + w.y), bias,
+                              bias_type, out, out_type, ld_out));
+  ctx->launches += 3;
   return PW_OK;
 }
 

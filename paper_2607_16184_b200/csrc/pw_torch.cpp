@@ -286,9 +286,9 @@ bool page_header(Call& c, PyObject* o, int arg, pw_page* out) {
   return true;
 }
 
-// x, pages, out_features, bias, out
+// x, pages, out_features, bias, out, and a function that makes a workspace of so many bytes
 PyObject* page_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  return guarded(args, n, 8, [](Call& c, PyObject* const* a) -> int {
+  return guarded(args, n, 9, [](Call& c, PyObject* const* a) -> int {
     const Matrix x = matrix(c, a[0], 1, PW_F16);
     pw_page page[PW_LINEAR_PAGES];
     int32_t features[PW_LINEAR_PAGES];
@@ -317,9 +317,17 @@ PyObject* page_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a[3] != Py_None) bias = vector(c, a[3], 4, -1, total);
     const Matrix out = matrix(c, a[4], 5, -1, x.rows, total);
     if (c.bad) return c.bad;
+    const size_t bytes = pw_page_linear_workspace(c.ctx, (int)x.rows, (int)x.cols, page, features, (int)count, out.type);
+    Ref made(nullptr);
+    void* workspace = nullptr;
+    if (bytes) {
+      made.o = PyObject_CallFunction(a[5], "n", (Py_ssize_t)bytes);
+      if (!made.o) return 0;
+      workspace = THPVariable_Unpack(made.o).data_ptr();
+    }
     Outside outside(c);
     return pw_page_linear(c.ctx, (int)x.rows, (int)x.cols, x.data, x.stride, page, features, (int)count, bias.data, bias.type, out.data, out.type, out.stride,
-                          c.stream);
+                          workspace, bytes, c.stream);
   });
 }
 

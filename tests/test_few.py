@@ -26,12 +26,12 @@ def page(codes=P, scales=None, zps=None, rows=256, cols=256, group=128, bits=4, 
     return B.pw_page(codes, scales, zps, rows, cols, group, bits, layout)
 
 
-def linear(lib, ctx, T=2, K=200, x=P, x_stride=200, pages=None, n=None, n_pages=None, bias=None, bias_type=0, out=P, out_type=1, out_stride=512):
+def linear(lib, ctx, T=2, K=200, x=P, x_stride=200, pages=None, n=None, n_pages=None, bias=None, bias_type=0, out=P, out_type=1, out_stride=512, workspace=None):
     pages = [page()] if pages is None else pages
     a = (B.pw_page * max(1, len(pages)))(*pages)
     f = None if n is None else (C.c_int32 * len(n))(*n)
     return lib.pw_page_linear(ctx, T, K, x, x_stride, a if pages else None, f, len(pages) if n_pages is None else n_pages, bias, bias_type, out,
-                              out_type, out_stride, None)
+                              out_type, out_stride, workspace, 0, None)
 
 
 PLANES = B.PW_LAYOUT_PLANES
@@ -47,7 +47,7 @@ PLANES = B.PW_LAYOUT_PLANES
     (BITS, dict(pages=[page(bits=5)])), (BITS, dict(pages=[page(bits=8, layout=PLANES)])), (BITS, dict(pages=[page(bits=16, layout=PLANES)])),
     (STATE, dict(pages=[page(layout=B.PW_LAYOUT_CANONICAL)])), (STATE, dict(pages=[page(bits=3, layout=PLANES)])),
     (STATE, dict(pages=[page(bits=4, scales=P, layout=PLANES)])), (ALIGN, dict(x=P + 8)), (ALIGN, dict(x_stride=204)), (ALIGN, dict(out=P + 4)),
-    (ALIGN, dict(bias=P + 4)), (ALIGN, dict(pages=[page(codes=P + 8)])), (ALIGN, dict(pages=[page(bits=3, scales=P + 8, layout=PLANES)])),
+    (ALIGN, dict(bias=P + 4)), (ALIGN, dict(workspace=P + 16)), (ALIGN, dict(pages=[page(codes=P + 8)])), (ALIGN, dict(pages=[page(bits=3, scales=P + 8, layout=PLANES)])),
     (OK, dict(T=0)), (OK, dict(T=0, x=None, out=None)), (OK, dict(T=0, pages=[page(bits=2, layout=PLANES)] * 8, n=[1] * 8))])
 def test_page_linear_refuses(lib, ctx, status, change):
     assert linear(lib, ctx, **change) == status

@@ -148,6 +148,57 @@ def test_products_repeat(ctx):
     assert torch.equal(ctx.pw_page_linear(y, pages, out_dtype=F32).flip(0), out)
 
 
+@pytest.mark.parametrize("T,K,sizes,formats,kernels", [
+    (1200, 128, [40], ["4"], 3), (700, 300, [130, 1, 300], ["16", "p3", "8"], 3), (64, 4096, [6000], ["2"], 3), (300, 1000, [1260], ["p4"], 1),
+    (600, 1000, [1260], ["p4"], 3), (130, 2050, [3129, 64], ["3", "4"], 3), (600, 640, [100], ["p2"], 3), (1000, 40, [133], ["16"], 3),
+    (70, 14336, [1128], ["8"], 3), (33, 8192, [2500, 2000], ["4", "4"], 3)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_product_of_many_tokens(ctx, T, K, sizes, formats, kernels, dtype):
+    """16-bit outputs of many tokens: weights are rounded to fp16, half a step each, where that many kernels run."""
+    g = gen(T)
+    pages = [plain.make_page(ctx, block_weights(g, n, K), f) for n, f in zip(sizes, formats)]
+    x, bias = operand(g, T, K, pitch=up(K)), normal(g, sum(sizes)) * 3
+    whole = torch.full((T, sum(sizes) + 5), 7.0, dtype=dtype, device="cuda")
+    launches = ctx.pw_launch_count()
+    out = ctx.pw_page_linear(x, pages, out_features=sizes, bias=bias, out=whole[:, :sum(sizes)])
+    assert ctx.pw_launch_count() - launches == kernels and ctx.pw_last_device_status() == 0
+    want, bound = [], []
+    for n, p in zip(sizes, pages):
+        block = [m[:n] for m in plain.stored(ctx, p)]
+        y, d = plain.product(f64(x), block)
+        w = np.abs(block[0] * block[1] + block[2])[:, :K]
+        want.append(y)
+        bound.append(d + (0 if p.bits == 16 else np.abs(f64(x)) @ (w * 2.0 ** -11 + 2.0 ** -25).T))
+    want, bound = np.concatenate(want, 1) + f64(bias), np.concatenate(bound, 1)
+    check(out, want, bound + (np.abs(want) + bound) * 2.0 ** -24, dtype)
+    assert torch.all(whole[:, sum(sizes):] == 7.0)
+    assert torch.equal(ctx.pw_page_linear(x, pages, out_features=sizes, bias=bias, out_dtype=dtype), out)
+
+
+def test_many_tokens_in_a_graph_and_on_two_streams(ctx):
+    g = gen(31)
+    page = plain.make_page(ctx, block_weights(g, 1000, 1024), "4")
+    xs = [operand(g, T, 1024) for T in (400, 300)]
+    want = [ctx.pw_page_linear(x, [page]) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    outs = [[torch.empty_like(w) for _ in range(10)] for w in want]
+    for i in range(10):
+        for x, s, o in zip(xs, streams, outs):
+            ctx.pw_page_linear(x, [page], out=o[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for w, many in zip(want, outs) for o in many)
+    out = torch.empty_like(want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.pw_page_linear(xs[0], [page], out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0])
+
+
 def test_no_tokens(ctx):
     page = plain.make_page(ctx, block_weights(gen(6), 40, 256), "4")
     out = ctx.pw_page_linear(torch.empty(0, 256, dtype=F16, device="cuda"), [page], out_features=[40])
