@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 
   const Fixed fixed;
   const uint32_t ring = smem_u32(smem) + warp * kRing;
-  Ring r{ring, ring, (uint32_t)slot_bytes(0), lane};
+  Ring r{ring, ring, lane};
   Feed f;
   f.left = 0;
   int next = 0;                                   // slice the feed takes next
@@ -111,10 +111,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
   auto ask_next = [&](uint32_t slot) {
     if (f.left == 0 && !more()) return;
     if constexpr (F == kAnyFormat) {
-      ask_any<false>(f, slot, lane);
+      ask_any<0>(f, slot, lane);
     } else {
       f.left--;
-      ask<F, false>(f, slot, lane);
+      ask<F, 0>(f, slot, lane);
     }
   };
 
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
       ask_next(r.slot);
-      ring_on<STAGES>(r);
+      ring_on<0, STAGES>(r);
     }
     if (!waited) {
       grid_dep_sync();
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
         const int steps = my_groups << step_shift(fmt), lo = (steps * member) >> ts;
         float tot[2][4] = {};
         Operand o{x_lane, sum0, sum1, a.room, (uint32_t)(xc & 1) << 2, lo};
-        walk<F, false, STAGES>(fixed, fmt, 0, ((steps * (member + 1)) >> ts) - lo, f, r, o, tot, ask_next);
+        walk<F, 0, STAGES>(fixed, fmt, ((steps * (member + 1)) >> ts) - lo, f, r, o, tot, ask_next);
         put_sums(sums + member * kSumFloats, lane, tot);
         team_sync(team, ts);
 #pragma unroll 1
@@ -331,7 +331,7 @@ static bool many_tokens(DenseCall* d, int T, const pw_page* pages, const int32_t
   if (T <= kUnitCols || out_type == PW_F32) return false;
   double m = 0;
   for (int i = 0; i < n_pages; ++i) m += 1e-6 * pages[i].cols * (out_features ? out_features[i] : (int32_t)pages[i].rows);
-  if (2.5 + (T + kUnitCols - 1) / kUnitCols * (0.115 * m + 0.1) <= 10. + m * (0.137 + 0.0032 * T)) return false;
+  if (2.5 + (T + kUnitCols - 1) / kUnitCols * (0.1 * m + 0.1) <= 10. + m * (0.137 + 0.0032 * T)) return false;
   *d = DenseCall{};
   d->T = T;
   d->cols = (int)pages[0].cols;

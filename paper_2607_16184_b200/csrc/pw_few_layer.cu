@@ -38,7 +38,6 @@ struct FewArgs {
   int segs, pairs;                                // room for active experts and for their (expert, token) pairs
   int n_parts;                                    // parts of the down blocks' columns
   uint32_t per_part;                              // 2^32 / n_parts, rounded up
-  int slot2;                                      // bytes of a slot of phase 2
 };
 
 // Tables in shared memory, built once per call.
@@ -247,9 +246,7 @@ __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, int fg, in
   if (lane == 0) to[segs] = carry;
 }
 
-// Both phases go through one loop: its code is by far the largest part of the kernel, and what a phase finds in the
-// instruction cache it does not wait for.
-template <class TAB, int STAGES>
+template <class TAB, int XC, int STAGES>
 __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __grid_constant__ FewArgs p) {
   extern __shared__ __align__(128) char smem[];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -260,7 +257,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   // ---- routing ----
   // phase 1: sums [16 warps], rings, staged operand; phase 2: sums [16 warps][T tokens], rings
   char* const ring1 = smem + kTableBytes<TAB> + kStreamWarps * kSumFloats * 4;
-  char* const pieces = ring1 + kStreamWarps * STAGES * slot_bytes(0);
+  float* const xsum = reinterpret_cast<float*>(ring1 + kStreamWarps * STAGES * slot_bytes(0));
+  char* const pieces = reinterpret_cast<char*>(xsum) + ((hg * 3 * p.T * 4 + 127) & ~127);
   // a few warps route and make the tables; the others bring the tokens into shared memory and ask the L2 cache for the
   // shared experts, which are wanted whatever the routing is
   if (warp < kFewRouters) {
@@ -298,7 +296,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 #pragma unroll 1
       for (size_t l = line; l < page_lines; l += lines) prefetch_line(page + l * 128);
     }
-    stage_operand(p.hidden, (size_t)p.H * 2, p.T, p.T, 0, hg, p.H * 2, pieces, nullptr, thread, threads);
+    stage_operand(p.hidden, (size_t)p.H * 2, p.T, p.T, 0, hg, p.H * 2, pieces, xsum, thread, threads);
   }
   __syncthreads();
   const int segs = t.count[0];
@@ -320,184 +318,49 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   const int G = (int)gridDim.x, b = (int)blockIdx.x;
   uint32_t before;                                // arrivals, seen before this CTA's: only the top bit matters
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(before) : "l"(p.sync) : "memory");
-  const int steps = t.step0[segs];                // of phase 2, in a slice
-  bool down = false;                              // phase 2
-  // Units of a CTA.  Phase 1: units, heaviest first, are dealt out in turn, the turns in alternating order.  A CTA does four
-  // at a time, each by a team of warps.
-  int mine = t.unit0[segs] / G + ((t.unit0[segs] / G) & 1 ? G - 1 - b < t.unit0[segs] % G : b < t.unit0[segs] % G);
-  auto unit_of = [&](int i) { return i * G + (!down && (i & 1) ? G - 1 - b : b); };
-  auto slice_of = [&](int unit) { return p.n_parts == 1 ? unit : (int)__umulhi((uint32_t)unit, p.per_part); };   // unit / n_parts
-  auto range = [&](int unit, int ts, int member, int& lo, int& hi) {
-    // phase 2: steps * i / (n_parts << ts), rounded down (steps * i is below 2^24)
-    const uint32_t i = ((uint32_t)(unit - slice_of(unit) * p.n_parts) << ts) + member;
-    lo = slice_of((int)(steps * i >> ts));
-    hi = slice_of((int)(steps * (i + 1) >> ts));
-  };
-
-  Ring r{0, 0, (uint32_t)slot_bytes(0), lane};
-  r.base = r.slot = smem_u32(ring1) + warp * STAGES * slot_bytes(0);
+  Ring r;
+  r.lane = lane;
   Feed f;
-  f.left = f.copies = 0;
-  // the feed's next four units; phase 2: its place in the list of steps, and its slice
-  int next = 0, at = 0, end = 0, hint = 0, slice = 0;
-  auto more = [&]() -> bool {
+  f.left = 0;
+
+  // ---- phase 1: gate and up ----
+  {
+    // the units, heaviest first, are dealt out in turn, the turns in alternating order; four at a time, each to a team
+    const int units = t.unit0[segs], turns = units / G;
+    const int mine = turns + (turns & 1 ? G - 1 - b < units - turns * G : b < units - turns * G);
+    auto unit_of = [&](int i) { return i * G + (i & 1 ? G - 1 - b : b); };
+    r.base = r.slot = smem_u32(ring1) + warp * STAGES * slot_bytes(0);
+    int next = 0;                                 // first of the four units that the feed looks at next
+    auto ask_next = [&](uint32_t slot) {
 #pragma unroll 1
-    for (;;) {
-      DownRun d;
-      if (down && down_run(t, fg, at, end, hint, d)) {
-        const SegPage& page = t.page[3 * d.a + PW_DOWN];
-        const int pair0 = t.off[d.a] + d.pass * kUnitCols;
-        feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * d.a + PW_DOWN], fg, slice, d.lo, d.lo + d.n);
-        feed_operand(f, lane, p.h + (size_t)pair0 * p.F * 2, (uint32_t)p.F * 2, min(kUnitCols, t.off[d.a + 1] - pair0), d.lo);
-        return true;
-      }
-      if (next >= mine) return false;
-      const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
-      const int unit = unit_of(next + team);
-      next += m;
-      if (team >= m) continue;
-      if (down) {
-        range(unit, ts, member, at, end);
-        hint = count_up_to(t.step0 + 1, segs, at, lane);
-        slice = slice_of(unit);
-      } else {
-        const GateUp g = gate_up_unit(t, segs, unit, hg, ts, member, lane);
+      while (f.left == 0) {
+        if (next >= mine) return;
+        const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts;
+        const int i = next + team;
+        next += m;
+        if (team >= m) continue;
+        const GateUp g = gate_up_unit(t, segs, unit_of(i), hg, ts, warp & ((1 << ts) - 1), lane);
         const SegPage& page = t.page[3 * g.a + g.kind];
         feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * g.a + g.kind], hg, g.slice, g.lo, g.lo + g.n);
-        if (f.left) return true;
       }
+      ask_any<0>(f, slot, lane);
+    };
+#pragma unroll 1
+    for (int i = 0; i < STAGES; ++i) {
+      ask_next(r.slot);
+      ring_on<0, STAGES>(r);
     }
-  };
-  // The first steps of phase 2 are asked for without their operand, which is not there yet.  What a lane will copy of it
-  // waits in the lane's place of the slot.
-  bool without = false;
-  int asked = 0;
-  auto ask_next = [&](uint32_t slot) {
-    if (f.left == 0 && !more()) return;
-    const int copies = f.copies;
-    if (without) {
-      const int ls = step_shift(f.fmt);
-      const char* x = f.x + (ls == 1 ? f.sub * 128 : ls == 2 ? (f.sub ^ ((lane >> 2) & 1)) * 64 : 0);
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(slot + kStepCodes + kStepMeta + lane * 16), "r"((uint32_t)(uintptr_t)x),
-                   "r"((uint32_t)((uintptr_t)x >> 32)), "r"(f.x_step), "r"((uint32_t)copies)
-                   : "memory");
-      ++asked;
-      f.copies = 0;
-    }
-    ask_any<true>(f, slot, lane);
-    f.copies = copies;
-  };
-
-  float* const own = sums + warp * p.T * kSumPitch;
-  int first = 0, prime = STAGES;                  // the first of the four units in work; steps to ask for before any are multiplied
-  bool open = false;                              // phase 2: a unit is in work,
-  int place = 0, stop = 0, where = 0;             // at this place of its steps
 #pragma unroll 1
-  for (;;) {
-    const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
-    const bool idle = team >= m;
-    const int unit = unit_of(first + team);
-    int fmt = 0, n = 0, pair0 = 0, cols = 1;
-    GateUp g{};
-    Operand o{};
-    if (!prime) {
-      if (first >= mine) {
-        if (down) break;
-        // ---- from phase 1 to phase 2 ----
-        cp_wait<0>();
-        __syncthreads();
-        // The CTAs add up to 2^31 between them: the top bit turns when the last one has come, and again in the next call.
-        // (The values were written before the barrier above: released with this addition.)
-        if (tid == 0)
-          asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(p.sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
-        down = true;
-        const int units = p.H / kUnitRows * p.n_parts;
-        mine = units / G + (b < units % G);
-        r.bytes = p.slot2;
-        r.base = r.slot = smem_u32(smem) + kTableBytes<TAB> + kStreamWarps * p.T * kSumPitch * 4 + warp * STAGES * p.slot2;
-        first = next = 0;
-        f.left = 0;
-        prime = STAGES;
-        without = true;
-        continue;
-      }
-      if (idle) {
-        first += 4;
-        continue;
-      }
-      if (!down) {
-        g = gate_up_unit(t, segs, unit, hg, ts, member, lane);
-        pair0 = t.off[g.a] + g.pass * kUnitCols;
-        cols = min(kUnitCols, t.off[g.a + 1] - pair0);
-        const int x = t.token[pair0 + min(lane >> 2, cols - 1)];
-        fmt = t.fmt[4 * g.a + g.kind];
-        n = g.n;
-        o = Operand{smem_u32(pieces) + x * 256, 0, 0, p.T, (uint32_t)(x & 1) << 2, g.lo};
-      } else {
-        if (!open) {
-          range(unit, ts, member, place, stop);
-          where = count_up_to(t.step0 + 1, segs, place, lane);
-#pragma unroll 1
-          for (int i = lane; i < p.T * kSumPitch; i += 32) own[i] = 0.f;
-          __syncwarp();
-          open = true;
-        }
-        DownRun d;
-        if (down_run(t, fg, place, stop, where, d)) {
-          fmt = t.fmt[4 * d.a + PW_DOWN];
-          const int ls = step_shift(fmt);
-          pair0 = t.off[d.a] + d.pass * kUnitCols;
-          cols = min(kUnitCols, t.off[d.a + 1] - pair0);
-          const int xc = min(lane >> 2, cols - 1);
-          n = d.n;
-          o = Operand{(uint32_t)(kStepCodes + kStepMeta + xc * (256 >> ls)), 0, 0, 0, ls == 2 ? 0 : (uint32_t)(xc & 1) << 2, d.lo};
-        }
-      }
-    }
-    float tot[2][4] = {};
-    walk<kAnyFormat, true, STAGES>(fixed, fmt, prime, n, f, r, o, tot, ask_next);
-    if (prime) {
-      prime = 0;
-      if (!down) continue;
-      // ---- all CTAs have arrived ----
-      // (a CTA that has to wait asks for its next steps' codes first, into the L2 cache: the memory works on meanwhile)
-      without = false;
-      uint32_t arrived;
-      asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(arrived) : "l"(p.sync) : "memory");
-      if (__shfl_sync(0xffffffffu, (arrived ^ before) >> 31, 0) == 0) {
-        const Feed ahead = f;
-        const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
-#pragma unroll 1
-        for (int i = 0; i < kFewAheadSteps && (f.left || more()); ++i) prefetch_step(f, lane);
-        f = ahead;
-        next = a0, at = a1, end = a2, hint = a3, slice = a4;
-      }
-      bool together = true;
-      if (tid == 0) {
-        uint32_t now;
-        together = false;
-#pragma unroll 1
-        for (uint32_t i = 0; i < kFewPolls && !together; ++i) {
-          asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(p.sync) : "memory");
-          together = (now ^ before) >> 31;
-        }
-        if (!together) atomicMax(p.status, (int)PW_ERR_TIMEOUT);
-      }
-      if (!__syncthreads_and(together)) break;
-#pragma unroll 1
-      for (int i = 0; i < STAGES; ++i) {
-        if (i < asked) {
-          const uint32_t to = r.base + i * r.bytes + kStepCodes + kStepMeta + lane * 16;
-          const uint4 w = lds16(to);
-          const char* x = reinterpret_cast<const char*>((uintptr_t)w.x | (uintptr_t)w.y << 32);
-#pragma unroll 1
-          for (int j = 0; j < (int)w.w; ++j) cp16(to + j * 512, x + (size_t)j * w.z);   // (rows behind the first lie behind all lanes' places)
-        }
-        cp_commit();
-      }
-      continue;
-    }
-    if (!down) {
+    for (int first = 0; first < mine; first += 4) {
+      const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
+      if (team >= m) continue;
+      const GateUp g = gate_up_unit(t, segs, unit_of(first + team), hg, ts, member, lane);
+      const int pair0 = t.off[g.a] + g.pass * kUnitCols, cols = min(kUnitCols, t.off[g.a + 1] - pair0);
+      const int x = t.token[pair0 + min(lane >> 2, cols - 1)];
+      const int t0 = t.token[pair0 + min(2 * (lane & 3), cols - 1)], t1 = t.token[pair0 + min(2 * (lane & 3) + 1, cols - 1)];
+      float tot[2][4] = {};
+      Operand o{smem_u32(pieces) + x * 256, smem_u32(xsum + t0), smem_u32(xsum + t1), p.T, (uint32_t)(x & 1) << 2, g.lo};
+      walk<kAnyFormat, 0, STAGES>(fixed, t.fmt[4 * g.a + g.kind], g.n, f, r, o, tot, ask_next);
       put_sums(sums + warp * kSumFloats, lane, tot);
       few_team_sync(team, ts);
       const float* set = sums + (team << ts) * kSumFloats;
@@ -518,63 +381,187 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         *reinterpret_cast<__half*>(p.h + (size_t)(pair0 + col) * p.F * 2 + piece_offset(g.slice * kUnitRows + row, col)) = __float2half_rn(h);
       }
       few_team_sync(team, ts);                    // the sums are written again
-      first += 4;
-      continue;
     }
-    if (n) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {               // the tokens of a run are different ones: no two lanes meet
-        const int col = 2 * (lane & 3) + c;
-        if (col < cols) {
-          const float gate = t.gate[pair0 + col];
-          float4* to = reinterpret_cast<float4*>(own + t.token[pair0 + col] * kSumPitch + 4 * (lane >> 2));
-          float4 v = *to;
-          v.x = __fadd_rn(v.x, __fmul_rn(gate, tot[0][c]));
-          v.y = __fadd_rn(v.y, __fmul_rn(gate, tot[0][c + 2]));
-          v.z = __fadd_rn(v.z, __fmul_rn(gate, tot[1][c]));
-          v.w = __fadd_rn(v.w, __fmul_rn(gate, tot[1][c + 2]));
-          *to = v;
-        }
-      }
-      __syncwarp();
-      if (place < stop) continue;
-    }
-    open = false;
-    first += 4;
-    few_team_sync(team, ts);
-    float* const set = sums + (team << ts) * p.T * kSumPitch;
-    const int row0 = slice_of(unit) * kUnitRows, part = unit - slice_of(unit) * p.n_parts;
-#pragma unroll 1
-    for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
-      const int row = i & (kUnitRows - 1), tok = i >> 5;
-      float v = 0.f;
-#pragma unroll 4
-      for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, set[(w * p.T + tok) * kSumPitch + row]);
-      if (p.n_parts == 1) store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
-      else p.parts[((size_t)part * p.T + tok) * p.H + row0 + row] = v;
-    }
-    if (p.n_parts > 1) {
-      // the last of the parts to finish adds all of them up, in their order
-      __threadfence();
-      few_team_sync(team, ts);
-      if (lane == 0 && member == 0) *reinterpret_cast<int32_t*>(set) = atomicAdd(p.sync + 64 + row0 / kUnitRows, 1) == p.n_parts - 1;
-      few_team_sync(team, ts);
-      if (*reinterpret_cast<volatile int32_t*>(set)) {
-        __threadfence();
-#pragma unroll 1
-        for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
-          const int row = i & (kUnitRows - 1), tok = i >> 5;
-          float v = 0.f;
-#pragma unroll 1
-          for (int q = 0; q < p.n_parts; ++q) v = __fadd_rn(v, __ldcg(p.parts + ((size_t)q * p.T + tok) * p.H + row0 + row));
-          store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
-        }
-        if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
-      }
-    }
-    few_team_sync(team, ts);                      // the sums are written again
   }
-  cp_commit();
+
+  // ---- from phase 1 to phase 2 ----
+  cp_wait<0>();
+  __syncthreads();
+  // The CTAs add up to 2^31 between them: the top bit turns when the last one has come, and again in the next call.
+  // (The values were written before the barrier above: released with this addition.)
+  if (tid == 0)
+    asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(p.sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
+
+  // ---- phase 2: down ----
+  {
+    const int steps = t.step0[segs];              // of a slice
+    const int units = p.H / kUnitRows * p.n_parts;
+    const int mine = units / G + (b < units % G);
+    auto slice_of = [&](int unit) { return p.n_parts == 1 ? unit : (int)__umulhi((uint32_t)unit, p.per_part); };   // unit / n_parts
+    auto range = [&](int unit, int ts, int member, int& lo, int& hi) {
+      // steps * i / (n_parts << ts), rounded down (steps * i is below 2^24)
+      const uint32_t i = ((uint32_t)(unit - slice_of(unit) * p.n_parts) << ts) + member;
+      lo = slice_of((int)(steps * i >> ts));
+      hi = slice_of((int)(steps * (i + 1) >> ts));
+    };
+    r.base = r.slot = smem_u32(smem) + kTableBytes<TAB> + kStreamWarps * p.T * kSumPitch * 4 + warp * STAGES * slot_bytes(XC);
+    f.left = 0;
+    // the feed's next four units, its place in the list of steps, and its slice
+    int next = 0, at = 0, end = 0, hint = 0, slice = 0;
+    auto more = [&]() -> bool {
+      DownRun d;
+#pragma unroll 1
+      while (!down_run(t, fg, at, end, hint, d)) {
+        if (next >= mine) return false;
+        const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts;
+        const int unit = (next + team) * G + b;
+        next += m;
+        at = end = 0;
+        if (team >= m) continue;
+        range(unit, ts, warp & ((1 << ts) - 1), at, end);
+        hint = count_up_to(t.step0 + 1, segs, at, lane);
+        slice = slice_of(unit);
+      }
+      const SegPage& page = t.page[3 * d.a + PW_DOWN];
+      const int pair0 = t.off[d.a] + d.pass * kUnitCols;
+      feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * d.a + PW_DOWN], fg, slice, d.lo, d.lo + d.n);
+      feed_operand(f, lane, p.h + (size_t)pair0 * p.F * 2, (uint32_t)p.F * 2, min(kUnitCols, t.off[d.a + 1] - pair0), d.lo);
+      return true;
+    };
+    // The first steps are asked for without their operand, which is not there yet.  What a lane will copy of it waits in the
+    // lane's place of the slot.
+    int asked = STAGES;
+    auto ask_next = [&](uint32_t slot) {
+      if (f.left == 0 && !more()) return;
+      const int copies = f.copies;
+      if (asked < STAGES) {
+        const int ls = step_shift(f.fmt);
+        const char* x = f.x + (ls == 1 ? f.sub * 128 : ls == 2 ? (f.sub ^ ((lane >> 2) & 1)) * 64 : 0);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(slot + kStepCodes + kStepMeta + lane * 16), "r"((uint32_t)(uintptr_t)x),
+                     "r"((uint32_t)((uintptr_t)x >> 32)), "r"(f.x_step), "r"((uint32_t)copies)
+                     : "memory");
+        ++asked;
+        f.copies = 0;
+      }
+      ask_any<XC>(f, slot, lane);
+      f.copies = copies;
+    };
+    asked = 0;
+#pragma unroll 1
+    for (int i = 0; i < STAGES; ++i) {
+      ask_next(r.slot);
+      ring_on<XC, STAGES>(r);
+    }
+    const int first_steps = asked;
+    asked = STAGES;
+    // a CTA that has to wait asks for its next steps' codes first, into the L2 cache: the memory works on meanwhile
+    uint32_t arrived;
+    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(arrived) : "l"(p.sync) : "memory");
+    if (__shfl_sync(0xffffffffu, (arrived ^ before) >> 31, 0) == 0) {
+      const Feed ahead = f;
+      const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
+#pragma unroll 1
+      for (int i = 0; i < kFewAheadSteps && (f.left || more()); ++i) prefetch_step(f, lane);
+      f = ahead;
+      next = a0, at = a1, end = a2, hint = a3, slice = a4;
+    }
+    bool together = true;
+    if (tid == 0) {
+      uint32_t now;
+      together = false;
+#pragma unroll 1
+      for (uint32_t i = 0; i < kFewPolls && !together; ++i) {
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(p.sync) : "memory");
+        together = (now ^ before) >> 31;
+      }
+      if (!together) atomicMax(p.status, (int)PW_ERR_TIMEOUT);
+    }
+    if (!__syncthreads_and(together)) {
+      cp_wait<0>();
+      return;
+    }
+#pragma unroll 1
+    for (int i = 0; i < STAGES; ++i) {
+      if (i < first_steps) {
+        const uint32_t to = r.base + i * slot_bytes(XC) + kStepCodes + kStepMeta + lane * 16;
+        const uint4 w = lds16(to);
+        const char* x = reinterpret_cast<const char*>((uintptr_t)w.x | (uintptr_t)w.y << 32);
+#pragma unroll 1
+        for (int j = 0; j < (int)w.w; ++j) cp16(to + j * 512, x + (size_t)j * w.z);   // (rows behind the first lie behind all lanes' places)
+      }
+      cp_commit();
+    }
+    float* const own = sums + warp * p.T * kSumPitch;
+#pragma unroll 1
+    for (int first = 0; first < mine; first += 4) {
+      const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
+      if (team >= m) continue;
+      const int unit = (first + team) * G + b;
+      int place, stop;
+      range(unit, ts, member, place, stop);
+      int where = count_up_to(t.step0 + 1, segs, place, lane);
+#pragma unroll 1
+      for (int i = lane; i < p.T * kSumPitch; i += 32) own[i] = 0.f;
+      __syncwarp();
+      DownRun d;
+#pragma unroll 1
+      while (down_run(t, fg, place, stop, where, d)) {
+        const int fmt = t.fmt[4 * d.a + PW_DOWN], ls = step_shift(fmt);
+        const int pair0 = t.off[d.a] + d.pass * kUnitCols, cols = min(kUnitCols, t.off[d.a + 1] - pair0);
+        const int xc = min(lane >> 2, cols - 1);
+        float tot[2][4] = {};
+        Operand o{(uint32_t)(kStepCodes + kStepMeta + xc * (256 >> ls)), 0, 0, 0, ls == 2 ? 0 : (uint32_t)(xc & 1) << 2, d.lo};
+        walk<kAnyFormat, XC, STAGES>(fixed, fmt, d.n, f, r, o, tot, ask_next);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {             // the tokens of a run are different ones: no two lanes meet
+          const int col = 2 * (lane & 3) + c;
+          if (col < cols) {
+            const float gate = t.gate[pair0 + col];
+            float4* to = reinterpret_cast<float4*>(own + t.token[pair0 + col] * kSumPitch + 4 * (lane >> 2));
+            float4 v = *to;
+            v.x = __fadd_rn(v.x, __fmul_rn(gate, tot[0][c]));
+            v.y = __fadd_rn(v.y, __fmul_rn(gate, tot[0][c + 2]));
+            v.z = __fadd_rn(v.z, __fmul_rn(gate, tot[1][c]));
+            v.w = __fadd_rn(v.w, __fmul_rn(gate, tot[1][c + 2]));
+            *to = v;
+          }
+        }
+        __syncwarp();
+      }
+      few_team_sync(team, ts);
+      float* const set = sums + (team << ts) * p.T * kSumPitch;
+      const int row0 = slice_of(unit) * kUnitRows, part = unit - slice_of(unit) * p.n_parts;
+#pragma unroll 1
+      for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
+        const int row = i & (kUnitRows - 1), tok = i >> 5;
+        float v = 0.f;
+#pragma unroll 4
+        for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, set[(w * p.T + tok) * kSumPitch + row]);
+        if (p.n_parts == 1) store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
+        else p.parts[((size_t)part * p.T + tok) * p.H + row0 + row] = v;
+      }
+      if (p.n_parts > 1) {
+        // the last of the parts to finish adds all of them up, in their order
+        __threadfence();
+        few_team_sync(team, ts);
+        if (lane == 0 && member == 0) *reinterpret_cast<int32_t*>(set) = atomicAdd(p.sync + 64 + row0 / kUnitRows, 1) == p.n_parts - 1;
+        few_team_sync(team, ts);
+        if (*reinterpret_cast<volatile int32_t*>(set)) {
+          __threadfence();
+#pragma unroll 1
+          for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
+            const int row = i & (kUnitRows - 1), tok = i >> 5;
+            float v = 0.f;
+#pragma unroll 1
+            for (int q = 0; q < p.n_parts; ++q) v = __fadd_rn(v, __ldcg(p.parts + ((size_t)q * p.T + tok) * p.H + row0 + row));
+            store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
+          }
+          if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
+        }
+      }
+      few_team_sync(team, ts);                    // the sums are written again
+    }
+  }
   cp_wait<0>();
 }
 
@@ -643,20 +630,21 @@ __global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, i
 // ---- host ----------------------------------------------------------------------------------------
 typedef void (*FewKernel)(FewArgs);
 struct FewVariant {
-  int segs, pairs, choices, table_bytes, stages;
+  int segs, pairs, choices, table_bytes, rows, stages;
   FewKernel kernel;
 };
-template <class TAB, int STAGES>
+template <class TAB, int XC, int STAGES>
 static constexpr FewVariant few_variant() {
-  return {TAB::kSegs, TAB::kPairs, TAB::kChoices, kTableBytes<TAB>, STAGES, few_layer_kernel<TAB, STAGES>};
+  return {TAB::kSegs, TAB::kPairs, TAB::kChoices, kTableBytes<TAB>, XC, STAGES, few_layer_kernel<TAB, XC, STAGES>};
 }
 // The first that fits is the fastest.
-static const FewVariant kFewVariants[] = {few_variant<FewSmall, 4>(), few_variant<FewSmall, 3>(), few_variant<FewAll, 3>(), few_variant<FewSmall, 2>(),
-                                          few_variant<FewAll, 2>()};
+static const FewVariant kFewVariants[] = {few_variant<FewSmall, 2, 4>(), few_variant<FewSmall, 4, 3>(), few_variant<FewSmall, 8, 3>(),
+                                          few_variant<FewAll, 8, 3>(),   few_variant<FewSmall, 8, 2>(), few_variant<FewAll, 8, 2>()};
 
 static size_t few_smem(const FewArgs& a, const FewVariant& v) {
-  const size_t first = (size_t)kStreamWarps * (kSumFloats * 4 + v.stages * slot_bytes(0)) + (size_t)a.T * a.H * 2;
-  const size_t second = (size_t)kStreamWarps * ((size_t)a.T * kSumPitch * 4 + (size_t)v.stages * a.slot2);
+  const size_t first = (size_t)kStreamWarps * (kSumFloats * 4 + v.stages * slot_bytes(0)) +
+                       (((size_t)a.H / kGroup * 3 * a.T * 4 + 127) & ~(size_t)127) + (size_t)a.T * a.H * 2;
+  const size_t second = (size_t)kStreamWarps * ((size_t)a.T * kSumPitch * 4 + (size_t)v.stages * slot_bytes(v.rows));
   return v.table_bytes + (first > second ? first : second);
 }
 
@@ -678,10 +666,9 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.out_type = out_type;
   a.segs = (c.n_experts < T * top_k ? c.n_experts : T * top_k) + c.n_shared;
   a.pairs = T * (top_k + c.n_shared);
-  a.slot2 = slot_bytes(T < 2 ? 2 : T < kUnitCols ? T : kUnitCols);   // (room for 512 bytes: see ask_next)
   const FewVariant* v = nullptr;
   for (const FewVariant& one : kFewVariants)
-    if (!v && a.segs <= one.segs && a.pairs <= one.pairs && T * top_k <= one.choices && few_smem(a, one) <= kSmemLimit) v = &one;
+    if (!v && (T < kUnitCols ? T : kUnitCols) <= one.rows && a.segs <= one.segs && a.pairs <= one.pairs && T * top_k <= one.choices && few_smem(a, one) <= kSmemLimit) v = &one;
   if (!v) return PW_ERR_SHAPE;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;

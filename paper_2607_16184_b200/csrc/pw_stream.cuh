@@ -143,18 +143,19 @@ __device__ __forceinline__ void feed_operand(Feed& f, int lane, const char* x, u
   f.x_step = pitch << (ls + 1);
 }
 
-// Asks for a step in format F and moves on; `left` is the caller's.  STREAM: with its streamed operand, if it has one.
-template <int F, bool STREAM>
+// Asks for a step in format F and moves on; `left` is the caller's.  XC: the most operand rows that are streamed with it, 0:
+// the operand is staged.
+template <int F, int XC>
 __device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
   constexpr int ls = step_shift(F);
-  if constexpr (STREAM) {
+  if constexpr (XC > 0) {
     // the step's part of a group's pieces: all, the half `sub`, or the quarter `sub` (quarters of odd rows are exchanged)
     const char* src = f.x;
     if constexpr (ls == 1) src += f.sub * 128;
     if constexpr (ls == 2) src += (f.sub ^ ((lane >> 2) & 1)) * 64;
     const uint32_t dst = slot + kStepCodes + kStepMeta + lane * 16;
 #pragma unroll
-    for (int j = 0; j < kUnitCols >> (ls + 1); ++j)
+    for (int j = 0; j < (XC >> (ls + 1) > 0 ? XC >> (ls + 1) : 1); ++j)
       if (j < f.copies) cp16(dst + j * 512, src + j * f.x_step);
     f.x += ls == 0 || f.sub == (1 << ls) - 1 ? 256 : 0;
   }
@@ -182,18 +183,18 @@ __device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
   }
   if constexpr (ls > 0) f.sub = (f.sub + 1) & ((1 << ls) - 1);
 }
-template <bool STREAM>
+template <int XC>
 __device__ __forceinline__ void ask_any(Feed& f, uint32_t slot, int lane) {
   f.left--;
   switch (f.fmt) {
-    case kFmt16: ask<kFmt16, STREAM>(f, slot, lane); break;
-    case kFmt8: ask<kFmt8, STREAM>(f, slot, lane); break;
-    case kFmt4: ask<kFmt4, STREAM>(f, slot, lane); break;
-    case kFmt3: ask<kFmt3, STREAM>(f, slot, lane); break;
-    case kFmt2: ask<kFmt2, STREAM>(f, slot, lane); break;
-    case kFmtP4: ask<kFmtP4, STREAM>(f, slot, lane); break;
-    case kFmtP3: ask<kFmtP3, STREAM>(f, slot, lane); break;
-    default: ask<kFmtP2, STREAM>(f, slot, lane); break;
+    case kFmt16: ask<kFmt16, XC>(f, slot, lane); break;
+    case kFmt8: ask<kFmt8, XC>(f, slot, lane); break;
+    case kFmt4: ask<kFmt4, XC>(f, slot, lane); break;
+    case kFmt3: ask<kFmt3, XC>(f, slot, lane); break;
+    case kFmt2: ask<kFmt2, XC>(f, slot, lane); break;
+    case kFmtP4: ask<kFmtP4, XC>(f, slot, lane); break;
+    case kFmtP3: ask<kFmtP3, XC>(f, slot, lane); break;
+    default: ask<kFmtP2, XC>(f, slot, lane); break;
   }
 }
 
@@ -274,7 +275,7 @@ __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int r
 struct Operand {
   uint32_t x;                                     // staged: this lane's row of group 0; streamed: the row's place in a slot
   uint32_t sum0, sum1;                            // staged, with sums: those of group 0, tokens 2t and 2t + 1
-  int room;                                       // staged: rows there is room for; 0: streamed
+  int room;                                       // staged: rows there is room for
   uint32_t flip;                                  // 4 for an odd row (see piece_at; not in a streamed quarter of a group)
   int step;                                       // next step of the block
 };
@@ -449,28 +450,26 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
 // ---- a warp's walk over its steps ----------------------------------------------------------------
 struct Ring {
   uint32_t base, slot;                            // shared memory: the warp's slots, the next step's
-  uint32_t bytes;                                 // of a slot
   int lane;
 };
-template <int STAGES>
+template <int XC, int STAGES>
 __device__ __forceinline__ void ring_on(Ring& r) {
   cp_commit();
-  r.slot = r.slot == r.base + (STAGES - 1) * r.bytes ? r.base : r.slot + r.bytes;
+  r.slot = r.slot == r.base + (STAGES - 1) * slot_bytes(XC) ? r.base : r.slot + slot_bytes(XC);
 }
 // Multiplies steps of a block in format F, at most n, and asks for the next step of the feed after each while that is in
-// the same format.  Returns with n = 0, or having multiplied a step without having asked (true).  STREAM: the operand may
-// be streamed, and has no sums.
-template <int F, bool STREAM, int STAGES>
+// the same format.  Returns with n = 0, or having multiplied a step without having asked (true).
+template <int F, int XC, int STAGES>
 __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4]) {
   constexpr int ls = step_shift(F);
   const uint32_t t = (uint32_t)r.lane & 3;
   // The lane's pieces of a step: e = 4t + i, 8q + 2t + i or 4q + t, q the step inside its group, in the order of piece_at:
   // at0 ^ (what q adds) ^ i.  A streamed row is the part of its step.
   const uint32_t at0 = (ls == 0 ? 5 * t : ls == 1 ? (2 * t) ^ (t >> 1) : t) ^ o.flip;
-  const bool streamed = STREAM && o.room == 0;
-  const uint32_t of_q = ls == 1 ? (streamed ? 2 : 10) : streamed ? 1 : 5;
+  constexpr uint32_t of_q = ls == 1 ? (XC ? 2 : 10) : XC ? 1 : 5;
   const uint32_t x_group = (uint32_t)o.room * 256, sum_part = (uint32_t)o.room * 4, sum_group = 3 * sum_part, grp = (uint32_t)o.step >> ls;
-  uint32_t x = o.x + grp * x_group, sum0 = o.sum0 + grp * sum_group, sum1 = o.sum1 + grp * sum_group;
+  uint32_t x = o.x, sum0 = o.sum0, sum1 = o.sum1;
+  if constexpr (XC == 0) x += grp * x_group, sum0 += grp * sum_group, sum1 += grp * sum_group;
   int asks = f.fmt == F ? min(n, f.left) : 0;
   f.left -= asks;
   bool due = false;
@@ -480,8 +479,8 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
     __syncwarp();                                 // what the other lanes have copied
     const uint32_t q = ls ? (uint32_t)o.step & ((1 << ls) - 1) : 0;
     const uint32_t part = ls == 1 ? q * sum_part : 2 * sum_part;
-    multiply_step<F, !STREAM>(k, r.slot, r.lane, streamed ? x + r.slot : x, ls ? at0 ^ (of_q * q) : at0, sum0 + part, sum1 + part, tot);
-    if (ls == 0 || q == (1 << ls) - 1) {
+    multiply_step<F, XC == 0>(k, r.slot, r.lane, XC ? x + r.slot : x, ls ? at0 ^ (of_q * q) : at0, sum0 + part, sum1 + part, tot);
+    if (XC == 0 && (ls == 0 || q == (1 << ls) - 1)) {
       x += x_group;
       sum0 += sum_group;
       sum1 += sum_group;
@@ -492,38 +491,36 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
     due = asks == 0;
     if (due) break;
     --asks;
-    ask<F, STREAM>(f, r.slot, r.lane);
-    ring_on<STAGES>(r);
+    ask<F, XC>(f, r.slot, r.lane);
+    ring_on<XC, STAGES>(r);
   } while (n);
   return due;
 }
-// Asks for `prime` steps, then multiplies the next n, all of one block in format `fmt` (F, if that is not kAnyFormat: all
-// blocks are), asking for as many.  ask_next(slot): asks for the feed's next step, of the next block if need be, or for
+// Multiplies the next n steps, all of one block in format `fmt` (F, if that is not kAnyFormat: all blocks are), and asks for
+// as many.  ask_next(slot): asks for the feed's next step, of the next block if need be, or for
 // nothing if there is none.
 constexpr int kAnyFormat = -1;
-template <int F, bool STREAM, int STAGES, class AskNext>
-__device__ __forceinline__ void walk(const Fixed& k, int fmt, int prime, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], AskNext ask_next) {
-  while (prime + n) {
-    bool due = true;
-    if (prime) {
-      --prime;
-    } else if constexpr (F != kAnyFormat) {
-      due = walk_format<F, STREAM, STAGES>(k, n, f, r, o, tot);
+template <int F, int XC, int STAGES, class AskNext>
+__device__ __forceinline__ void walk(const Fixed& k, int fmt, int n, Feed& f, Ring& r, Operand& o, float (&tot)[2][4], AskNext ask_next) {
+  while (n) {
+    bool due;
+    if constexpr (F != kAnyFormat) {
+      due = walk_format<F, XC, STAGES>(k, n, f, r, o, tot);
     } else {
       switch (fmt) {
-        case kFmt16: due = walk_format<kFmt16, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt8: due = walk_format<kFmt8, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt4: due = walk_format<kFmt4, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt3: due = walk_format<kFmt3, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        case kFmtP4: due = walk_format<kFmtP4, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        case kFmtP3: due = walk_format<kFmtP3, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        case kFmt2: due = walk_format<kFmt2, STREAM, STAGES>(k, n, f, r, o, tot); break;
-        default: due = walk_format<kFmtP2, STREAM, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt16: due = walk_format<kFmt16, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt8: due = walk_format<kFmt8, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt4: due = walk_format<kFmt4, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt3: due = walk_format<kFmt3, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmtP4: due = walk_format<kFmtP4, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmtP3: due = walk_format<kFmtP3, XC, STAGES>(k, n, f, r, o, tot); break;
+        case kFmt2: due = walk_format<kFmt2, XC, STAGES>(k, n, f, r, o, tot); break;
+        default: due = walk_format<kFmtP2, XC, STAGES>(k, n, f, r, o, tot); break;
       }
     }
     if (due) {
       ask_next(r.slot);
-      ring_on<STAGES>(r);
+      ring_on<XC, STAGES>(r);
     }
   }
 }
