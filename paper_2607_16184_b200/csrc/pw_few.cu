@@ -73,7 +73,7 @@ __device__ __forceinline__ void put_linear(const PageLinearArgs& a, const Linear
 // spends a large part of its time on fetching code.
 template <int F, int STAGES>
 __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __grid_constant__ PageLinearArgs a) {
-  constexpr int kRing = STAGES * slot_bytes(0);
+  constexpr int kRing = STAGES * kSlotBytes;
   extern __shared__ __align__(128) char smem[];
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int ts = a.team_shift, team = warp >> ts, member = warp & ((1 << ts) - 1);
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 
   const Fixed fixed;
   const uint32_t ring = smem_u32(smem) + warp * kRing;
-  Ring r{ring, ring, lane};
+  Ring r{ring, ring, 0, lane};
   Feed f;
   f.left = 0;
   int next = 0;                                   // slice the feed takes next
@@ -108,13 +108,13 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     }
     return false;
   };
-  auto ask_next = [&](uint32_t slot) {
+  auto ask_next = [&]() {
     if (f.left == 0 && !more()) return;
     if constexpr (F == kAnyFormat) {
-      ask_any<0>(f, slot, lane);
+      ask_any<0>(f, r.slot, 0, lane);
     } else {
       f.left--;
-      ask<F, 0>(f, slot, lane);
+      ask<F, 0>(f, r.slot, 0, lane);
     }
   };
 
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     r.slot = r.base;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
-      ask_next(r.slot);
+      ask_next();
       ring_on<0, STAGES>(r);
     }
     if (!waited) {
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     }
     const int token0 = pass * a.width, cols = min(a.width, a.T - token0);
     __syncthreads();                              // the pass before has read its operand
-    stage_operand(a.x + (size_t)token0 * a.x_pitch, a.x_pitch, cols, a.room, g0, my_groups, a.x_bytes, pieces, xsum, threadIdx.x,
+    stage_operand<1>(a.x + (size_t)token0 * a.x_pitch, a.x_pitch, cols, a.room, g0, my_groups, a.x_bytes, pieces, xsum, threadIdx.x,
                   kStreamThreads);
     __syncthreads();
     // (tokens that there are not: any row and sum, their products are not used)
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
 }
 
 static size_t page_linear_smem(const PageLinearArgs& a, int stages) {
-  return (size_t)kStreamWarps * stages * slot_bytes(0) + kSumsBytes + (a.split > 1 ? kPartsBytes : 0) +
+  return (size_t)kStreamWarps * stages * kSlotBytes + kSumsBytes + (a.split > 1 ? kPartsBytes : 0) +
          (((size_t)a.split_groups * 3 * a.room * 4 + 127) & ~(size_t)127) + (size_t)a.split_groups * a.room * 256;
 }
 typedef void (*PageLinearKernel)(PageLinearArgs);

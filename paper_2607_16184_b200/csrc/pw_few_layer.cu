@@ -19,6 +19,7 @@ namespace pw {
 constexpr int kFewParts = 8;                      // most parts of the down blocks' columns
 constexpr int kFewRouters = 4;                    // warps that route
 constexpr size_t kFewAhead = 16 << 20;            // bytes of shared experts that are asked for while the tokens are routed (2.5 us)
+constexpr uint32_t kFewAheadPiece = 4096;
 constexpr int kFewAheadSteps = 8;                 // steps of phase 2 that a warp asks the L2 cache for before all CTAs meet
 constexpr uint32_t kFewPolls = 1u << 22;          // about 3 s
 
@@ -54,11 +55,12 @@ struct FewTables {
   float gate[PAIRS];
   float own_gates[CHOICES];                       // [T * k]
   int32_t own_ids[CHOICES];
-  uint32_t mask[256];                             // tokens of an expert
+  uint32_t mask[256];                             // tokens of an expert, and above them (16 bits) its first pair
   int32_t unit0[SEGS + 1];                        // first unit of phase 1, by rank
   int32_t step0[SEGS + 1];                        // first step of phase 2, of the segment's first pass
-  int32_t weight[SEGS];                           // bytes of a tile of the gate and the up block
+  uint32_t key[SEGS];                             // by which they are ordered, heaviest first: see make_tables
   int32_t count[2];                               // active segments, pairs
+  uint32_t done;                                  // warps that are through with phase 1
   uint16_t seg[SEGS];                             // expert, ascending
   uint16_t off[SEGS + 1];                         // first pair
   uint16_t order[SEGS];                           // shared experts first, then by weight, heaviest first
@@ -138,112 +140,102 @@ __device__ __forceinline__ bool down_run(const TAB& t, int groups, int& at, int 
   return true;
 }
 
-// The tables of a call from its routing (own_ids, own_gates), by the first kFewRouters warps; t.mask is all zeros.
+// The tables of a call from its routing (own_ids, own_gates, and every expert's tokens in mask), by the first kFewRouters
+// warps.  rows: the layer's, in shared memory.
 __device__ __forceinline__ void routers_sync() { asm volatile("bar.sync 8, %0;" ::"n"(32 * kFewRouters) : "memory"); }
 template <class TAB>
-__device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, int fg, int warp, int lane) {
-  if (warp == 0) {
-#pragma unroll 1
-    for (int tok = 0; tok < p.T; ++tok)
-      if (lane < p.k) {
-        const int e = t.own_ids[tok * p.k + lane];
-        if (e >= 0) atomicOr(&t.mask[e], 1u << tok);
-      }
-    __syncwarp();
-    int segs = 0, pairs = 0;                      // experts with tokens, ascending, then the shared ones
-#pragma unroll 1
-    for (int base = 0; base < p.E; base += 32) {
-      const uint32_t m = base + lane < p.E ? t.mask[base + lane] : 0;
-      const uint32_t any = __ballot_sync(0xffffffffu, m != 0);
-      if (!any) continue;
-      const int n = __popc(m);
-      int incl = n;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += y;
-      }
-      if (n) {
-        const int i = segs + __popc(any & ((1u << lane) - 1));
-        t.seg[i] = (uint16_t)(base + lane);
-        t.off[i] = (uint16_t)(pairs + incl - n);
-      }
-      segs += __popc(any);
-      pairs += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane < p.n_shared) {
-      t.seg[segs + lane] = (uint16_t)(p.E + lane);
-      t.off[segs + lane] = (uint16_t)(pairs + lane * p.T);
-    }
-    segs += p.n_shared;
-    pairs += p.n_shared * p.T;
-    if (lane == 0) {
-      t.off[segs] = (uint16_t)pairs;
-      t.count[0] = segs;
-      t.count[1] = pairs;
-    }
-  }
-  routers_sync();
-  const int segs = t.count[0], first = 32 * warp + lane;
-#pragma unroll 1
-  for (int a = first; a < segs; a += 32 * kFewRouters) {
-    const int e = t.seg[a];
-    DevRow row[3];
-#pragma unroll
-    for (int u = 0; u < 3; ++u) row[u] = p.rows[e * 3 + u];
-    // its tokens; an expert that a token names twice takes it once, with both gates
-    int at = t.off[a];
-#pragma unroll 1
-    for (uint32_t m = e < p.E ? t.mask[e] : (1u << p.T) - 1; m; m &= m - 1) {
-      const int tok = __ffs(m) - 1;
-      float g = 1.f;
-      if (e < p.E) {
-        g = 0.f;
-#pragma unroll 1
-        for (int j = 0; j < p.k; ++j)
-          if (t.own_ids[tok * p.k + j] == e) g = __fadd_rn(g, t.own_gates[tok * p.k + j]);
-      }
-      t.token[at] = (uint8_t)tok;
-      t.gate[at++] = g;
-    }
-    int fmt[3];
+__device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevRow* rows, int fg, int warp, int lane) {
+  // Segment a: expert e with n tokens, pairs first .. first + n.  Its key: shared or not, the bytes of a tile of its gate
+  // and its up block, then (for the sums below) its passes and passes * steps of a group of its down block, 8 at most.
+  auto put = [&](int a, int e, int n, int first) {
+    uint32_t tiles = 0, shift = 0;
+    t.seg[a] = (uint16_t)e;
+    t.off[a] = (uint16_t)first;
 #pragma unroll
     for (int u = 0; u < 3; ++u) {
-      fmt[u] = stream_format((int)row[u].bits, row[u].valid == 2);
-      t.page[3 * a + u] = SegPage{static_cast<const char*>(row[u].codes), static_cast<const char*>(row[u].bit1), static_cast<const char*>(row[u].bit0)};
-      t.fmt[4 * a + u] = (uint8_t)fmt[u];
+      const DevRow& row = rows[e * 3 + u];
+      const bool planes = row.valid == 2;
+      if (u == PW_DOWN) shift = row.bits == 16 ? 2 : row.bits == 8 ? 1 : 0;
+      else tiles += planes ? kPlaneTopTile : row.bits == 16 ? 32768 : row.bits * 2048 + 512;
+      t.page[3 * a + u] = SegPage{static_cast<const char*>(row.codes), static_cast<const char*>(row.bit1), static_cast<const char*>(row.bit0)};
+      t.fmt[4 * a + u] = (uint8_t)stream_format((int)row.bits, planes);
     }
-    t.weight[a] = (int)(kTileBytes[fmt[PW_GATE]] + kTileBytes[fmt[PW_UP]]) + (e < p.E ? 0 : 1 << 20);
-  }
-  routers_sync();
+    const uint32_t passes = (uint32_t)(n + kUnitCols - 1) / kUnitCols;
+    t.key[a] = (e < p.E ? 0u : 1u << 31) | tiles << 8 | passes << 4 | passes << shift;
+  };
+  // experts with tokens, ascending, then the shared ones: every warp counts all, and makes the segments of some
+  int segs = 0, pairs = 0;
 #pragma unroll 1
-  for (int a = first; a < segs; a += 32 * kFewRouters) {
-    const int mine = t.weight[a];
-    int rank = 0;
-#pragma unroll 8
-    for (int o = 0; o < segs; ++o) rank += t.weight[o] > mine || (t.weight[o] == mine && o < a);
-    t.order[rank] = (uint16_t)a;
-  }
-  routers_sync();
-  if (warp > 1) return;
-  // first units of phase 1 by rank; first steps of phase 2
-  int32_t* const to = warp == 0 ? t.unit0 : t.step0;
-  int carry = 0;
-#pragma unroll 1
-  for (int base = 0; base < segs; base += 32) {
-    const int i = base + lane;
-    int n = 0;
-    if (i < segs) n = warp == 0 ? passes_of(t, t.order[i]) * (p.F / kUnitRows) : passes_of(t, i) * (fg << step_shift(t.fmt[4 * i + PW_DOWN]));
-    int incl = n;
+  for (int base = 0; base < p.E; base += 32) {
+    const uint32_t m = base + lane < p.E ? t.mask[base + lane] & 0xffffu : 0;   // (another warp may have set the upper half)
+    const uint32_t any = __ballot_sync(0xffffffffu, m != 0);
+    if (!any) continue;
+    const uint32_t below = (1u << lane) - 1;
+    const int n = __popc(m);                      // <= 16
+    int before = 0, all = 0;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += y;
+    for (int bit = 0; bit < 5; ++bit) {
+      const uint32_t have = __ballot_sync(0xffffffffu, n >> bit & 1);
+      before += __popc(have & below) << bit;
+      all += __popc(have) << bit;
     }
-    if (i < segs) to[i] = carry + incl - n;
-    carry += __shfl_sync(0xffffffffu, incl, 31);
+    if (n && (base >> 5) % kFewRouters == warp) {
+      put(segs + __popc(any & below), base + lane, n, pairs + before);
+      t.mask[base + lane] = m | (uint32_t)(pairs + before) << 16;
+    }
+    segs += __popc(any);
+    pairs += all;
   }
-  if (lane == 0) to[segs] = carry;
+  if (warp == kFewRouters - 1) {
+    if (lane < p.n_shared) put(segs + lane, p.E + lane, p.T, pairs + lane * p.T);
+    if (lane == 0) {
+      t.off[segs + p.n_shared] = (uint16_t)(pairs + p.n_shared * p.T);
+      t.count[0] = segs + p.n_shared;
+      t.count[1] = pairs + p.n_shared * p.T;
+    }
+  }
+  routers_sync();
+  // the experts' tokens, ascending; an expert that a token names twice takes it once, with both gates
+  const int first = 32 * warp + lane, last = 32 * kFewRouters - 1 - first;
+#pragma unroll 1
+  for (int i = last; i < p.T * p.k; i += 32 * kFewRouters) {
+    const int e = t.own_ids[i], tok = i / p.k, j0 = tok * p.k;
+    if (e < 0) continue;
+    const uint32_t m = t.mask[e];
+    bool again = false;
+    float g = 0.f;
+#pragma unroll 1
+    for (int j = j0; j < j0 + p.k; ++j)
+      if (t.own_ids[j] == e) {
+        again |= j < i;
+        g = __fadd_rn(g, t.own_gates[j]);
+      }
+    if (again) continue;
+    const int at = (int)(m >> 16) + __popc(m & ((1u << tok) - 1));
+    t.token[at] = (uint8_t)tok;
+    t.gate[at] = g;
+  }
+#pragma unroll 1
+  for (int i = last; i < p.n_shared * p.T; i += 32 * kFewRouters) {
+    t.token[pairs + i] = (uint8_t)(i % p.T);
+    t.gate[pairs + i] = 1.f;
+  }
+  // places in the order, first units of phase 1 by place, first steps of phase 2
+  segs += p.n_shared;
+#pragma unroll 1
+  for (int a = first; a <= segs; a += 32 * kFewRouters) {   // (a = segs: the ends)
+    const uint32_t mine = a < segs ? t.key[a] : 0;
+    int place = 0, units = 0, steps = 0;
+#pragma unroll 4
+    for (int o = 0; o < segs; ++o) {
+      const uint32_t key = t.key[o];
+      if (key > mine || (key == mine && o < a)) ++place, units += key >> 4 & 15;
+      if (o < a) steps += key & 15;
+    }
+    if (a < segs) t.order[place] = (uint16_t)a;
+    t.unit0[place] = units * (p.F / kUnitRows);
+    t.step0[a] = steps * fg;
+  }
 }
 
 template <class TAB, int XC, int STAGES>
@@ -255,21 +247,25 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   const int hg = p.H / kGroup, fg = p.F / kGroup;
 
   // ---- routing ----
-  // phase 1: sums [16 warps], rings, staged operand; phase 2: sums [16 warps][T tokens], rings
-  char* const ring1 = smem + kTableBytes<TAB> + kStreamWarps * kSumFloats * 4;
-  float* const xsum = reinterpret_cast<float*>(ring1 + kStreamWarps * STAGES * slot_bytes(0));
-  char* const pieces = reinterpret_cast<char*>(xsum) + ((hg * 3 * p.T * 4 + 127) & ~127);
-  // a few warps route and make the tables; the others bring the tokens into shared memory and ask the L2 cache for the
-  // shared experts, which are wanted whatever the routing is
+  // shared memory: tables, sums of 16 warps, rings of 16 warps; then in phase 1 the staged operand and its sums, in phase 2
+  // slots of the streamed operand of 16 warps, and sums of 16 warps for all tokens, if those are more than a unit's
+  char* const ring = smem + kTableBytes<TAB> + kStreamWarps * kSumFloats * 4;
+  char* const rest = ring + kStreamWarps * STAGES * kSlotBytes;
+  float* const xsum = reinterpret_cast<float*>(rest);
+  char* const pieces = rest + ((hg * 3 * p.T * 4 + 127) & ~127);
+  // a few warps route and make the tables; the others bring the layer's rows of the page table into shared memory (the rings
+  // are still empty), ask the L2 cache for the shared experts, which are wanted whatever the routing is, and bring the tokens
   if (warp < kFewRouters) {
-    if (warp == 0)
 #pragma unroll 1
-      for (int e = lane; e < p.E; e += 32) t.mask[e] = 0;
+    for (int e = tid; e < 256; e += 32 * kFewRouters) t.mask[e] = 0;
+    if (tid == 0) t.done = 0;
+    routers_sync();
     if (p.logits) {
 #pragma unroll 1
       for (int tok = warp; tok < p.T; tok += kFewRouters) {
         if (p.E <= 64) route_token_n<2>(p.logits, tok, p.E, p.k, t.own_ids, t.own_gates, lane);
         else route_token_n<kMaxExpertsPerLane>(p.logits, tok, p.E, p.k, t.own_ids, t.own_gates, lane);
+        if (lane < p.k) atomicOr(&t.mask[t.own_ids[tok * p.k + lane]], 1u << tok);
       }
     } else {
 #pragma unroll 1
@@ -281,22 +277,31 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         }
         t.own_ids[i] = id;
         t.own_gates[i] = p.gates[i];
+        if (id >= 0) atomicOr(&t.mask[id], 1u << (i / p.k));
       }
     }
-    routers_sync();
-    make_tables(p, t, fg, warp, lane);
+    asm volatile("bar.sync 9, %0;" ::"n"(kStreamThreads) : "memory");   // the rows are there (and the routing of all)
+    make_tables(p, t, reinterpret_cast<const DevRow*>(ring), fg, warp, lane);
   } else {
     const int thread = tid - 32 * kFewRouters, threads = kStreamThreads - 32 * kFewRouters;
-    const int line = (int)blockIdx.x * threads + thread, lines = (int)gridDim.x * threads;
-    const size_t page_lines = (size_t)p.F * p.H * 2 / 128;
-    int64_t left = kFewAhead / 128;
 #pragma unroll 1
-    for (int i = 0; i < p.n_shared * 2 && left > 0; ++i, left -= page_lines) {
-      const char* page = static_cast<const char*>(p.rows[(p.E + (i >> 1)) * 3 + (i & 1)].codes);
+    for (int i = thread; i < (p.E + p.n_shared) * (3 * (int)sizeof(DevRow) / 16); i += threads)
+      cp16(smem_u32(ring) + i * 16, reinterpret_cast<const char*>(p.rows) + i * 16);
+    cp_commit();
+    cp_wait<0>();
+    asm volatile("bar.arrive 9, %0;" ::"n"(kStreamThreads) : "memory");
+    if (warp == kFewRouters) {
+      // (pages are whole tiles of 32 KB; asked for by the bulk copy engine, not by loads in front of everyone else's)
+      const size_t pieces_of_page = (size_t)p.F * p.H * 2 / kFewAheadPiece;
+      int64_t left = kFewAhead / kFewAheadPiece;
 #pragma unroll 1
-      for (size_t l = line; l < page_lines; l += lines) prefetch_line(page + l * 128);
+      for (int i = 0; i < p.n_shared * 2 && left > 0; ++i, left -= pieces_of_page) {
+        const char* page = static_cast<const char*>(p.rows[(p.E + (i >> 1)) * 3 + (i & 1)].codes);
+#pragma unroll 1
+        for (size_t l = (size_t)lane * gridDim.x + blockIdx.x; l < pieces_of_page; l += 32 * (size_t)gridDim.x) prefetch_bytes(page + l * kFewAheadPiece, kFewAheadPiece);
+      }
     }
-    stage_operand(p.hidden, (size_t)p.H * 2, p.T, p.T, 0, hg, p.H * 2, pieces, xsum, thread, threads);
+    stage_operand<XC <= 2 ? 1 : 4>(p.hidden, (size_t)p.H * 2, p.T, p.T, 0, hg, p.H * 2, pieces, xsum, thread, threads);
   }
   __syncthreads();
   const int segs = t.count[0];
@@ -318,8 +323,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   const int G = (int)gridDim.x, b = (int)blockIdx.x;
   uint32_t before;                                // arrivals, seen before this CTA's: only the top bit matters
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(before) : "l"(p.sync) : "memory");
-  Ring r;
-  r.lane = lane;
+  Ring r{smem_u32(ring) + warp * STAGES * kSlotBytes, 0, smem_u32(rest) + warp * STAGES * 256 * XC, lane};
+  r.slot = r.base;
   Feed f;
   f.left = 0;
 
@@ -329,9 +334,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     const int units = t.unit0[segs], turns = units / G;
     const int mine = turns + (turns & 1 ? G - 1 - b < units - turns * G : b < units - turns * G);
     auto unit_of = [&](int i) { return i * G + (i & 1 ? G - 1 - b : b); };
-    r.base = r.slot = smem_u32(ring1) + warp * STAGES * slot_bytes(0);
     int next = 0;                                 // first of the four units that the feed looks at next
-    auto ask_next = [&](uint32_t slot) {
+    auto ask_next = [&]() {
 #pragma unroll 1
       while (f.left == 0) {
         if (next >= mine) return;
@@ -343,11 +347,11 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         const SegPage& page = t.page[3 * g.a + g.kind];
         feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * g.a + g.kind], hg, g.slice, g.lo, g.lo + g.n);
       }
-      ask_any<0>(f, slot, lane);
+      ask_any<0>(f, r.slot, 0, lane);
     };
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
-      ask_next(r.slot);
+      ask_next();
       ring_on<0, STAGES>(r);
     }
 #pragma unroll 1
@@ -385,12 +389,16 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   }
 
   // ---- from phase 1 to phase 2 ----
-  cp_wait<0>();
-  __syncthreads();
-  // The CTAs add up to 2^31 between them: the top bit turns when the last one has come, and again in the next call.
-  // (The values were written before the barrier above: released with this addition.)
-  if (tid == 0)
-    asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(p.sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
+  // The CTAs add up to 2^31 between them: the top bit turns when the last one has come, and again in the next call.  The last
+  // warp of a CTA adds for it (the values of the others, released to this warp, are released with its own).  Each warp then
+  // asks for its first codes of phase 2; the places that are written anew meanwhile are its own.
+  __syncwarp();
+  if (lane == 0) {
+    uint32_t n;
+    asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], 1;" : "=r"(n) : "r"(smem_u32(&t.done)) : "memory");
+    if (n == kStreamWarps - 1)
+      asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(p.sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
+  }
 
   // ---- phase 2: down ----
   {
@@ -404,7 +412,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       lo = slice_of((int)(steps * i >> ts));
       hi = slice_of((int)(steps * (i + 1) >> ts));
     };
-    r.base = r.slot = smem_u32(smem) + kTableBytes<TAB> + kStreamWarps * p.T * kSumPitch * 4 + warp * STAGES * slot_bytes(XC);
+    cp_wait<0>();
+    r.slot = r.base;
     f.left = 0;
     // the feed's next four units, its place in the list of steps, and its slice
     int next = 0, at = 0, end = 0, hint = 0, slice = 0;
@@ -428,28 +437,27 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       feed_operand(f, lane, p.h + (size_t)pair0 * p.F * 2, (uint32_t)p.F * 2, min(kUnitCols, t.off[d.a + 1] - pair0), d.lo);
       return true;
     };
-    // The first steps are asked for without their operand, which is not there yet.  What a lane will copy of it waits in the
-    // lane's place of the slot.
-    int asked = STAGES;
-    auto ask_next = [&](uint32_t slot) {
+    // The first steps are asked for without their operand, which is not there yet.  What a lane will copy of it is noted in
+    // the warp's sums of phase 1: its place in p.h, the rows, and log2 of the steps of a group.
+    const uint32_t notes = smem_u32(sums + warp * kSumFloats) + lane * 8;
+    static_assert(STAGES * 256 <= kSumFloats * 4, "room for the notes");
+    int asked = 0;
+    auto ask_next = [&]() {
       if (f.left == 0 && !more()) return;
       const int copies = f.copies;
       if (asked < STAGES) {
         const int ls = step_shift(f.fmt);
         const char* x = f.x + (ls == 1 ? f.sub * 128 : ls == 2 ? (f.sub ^ ((lane >> 2) & 1)) * 64 : 0);
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(slot + kStepCodes + kStepMeta + lane * 16), "r"((uint32_t)(uintptr_t)x),
-                     "r"((uint32_t)((uintptr_t)x >> 32)), "r"(f.x_step), "r"((uint32_t)copies)
-                     : "memory");
+        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(notes + asked * 256), "r"((uint32_t)(x - p.h)), "r"((uint32_t)(copies << 2 | ls)) : "memory");
         ++asked;
         f.copies = 0;
       }
-      ask_any<XC>(f, slot, lane);
+      ask_any<XC>(f, r.slot, r.x, lane);
       f.copies = copies;
     };
-    asked = 0;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
-      ask_next(r.slot);
+      ask_next();
       ring_on<XC, STAGES>(r);
     }
     const int first_steps = asked;
@@ -461,7 +469,11 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       const Feed ahead = f;
       const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
 #pragma unroll 1
-      for (int i = 0; i < kFewAheadSteps && (f.left || more()); ++i) prefetch_step(f, lane);
+      for (int i = 0; i < kFewAheadSteps && (f.left || more());) {
+        const int n = min(f.left, kFewAheadSteps - i);
+        prefetch_steps(f, lane, n);
+        i += n;
+      }
       f = ahead;
       next = a0, at = a1, end = a2, hint = a3, slice = a4;
     }
@@ -483,15 +495,17 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
       if (i < first_steps) {
-        const uint32_t to = r.base + i * slot_bytes(XC) + kStepCodes + kStepMeta + lane * 16;
-        const uint4 w = lds16(to);
-        const char* x = reinterpret_cast<const char*>((uintptr_t)w.x | (uintptr_t)w.y << 32);
+        const uint2 w = lds8(notes + i * 256);
+        const uint32_t to = r.x + i * (256 * XC) + lane * 16, step = (uint32_t)p.F * 2 << ((w.y & 3) + 1);
 #pragma unroll 1
-        for (int j = 0; j < (int)w.w; ++j) cp16(to + j * 512, x + (size_t)j * w.z);   // (rows behind the first lie behind all lanes' places)
+        for (uint32_t j = 0; j < w.y >> 2; ++j) cp16(to + j * 512, p.h + w.x + (size_t)j * step);
       }
       cp_commit();
     }
-    float* const own = sums + warp * p.T * kSumPitch;
+    // (for no more tokens than a unit's where those of phase 1 were, and the notes: a warp's place is its own)
+    const int set_floats = max(p.T, kUnitCols) * kSumPitch;
+    float* const sums2 = p.T <= kUnitCols ? sums : reinterpret_cast<float*>(rest + kStreamWarps * STAGES * 256 * XC);
+    float* const own = sums2 + warp * set_floats;
 #pragma unroll 1
     for (int first = 0; first < mine; first += 4) {
       const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
@@ -510,7 +524,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         const int pair0 = t.off[d.a] + d.pass * kUnitCols, cols = min(kUnitCols, t.off[d.a + 1] - pair0);
         const int xc = min(lane >> 2, cols - 1);
         float tot[2][4] = {};
-        Operand o{(uint32_t)(kStepCodes + kStepMeta + xc * (256 >> ls)), 0, 0, 0, ls == 2 ? 0 : (uint32_t)(xc & 1) << 2, d.lo};
+        Operand o{(uint32_t)(xc * (256 >> ls)), 0, 0, 0, ls == 2 ? 0 : (uint32_t)(xc & 1) << 2, d.lo};
         walk<kAnyFormat, XC, STAGES>(fixed, fmt, d.n, f, r, o, tot, ask_next);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {             // the tokens of a run are different ones: no two lanes meet
@@ -529,14 +543,14 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         __syncwarp();
       }
       few_team_sync(team, ts);
-      float* const set = sums + (team << ts) * p.T * kSumPitch;
+      float* const set = sums2 + (team << ts) * set_floats;
       const int row0 = slice_of(unit) * kUnitRows, part = unit - slice_of(unit) * p.n_parts;
 #pragma unroll 1
       for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
         const int row = i & (kUnitRows - 1), tok = i >> 5;
         float v = 0.f;
 #pragma unroll 4
-        for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, set[(w * p.T + tok) * kSumPitch + row]);
+        for (int w = 0; w < 1 << ts; ++w) v = __fadd_rn(v, set[w * set_floats + tok * kSumPitch + row]);
         if (p.n_parts == 1) store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
         else p.parts[((size_t)part * p.T + tok) * p.H + row0 + row] = v;
       }
@@ -642,10 +656,9 @@ static const FewVariant kFewVariants[] = {few_variant<FewSmall, 2, 4>(), few_var
                                           few_variant<FewAll, 8, 3>(),   few_variant<FewSmall, 8, 2>(), few_variant<FewAll, 8, 2>()};
 
 static size_t few_smem(const FewArgs& a, const FewVariant& v) {
-  const size_t first = (size_t)kStreamWarps * (kSumFloats * 4 + v.stages * slot_bytes(0)) +
-                       (((size_t)a.H / kGroup * 3 * a.T * 4 + 127) & ~(size_t)127) + (size_t)a.T * a.H * 2;
-  const size_t second = (size_t)kStreamWarps * ((size_t)a.T * kSumPitch * 4 + (size_t)v.stages * slot_bytes(v.rows));
-  return v.table_bytes + (first > second ? first : second);
+  const size_t first = (((size_t)a.H / kGroup * 3 * a.T * 4 + 127) & ~(size_t)127) + (size_t)a.T * a.H * 2;
+  const size_t second = (size_t)kStreamWarps * (v.stages * 256 * v.rows + (a.T <= kUnitCols ? 0 : a.T * kSumPitch * 4));
+  return v.table_bytes + (size_t)kStreamWarps * (kSumFloats * 4 + v.stages * kSlotBytes) + (first > second ? first : second);
 }
 
 static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, const Routing& routing, int T, int top_k, const pw_page_table* table,

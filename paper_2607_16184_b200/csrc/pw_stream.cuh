@@ -67,10 +67,11 @@ constexpr int kStreamWarps = 16;
 constexpr int kStreamThreads = kStreamWarps * 32;
 constexpr int kUnitRows = 32;
 constexpr int kUnitCols = 8;                      // tokens of a unit
-constexpr int kStepCodes = 2048;                  // bytes of a slot: codes, scales and zero-points, streamed operand rows
+constexpr int kStepCodes = 2048;                  // bytes of a slot: codes, scales and zero-points
 constexpr int kStepMeta = 128;
-// rows: operand rows that are streamed with the codes; 0: they are staged
-__host__ __device__ constexpr int slot_bytes(int rows) { return kStepCodes + kStepMeta + 256 * rows; }
+constexpr int kSlotBytes = kStepCodes + kStepMeta;
+// Operand rows that are streamed with the codes have slots of 256 bytes a row, two rows at least (every lane's 16 bytes),
+// in a place of their own.
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -98,9 +99,15 @@ __device__ __forceinline__ uint32_t lds4(uint32_t at) {
 // Where the 16 bytes of unit u of row `row` lie in a slot, and with 16-byte (u < 4), 8-byte (u < 2) or 4-byte loads of the
 // product's lanes: the loads take rows 4g + j, j fixed, and what makes them meet different banks goes into bits 0, 1 of the
 // row.
-template <int F>
-__host__ __device__ constexpr uint32_t code_at(uint32_t u, uint32_t row) {
-  return 512 * u + 16 * (row ^ (F <= kFmt4 ? u : u < 2 ? ((row >> 3) & 1) ^ (2 * u) : (row >> 3) & 3));
+//     512 * u + 16 * (row ^ (F <= kFmt4 ? u : u < 2 ? ((row >> 3) & 1) ^ (2 * u) : (row >> 3) & 3))
+// Slots start at multiples of 64, so what is exchanged is two bits of an address: one instruction from one row or unit to
+// the next.  The writing lane's place in unit u, row = lane:
+template <int F, int U>
+__device__ __forceinline__ uint32_t write_at(uint32_t slot, uint32_t lane) {
+  const uint32_t row = slot + 16 * lane;
+  if constexpr (F <= kFmt4) return (row ^ (16 * U)) + 512 * U;
+  else if constexpr (U < 2) return (row ^ (lane << 1 & 16) ^ (32 * U)) + 512 * U;
+  else return (row ^ (lane << 1 & 48)) + 512 * U;
 }
 __host__ __device__ constexpr uint32_t piece_at(uint32_t e, uint32_t row) { return e ^ (e >> 2) ^ ((row & 1) << 2); }
 
@@ -146,14 +153,14 @@ __device__ __forceinline__ void feed_operand(Feed& f, int lane, const char* x, u
 // Asks for a step in format F and moves on; `left` is the caller's.  XC: the most operand rows that are streamed with it, 0:
 // the operand is staged.
 template <int F, int XC>
-__device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
+__device__ __forceinline__ void ask(Feed& f, uint32_t slot, uint32_t xslot, int lane) {
   constexpr int ls = step_shift(F);
   if constexpr (XC > 0) {
     // the step's part of a group's pieces: all, the half `sub`, or the quarter `sub` (quarters of odd rows are exchanged)
     const char* src = f.x;
     if constexpr (ls == 1) src += f.sub * 128;
     if constexpr (ls == 2) src += (f.sub ^ ((lane >> 2) & 1)) * 64;
-    const uint32_t dst = slot + kStepCodes + kStepMeta + lane * 16;
+    const uint32_t dst = xslot + lane * 16;
 #pragma unroll
     for (int j = 0; j < (XC >> (ls + 1) > 0 ? XC >> (ls + 1) : 1); ++j)
       if (j < f.copies) cp16(dst + j * 512, src + j * f.x_step);
@@ -161,15 +168,17 @@ __device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
   }
   constexpr uint32_t tile = stream_tile_bytes(F);
   constexpr int units = F <= kFmt4 ? 4 : F == kFmt3 ? 3 : 2;
-#pragma unroll
-  for (int u = 0; u < units; ++u) cp16(slot + code_at<F>(u, lane), f.codes + u * 2048);
+  cp16(write_at<F, 0>(slot, lane), f.codes);
+  cp16(write_at<F, 1>(slot, lane), f.codes + 2048);
+  if constexpr (units > 2) cp16(write_at<F, 2>(slot, lane), f.codes + 4096);
+  if constexpr (units > 3) cp16(write_at<F, 3>(slot, lane), f.codes + 6144);
   if (F != kFmt16 && lane < 8) cp16(slot + kStepCodes + lane * 16, f.meta);
   if constexpr (F == kFmtP4 || F == kFmtP3) {
-    cp16(slot + code_at<F>(2, lane), f.bit1);
+    cp16(write_at<F, 2>(slot, lane), f.bit1);
     f.bit1 += kPlaneBitTile;
   }
   if constexpr (F == kFmtP4) {
-    cp16(slot + code_at<F>(3, lane), f.bit0);
+    cp16(write_at<F, 3>(slot, lane), f.bit0);
     f.bit0 += kPlaneBitTile;
   }
   if constexpr (F == kFmt16) {
@@ -184,37 +193,41 @@ __device__ __forceinline__ void ask(Feed& f, uint32_t slot, int lane) {
   if constexpr (ls > 0) f.sub = (f.sub + 1) & ((1 << ls) - 1);
 }
 template <int XC>
-__device__ __forceinline__ void ask_any(Feed& f, uint32_t slot, int lane) {
+__device__ __forceinline__ void ask_any(Feed& f, uint32_t slot, uint32_t xslot, int lane) {
   f.left--;
   switch (f.fmt) {
-    case kFmt16: ask<kFmt16, XC>(f, slot, lane); break;
-    case kFmt8: ask<kFmt8, XC>(f, slot, lane); break;
-    case kFmt4: ask<kFmt4, XC>(f, slot, lane); break;
-    case kFmt3: ask<kFmt3, XC>(f, slot, lane); break;
-    case kFmt2: ask<kFmt2, XC>(f, slot, lane); break;
-    case kFmtP4: ask<kFmtP4, XC>(f, slot, lane); break;
-    case kFmtP3: ask<kFmtP3, XC>(f, slot, lane); break;
-    default: ask<kFmtP2, XC>(f, slot, lane); break;
+    case kFmt16: ask<kFmt16, XC>(f, slot, xslot, lane); break;
+    case kFmt8: ask<kFmt8, XC>(f, slot, xslot, lane); break;
+    case kFmt4: ask<kFmt4, XC>(f, slot, xslot, lane); break;
+    case kFmt3: ask<kFmt3, XC>(f, slot, xslot, lane); break;
+    case kFmt2: ask<kFmt2, XC>(f, slot, xslot, lane); break;
+    case kFmtP4: ask<kFmtP4, XC>(f, slot, xslot, lane); break;
+    case kFmtP3: ask<kFmtP3, XC>(f, slot, xslot, lane); break;
+    default: ask<kFmtP2, XC>(f, slot, xslot, lane); break;
   }
 }
 
-// Asks the L2 cache for the codes of a step, and moves on.
-__device__ __forceinline__ void prefetch_line(const char* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
-__device__ __forceinline__ void prefetch_step(Feed& f, int lane) {
-  const int ls = step_shift(f.fmt), units = f.fmt <= kFmt4 ? 4 : f.fmt == kFmt3 ? 3 : 2;
-  const uint32_t tile = kTileBytes[f.fmt];
-  const int u = lane >> 2, line = (lane & 3) * 128;   // lanes 0 .. 15: the lines of unit u; 16, 17: scales and zero-points
-  if (u < units) prefetch_line(f.codes - lane * 16 + u * 2048 + line);
-  else if (u == 2 && (f.fmt == kFmtP4 || f.fmt == kFmtP3)) prefetch_line(f.bit1 - lane * 16 + line);
-  else if (u == 3 && f.fmt == kFmtP4) prefetch_line(f.bit0 - lane * 16 + line);
-  else if (u == 4 && (lane & 3) < 2 && f.fmt != kFmt16) prefetch_line(f.meta - u * 256 - (lane & 3) * 16 + (lane & 3) * 256);
-  f.left--;
-  const bool last = f.sub == (1 << ls) - 1;
-  f.codes += last ? tile - (((uint32_t)1 << ls) - 1) * 8192u : 8192u;
-  f.meta += last ? tile : 0u;
-  f.bit1 += kPlaneBitTile;
-  f.bit0 += kPlaneBitTile;
-  f.sub = last ? 0 : f.sub + 1;
+// Asks the L2 cache for the codes of the next n steps, eight at most, and moves on: each lane for a piece of 512 bytes, of
+// unit lane % 4 of step lane / 4.
+__device__ __forceinline__ void prefetch_bytes(const char* p, uint32_t n) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(n) : "memory");
+}
+__device__ __forceinline__ void prefetch_steps(Feed& f, int lane, int n) {
+  const int ls = step_shift(f.fmt), last = (1 << ls) - 1, units = f.fmt <= kFmt4 ? 4 : f.fmt == kFmt3 ? 3 : 2;
+  const size_t tile = kTileBytes[f.fmt];
+  const int i = lane >> 2, u = lane & 3, at = f.sub + i;
+  if (i < n) {
+    if (u < units) prefetch_bytes(f.codes - lane * 16 + (at >> ls) * tile + ((at & last) - f.sub) * 8192 + u * 2048, 512);
+    else if (f.fmt == kFmtP4 || (f.fmt == kFmtP3 && u == 2)) prefetch_bytes((u == 2 ? f.bit1 : f.bit0) - lane * 16 + (size_t)i * kPlaneBitTile, 512);
+    if (u < 2 && f.fmt != kFmt16) prefetch_bytes(f.meta - (lane >> 2) * 256 - (lane & 3) * 16 + (at >> ls) * tile + u * 256, 64);
+  }
+  const int to = f.sub + n;
+  f.left -= n;
+  f.codes += (to >> ls) * tile + ((to & last) - f.sub) * 8192;
+  f.meta += (to >> ls) * tile;
+  f.bit1 += n * kPlaneBitTile;
+  f.bit0 += n * kPlaneBitTile;
+  f.sub = to & last;
 }
 
 // ---- staged operand ------------------------------------------------------------------------------
@@ -229,44 +242,58 @@ __device__ __forceinline__ float sum_halves(const uint4& v) {
 }
 // Groups g0 .. g0 + groups of `rows` operand rows (fp16, `pitch` bytes apart, k_bytes of a row count, zeros behind them) ->
 // pieces [group][room][256 bytes] and the sums of the first half, the second half and the whole of every group,
-// [group][3][room] (sums may be null).  By `threads` threads (whole warps).
+// [group][3][room].  By `threads` threads (whole warps), with AHEAD stretches of each in flight.
+template <int AHEAD>
 __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int rows, int room, int g0, int groups, int k_bytes, char* pieces, float* sums,
                                               int thread, int threads) {
   const int n = rows * groups * 8;
 #pragma unroll 1
-  for (int base = thread & ~31; base < n; base += threads) {
-    const int i = base + (thread & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
-    uint4 v[2] = {};
-    if (i < n) {
-      const int k = (g0 + g) * 256 + s * 32;
-      const char* src = x + (size_t)c * pitch + k;
-      if (k + 32 <= k_bytes) {
-        v[0] = reinterpret_cast<const uint4*>(src)[0];
-        v[1] = reinterpret_cast<const uint4*>(src)[1];
-      } else {
-        // (one way only for the last, short stretch: it is met once in a row)
-        uint32_t w[8] = {};
+  for (int base = thread & ~31; base < n; base += AHEAD * threads) {
+    uint4 v[AHEAD][2];
+    int place[AHEAD];                            // g * room + c
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (k + 4 * j < k_bytes) w[j] = reinterpret_cast<const uint16_t*>(src)[2 * j];
-          if (k + 4 * j + 2 < k_bytes) w[j] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[2 * j + 1] << 16;
+    for (int a = 0; a < AHEAD; ++a) {
+      const int i = base + a * threads + (thread & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
+      place[a] = g * room + c;
+      v[a][0] = v[a][1] = make_uint4(0, 0, 0, 0);
+      if (i < n) {
+        const int k = (g0 + g) * 256 + s * 32;
+        const char* src = x + (size_t)c * pitch + k;
+        if (k + 32 <= k_bytes) {
+          v[a][0] = reinterpret_cast<const uint4*>(src)[0];
+          v[a][1] = reinterpret_cast<const uint4*>(src)[1];
+        } else if (k < k_bytes) {
+          // (one way only for the last, short stretch: it is met once in a row)
+          uint32_t w[8] = {};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (k + 4 * j < k_bytes) w[j] = reinterpret_cast<const uint16_t*>(src)[2 * j];
+            if (k + 4 * j + 2 < k_bytes) w[j] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[2 * j + 1] << 16;
+          }
+          v[a][0] = make_uint4(w[0], w[1], w[2], w[3]);
+          v[a][1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
-        v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        v[1] = make_uint4(w[4], w[5], w[6], w[7]);
       }
-      uint4 piece[2];
-      make_pieces(v[0], v[1], piece);
-      char* row = pieces + (size_t)(g * room + c) * 256;
-      *reinterpret_cast<uint4*>(row + piece_at(2 * s, c) * 16) = piece[0];
-      *reinterpret_cast<uint4*>(row + piece_at(2 * s + 1, c) * 16) = piece[1];
     }
-    float a = sum_halves(v[0]) + sum_halves(v[1]);
-    a += __shfl_xor_sync(0xffffffffu, a, 1);
-    a += __shfl_xor_sync(0xffffffffu, a, 2);
-    const float b = a + __shfl_xor_sync(0xffffffffu, a, 4);
-    if (sums && i < n && (s & 3) == 0) {
-      sums[(g * 3 + (s >> 2)) * room + c] = a;
-      if (s == 0) sums[(g * 3 + 2) * room + c] = b;
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      if (base + a * threads >= n) break;         // (the same for a whole warp)
+      const int i = base + a * threads + (thread & 31), s = i & 7, g = place[a] / room, c = place[a] - g * room;
+      if (i < n) {
+        uint4 piece[2];
+        make_pieces(v[a][0], v[a][1], piece);
+        char* row = pieces + (size_t)place[a] * 256;
+        *reinterpret_cast<uint4*>(row + piece_at(2 * s, c) * 16) = piece[0];
+        *reinterpret_cast<uint4*>(row + piece_at(2 * s + 1, c) * 16) = piece[1];
+      }
+      float part = sum_halves(v[a][0]) + sum_halves(v[a][1]);
+      part += __shfl_xor_sync(0xffffffffu, part, 1);
+      part += __shfl_xor_sync(0xffffffffu, part, 2);
+      const float whole = part + __shfl_xor_sync(0xffffffffu, part, 4);
+      if (i < n && (s & 3) == 0) {
+        sums[(g * 3 + (s >> 2)) * room + c] = part;
+        if (s == 0) sums[(g * 3 + 2) * room + c] = whole;
+      }
     }
   }
 }
@@ -290,7 +317,11 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
 // instruction, which was a sixth of a 4-bit step's instructions.
 struct Fixed {
   float zero[4];
+  uint32_t up[3];                                 // 16 (4 bits); 64, 16, 4: a multiplication is not for the pipe of the shifts
   __device__ __forceinline__ Fixed() {
+    asm volatile("mov.b32 %0, 64;" : "=r"(up[0]));
+    asm volatile("mov.b32 %0, 16;" : "=r"(up[1]));
+    asm volatile("mov.b32 %0, 4;" : "=r"(up[2]));
 #pragma unroll
     for (int i = 0; i < 4; ++i) asm volatile("mov.b32 %0, 0f00000000;" : "=f"(zero[i]));
   }
@@ -356,22 +387,22 @@ struct Codes {
       }
     }
   }
-  __device__ __forceinline__ uint32_t pair(int j, int p) const {
+  __device__ __forceinline__ uint32_t pair(const Fixed& k, int j, int p) const {
     if constexpr (F == kFmt8) {
       return __byte_perm(w[2 * p + (j >> 1)], 0, j & 1 ? 0x4342 : 0x4140);
     } else if constexpr (F == kFmt4) {
       const uint32_t byte = j & 2 ? w[p] >> 8 : w[p];
-      return (j & 1 ? byte : byte * 16) & 0x00f000f0u;
+      return (j & 1 ? byte : byte * k.up[1]) & 0x00f000f0u;
     } else {
       constexpr uint32_t one = 0x00010001u;
       uint32_t v = w[p] & ((3u << (2 * j + up)) * one);
       if constexpr (third || up) v = and_or(w[2 + p], (third ? 4u << (2 * j) : up == 2 ? 3u << (2 * j) : 1u << (2 * j)) * one, v);
-      return v * (64u >> (2 * j));
+      return j == 3 ? v : v * k.up[j];
     }
   }
 };
 
-// One step in format F out of a slot.  x: this lane's operand row, with the step's pieces at (at0 ^ i) * 16 bytes.  SUMS:
+// One step in format F out of a slot.  xrow: this lane's operand row, with the step's pieces at at0 ^ 16 i.  SUMS:
 // the operands' sums are at at_sum0 and at_sum1, else they are made here, by a row of ones on the same fragments.
 template <int F, bool SUMS>
 __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int lane, uint32_t xrow, uint32_t at0, uint32_t at_sum0, uint32_t at_sum1,
@@ -379,13 +410,12 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
   const uint32_t g = (uint32_t)lane >> 2, t = (uint32_t)lane & 3;
   if constexpr (F == kFmt16) {
     // columns of the lane: pairs 2b, 2b + 1 (b = t mod 2) of both halves of stretch t / 2
-    const uint32_t at = slot + 1024 * (t >> 1) + 8 * (t & 1);
-    const uint4 x = lds16(xrow + (at0 << 4));
+    const uint32_t at = slot + 1024 * (t >> 1) + 8 * (t & 1) + 64 * g + 32 * (t >> 1);   // unit 2 (t / 2), row 4g
+    const uint4 x = lds16(xrow + at0);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t r = 4 * g + 2 * h, u = 2 * (t >> 1);
-      const uint2 a0 = lds8(at + 16 * (r ^ u)), b0 = lds8(at + 16 * ((r + 1) ^ u));
-      const uint2 a1 = lds8(at + 16 * (r ^ (u + 1)) + 512), b1 = lds8(at + 16 * ((r + 1) ^ (u + 1)) + 512);
+      const uint32_t r0 = at ^ (32 * h), r1 = r0 ^ 16;
+      const uint2 a0 = lds8(r0), b0 = lds8(r1), a1 = lds8(r1 + 512), b1 = lds8(r0 + 512);
       mma16(tot[h], a0.x, b0.x, a1.x, b1.x, x.x, x.y);
       mma16(tot[h], a0.y, b0.y, a1.y, b1.y, x.z, x.w);
     }
@@ -394,7 +424,7 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
     constexpr int S = F == kFmt8 ? 1 : 2;         // stretches of a lane
     uint4 x[2 * S];
 #pragma unroll
-    for (int i = 0; i < 2 * S; ++i) x[i] = lds16(xrow + ((at0 ^ i) << 4));
+    for (int i = 0; i < 2 * S; ++i) x[i] = lds16((xrow + at0) ^ (16 * i));
     float sum0, sum1;
     if constexpr (SUMS) {
       sum0 = __uint_as_float(lds4(at_sum0)), sum1 = __uint_as_float(lds4(at_sum1));
@@ -410,6 +440,10 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
     }
     Scales m;
     load_scales<F>(slot, g, m);
+    // row 4g of the lane's unit, of its part of a leading unit, of its part of units 2 and 3
+    const uint32_t wide_at = slot + 64 * g + 528 * t;
+    const uint32_t lead_at = slot + 64 * g + 16 * ((g >> 1 & 1) ^ (t & 2)) + 512 * (t >> 1) + 8 * (t & 1);
+    const uint32_t low_at = slot + 64 * g + 16 * (g >> 1 & 3) + 4 * t;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint4 wide[2];
@@ -417,12 +451,12 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
       uint32_t h1[2], h0[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const uint32_t row = 4 * g + 2 * h + r;
+        const uint32_t row = 16 * (2 * h + r);
         wide[r] = make_uint4(0, 0, 0, 0), lead[r] = make_uint2(0, 0), h1[r] = h0[r] = 0;
-        if constexpr (F <= kFmt4) wide[r] = lds16(slot + code_at<F>(t, row));
-        else lead[r] = lds8(slot + code_at<F>(t >> 1, row) + 8 * (t & 1));
-        if constexpr (C::third || C::up) h1[r] = lds4(slot + code_at<F>(2, row) + 4 * t);
-        if constexpr (C::up == 2) h0[r] = lds4(slot + code_at<F>(3, row) + 4 * t);
+        if constexpr (F <= kFmt4) wide[r] = lds16(wide_at ^ row);
+        else lead[r] = lds8(lead_at ^ row);
+        if constexpr (C::third || C::up) h1[r] = lds4((low_at ^ row) + 1024);
+        if constexpr (C::up == 2) h0[r] = lds4((low_at ^ row) + 1536);
       }
       float acc[S][4];
 #pragma unroll
@@ -434,8 +468,8 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
         for (int j = 0; j < 4; ++j) {
           const uint4& xs = x[2 * s + (j >> 1)];
           const uint32_t b0 = j & 1 ? xs.z : xs.x, b1 = j & 1 ? xs.w : xs.y;
-          if (j == 0) mma16_first(k, acc[s], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
-          else mma16(acc[s], c[0].pair(j, 0), c[1].pair(j, 0), c[0].pair(j, 1), c[1].pair(j, 1), b0, b1);
+          if (j == 0) mma16_first(k, acc[s], c[0].pair(k, j, 0), c[1].pair(k, j, 0), c[0].pair(k, j, 1), c[1].pair(k, j, 1), b0, b1);
+          else mma16(acc[s], c[0].pair(k, j, 0), c[1].pair(k, j, 0), c[0].pair(k, j, 1), c[1].pair(k, j, 1), b0, b1);
         }
       }
       if constexpr (S == 2) {
@@ -450,12 +484,15 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
 // ---- a warp's walk over its steps ----------------------------------------------------------------
 struct Ring {
   uint32_t base, slot;                            // shared memory: the warp's slots, the next step's
+  uint32_t x;                                     // the next step's slot of the streamed operand
   int lane;
 };
 template <int XC, int STAGES>
 __device__ __forceinline__ void ring_on(Ring& r) {
   cp_commit();
-  r.slot = r.slot == r.base + (STAGES - 1) * slot_bytes(XC) ? r.base : r.slot + slot_bytes(XC);
+  const bool last = r.slot == r.base + (STAGES - 1) * kSlotBytes;
+  r.slot = last ? r.base : r.slot + kSlotBytes;
+  if constexpr (XC > 0) r.x += last ? -(STAGES - 1) * 256 * XC : 256 * XC;
 }
 // Multiplies steps of a block in format F, at most n, and asks for the next step of the feed after each while that is in
 // the same format.  Returns with n = 0, or having multiplied a step without having asked (true).
@@ -465,8 +502,8 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
   const uint32_t t = (uint32_t)r.lane & 3;
   // The lane's pieces of a step: e = 4t + i, 8q + 2t + i or 4q + t, q the step inside its group, in the order of piece_at:
   // at0 ^ (what q adds) ^ i.  A streamed row is the part of its step.
-  const uint32_t at0 = (ls == 0 ? 5 * t : ls == 1 ? (2 * t) ^ (t >> 1) : t) ^ o.flip;
-  constexpr uint32_t of_q = ls == 1 ? (XC ? 2 : 10) : XC ? 1 : 5;
+  const uint32_t at0 = 16 * ((ls == 0 ? 5 * t : ls == 1 ? (2 * t) ^ (t >> 1) : t) ^ o.flip);
+  constexpr uint32_t of_q = 16 * (ls == 1 ? (XC ? 2 : 10) : XC ? 1 : 5);
   const uint32_t x_group = (uint32_t)o.room * 256, sum_part = (uint32_t)o.room * 4, sum_group = 3 * sum_part, grp = (uint32_t)o.step >> ls;
   uint32_t x = o.x, sum0 = o.sum0, sum1 = o.sum1;
   if constexpr (XC == 0) x += grp * x_group, sum0 += grp * sum_group, sum1 += grp * sum_group;
@@ -479,7 +516,7 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
     __syncwarp();                                 // what the other lanes have copied
     const uint32_t q = ls ? (uint32_t)o.step & ((1 << ls) - 1) : 0;
     const uint32_t part = ls == 1 ? q * sum_part : 2 * sum_part;
-    multiply_step<F, XC == 0>(k, r.slot, r.lane, XC ? x + r.slot : x, ls ? at0 ^ (of_q * q) : at0, sum0 + part, sum1 + part, tot);
+    multiply_step<F, XC == 0>(k, r.slot, r.lane, XC ? x + r.x : x, ls ? at0 ^ (of_q * q) : at0, sum0 + part, sum1 + part, tot);
     if (XC == 0 && (ls == 0 || q == (1 << ls) - 1)) {
       x += x_group;
       sum0 += sum_group;
@@ -491,13 +528,13 @@ __device__ __forceinline__ bool walk_format(const Fixed& k, int& n, Feed& f, Rin
     due = asks == 0;
     if (due) break;
     --asks;
-    ask<F, XC>(f, r.slot, r.lane);
+    ask<F, XC>(f, r.slot, r.x, r.lane);
     ring_on<XC, STAGES>(r);
   } while (n);
   return due;
 }
 // Multiplies the next n steps, all of one block in format `fmt` (F, if that is not kAnyFormat: all blocks are), and asks for
-// as many.  ask_next(slot): asks for the feed's next step, of the next block if need be, or for
+// as many.  ask_next(): asks for the feed's next step, of the next block if need be, into the ring's next slot, or for
 // nothing if there is none.
 constexpr int kAnyFormat = -1;
 template <int F, int XC, int STAGES, class AskNext>
@@ -519,7 +556,7 @@ __device__ __forceinline__ void walk(const Fixed& k, int fmt, int n, Feed& f, Ri
       }
     }
     if (due) {
-      ask_next(r.slot);
+      ask_next();
       ring_on<XC, STAGES>(r);
     }
   }

@@ -13,43 +13,39 @@ template <int NS>   // NS = 32-expert strides a lane holds (1, 2, 4 or 8): the l
 __device__ __forceinline__ void route_token_n(const float* logits, int token, int E, int k,
                                               int32_t* __restrict__ topk_ids, float* __restrict__ gates, int lane) {
   const float* l = logits + (size_t)token * E;
-  float v[NS];
+  // Logits in an order-preserving form: a warp's largest whole number is one instruction.  Both zeros are the same logit.
+  uint32_t v[NS];
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     const int e = lane + 32 * i;
-    v[i] = e < E ? fmaxf(l[e], -INFINITY) : -INFINITY;   // a NaN loses every comparison: without k others no expert would be found
+    // a NaN loses every comparison: without k others no expert would be found
+    const uint32_t bits = __float_as_uint((e < E ? fmaxf(l[e], -INFINITY) : -INFINITY) + 0.f);
+    v[i] = e < E ? bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u) : 0u;   // 0: no expert, or taken (no float has it)
   }
-  uint32_t taken = 0;
   float l0 = 0.f, S = 0.f, myp = 0.f;
   int myid = 0;
+#pragma unroll 1
   for (int j = 0; j < k; ++j) {
-    float bv = -INFINITY;
-    int bi = 0x7fffffff;
+    uint32_t top = v[0];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const int e = lane + 32 * i;
-      const bool ok = e < E && !((taken >> i) & 1u);
-      if (ok && (v[i] > bv || (v[i] == bv && e < bi))) {
-        bv = v[i];
-        bi = e;
-      }
+    for (int i = 1; i < NS; ++i) top = max(top, v[i]);
+    top = __reduce_max_sync(0xffffffffu, top);
+    int best = 0;
+#pragma unroll
+    for (int i = NS - 1; i >= 0; --i) {
+      const uint32_t has = __ballot_sync(0xffffffffu, v[i] == top);
+      if (has) best = 32 * i + __ffs(has) - 1;
     }
 #pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) {
-      const float ov = __shfl_xor_sync(0xffffffffu, bv, d);
-      const int oi = __shfl_xor_sync(0xffffffffu, bi, d);
-      if (ov > bv || (ov == bv && oi < bi)) {
-        bv = ov;
-        bi = oi;
-      }
-    }
-    if ((bi & 31) == lane) taken |= 1u << (bi >> 5);
-    if (j == 0) l0 = bv;
-    const float p = expf(__fsub_rn(bv, l0));
+    for (int i = 0; i < NS; ++i)
+      if (best == lane + 32 * i) v[i] = 0u;
+    const float logit = __uint_as_float(top & 0x80000000u ? top ^ 0x80000000u : ~top);
+    if (j == 0) l0 = logit;
+    const float p = expf(__fsub_rn(logit, l0));
     S = __fadd_rn(S, p);  // summed in slot order, identically on every lane
     if (lane == j) {
       myp = p;
-      myid = bi;
+      myid = best;
     }
   }
   // k <= 32: lane j owns slot j
