@@ -458,7 +458,7 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
         if constexpr (C::third || C::up) h1[r] = lds4((low_at ^ row) + 1024);
         if constexpr (C::up == 2) h0[r] = lds4((low_at ^ row) + 1536);
       }
-      float acc[S][4];
+      float acc[4];
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         C c[2];
@@ -468,15 +468,11 @@ __device__ __forceinline__ void multiply_step(const Fixed& k, uint32_t slot, int
         for (int j = 0; j < 4; ++j) {
           const uint4& xs = x[2 * s + (j >> 1)];
           const uint32_t b0 = j & 1 ? xs.z : xs.x, b1 = j & 1 ? xs.w : xs.y;
-          if (j == 0) mma16_first(k, acc[s], c[0].pair(k, j, 0), c[1].pair(k, j, 0), c[0].pair(k, j, 1), c[1].pair(k, j, 1), b0, b1);
-          else mma16(acc[s], c[0].pair(k, j, 0), c[1].pair(k, j, 0), c[0].pair(k, j, 1), c[1].pair(k, j, 1), b0, b1);
+          if (s == 0 && j == 0) mma16_first(k, acc, c[0].pair(k, j, 0), c[1].pair(k, j, 0), c[0].pair(k, j, 1), c[1].pair(k, j, 1), b0, b1);
+          else mma16(acc, c[0].pair(k, j, 0), c[1].pair(k, j, 0), c[0].pair(k, j, 1), c[1].pair(k, j, 1), b0, b1);
         }
       }
-      if constexpr (S == 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[0][i] += acc[1][i];
-      }
-      apply_scales(m, h, acc[0], sum0, sum1, tot[h]);
+      apply_scales(m, h, acc, sum0, sum1, tot[h]);
     }
   }
 }
