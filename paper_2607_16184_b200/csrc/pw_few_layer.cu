@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     const int mine = units / G + (b < units % G);
     auto slice_of = [&](int unit) { return p.n_parts == 1 ? unit : (int)__umulhi((uint32_t)unit, p.per_part); };   // unit / n_parts
     auto range = [&](int unit, int ts, int member, int& lo, int& hi) {
-      // steps * i / (n_parts << ts), rounded down (steps * i is below 2^24)
+      // steps * i / (n_parts << ts), rounded down (steps * i is below 2^29: exact)
       const uint32_t i = ((uint32_t)(unit - slice_of(unit) * p.n_parts) << ts) + member;
       lo = slice_of((int)(steps * i >> ts));
       hi = slice_of((int)(steps * (i + 1) >> ts));
@@ -701,14 +701,20 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.sync = reinterpret_cast<int32_t*>(b + w.few_sync);
   a.status = reinterpret_cast<int32_t*>(b + w.status);
   a.seen = ctx->obs_acc ? reinterpret_cast<int32_t*>(b + w.few_seen) : nullptr;
-  // parts of the down blocks' columns: as few as give every SM work, in rounds that are nearly full
-  const int slices = c.hidden / kUnitRows;
+  // Parts of the down blocks' columns: as few as give every SM work, in rounds that are nearly full.  By an estimate in us:
+  // an SM streams 45 KB/us (routed blocks taken for 4 bits), and to add parts up takes 2 us at the end (measured, 1 part /
+  // 2 / 4: one token of 256 x 512 10.8 / 11.6 / 12.2, of 60 + 4 experts of 2048 x 1408 34.1 / 31.1 / 32.5, of 4096 x 14336
+  // 74.0 / 77.7 / 78.1).
+  const int slices = c.hidden / kUnitRows, routed = c.n_experts < T * top_k ? c.n_experts : T * top_k;
+  const double slice_us = 32e-3 * c.ffn * (0.5 * routed + 2. * c.n_shared) / 45.;
   double best = -1.;
   for (int parts = 1; parts <= kFewParts; ++parts) {
     const int rounds = (slices * parts + ctx->num_sms - 1) / ctx->num_sms;
-    const double cost = (double)rounds / parts * (1. + 0.05 * parts) + (parts > 1 ? 0.05 : 0.);
-    if (best < 0 || cost < best) best = cost, a.n_parts = parts;
+    const double us = slice_us * rounds / parts * (1. + 0.05 * parts) + (parts > 1 ? 2. : 0.);
+    if (best < 0 || us < best) best = us, a.n_parts = parts;
   }
+  // (see `range`: a place in the list of steps, times the parts of it, divided by multiplication)
+  if (((int64_t)a.segs + a.pairs / kUnitCols) * (c.ffn / kGroup) * 4 * (kFewParts * kStreamWarps) >= 1 << 29) return PW_ERR_SHAPE;
   a.per_part = a.n_parts > 1 ? (uint32_t)((0xffffffffull + a.n_parts) / a.n_parts) : 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctx->num_sms);
