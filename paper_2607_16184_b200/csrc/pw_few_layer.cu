@@ -20,7 +20,7 @@ constexpr int kFewParts = 8;                      // most parts of the down bloc
 constexpr int kFewRouters = 4;                    // warps that route
 constexpr size_t kFewAhead = 16 << 20;            // bytes of shared experts that are asked for while the tokens are routed (2.5 us)
 constexpr uint32_t kFewAheadPiece = 4096;
-constexpr int kFewAheadSteps = 8;                 // steps of phase 2 that a warp asks the L2 cache for before all CTAs meet
+constexpr int kFewAheadSteps = 4;                 // steps of phase 2 that a warp asks the L2 cache for before all CTAs meet
 constexpr uint32_t kFewPolls = 1u << 22;          // about 3 s
 
 struct FewArgs {
@@ -462,17 +462,22 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     }
     const int first_steps = asked;
     asked = STAGES;
-    // a CTA that has to wait asks for its next steps' codes first, into the L2 cache: the memory works on meanwhile
-    uint32_t arrived;
-    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(arrived) : "l"(p.sync) : "memory");
-    if (__shfl_sync(0xffffffffu, (arrived ^ before) >> 31, 0) == 0) {
+    // a warp that has to wait asks for its next steps' codes meanwhile, into the L2 cache: the memory works on
+    auto open = [&]() {
+      uint32_t now;
+      asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(p.sync) : "memory");
+      return (now ^ before) >> 31;
+    };
+    if (__shfl_sync(0xffffffffu, open(), 0) == 0) {
       const Feed ahead = f;
       const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
 #pragma unroll 1
       for (int i = 0; i < kFewAheadSteps && (f.left || more());) {
-        const int n = min(f.left, kFewAheadSteps - i);
+        const uint32_t is_open = open();          // (on its way while the copies are asked for: those take longer)
+        const int n = min(f.left, 2);
         prefetch_steps(f, lane, n);
         i += n;
+        if (__shfl_sync(0xffffffffu, is_open, 0)) break;
       }
       f = ahead;
       next = a0, at = a1, end = a2, hint = a3, slice = a4;
