@@ -322,23 +322,53 @@ static pw_status check_page(const pw_page& p) {
   return PW_OK;
 }
 
-// Whether a call goes through the tensor-core kernel of the layer calls (three launches, and weights rounded to fp16, which
-// an fp32 output would show), and what of its cut does not depend on the device; the pages have been checked.  By estimates
-// of both times in us, linear in the weights (millions) and the tokens; measured, here / there, at 4 bits: 4096 x 4096
-// 24 tokens 9.2 / 12.8, 64 tokens 17.2 / 15.7; 14336 x 4096 17 tokens 23.7 / 21.0, 64 tokens 48.8 / 26.9, 256 tokens - / 63;
-// 1000 x 1024 64 tokens 3.9 / 11.5.
-static bool many_tokens(DenseCall* d, int T, const pw_page* pages, const int32_t* out_features, int n_pages, int out_type) {
-  if (T <= kUnitCols || out_type == PW_F32) return false;
-  double m = 0;
-  for (int i = 0; i < n_pages; ++i) m += 1e-6 * pages[i].cols * (out_features ? out_features[i] : (int32_t)pages[i].rows);
-  if (2.5 + (T + kUnitCols - 1) / kUnitCols * (0.1 * m + 0.1) <= 10. + m * (0.137 + 0.0032 * T)) return false;
-  *d = DenseCall{};
-  d->T = T;
-  d->cols = (int)pages[0].cols;
-  d->n_pages = n_pages;
+// The fields of `a` that describe the operands; the pages have been checked.  Returns the columns of the output.
+static int64_t set_pages(PageLinearArgs& a, int T, int K, const pw_page* pages, const int32_t* out_features, int n_pages) {
+  int64_t slices = 0, columns = 0;
   for (int i = 0; i < n_pages; ++i) {
+    const pw_page& p = pages[i];
+    const int64_t n = out_features ? out_features[i] : (int64_t)p.rows;
+    LinearPage& l = a.page[i];
+    l.codes = static_cast<const char*>(p.codes);
+    l.bit1 = static_cast<const char*>(p.scales);
+    l.bit0 = static_cast<const char*>(p.zps);
+    l.fmt = stream_format(p.bits, p.layout == PW_LAYOUT_PLANES);
+    l.rows = (int)n;
+    l.col0 = (int)columns;
+    slices += (n + kUnitRows - 1) / kUnitRows;
+    columns += n;
+    l.end = (int)slices;
+  }
+  a.T = T;
+  a.groups = (int)(pages[0].cols / kGroup);
+  a.x_bytes = 2 * K;
+  a.slices = (int)slices;
+  a.pages = n_pages;
+  return columns;
+}
+// Whether a call goes through the tensor-core kernel of the layer calls (three launches, and weights rounded to fp16, which
+// an fp32 output would show), and what of its cut does not depend on the device.  By estimates of both times in us: this
+// kernel's from its cut, the other's linear in the weights (millions) and the tokens.  Measured, here / there: 4096 x 4096
+// at 4 bits, 64 tokens 16.9 / 14.3; 14336 x 4096 at 4 bits, 32 tokens 27.5 / 20.2, 64 tokens 47.5 / 21.7; 4096 x 14336 at
+// 8 bits, 64 tokens 60.4 / 23.3; 1260 x 1000 in planes of 4 bits, 300 tokens 13.7 / 13.5, 600 tokens 34.2 / 16.4; 40 x 128
+// at 4 bits, 1200 tokens 5.0 / 10.7.
+static bool many_tokens(DenseCall* d, const PageLinearArgs& call, const pw_page* pages, int out_type, int sms) {
+  if (call.T <= kUnitCols || out_type == PW_F32) return false;
+  double m = 0;
+  for (int i = 0; i < call.pages; ++i) m += 1e-6 * pages[i].cols * call.page[i].rows;
+  // (about as many clusters as run at the same time: the workspace's size must not depend on the current device)
+  int clusters[kSplits];
+  for (int i = 0; i < kSplits; ++i) clusters[i] = sms * 7 / (8 * (2 << i));
+  PageLinearArgs a = call;
+  const PageLinearPlan here = plan_page_linear(a, sms, clusters);
+  if (here.stages && 2.5 + here.cycles / 1680. <= 12. + m * (0.09 + 0.0017 * call.T) + 0.0005 * call.T) return false;
+  *d = DenseCall{};
+  d->T = call.T;
+  d->cols = (int)pages[0].cols;
+  d->n_pages = call.pages;
+  for (int i = 0; i < call.pages; ++i) {
     d->page[i] = pages[i];
-    d->features[i] = out_features ? out_features[i] : (int32_t)pages[i].rows;
+    d->features[i] = call.page[i].rows;
   }
   return true;
 }
@@ -360,9 +390,11 @@ static pw_status check_pages(int T, int K, const pw_page* pages, const int32_t* 
 }
 
 extern "C" size_t pw_page_linear_workspace(pw_ctx* ctx, int T, int K, const pw_page* pages, const int32_t* out_features, int n_pages, int out_type) {
+  if (!ctx || !type_ok(out_type) || check_pages(T, K, pages, out_features, n_pages) != PW_OK) return 0;
+  PageLinearArgs a{};
+  set_pages(a, T, K, pages, out_features, n_pages);
   DenseCall d;
-  if (!ctx || !type_ok(out_type) || check_pages(T, K, pages, out_features, n_pages) != PW_OK || !many_tokens(&d, T, pages, out_features, n_pages, out_type)) return 0;
-  return dense_plan(&d, ctx->num_sms);
+  return many_tokens(&d, a, pages, out_type, ctx->num_sms) ? dense_plan(&d, ctx->num_sms) : 0;
 }
 
 extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp16, int64_t x_stride, const pw_page* pages,
@@ -372,21 +404,7 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
   const pw_status cs = check_pages(T, K, pages, out_features, n_pages);
   if (cs != PW_OK) return cs;
   PageLinearArgs a{};
-  int64_t slices = 0, columns = 0;
-  for (int i = 0; i < n_pages; ++i) {
-    const pw_page& p = pages[i];
-    const int64_t n = out_features ? out_features[i] : (int64_t)p.rows;
-    LinearPage& l = a.page[i];
-    l.codes = static_cast<const char*>(p.codes);
-    l.bit1 = static_cast<const char*>(p.scales);
-    l.bit0 = static_cast<const char*>(p.zps);
-    l.fmt = stream_format(p.bits, p.layout == PW_LAYOUT_PLANES);
-    l.rows = (int)n;
-    l.col0 = (int)columns;
-    slices += (n + kUnitRows - 1) / kUnitRows;
-    columns += n;
-    l.end = (int)slices;
-  }
+  const int64_t columns = set_pages(a, T, K, pages, out_features, n_pages);
   if (T == 0) return PW_OK;
   if (!x_fp16 || !out) return PW_ERR_INVALID_ARG;
   if (T > 1 && (x_stride < K || out_stride < columns)) return PW_ERR_SHAPE;
@@ -394,7 +412,7 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
   DenseCall d;
-  if (workspace && many_tokens(&d, T, pages, out_features, n_pages, out_type)) {
+  if (workspace && many_tokens(&d, a, pages, out_type, ctx->num_sms)) {
     const size_t need = dense_plan(&d, ctx->num_sms);
     if (need && need <= workspace_bytes)
       return launch_dense(ctx, d, x_fp16, (size_t)x_stride * 2, 2 * K, bias, bias_type, out, out_type, out_stride, workspace, stream);
@@ -406,11 +424,6 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
   a.out = out;
   a.bias = bias;
   a.ld_out = out_stride;
-  a.T = T;
-  a.groups = (int)(pages[0].cols / kGroup);
-  a.x_bytes = 2 * K;
-  a.slices = (int)slices;
-  a.pages = n_pages;
   a.out_type = out_type;
   a.bias_type = bias_type;
   int max_clusters[kSplits];

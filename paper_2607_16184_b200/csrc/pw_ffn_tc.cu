@@ -1425,7 +1425,7 @@ size_t dense_plan(DenseCall* d, int sms) {
       d->splits = ks;
     }
   }
-  if (units * d->splits > 0x3fffffff || (int64_t)d->T * d->splits > 0x3fffffff) return 0;
+  if (units * d->splits > 0x3fffffff || (int64_t)d->T * d->splits * d->width > 0x7fffffff) return 0;   // 8 GB of partial sums
   d->units = (int)(units * d->splits);
   d->Rpad = d->token_tiles * d->nt_tile < 128 ? 128 : d->token_tiles * d->nt_tile;   // at least a box of the widest map
   return dense_ws(*d).total;
@@ -1490,27 +1490,43 @@ __global__ void __launch_bounds__(256) dense_prepare_kernel(const __grid_constan
 }
 
 // out[t, column] = sum of the parts of the contraction, in their order (+ bias), rounded once.
-__global__ void __launch_bounds__(256) dense_finish_kernel(const __grid_constant__ DenseCall d, const float* y, const void* bias, int bias_type, void* __restrict__ out,
+__global__ void __launch_bounds__(128) dense_finish_kernel(const __grid_constant__ DenseCall d, const float* y, const void* bias, int bias_type, void* __restrict__ out,
                                                            int out_type, int64_t ld_out) {
   grid_dep_sync();
   grid_dep_trigger();
-  const int t = blockIdx.y;
-  const size_t stride = (size_t)d.T * d.width;
-  for (int c = blockIdx.x * blockDim.x + threadIdx.x; c < d.width; c += gridDim.x * blockDim.x) {
-    int page = 0, col0 = 0, pad0 = 0;              // first column of the page, in the output and in y
-    while (page < d.n_pages) {
-      const int wide = (d.features[page] + kTileRows - 1) / kTileRows * kTileRows;
-      if (c < pad0 + wide) break;
-      pad0 += wide;
-      col0 += d.features[page++];
+  const size_t stride = (size_t)d.T * d.width / 4;
+  const int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8;   // eight columns, of one page: each starts at a tile of 128
+  if (c >= d.width) return;
+  int page = 0, col0 = 0, pad0 = 0;                // first column of the page, in the output and in y
+  while (true) {
+    const int wide = (d.features[page] + kTileRows - 1) / kTileRows * kTileRows;
+    if (c < pad0 + wide) break;
+    pad0 += wide;
+    col0 += d.features[page++];
+  }
+  const int n = min(8, d.features[page] - (c - pad0)), to = col0 + c - pad0;
+  if (n <= 0) return;
+  for (int t = blockIdx.y; t < d.T; t += gridDim.y) {
+    const float4* from = reinterpret_cast<const float4*>(y + (size_t)t * d.width + c);
+    float4 lo = from[0], hi = from[1];
+    for (int s = 1; s < d.splits; ++s) {
+      const float4 l = from[s * stride], h = from[s * stride + 1];
+      lo.x = __fadd_rn(lo.x, l.x), lo.y = __fadd_rn(lo.y, l.y), lo.z = __fadd_rn(lo.z, l.z), lo.w = __fadd_rn(lo.w, l.w);
+      hi.x = __fadd_rn(hi.x, h.x), hi.y = __fadd_rn(hi.y, h.y), hi.z = __fadd_rn(hi.z, h.z), hi.w = __fadd_rn(hi.w, h.w);
     }
-    if (c - pad0 >= d.features[page]) continue;
-    const int to = col0 + c - pad0;
-    const float* from = y + (size_t)t * d.width + c;
-    float v = from[0];
-    for (int s = 1; s < d.splits; ++s) v = __fadd_rn(v, from[s * stride]);
-    if (bias) v = __fadd_rn(v, load1(bias, to, bias_type));
-    store1(out, (int64_t)t * ld_out + to, out_type, v);
+    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (bias)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) v[i] = __fadd_rn(v[i], load1(bias, to + i, bias_type));
+    const int64_t at = (int64_t)t * ld_out + to;
+    if (n == 8 && at % 8 == 0) {
+      store8(out, at, out_type, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) store1(out, at + i, out_type, v[i]);
+    }
   }
 }
 
@@ -1551,8 +1567,7 @@ pw_status launch_dense(pw_ctx* ctx, const DenseCall& d, const void* x, size_t x_
       (__half*)nullptr, reinterpret_cast<float*>(b + w.y), d.width, (size_t)d.T * d.width, counters, status, reinterpret_cast<int32_t*>(b + w.done), d.splits,
       d.cols / kTileRows, 0u);
   PW_CUDA_OK(cudaGetLastError());
-  const int columns = (d.width + 255) / 256;
-  PW_CUDA_OK(launch_dependent(dense_finish_kernel, dim3(columns < 64 ? columns : 64, d.T), dim3(256), 0, s, d, reinterpret_cast<const float*>(b + w.y), bias,
+  PW_CUDA_OK(launch_dependent(dense_finish_kernel, dim3((d.width + 1023) / 1024, d.T < 4096 ? d.T : 4096), dim3(128), 0, s, d, reinterpret_cast<const float*>(b + w.y), bias,
                               bias_type, out, out_type, ld_out));
   ctx->launches += 3;
   return PW_OK;

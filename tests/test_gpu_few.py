@@ -149,9 +149,10 @@ def test_products_repeat(ctx):
 
 
 @pytest.mark.parametrize("T,K,sizes,formats,kernels", [
-    (1200, 128, [40], ["4"], 3), (700, 300, [130, 1, 300], ["16", "p3", "8"], 3), (64, 4096, [6000], ["2"], 3), (300, 1000, [1260], ["p4"], 1),
-    (600, 1000, [1260], ["p4"], 3), (130, 2050, [3129, 64], ["3", "4"], 3), (600, 640, [100], ["p2"], 3), (1000, 40, [133], ["16"], 3),
-    (70, 14336, [1128], ["8"], 3), (33, 8192, [2500, 2000], ["4", "4"], 3)])
+    (1200, 128, [40], ["4"], 1), (700, 300, [130, 1, 300], ["16", "p3", "8"], 1), (64, 4096, [6000], ["2"], 3), (300, 1000, [1260], ["p4"], 1),
+    (600, 1000, [1260], ["p4"], 3), (130, 2050, [3129, 64], ["3", "4"], 3), (600, 640, [100], ["p2"], 1), (1000, 40, [133], ["16"], 1),
+    (70, 14336, [1128], ["8"], 3), (33, 8192, [2500, 2000], ["4", "4"], 3), (4500, 300, [130, 1, 300], ["16", "p3", "8"], 3),
+    (12000, 640, [100], ["p2"], 3), (70000, 40, [133], ["16"], 3)])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_product_of_many_tokens(ctx, T, K, sizes, formats, kernels, dtype):
     """16-bit outputs of many tokens: weights are rounded to fp16, half a step each, where that many kernels run."""
