@@ -20,7 +20,6 @@ constexpr int kFewParts = 8;                      // most parts of the down bloc
 constexpr int kFewRouters = 4;                    // warps that route
 constexpr size_t kFewAhead = 16 << 20;            // bytes of shared experts that are asked for while the tokens are routed (2.5 us)
 constexpr uint32_t kFewAheadPiece = 4096;
-constexpr int kFewAheadSteps = 4;                 // steps of phase 2 that a warp asks the L2 cache for before all CTAs meet
 constexpr uint32_t kFewPolls = 1u << 22;          // about 3 s
 
 struct FewArgs {
@@ -75,11 +74,21 @@ constexpr int kTableBytes = (int)((sizeof(TAB) + 127) & ~(size_t)127);
 template <class TAB>
 __device__ __forceinline__ int passes_of(const TAB& t, int a) { return (t.off[a + 1] - t.off[a] + kUnitCols - 1) / kUnitCols; }
 
-// Teams of a CTA that has m units to do (at most four at a time): log2 of the warps of one.
-__device__ __forceinline__ int few_team_shift(int m) { return m == 1 ? 4 : m == 2 ? 3 : 2; }
+// A warp's team in a CTA that has m units to do, at most four at a time: the unit it takes, its first warp, log2 of its
+// warps.  Of three units the first, which is the heaviest, has half of the warps.
+struct Team {
+  int unit, first, shift;
+};
+__device__ __forceinline__ Team few_team(int m, int warp) {
+  Team w;
+  w.shift = m == 1 ? 4 : m == 2 || (m == 3 && warp < 8) ? 3 : 2;
+  w.first = warp >> w.shift << w.shift;
+  w.unit = (warp >> w.shift) - (m == 3 && warp >= 8);
+  return w;
+}
 // Every kind of team has barriers of its own: a warp may be in the next one's while others are in this one's.
-__device__ __forceinline__ void few_team_sync(int team, int ts) {
-  asm volatile("bar.sync %0, %1;" ::"r"((ts == 2 ? 1 : ts == 3 ? 5 : 7) + team), "r"(32 << ts) : "memory");
+__device__ __forceinline__ void few_team_sync(const Team& w) {
+  asm volatile("bar.sync %0, %1;" ::"r"((w.shift == 2 ? 1 : w.shift == 3 ? 5 : 7) + (w.first >> w.shift)), "r"(32 << w.shift) : "memory");
 }
 
 // A unit of phase 1 for one warp.
@@ -339,11 +348,11 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 #pragma unroll 1
       while (f.left == 0) {
         if (next >= mine) return;
-        const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts;
-        const int i = next + team;
+        const int m = min(4, mine - next);
+        const Team w = few_team(m, warp);
+        const int i = next + w.unit;
         next += m;
-        if (team >= m) continue;
-        const GateUp g = gate_up_unit(t, segs, unit_of(i), hg, ts, warp & ((1 << ts) - 1), lane);
+        const GateUp g = gate_up_unit(t, segs, unit_of(i), hg, w.shift, warp - w.first, lane);
         const SegPage& page = t.page[3 * g.a + g.kind];
         feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * g.a + g.kind], hg, g.slice, g.lo, g.lo + g.n);
       }
@@ -356,9 +365,9 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     }
 #pragma unroll 1
     for (int first = 0; first < mine; first += 4) {
-      const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
-      if (team >= m) continue;
-      const GateUp g = gate_up_unit(t, segs, unit_of(first + team), hg, ts, member, lane);
+      const Team w = few_team(min(4, mine - first), warp);
+      const int ts = w.shift, member = warp - w.first;
+      const GateUp g = gate_up_unit(t, segs, unit_of(first + w.unit), hg, ts, member, lane);
       const int pair0 = t.off[g.a] + g.pass * kUnitCols, cols = min(kUnitCols, t.off[g.a + 1] - pair0);
       const int x = t.token[pair0 + min(lane >> 2, cols - 1)];
       const int t0 = t.token[pair0 + min(2 * (lane & 3), cols - 1)], t1 = t.token[pair0 + min(2 * (lane & 3) + 1, cols - 1)];
@@ -366,8 +375,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       Operand o{smem_u32(pieces) + x * 256, smem_u32(xsum + t0), smem_u32(xsum + t1), p.T, (uint32_t)(x & 1) << 2, g.lo};
       walk<kAnyFormat, 0, STAGES>(fixed, t.fmt[4 * g.a + g.kind], g.n, f, r, o, tot, ask_next);
       put_sums(sums + warp * kSumFloats, lane, tot);
-      few_team_sync(team, ts);
-      const float* set = sums + (team << ts) * kSumFloats;
+      few_team_sync(w);
+      const float* set = sums + w.first * kSumFloats;
 #pragma unroll 1
       for (int i = member * 32 + lane; i < kUnitRows * cols; i += 32 << ts) {
         const int row = i & (kUnitRows - 1), col = i >> 5;
@@ -384,7 +393,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         const float h = __fmul_rn(__fdividef(gate, __fadd_rn(1.0f, __expf(-gate))), up);
         *reinterpret_cast<__half*>(p.h + (size_t)(pair0 + col) * p.F * 2 + piece_offset(g.slice * kUnitRows + row, col)) = __float2half_rn(h);
       }
-      few_team_sync(team, ts);                    // the sums are written again
+      few_team_sync(w);                    // the sums are written again
     }
   }
 
@@ -422,12 +431,12 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 #pragma unroll 1
       while (!down_run(t, fg, at, end, hint, d)) {
         if (next >= mine) return false;
-        const int m = min(4, mine - next), ts = few_team_shift(m), team = warp >> ts;
-        const int unit = (next + team) * G + b;
+        const int m = min(4, mine - next);
+        const Team w = few_team(m, warp);
+        const int unit = (next + w.unit) * G + b;
         next += m;
         at = end = 0;
-        if (team >= m) continue;
-        range(unit, ts, warp & ((1 << ts) - 1), at, end);
+        range(unit, w.shift, warp - w.first, at, end);
         hint = count_up_to(t.step0 + 1, segs, at, lane);
         slice = slice_of(unit);
       }
@@ -462,26 +471,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     }
     const int first_steps = asked;
     asked = STAGES;
-    // a warp that has to wait asks for its next steps' codes meanwhile, into the L2 cache: the memory works on
-    auto open = [&]() {
-      uint32_t now;
-      asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(p.sync) : "memory");
-      return (now ^ before) >> 31;
-    };
-    if (__shfl_sync(0xffffffffu, open(), 0) == 0) {
-      const Feed ahead = f;
-      const int a0 = next, a1 = at, a2 = end, a3 = hint, a4 = slice;
-#pragma unroll 1
-      for (int i = 0; i < kFewAheadSteps && (f.left || more());) {
-        const uint32_t is_open = open();          // (on its way while the copies are asked for: those take longer)
-        const int n = min(f.left, 2);
-        prefetch_steps(f, lane, n);
-        i += n;
-        if (__shfl_sync(0xffffffffu, is_open, 0)) break;
-      }
-      f = ahead;
-      next = a0, at = a1, end = a2, hint = a3, slice = a4;
-    }
     bool together = true;
     if (tid == 0) {
       uint32_t now;
@@ -513,9 +502,9 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     float* const own = sums2 + warp * set_floats;
 #pragma unroll 1
     for (int first = 0; first < mine; first += 4) {
-      const int m = min(4, mine - first), ts = few_team_shift(m), team = warp >> ts, member = warp & ((1 << ts) - 1);
-      if (team >= m) continue;
-      const int unit = (first + team) * G + b;
+      const Team w = few_team(min(4, mine - first), warp);
+      const int ts = w.shift, member = warp - w.first;
+      const int unit = (first + w.unit) * G + b;
       int place, stop;
       range(unit, ts, member, place, stop);
       int where = count_up_to(t.step0 + 1, segs, place, lane);
@@ -547,8 +536,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         }
         __syncwarp();
       }
-      few_team_sync(team, ts);
-      float* const set = sums2 + (team << ts) * set_floats;
+      few_team_sync(w);
+      float* const set = sums2 + w.first * set_floats;
       const int row0 = slice_of(unit) * kUnitRows, part = unit - slice_of(unit) * p.n_parts;
 #pragma unroll 1
       for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
@@ -562,9 +551,9 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       if (p.n_parts > 1) {
         // the last of the parts to finish adds all of them up, in their order
         __threadfence();
-        few_team_sync(team, ts);
+        few_team_sync(w);
         if (lane == 0 && member == 0) *reinterpret_cast<int32_t*>(set) = atomicAdd(p.sync + 64 + row0 / kUnitRows, 1) == p.n_parts - 1;
-        few_team_sync(team, ts);
+        few_team_sync(w);
         if (*reinterpret_cast<volatile int32_t*>(set)) {
           __threadfence();
 #pragma unroll 1
@@ -578,7 +567,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
           if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
         }
       }
-      few_team_sync(team, ts);                    // the sums are written again
+      few_team_sync(w);                    // the sums are written again
     }
   }
   cp_wait<0>();

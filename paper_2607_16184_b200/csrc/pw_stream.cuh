@@ -207,27 +207,9 @@ __device__ __forceinline__ void ask_any(Feed& f, uint32_t slot, uint32_t xslot, 
   }
 }
 
-// Asks the L2 cache for the codes of the next n steps, eight at most, and moves on: each lane for a piece of 512 bytes, of
-// unit lane % 4 of step lane / 4.
+// Asks the L2 cache for n bytes, a multiple of 16 at a multiple of 16.
 __device__ __forceinline__ void prefetch_bytes(const char* p, uint32_t n) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(n) : "memory");
-}
-__device__ __forceinline__ void prefetch_steps(Feed& f, int lane, int n) {
-  const int ls = step_shift(f.fmt), last = (1 << ls) - 1, units = f.fmt <= kFmt4 ? 4 : f.fmt == kFmt3 ? 3 : 2;
-  const size_t tile = kTileBytes[f.fmt];
-  const int i = lane >> 2, u = lane & 3, at = f.sub + i;
-  if (i < n) {
-    if (u < units) prefetch_bytes(f.codes - lane * 16 + (at >> ls) * tile + ((at & last) - f.sub) * 8192 + u * 2048, 512);
-    else if (f.fmt == kFmtP4 || (f.fmt == kFmtP3 && u == 2)) prefetch_bytes((u == 2 ? f.bit1 : f.bit0) - lane * 16 + (size_t)i * kPlaneBitTile, 512);
-    if (u < 2 && f.fmt != kFmt16) prefetch_bytes(f.meta - (lane >> 2) * 256 - (lane & 3) * 16 + (at >> ls) * tile + u * 256, 64);
-  }
-  const int to = f.sub + n;
-  f.left -= n;
-  f.codes += (to >> ls) * tile + ((to & last) - f.sub) * 8192;
-  f.meta += (to >> ls) * tile;
-  f.bit1 += n * kPlaneBitTile;
-  f.bit0 += n * kPlaneBitTile;
-  f.sub = to & last;
 }
 
 // ---- staged operand ------------------------------------------------------------------------------
