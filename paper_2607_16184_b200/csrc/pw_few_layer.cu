@@ -471,6 +471,12 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
     }
     const int first_steps = asked;
     asked = STAGES;
+    int place = 0, stop = 0, where = 0;           // of the warp's first unit
+    if (mine) {
+      const Team w = few_team(min(4, mine), warp);
+      range(w.unit * G + b, w.shift, warp - w.first, place, stop);
+      where = count_up_to(t.step0 + 1, segs, place, lane);
+    }
     bool together = true;
     if (tid == 0) {
       uint32_t now;
@@ -486,14 +492,15 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       cp_wait<0>();
       return;
     }
-#pragma unroll 1
+    uint2 note[STAGES];
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) note[i] = i < first_steps ? lds8(notes + i * 256) : make_uint2(0, 0);
+#pragma unroll
     for (int i = 0; i < STAGES; ++i) {
-      if (i < first_steps) {
-        const uint2 w = lds8(notes + i * 256);
-        const uint32_t to = r.x + i * (256 * XC) + lane * 16, step = (uint32_t)p.F * 2 << ((w.y & 3) + 1);
+      const uint32_t to = r.x + i * (256 * XC) + lane * 16, step = (uint32_t)p.F * 2 << ((note[i].y & 3) + 1);
+      const char* x = p.h + note[i].x;
 #pragma unroll 1
-        for (uint32_t j = 0; j < w.y >> 2; ++j) cp16(to + j * 512, p.h + w.x + (size_t)j * step);
-      }
+      for (uint32_t j = 0; j < note[i].y >> 2; ++j) cp16(to + j * 512, x + (size_t)j * step);
       cp_commit();
     }
     // (for no more tokens than a unit's where those of phase 1 were, and the notes: a warp's place is its own)
@@ -505,9 +512,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       const Team w = few_team(min(4, mine - first), warp);
       const int ts = w.shift, member = warp - w.first;
       const int unit = (first + w.unit) * G + b;
-      int place, stop;
-      range(unit, ts, member, place, stop);
-      int where = count_up_to(t.step0 + 1, segs, place, lane);
+      if (first) {
+        range(unit, ts, member, place, stop);
+        where = count_up_to(t.step0 + 1, segs, place, lane);
+      }
 #pragma unroll 1
       for (int i = lane; i < p.T * kSumPitch; i += 32) own[i] = 0.f;
       __syncwarp();
@@ -550,18 +558,23 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       }
       if (p.n_parts > 1) {
         // the last of the parts to finish adds all of them up, in their order
-        __threadfence();
         few_team_sync(w);
-        if (lane == 0 && member == 0) *reinterpret_cast<int32_t*>(set) = atomicAdd(p.sync + 64 + row0 / kUnitRows, 1) == p.n_parts - 1;
+        if (lane == 0 && member == 0) {
+          uint32_t n;
+          asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(n) : "l"(p.sync + 64 + row0 / kUnitRows) : "memory");
+          *reinterpret_cast<uint32_t*>(set) = n == (uint32_t)p.n_parts - 1;
+        }
         few_team_sync(w);
-        if (*reinterpret_cast<volatile int32_t*>(set)) {
-          __threadfence();
+        if (*reinterpret_cast<volatile uint32_t*>(set)) {
 #pragma unroll 1
           for (int i = member * 32 + lane; i < kUnitRows * p.T; i += 32 << ts) {
             const int row = i & (kUnitRows - 1), tok = i >> 5;
-            float v = 0.f;
-#pragma unroll 1
-            for (int q = 0; q < p.n_parts; ++q) v = __fadd_rn(v, __ldcg(p.parts + ((size_t)q * p.T + tok) * p.H + row0 + row));
+            const float* from = p.parts + (size_t)tok * p.H + row0 + row;
+            float v = 0.f, part[kFewParts];
+#pragma unroll
+            for (int q = 0; q < kFewParts; ++q) part[q] = q < p.n_parts ? __ldcg(from + (size_t)q * p.T * p.H) : 0.f;
+#pragma unroll
+            for (int q = 0; q < kFewParts; ++q) v = __fadd_rn(v, part[q]);
             store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
           }
           if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
