@@ -325,8 +325,8 @@ pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16,
  * (TILED and PLANES), page table, routing rule, routed ids and gates, observation taps; out: device [T, H] of out_type
  * (pw_type).  They differ from pw_moe_forward in the weights, which are code * scale + zero-point without the rounding to
  * fp16, and in that a token that names an expert twice is multiplied once, with the sum of the gates.
- * The activations of the call are kept in an SM's shared memory: T * hidden up to 65536, in a layer of very many
- * experts somewhat less (SHAPE beyond; T = 1 always has room up to hidden = 32768).
+ * The activations of the call are kept in an SM's shared memory: T * hidden up to 65536 where T * (top_k + n_shared) is
+ * at most 48, up to 49152 otherwise (SHAPE where there is no room).
  * All CTAs of the kernel run at the same time (a cooperative launch): on a device that other kernels keep busy it starts
  * when they leave room for one CTA per SM.  Works in the context's workspace, like pw_moe_forward, and is ordered with
  * its calls; pw_get_routing and pw_kernel_timing do not see this call.
@@ -442,14 +442,18 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
  * columns of page i follow those of page i - 1.  A dense block of the model (queries, keys and values of one input, an
  * output projection, the router, the vocabulary) kept and demoted like an expert's.
  * x: device fp16 [T, K], rows x_stride elements apart.  pages: host, TILED or PLANES, any bitwidth each, with the same
- * cols; they are read as they are when the call runs.  A page is made of whole tiles and the block may be smaller:
+ * cols; they are read as they are when the call runs.  (The call may start to read pages while the kernel directly ahead
+ * of it in the stream still runs, unless that is one of this context's that writes pages: a kernel of the caller's own
+ * that writes one, and lets its successor start early, needs another operation between the two.)  A page is made of whole tiles and the block may be smaller:
  * out_features[i] <= rows of page i (host, or NULL: all its rows) and cols - 128 < K <= cols; what the page holds past
  * them must be finite and does not count.  bias: device [sum of out_features] of bias_type, or NULL.  out: device
  * [T, sum of out_features] of out_type; sums in fp32 in a fixed order, rounded once.
- * Any T: the weights are read once per eight tokens (from the L2 cache after the first time).  T = 0 enqueues nothing.
- * workspace: device, or NULL.  With the bytes that pw_page_linear_workspace reports (0: the call has no use for any), many
- * tokens with a 16-bit output go through the tensor-core kernel of the layer calls instead, with the weights rounded to
- * fp16 like theirs; with less, or none, the call does without.  pw_page_linear_workspace is 0 for invalid arguments too.
+ * Any T: one kernel, which reads the weights once per eight tokens (from the L2 cache after the first time).  T = 0
+ * enqueues nothing.
+ * workspace: device, or NULL.  With the bytes that pw_page_linear_workspace reports (0: the call has no use for any), calls
+ * with a 16-bit output of more tokens than that pays for (more than eight; by an estimate of the times) go through the
+ * tensor-core kernel of the layer calls instead, in three launches, with the weights rounded to fp16 like theirs; with
+ * less, or none, the call does without.  pw_page_linear_workspace is 0 for invalid arguments too.
  * Needs a context of the current device, but neither its page table nor its workspace: calls on different streams may run
  * at the same time, each with a workspace of its own.
  * Errors: INVALID_ARG (a null pointer, a type, n_pages, out_features below 1), SHAPE (page shapes, K or out_features

@@ -692,9 +692,9 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   if (!v) return PW_ERR_SHAPE;
   const pw_status ds = check_device(ctx);
   if (ds != PW_OK) return ds;
-  if (!ctx->few_layer_ready) {
+  if (!ctx->few_layer_ready.load(std::memory_order_acquire)) {
     for (const FewVariant& one : kFewVariants) PW_CUDA_OK(cudaFuncSetAttribute(one.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
-    ctx->few_layer_ready = true;
+    ctx->few_layer_ready.store(1, std::memory_order_release);
   }
   char* b = ctx->base;
   a.rows = reinterpret_cast<const DevRow*>(b + w.table) + (size_t)layer * w.S * 3;

@@ -254,6 +254,37 @@ def test_calls_of_two_threads(ctx):
     assert not wrong
 
 
+def test_a_page_that_is_written_directly_ahead(ctx):
+    """The product may begin while the kernel ahead of it still runs, but not with a page that kernel writes."""
+    g = gen(77)
+    blocks = [block_weights(g, 512, 4096) for _ in range(6)]
+    x = operand(g, 3, 4096)
+    page, demoted = B.Page(512, 4096, 8, ctx.device), B.Page(512, 4096, 4, ctx.device)
+    want = []
+    for w in blocks:
+        ctx.pw_quantize_block(w, 8, dst=page)
+        ctx.pw_demote_block(page, 4, dst=demoted)
+        torch.cuda.synchronize()
+        want.append([ctx.pw_page_linear(x, [p]) for p in (page, demoted)])
+        torch.cuda.synchronize()
+
+    def step(w):
+        ctx.pw_quantize_block(w, 8, dst=page)
+        first = ctx.pw_page_linear(x, [page])
+        ctx.pw_demote_block(page, 4, dst=demoted)
+        return [first, ctx.pw_page_linear(x, [demoted])]
+
+    for w, two in zip(blocks, want):
+        assert all(torch.equal(a, b) for a, b in zip(step(w), two))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [step(w) for w in blocks]
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
 def test_product_refuses(ctx):
     g = gen(9)
     page = plain.make_page(ctx, block_weights(g, 128, 256), "4")
@@ -345,6 +376,25 @@ def test_layer_shapes(E, ns, H, F, k, T):
     x, l = layer.tokens(T), layer.logits(T)
     layer.check(layer.ctx.pw_moe_forward_few(0, x, l, k), x, plain.routing(f64(l), k))
     layer.ctx.close()
+
+
+@pytest.mark.parametrize("T", [1, 2, 4, 7, 8, 9, 13, 16])
+def test_layer_whose_down_blocks_are_cut_in_parts(T):
+    layer = Layer(20, 4, 256, 768, MIX, seed=6, k=4)
+    x = layer.tokens(T)
+    for _ in range(3):
+        l = layer.logits(T)
+        layer.check(layer.ctx.pw_moe_forward_few(0, x, l, 4), x, plain.routing(f64(l), 4))
+    layer.ctx.close()
+
+
+def test_the_room_that_is_promised():
+    """T * hidden up to 65536 for 48 pairs, up to 49152 for more."""
+    for E, ns, H, k, T in ((8, 0, 4096, 3, 16), (4, 0, 8192, 2, 8), (20, 0, 4096, 8, 12), (18, 0, 16384, 17, 3), (2, 0, 32768, 2, 2)):
+        layer = Layer(E, ns, H, 128, ["2"], seed=E, k=k)
+        x, l = layer.tokens(T), layer.logits(T)
+        layer.check(layer.ctx.pw_moe_forward_few(0, x, l, k), x, plain.routing(f64(l), k))
+        layer.ctx.close()
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
