@@ -1,15 +1,20 @@
 // The whole layer for few tokens in one kernel (pw_moe_forward_few, pw_moe_forward_few_routed).
 //
 // The layer call for batches takes five or six launches, and its kernels work on tiles of 128 weight rows; one token of a
-// layer with 60 + 4 experts takes them 45 us, where the pages' bytes need 16.  Here one CTA per SM
-//   - routes the tokens (every CTA does, it is cheaper than to wait for one that does) and lists the experts that have any,
+// layer with 60 + 4 experts takes them 40 us, where the pages' bytes need 16.  Here (28 us) one CTA per SM
+//   - routes the tokens (every CTA does, it is cheaper than to wait for one that does) and lists the experts that have any;
+//     meanwhile it brings the tokens into shared memory and asks the L2 cache for the shared experts,
 //   - phase 1: units of 32 rows of an expert's gate and up blocks -> 32 values h = silu(gate) * up of its tokens,
-//   - waits for all CTAs (the kernel is launched cooperatively, so they run at the same time), having asked for the first
-//     weights of
+//   - waits for all CTAs (the kernel is launched cooperatively, so they run at the same time); each of its warps has gone on
+//     by then to ask for its first weights of
 //   - phase 2: units of 32 rows of the output and a part of all down blocks' columns; where the columns are in parts, the
 //     CTA that finishes last of a unit's parts adds them up.
-// Bound by the pages' bytes; the inner loop and what bounds it below that are in pw_stream.cuh.  Sums are in fp32 in an order
-// that depends on the routing alone.
+// Bound by the pages' bytes: phase 1 runs at the HBM rate (one token of the 8 x (4096, 14336) layer at mixed bitwidths, 350 MB:
+// 233 MB in 31 us of 72), phase 2 of narrow formats by its instructions (a 4-bit step of 2 KB: about 300 of a warp), where
+// the hidden size gives 128 of the 148 SMs a unit.  Besides that a call takes about 3 us to launch, 3 to route and make its
+// tables (6 for 16 tokens of 128 experts) and 4 between the phases.  Asking the L2 cache for more of phase 2 while waiting was
+// slower (one token of the 60 + 4 expert layer 30.3 us against 28.9).  Sums are in fp32 in an order that depends on the routing
+// alone.
 #include "pw_scaled.cuh"
 #include "pw_stream.cuh"
 #include "pw_topk.cuh"
@@ -18,7 +23,9 @@ namespace pw {
 
 constexpr int kFewParts = 8;                      // most parts of the down blocks' columns
 constexpr int kFewRouters = 4;                    // warps that route
-constexpr size_t kFewAhead = 16 << 20;            // bytes of shared experts that are asked for while the tokens are routed (2.5 us)
+// bytes of shared experts that are asked for while the tokens are routed: 2.5 us (none / 16 MB / 48 MB, 60 + 4 experts: one token
+// 28.8 / 28.9 / 31.1 us, four 40.2 / 39.5 / 41.2)
+constexpr size_t kFewAhead = 16 << 20;
 constexpr uint32_t kFewAheadPiece = 4096;
 constexpr uint32_t kFewPolls = 1u << 22;          // about 3 s
 
@@ -709,15 +716,15 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.status = reinterpret_cast<int32_t*>(b + w.status);
   a.seen = ctx->obs_acc ? reinterpret_cast<int32_t*>(b + w.few_seen) : nullptr;
   // Parts of the down blocks' columns: as few as give every SM work, in rounds that are nearly full.  By an estimate in us:
-  // an SM streams 45 KB/us (routed blocks taken for 4 bits), and to add parts up takes 2 us at the end (measured, 1 part /
-  // 2 / 4: one token of 256 x 512 10.8 / 11.6 / 12.2, of 60 + 4 experts of 2048 x 1408 34.1 / 31.1 / 32.5, of 4096 x 14336
-  // 74.0 / 77.7 / 78.1).
+  // an SM streams 45 KB/us (routed blocks taken for 4 bits), and to add parts up takes about 1 us at the end (measured, 1 part
+  // / 2 / 4: one token of 256 x 512 10.3 / 10.9 / 10.9, of 60 + 4 experts of 2048 x 1408 31.0 / 28.3 / 28.9, of 4096 x 14336
+  // 71.5 / 75.4 / 75.5).
   const int slices = c.hidden / kUnitRows, routed = c.n_experts < T * top_k ? c.n_experts : T * top_k;
   const double slice_us = 32e-3 * c.ffn * (0.5 * routed + 2. * c.n_shared) / 45.;
   double best = -1.;
   for (int parts = 1; parts <= kFewParts; ++parts) {
     const int rounds = (slices * parts + ctx->num_sms - 1) / ctx->num_sms;
-    const double us = slice_us * rounds / parts * (1. + 0.05 * parts) + (parts > 1 ? 2. : 0.);
+    const double us = slice_us * rounds / parts * (1. + 0.05 * parts) + (parts > 1 ? 1. : 0.);
     if (best < 0 || us < best) best = us, a.n_parts = parts;
   }
   // (see `range`: a place in the list of steps, times the parts of it, divided by multiplication)

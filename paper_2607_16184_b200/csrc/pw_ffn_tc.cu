@@ -1385,7 +1385,8 @@ pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, i
 // The down kernel on pages that are no layer's: a "segment" is a page, whose row tiles are numbered on from those of the
 // page before it.  The kernel ahead of it writes what the layer's call has from its routing: the operand in k-chunk-major
 // form, the page rows, the unit list (K range outermost, then row tile, then token tile), and completion counters that no
-// unit has to wait for.
+// unit has to wait for.  The kernel behind it adds the K ranges up, adds the bias and rounds.  14336 x 4096 at 4 bits: 64
+// tokens 21.7 us (most of it the down kernel), 256 tokens 43.
 struct DenseWs {
   size_t rows, units, done, counters, xt, y, total;
 };

@@ -18,15 +18,18 @@
 // subnormal are bits that the sum does not have (a field at bits 0 .. 3: results off by 1.5e-6 of their norm, at bits 4 .. 7
 // by 1e-7).  So narrow fields are moved up, by a multiplication, which is not the pipe that the logic instructions keep busy.
 // The power of two goes into the scale, which is applied with the zero-point once per group, in fp32.  A pair of weights
-// costs one or two instructions, where turning it into fp16(code * scale + zero) costs three; weights are not rounded to
-// fp16 on this path.
+// costs two instructions, where turning it into fp16(code * scale + zero) costs three; weights are not rounded to fp16 on
+// this path.  A 4-bit step of a warp is about 265 instructions (112 to cut the codes out, 16 matrix instructions, 32 for
+// scales and zero-points, 17 copies and loads), half of them for the pipe that starts one every other cycle: an SM then
+// does a 2 KB step of each of its 16 warps in 1530 cycles, 22 bytes a cycle, where its share of the HBM rate is 24; steps
+// of 8 and 16 bits keep up with that rate.
 //
 // Steps: 32 columns of a 16-bit block, 64 of an 8-bit one, a group of 128 otherwise, so that a step is 1 to 2 KB of
 // codes.  Lane (g, t) = (lane / 4, lane % 4) multiplies part t of the step's columns, rows 4g .. 4g + 3 (as rows g and
 // g + 8 of the two products), so that the scales of its rows are one 8-byte load.  The copies are cut the other way, a
 // row's 16 bytes per lane: an instruction then takes 512 bytes in one piece, where one that follows the lanes of the
 // product takes four pieces 2 KB apart (streaming alone, 71 MB out of the L2 cache: 7.6 us against 18.9).  Rows are
-// exchanged inside a unit so that the loads of the product meet 32 banks (code_at).
+// exchanged inside a unit so that the loads of the product meet 32 banks (write_at).
 //
 // Operand rows are kept in pieces of 16 bytes.  A group's 128 columns are eight stretches of 16, as pairs W0 .. W7; piece
 // 2s + h of stretch s holds W(2h), W(2h + 4), W(2h + 1), W(2h + 5): pairs next to one another are the two halves of an
