@@ -323,7 +323,7 @@ pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16,
 
 /* The two layer calls for a handful of tokens, T <= PW_FEW_TOKENS, in one kernel: the latency of a decode step.  Same pages
  * (TILED and PLANES), page table, routing rule, routed ids and gates, observation taps; out: device [T, H] of out_type
- * (pw_type).  They differ from pw_moe_forward in the weights, which are code * scale + zero-point without the rounding to
+ * (pw_type), apart from the inputs.  They differ from pw_moe_forward in the weights, which are code * scale + zero-point without the rounding to
  * fp16, and in that a token that names an expert twice is multiplied once, with the sum of the gates.
  * The activations of the call are kept in an SM's shared memory: T * hidden up to 65536 where T * (top_k + n_shared) is
  * at most 48, up to 49152 otherwise (SHAPE where there is no room).
@@ -447,7 +447,8 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
  * that writes one, and lets its successor start early, needs another operation between the two.)  A page is made of whole tiles and the block may be smaller:
  * out_features[i] <= rows of page i (host, or NULL: all its rows) and cols - 128 < K <= cols; what the page holds past
  * them must be finite and does not count.  bias: device [sum of out_features] of bias_type, or NULL.  out: device
- * [T, sum of out_features] of out_type; sums in fp32 in a fixed order, rounded once.
+ * [T, sum of out_features] of out_type, apart from the inputs; sums in fp32 in a fixed order, rounded once.  A token with an
+ * infinity or NaN gets results that are not finite; other tokens do not see it.
  * Any T: one kernel, which reads the weights once per eight tokens (from the L2 cache after the first time).  T = 0
  * enqueues nothing.
  * workspace: device, or NULL.  With the bytes that pw_page_linear_workspace reports (0: the call has no use for any), calls

@@ -254,6 +254,19 @@ def test_calls_of_two_threads(ctx):
     assert not wrong
 
 
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("T,dtype", [(5, F32), (40, F16)])
+def test_a_token_that_is_not_finite_stays_alone(ctx, T, dtype, bad):
+    g = gen(5)
+    pages = [plain.make_page(ctx, block_weights(g, n, 640), f) for n, f in ((100, "4"), (64, "8"), (33, "16"), (40, "p3"))]
+    x = operand(g, T, 600)
+    want = ctx.pw_page_linear(x, pages, out_dtype=dtype)
+    x[3, 77] = bad
+    got = ctx.pw_page_linear(x, pages, out_dtype=dtype)
+    assert not torch.any(torch.isfinite(got[3]))
+    assert torch.equal(got[[t for t in range(T) if t != 3]], want[[t for t in range(T) if t != 3]])
+
+
 def test_a_page_that_is_written_directly_ahead(ctx):
     """The product may begin while the kernel ahead of it still runs, but not with a page that kernel writes."""
     g = gen(77)
@@ -406,6 +419,18 @@ def test_layer_for_a_given_routing(mixed, dtype):
     out = mixed.ctx.pw_moe_forward_few_routed(0, x, ids, gates, out_dtype=dtype)
     pairs = [(t, e, float(gates[t, j])) for t, row in enumerate(ids.tolist()) for j, e in enumerate(row) if e >= 0]
     mixed.check(out, x, pairs)
+
+
+@pytest.mark.parametrize("T", [4, 11])
+def test_a_token_of_a_layer_that_is_not_finite_stays_alone(mixed, T):
+    x, l = mixed.tokens(T), mixed.logits(T)
+    x[2, 5], l[0, :] = float("nan"), float("nan")
+    got = mixed.ctx.pw_moe_forward_few(0, x, l, 3)
+    assert torch.all(torch.isnan(got[[0, 2]])) and mixed.ctx.pw_last_device_status() == 0
+    # (which experts take part is part of the sums' order: the others' bits may change, their values may not)
+    rest = [t for t in range(T) if t not in (0, 2)]
+    want, bound = mixed.want(x[rest], plain.routing(f64(l[rest]), 3))
+    check(got[rest], want, bound, got.dtype)
 
 
 def test_rows_without_anything_are_zero():
