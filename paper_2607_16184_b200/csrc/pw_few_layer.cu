@@ -64,7 +64,7 @@ struct FewTables {
   uint32_t mask[256];                             // tokens of an expert, and above them (16 bits) its first pair
   int32_t unit0[SEGS + 1];                        // first unit of phase 1, by rank
   int32_t step0[SEGS + 1];                        // first step of phase 2, of the segment's first pass
-  uint32_t key[SEGS];                             // by which they are ordered, heaviest first: see make_tables
+  uint2 weight[SEGS];                             // by which they are ordered, heaviest first, and their passes: see make_tables
   int32_t count[2];                               // active segments, pairs
   uint32_t done;                                  // warps that are through with phase 1
   uint16_t seg[SEGS];                             // expert, ascending
@@ -161,8 +161,8 @@ __device__ __forceinline__ bool down_run(const TAB& t, int groups, int& at, int 
 __device__ __forceinline__ void routers_sync() { asm volatile("bar.sync 8, %0;" ::"n"(32 * kFewRouters) : "memory"); }
 template <class TAB>
 __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevRow* rows, int fg, int warp, int lane) {
-  // Segment a: expert e with n tokens, pairs first .. first + n.  Its key: shared or not, the bytes of a tile of its gate
-  // and its up block, then (for the sums below) its passes and passes * steps of a group of its down block, 8 at most.
+  // Segment a: expert e with n tokens, pairs first .. first + n.  Its weight: shared or not, the bytes of a tile of its gate
+  // and its up block, no two alike; beside it one in the upper half, for counting, and its passes.
   auto put = [&](int a, int e, int n, int first) {
     uint32_t tiles = 0, shift = 0;
     t.seg[a] = (uint16_t)e;
@@ -177,7 +177,8 @@ __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevR
       t.fmt[4 * a + u] = (uint8_t)stream_format((int)row.bits, planes);
     }
     const uint32_t passes = (uint32_t)(n + kUnitCols - 1) / kUnitCols;
-    t.key[a] = (e < p.E ? 0u : 1u << 31) | tiles << 8 | passes << 4 | passes << shift;
+    t.weight[a] = make_uint2((e < p.E ? 0u : 1u << 31) | tiles << 9 | (511u - a), 1u << 16 | passes);
+    t.step0[a] = (int32_t)(passes << shift);      // (summed up below)
   };
   // experts with tokens, ascending, then the shared ones: every warp counts all, and makes the segments of some
   int segs = 0, pairs = 0;
@@ -186,21 +187,19 @@ __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevR
     const uint32_t m = base + lane < p.E ? t.mask[base + lane] & 0xffffu : 0;   // (another warp may have set the upper half)
     const uint32_t any = __ballot_sync(0xffffffffu, m != 0);
     if (!any) continue;
-    const uint32_t below = (1u << lane) - 1;
     const int n = __popc(m);                      // <= 16
-    int before = 0, all = 0;
+    if ((base >> 5) % kFewRouters == warp) {
+      const uint32_t below = (1u << lane) - 1;
+      int before = pairs;
 #pragma unroll
-    for (int bit = 0; bit < 5; ++bit) {
-      const uint32_t have = __ballot_sync(0xffffffffu, n >> bit & 1);
-      before += __popc(have & below) << bit;
-      all += __popc(have) << bit;
-    }
-    if (n && (base >> 5) % kFewRouters == warp) {
-      put(segs + __popc(any & below), base + lane, n, pairs + before);
-      t.mask[base + lane] = m | (uint32_t)(pairs + before) << 16;
+      for (int bit = 0; bit < 5; ++bit) before += __popc(__ballot_sync(0xffffffffu, n >> bit & 1) & below) << bit;
+      if (n) {
+        put(segs + __popc(any & below), base + lane, n, before);
+        t.mask[base + lane] = m | (uint32_t)before << 16;
+      }
     }
     segs += __popc(any);
-    pairs += all;
+    pairs += (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
   }
   if (warp == kFewRouters - 1) {
     if (lane < p.n_shared) put(segs + lane, p.E + lane, p.T, pairs + lane * p.T);
@@ -236,21 +235,36 @@ __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevR
     t.token[pairs + i] = (uint8_t)(i % p.T);
     t.gate[pairs + i] = 1.f;
   }
-  // places in the order, first units of phase 1 by place, first steps of phase 2
   segs += p.n_shared;
+  // first steps of phase 2
+  if (warp == 1) {
+    int carry = 0;
 #pragma unroll 1
-  for (int a = first; a <= segs; a += 32 * kFewRouters) {   // (a = segs: the ends)
-    const uint32_t mine = a < segs ? t.key[a] : 0;
-    int place = 0, units = 0, steps = 0;
+    for (int base = 0; base < segs; base += 32) {
+      const int i = base + lane, n = i < segs ? t.step0[i] : 0;
+      int incl = n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += y;
+      }
+      if (i < segs) t.step0[i] = (carry + incl - n) * fg;
+      carry += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) t.step0[segs] = carry * fg;
+  }
+  // places in the order, first units of phase 1 by place
+#pragma unroll 1
+  for (int a = first; a <= segs; a += 32 * kFewRouters) {   // (a = segs: the end)
+    const uint32_t mine = a < segs ? t.weight[a].x : 0;
+    uint32_t heavier = 0;
 #pragma unroll 4
     for (int o = 0; o < segs; ++o) {
-      const uint32_t key = t.key[o];
-      if (key > mine || (key == mine && o < a)) ++place, units += key >> 4 & 15;
-      if (o < a) steps += key & 15;
+      const uint2 w = t.weight[o];
+      heavier += w.x > mine ? w.y : 0;
     }
-    if (a < segs) t.order[place] = (uint16_t)a;
-    t.unit0[place] = units * (p.F / kUnitRows);
-    t.step0[a] = steps * fg;
+    if (a < segs) t.order[heavier >> 16] = (uint16_t)a;
+    t.unit0[heavier >> 16] = (int)(heavier & 0xffffu) * (p.F / kUnitRows);
   }
 }
 

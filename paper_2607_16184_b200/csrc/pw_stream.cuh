@@ -232,14 +232,15 @@ template <int AHEAD>
 __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int rows, int room, int g0, int groups, int k_bytes, char* pieces, float* sums,
                                               int thread, int threads) {
   const int n = rows * groups * 8;
+  const uint32_t per_row = ((1u << 20) + rows - 1) / rows;   // (i / rows for i below 2^16: there is no room for more)
 #pragma unroll 1
   for (int base = thread & ~31; base < n; base += AHEAD * threads) {
     uint4 v[AHEAD][2];
-    int place[AHEAD];                            // g * room + c
+    int place[AHEAD];                            // group, row
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
-      const int i = base + a * threads + (thread & 31), s = i & 7, rg = i >> 3, g = rg / rows, c = rg - g * rows;
-      place[a] = g * room + c;
+      const int i = base + a * threads + (thread & 31), s = i & 7, rg = i >> 3, g = (int)(rg * per_row >> 20), c = rg - g * rows;
+      place[a] = g << 8 | c;
       v[a][0] = v[a][1] = make_uint4(0, 0, 0, 0);
       if (i < n) {
         const int k = (g0 + g) * 256 + s * 32;
@@ -263,11 +264,11 @@ __device__ __forceinline__ void stage_operand(const char* x, size_t pitch, int r
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       if (base + a * threads >= n) break;         // (the same for a whole warp)
-      const int i = base + a * threads + (thread & 31), s = i & 7, g = place[a] / room, c = place[a] - g * room;
+      const int i = base + a * threads + (thread & 31), s = i & 7, g = place[a] >> 8, c = place[a] & 255;
       if (i < n) {
         uint4 piece[2];
         make_pieces(v[a][0], v[a][1], piece);
-        char* row = pieces + (size_t)place[a] * 256;
+        char* row = pieces + (size_t)(g * room + c) * 256;
         *reinterpret_cast<uint4*>(row + piece_at(2 * s, c) * 16) = piece[0];
         *reinterpret_cast<uint4*>(row + piece_at(2 * s + 1, c) * 16) = piece[1];
       }
