@@ -61,7 +61,7 @@ WsMap make_wsmap(const pw_config& c) {
   const size_t few = c.max_tokens < PW_FEW_TOKENS ? c.max_tokens : PW_FEW_TOKENS, few_pairs = few * (c.max_top_k + c.n_shared);
   m.few_sync = take(4 * (64 + (size_t)c.hidden / 32));
   m.few_seen = take(4 * (4 + 2 * (size_t)m.S + 2 * few_pairs));
-  m.few_h = take(few_pairs * c.ffn * 2);
+  m.few_h = take(2 * few_pairs * c.ffn * 2);
   m.total = o;
   return m;
 }

@@ -54,8 +54,10 @@ def rounded(values, bound, dtype):
     return bound + np.maximum((np.abs(values) + bound) * HALF_STEP[dtype], TINY_STEP[dtype] / 2)
 
 
-def layer(x, blocks, pairs):
-    """(out, bound) of the layer: x [T, H] in 64 bits, blocks[e] = three of stored(), pairs = (token, expert, gate)."""
+def layer(x, blocks, pairs, parts=1):
+    """(out, bound) of the layer: x [T, H] in 64 bits, blocks[e] = three of stored(), pairs = (token, expert, gate).
+    parts: fp16 numbers that h is rounded to; the second takes what the first leaves (at most 2^-11 of h) and is off by half
+    a step of that."""
     out, bound = np.zeros_like(x), np.zeros_like(x)
     cache = {}
     for t, e, gate in pairs:
@@ -68,7 +70,7 @@ def layer(x, blocks, pairs):
             # the slope of silu is at most 1.1; its fast exponential and division: a few units of 2^-21, and all that may
             # be lost where exp(-g) overflows is less than 2^-24
             dh = (1.1 * dg + np.abs(silu) * 2.0 ** -19 + 2.0 ** -24) * (np.abs(u) + du) + np.abs(silu) * du
-            dh = dh + np.maximum((np.abs(h) + dh) * HALF_STEP[torch.float16], TINY_STEP[torch.float16] / 2)
+            dh = dh + np.maximum((np.abs(h) + dh) * HALF_STEP[torch.float16] ** parts, TINY_STEP[torch.float16] / 2)
             y, dy = product(h, blocks[e][2])
             c, s, z = blocks[e][2]
             cache[t, e] = y[0], dy[0] + (dh @ np.abs(c * s + z).T)[0] * 1.001
