@@ -731,8 +731,10 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.pairs = T * (top_k + c.n_shared);
   // h in two numbers costs next to nothing while the matrix instructions have columns to spare, four tokens of an expert at a
   // time: an output of more than bf16's precision is then as near to the definition as an fp32 operand would make it
-  // (fp16: 2.1e-4 of its norm, with one number 2.9e-4; fp32: 1e-6, 2e-4).
-  a.halves = out_type == PW_BF16 ? 1 : 2;
+  // (fp16: 2.1e-4 of its norm, with one number 2.9e-4; fp32: 1e-6, 2e-4).  With more tokens experts need more passes, and an
+  // fp16 output shows little of it: 16 tokens of the 60 + 4 expert layer 88 us with two, 79 with one, of the 8-expert layer
+  // 177 and 147; 8 tokens 55 and 51, 132 and 131.
+  a.halves = out_type == PW_F32 || (out_type == PW_F16 && T <= kUnitCols) ? 2 : 1;
   const int operand_rows = a.halves == 1 ? (T < kUnitCols ? T : kUnitCols) : 2 * T < kUnitCols ? 2 * T : kUnitCols;
   const FewVariant* v = nullptr;
   for (const FewVariant& one : kFewVariants)

@@ -394,11 +394,11 @@ def test_layer_shapes(E, ns, H, F, k, T):
 @pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 9, 16])
 @pytest.mark.parametrize("dtype", [F32, F16])
 def test_layer_keeps_what_its_output_can_show(mixed, T, dtype):
-    """The operand of the down blocks is two fp16 numbers where the output has more than bf16's precision."""
+    """The operand of the down blocks is two fp16 numbers where the output is fp32, or fp16 with up to eight tokens."""
     x, l = mixed.tokens(T), mixed.logits(T)
     out = mixed.ctx.pw_moe_forward_few(0, x, l, 3, out_dtype=dtype)
     pairs = plain.routing(f64(l), 3) + [(t, mixed.E + s, 1.0) for t in range(T) for s in range(mixed.ns)]
-    check(out, *plain.layer(f64(x), mixed.blocks, pairs, parts=2), dtype)
+    check(out, *plain.layer(f64(x), mixed.blocks, pairs, parts=2 if dtype == F32 or T <= 8 else 1), dtype)
 
 
 @pytest.mark.parametrize("T", [1, 2, 4, 7, 8, 9, 13, 16])
