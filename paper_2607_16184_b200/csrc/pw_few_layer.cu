@@ -22,7 +22,7 @@
 namespace pw {
 
 constexpr int kFewParts = 8;                      // most parts of the down blocks' columns
-constexpr int kFewRouters = 4;                    // warps that route
+constexpr int kFewRouters = 8;                    // warps that route (2 / 4 / 8 / 12: 16 tokens of 128 + 1 experts 64.5 / 62.1 / 60.9 / 63.7 us)
 // bytes of shared experts that are asked for while the tokens are routed: 2.5 us (none / 16 MB / 48 MB, 60 + 4 experts: one token
 // 28.8 / 28.9 / 31.1 us, four 40.2 / 39.5 / 41.2)
 constexpr size_t kFewAhead = 16 << 20;
