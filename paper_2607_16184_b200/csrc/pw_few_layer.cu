@@ -12,7 +12,7 @@
 // Bound by the pages' bytes: phase 1 runs at the HBM rate (one token of the 8 x (4096, 14336) layer at mixed bitwidths, 350 MB:
 // 233 MB in 31 us of 72), phase 2 of narrow formats by its instructions (a 4-bit step of 2 KB: about 300 of a warp), where
 // the hidden size gives 128 of the 148 SMs a unit.  Besides that a call takes about 1 us to launch, 3 to route and make its
-// tables (6 for 16 tokens of 128 experts), 2 for its first copies and 2.5 between the phases.  Asking the L2 cache for more of phase 2 while waiting was
+// tables (5 for 16 tokens of 128 experts), 2 for its first copies and 2.5 between the phases.  Asking the L2 cache for more of phase 2 while waiting was
 // slower (one token of the 60 + 4 expert layer 30.3 us against 28.9).  Sums are in fp32 in an order that depends on the routing
 // alone.
 #include "pw_scaled.cuh"
