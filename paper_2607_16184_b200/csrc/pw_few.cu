@@ -24,8 +24,11 @@ __device__ __forceinline__ void store_to_rank(uint32_t own_s, uint32_t rank, flo
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own_s), "r"(rank));
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
 __device__ __forceinline__ void team_sync(int team, int ts) { asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 << ts) : "memory"); }
 
@@ -89,6 +92,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
   float* const xsum = parts + (a.split > 1 ? kPartsBytes / 4 : 0);
   char* const pieces = reinterpret_cast<char*>(xsum) + ((a.split_groups * 3 * a.room * 4 + 127) & ~127);
 
+  if (a.split > 1) cluster_arrive();              // this CTA has started: the others may write to its memory
   const int rank = a.split > 1 ? (int)cluster_rank() : 0;
   const int cluster = a.split > 1 ? (int)blockIdx.x / a.split : (int)blockIdx.x, clusters = a.split > 1 ? (int)gridDim.x / a.split : (int)gridDim.x;
   const int g0 = a.groups * rank / a.split, my_groups = a.groups * (rank + 1) / a.split - g0;
@@ -125,7 +129,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     }
   };
 
-  bool waited = false, exchanged = false;
+  bool waited = false, met = false, exchanged = false;
 #pragma unroll 1
   for (int pass = cluster % a.passes; pass < a.passes; pass += clusters) {
     // the operand may be written by the kernel directly ahead, pages are not (see launch_page_linear): codes first
@@ -146,6 +150,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     stage_operand<1>(a.x + (size_t)token0 * a.x_pitch, a.x_pitch, cols, a.room, g0, my_groups, a.x_bytes, pieces, xsum, threadIdx.x,
                   kStreamThreads);
     __syncthreads();
+    if (a.split > 1 && !met) {
+      cluster_wait();                             // all CTAs of the cluster have started
+      met = true;
+    }
     // (tokens that there are not: any row and sum, their products are not used)
     const int xc = min(lane >> 2, cols - 1), c0 = min(2 * (lane & 3), cols - 1), c1 = min(2 * (lane & 3) + 1, cols - 1);
     const uint32_t x_lane = smem_u32(pieces) + xc * 256, sum0 = smem_u32(xsum + c0), sum1 = smem_u32(xsum + c1);
