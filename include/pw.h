@@ -444,9 +444,8 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
  * columns of page i follow those of page i - 1.  A dense block of the model (queries, keys and values of one input, an
  * output projection, the router, the vocabulary) kept and demoted like an expert's.
  * x: device fp16 [T, K], rows x_stride elements apart.  pages: host, TILED or PLANES, any bitwidth each, with the same
- * cols; they are read as they are when the call runs.  (The call may start to read pages while the kernel directly ahead
- * of it in the stream still runs, unless that is one of this context's that writes pages: a kernel of the caller's own
- * that writes one, and lets its successor start early, needs another operation between the two.)  A page is made of whole tiles and the block may be smaller:
+ * cols; they are read as they are when the stream comes to the call, whoever writes them ahead of it.  A page is made of
+ * whole tiles and the block may be smaller:
  * out_features[i] <= rows of page i (host, or NULL: all its rows) and cols - 128 < K <= cols; what the page holds past
  * them must be finite and does not count.  bias: device [sum of out_features] of bias_type, or NULL.  out: device
  * [T, sum of out_features] of out_type, apart from the inputs; sums in fp32 in a fixed order, rounded once.  A token with an

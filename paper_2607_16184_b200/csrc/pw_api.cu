@@ -126,7 +126,6 @@ extern "C" pw_status pw_create(pw_ctx** out, const pw_config* cfg) {
   ctx->last_T = ctx->last_k = 0;
   ctx->few_ready = 0;
   ctx->few_layer_ready = 0;
-  ctx->page_writers = 0;
   ctx->dense_encode = nullptr;
   ctx->tc_state = nullptr;
   ctx->wait_polls = 0;

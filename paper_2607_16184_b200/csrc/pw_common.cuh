@@ -124,7 +124,6 @@ struct pw_ctx {
   std::atomic<int> max_clusters[5];   // clusters of that product's CTAs that run at the same time, by size
   std::atomic<int> few_clusters[3];   // the same for the kernels for few tokens: clusters of 2, 4, 8 of their CTAs
   std::atomic<int> few_ready;     // those are looked up
-  std::atomic<uint64_t> page_writers; // streams (by a hash) that a page was written on, and no product has been called on since
   std::atomic<void*> dense_encode;    // driver entry point for tensor maps, once the dense product's kernels have their attributes
   std::atomic<int> few_layer_ready;   // the few-token layer's kernels have their attributes
   void* tc_state;                 // tensor-core path state (set up lazily)
@@ -214,14 +213,6 @@ void timing_mark(pw_ctx* ctx, int i, cudaStream_t s);
 // Pointer qualifiers follow from this: `const __restrict__` (which allows non-coherent loads) only on data that
 // is final when the kernel is placed -- pages, page-table rows, anything written two or more kernels back; a
 // buffer that the kernel directly ahead writes is passed as a plain pointer and read after grid_dep_sync().
-// pw_page_linear's kernel reads pages before its grid_dep_sync() as well, and a page may be the work of the kernel directly
-// ahead: calls that write one note the stream, and the next product there is launched without the attribute.
-inline uint64_t stream_bit(cudaStream_t s) { return 1ull << ((reinterpret_cast<uintptr_t>(s) * 0x9e3779b97f4a7c15ull) >> 58); }
-inline void note_page_write(pw_ctx* ctx, cudaStream_t s) { ctx->page_writers.fetch_or(stream_bit(s), std::memory_order_relaxed); }
-inline bool take_page_write(pw_ctx* ctx, cudaStream_t s) {
-  const uint64_t bit = stream_bit(s);
-  return (ctx->page_writers.load(std::memory_order_relaxed) & bit) && (ctx->page_writers.fetch_and(~bit, std::memory_order_relaxed) & bit);
-}
 __device__ __forceinline__ void grid_dep_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_dep_sync() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -129,21 +129,23 @@ __global__ void __launch_bounds__(kStreamThreads, 1) page_linear_kernel(const __
     }
   };
 
-  bool waited = false, met = false, exchanged = false;
+  // The operand and the pages may be the work of the kernel directly ahead, which may still run: nothing is read before the
+  // wait.  The first codes are only asked to come into the L2 cache, where what that kernel writes goes as well.
+  next = first + sharing * team;
+  if (more()) prefetch_steps<STAGES>(f, lane);
+  f.left = 0;
+  grid_dep_sync();
+  grid_dep_trigger();
+
+  bool met = false, exchanged = false;
 #pragma unroll 1
   for (int pass = cluster % a.passes; pass < a.passes; pass += clusters) {
-    // the operand may be written by the kernel directly ahead, pages are not (see launch_page_linear): codes first
     next = first + sharing * team;
     r.slot = r.base;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) {
       ask_next();
       ring_on<0, STAGES>(r);
-    }
-    if (!waited) {
-      grid_dep_sync();
-      grid_dep_trigger();
-      waited = true;
     }
     const int token0 = pass * a.width, cols = min(a.width, a.T - token0);
     __syncthreads();                              // the pass before has read its operand
@@ -226,8 +228,7 @@ static PageLinearKernel page_linear_kernel_of(int fmt) {
   }
 }
 static PageLinearKernel page_linear_kernel_of(int fmt, int stages) { return stages == 4 ? page_linear_kernel_of<4>(fmt) : page_linear_kernel_of<2>(fmt); }
-// overlap: the kernel may be placed while the one directly ahead still runs, which has not written a page then.
-static cudaError_t launch_page_linear(const PageLinearArgs& a, PageLinearKernel kernel, int clusters, size_t smem, bool overlap, cudaStream_t s) {
+static cudaError_t launch_page_linear(const PageLinearArgs& a, PageLinearKernel kernel, int clusters, size_t smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(clusters * a.split));
   cfg.blockDim = dim3(kStreamThreads);
@@ -235,7 +236,7 @@ static cudaError_t launch_page_linear(const PageLinearArgs& a, PageLinearKernel 
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = overlap;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = a.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
@@ -450,7 +451,7 @@ extern "C" pw_status pw_page_linear(pw_ctx* ctx, int T, int K, const void* x_fp1
   int fmt = a.page[0].fmt;
   for (int i = 1; i < n_pages; ++i)
     if (a.page[i].fmt != fmt) fmt = kAnyFormat;
-  PW_CUDA_OK(launch_page_linear(a, page_linear_kernel_of(fmt, p.stages), p.clusters, smem, !take_page_write(ctx, stream), stream));
+  PW_CUDA_OK(launch_page_linear(a, page_linear_kernel_of(fmt, p.stages), p.clusters, smem, stream));
   ctx->launches++;
   return PW_OK;
 }

@@ -156,7 +156,6 @@ extern "C" pw_status pw_quantize_planes(pw_ctx* ctx, const void* w, uint32_t row
   quant_planes_kernel<<<grid, 512, 0, stream>>>(reinterpret_cast<const __half*>(w), cols, reinterpret_cast<char*>(dst->codes),
                                                 reinterpret_cast<char*>(dst->scales), reinterpret_cast<char*>(dst->zps));
   ctx->launches++;
-  note_page_write(ctx, stream);
   PW_CUDA_OK(cudaGetLastError());
   return PW_OK;
 }

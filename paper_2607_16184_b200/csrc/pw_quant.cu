@@ -452,7 +452,6 @@ extern "C" pw_status pw_quantize_block(pw_ctx* ctx, const void* w, uint32_t rows
   dim3 grid(cols / kGroup, rows / kTileRows);
   launch_quant_dst<SRC_RAW, 16>(bits, grid, stream, w, cols, dst);
   ctx->launches++;
-  note_page_write(ctx, stream);
   PW_CUDA_OK(cudaGetLastError());
   return PW_OK;
 }
@@ -482,7 +481,6 @@ extern "C" pw_status pw_demote_block(pw_ctx* ctx, const pw_page* src, int dst_bi
     case 3: launch_quant_dst<SRC_TILED, 3>(dst_bits, grid, stream, src->codes, src->cols, dst); break;
   }
   ctx->launches++;
-  note_page_write(ctx, stream);
   PW_CUDA_OK(cudaGetLastError());
   return PW_OK;
 }
@@ -518,7 +516,6 @@ static pw_status relayout(pw_ctx* ctx, const pw_page* src, pw_page* dst, cudaStr
     case 2: relayout_kernel<2, EXPORT><<<grid, 512, 0, stream>>>(src->codes, src->cols, dst->codes, cs, cz); break;
   }
   ctx->launches++;
-  note_page_write(ctx, stream);
   PW_CUDA_OK(cudaGetLastError());
   return PW_OK;
 }

@@ -215,6 +215,33 @@ __device__ __forceinline__ void prefetch_bytes(const char* p, uint32_t n) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(n) : "memory");
 }
 
+// Asks the L2 cache for the feed's first steps, at most STAGES: a lane per line of a step.
+template <int STAGES>
+__device__ __forceinline__ void prefetch_steps(const Feed& f, int lane) {
+  const int ls = step_shift(f.fmt), units = f.fmt <= kFmt4 ? 4 : f.fmt == kFmt3 ? 3 : 2;
+  const int bits = f.fmt == kFmtP4 ? 2 : f.fmt == kFmtP3 ? 1 : 0;   // planes of single bits
+  // lanes 0 .. 15: units of 512 bytes, four lines each; 16 .. 23: the planes'; 24, 25: scales and zero-points
+  const char* line = f.codes - 16 * lane + 2048 * (lane >> 2) + 128 * (lane & 3);
+  bool on = lane < 4 * units;
+  if (lane >= 16 && lane < 16 + 4 * bits) {
+    line = (lane < 20 ? f.bit1 : f.bit0) - 16 * lane + 128 * (lane & 3);
+    on = true;
+  } else if (lane >= 24 && lane < 26 && f.fmt != kFmt16) {
+    line = f.meta - (lane >> 2) * 256 - (lane & 3) * 16 + (lane - 24) * 256;
+    on = true;
+  }
+  const bool plane = lane >= 16 && lane < 24, meta = lane >= 24;
+  const uint32_t tile = plane ? (uint32_t)kPlaneBitTile : kTileBytes[f.fmt];
+  const int steps = min(STAGES, f.left);
+#pragma unroll
+  for (int i = 0; i < STAGES; ++i) {
+    const int q = f.sub + i;
+    const char* at = line + (uint32_t)(q >> ls) * tile;
+    if (!plane && !meta) at += ((q & ((1 << ls) - 1)) - f.sub) * 8192;
+    if (on && i < steps) asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+  }
+}
+
 // ---- staged operand ------------------------------------------------------------------------------
 // Two neighbouring pieces (a stretch of 16 columns) of columns as they lie in memory.
 __device__ __forceinline__ void make_pieces(const uint4& lo, const uint4& hi, uint4 (&piece)[2]) {
