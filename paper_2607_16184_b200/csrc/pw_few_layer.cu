@@ -539,6 +539,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       for (uint32_t j = 0; j < note[i].y >> 2; ++j) cp16(to + j * 512, x + (size_t)j * step);
       cp_commit();
     }
+    __syncwarp();                                 // every lane has read its notes
     // (for no more tokens than a unit's where those of phase 1 were, and the notes: a warp's place is its own)
     const int set_floats = max(p.T, kUnitCols) * kSumPitch;
     float* const sums2 = p.T <= kUnitCols ? sums : reinterpret_cast<float*>(rest + kStreamWarps * STAGES * 256 * XC);

@@ -37,3 +37,16 @@ def test_no_note_of_written_pages_decides_how_a_product_is_launched():
     """Such a note could be lost: to another stream, to a capture, to another context."""
     for name in ("pw_few.cu", "pw_quant.cu", "pw_planes.cu", "pw_common.cuh"):
         assert "page_write" not in source(name)
+
+
+def test_notes_of_the_layer_are_read_by_all_lanes_before_any_lane_writes_there():
+    """The sums of the second phase lie where the notes are, and a lane clears what others have noted."""
+    kernel = body(source("pw_few_layer.cu"), "few_layer_kernel(const __grid_constant__")
+    read, clear = kernel.index("lds8(notes"), kernel.index("own[i] = 0.f")
+    between = kernel[read:clear]
+    # outside of every loop and branch: at the depth of braces of the reading
+    depth, found = 0, False
+    for part in re.findall(r"[{}]|__syncwarp\(\);", between):
+        depth += {"{": 1, "}": -1}.get(part, 0)
+        found |= part == "__syncwarp();" and depth == 0
+    assert found
