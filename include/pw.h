@@ -324,9 +324,9 @@ pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16,
 /* The two layer calls for a handful of tokens, T <= PW_FEW_TOKENS, in one kernel: the latency of a decode step.  Same pages
  * (TILED and PLANES), page table, routing rule, routed ids and gates, observation taps; out: device [T, H] of out_type
  * (pw_type), apart from the inputs.  They differ from pw_moe_forward in the weights, which are code * scale + zero-point
- * without the rounding to fp16, in the operand of the down blocks, which is kept to 22 bits (fp16 where out_type is bf16, or
- * is fp16 with more than eight tokens), and in that a token that names an expert twice is multiplied once, with the sum of
- * the gates.
+ * without the rounding to fp16, in the operand of the down blocks, silu(gate) * up, which is kept to 22 bits (to 2^-36 below
+ * 2^-14; beyond 65504 it is infinite, as in pw_moe_forward), and in that a token that names an expert twice is multiplied
+ * once, with the sum of the gates.
  * The activations of the call are kept in an SM's shared memory: T * hidden up to 65536 where T * (top_k + n_shared) is
  * at most 48, up to 49152 otherwise (SHAPE where there is no room).
  * All CTAs of the kernel run at the same time (a cooperative launch): on a device that other kernels keep busy it starts

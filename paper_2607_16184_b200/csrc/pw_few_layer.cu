@@ -22,6 +22,15 @@
 namespace pw {
 
 constexpr int kFewParts = 8;                      // most parts of the down blocks' columns
+// The operand h of the down blocks is kept in two fp16 numbers: the nearest one, and what that leaves, times 2^11, so that
+// the second has as many bits as the first wherever the first has all of its own: 22 bits of h, or 2^-36 where h is below
+// 2^-14 (without the factor everything below 2^-25 was lost, 1.7e-4 of an h of 1e-4).  They stand in neighbouring columns of
+// the matrix instructions, which most experts leave empty: an expert of more than four tokens takes a second pass.  (One
+// number would save that, and cost 2e-4 of the output's norm: 16 tokens of the 8-expert layer 147 us against 177, of the
+// 60 + 4 expert layer 79 against 88; 8 tokens 131 and 132, 51 and 55.)
+constexpr int kHalves = 2;
+constexpr int kDownCols = kUnitCols / kHalves;    // tokens of a pass of the second phase
+constexpr float kRestUp = 2048.f, kRestDown = 1.f / kRestUp;
 constexpr int kFewRouters = 8;                    // warps that route (2 / 4 / 8 / 12: 16 tokens of 128 + 1 experts 64.5 / 62.1 / 60.9 / 63.7 us)
 // bytes of shared experts that are asked for while the tokens are routed: 2.5 us (none / 16 MB / 48 MB, 60 + 4 experts: one token
 // 28.8 / 28.9 / 31.1 us, four 40.2 / 39.5 / 41.2)
@@ -36,13 +45,12 @@ struct FewArgs {
   const int32_t* ids;
   const float* gates;
   void* out;
-  char* h;                                        // [pair][halves][F] pieces
+  char* h;                                        // [pair][kHalves][F] pieces
   float* parts;                                   // [part][T][H]
   int32_t* sync;                                  // arrivals; from 64 on: finished parts of every 32 output rows
   int32_t* status;
   int32_t* seen;                                  // for the observation taps (or null): see few_observe_kernel
   int T, k, E, n_shared, H, F, out_type;
-  int halves;                                     // fp16 numbers that a value of h is kept in: their sum
   int segs, pairs;                                // room for active experts and for their (expert, token) pairs
   int n_parts;                                    // parts of the down blocks' columns
   uint32_t per_part;                              // 2^32 / n_parts, rounded up
@@ -140,7 +148,7 @@ __device__ __forceinline__ uint32_t piece_offset(int f, int c) {
 }
 
 // Walks the steps lo .. hi of the list of all down blocks, (segment, pass) after (segment, pass); at most four passes of a
-// segment, of kUnitCols / halves tokens.
+// segment, of kDownCols tokens.
 struct DownRun {
   int a, pass, lo, n;
 };
@@ -182,7 +190,7 @@ __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevR
     }
     const uint32_t passes = (uint32_t)(n + kUnitCols - 1) / kUnitCols;
     t.weight[a] = make_uint2((e < p.E ? 0u : 1u << 31) | tiles << 9 | (511u - a), 1u << 16 | passes);
-    t.step0[a] = (int32_t)((uint32_t)(n * p.halves + kUnitCols - 1) / kUnitCols << shift);   // (summed up below)
+    t.step0[a] = (int32_t)((uint32_t)(n + kDownCols - 1) / kDownCols << shift);   // (summed up below)
   };
   // experts with tokens, ascending, then the shared ones: every warp counts all, and makes the segments of some
   int segs = 0, pairs = 0;
@@ -415,18 +423,13 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         }
         // (fast exponential and division: relative error ~1e-6)
         const float h = __fmul_rn(__fdividef(gate, __fadd_rn(1.0f, __expf(-gate))), up);
-        // The operand of the down block is fp16, like that of the layer call for batches; with a second fp16 number for
-        // what the first leaves, it is h to 22 bits.  Beyond the largest fp16 number there is nothing to leave.
+        // (beyond the largest fp16 number h is infinite, like the operand of the layer call for batches)
         const __half high = __float2half_rn(h);
-        const float left = __hisinf(high) ? 0.f : __fsub_rn(h, __half2float(high));
-        char* const to = p.h + (size_t)(pair0 + col) * p.halves * p.F * 2;
+        const float left = __hisinf(high) ? 0.f : __fmul_rn(__fsub_rn(h, __half2float(high)), kRestUp);
+        char* const to = p.h + (size_t)(pair0 + col) * kHalves * p.F * 2;
         const int f = g.slice * kUnitRows + row;
-        if (p.halves == 1) {
-          *reinterpret_cast<__half*>(to + piece_offset(f, col)) = high;
-        } else {
-          *reinterpret_cast<__half*>(to + piece_offset(f, 0)) = high;
-          *reinterpret_cast<__half*>(to + (size_t)p.F * 2 + piece_offset(f, 1)) = __float2half_rn(left);
-        }
+        *reinterpret_cast<__half*>(to + piece_offset(f, 0)) = high;
+        *reinterpret_cast<__half*>(to + (size_t)p.F * 2 + piece_offset(f, 1)) = __float2half_rn(left);
       }
       few_team_sync(w);                    // the sums are written again
     }
@@ -447,7 +450,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   // ---- phase 2: down ----
   {
     const int steps = t.step0[segs];              // of a slice
-    const int per_pass = kUnitCols / p.halves;    // tokens
     const int units = p.H / kUnitRows * p.n_parts;
     const int mine = units / G + (b < units % G);
     auto slice_of = [&](int unit) { return p.n_parts == 1 ? unit : (int)__umulhi((uint32_t)unit, p.per_part); };   // unit / n_parts
@@ -477,9 +479,9 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
         slice = slice_of(unit);
       }
       const SegPage& page = t.page[3 * d.a + PW_DOWN];
-      const int pair0 = t.off[d.a] + d.pass * per_pass;
+      const int pair0 = t.off[d.a] + d.pass * kDownCols;
       feed_codes(f, lane, page.codes, page.bit1, page.bit0, t.fmt[4 * d.a + PW_DOWN], fg, slice, d.lo, d.lo + d.n);
-      feed_operand(f, lane, p.h + (size_t)pair0 * p.halves * p.F * 2, (uint32_t)p.F * 2, min(per_pass, t.off[d.a + 1] - pair0) * p.halves, d.lo);
+      feed_operand(f, lane, p.h + (size_t)pair0 * kHalves * p.F * 2, (uint32_t)p.F * 2, min(kDownCols, t.off[d.a + 1] - pair0) * kHalves, d.lo);
       return true;
     };
     // The first steps are asked for without their operand, which is not there yet.  What a lane will copy of it is noted in
@@ -560,31 +562,22 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 #pragma unroll 1
       while (down_run(t, fg, place, stop, where, d)) {
         const int fmt = t.fmt[4 * d.a + PW_DOWN], ls = step_shift(fmt);
-        const int pair0 = t.off[d.a] + d.pass * per_pass, cols = min(per_pass, t.off[d.a + 1] - pair0);
-        const int xc = min(lane >> 2, cols * p.halves - 1);
+        const int pair0 = t.off[d.a] + d.pass * kDownCols, cols = min(kDownCols, t.off[d.a + 1] - pair0);
+        const int xc = min(lane >> 2, cols * kHalves - 1);
         float tot[2][4] = {};
         Operand o{(uint32_t)(xc * (256 >> ls)), 0, 0, 0, ls == 2 ? 0 : (uint32_t)(xc & 1) << 2, d.lo};
         walk<kAnyFormat, XC, STAGES>(fixed, fmt, d.n, f, r, o, tot, ask_next);
-        // the tokens of a run are different ones: no two lanes meet
-        auto add = [&](int col, const float4& y) {
+        // Columns 2t and 2t + 1 are the two numbers of token t.  The tokens of a run are different ones: no two lanes meet.
+        const int col = lane & 3;
+        if (col < cols) {
           const float gate = t.gate[pair0 + col];
           float4* to = reinterpret_cast<float4*>(own + t.token[pair0 + col] * kSumPitch + 4 * (lane >> 2));
           float4 v = *to;
-          v.x = __fadd_rn(v.x, __fmul_rn(gate, y.x));
-          v.y = __fadd_rn(v.y, __fmul_rn(gate, y.y));
-          v.z = __fadd_rn(v.z, __fmul_rn(gate, y.z));
-          v.w = __fadd_rn(v.w, __fmul_rn(gate, y.w));
+          v.x = __fadd_rn(v.x, __fmul_rn(gate, fmaf(tot[0][1], kRestDown, tot[0][0])));
+          v.y = __fadd_rn(v.y, __fmul_rn(gate, fmaf(tot[0][3], kRestDown, tot[0][2])));
+          v.z = __fadd_rn(v.z, __fmul_rn(gate, fmaf(tot[1][1], kRestDown, tot[1][0])));
+          v.w = __fadd_rn(v.w, __fmul_rn(gate, fmaf(tot[1][3], kRestDown, tot[1][2])));
           *to = v;
-        };
-        if (p.halves == 1) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int col = 2 * (lane & 3) + c;
-            if (col < cols) add(col, make_float4(tot[0][c], tot[0][c + 2], tot[1][c], tot[1][c + 2]));
-          }
-        } else if ((lane & 3) < cols) {           // columns 2t and 2t + 1 are the two parts of token t
-          add(lane & 3, make_float4(__fadd_rn(tot[0][0], tot[0][1]), __fadd_rn(tot[0][2], tot[0][3]), __fadd_rn(tot[1][0], tot[1][1]),
-                                    __fadd_rn(tot[1][2], tot[1][3])));
         }
         __syncwarp();
       }
@@ -651,7 +644,7 @@ __device__ __forceinline__ float square_sum(const uint4* row, int n, int lane) {
   for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
   return a;
 }
-__global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, int room, int pairs, const uint4* hidden, const uint4* h, int halves, int H, int F, int E,
+__global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, int room, int pairs, const uint4* hidden, const uint4* h, int H, int F, int E,
                                                           const int32_t* ids, int Tk, float* __restrict__ acc) {
   const int a = (int)(blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
   if (a >= seen[0]) return;
@@ -661,7 +654,7 @@ __global__ void __launch_bounds__(256) few_observe_kernel(const int32_t* seen, i
   float sr = 0.f, srx = 0.f, srx2 = 0.f, mx = 0.f, srh = 0.f, srh2 = 0.f, mh = 0.f;
 #pragma unroll 1
   for (int i = p0; i < p1; ++i) {
-    const float r = gates[i], x2 = square_sum(hidden + (size_t)tokens[i] * (H / 8), H / 8, lane), h2 = square_sum(h + (size_t)i * halves * (F / 8), F / 8, lane);
+    const float r = gates[i], x2 = square_sum(hidden + (size_t)tokens[i] * (H / 8), H / 8, lane), h2 = square_sum(h + (size_t)i * kHalves * (F / 8), F / 8, lane);
     const float nx = sqrtf(x2), nh = sqrtf(h2);
     sr += r;
     srx = fmaf(r, nx, srx);
@@ -730,13 +723,7 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.out_type = out_type;
   a.segs = (c.n_experts < T * top_k ? c.n_experts : T * top_k) + c.n_shared;
   a.pairs = T * (top_k + c.n_shared);
-  // h in two numbers costs next to nothing while the matrix instructions have columns to spare, four tokens of an expert at a
-  // time: an output of more than bf16's precision is then as near to the definition as an fp32 operand would make it
-  // (fp16: 2.1e-4 of its norm, with one number 2.9e-4; fp32: 1e-6, 2e-4).  With more tokens experts need more passes, and an
-  // fp16 output shows little of it: 16 tokens of the 60 + 4 expert layer 88 us with two, 79 with one, of the 8-expert layer
-  // 177 and 147; 8 tokens 55 and 51, 132 and 131.
-  a.halves = out_type == PW_F32 || (out_type == PW_F16 && T <= kUnitCols) ? 2 : 1;
-  const int operand_rows = a.halves == 1 ? (T < kUnitCols ? T : kUnitCols) : 2 * T < kUnitCols ? 2 * T : kUnitCols;
+  const int operand_rows = kHalves * T < kUnitCols ? kHalves * T : kUnitCols;
   const FewVariant* v = nullptr;
   for (const FewVariant& one : kFewVariants)
     if (!v && operand_rows <= one.rows && a.segs <= one.segs && a.pairs <= one.pairs && T * top_k <= one.choices && few_smem(a, one) <= kSmemLimit) v = &one;
@@ -772,7 +759,7 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
     if (best < 0 || us < best) best = us, a.n_parts = parts;
   }
   // (see `range`: a place in the list of steps, times the parts of it, divided by multiplication)
-  if (((int64_t)a.segs + a.pairs * a.halves / kUnitCols) * (c.ffn / kGroup) * 4 * (kFewParts * kStreamWarps) >= 1 << 29) return PW_ERR_SHAPE;
+  if (((int64_t)a.segs + a.pairs / kDownCols) * (c.ffn / kGroup) * 4 * (kFewParts * kStreamWarps) >= 1 << 29) return PW_ERR_SHAPE;
   a.per_part = a.n_parts > 1 ? (uint32_t)((0xffffffffull + a.n_parts) / a.n_parts) : 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctx->num_sms);
@@ -787,7 +774,7 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   PW_CUDA_OK(cudaLaunchKernelEx(&cfg, v->kernel, a));
   ctx->launches++;
   if (ctx->obs_acc) {
-    few_observe_kernel<<<(a.segs + 7) / 8, 256, 0, stream>>>(a.seen, a.segs, a.pairs, static_cast<const uint4*>(hidden), reinterpret_cast<const uint4*>(a.h), a.halves,
+    few_observe_kernel<<<(a.segs + 7) / 8, 256, 0, stream>>>(a.seen, a.segs, a.pairs, static_cast<const uint4*>(hidden), reinterpret_cast<const uint4*>(a.h),
                                                             a.H, a.F, a.E, routing.logits ? nullptr : routing.ids, T * top_k,
                                                             ctx->obs_acc + (size_t)layer * w.S * PW_OBS_FIELDS);
     ctx->launches++;
