@@ -437,8 +437,7 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
 /* ---- few tokens ------------------------------------------------------------------------- */
 
 /* Products that read weight pages for a handful of tokens at a time, as decoding does.  Here the weight of a code is
- * code * scale + zero-point, not rounded to fp16 (scale and zero-point are applied to a group's sums, in fp32), except
- * where a call says otherwise. */
+ * code * scale + zero-point, not rounded to fp16 (scale and zero-point are applied to a group's sums, in fp32). */
 
 /* out[t, col] = sum_k x[t, k] * w[col, k] (+ bias[col]) for the blocks of up to PW_LINEAR_PAGES pages side by side: the
  * columns of page i follow those of page i - 1.  A dense block of the model (queries, keys and values of one input, an
@@ -454,8 +453,10 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
  * enqueues nothing.
  * workspace: device, or NULL.  With the bytes that pw_page_linear_workspace reports (0: the call has no use for any), calls
  * with a 16-bit output of more tokens than that pays for (more than eight; by an estimate of the times) go through the
- * tensor-core kernel of the layer calls instead, in three launches, with the weights rounded to fp16 like theirs; with
- * less, or none, the call does without.  pw_page_linear_workspace is 0 for invalid arguments too.
+ * tensor-core kernel of the layer calls instead, in three launches and another order of sums; with less, or none, the call
+ * does without.  (There code * scale is taken about the middle of the codes, in two fp16 numbers that hold all of it for
+ * scales up to 131008 / 2^bits, which every block of fp16 weights has; beyond, results may be infinite.)
+ * pw_page_linear_workspace is 0 for invalid arguments too.
  * Needs a context of the current device, but neither its page table nor its workspace: calls on different streams may run
  * at the same time, each with a workspace of its own.
  * Errors: INVALID_ARG (a null pointer, a type, n_pages, out_features below 1), SHAPE (page shapes, K or out_features

@@ -363,22 +363,27 @@ static int64_t set_pages(PageLinearArgs& a, int T, int K, const pw_page* pages, 
   a.pages = n_pages;
   return columns;
 }
-// Whether a call goes through the tensor-core kernel of the layer calls (three launches, and weights rounded to fp16, which
-// an fp32 output would show), and what of its cut does not depend on the device.  By estimates of both times in us: this
-// kernel's from its cut, the other's linear in the weights (millions) and the tokens.  Measured, here / there: 4096 x 4096
-// at 4 bits, 64 tokens 16.9 / 14.3; 14336 x 4096 at 4 bits, 32 tokens 27.5 / 20.2, 64 tokens 47.5 / 21.7; 4096 x 14336 at
-// 8 bits, 64 tokens 60.4 / 23.3; 1260 x 1000 in planes of 4 bits, 300 tokens 13.7 / 13.5, 600 tokens 34.2 / 16.4; 40 x 128
-// at 4 bits, 1200 tokens 5.0 / 10.7.
+// Whether a call goes through the tensor-core kernel of the layer calls (three launches; outputs of 16 bits), and what of its
+// cut does not depend on the device.  By estimates of both times in us: this kernel's from its cut; the other's as a sum of
+// terms, 11 for the launches, 0.2 per million weights (decoding), 2.3 per billion products, 4 per million outputs (parts of
+// sums, written and read), fitted to thirty shapes.  Of those it takes the faster kernel, or one within 5 %.  Measured, here /
+// there: 14336 x 4096 at 4 bits, 16 tokens 16.4 / 26.5, 32 tokens 27.0 / 27.6, 64 tokens 46.9 / 32.0, 256 tokens 188 / 72;
+// 4096 x 4096 at 4 bits, 64 tokens 17.6 / 17.3; 4096 x 14336 at 8 bits, 64 tokens 61 / 32; 28672 x 8192 at 4 bits, 16 tokens
+// 51 / 73; 1260 x 1000 in planes of 4 bits, 300 tokens 15.4 / 14.6, 600 tokens 37 / 17.7; 40 x 128 at 4 bits, 1200 tokens
+// 5.4 / 11.5.
 static bool many_tokens(DenseCall* d, const PageLinearArgs& call, const pw_page* pages, int out_type, int sms) {
   if (call.T <= kUnitCols || out_type == PW_F32) return false;
-  double m = 0;
-  for (int i = 0; i < call.pages; ++i) m += 1e-6 * pages[i].cols * call.page[i].rows;
+  double m = 0, width = 0;                         // millions of weights; columns, in whole tiles
+  for (int i = 0; i < call.pages; ++i) {
+    m += 1e-6 * pages[i].cols * call.page[i].rows;
+    width += (call.page[i].rows + kTileRows - 1) / kTileRows * kTileRows;
+  }
   // (about as many clusters as run at the same time: the workspace's size must not depend on the current device)
   int clusters[kSplits];
   for (int i = 0; i < kSplits; ++i) clusters[i] = sms * 7 / (8 * (2 << i));
   PageLinearArgs a = call;
   const PageLinearPlan here = plan_page_linear(a, sms, clusters);
-  if (here.stages && 2.5 + here.cycles / 1680. <= 12. + m * (0.09 + 0.0017 * call.T) + 0.0005 * call.T) return false;
+  if (here.stages && 2.5 + here.cycles / 1680. <= 11. + 0.2 * m + 2.3e-3 * m * call.T + 4e-6 * call.T * width) return false;
   *d = DenseCall{};
   d->T = call.T;
   d->cols = (int)pages[0].cols;

@@ -293,6 +293,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const __half2* v) {
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const __half2* v) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // The slot ring.  Everything that travels through it is one "slot item" of at most kSlotBytes: a quantized
@@ -421,6 +429,28 @@ __device__ __forceinline__ void mbar_arrive_if_s(uint32_t bar_s, bool pred) {
                : "memory");
 }
 
+// Codes are used about their middle where weights must not be rounded: code' = code - 2^(bits - 1), weight = code' * scale +
+// (zero-point + 2^(bits - 1) * scale), the second term being the same for a row's whole group (see dense_finish_kernel).
+// code' * scale has up to 19 bits: the nearest fp16 number, and what that leaves, which is an fp16 number too (both are
+// multiples of the scale's last place).  So that the first stays finite where a group spans more than half of fp16's range it
+// is made from a scale of at most 65504 / 2^(bits - 1); the second then takes the difference.
+// Quarter t of row r of a tile: the two numbers of its 32 weights.
+template <uint32_t UB>
+__device__ __forceinline__ void decode_quarter_exact(const char* item, int r, int t, __half2 scale, __half2* near, __half2* rest) {
+  constexpr int bits = (int)(UB & 63u);
+  constexpr bool planes = (UB & kPlanesFlag) != 0 && bits > 2;
+  __half2 code[16];
+  if constexpr (planes) decode_quarter_planes<bits>(item, r, t, CentredCodes<bits>{}, code);
+  else decode_quarter<bits>(reinterpret_cast<const uint4*>(item) + r, t, CentredCodes<bits>{}, code);
+  const __half2 most = u32_as_h2((0x7bffu - ((uint32_t)(bits - 1) << 10)) * 0x00010001u);
+  const __half2 first = __hmax2(__hmin2(scale, most), __hneg2(most));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    near[i] = __hmul2(code[i], first);
+    rest[i] = __hfma2(code[i], scale, __hneg2(near[i]));
+  }
+}
+
 // What a dequantizer warp carries from tile to tile.
 struct DqState {
   uint32_t sq;                                   // number of my next slot item
@@ -436,7 +466,8 @@ struct DqState {
 // in, and nothing about the format is decided per tile.  The per-tile control path is a chain of dependent
 // instructions that the decoders of the other groups do not hide, so it is kept as short as it gets.
 // UB: bitwidth, with kPlanesFlag for a tile of a bit-plane block.
-template <uint32_t UB, uint32_t LIM>
+// EXACT: a tile is handed over in K-halves, each as the two fp16 numbers of code' * scale (see decode_quarter_exact).
+template <uint32_t UB, uint32_t LIM, bool EXACT>
 __device__ __forceinline__ bool dq_run(DqState& st, uint32_t count, uint32_t step, uint32_t n_slots, uint32_t wring_s,
                                        int r, bool lane0, uint32_t lane_addr, uint32_t full_s, uint32_t empty_s,
                                        uint32_t a_full_s, uint32_t a_empty_s, Ctrl* c, int32_t* status) {
@@ -464,25 +495,50 @@ __device__ __forceinline__ bool dq_run(DqState& st, uint32_t count, uint32_t ste
       z2 = __half2half2(__ushort_as_half(zv));
     }
     const char* item = reinterpret_cast<const char*>(c) + kCtrlBytes + st.s * kSlotBytes;
+    if constexpr (!EXACT) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      __half2 w[32];
-      if constexpr ((UB & kPlanesFlag) != 0) decode_half_planes<(int)(UB & ~kPlanesFlag)>(item, r, h, s2, z2, w);
-      else decode_half<(int)UB>(reinterpret_cast<const uint4*>(item) + r, h, s2, z2, w);
-      if (h == 0) {
-        if (!mbar_wait_s<LIM>(a_empty_s, st.a_par ^ 1, c, status)) return false;
-        tc_fence_after();
-      } else {
-        __syncwarp();
-        mbar_arrive_if_s(empty_s + 8 * st.s, lane0);   // this warp has read its rows of the tile
+      for (int h = 0; h < 2; ++h) {
+        __half2 w[32];
+        if constexpr ((UB & kPlanesFlag) != 0) decode_half_planes<(int)(UB & ~kPlanesFlag)>(item, r, h, s2, z2, w);
+        else decode_half<(int)UB>(reinterpret_cast<const uint4*>(item) + r, h, s2, z2, w);
+        if (h == 0) {
+          if (!mbar_wait_s<LIM>(a_empty_s, st.a_par ^ 1, c, status)) return false;
+          tc_fence_after();
+        } else {
+          __syncwarp();
+          mbar_arrive_if_s(empty_s + 8 * st.s, lane0);   // this warp has read its rows of the tile
+        }
+        tmem_st32(lane_addr + h * 32, w);
       }
-      tmem_st32(lane_addr + h * 32, w);
+      // hand the tile over: both stores have landed, then one arrival per warp
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive_if_s(a_full_s, lane0);
+      st.a_par ^= 1u;
+    } else {
+      // a K-half at a time: the nearest numbers in the slot's first 32 columns, what they leave in the others
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          __half2 near[16], rest[16];
+          decode_quarter_exact<UB>(item, r, 2 * h + t, s2, near, rest);
+          if (t == 0) {
+            if (!mbar_wait_s<LIM>(a_empty_s, st.a_par ^ 1, c, status)) return false;
+            tc_fence_after();
+          } else if (h == 1) {
+            __syncwarp();
+            mbar_arrive_if_s(empty_s + 8 * st.s, lane0);   // this warp has read its rows of the tile
+          }
+          tmem_st16(lane_addr + t * 16, near);
+          tmem_st16(lane_addr + 32 + t * 16, rest);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive_if_s(a_full_s, lane0);
+        st.a_par ^= 1u;
+      }
     }
-    // hand the tile over: both stores have landed, then one arrival per warp
-    tmem_wait_st();
-    tc_fence_before();
-    mbar_arrive_if_s(a_full_s, lane0);
-    st.a_par ^= 1u;
     st.sq += step;
     st.s += step;
     if (st.s >= n_slots) {                       // step never exceeds the number of slots
@@ -530,7 +586,9 @@ __device__ __forceinline__ int unit_accumulators(int npart, int nb_rows, int aco
 // SHORT: the instantiation with the short wait limit (kTestWaitPolls instead of kDefaultWaitPolls), for the test of
 // the failure path.  hook: test hook, bit 0 = the token-tile producer stops before its second tile (so that the
 // waits on it run out).
-template <int PHASE, bool HELP, bool PLANES, bool SHORT, bool SHARE = false>
+// EXACT: the instantiation for products whose weights are not rounded to fp16 (see decode_quarter_exact); the terms of the middles
+// are the caller's.
+template <int PHASE, bool HELP, bool PLANES, bool SHORT, bool SHARE = false, bool EXACT = false>
 __global__ void __launch_bounds__(kThreads, 1)
 ffn_tc_kernel(const DevRow* __restrict__ rows, const Unit* units, const int32_t* __restrict__ n_units_ptr,
               const __grid_constant__ TmapSet tmaps, int Rpad, int nt_tile, int n_bslots, int n_slots,
@@ -874,22 +932,27 @@ ffn_tc_kernel(const DevRow* __restrict__ rows, const Unit* units, const int32_t*
             sq += (uint32_t)ipa * W;
             ring_advance(rp, (uint32_t)ipa * W, (uint32_t)n_slots);
           } else {
-            // the group that dequantizes this tile, and the parity of this use of its operand slot
+            // the group that dequantizes this tile
             const uint32_t k = base + j;
             const uint32_t grp = NMAT == 2 ? 2u * (uint32_t)my_m + (k & 1u) : (k & 3u);
-            const uint32_t use_par = (upar >> grp) & 1u;
-            upar ^= 1u << grp;
             const uint32_t f0 = af_s + 8 * grp, e0 = ae_s + 8 * grp;       // barriers of the group's operand slot
             const uint32_t a_t = a_base + grp * 64;
-            ok = mbar_wait_s<LIM>(f0, use_par, c, status);
-            if (ok && after) ok = flag_wait<LIM>(turn_s, tord - npe, c, status);
+#pragma unroll 1
+            for (uint32_t part = 0; part < (EXACT ? 2u : 1u); ++part) {
+              const uint32_t use_par = (upar >> grp) & 1u;
+              upar ^= 1u << grp;
+              ok = mbar_wait_s<LIM>(f0, use_par, c, status);
+              if (ok && after && part == 0) ok = flag_wait<LIM>(turn_s, tord - npe, c, status);
+              if (!ok) break;
+              tc_fence_after();
+              // all eight k-steps of the tile (EXACT: four of a K-half, of both numbers), then one commit hands the group's
+              // operand slot back
+              tc_mma_ts_burst<4>(d_t, a_t, 8, b_lo + 4 * part * b_step, desc_hi, b_step, idesc, later | part, on);
+              tc_mma_ts_burst<4>(d_t, a_t + 32, 8, b_lo + (EXACT ? 4 * part : 4) * b_step, desc_hi, b_step, idesc, 1u, on);
+              if (part == (EXACT ? 1u : 0u)) release_turn(tord);
+              tc_commit_if_s(e0, on);
+            }
             if (!ok) break;
-            tc_fence_after();
-            // all eight k-steps of the tile, then one commit hands the group's operand slot back
-            tc_mma_ts_burst<4>(d_t, a_t, 8, b_lo, desc_hi, b_step, idesc, later, on);
-            tc_mma_ts_burst<4>(d_t, a_t + 32, 8, b_lo + 4 * b_step, desc_hi, b_step, idesc, 1u, on);
-            release_turn(tord);
-            tc_commit_if_s(e0, on);
           }
           tc_commit_if_s(be_s + 8 * bp.s, on);
           later = 1;
@@ -1117,7 +1180,7 @@ ffn_tc_kernel(const DevRow* __restrict__ rows, const Unit* units, const int32_t*
         st.par = rp.par;
         st.known = 0;                                // my items of this unit may be another producer's than before
 #define PW_DQ_RUN(UB) \
-  dq_run<UB, LIM>(st, count, step, (uint32_t)n_slots, wring_s, r, lane0, lane_addr, full_s, empty_s, a_full_s, a_empty_s, c, status)
+  dq_run<UB, LIM, EXACT>(st, count, step, (uint32_t)n_slots, wring_s, r, lane0, lane_addr, full_s, empty_s, a_full_s, a_empty_s, c, status)
         switch (bits) {
           case 8: ok = PW_DQ_RUN(8); break;
           case 4: ok = PW_DQ_RUN(4); break;
@@ -1263,6 +1326,14 @@ static FfnKernel ffn_kernel_of(int phase, int help, int planes, int share = 0) {
       ffn_tc_kernel<0, true, true, false>,   ffn_tc_kernel<1, true, true, false>};
   return tab[phase + 2 * help + 4 * planes];
 }
+// the down kernel for dense products
+static FfnKernel dense_kernel_of(int help, int planes, int share) {
+  static const FfnKernel shared[2] = {ffn_tc_kernel<1, false, false, false, true, true>, ffn_tc_kernel<1, false, true, false, true, true>};
+  if (share && !help) return shared[planes];
+  static const FfnKernel tab[4] = {ffn_tc_kernel<1, false, false, false, false, true>, ffn_tc_kernel<1, true, false, false, false, true>,
+                                   ffn_tc_kernel<1, false, true, false, false, true>, ffn_tc_kernel<1, true, true, false, false, true>};
+  return tab[help + 2 * planes];
+}
 // the gate/up kernel with the short wait limit (narrow token tiles, ordinary pages): what the failure-path test runs
 static FfnKernel ffn_kernel_short() { return ffn_tc_kernel<0, false, false, true>; }
 
@@ -1385,10 +1456,13 @@ pw_status launch_ffn_tensor(pw_ctx* ctx, int layer, int T, int k, int nt_tile, i
 // The down kernel on pages that are no layer's: a "segment" is a page, whose row tiles are numbered on from those of the
 // page before it.  The kernel ahead of it writes what the layer's call has from its routing: the operand in k-chunk-major
 // form, the page rows, the unit list (K range outermost, then row tile, then token tile), and completion counters that no
-// unit has to wait for.  The kernel behind it adds the K ranges up, adds the bias and rounds.  14336 x 4096 at 4 bits: 64
-// tokens 21.7 us (most of it the down kernel), 256 tokens 43.
+// unit has to wait for.  It also sums the operand over every group of 128 columns.  The down kernel multiplies code' * scale,
+// in two fp16 numbers (see decode_quarter_exact), and the kernel behind it adds the K ranges up, then the terms of the groups'
+// middles, (zero-point + 2^(bits - 1) * scale) * (sum of the group's operand), and the bias, and rounds.  14336 x 4096 at 4
+// bits: 64 tokens 32 us (the down kernel 24), 256 tokens 72; with weights rounded to fp16 it was 21.7 and 43, and outputs of
+// fp16 were 2.8e-4 of their norm from the definition, where their own rounding is 2.1e-4.
 struct DenseWs {
-  size_t rows, units, done, counters, xt, y, total;
+  size_t rows, units, done, counters, xt, xsum, y, total;
 };
 static DenseWs dense_ws(const DenseCall& d) {
   DenseWs w{};
@@ -1402,6 +1476,7 @@ static DenseWs dense_ws(const DenseCall& d) {
   w.done = take(4 * (size_t)d.T * d.splits);
   w.counters = take(256);
   w.xt = take((size_t)d.cols * 2 * d.Rpad);
+  w.xsum = take((size_t)(d.cols / kGroup) * 4 * d.T);
   w.y = take(4 * (size_t)d.splits * d.T * d.width);
   return w;
 }
@@ -1432,9 +1507,18 @@ size_t dense_plan(DenseCall* d, int sms) {
   return dense_ws(*d).total;
 }
 
+// Eight operand columns of which `left` bytes count.
+__device__ __forceinline__ uint4 operand_chunk(const char* src, int left) {
+  if (left >= 16) return *reinterpret_cast<const uint4*>(src);
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < 7; ++k)
+    if (k < left / 2) w[k >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[k] << (16 * (k & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 __global__ void __launch_bounds__(256) dense_prepare_kernel(const __grid_constant__ DenseCall d, const char* x, size_t x_pitch, int x_bytes, DevRow* __restrict__ rows,
                                                             Unit* __restrict__ units, int32_t* __restrict__ done, int32_t* __restrict__ counters,
-                                                            uint4* __restrict__ xt) {
+                                                            uint4* __restrict__ xt, float* __restrict__ xsum) {
   grid_dep_sync();
   const int threads = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + threadIdx.x;
   const int ng = d.cols / kGroup, row_tiles = d.width / kTileRows;
@@ -1474,59 +1558,166 @@ __global__ void __launch_bounds__(256) dense_prepare_kernel(const __grid_constan
   const int64_t chunks = (int64_t)(d.cols / 8) * d.Rpad;
   for (int64_t i = first; i < chunks; i += threads) {
     const int c = (int)(i / d.Rpad), n = (int)(i - (int64_t)c * d.Rpad);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (n < d.T) {
-      const char* src = x + (size_t)n * x_pitch + (size_t)c * 16;
-      const int left = x_bytes - c * 16;
-      if (left >= 16) {
-        v = *reinterpret_cast<const uint4*>(src);
-      } else if (left > 0) {
-        uint32_t w[4] = {0, 0, 0, 0};
-        for (int k = 0; k < left / 2; ++k) w[k >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[k] << (16 * (k & 1));
-        v = make_uint4(w[0], w[1], w[2], w[3]);
+    const char* src = x + (size_t)n * x_pitch + (size_t)c * 16;
+    xt[i] = n < d.T ? operand_chunk(src, x_bytes - c * 16) : make_uint4(0, 0, 0, 0);
+  }
+  // sums of a group's columns, by 16 lanes
+  const int64_t pieces = (int64_t)d.T * ng * 16;
+  for (int64_t i = first; i < (pieces + 31) / 32 * 32; i += threads) {
+    const int lane = (int)(i & 15), g = (int)((i >> 4) % ng);
+    const int64_t t = (i >> 4) / ng;
+    float v = 0.f;
+    if (i < pieces) {
+      const uint4 q = operand_chunk(x + (size_t)t * x_pitch + (size_t)g * 256 + lane * 16, x_bytes - g * 256 - lane * 16);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = __half22float2(u32_as_h2(w[j]));
+        v += f.x + f.y;
       }
     }
-    xt[i] = v;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (i < pieces && lane == 0) xsum[t * ng + g] = v;
   }
 }
 
-// out[t, column] = sum of the parts of the contraction, in their order (+ bias), rounded once.
-__global__ void __launch_bounds__(128) dense_finish_kernel(const __grid_constant__ DenseCall d, const float* y, const void* bias, int bias_type, void* __restrict__ out,
-                                                           int out_type, int64_t ld_out) {
-  grid_dep_sync();
-  grid_dep_trigger();
+// out[t, column] = sum of the parts of the contraction, in their order, + the terms of the groups' middles (+ bias), rounded
+// once.  A block has the 128 columns of a row tile and TOKENS tokens.  The middles and the operand's sums of 32 groups at a
+// time go through shared memory, so that their loads are in flight together (read straight by a thread of eight columns and
+// four tokens, two groups at a time, the call took 51 us for 64 tokens x 14336 x 4096, and takes 32); a thread has four columns and four
+// tokens, and every (32 / TOKENS)-th group where the block has fewer tokens: their sums then meet in shared memory.  With 32
+// tokens a middle is made a quarter as often, with 8 there are four times the blocks: see launch_dense.
+constexpr int kFinishGroups = 32;
+template <int TOKENS>
+__global__ void __launch_bounds__(256) dense_finish_kernel(const __grid_constant__ DenseCall d, const float* y, const float* xsum, const void* bias, int bias_type,
+                                                           void* __restrict__ out, int out_type, int64_t ld_out) {
+  constexpr int kShares = 32 / TOKENS;             // of the groups
+  __shared__ __align__(16) float mid[kFinishGroups][kTileRows], xs[kFinishGroups][TOKENS + 4];
   const size_t stride = (size_t)d.T * d.width / 4;
-  const int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 8;   // eight columns, of one page: each starts at a tile of 128
-  if (c >= d.width) return;
-  int page = 0, col0 = 0, pad0 = 0;                // first column of the page, in the output and in y
+  const int tid = threadIdx.x, warp = tid >> 5, col = (tid & 31) * 4, tok = warp % (TOKENS / 4) * 4, share = warp / (TOKENS / 4);
+  int page = 0, col0 = 0, tile0 = 0;               // first column and row tile of the page
   while (true) {
-    const int wide = (d.features[page] + kTileRows - 1) / kTileRows * kTileRows;
-    if (c < pad0 + wide) break;
-    pad0 += wide;
+    const int tiles = (d.features[page] + kTileRows - 1) / kTileRows;
+    if ((int)blockIdx.x < tile0 + tiles) break;
+    tile0 += tiles;
     col0 += d.features[page++];
   }
-  const int n = min(8, d.features[page] - (c - pad0)), to = col0 + c - pad0;
-  if (n <= 0) return;
-  for (int t = blockIdx.y; t < d.T; t += gridDim.y) {
-    const float4* from = reinterpret_cast<const float4*>(y + (size_t)t * d.width + c);
-    float4 lo = from[0], hi = from[1];
+  const int row_tile = (int)blockIdx.x - tile0;
+  const int n = min(4, d.features[page] - row_tile * kTileRows - col), to = col0 + row_tile * kTileRows + col;   // n < 1: columns of the padding
+  // the row tile's scales in the first of its page tiles; the zero-points stand 256 bytes on
+  const pw_page& p = d.page[page];
+  const bool planes = p.layout == PW_LAYOUT_PLANES;
+  const int ng = d.cols / kGroup, groups = p.bits == 16 ? 0 : ng;
+  const size_t tile = planes ? (size_t)kPlaneTopTile : tile_bytes(p.bits);
+  const char* scales = static_cast<const char*>(p.codes) + (size_t)row_tile * ng * tile + (planes ? (size_t)plane_lut_offset(p.bits) : tile_scale_offset(p.bits, 0));
+  const float middle = (float)(1 << (p.bits - 1));
+  auto put = [&](int t, const float (&v)[4]) {     // v: the terms of the middles
+    if (t >= d.T || n < 1) return;
+    const float4* from = reinterpret_cast<const float4*>(y + (size_t)t * d.width + (size_t)blockIdx.x * kTileRows + col);
+    float4 a = from[0];
     for (int s = 1; s < d.splits; ++s) {
-      const float4 l = from[s * stride], h = from[s * stride + 1];
-      lo.x = __fadd_rn(lo.x, l.x), lo.y = __fadd_rn(lo.y, l.y), lo.z = __fadd_rn(lo.z, l.z), lo.w = __fadd_rn(lo.w, l.w);
-      hi.x = __fadd_rn(hi.x, h.x), hi.y = __fadd_rn(hi.y, h.y), hi.z = __fadd_rn(hi.z, h.z), hi.w = __fadd_rn(hi.w, h.w);
+      const float4 b = from[s * stride];
+      a.x = __fadd_rn(a.x, b.x), a.y = __fadd_rn(a.y, b.y), a.z = __fadd_rn(a.z, b.z), a.w = __fadd_rn(a.w, b.w);
     }
-    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    float o[4] = {__fadd_rn(a.x, v[0]), __fadd_rn(a.y, v[1]), __fadd_rn(a.z, v[2]), __fadd_rn(a.w, v[3])};
     if (bias)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) v[i] = __fadd_rn(v[i], load1(bias, to + i, bias_type));
+      for (int i = 0; i < 4; ++i)
+        if (i < n) o[i] = __fadd_rn(o[i], load1(bias, to + i, bias_type));
     const int64_t at = (int64_t)t * ld_out + to;
-    if (n == 8 && at % 8 == 0) {
-      store8(out, at, out_type, v);
+    if (n == 4 && at % 4 == 0) {                   // (the type is a 16-bit one)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
+          out_type == PW_F16 ? make_uint2(pack_half(o[0], o[1]), pack_half(o[2], o[3])) : make_uint2(pack_bf(o[0], o[1]), pack_bf(o[2], o[3]));
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) store1(out, at + i, out_type, v[i]);
+      for (int i = 0; i < 4; ++i)
+        if (i < n) store1(out, at + i, out_type, o[i]);
+    }
+  };
+  // The kernel directly ahead is the down kernel, which was launched when the one ahead of it, and with it all that came
+  // before the call, had finished: pages and the operand's sums are there, its own results are not.
+  bool waited = false;
+  for (int t0 = blockIdx.y * TOKENS; t0 < d.T; t0 += gridDim.y * TOKENS) {
+    float v[4][4] = {};                            // [token][column]
+    uint4 s[2], z[2];                              // a thread's part of the next groups, on its way
+    float x[TOKENS / 8];
+    auto ask = [&](int g0) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int i = tid + 256 * k, g = g0 + (i >> 4);
+        if (g < groups) {
+          const uint4* from = reinterpret_cast<const uint4*>(scales + (size_t)g * tile + (i & 15) * 16);
+          s[k] = from[0], z[k] = from[16];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < TOKENS / 8; ++k) {
+        const int t = t0 + warp + 8 * k, g = g0 + (tid & 31);
+        x[k] = t < d.T && g < groups ? xsum[(size_t)t * ng + g] : 0.f;
+      }
+    };
+    ask(0);
+    for (int g0 = 0; g0 < groups; g0 += kFinishGroups) {
+      const int some = min(kFinishGroups, groups - g0);
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int i = tid + 256 * k;
+        const uint32_t sw[4] = {s[k].x, s[k].y, s[k].z, s[k].w}, zw[4] = {z[k].x, z[k].y, z[k].z, z[k].w};
+        float m[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 a = __half22float2(u32_as_h2(sw[j])), b = __half22float2(u32_as_h2(zw[j]));
+          m[2 * j] = fmaf(a.x, middle, b.x);
+          m[2 * j + 1] = fmaf(a.y, middle, b.y);
+        }
+        if ((i >> 4) < some) {
+          float4* at = reinterpret_cast<float4*>(&mid[i >> 4][(i & 15) * 8]);
+          at[0] = make_float4(m[0], m[1], m[2], m[3]);
+          at[1] = make_float4(m[4], m[5], m[6], m[7]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < TOKENS / 8; ++k) xs[tid & 31][warp + 8 * k] = x[k];
+      __syncthreads();
+      if (g0 + kFinishGroups < groups) ask(g0 + kFinishGroups);
+#pragma unroll 4
+      for (int g = share; g < some; g += kShares) {
+        const float4 m = *reinterpret_cast<const float4*>(&mid[g][col]), x = *reinterpret_cast<const float4*>(&xs[g][tok]);
+        const float xv[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[j][0] = fmaf(m.x, xv[j], v[j][0]);
+          v[j][1] = fmaf(m.y, xv[j], v[j][1]);
+          v[j][2] = fmaf(m.z, xv[j], v[j][2]);
+          v[j][3] = fmaf(m.w, xv[j], v[j][3]);
+        }
+      }
+    }
+    if constexpr (kShares > 1) {                   // mid, anew: [share][token][column]
+      static_assert(32 / TOKENS * TOKENS <= kFinishGroups && TOKENS <= 8, "room, a token per warp");
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(&mid[share * TOKENS + tok + j][col]) = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
+      __syncthreads();
+    }
+    if (!waited) {
+      grid_dep_sync();
+      grid_dep_trigger();
+      waited = true;
+    }
+    if constexpr (kShares > 1) {
+      float sum[4] = {};
+#pragma unroll
+      for (int k = 0; k < kShares; ++k) {
+        const float4 a = *reinterpret_cast<const float4*>(&mid[k * TOKENS + warp][col]);
+        sum[0] = __fadd_rn(sum[0], a.x), sum[1] = __fadd_rn(sum[1], a.y), sum[2] = __fadd_rn(sum[2], a.z), sum[3] = __fadd_rn(sum[3], a.w);
+      }
+      if (warp < TOKENS) put(t0 + warp, sum);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) put(t0 + tok + j, v[j]);
     }
   }
 }
@@ -1539,8 +1730,8 @@ pw_status launch_dense(pw_ctx* ctx, const DenseCall& d, const void* x, size_t x_
     PW_CUDA_OK(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
     if (!fn || found != cudaDriverEntryPointSuccess) return PW_ERR_CUDA;
     for (int i = 0; i < 4; ++i) {
-      PW_CUDA_OK(cudaFuncSetAttribute(ffn_kernel_of(1, i & 1, i >> 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
-      PW_CUDA_OK(cudaFuncSetAttribute(ffn_kernel_of(1, 0, i >> 1, 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
+      PW_CUDA_OK(cudaFuncSetAttribute(dense_kernel_of(i & 1, i >> 1, 0), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
+      PW_CUDA_OK(cudaFuncSetAttribute(dense_kernel_of(0, i >> 1, 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
     }
     ctx->dense_encode.store(fn, std::memory_order_release);
   }
@@ -1560,16 +1751,20 @@ pw_status launch_dense(pw_ctx* ctx, const DenseCall& d, const void* x, size_t x_
   const int most = 8 * ctx->num_sms;
   PW_CUDA_OK(launch_dependent(dense_prepare_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, d, static_cast<const char*>(x), x_pitch,
                               x_bytes, reinterpret_cast<DevRow*>(b + w.rows), reinterpret_cast<Unit*>(b + w.units), reinterpret_cast<int32_t*>(b + w.done), counters,
-                              reinterpret_cast<uint4*>(b + w.xt)));
+                              reinterpret_cast<uint4*>(b + w.xt), reinterpret_cast<float*>(b + w.xsum)));
   // (launched without overlap: what the kernel reads of its list and counters before it waits for anything is the work of
   // the kernel directly ahead)
-  ffn_kernel_of(1, help, planes, share)<<<dim3(ctx->num_sms), dim3(kThreads), (size_t)smem, s>>>(
+  dense_kernel_of(help, planes, share)<<<dim3(ctx->num_sms), dim3(kThreads), (size_t)smem, s>>>(
       reinterpret_cast<const DevRow*>(b + w.rows), reinterpret_cast<const Unit*>(b + w.units), counters + 2, maps, d.Rpad, d.nt_tile, n_bslots, n_slots,
       (__half*)nullptr, reinterpret_cast<float*>(b + w.y), d.width, (size_t)d.T * d.width, counters, status, reinterpret_cast<int32_t*>(b + w.done), d.splits,
       d.cols / kTileRows, 0u);
   PW_CUDA_OK(cudaGetLastError());
-  PW_CUDA_OK(launch_dependent(dense_finish_kernel, dim3((d.width + 1023) / 1024, d.T < 4096 ? d.T : 4096), dim3(128), 0, s, d, reinterpret_cast<const float*>(b + w.y), bias,
-                              bias_type, out, out_type, ld_out));
+  // 32 tokens to a block where that gives every SM one (70 tokens x 1128 x 14336 at 8 bits: 25.5 us with 32, 21.5
+  // with 8; 33 tokens x 4500 x 8192 28.5 and 22.3; 32 tokens x 4096 x 14336 29.2 and 31.5)
+  const int tiles = d.width / kTileRows, wide = (d.T + 31) / 32, narrow = (d.T + 7) / 8;
+  const bool few = (int64_t)tiles * wide < ctx->num_sms;
+  PW_CUDA_OK(launch_dependent(few ? dense_finish_kernel<8> : dense_finish_kernel<32>, dim3(tiles, few ? narrow : wide < 65535 ? wide : 65535), dim3(256), 0, s, d,
+                              reinterpret_cast<const float*>(b + w.y), reinterpret_cast<const float*>(b + w.xsum), bias, bias_type, out, out_type, ld_out));
   ctx->launches += 3;
   return PW_OK;
 }

@@ -185,15 +185,22 @@ __device__ inline void pack_slice(const int (&code)[32], uint32_t* w) {
 // code -> fp16 via the 0x6400 (= 1024.0) mantissa trick, then one HFMA2 with (scale, zero-point).
 __device__ inline __half2 u32_as_h2(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
 
-__device__ inline __half2 dq_pair(uint32_t magic_or_code, __half2 s2, __half2 z2) {
-  const __half2 k1024 = u32_as_h2(0x64006400u);
-  return __hfma2(__hsub2(u32_as_h2(magic_or_code), k1024), s2, z2);
-}
-
-// the same with the bias to subtract given as a half2 bit pattern (the constant whose mantissa carried the code)
-__device__ inline __half2 dq_pair_k(uint32_t biased, uint32_t bias, __half2 s2, __half2 z2) {
-  return __hfma2(__hsub2(u32_as_h2(biased), u32_as_h2(bias)), s2, z2);
-}
+// What becomes of a pair of codes; the bias to subtract is given as a half2 bit pattern (the constant whose mantissa carried
+// the code).  The weights:
+struct Weights {
+  __half2 s2, z2;
+  __device__ __forceinline__ __half2 operator()(uint32_t biased, uint32_t bias) const {
+    return __hfma2(__hsub2(u32_as_h2(biased), u32_as_h2(bias)), s2, z2);
+  }
+};
+// ... or code - 2^(BITS - 1): the middle goes into the constant, at the place where the code's last bit is (see field_magic)
+template <int BITS>
+struct CentredCodes {
+  __device__ __forceinline__ __half2 operator()(uint32_t biased, uint32_t bias) const {
+    const uint32_t pos = 25u - ((bias >> 10) & 31u);
+    return __hsub2(u32_as_h2(biased), u32_as_h2(bias | ((1u << (BITS - 1)) << pos) * 0x00010001u));
+  }
+};
 
 // (a & b) | c as ONE instruction.  Written out because the compiler, given two immediates, emits an AND and an
 // OR; with the constants in registers the three-input logic unit does both.
@@ -209,21 +216,21 @@ __device__ __forceinline__ constexpr uint32_t field_magic() {
   return (uint32_t)((25 - POS) << 10) * 0x00010001u;
 }
 // The pair of W-bit fields at bit POS of the two half-words of `word` -> (field * scale + zero-point) as half2.
-template <int POS, int W>
-__device__ __forceinline__ __half2 dq_field(uint32_t word, __half2 s2, __half2 z2) {
+template <int POS, int W, class Q>
+__device__ __forceinline__ __half2 dq_field(uint32_t word, const Q& q) {
   constexpr uint32_t mask = (((1u << W) - 1u) << POS) * 0x00010001u;
   constexpr uint32_t magic = field_magic<POS>();
-  return dq_pair_k(and_or(word, mask, magic), magic, s2, z2);
+  return q(and_or(word, mask, magic), magic);
 }
 // The same for a 2-bit field, with (BITS == 3) the code's third bit, already moved to bit POS + 2 of `hi`, put just
 // above it.
-template <int POS, int BITS>
-__device__ __forceinline__ __half2 dq_field23(uint32_t word, uint32_t hi, __half2 s2, __half2 z2) {
+template <int POS, int BITS, class Q>
+__device__ __forceinline__ __half2 dq_field23(uint32_t word, uint32_t hi, const Q& q) {
   constexpr uint32_t mask = (3u << POS) * 0x00010001u;
   constexpr uint32_t magic = field_magic<POS>();
   uint32_t v = and_or(word, mask, magic);
   if constexpr (BITS == 3) v = and_or(hi, (1u << (POS + 2)) * 0x00010001u, v);
-  return dq_pair_k(v, magic, s2, z2);
+  return q(v, magic);
 }
 
 // Quarter t (0 .. 3) of a row-group: out[p] = weights (32t + 2p, 32t + 2p + 1), p = 0 .. 15.
@@ -231,8 +238,8 @@ __device__ __forceinline__ __half2 dq_field23(uint32_t word, uint32_t hi, __half
 // of the same row is kUnitStride uint4 further on.
 constexpr int kUnitStride = 128;  // uint4 elements between consecutive units of one row
 
-template <int BITS>
-__device__ __forceinline__ void decode_quarter(const uint4* row_units, int t, __half2 s2, __half2 z2, __half2* out) {
+template <int BITS, class Q>
+__device__ __forceinline__ void decode_quarter(const uint4* row_units, int t, const Q& q, __half2* out) {
   if constexpr (BITS == 16) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -249,8 +256,8 @@ __device__ __forceinline__ void decode_quarter(const uint4* row_units, int t, __
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        out[8 * j + 2 * i] = dq_pair(__byte_perm(w[i], 0x64646464u, 0x4140), s2, z2);
-        out[8 * j + 2 * i + 1] = dq_pair(__byte_perm(w[i], 0x64646464u, 0x4342), s2, z2);
+        out[8 * j + 2 * i] = q(__byte_perm(w[i], 0x64646464u, 0x4140), 0x64006400u);
+        out[8 * j + 2 * i + 1] = q(__byte_perm(w[i], 0x64646464u, 0x4342), 0x64006400u);
       }
     }
   } else if constexpr (BITS == 4) {
@@ -261,10 +268,10 @@ __device__ __forceinline__ void decode_quarter(const uint4* row_units, int t, __
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t w8 = w[i] >> 8;
-      out[4 * i + 0] = dq_field<0, 4>(w[i], s2, z2);
-      out[4 * i + 1] = dq_field<4, 4>(w[i], s2, z2);
-      out[4 * i + 2] = dq_field<0, 4>(w8, s2, z2);
-      out[4 * i + 3] = dq_field<4, 4>(w8, s2, z2);
+      out[4 * i + 0] = dq_field<0, 4>(w[i], q);
+      out[4 * i + 1] = dq_field<4, 4>(w[i], q);
+      out[4 * i + 2] = dq_field<0, 4>(w8, q);
+      out[4 * i + 3] = dq_field<4, 4>(w8, q);
     }
   } else {
     // 2 bits: words 2(t%2), 2(t%2)+1 of unit t/2.  3 bits: the same low-plane words plus word t of unit 2.
@@ -287,10 +294,10 @@ __device__ __forceinline__ void decode_quarter(const uint4* row_units, int t, __
         const int p = 8 * i + m;                   // pair index inside the quarter
         const uint32_t src = m < 4 ? w[i] : w8, hi = m < 4 ? ha : hb;
         switch (m & 3) {
-          case 0: out[p] = dq_field23<0, BITS>(src, hi, s2, z2); break;
-          case 1: out[p] = dq_field23<2, BITS>(src, hi, s2, z2); break;
-          case 2: out[p] = dq_field23<4, BITS>(src, hi, s2, z2); break;
-          default: out[p] = dq_field23<6, BITS>(src, hi, s2, z2); break;
+          case 0: out[p] = dq_field23<0, BITS>(src, hi, q); break;
+          case 1: out[p] = dq_field23<2, BITS>(src, hi, q); break;
+          case 2: out[p] = dq_field23<4, BITS>(src, hi, q); break;
+          default: out[p] = dq_field23<6, BITS>(src, hi, q); break;
         }
       }
     }
@@ -300,8 +307,8 @@ __device__ __forceinline__ void decode_quarter(const uint4* row_units, int t, __
 // Half h (0 or 1) of a row-group: out[p] = weights (64h + 2p, 64h + 2p + 1), p = 0 .. 31.
 template <int BITS>
 __device__ __forceinline__ void decode_half(const uint4* row_units, int h, __half2 s2, __half2 z2, __half2* out) {
-  decode_quarter<BITS>(row_units, 2 * h, s2, z2, out);
-  decode_quarter<BITS>(row_units, 2 * h + 1, s2, z2, out + 16);
+  decode_quarter<BITS>(row_units, 2 * h, Weights{s2, z2}, out);
+  decode_quarter<BITS>(row_units, 2 * h + 1, Weights{s2, z2}, out + 16);
 }
 
 // ---- overlaid bit-plane pages (PW_LAYOUT_PLANES) -----------------------------------------------
@@ -331,8 +338,8 @@ constexpr int kPlaneSlotBytes = kPlaneSlotLut + 512;
 
 // Quarter t of a row-group read from such an image at Q = 3 or 4 bits (Q = 2 is the plain 2-bit decoder on the
 // top codes): out[p] = weights (32t + 2p, 32t + 2p + 1).
-template <int Q>
-__device__ __forceinline__ void decode_quarter_planes(const char* image, int r, int t, __half2 s2, __half2 z2, __half2* out) {
+template <int Q, class P>
+__device__ __forceinline__ void decode_quarter_planes(const char* image, int r, int t, const P& pair, __half2* out) {
   const uint4* row_units = reinterpret_cast<const uint4*>(image) + r;
   const uint2 u = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint32_t*>(row_units + (t >> 1) * kUnitStride) +
                                                    2 * (t & 1));
@@ -365,7 +372,7 @@ __device__ __forceinline__ void decode_quarter_planes(const char* image, int r, 
       const uint32_t magic = (uint32_t)((25 - U) << 10) * 0x00010001u;
       uint32_t v = and_or(m < 4 ? lo4 : hi4, (3u << (U + up)) * 0x00010001u, magic);
       v = and_or(m < 4 ? a1 : b1, (Q == 4 ? 3u << U : 1u << U) * 0x00010001u, v);
-      out[p] = dq_pair_k(v, magic, s2, z2);
+      out[p] = pair(v, magic);
     }
   }
 }
@@ -374,8 +381,8 @@ __device__ __forceinline__ void decode_half_planes(const char* image, int r, int
   if constexpr (Q == 2) {
     decode_half<2>(reinterpret_cast<const uint4*>(image) + r, h, s2, z2, out);
   } else {
-    decode_quarter_planes<Q>(image, r, 2 * h, s2, z2, out);
-    decode_quarter_planes<Q>(image, r, 2 * h + 1, s2, z2, out + 16);
+    decode_quarter_planes<Q>(image, r, 2 * h, Weights{s2, z2}, out);
+    decode_quarter_planes<Q>(image, r, 2 * h + 1, Weights{s2, z2}, out + 16);
   }
 }
 

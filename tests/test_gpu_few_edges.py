@@ -176,3 +176,69 @@ def test_few_outputs_are_a_neighbour_of_the_rounded_definition(mixed, T, dtype, 
     want, _ = layer_of_two(f64(x), mixed.blocks, all_pairs(mixed, l, 3))
     moved = torch.from_numpy(want).to(dtype).cuda() != out
     assert float(moved.double().mean()) <= share
+
+
+# ---- products of many tokens -----------------------------------------------------------------------
+
+def centred_product(x, block, bits):
+    """(x . w^T, bound) where code - 2^(bits - 1), times the scale in two fp16 numbers, is multiplied, and the rest of the
+    weight with the sum of a group's operand.
+
+    Twice K / 16 accumulations of at most two half steps, K / 128 groups, and the joins of plain_few.product."""
+    c, s, z = (m[:, :x.shape[1]] for m in block)
+    middle = 2.0 ** (bits - 1) if bits < 16 else 0.0
+    size = np.abs(x) @ (np.abs((c - middle) * s) + np.abs(z) + middle * np.abs(s)).T
+    return x @ (c * s + z).T, size * (x.shape[1] / 4 + x.shape[1] / 128 + 64) * 2.0 ** -24
+
+
+def many_tokens(ctx, x, pages, sizes, dtype):
+    launches = ctx.pw_launch_count()
+    out = ctx.pw_page_linear(x, pages, out_features=sizes, out_dtype=dtype)
+    assert ctx.pw_launch_count() - launches == 3 and ctx.pw_last_device_status() == 0
+    return out
+
+
+@pytest.mark.parametrize("T,K,sizes,formats", [(64, 4096, [6000], ["2"]), (33, 8192, [2500, 2000], ["4", "4"]), (130, 2050, [3129, 64], ["3", "4"]),
+                                               (70, 14336, [1128], ["8"]), (600, 1000, [1260], ["p4"]), (12000, 640, [100], ["p2"]),
+                                               (2000, 900, [700, 33], ["p3", "16"]), (64, 4096, [6000], ["4"])])
+@pytest.mark.parametrize("dtype,share", [(F16, 0.02), (BF16, 0.005)])
+def test_many_tokens_round_nothing_but_the_output(ctx, T, K, sizes, formats, dtype, share):
+    """Weights are not rounded to fp16: see test_few_outputs_are_a_neighbour_of_the_rounded_definition for the share."""
+    g = gen(T + K)
+    pages = [plain.make_page(ctx, block_weights(g, n, K), f) for n, f in zip(sizes, formats)]
+    x = operand(g, T, K, pitch=up(K))
+    out = many_tokens(ctx, x, pages, sizes, dtype)
+    parts = [centred_product(f64(x), [m[:n] for m in plain.stored(ctx, p)], p.bits) for n, p in zip(sizes, pages)]
+    want, bound = (np.concatenate([p[i] for p in parts], 1) for i in (0, 1))
+    check(out, want, bound, dtype)
+    moved = torch.from_numpy(want).to(dtype).cuda() != out
+    assert float(moved.double().mean()) <= share
+
+
+@pytest.mark.parametrize("fmt", ["8", "4", "3", "2", "p4", "p3", "p2"])
+def test_extreme_groups_of_many_tokens(ctx, fmt):
+    """Groups that span nearly all of fp16's range, its subnormals, one value, zeros; operands at both ends; tokens that are not
+    finite."""
+    T, K, N = 2000, 600, 1500
+    g = gen(17)
+    w = normal(g, up(N), up(K))
+    w[:, :128] *= 65000.0 / w[:, :128].abs().amax(1, keepdim=True)
+    w[:, 100] = 65504.0
+    w[:, 101] = -65504.0
+    w[:, 128:256] *= 2.0 ** -18
+    w[:, 256:384] = 0.75
+    w[:, 384:512] = 0
+    page = plain.make_page(ctx, w.half(), fmt)
+    x = operand(g, T, K, pitch=up(K))
+    x[0] *= 2.0 ** -20
+    x[1] *= 60000.0 / x[1].abs().max()
+    x[2] = 0
+    x[3:40, :128] = 0                              # the other groups show
+    out = many_tokens(ctx, x, [page], [N], BF16)
+    check(out, *centred_product(f64(x), [m[:N] for m in plain.stored(ctx, page)], page.bits), BF16)
+    assert torch.all(out[2] == 0)
+    y = x.clone()
+    y[50, 77], y[60, 300] = float("nan"), float("-inf")
+    odd = many_tokens(ctx, y, [page], [N], BF16)
+    rest = [t for t in range(T) if t not in (50, 60)]
+    assert torch.equal(odd[rest], out[rest]) and not torch.isfinite(odd[[50, 60]]).any()
