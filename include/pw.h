@@ -332,7 +332,8 @@ pw_status pw_moe_forward_routed(pw_ctx* ctx, int layer, const void* hidden_fp16,
  * All CTAs of the kernel run at the same time (a cooperative launch): on a device that other kernels keep busy it starts
  * when they leave room for one CTA per SM.  Works in the context's workspace, like pw_moe_forward, and is ordered with
  * its calls; pw_get_routing and pw_kernel_timing do not see this call.
- * A device-side wait that runs out is reported by pw_last_device_status.
+ * A device-side wait that runs out (a CTA waits about 3 s for the others) is reported by pw_last_device_status; the call's
+ * output is then undefined, later ones of these calls are not touched by it.
  * Errors: as pw_moe_forward, and INVALID_ARG (T > PW_FEW_TOKENS, out_type), SHAPE (no room). */
 #define PW_FEW_TOKENS 16
 pw_status pw_moe_forward_few(pw_ctx* ctx, int layer, const void* hidden_fp16, const float* router_logits, int T, int top_k,
@@ -651,11 +652,12 @@ uint64_t pw_launch_count(pw_ctx* ctx);
  * wait of those kernels is bounded, by 100000 polls of up to 20 us each (2 s).  The limit is compiled into the
  * kernels (carried in a register it cost the decode step 5 %), so `polls` only chooses: 0 = that default;
  * any other value = the gate/up kernel (narrow token tiles, ordinary pages) runs an instantiation whose limit
- * is 200 polls (4 ms).
+ * is 200 polls (4 ms), and the layer for few tokens waits about as long for its CTAs.
  * When a wait runs out the CTA records PW_ERR_TIMEOUT in the status word, stops issuing work, frees its tensor
  * memory and returns; the call's output is then undefined and pw_last_device_status reports the timeout.
  * hook: 0 = none; bit 0 = the token-tile producer of the gate/up kernel stops before its second tile, so that
- * the waits on that tile run out -- the one safe way to exercise the path (nothing faults, traps or spins
+ * the waits on that tile run out, and the last CTA of the layer for few tokens comes to the meeting of all CTAs when its
+ * own wait there has run out -- the one safe way to exercise the path (nothing faults, traps or spins
  * without a limit).  Applies to forward calls enqueued after it.  Errors: INVALID_ARG. */
 pw_status pw_debug_set_wait(pw_ctx* ctx, uint32_t polls, uint32_t hook);
 

@@ -790,5 +790,6 @@ class Context:
         return int(self.L.pw_launch_count(self.handle))
 
     def pw_debug_set_wait(self, polls: int = 0, hook: int = 0) -> None:
-        """Wait limit of the gate/up FFN kernel (0 = the default 2 s, else the 4 ms test build) and test hooks."""
+        """Wait limit of the gate/up FFN kernel and of the layer for few tokens (0 = the default, 2 and 3 s, else 4 ms) and
+        test hooks."""
         _check(self.L.pw_debug_set_wait(self.handle, polls, hook), "pw_debug_set_wait")

@@ -385,10 +385,7 @@ extern "C" pw_status pw_last_device_status(pw_ctx* ctx) {
   int32_t v = 0;
   PW_CUDA_OK(cudaDeviceSynchronize());
   PW_CUDA_OK(cudaMemcpy(&v, ctx->base + ctx->ws.status, 4, cudaMemcpyDeviceToHost));
-  if (v != 0) {
-    PW_CUDA_OK(cudaMemset(ctx->base + ctx->ws.status, 0, 4));
-    if (v == PW_ERR_TIMEOUT) PW_CUDA_OK(cudaMemset(ctx->base + ctx->ws.few_sync, 0, ctx->ws.few_seen - ctx->ws.few_sync));
-  }
+  if (v != 0) PW_CUDA_OK(cudaMemset(ctx->base + ctx->ws.status, 0, 4));
   return (pw_status)v;
 }
 

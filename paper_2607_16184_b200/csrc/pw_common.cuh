@@ -65,7 +65,7 @@ struct WsMap {
   size_t io_logits;   // float [Tmax][E]
   size_t io_out;      // float [Tmax][H]
   size_t obs_part;    // float [kNormSplit][2][Rpad]  partial squared norms of the operand rows (observation taps)
-  size_t few_sync;    // int32[64 + hidden / 32]  layer for few tokens: meeting of its CTAs, finished parts of the output (zeros between calls)
+  size_t few_sync;    // int32[64 + hidden / 32]  layer for few tokens: meeting of its CTAs, finished parts of the output
   size_t few_seen;    // int32[]       its active experts and pairs, for the observation taps
   size_t few_h;       // fp16 [pairs of PW_FEW_TOKENS tokens][2 numbers][F]  its SwiGLU output, in pieces
   size_t total;

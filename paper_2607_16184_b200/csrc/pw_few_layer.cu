@@ -36,7 +36,8 @@ constexpr int kFewRouters = 8;                    // warps that route (2 / 4 / 8
 // 28.8 / 28.9 / 31.1 us, four 40.2 / 39.5 / 41.2)
 constexpr size_t kFewAhead = 16 << 20;
 constexpr uint32_t kFewAheadPiece = 4096;
-constexpr uint32_t kFewPolls = 1u << 22;          // about 3 s
+constexpr uint32_t kFewPolls = 1u << 22;          // of the meeting's counter: about 3 s
+constexpr uint32_t kFewPollsTest = 6400;          // about 4 ms, for the test of a wait that runs out (pw_debug_set_wait)
 
 struct FewArgs {
   const DevRow* rows;                             // of the layer
@@ -48,6 +49,7 @@ struct FewArgs {
   char* h;                                        // [pair][kHalves][F] pieces
   float* parts;                                   // [part][T][H]
   int32_t* sync;                                  // arrivals; from 64 on: finished parts of every 32 output rows
+  uint32_t polls, hook;                           // limit of the wait; test hook: the last CTA arrives when its own wait has run out
   int32_t* status;
   int32_t* seen;                                  // for the observation taps (or null): see few_observe_kernel
   int T, k, E, n_shared, H, F, out_type;
@@ -280,6 +282,10 @@ __device__ __forceinline__ void make_tables(const FewArgs& p, TAB& t, const DevR
   }
 }
 
+__device__ __forceinline__ void few_arrive(int32_t* sync, int b, int G) {
+  asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
+}
+
 template <class TAB, int XC, int STAGES>
 __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __grid_constant__ FewArgs p) {
   extern __shared__ __align__(128) char smem[];
@@ -363,6 +369,10 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
 
   const Fixed fixed;
   const int G = (int)gridDim.x, b = (int)blockIdx.x;
+  if (p.n_parts > 1) {                            // counted from the meeting on: whatever a call before this one has left
+#pragma unroll 1
+    for (int i = b * kStreamThreads + tid; i < p.H / kUnitRows; i += G * kStreamThreads) p.sync[64 + i] = 0;
+  }
   uint32_t before;                                // arrivals, seen before this CTA's: only the top bit matters
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(before) : "l"(p.sync) : "memory");
   Ring r{smem_u32(ring) + warp * STAGES * kSlotBytes, 0, smem_u32(rest) + warp * STAGES * 256 * XC, lane};
@@ -443,8 +453,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
   if (lane == 0) {
     uint32_t n;
     asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], 1;" : "=r"(n) : "r"(smem_u32(&t.done)) : "memory");
-    if (n == kStreamWarps - 1)
-      asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(p.sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
+    if (n == kStreamWarps - 1 && !(p.hook && b == G - 1)) few_arrive(p.sync, b, G);
   }
 
   // ---- phase 2: down ----
@@ -520,13 +529,15 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
       uint32_t now;
       together = false;
 #pragma unroll 1
-      for (uint32_t i = 0; i < kFewPolls && !together; ++i) {
+      for (uint32_t i = 0; i < p.polls && !together; ++i) {
         asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(p.sync) : "memory");
         together = (now ^ before) >> 31;
       }
       if (!together) atomicMax(p.status, (int)PW_ERR_TIMEOUT);
     }
     if (!__syncthreads_and(together)) {
+      // every CTA arrives once, also one that has given up: the next call finds the counter as it should be
+      if (p.hook && b == G - 1 && tid == 0) few_arrive(p.sync, b, G);
       cp_wait<0>();
       return;
     }
@@ -614,7 +625,6 @@ __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __gr
             for (int q = 0; q < kFewParts; ++q) v = __fadd_rn(v, part[q]);
             store1(p.out, (int64_t)tok * p.H + row0 + row, p.out_type, v);
           }
-          if (lane == 0 && member == 0) p.sync[64 + row0 / kUnitRows] = 0;
         }
       }
       few_team_sync(w);                    // the sums are written again
@@ -744,6 +754,8 @@ static pw_status moe_forward_few(pw_ctx* ctx, int layer, const void* hidden, con
   a.h = b + w.few_h;
   a.parts = reinterpret_cast<float*>(b + w.y);
   a.sync = reinterpret_cast<int32_t*>(b + w.few_sync);
+  a.polls = ctx->wait_polls ? kFewPollsTest : kFewPolls;
+  a.hook = ctx->test_hook & 1u;
   a.status = reinterpret_cast<int32_t*>(b + w.status);
   a.seen = ctx->obs_acc ? reinterpret_cast<int32_t*>(b + w.few_seen) : nullptr;
   // Parts of the down blocks' columns: as few as give every SM work, in rounds that are nearly full.  By an estimate in us:

@@ -242,3 +242,31 @@ def test_extreme_groups_of_many_tokens(ctx, fmt):
     odd = many_tokens(ctx, y, [page], [N], BF16)
     rest = [t for t in range(T) if t not in (50, 60)]
     assert torch.equal(odd[rest], out[rest]) and not torch.isfinite(odd[[50, 60]]).any()
+
+
+# ---- a wait that runs out --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("F", [768, 3584])
+def test_a_meeting_that_runs_out_is_reported_and_leaves_nothing_behind(F):
+    """The last CTA comes to the meeting of all CTAs when its own wait there, of some milliseconds, has run out; with the down
+    blocks' columns in parts (short blocks) and in one piece.  Calls queued behind are whole, read or unread status."""
+    layer = Layer(20, 2, 256, F, MIX, seed=8, k=4)
+    c = layer.ctx
+    x, l = layer.tokens(5), layer.logits(5)
+    good = c.pw_moe_forward_few(0, x, l, 4)
+    layer.check(good, x, plain.routing(f64(l), 4))
+    for _ in range(2):
+        c.pw_debug_set_wait(polls=200, hook=1)
+        c.pw_moe_forward_few(0, x, l, 4)
+        torch.cuda.synchronize()
+        assert c.pw_last_device_status() == 8 and c.pw_last_device_status() == 0
+        c.pw_moe_forward_few(0, x, l, 4)
+        c.pw_moe_forward_few(0, x, l, 4)
+        c.pw_debug_set_wait(polls=0, hook=0)
+        behind = [c.pw_moe_forward_few(0, x, l, 4) for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, good) for y in behind)
+        assert c.pw_last_device_status() == 8 and c.pw_last_device_status() == 0
+        assert torch.equal(c.pw_moe_forward_few(0, x, l, 4), good)
+    assert c.pw_last_device_status() == 0
+    c.close()
