@@ -456,7 +456,7 @@ pw_status pw_route_tokens(pw_ctx* ctx, const pw_routing* rule, const void* route
  * with a 16-bit output of more tokens than that pays for (more than eight; by an estimate of the times) go through the
  * tensor-core kernel of the layer calls instead, in three launches and another order of sums; with less, or none, the call
  * does without.  (There code * scale is taken about the middle of the codes, in two fp16 numbers that hold all of it for
- * scales up to 131008 / 2^bits, which every block of fp16 weights has; beyond, results may be infinite.)
+ * every block of fp16 weights, and in any other for scales up to 131008 / 2^bits; beyond twice that results are infinite.)
  * pw_page_linear_workspace is 0 for invalid arguments too.
  * Needs a context of the current device, but neither its page table nor its workspace: calls on different streams may run
  * at the same time, each with a workspace of its own.

@@ -270,3 +270,48 @@ def test_a_meeting_that_runs_out_is_reported_and_leaves_nothing_behind(F):
         assert torch.equal(c.pw_moe_forward_few(0, x, l, 4), good)
     assert c.pw_last_device_status() == 0
     c.close()
+
+
+# ---- pages that no block of fp16 weights makes -----------------------------------------------------
+
+@pytest.mark.parametrize("bits", [8, 4, 3, 2])
+def test_scales_of_any_sign_and_size(ctx, bits):
+    """Imported pages: scales that are zero, negative, subnormal, and as large as the many-token way takes them."""
+    rows, cols, T = 1280, 1024, 1000
+    g = gen(bits)
+    raw = B.Page(rows, cols, bits, ctx.device, B.PW_LAYOUT_CANONICAL)
+    raw.codes.copy_(torch.randint(0, 256, raw.codes.shape, generator=g, device="cuda", dtype=torch.int32).to(torch.uint8))
+    s = normal(g, rows, cols // 128)
+    s[:, 0] = 0
+    s[:, 1] *= 2.0 ** -20
+    s[:, 2] = 131008.0 / 2 ** bits * torch.sign(s[:, 2])
+    s[:, 3] = 2.0 ** -24 * torch.round(8 * s[:, 3])
+    raw.scales.copy_(s.half().reshape(raw.scales.shape))
+    raw.zps.copy_((normal(g, rows, cols // 128) * 3).half().reshape(raw.zps.shape))
+    page = ctx.pw_import_page(raw)
+    x = operand(g, T, cols)
+    x[:500, 256:384] = 0                           # without the largest group, so that the others show
+    block = plain.stored(ctx, page)
+    check(many_tokens(ctx, x, [page], [rows], BF16), *centred_product(f64(x), block, bits), BF16)
+    check(ctx.pw_page_linear(x[:7], [page], out_dtype=F32), *plain.product(f64(x[:7]), block), F32)
+    check(ctx.pw_page_linear(x[600:607], [page], out_dtype=F32), *plain.product(f64(x[600:607]), block), F32)
+
+
+@pytest.mark.parametrize("T,dtype", [(3, F32), (13, BF16)])
+def test_an_h_beyond_fp16_makes_its_token_infinite_and_no_other(mixed, T, dtype):
+    """As in the call for batches, whose operand is fp16 too; the largest that fits gives what it should."""
+    x, l = mixed.tokens(T), mixed.logits(T)
+    want = mixed.ctx.pw_moe_forward_few(0, x, l, 3, out_dtype=dtype)
+    pairs = all_pairs(mixed, l, 3)
+    g, u = (plain.product(f64(x[1:2]), mixed.blocks[mixed.E][k])[0] for k in (0, 1))   # of a shared expert: every token has it
+    y = x.clone()
+    for scale, fits in ((64.0, True), (20000.0, False)):
+        y[1] = (x[1].float() * scale).half()
+        h = np.abs(np.concatenate([(a * scale) / (1 + np.exp(np.clip(-a * scale, -700, 700))) * b * scale for a, b in zip(g, u)]))
+        assert (h.max() < 60000) == fits
+        out = mixed.ctx.pw_moe_forward_few(0, y, l, 3, out_dtype=dtype)
+        rest = [t for t in range(T) if t != 1]
+        assert torch.equal(out[rest], want[rest])
+        if not fits:
+            assert not torch.isfinite(out[1]).any() and not torch.isfinite(mixed.ctx.pw_moe_forward(0, y, l, 3)[1]).any()
+    assert pairs and mixed.ctx.pw_last_device_status() == 0
