@@ -299,8 +299,10 @@ static PageLinearPlan cut_page_linear(PageLinearArgs& a, int width, int split, i
   int64_t steps = 0;                              // of a warp, for a slice of the average page
   for (int i = 0; i < a.pages; ++i) steps += (int64_t)a.split_groups << step_shift(a.page[i].fmt);
   steps = (steps + ((int64_t)a.pages << ts) - 1) / ((int64_t)a.pages << ts);
-  // a step of each of the 16 warps takes the SM about 1100 cycles, and one of few warps 400; then the hand-over of a unit,
-  // the exchange of a cluster, and the operands' way into shared memory
+  // Constants fitted to measured cuts, most of them of 4-bit blocks (not the time of a step, which is 1530 cycles there with
+  // every warp at work): 1100 cycles of the SM for a step of each of the 16 warps, 400 for one of few warps; then the
+  // hand-over of a unit, the exchange of a cluster, and the operands' way into shared memory.  Formats differ by what their
+  // steps hold, which is all that the estimate knows of them: times at 16 bits come out 30 to 70 % too long.
   const double busy = (double)a.slices / (double)(sharing * teams);
   double c = (double)rounds * ((double)steps * (busy >= 1. ? 1100. : 1100. * busy > 400. ? 1100. * busy : 400.) + 1500.);
   if (split > 1) c += 4000. + (double)((rounds + a.batch - 1) / a.batch) * 3000.;
@@ -365,8 +367,10 @@ static int64_t set_pages(PageLinearArgs& a, int T, int K, const pw_page* pages, 
 }
 // Whether a call goes through the tensor-core kernel of the layer calls (three launches; outputs of 16 bits), and what of its
 // cut does not depend on the device.  By estimates of both times in us: this kernel's from its cut; the other's as a sum of
-// terms, 11 for the launches, 0.2 per million weights (decoding), 2.3 per billion products, 4 per million outputs (parts of
-// sums, written and read), fitted to thirty shapes.  Of those it takes the faster kernel, or one within 5 %.  Measured, here /
+// terms, 11 for the launches, for decoding 0.2 per million weights or 0.09 per group of columns, 2.3 per billion products, 4
+// per million outputs (parts of sums, written and read).  Fitted to thirty shapes, where it takes the faster kernel or one
+// within 5 %; of forty drawn afterwards, of all formats and mixed ones, the kernel it takes is 1 % slower than the faster one
+// in the mean, 28 % at worst (13986 x 468 at 4 bits, 91 tokens 19.7 / 15.4).  Measured, here /
 // there: 14336 x 4096 at 4 bits, 16 tokens 16.4 / 26.5, 32 tokens 27.0 / 27.6, 64 tokens 46.9 / 32.0, 256 tokens 188 / 72;
 // 4096 x 4096 at 4 bits, 64 tokens 17.6 / 17.3; 4096 x 14336 at 8 bits, 64 tokens 61 / 32; 28672 x 8192 at 4 bits, 16 tokens
 // 51 / 73; 1260 x 1000 in planes of 4 bits, 300 tokens 15.4 / 14.6, 600 tokens 37 / 17.7; 40 x 128 at 4 bits, 1200 tokens
@@ -381,9 +385,11 @@ static bool many_tokens(DenseCall* d, const PageLinearArgs& call, const pw_page*
   // (about as many clusters as run at the same time: the workspace's size must not depend on the current device)
   int clusters[kSplits];
   for (int i = 0; i < kSplits; ++i) clusters[i] = sms * 7 / (8 * (2 << i));
+  const double decode = 0.2 * m > 0.09 * call.groups ? 0.2 * m : 0.09 * call.groups;
+  const double there = 11. + decode + 2.3e-3 * m * call.T + 4e-6 * call.T * width;
   PageLinearArgs a = call;
   const PageLinearPlan here = plan_page_linear(a, sms, clusters);
-  if (here.stages && 2.5 + here.cycles / 1680. <= 11. + 0.2 * m + 2.3e-3 * m * call.T + 4e-6 * call.T * width) return false;
+  if (here.stages && 2.5 + here.cycles / 1680. <= there) return false;
   *d = DenseCall{};
   d->T = call.T;
   d->cols = (int)pages[0].cols;
