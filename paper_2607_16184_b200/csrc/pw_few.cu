@@ -1,9 +1,9 @@
 // Dense products on weight pages for few tokens (pw_page_linear).  The inner loop is in pw_stream.cuh.
 //
-// Bound: the pages' bytes for wide blocks (32003 x 4096 at 4 bits, one token: 15.3 us, 4.6 TB/s while the copy rate is 6.6),
-// the launch and one round trip to memory for small ones (4096 x 4096, one token: 4.5 us, of which an empty launch takes
+// Bound: the pages' bytes for wide blocks (32003 x 4096 at 4 bits, one token: 16 us, 4.4 TB/s while the copy rate is 6.6),
+// the launch and one round trip to memory for small ones (4096 x 4096, one token: 4.8 us, of which an empty launch takes
 // 1.9 and the bytes 1.4), and with eight tokens of long rows the operand, which does not fit one SM (4096 x 14336, 3 of 4
-// planes: 14.8 us; clusters of four CTAs share the columns, their launch alone takes 3 us more).  How a product is cut is
+// planes: 15.7 us; clusters of four CTAs share the columns, their launch alone takes 3 us more).  How a product is cut is
 // decided by an estimate (cut_page_linear); of the cuts there are (24 to 48) it took the fastest, or one within 2 %, for all
 // of ten shapes.
 #include "pw_scaled.cuh"

@@ -1,7 +1,7 @@
 // The whole layer for few tokens in one kernel (pw_moe_forward_few, pw_moe_forward_few_routed).
 //
 // The layer call for batches takes five or six launches, and its kernels work on tiles of 128 weight rows; one token of a
-// layer with 60 + 4 experts takes them 40 us, where the pages' bytes need 16.  Here (28 us) one CTA per SM
+// layer with 60 + 4 experts takes them 40 us, where the pages' bytes need 16.  Here (28 to 31 us) one CTA per SM
 //   - routes the tokens (every CTA does, it is cheaper than to wait for one that does) and lists the experts that have any;
 //     meanwhile it brings the tokens into shared memory and asks the L2 cache for the shared experts,
 //   - phase 1: units of 32 rows of an expert's gate and up blocks -> 32 values h = silu(gate) * up of its tokens,
@@ -286,6 +286,7 @@ __device__ __forceinline__ void few_arrive(int32_t* sync, int b, int G) {
   asm volatile("red.add.release.gpu.global.u32 [%0], %1;" ::"l"(sync), "r"(b == 0 ? 0x80000000u - (uint32_t)(G - 1) : 1u) : "memory");
 }
 
+// (16 warps: 128 registers a thread, all of which it takes; 4 bytes are spilled, once)
 template <class TAB, int XC, int STAGES>
 __global__ void __launch_bounds__(kStreamThreads, 1) few_layer_kernel(const __grid_constant__ FewArgs p) {
   extern __shared__ __align__(128) char smem[];
