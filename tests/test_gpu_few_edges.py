@@ -200,7 +200,9 @@ def many_tokens(ctx, x, pages, sizes, dtype):
 
 @pytest.mark.parametrize("T,K,sizes,formats", [(64, 4096, [6000], ["2"]), (33, 8192, [2500, 2000], ["4", "4"]), (130, 2050, [3129, 64], ["3", "4"]),
                                                (70, 14336, [1128], ["8"]), (600, 1000, [1260], ["p4"]), (12000, 640, [100], ["p2"]),
-                                               (2000, 900, [700, 33], ["p3", "16"]), (64, 4096, [6000], ["4"])])
+                                               (2000, 900, [700, 33], ["p3", "16"]), (64, 4096, [6000], ["4"]),
+                                               (64, 4096, [6000], ["p4"]), (48, 4200, [9700], ["4"]), (48, 4200, [9700], ["p4"]),
+                                               (20, 8192, [6000], ["8"]), (17, 4200, [9700], ["16"]), (48, 14336, [2300], ["p3"])])
 @pytest.mark.parametrize("dtype,share", [(F16, 0.02), (BF16, 0.005)])
 def test_many_tokens_round_nothing_but_the_output(ctx, T, K, sizes, formats, dtype, share):
     """Weights are not rounded to fp16: see test_few_outputs_are_a_neighbour_of_the_rounded_definition for the share."""
